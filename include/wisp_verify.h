@@ -83,7 +83,8 @@ typedef enum {
   WISP_DEV_NO_BLOCKS = 7     /* (wisp_kv.h) the free page pool could not serve the request */
 } wisp_device_code;
 
-typedef enum { WISP_F32 = 0, WISP_BF16 = 1 } wisp_dtype;
+/* WISP_E4M3 is a type of KV caches only (wisp_kv8.h); the entry points of this header refuse it. */
+typedef enum { WISP_F32 = 0, WISP_BF16 = 1, WISP_E4M3 = 2 } wisp_dtype;
 
 /*
  * Attention of the verification forward (Sec. 4.4-4.5).

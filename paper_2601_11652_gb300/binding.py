@@ -16,7 +16,7 @@ import torch
 from . import build as _build
 
 WISP_OK, WISP_ERR_INVALID_ARG, WISP_ERR_UNSUPPORTED, WISP_ERR_CUDA, WISP_ERR_WORKSPACE = range(5)
-WISP_F32, WISP_BF16 = 0, 1
+WISP_F32, WISP_BF16, WISP_E4M3 = 0, 1, 2
 DEVICE_CODES = {0: "ok", 1: "bad_length", 2: "bad_block", 3: "bad_token", 4: "bad_prob", 5: "unsupported",
                 6: "timeout"}
 
@@ -46,6 +46,12 @@ class wisp_kv_args(ctypes.Structure):
                 ("accepted_len", _P)]
 
 
+class wisp_kv_rope_args(ctypes.Structure):
+    _fields_ = [("kv", wisp_kv_args), ("cache_dtype", ctypes.c_int), ("k_scale", _P), ("v_scale", _P), ("rope", _P),
+                ("rope_positions", _I32), ("rot_dim", _I32), ("interleaved", _I32), ("Hq", _I32), ("q", _P), ("q_out", _P),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
 class WispError(RuntimeError):
     def __init__(self, fn: str, code: int, text: str):
         super().__init__(f"{fn}: {text} (status {code})")
@@ -57,7 +63,7 @@ _lib = None
 EXPORTED = ["wisp_verify_workspace_size", "wisp_verify_attention", "wisp_verify_accept", "wisp_verify_step",
             "wisp_verify_get_device_status", "wisp_verify_status_string", "wisp_verify_device_code_string",
             "wisp_verify_accept_noalloc", "wisp_verify_accept_greedy", "wisp_kv_workspace_size",
-            "wisp_kv_reserve_append", "wisp_kv_commit"]
+            "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope"]
 
 
 def lib_path() -> str:
@@ -99,6 +105,11 @@ def load(path: str | None = None):
     for fn in ("wisp_kv_reserve_append", "wisp_kv_commit"):
         getattr(lib, fn).argtypes = [KP, _P, ctypes.c_size_t, _P]
         getattr(lib, fn).restype = ctypes.c_int
+    RP = ctypes.POINTER(wisp_kv_rope_args)
+    lib.wisp_kv_rope_workspace_size.argtypes = [RP]
+    lib.wisp_kv_rope_workspace_size.restype = ctypes.c_size_t
+    lib.wisp_kv_reserve_append_rope.argtypes = [RP, _P, ctypes.c_size_t, _P]
+    lib.wisp_kv_reserve_append_rope.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -124,6 +135,19 @@ def _stream(stream) -> int | None:
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+def _rows_ptr(t) -> tuple[int, int]:
+    """Pointer and row stride (elements) of [rows, heads, D] rows that may lie apart, as parts of one projection output."""
+    if not t.is_cuda:
+        raise ValueError("device tensors only: the verification step runs on the GPU")
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError("the heads of a row must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _cache_code(t: torch.Tensor) -> int:
+    return WISP_E4M3 if t.dtype in (torch.float8_e4m3fn, torch.uint8) else _dtype_code(t)
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -252,3 +276,58 @@ def wisp_kv_reserve_append(kv: wisp_kv_args, workspace: torch.Tensor, stream=Non
 
 def wisp_kv_commit(kv: wisp_kv_args, workspace: torch.Tensor, stream=None) -> None:
     _check("wisp_kv_commit", load().wisp_kv_commit(ctypes.byref(kv), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+# ---- rotation on the way into the cache, 8-bit caches (include/wisp_kv8.h) ------------------------
+def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, free_count, k_cache, v_cache, k_new, v_new,
+                      rope=None, q=None, q_out=None, k_scale=None, v_scale=None, interleaved=False, request_ids=None,
+                      total_q_rows=None) -> wisp_kv_rope_args:
+    """Fill wisp_kv_rope_args from device tensors: k_new / v_new [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart),
+    caches of their type or e4m3 (torch.float8_e4m3fn or uint8) with k_scale / v_scale [num_blocks, Hkv], rope
+    [positions, rot_dim] of cosines and sines (None: no rotation)."""
+    (kp, ks), (vp, vs) = _rows_ptr(k_new), _rows_ptr(v_new)
+    if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.shape[1::2] != k_new.shape[1:]:
+        raise ValueError("k_cache and v_cache must be [num_blocks, Hkv, 16, D] of one type")
+    if k_cache.shape[0] < free_blocks.shape[0]:
+        raise ValueError("free_blocks must not be longer than the pool")
+    a = wisp_kv_rope_args()
+    a.kv = make_kv_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, free_blocks=free_blocks,
+                        free_count=free_count, request_ids=request_ids,
+                        total_q_rows=k_new.shape[0] if total_q_rows is None else total_q_rows)
+    a.kv.Hkv, a.kv.D, a.kv.kv_dtype, a.cache_dtype = k_new.shape[1], k_new.shape[2], _dtype_code(k_new), _cache_code(k_cache)
+    a.kv.block_size = k_cache.shape[2]
+    a.kv.k_cache, a.kv.v_cache, a.kv.k_new, a.kv.v_new = _ptr(k_cache), _ptr(v_cache), kp, vp
+    a.k_stride, a.v_stride = ks, vs
+    if a.cache_dtype == WISP_E4M3:
+        _check_scales(k_cache, k_scale, v_scale)
+        a.k_scale, a.v_scale = _ptr(k_scale), _ptr(v_scale)
+    if rope is not None:
+        if rope.dtype != torch.float32:
+            raise ValueError("the rotation's table is float32")
+        a.rope, a.rope_positions, a.rot_dim = _ptr(rope), rope.shape[0], rope.shape[1]
+    a.interleaved = int(interleaved)
+    if q is not None:
+        if q.dtype != k_new.dtype or q_out.dtype != q.dtype or q_out.shape != q.shape or q.shape[2] != k_new.shape[2]:
+            raise ValueError("q and q_out must have the type and head dim of k_new")
+        a.Hq = q.shape[1]
+        a.q, a.q_stride = _rows_ptr(q)
+        a.q_out = _ptr(q_out)
+    return a
+
+
+def _check_scales(cache, *scales):
+    for s in scales:
+        if s is None or s.dtype != torch.float32 or tuple(s.shape) != tuple(cache.shape[:2]):
+            raise ValueError("an 8-bit cache has float32 scales [num_blocks, Hkv]")
+
+
+def wisp_kv_rope_workspace_size(a: wisp_kv_rope_args) -> int:
+    n = load().wisp_kv_rope_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise WispError("wisp_kv_rope_workspace_size", WISP_ERR_INVALID_ARG, "invalid arguments")
+    return int(n)
+
+
+def wisp_kv_reserve_append_rope(a: wisp_kv_rope_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_kv_reserve_append_rope", load().wisp_kv_reserve_append_rope(
+        ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))

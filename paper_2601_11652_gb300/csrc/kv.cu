@@ -9,32 +9,17 @@
 //   kv_append_kernel: one warp per (new row, KV head) copies the row into its page slot;
 //   kv_commit_kernel (one CTA): c <- c + 1 + L (Eq. 2's L), and the pages past the new length
 //     among those the step could use go back on the free stack in table order.
-#include "common.cuh"
+#include "kv.cuh"
 
 #include <cstring>
-
-#include "wisp_kv.h"
 
 namespace wisp {
 
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kPage = 16;
+constexpr int kPage = kKvPage;
 constexpr int kReserveCtas = 8;  // one cluster (the portable maximum): its barrier orders counting before serving
-
-struct KvParams {
-  int B, Hkv, D, max_blocks, num_blocks, total_rows, esize;
-  const int64_t *request_ids;
-  const int32_t *draft_lens;
-  int32_t *context_lens, *block_tables, *free_blocks, *free_count;
-  char *k_cache, *v_cache;
-  const char *k_new, *v_new;
-  const int32_t *accepted_len;
-  DeviceStatus *status;
-  int32_t *row_req, *row_pos;  // [total_rows]: request of a new row (-1: skipped) and its position
-  int32_t *need, *first;       // [B]: a request's missing pages (-code: refused), its first missing table entry
-};
 
 __device__ __forceinline__ int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 
@@ -99,7 +84,7 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kReserveCtas, 1, 1)
     p.status->pad = 0;
     p.status->request_id = 0;
   }
-  const int64_t cap = (int64_t)p.max_blocks * kPage;
+  const int64_t cap = p.max_tokens;
 
   // count: request r by warp r mod NWARPS
   for (int r = gw; r < p.B; r += NWARPS) {
@@ -269,9 +254,7 @@ __global__ void __launch_bounds__(kThreads) kv_commit_kernel(const KvParams p) {
   if (threadIdx.x == 0) *p.free_count = (int32_t)min64(F + carry, p.num_blocks);
 }
 
-struct KvLayout {
-  size_t status = 0, row_req = 0, row_pos = 0, need = 0, first = 0, total = 0;
-};
+}  // namespace
 
 KvLayout kv_layout(const wisp_kv_args *a) {
   KvLayout L;
@@ -289,8 +272,6 @@ KvLayout kv_layout(const wisp_kv_args *a) {
   L.total = off;
   return L;
 }
-
-bool al16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 wisp_status kv_check(const wisp_kv_args *a, bool need_new, bool need_accepted) {
   if (!a) return WISP_ERR_INVALID_ARG;
@@ -319,6 +300,7 @@ KvParams kv_params(const wisp_kv_args *a, void *ws, const KvLayout &L) {
   p.max_blocks = a->max_blocks_per_seq;
   p.num_blocks = a->num_blocks;
   p.total_rows = a->total_q_rows;
+  p.max_tokens = (int64_t)a->max_blocks_per_seq * kPage;
   p.esize = a->kv_dtype == WISP_BF16 ? 2 : 4;
   p.request_ids = a->request_ids;
   p.draft_lens = a->draft_lens;
@@ -343,7 +325,10 @@ wisp_status kv_ws_ok(void *ws, size_t bytes, const KvLayout &L) {
   return !ws || ((uintptr_t)ws & 255) != 0 || bytes < L.total ? WISP_ERR_WORKSPACE : WISP_OK;
 }
 
-}  // namespace
+cudaError_t kv_reserve_launch(const KvParams &p, cudaStream_t s) {
+  kv_reserve_kernel<<<kReserveCtas, kThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
 
 }  // namespace wisp
 
@@ -365,8 +350,7 @@ wisp_status wisp_kv_reserve_append(const wisp_kv_args *kv, void *ws, size_t ws_b
   const KvParams p = kv_params(kv, ws, L);
   if (kv->B == 0)
     return cudaMemsetAsync(p.status, 0, sizeof(DeviceStatus), s) == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
-  kv_reserve_kernel<<<kReserveCtas, kThreads, 0, s>>>(p);
-  if (cudaGetLastError() != cudaSuccess) return WISP_ERR_CUDA;
+  if (kv_reserve_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   const int64_t warps = (int64_t)kv->total_q_rows * kv->Hkv;
   const int64_t blocks = (warps + 7) / 8;
   cudaLaunchConfig_t cfg;

@@ -1,0 +1,84 @@
+"""wisp_kv_reserve_append_rope without a GPU: the header compiles as C, its symbols are exported, and arguments that the
+host can judge are refused before the device is touched."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "wisp_kv8.h")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2601_11652_gb300 import binding, build
+    build.build()
+    return binding.load()
+
+
+def test_header_and_exports(lib, tmp_path):
+    from paper_2601_11652_gb300 import binding
+    src = tmp_path / "t.c"
+    src.write_text('#include "wisp_kv8.h"\nint main(void){ return sizeof(wisp_kv_rope_args) > 0 ? 0 : 1; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-c", str(src),
+                    "-o", str(tmp_path / "t.o")], check=True)
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(wisp_(?:verify|kv)_\w+)\s*\(", text))
+    assert {"wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope"} <= names
+    for n in names:
+        assert hasattr(lib, n) and n in binding.EXPORTED, n
+
+
+def _args(kv=None, **kw):
+    from paper_2601_11652_gb300 import binding as wb
+    a = wb.wisp_kv_rope_args()
+    base_kv = dict(B=2, Hkv=2, D=128, block_size=16, max_blocks_per_seq=4, num_blocks=8, total_q_rows=4, draft_lens=0x1000,
+                   context_lens=0x2000, block_tables=0x3000, free_blocks=0x4000, free_count=0x5000, kv_dtype=1,
+                   k_cache=0x10000, v_cache=0x20000, k_new=0x30000, v_new=0x40000)
+    base = dict(cache_dtype=2, k_scale=0x50000, v_scale=0x60000, rope=0x70000, rope_positions=64, rot_dim=128, interleaved=0,
+                Hq=8, q=0x80000, q_out=0x90000, q_stride=0, k_stride=0, v_stride=0)
+    for k, v in {**base_kv, **(kv or {})}.items():
+        setattr(a.kv, k, v)
+    for k, v in {**base, **kw}.items():
+        setattr(a, k, v)
+    return a
+
+
+INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 4
+BAD = [(dict(kv=dict(B=-1)), INVALID), (dict(kv=dict(D=96)), UNSUPPORTED), (dict(kv=dict(block_size=32)), UNSUPPORTED),
+       (dict(kv=dict(kv_dtype=2)), INVALID), (dict(kv=dict(k_new=None)), INVALID), (dict(kv=dict(v_cache=0x20008)), INVALID),
+       (dict(kv=dict(total_q_rows=1)), INVALID), (dict(cache_dtype=0), INVALID), (dict(cache_dtype=3), INVALID),
+       (dict(k_scale=None), INVALID), (dict(rope=None), INVALID), (dict(rope=0x70004), INVALID),
+       (dict(rope_positions=0), INVALID), (dict(rot_dim=24), UNSUPPORTED), (dict(rot_dim=144), INVALID),
+       (dict(rot_dim=-16), INVALID), (dict(Hq=-1), INVALID), (dict(q=None), INVALID), (dict(q_out=0x90002), INVALID),
+       (dict(q_stride=8 * 128 - 8), INVALID), (dict(k_stride=2 * 128 + 4), INVALID), (dict(v_stride=-256), INVALID)]
+
+
+@pytest.mark.parametrize("kw,code", BAD, ids=[str(b[0]) for b in BAD])
+def test_bad_arguments_are_refused(lib, kw, code):
+    a = _args(**kw)
+    assert lib.wisp_kv_reserve_append_rope(ctypes.byref(a), ctypes.c_void_p(0x100000), 1 << 30, None) == code
+
+
+def test_null_and_workspace(lib):
+    assert lib.wisp_kv_reserve_append_rope(None, ctypes.c_void_p(0x100000), 1 << 30, None) == INVALID
+    assert lib.wisp_kv_rope_workspace_size(None) == 0
+    a = _args()
+    n = lib.wisp_kv_rope_workspace_size(ctypes.byref(a))
+    assert n > 0
+    for ws, size in ((None, 1 << 30), (0x100010, 1 << 30), (0x100000, n - 1)):
+        assert lib.wisp_kv_reserve_append_rope(ctypes.byref(a), ctypes.c_void_p(ws), size, None) == WORKSPACE
+
+
+def test_binding_refuses_what_it_can_see():
+    import torch
+
+    from paper_2601_11652_gb300 import binding as wb
+    with pytest.raises(ValueError):
+        wb._rows_ptr(torch.zeros(2, 2, 64))
+    with pytest.raises(ValueError):
+        wb._check_scales(torch.zeros(4, 2, 16, 64, dtype=torch.uint8), torch.zeros(4, 2), None)
+    with pytest.raises(ValueError):
+        wb._check_scales(torch.zeros(4, 2, 16, 64, dtype=torch.uint8), torch.zeros(4, 3))
