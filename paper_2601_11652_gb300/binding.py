@@ -52,6 +52,11 @@ class wisp_kv_rope_args(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
+class wisp_logprobs_args(ctypes.Structure):
+    _fields_ = [("rows", _I32), ("V", _I32), ("row_stride", ctypes.c_int64), ("logits_dtype", ctypes.c_int), ("logits", _P),
+                ("tokens", _P), ("top_n", _I32), ("logprob", _P), ("entropy", _P), ("top_tokens", _P), ("top_logprobs", _P)]
+
+
 class WispError(RuntimeError):
     def __init__(self, fn: str, code: int, text: str):
         super().__init__(f"{fn}: {text} (status {code})")
@@ -63,7 +68,8 @@ _lib = None
 EXPORTED = ["wisp_verify_workspace_size", "wisp_verify_attention", "wisp_verify_accept", "wisp_verify_step",
             "wisp_verify_get_device_status", "wisp_verify_status_string", "wisp_verify_device_code_string",
             "wisp_verify_accept_noalloc", "wisp_verify_accept_greedy", "wisp_kv_workspace_size",
-            "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope"]
+            "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope",
+            "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
 
 
 def lib_path() -> str:
@@ -110,6 +116,13 @@ def load(path: str | None = None):
     lib.wisp_kv_rope_workspace_size.restype = ctypes.c_size_t
     lib.wisp_kv_reserve_append_rope.argtypes = [RP, _P, ctypes.c_size_t, _P]
     lib.wisp_kv_reserve_append_rope.restype = ctypes.c_int
+    LP = ctypes.POINTER(wisp_logprobs_args)
+    lib.wisp_verify_logprobs_workspace_size.argtypes = [LP]
+    lib.wisp_verify_logprobs_workspace_size.restype = ctypes.c_size_t
+    lib.wisp_verify_logprobs.argtypes = [LP, _P, ctypes.c_size_t, _P]
+    lib.wisp_verify_logprobs.restype = ctypes.c_int
+    lib.wisp_verify_committed_tokens.argtypes = [CP, _P, _P]
+    lib.wisp_verify_committed_tokens.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -331,3 +344,53 @@ def wisp_kv_rope_workspace_size(a: wisp_kv_rope_args) -> int:
 def wisp_kv_reserve_append_rope(a: wisp_kv_rope_args, workspace: torch.Tensor, stream=None) -> None:
     _check("wisp_kv_reserve_append_rope", load().wisp_kv_reserve_append_rope(
         ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+# ---- log probabilities (include/wisp_logprobs.h) ----------------------------------------------------
+def make_logprobs_args(*, logits, tokens, logprob, entropy=None, top_tokens=None, top_logprobs=None) -> wisp_logprobs_args:
+    """Fill wisp_logprobs_args from device tensors: logits [rows, V] (rows may lie apart), tokens [rows] int32 (negative:
+    the row is skipped), logprob / entropy [rows] float32, top_tokens int32 and top_logprobs float32 [rows, top_n]."""
+    if not logits.is_cuda:
+        raise ValueError("device tensors only: the verification step runs on the GPU")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows, V], each row contiguous")
+    rows, V = logits.shape
+    if (top_tokens is None) != (top_logprobs is None):
+        raise ValueError("top_tokens and top_logprobs go together")
+    if tokens.dtype != torch.int32 or tokens.numel() != rows:
+        raise ValueError("tokens must be [rows] int32")
+    for t in (logprob, entropy):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != rows):
+            raise ValueError("logprob and entropy must be [rows] float32")
+    a = wisp_logprobs_args()
+    a.rows, a.V = rows, V
+    a.row_stride = logits.stride(0) if rows > 1 else 0
+    a.logits_dtype = _dtype_code(logits)
+    a.logits, a.tokens = logits.data_ptr(), _ptr(tokens)
+    a.logprob, a.entropy = _ptr(logprob), _ptr(entropy)
+    if top_tokens is not None:
+        a.top_n = top_tokens.shape[1]
+        if top_tokens.dtype != torch.int32 or top_logprobs.dtype != torch.float32 or top_tokens.shape[0] != rows or \
+                top_logprobs.shape != top_tokens.shape:
+            raise ValueError("top_tokens must be [rows, top_n] int32, top_logprobs the same in float32")
+        a.top_tokens, a.top_logprobs = _ptr(top_tokens), _ptr(top_logprobs)
+    return a
+
+
+def wisp_verify_logprobs_workspace_size(a: wisp_logprobs_args) -> int:
+    n = load().wisp_verify_logprobs_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise WispError("wisp_verify_logprobs_workspace_size", WISP_ERR_INVALID_ARG, "invalid arguments")
+    return int(n)
+
+
+def wisp_verify_logprobs(a: wisp_logprobs_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_verify_logprobs", load().wisp_verify_logprobs(
+        ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def wisp_verify_committed_tokens(acc: wisp_accept_args, row_tokens: torch.Tensor, stream=None) -> None:
+    if row_tokens.dtype != torch.int32 or row_tokens.numel() < acc.total_q_rows:
+        raise ValueError("row_tokens must be [total_q_rows] int32")
+    _check("wisp_verify_committed_tokens", load().wisp_verify_committed_tokens(
+        ctypes.byref(acc), _ptr(row_tokens), _stream(stream)))

@@ -304,7 +304,7 @@ wisp_status rope_check(const wisp_kv_rope_args *a, bool call) {
   if (a->Hq > 0 && (!a->q || !a->q_out || !al16(a->q) || !al16(a->q_out))) return WISP_ERR_INVALID_ARG;
   const int es = kv.kv_dtype == WISP_BF16 ? 2 : 4;
   auto bad = [&](int64_t stride, int64_t heads) {
-    return stride != 0 && (stride < heads * kv.D || stride > (INT64_MAX >> 34) || stride * es % 16 != 0);
+    return stride != 0 && (stride < heads * kv.D || stride > INT64_MAX / es / kv.total_q_rows || stride * es % 16 != 0);
   };
   if (bad(a->k_stride, kv.Hkv) || bad(a->v_stride, kv.Hkv) || (a->Hq > 0 && bad(a->q_stride, a->Hq))) return WISP_ERR_INVALID_ARG;
   return WISP_OK;
