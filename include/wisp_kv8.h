@@ -54,6 +54,26 @@ size_t wisp_kv_rope_workspace_size(const wisp_kv_rope_args *a);
  * the way, and the rotated queries in q_out.  wisp_kv_commit follows a step as for any other cache: it moves no K/V. */
 wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Attention over an 8-bit cache: wisp_attn_args with k_cache and v_cache e4m3 codes; qkv_dtype is the type of q and out.
+ * Workspace: wisp_verify_workspace_size(&a->attn, acc).
+ *   out[row, h] = sum_t softmax_t(<q[row, h], K[t]> / sqrt(D)) V[t], K[t] = k_code * k_scale, V[t] = v_code * v_scale
+ * Scales are finite and not negative (those that the append writes are; others may be any such fp32 value).  Codes past a
+ * request's tokens are not judged: pages may hold anything there.  Accumulation is fp32.  With bf16 queries, a query and a
+ * weight each enter the products with 8 significant bits or more (a bf16 query's own), small ones with at least 2^-20 of
+ * the row's largest in absolute terms.
+ */
+typedef struct {
+  wisp_attn_args attn;
+  const float *k_scale, *v_scale;  /* [num_blocks, Hkv] */
+} wisp_attn_kv8_args;
+
+wisp_status wisp_verify_attention_kv8(const wisp_attn_kv8_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/* wisp_verify_step over an 8-bit cache: attention and acceptance in one call. */
+wisp_status wisp_verify_step_kv8(const wisp_attn_kv8_args *a, const wisp_accept_args *acc, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

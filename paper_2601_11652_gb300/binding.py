@@ -52,6 +52,10 @@ class wisp_kv_rope_args(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
+class wisp_attn_kv8_args(ctypes.Structure):
+    _fields_ = [("attn", wisp_attn_args), ("k_scale", _P), ("v_scale", _P)]
+
+
 class wisp_logprobs_args(ctypes.Structure):
     _fields_ = [("rows", _I32), ("V", _I32), ("row_stride", ctypes.c_int64), ("logits_dtype", ctypes.c_int), ("logits", _P),
                 ("tokens", _P), ("top_n", _I32), ("logprob", _P), ("entropy", _P), ("top_tokens", _P), ("top_logprobs", _P)]
@@ -69,7 +73,7 @@ EXPORTED = ["wisp_verify_workspace_size", "wisp_verify_attention", "wisp_verify_
             "wisp_verify_get_device_status", "wisp_verify_status_string", "wisp_verify_device_code_string",
             "wisp_verify_accept_noalloc", "wisp_verify_accept_greedy", "wisp_kv_workspace_size",
             "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope",
-            "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
+            "wisp_verify_attention_kv8", "wisp_verify_step_kv8", "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
 
 
 def lib_path() -> str:
@@ -116,6 +120,11 @@ def load(path: str | None = None):
     lib.wisp_kv_rope_workspace_size.restype = ctypes.c_size_t
     lib.wisp_kv_reserve_append_rope.argtypes = [RP, _P, ctypes.c_size_t, _P]
     lib.wisp_kv_reserve_append_rope.restype = ctypes.c_int
+    A8 = ctypes.POINTER(wisp_attn_kv8_args)
+    lib.wisp_verify_attention_kv8.argtypes = [A8, _P, ctypes.c_size_t, _P]
+    lib.wisp_verify_attention_kv8.restype = ctypes.c_int
+    lib.wisp_verify_step_kv8.argtypes = [A8, CP, _P, ctypes.c_size_t, _P]
+    lib.wisp_verify_step_kv8.restype = ctypes.c_int
     LP = ctypes.POINTER(wisp_logprobs_args)
     lib.wisp_verify_logprobs_workspace_size.argtypes = [LP]
     lib.wisp_verify_logprobs_workspace_size.restype = ctypes.c_size_t
@@ -344,6 +353,29 @@ def wisp_kv_rope_workspace_size(a: wisp_kv_rope_args) -> int:
 def wisp_kv_reserve_append_rope(a: wisp_kv_rope_args, workspace: torch.Tensor, stream=None) -> None:
     _check("wisp_kv_reserve_append_rope", load().wisp_kv_reserve_append_rope(
         ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def make_attn_kv8_args(*, draft_lens, context_lens, block_tables, q, k_cache, v_cache, k_scale, v_scale, out, request_ids=None,
+                       num_blocks=None, total_q_rows=None) -> wisp_attn_kv8_args:
+    """make_attn_args over an e4m3 cache (torch.float8_e4m3fn or uint8) with scales [num_blocks, Hkv]."""
+    if _cache_code(k_cache) != WISP_E4M3 or v_cache.dtype != k_cache.dtype:
+        raise ValueError("k_cache and v_cache must be e4m3 (torch.float8_e4m3fn or uint8)")
+    _check_scales(k_cache, k_scale, v_scale)
+    a = wisp_attn_kv8_args()
+    a.attn = make_attn_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, q=q, k_cache=k_cache,
+                            v_cache=v_cache, out=out, request_ids=request_ids, num_blocks=num_blocks, total_q_rows=total_q_rows)
+    a.k_scale, a.v_scale = _ptr(k_scale), _ptr(v_scale)
+    return a
+
+
+def wisp_verify_attention_kv8(a: wisp_attn_kv8_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_verify_attention_kv8", load().wisp_verify_attention_kv8(
+        ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def wisp_verify_step_kv8(a: wisp_attn_kv8_args, acc: wisp_accept_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_verify_step_kv8", load().wisp_verify_step_kv8(
+        ctypes.byref(a), ctypes.byref(acc), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 # ---- log probabilities (include/wisp_logprobs.h) ----------------------------------------------------

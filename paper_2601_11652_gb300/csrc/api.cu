@@ -7,6 +7,7 @@
 
 #include "accept.cuh"
 #include "attn.cuh"
+#include "wisp_kv8.h"
 
 using namespace wisp;
 
@@ -72,6 +73,7 @@ wisp_status device_setup(int *dev_out, int *sms_out) {
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return WISP_ERR_CUDA;
     cudaError_t e = attn_f32_setup();
     if (e == cudaSuccess) e = attn_tc_setup();
+    if (e == cudaSuccess) e = attn_kv8_setup();
     if (e == cudaSuccess) e = accept_setup();
     if (e != cudaSuccess) return WISP_ERR_CUDA;
     d.sms = sms;
@@ -312,7 +314,12 @@ PlanParams plan_params(const wisp_attn_args *a, const wisp_accept_args *c, void 
   return pp;
 }
 
-wisp_status launch_attention(const wisp_attn_args *a, void *ws, const Layout &L, cudaStream_t s) {
+// The scales of an e4m3 cache (null pointers: the cache has the queries' type).
+struct KvScales {
+  const float *k = nullptr, *v = nullptr;
+};
+
+wisp_status launch_attention(const wisp_attn_args *a, KvScales sc, void *ws, const Layout &L, cudaStream_t s) {
   AttnParams ap;
   ap.B = a->B;
   ap.Hq = a->Hq;
@@ -325,6 +332,8 @@ wisp_status launch_attention(const wisp_attn_args *a, void *ws, const Layout &L,
   ap.q = a->q;
   ap.k_cache = a->k_cache;
   ap.v_cache = a->v_cache;
+  ap.k_scale = sc.k;
+  ap.v_scale = sc.v;
   ap.out = a->out;
   ap.status = at<DeviceStatus>(ws, L.status);
   ap.req_chunks = at<int32_t>(ws, L.req_chunks);
@@ -337,7 +346,8 @@ wisp_status launch_attention(const wisp_attn_args *a, void *ws, const Layout &L,
   // persistent kernels, one CTA per SM: the work counter lives in the plan header written by the planner
   // on this stream, and split items are merged inside the kernel by the last chunk to finish
   const int grid = (int)(L.max_items < L.target_items / kItemsPerSM ? L.max_items : L.target_items / kItemsPerSM);
-  const cudaError_t e = a->qkv_dtype == WISP_BF16 ? attn_tc_launch(ap, grid, s) : attn_f32_launch(ap, grid, s);
+  const bool bf = a->qkv_dtype == WISP_BF16;
+  const cudaError_t e = sc.k ? attn_kv8_launch(ap, !bf, grid, s) : bf ? attn_tc_launch(ap, grid, s) : attn_f32_launch(ap, grid, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 
@@ -421,6 +431,64 @@ wisp_status launch_accept(const wisp_accept_args *c, void *ws, const Layout &L, 
   return accept_launch(ap, c->logits_dtype == WISP_BF16, sms, s) == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 
+// (the queries' side of an 8-bit cache's arguments is that of any attention; an empty batch needs no scales)
+wisp_status check_kv8(const wisp_attn_kv8_args *a) {
+  const wisp_status st = check_attn(a ? &a->attn : nullptr);
+  if (st != WISP_OK || a->attn.B == 0) return st;
+  return a->k_scale && a->v_scale ? WISP_OK : WISP_ERR_INVALID_ARG;
+}
+
+wisp_status attention_call(const wisp_attn_args *attn, KvScales sc, void *ws, size_t ws_bytes, void *stream) {
+  wisp_status st = check_attn(attn);
+  if (st != WISP_OK) return st;
+  int dev = 0, sms = 0;
+  if ((st = device_setup(&dev, &sms)) != WISP_OK) return st;
+  const Layout L = make_layout(attn, nullptr, sms);
+  if ((st = check_ws(ws, ws_bytes, L)) != WISP_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = launch_plan(attn, nullptr, ws, L, sms, false, s)) != WISP_OK) return st;
+  if (attn->B == 0) return WISP_OK;
+  // alone on the stream after the planner: the attention CTAs set up while the planner runs
+  return launch_attention(attn, sc, ws, L, s);
+}
+
+wisp_status step_call(const wisp_attn_args *attn, KvScales sc, const wisp_accept_args *acc, void *ws, size_t ws_bytes,
+                      void *stream) {
+  wisp_status st = check_attn(attn);
+  if (st != WISP_OK) return st;
+  if ((st = check_accept(acc)) != WISP_OK) return st;
+  if (attn->B != acc->B || attn->total_q_rows != acc->total_q_rows) return WISP_ERR_INVALID_ARG;
+  int dev = 0, sms = 0;
+  if ((st = device_setup(&dev, &sms)) != WISP_OK) return st;
+  const Layout L = make_layout(attn, acc, sms);
+  if ((st = check_ws(ws, ws_bytes, L)) != WISP_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (attn->B == 0) return launch_plan(attn, acc, ws, L, sms, true, s);
+  // One planner for both parts.  The attention follows it on `s` as its programmatic dependent
+  // (persistent, one CTA per SM); the acceptance pass reads only the logits and the planner's
+  // state, so it runs on the library's side stream, forked after the planner and joined back.  The
+  // planner gives the attention a share of the SMs: its other CTAs exit at once, and the acceptance
+  // CTAs start there.
+  DeviceInfo &d = g_dev[dev];
+  std::lock_guard<std::mutex> lk(d.step_mu);
+  SideSlot *sl = side_slot(d, s);
+  if (!sl) return WISP_ERR_CUDA;
+  if ((st = launch_plan(attn, acc, ws, L, sms, true, s, true)) != WISP_OK) return st;
+  const AcceptParams ap = accept_params(acc, ws, L, sms);
+  const bool bf = acc->logits_dtype == WISP_BF16;
+  // the attention is enqueued first, so that its CTAs take the SMs first; the acceptance part of
+  // the plan and the acceptance CTAs follow on the side stream
+  bool ok = cudaEventRecord(sl->ev_fork, s) == cudaSuccess;
+  ok = ok && launch_attention(attn, sc, ws, L, s) == WISP_OK;
+  const bool forked = ok && cudaStreamWaitEvent(sl->side, sl->ev_fork, 0) == cudaSuccess;
+  ok = forked && launch_plan_accept(attn, acc, ws, L, sms, sl->side) == WISP_OK;
+  ok = ok && accept_launch(ap, bf, sms, sl->side) == cudaSuccess;
+  // join what was forked even after a failed launch, so that `s` never runs ahead of `side`
+  const bool joined = !forked || (cudaEventRecord(sl->ev_join, sl->side) == cudaSuccess &&
+                                  cudaStreamWaitEvent(s, sl->ev_join, 0) == cudaSuccess);
+  return ok && joined ? WISP_OK : WISP_ERR_CUDA;
+}
+
 }  // namespace
 
 // Workspace of wisp_verify_accept_noalloc: status word, per-request offsets, flags and state,
@@ -469,17 +537,12 @@ size_t wisp_verify_workspace_size(const wisp_attn_args *attn, const wisp_accept_
 }
 
 wisp_status wisp_verify_attention(const wisp_attn_args *attn, void *ws, size_t ws_bytes, void *stream) {
-  wisp_status st = check_attn(attn);
-  if (st != WISP_OK) return st;
-  int dev = 0, sms = 0;
-  if ((st = device_setup(&dev, &sms)) != WISP_OK) return st;
-  const Layout L = make_layout(attn, nullptr, sms);
-  if ((st = check_ws(ws, ws_bytes, L)) != WISP_OK) return st;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((st = launch_plan(attn, nullptr, ws, L, sms, false, s)) != WISP_OK) return st;
-  if (attn->B == 0) return WISP_OK;
-  // alone on the stream after the planner: the attention CTAs set up while the planner runs
-  return launch_attention(attn, ws, L, s);
+  return attention_call(attn, KvScales(), ws, ws_bytes, stream);
+}
+
+wisp_status wisp_verify_attention_kv8(const wisp_attn_kv8_args *a, void *ws, size_t ws_bytes, void *stream) {
+  const wisp_status st = check_kv8(a);
+  return st != WISP_OK ? st : attention_call(&a->attn, KvScales{a->k_scale, a->v_scale}, ws, ws_bytes, stream);
 }
 
 wisp_status wisp_verify_accept(const wisp_accept_args *acc, void *ws, size_t ws_bytes, void *stream) {
@@ -509,39 +572,13 @@ wisp_status wisp_verify_accept_greedy(const wisp_accept_args *acc, void *ws, siz
 
 wisp_status wisp_verify_step(const wisp_attn_args *attn, const wisp_accept_args *acc, void *ws, size_t ws_bytes,
                              void *stream) {
-  wisp_status st = check_attn(attn);
-  if (st != WISP_OK) return st;
-  if ((st = check_accept(acc)) != WISP_OK) return st;
-  if (attn->B != acc->B || attn->total_q_rows != acc->total_q_rows) return WISP_ERR_INVALID_ARG;
-  int dev = 0, sms = 0;
-  if ((st = device_setup(&dev, &sms)) != WISP_OK) return st;
-  const Layout L = make_layout(attn, acc, sms);
-  if ((st = check_ws(ws, ws_bytes, L)) != WISP_OK) return st;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (attn->B == 0) return launch_plan(attn, acc, ws, L, sms, true, s);
-  // One planner for both parts.  The attention follows it on `s` as its programmatic dependent
-  // (persistent, one CTA per SM); the acceptance pass reads only the logits and the planner's
-  // state, so it runs on the library's side stream, forked after the planner and joined back.  The
-  // planner gives the attention a share of the SMs: its other CTAs exit at once, and the acceptance
-  // CTAs start there.
-  DeviceInfo &d = g_dev[dev];
-  std::lock_guard<std::mutex> lk(d.step_mu);
-  SideSlot *sl = side_slot(d, s);
-  if (!sl) return WISP_ERR_CUDA;
-  if ((st = launch_plan(attn, acc, ws, L, sms, true, s, true)) != WISP_OK) return st;
-  const AcceptParams ap = accept_params(acc, ws, L, sms);
-  const bool bf = acc->logits_dtype == WISP_BF16;
-  // the attention is enqueued first, so that its CTAs take the SMs first; the acceptance part of
-  // the plan and the acceptance CTAs follow on the side stream
-  bool ok = cudaEventRecord(sl->ev_fork, s) == cudaSuccess;
-  ok = ok && launch_attention(attn, ws, L, s) == WISP_OK;
-  const bool forked = ok && cudaStreamWaitEvent(sl->side, sl->ev_fork, 0) == cudaSuccess;
-  ok = forked && launch_plan_accept(attn, acc, ws, L, sms, sl->side) == WISP_OK;
-  ok = ok && accept_launch(ap, bf, sms, sl->side) == cudaSuccess;
-  // join what was forked even after a failed launch, so that `s` never runs ahead of `side`
-  const bool joined = !forked || (cudaEventRecord(sl->ev_join, sl->side) == cudaSuccess &&
-                                  cudaStreamWaitEvent(s, sl->ev_join, 0) == cudaSuccess);
-  return ok && joined ? WISP_OK : WISP_ERR_CUDA;
+  return step_call(attn, KvScales(), acc, ws, ws_bytes, stream);
+}
+
+wisp_status wisp_verify_step_kv8(const wisp_attn_kv8_args *a, const wisp_accept_args *acc, void *ws, size_t ws_bytes,
+                                 void *stream) {
+  const wisp_status st = check_kv8(a);
+  return st != WISP_OK ? st : step_call(&a->attn, KvScales{a->k_scale, a->v_scale}, acc, ws, ws_bytes, stream);
 }
 
 wisp_status wisp_verify_get_device_status(const void *ws, int32_t *code, int64_t *request_id) {

@@ -10,6 +10,7 @@ struct AttnParams {
   const int64_t *request_ids;
   const int32_t *block_tables;
   const void *q, *k_cache, *v_cache;
+  const float *k_scale, *v_scale;  // [num_blocks, Hkv], of an e4m3 cache; else null
   void *out;
   DeviceStatus *status;
   const int32_t *req_chunks;
@@ -30,5 +31,9 @@ cudaError_t attn_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
 // tcgen05 / TMA kernel for bf16 KV, D in {64, 128}; `grid` persistent CTAs
 cudaError_t attn_tc_setup();
 cudaError_t attn_tc_launch(const AttnParams &p, int grid, cudaStream_t s);
+
+// kernel for e4m3 KV, queries and outputs in fp32 or bf16, D in {64, 128}; `grid` persistent CTAs
+cudaError_t attn_kv8_setup();
+cudaError_t attn_kv8_launch(const AttnParams &p, bool f32, int grid, cudaStream_t s);
 
 }  // namespace wisp
