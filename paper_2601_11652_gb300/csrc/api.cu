@@ -73,7 +73,7 @@ wisp_status device_setup(int *dev_out, int *sms_out) {
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return WISP_ERR_CUDA;
     cudaError_t e = attn_f32_setup();
     if (e == cudaSuccess) e = attn_tc_setup();
-    if (e == cudaSuccess) e = attn_kv8_setup();
+    if (e == cudaSuccess) e = attn_kv8_tc_setup();
     if (e == cudaSuccess) e = accept_setup();
     if (e != cudaSuccess) return WISP_ERR_CUDA;
     d.sms = sms;
@@ -347,7 +347,8 @@ wisp_status launch_attention(const wisp_attn_args *a, KvScales sc, void *ws, con
   // on this stream, and split items are merged inside the kernel by the last chunk to finish
   const int grid = (int)(L.max_items < L.target_items / kItemsPerSM ? L.max_items : L.target_items / kItemsPerSM);
   const bool bf = a->qkv_dtype == WISP_BF16;
-  const cudaError_t e = sc.k ? attn_kv8_launch(ap, !bf, grid, s) : bf ? attn_tc_launch(ap, grid, s) : attn_f32_launch(ap, grid, s);
+  const cudaError_t e = sc.k ? (bf ? attn_kv8_tc_launch(ap, grid, s) : attn_kv8_f32_launch(ap, grid, s))
+                             : (bf ? attn_tc_launch(ap, grid, s) : attn_f32_launch(ap, grid, s));
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 

@@ -32,8 +32,10 @@ cudaError_t attn_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
 cudaError_t attn_tc_setup();
 cudaError_t attn_tc_launch(const AttnParams &p, int grid, cudaStream_t s);
 
-// kernel for e4m3 KV, queries and outputs in fp32 or bf16, D in {64, 128}; `grid` persistent CTAs
-cudaError_t attn_kv8_setup();
-cudaError_t attn_kv8_launch(const AttnParams &p, bool f32, int grid, cudaStream_t s);
+// CUDA-core kernel for e4m3 KV with fp32 queries and outputs, D in {64, 128}; `grid` persistent CTAs
+cudaError_t attn_kv8_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
+// tcgen05 / TMA kernel for e4m3 KV with bf16 queries and outputs
+cudaError_t attn_kv8_tc_setup();
+cudaError_t attn_kv8_tc_launch(const AttnParams &p, int grid, cudaStream_t s);
 
 }  // namespace wisp

@@ -1,15 +1,15 @@
-// attn_kv8.cu -- paged GQA attention of the verification forward over an e4m3 cache, on the CUDA cores.
+// attn_kv8_f32.cu -- paged GQA attention of the verification forward over an e4m3 cache with fp32 queries, on the CUDA
+// cores (the tensor cores would round the queries).
 //
-// Same contract as attn_tc.cu, with K and V of a page of one head worth code * scale (include/wisp_kv8.h).
+// Same contract as attn_f32.cu, with K and V of a page of one head worth code * scale (include/wisp_kv8.h).
 //
-// Persistent CTAs (one per SM) of eight warps take work items from the plan's counter.  A warp keeps eight of
-// an item's rows: their scores against a page of 16 keys (lane: one key, four rows), running maxima and sums, and O
-// (lane: D / 32 columns of the eight rows).  The CTA decodes each page into shared memory once.
+// Persistent CTAs (one per SM) of eight warps take work items from the plan's counter.  A warp keeps four of
+// an item's rows: their scores against a page of 16 keys (lane: one key, two rows), running maxima and sums, and O
+// (lane: D / 32 columns of the four rows).  The CTA decodes each page into shared memory once.
 #include "attn_merge.cuh"
 #include "fp8.cuh"
 
 #include <cstring>
-#include <type_traits>
 
 namespace wisp {
 
@@ -18,18 +18,15 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kPage = 16;
-constexpr int kRowsPerWarp = kTcRowsPerItem / kWarps;
-static_assert(kF32RowsPerItem <= kTcRowsPerItem && kRowsPerWarp == 8, "rows of an item");
-
-__device__ __forceinline__ float to_float(uint16_t b) { return bf16_bits_to_float(b); }
-__device__ __forceinline__ float to_float(float x) { return x; }
+constexpr int kRowsPerWarp = kF32RowsPerItem / kWarps;
+static_assert(kRowsPerWarp == 4, "rows of an item");
 
 }  // namespace
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_constant__ AttnParams p) {
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attn_kv8_f32_kernel(const __grid_constant__ AttnParams p) {
   constexpr int LD = D + 4, CPL = D / 32;
-  __shared__ __align__(16) float s_q[kTcRowsPerItem * LD];
+  __shared__ __align__(16) float s_q[kF32RowsPerItem * LD];
   extern __shared__ __align__(16) float s_kv[];  // K [16][LD], V [16][LD]
   __shared__ float s_p[kWarps][kRowsPerWarp][kPage];
   __shared__ int s_item, s_last;
@@ -54,18 +51,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_cons
     const int it = s_item;
     if (it < 0) break;
     const WorkItem w = p.items[it];
-    for (int c = tid; c < kTcRowsPerItem * D; c += kThreads) {
+    for (int c = tid; c < kF32RowsPerItem * D; c += kThreads) {
       const int row = c / D, d = c % D, rj = w.row0 + row;
       s_q[row * LD + d] =
-          row < w.rows ? to_float(static_cast<const T *>(p.q)[((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + d]) : 0.0f;
+          row < w.rows ? static_cast<const float *>(p.q)[((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + d] : 0.0f;
     }
-    float o[kRowsPerWarp][CPL], m[4], l[4];
+    float o[kRowsPerWarp][CPL], m[2], l[2];
 #pragma unroll
     for (int i = 0; i < kRowsPerWarp; ++i)
 #pragma unroll
       for (int q = 0; q < CPL; ++q) o[i][q] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.0f;
     }
@@ -94,10 +91,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_cons
       }
       __syncthreads();
       const int tok = t + key;
-      float al[4];
+      float al[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = warp * kRowsPerWarp + half * 4 + i;
+      for (int i = 0; i < 2; ++i) {
+        const int row = warp * kRowsPerWarp + half * 2 + i;
         float s = 0.0f;
         for (int d = 0; d < D; d += 4) {
           const float4 a = *reinterpret_cast<const float4 *>(s_q + row * LD + d);
@@ -113,12 +110,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_cons
         m[i] = mn;
         const float e = s == -INFINITY ? 0.0f : exp2f(s - mn);
         l[i] = fmaf(l[i], al[i], e);
-        s_p[warp][half * 4 + i][key] = e;
+        s_p[warp][half * 2 + i][key] = e;
       }
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < kRowsPerWarp; ++i) {
-        const float a = __shfl_sync(0xffffffffu, al[i & 3], (i >> 2) * 16);
+        const float a = __shfl_sync(0xffffffffu, al[i & 1], (i >> 1) * 16);
 #pragma unroll
         for (int q = 0; q < CPL; ++q) o[i][q] *= a;
         for (int x = 0; x < kPage; ++x) {
@@ -132,16 +129,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_cons
       __syncwarp();
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
 #pragma unroll
     for (int i = 0; i < kRowsPerWarp; ++i) {
       const int row = warp * kRowsPerWarp + i;
-      const float den = __shfl_sync(0xffffffffu, l[i & 3], (i >> 2) * 16), mx = __shfl_sync(0xffffffffu, m[i & 3], (i >> 2) * 16);
+      const float den = __shfl_sync(0xffffffffu, l[i & 1], (i >> 1) * 16), mx = __shfl_sync(0xffffffffu, m[i & 1], (i >> 1) * 16);
       if (row >= w.rows) continue;
       if (w.poff < 0) {
         const int rj = w.row0 + row;
-        st_cols<CPL>(static_cast<T *>(p.out) + ((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + lane * CPL, o[i], 1.0f / den);
+        st_cols<CPL>(static_cast<float *>(p.out) + ((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + lane * CPL, o[i], 1.0f / den);
       } else {
         float *part = p.partials + w.poff;
 #pragma unroll
@@ -163,24 +160,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv8_kernel(const __grid_cons
         __threadfence();
       }
       __syncthreads();
-      if (s_last > 0) merge_chunks<D, T>(p, w, g, s_last, warp, kWarps);
+      if (s_last > 0) merge_chunks<D, float>(p, w, g, s_last, warp, kWarps);
     }
   }
 }
 
-namespace {
-template <int D>
-constexpr int smem_bytes() { return 2 * kPage * (D + 4) * 4; }
-}  // namespace
-
-cudaError_t attn_kv8_setup() {  // (with the static part more than the 48 KB that need no asking)
-  cudaError_t e = cudaFuncSetAttribute(attn_kv8_kernel<128, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<128>());
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attn_kv8_kernel<128, uint16_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<128>());
-  return e;
-}
-
-cudaError_t attn_kv8_launch(const AttnParams &p, bool f32, int grid, cudaStream_t s) {
+cudaError_t attn_kv8_f32_launch(const AttnParams &p, int grid, cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cudaLaunchAttribute attr[1];
@@ -191,10 +176,8 @@ cudaError_t attn_kv8_launch(const AttnParams &p, bool f32, int grid, cudaStream_
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cfg.dynamicSmemBytes = p.D == 128 ? smem_bytes<128>() : smem_bytes<64>();
-  if (p.D == 128)
-    return f32 ? cudaLaunchKernelEx(&cfg, attn_kv8_kernel<128, float>, p) : cudaLaunchKernelEx(&cfg, attn_kv8_kernel<128, uint16_t>, p);
-  return f32 ? cudaLaunchKernelEx(&cfg, attn_kv8_kernel<64, float>, p) : cudaLaunchKernelEx(&cfg, attn_kv8_kernel<64, uint16_t>, p);
+  cfg.dynamicSmemBytes = 2 * kPage * (p.D + 4) * 4;
+  return p.D == 128 ? cudaLaunchKernelEx(&cfg, attn_kv8_f32_kernel<128>, p) : cudaLaunchKernelEx(&cfg, attn_kv8_f32_kernel<64>, p);
 }
 
 }  // namespace wisp
