@@ -34,6 +34,7 @@
 #include <cudaTypedefs.h>
 #include <cstring>
 #include <mutex>
+#include <type_traits>
 
 namespace wisp {
 
@@ -71,8 +72,8 @@ struct Cfg {
   static constexpr int N_BAR = 2 * NSK + 2 * NSV + 18 + 2 * RING + 5;
   static constexpr int OFF_SC = (OFF_BAR + N_BAR * 8 + 15) / 16 * 16;  // float2 [SC][8]: a page's K and V scale
   static constexpr int OFF_RF = OFF_SC + SC * 64;                      // float [RF][64]
-  static constexpr int OFF_RED = OFF_RF + RF * kNR * 4;                // float [2 groups][2][4][64] row maxima per quadrant
-  static constexpr int OFF_MW = OFF_RED + 2 * 2 * 4 * kNR * 4;         // float [8][2][64] per warp: 8 - m, sum factors
+  static constexpr int OFF_RED = OFF_RF + RF * kNR * 4;                // [2 groups][2][4][32] row maxima per quadrant, bf16 pairs
+  static constexpr int OFF_MW = OFF_RED + 2 * 2 * 4 * 32 * 4;         // float [8][2][64] per warp: 8 - m, sum factors
   static constexpr int OFF_M = OFF_MW + kSoftmaxWarps * 2 * kNR * 4;   // float [4][64] m of tile n in n % 4
   static constexpr int OFF_CW = OFF_M + 4 * kNR * 4;                   // float [4][64] per correction warp
   static constexpr int OFF_HL = OFF_CW + 4 * kNR * 4;                  // float [2][2][4][64] row-sum shares
@@ -141,6 +142,27 @@ __device__ __forceinline__ float warp_transpose_sum(float (&v)[32], int lane) {
     }
   }
   return v[0];
+}
+
+__device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {  // NaN never wins
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Transposing maximum of bf16 pairs over the 32 lanes of a warp (v is consumed): lanes i and 16 + i get that of v[i].
+__device__ __forceinline__ uint32_t warp_transpose_max(uint32_t (&v)[16], int lane) {
+#pragma unroll
+  for (int w = 8; w >= 1; w >>= 1) {
+    const bool up = (lane & w) != 0;
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const uint32_t keep = up ? v[i + w] : v[i];
+      const uint32_t send = up ? v[i] : v[i + w];
+      v[i] = bmax2(keep, __shfl_xor_sync(0xffffffffu, send, w));
+    }
+  }
+  return bmax2(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
 }
 
 __device__ __forceinline__ float lg2(float x) {
@@ -257,7 +279,82 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto div_g = [&](int row) -> int { return (int)(((unsigned)row * gm) >> 16); };
   bool ok = true;
 
-  // registers: 20 warps launch with 96 each, 1920 a lane in all = 8 x 144 + 4 x 112 + 8 x 40.  (Each split stands at the
+  // ------------------------------------------------------------------ MMA issuers: S^T by warp 1, PV by warp 16
+  auto issue = [&](auto which) {
+    constexpr bool is_s = decltype(which)::value;
+    uint32_t n = 0;
+    int li = 0;
+    for (uint32_t j = 0; ok; ++j, ++li) {
+      const int slot = j % C::RING;
+      if (!wait_bar(B.at(BR::IT_FULL + slot), (j / C::RING) & 1, s_abort)) { ok = false; break; }
+      const int it = s_ring[slot].it;
+      const int rows = s_ring[slot].w.rows, ntok = s_ring[slot].w.t1 - s_ring[slot].w.t0;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
+      if (it < 0) break;
+      const int nt = (ntok + kBT - 1) / kBT;
+      const int ncol = (rows + 7) / 8 * 16;  // the MMA's N: hi and lo of the rows rounded up to 8
+      if constexpr (is_s) {
+        // S^T(n): K(n) has landed, the item's Q is loaded, the TMEM tile has been read
+        const uint32_t idesc = ptx::idesc_e4m3_f32(kBT, ncol, false, false);
+        const int qb = li & 1;
+        if (!wait_bar(B.at(BR::Q_FULL + qb), (li >> 1) & 1, s_abort)) { ok = false; break; }
+        const uint64_t qd = sdesc<D>(sbase + C::OFF_Q + qb * C::Q_BYTES);
+        for (int t = 0; t < nt; ++t, ++n) {
+          const int st = (int)(n % C::NSK), sb = n & 1;
+          if (!wait_bar(B.at(BR::K_FULL + st), (n / C::NSK) & 1, s_abort) ||
+              !wait_bar(B.at(BR::S_EMPTY + sb), ((n >> 1) & 1) ^ 1, s_abort)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) {
+            ptx::tc_fence_after();
+            const uint64_t kd = sdesc<D>(sbase + C::OFF_K + st * C::KV_TILE);
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks)  // descriptor addresses are in units of 16 bytes
+              ptx::umma_f8(tmem + sb * 128, kd + 2 * ks, qd + 2 * ks, idesc, ks > 0);
+            ptx::umma_commit(B.at(BR::S_FULL + sb));
+            ptx::umma_commit(B.at(BR::K_EMPTY + st));
+            if (t == nt - 1) ptx::umma_commit(B.at(BR::Q_EMPTY + qb));
+          }
+          __syncwarp();
+        }
+      } else {
+        // PV(n): P(n) is published, V(n) has landed, the accumulator has been read.  A = V^T, MN-major (for D = 64
+        // both halves of M read the same 64 columns: lanes 64..127 repeat lanes 0..63 and are not used)
+        const uint32_t idesc = ptx::idesc_e4m3_f32(128, ncol, true, true);
+        for (int t = 0; t < nt; ++t, ++n) {
+          const int st = (int)(n % C::NSV), b = n & 1;
+          if (!wait_bar(B.at(BR::O_EMPTY + b), ((n >> 1) & 1) ^ 1, s_abort) ||
+              !wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort) ||
+              !wait_bar(B.at(BR::P_FULL + b), (n >> 1) & 1, s_abort)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) {
+            ptx::tc_fence_after();
+            const uint64_t vd = sdesc<D>(sbase + C::OFF_V + st * C::KV_TILE);
+            const uint64_t pd = ptx::sdesc_sw128(sbase + C::OFF_P + b * C::P_BYTES, C::P_BYTES, 1024);
+#pragma unroll
+            for (int ks = 0; ks < kBT / 32; ++ks)
+              ptx::umma_f8(tmem + 256 + b * 128, vd + ((ks * 32 * D) >> 4), pd + ((ks * 32 * 128) >> 4), idesc, ks > 0);
+            ptx::umma_commit(B.at(BR::O_FULL + b));
+            ptx::umma_commit(B.at(BR::V_EMPTY + st));
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (lane == 0) {
+      // every MMA the issuers issued must finish before the TMEM is released
+      ptx::umma_commit(B.at(BR::MMA_DONE));
+      const long long c0 = clock64();
+      while (!ptx::mbar_try_wait(B.at(BR::MMA_DONE), 0) && clock64() - c0 < kWaitCycles) {
+      }
+    }
+  };
+
+  // registers: 20 warps launch with 96 each, 1920 a lane in all = 8 x 144 + 4 x 112 + 4 x 48 + 4 x 32.  (Each split stands at the
   // head of its own branch: after a join the compiler counts with the least.)
   const int wg = warp >> 2;
   if (wg == 1 || wg == 3) {
@@ -288,141 +385,138 @@ __global__ void __launch_bounds__(kThreads, 1)
       float2 lp[kNR / 2];  // this thread's (key's) share of every row sum
 #pragma unroll
       for (int i = 0; i < kNR / 2; ++i) lp[i] = make_float2(0.0f, 0.0f);
-      float L[2] = {-INFINITY, -INFINITY};  // the sums' references, rows lane and 32 + lane
+      float L[2] = {-INFINITY, -INFINITY};  // the sums' references, rows 2 lane and 2 lane + 1
       for (int t = (int)((n0 ^ grp) & 1); t < ntiles; t += 2, ++mine) {
         const uint32_t n = n0 + t;
         if (!wait_bar(B.at(BR::S_FULL + grp), (n >> 1) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
         const float2 sc = s_sc[(n % C::SC) * 8 + qd * 2 + (lane >> 4)];
         const float lsv = fmaxf(lg2(sc.y), kLeastScaleLog2);
-        float x[kNR];  // log2-scaled scores plus log2 of V's scale
         const uint32_t at = tmem + lane_addr + grp * 128;
-        // 16 rows from their two halves
-        auto join = [&](int c, const uint32_t (&hi)[16], const uint32_t (&lo)[16]) {
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const float4 r4 = *reinterpret_cast<const float4 *>(rf + 16 * c + i);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int y = i + 2 * q;
-              const float2 s = __ffma2_rn(make_float2(__uint_as_float(lo[y]), __uint_as_float(lo[y + 1])), both(0.0625f),
-                                          make_float2(__uint_as_float(hi[y]), __uint_as_float(hi[y + 1])));
-              const float2 u = __fmul2_rn(q == 0 ? make_float2(r4.x, r4.y) : make_float2(r4.z, r4.w), both(sc.x));
-              const float2 v = __ffma2_rn(s, u, both(lsv));
-              x[16 * c + y] = v.x;
-              x[16 * c + y + 1] = v.y;
-            }
-          }
-        };
-        {
-          uint32_t hi[2][16], lo[2][16];
-          ptx::tmem_ld16(at, hi[0]);
-          ptx::tmem_ld16(at + nrow, lo[0]);
-          if (nu > 2) {
-            ptx::tmem_ld16(at + 16, hi[1]);
-            ptx::tmem_ld16(at + nrow + 16, lo[1]);
-          }
-          ptx::tmem_wait_ld();
-          join(0, hi[0], lo[0]);
-          if (nu > 2) join(1, hi[1], lo[1]);
-        }
-#pragma unroll
-        for (int c = 2; c < kNR / 16; ++c) {
-          if (nu > 2 * c) {
-            uint32_t hi[16], lo[16];
-            ptx::tmem_ld16(at + 16 * c, hi);
-            ptx::tmem_ld16(at + nrow + 16 * c, lo);
-            ptx::tmem_wait_ld();
-            join(c, hi, lo);
-          }
-        }
-        // the tile is in registers: it may be overwritten
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(B.at(BR::S_EMPTY + grp));
         // causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked
         // too.  Only an item's last tiles (from nfull on) have such keys.
         const int tok = t0 + t * kBT + qd * 32 + lane;
-        if (t >= nfull) {
-          const int jmin = tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0));
+        const int jmin = t < nfull ? 0 : tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0));
+        // First pass: the scores (log2 units, plus log2 of V's scale) from their halves, back to TMEM, and the maxima
+        // of the rows over this warp's keys as bf16 pairs: lane i gets rows 2 i and 2 i + 1.
+        uint32_t top = 0xff80ff80u;
 #pragma unroll
-          for (int i = 0; i < kNR; ++i)
-            if (i < jmin) x[i] = -INFINITY;
-        }
-        // the rows' maxima over this warp's keys, then over the group's
-        float mx[2] = {-INFINITY, -INFINITY};
+        for (int hf = 0; hf < 2; ++hf) {
+          if (nu > 4 * hf) {
+            uint32_t wd[16];
 #pragma unroll
-        for (int u = 0; u < kNR / 8; ++u) {
-          if (u < nu) {
+            for (int c = 2 * hf; c < 2 * hf + 2; ++c) {
+              if (nu > 2 * c) {
+                uint32_t hi[16], lo[16];
+                ptx::tmem_ld16(at + 16 * c, hi);
+                ptx::tmem_ld16(at + nrow + 16 * c, lo);
+                ptx::tmem_wait_ld();
 #pragma unroll
-            for (int i = 8 * u; i < 8 * u + 8; ++i) {
-              const float rm = ptx::warp_max(x[i]);
-              if (lane == (i & 31)) mx[i >> 5] = rm;
+                for (int i = 0; i < 16; i += 4) {
+                  const float4 r4 = *reinterpret_cast<const float4 *>(rf + 16 * c + i);
+#pragma unroll
+                  for (int q = 0; q < 4; q += 2) {
+                    const float2 s = __ffma2_rn(make_float2(__uint_as_float(lo[i + q]), __uint_as_float(lo[i + q + 1])), both(0.0625f),
+                                                make_float2(__uint_as_float(hi[i + q]), __uint_as_float(hi[i + q + 1])));
+                    const float2 u = __fmul2_rn(q == 0 ? make_float2(r4.x, r4.y) : make_float2(r4.z, r4.w), both(sc.x));
+                    const float2 v = __ffma2_rn(s, u, both(lsv));
+                    hi[i + q] = __float_as_uint(v.x);
+                    hi[i + q + 1] = __float_as_uint(v.y);
+                  }
+                }
+                if (t >= nfull) {
+#pragma unroll
+                  for (int i = 0; i < 16; ++i)
+                    if (16 * c + i < jmin) hi[i] = 0xff800000u;
+                }
+                ptx::tmem_st16(at + 16 * c, hi);  // (past nrow: over low halves that have been read)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wd[8 * (c & 1) + i] = pack_bf16(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1]));
+              } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wd[8 * (c & 1) + i] = 0xff80ff80u;
+              }
             }
+            const uint32_t tw = warp_transpose_max(wd, lane);
+            if (lane >> 4 == hf) top = tw;
           }
         }
-        float *red = reinterpret_cast<float *>(smem + C::OFF_RED) + (grp * 2 + (mine & 1)) * 4 * kNR;
-        red[qd * kNR + lane] = mx[0];
-        red[qd * kNR + 32 + lane] = mx[1];
+        ptx::tmem_wait_st();
+        uint32_t *red = reinterpret_cast<uint32_t *>(smem + C::OFF_RED) + (grp * 2 + (mine & 1)) * 4 * 32;
+        red[qd * 32 + lane] = top;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(B.at(BR::RED + grp));
         if (!wait_bar(B.at(BR::RED + grp), mine & 1, s_abort)) { ok = false; break; }
+        // the group's maxima, rounded up: 2^-8 of their magnitude covers the rounding to bf16
+        top = bmax2(bmax2(red[lane], red[32 + lane]), bmax2(red[64 + lane], red[96 + lane]));
+        float m[2] = {__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)};
         bool move = false;
-        float al[2];
+        float al[2], f0[2], f1[2];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const float *rd = red + 32 * y + lane;
-          const float m = fmaxf(fmaxf(rd[0], rd[kNR]), fmaxf(rd[2 * kNR], rd[3 * kNR]));
-          mx[y] = m;
+          if (m[y] != -INFINITY) m[y] = fmaf(fabsf(m[y]), 0x1p-8f, m[y]);
           al[y] = 1.0f;
-          if (!(m <= L[y] + kLazy)) {  // (a NaN too)
+          if (!(m[y] <= L[y] + kLazy)) {  // (a NaN too)
             if (L[y] != -INFINITY) {
-              al[y] = ptx::ex2(L[y] - m);
+              al[y] = ptx::ex2(L[y] - m[y]);
               move = true;
             }
-            L[y] = m;
+            L[y] = m[y];
           }
-          mw[32 * y + lane] = m == -INFINITY ? 0.0f : kHead - m;
-          bw[32 * y + lane] = m == -INFINITY ? 0.0f : ptx::ex2(m - L[y] - kHead);
+          f0[y] = m[y] == -INFINITY ? 0.0f : kHead - m[y];
+          f1[y] = m[y] == -INFINITY ? 0.0f : ptx::ex2(m[y] - L[y] - kHead);
         }
+        reinterpret_cast<float2 *>(mw)[lane] = make_float2(f0[0], f0[1]);
+        reinterpret_cast<float2 *>(bw)[lane] = make_float2(f1[0], f1[1]);
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
           for (int i = 0; i < kNR / 2; ++i) {
-            const float a0 = __shfl_sync(0xffffffffu, al[i >= 16], (2 * i) & 31), a1 = __shfl_sync(0xffffffffu, al[i >= 16], (2 * i + 1) & 31);
+            const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
             lp[i] = __fmul2_rn(lp[i], make_float2(a0, a1));
           }
         }
         // P buffer n & 1 is free again once PV(n - 2) is done (and the maxima of tile n - 4 have been read by then)
         if (n >= 2 && !wait_bar(B.at(BR::O_FULL + grp), ((n - 2) >> 1) & 1, s_abort)) { ok = false; break; }
-        if (qd == 0) {
-          s_m[(n & 3) * kNR + lane] = mx[0];
-          s_m[(n & 3) * kNR + 32 + lane] = mx[1];
-        }
+        if (qd == 0) reinterpret_cast<float2 *>(s_m + (n & 3) * kNR)[lane] = make_float2(m[0], m[1]);
         __syncwarp();
+        // Second pass: P = 2^(s - m + 8), its shares of the sums, its two parts
         const float2 inv2 = both(ptx::ex2(-lsv));
         uint8_t *prow = smem + C::OFF_P + grp * C::P_BYTES + (qd * 32 + lane) * 128;
         const int sw = lane & 7;
 #pragma unroll
-        for (int u = 0; u < kNR / 8; ++u) {
-          if (u < nu) {
-            uint32_t hi[4], lo[4];
+        for (int c = 0; c < kNR / 16; ++c) {
+          if (nu > 2 * c) {
+            uint32_t x[16];
+            ptx::tmem_ld16(at + 16 * c, x);
+            ptx::tmem_wait_ld();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float4 m4 = reinterpret_cast<const float4 *>(mw + 8 * u)[h], b4 = reinterpret_cast<const float4 *>(bw + 8 * u)[h];
+            for (int u = 2 * c; u < 2 * c + 2; ++u) {
+              if (u < nu) {
+                uint32_t hi[4], lo[4];
 #pragma unroll
-              for (int q = 0; q < 2; ++q) {
-                const int i = 8 * u + 4 * h + 2 * q;
-                const float2 a = __fadd2_rn(make_float2(x[i], x[i + 1]), q == 0 ? make_float2(m4.x, m4.y) : make_float2(m4.z, m4.w));
-                const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
-                lp[i >> 1] = __ffma2_rn(e, __fmul2_rn(q == 0 ? make_float2(b4.x, b4.y) : make_float2(b4.z, b4.w), inv2), lp[i >> 1]);
-                split2(e.x, e.y, hi[2 * h + q], lo[2 * h + q]);
+                for (int h = 0; h < 2; ++h) {
+                  const float4 m4 = reinterpret_cast<const float4 *>(mw + 8 * u)[h], b4 = reinterpret_cast<const float4 *>(bw + 8 * u)[h];
+#pragma unroll
+                  for (int q = 0; q < 2; ++q) {
+                    const int i = 8 * u + 4 * h + 2 * q;
+                    const float2 a = __fadd2_rn(make_float2(__uint_as_float(x[i & 15]), __uint_as_float(x[(i & 15) + 1])),
+                                                q == 0 ? make_float2(m4.x, m4.y) : make_float2(m4.z, m4.w));
+                    const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
+                    lp[i >> 1] = __ffma2_rn(e, __fmul2_rn(q == 0 ? make_float2(b4.x, b4.y) : make_float2(b4.z, b4.w), inv2), lp[i >> 1]);
+                    split2(e.x, e.y, hi[2 * h + q], lo[2 * h + q]);
+                  }
+                }
+                const int oh = 8 * u, ol = nrow + 8 * u;
+                *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
               }
             }
-            const int oh = 8 * u, ol = nrow + 8 * u;
-            *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-            *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
           }
         }
+        // the scores have been read: the tile may be overwritten
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(B.at(BR::S_EMPTY + grp));
         if (t >= nfull) {
           // slots past the request's tokens hold anything, and a NaN times a weight of zero is NaN: zeros in their
           // place.  A value of the new tokens that is NaN is taken out, too, and put back at the end for the rows
@@ -479,10 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float *hl = s_hl + ((ob * 2 + grp) * 4 + qd) * kNR;
       hl[lane] = sh0;
       hl[32 + lane] = sh1;
-      if (qd == 0) {
-        s_lr[(ob * 2 + grp) * kNR + lane] = L[0];
-        s_lr[(ob * 2 + grp) * kNR + 32 + lane] = L[1];
-      }
+      if (qd == 0) reinterpret_cast<float2 *>(s_lr + (ob * 2 + grp) * kNR)[lane] = make_float2(L[0], L[1]);
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_FULL + ob));
     }
@@ -512,56 +603,54 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
       if (it < 0) break;
-      const int ob = li & 1, nrow = (w.rows + 7) / 8 * 8, nc = (nrow + 15) / 16;
+      const int ob = li & 1, nrow = (w.rows + 7) / 8 * 8;
       const int ntiles = (w.t1 - w.t0 + kBT - 1) / kBT;
       float2 acc[kNR / 2];
 #pragma unroll
       for (int i = 0; i < kNR / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
-      float M[2] = {-INFINITY, -INFINITY};  // rows lane and 32 + lane
+      float M[2] = {-INFINITY, -INFINITY};  // rows 2 lane and 2 lane + 1
       for (int t = 0; t < ntiles; ++t, ++n) {
         const int b = n & 1;
         if (!wait_bar(B.at(BR::O_FULL + b), (n >> 1) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
         bool move = false;
-        float al[2];
+        const float2 m2 = reinterpret_cast<const float2 *>(s_m + (n & 3) * kNR)[lane];
+        const float m[2] = {m2.x, m2.y};
+        float al[2], f[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const float m = s_m[(n & 3) * kNR + 32 * x + lane];
           al[x] = 1.0f;
-          if (!(m <= M[x] + kLazy)) {  // (a NaN too)
+          if (!(m[x] <= M[x] + kLazy)) {  // (a NaN too)
             if (M[x] != -INFINITY) {
-              al[x] = ptx::ex2(M[x] - m);
+              al[x] = ptx::ex2(M[x] - m[x]);
               move = true;
             }
-            M[x] = m;
+            M[x] = m[x];
           }
-          cw[32 * x + lane] = m == -INFINITY ? 0.0f : ptx::ex2(m - M[x] - kHead);
+          f[x] = m[x] == -INFINITY ? 0.0f : ptx::ex2(m[x] - M[x] - kHead);
         }
+        reinterpret_cast<float2 *>(cw)[lane] = make_float2(f[0], f[1]);
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
           for (int i = 0; i < kNR / 2; ++i) {
-            const float a0 = __shfl_sync(0xffffffffu, al[i >= 16], (2 * i) & 31), a1 = __shfl_sync(0xffffffffu, al[i >= 16], (2 * i + 1) & 31);
+            const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
             acc[i] = __fmul2_rn(acc[i], make_float2(a0, a1));
           }
         }
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < kNR / 16; ++c) {
-          if (c < nc) {
-            uint32_t hi[16], lo[16];
-            ptx::tmem_ld16(tmem + lane_addr + 256 + b * 128 + 16 * c, hi);
-            ptx::tmem_ld16(tmem + lane_addr + 256 + b * 128 + nrow + 16 * c, lo);
+        for (int c = 0; c < kNR / 8; ++c) {
+          if (8 * c < nrow) {
+            uint32_t hi[8], lo[8];
+            ptx::tmem_ld8(tmem + lane_addr + 256 + b * 128 + 8 * c, hi);
+            ptx::tmem_ld8(tmem + lane_addr + 256 + b * 128 + nrow + 8 * c, lo);
             ptx::tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const float4 f = *reinterpret_cast<const float4 *>(cw + 16 * c + 2 * i);
-#pragma unroll
-              for (int q = 0; q < 2; ++q) {
-                const int y = 2 * (i + q);
-                const float2 o = __ffma2_rn(make_float2(__uint_as_float(lo[y]), __uint_as_float(lo[y + 1])), both(0.0625f),
-                                            make_float2(__uint_as_float(hi[y]), __uint_as_float(hi[y + 1])));
-                acc[8 * c + i + q] = __ffma2_rn(o, q == 0 ? make_float2(f.x, f.y) : make_float2(f.z, f.w), acc[8 * c + i + q]);
-              }
+            for (int i = 0; i < 4; ++i) {
+              const float2 fr = *reinterpret_cast<const float2 *>(cw + 8 * c + 2 * i);
+              const float2 o = __ffma2_rn(make_float2(__uint_as_float(lo[2 * i]), __uint_as_float(lo[2 * i + 1])), both(0.0625f),
+                                          make_float2(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1])));
+              acc[4 * c + i] = __ffma2_rn(o, fr, acc[4 * c + i]);
             }
           }
         }
@@ -575,17 +664,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t first = (n - ntiles) & 1;
       const int nan0 = dval ? s_nan[ob * D + d] : INT32_MAX;
       if (dval) s_nan[ob * D + d] = INT32_MAX;
-      float l[2];
+      float l[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        l[x] = 0.0f;
-#pragma unroll
-        for (int gr = 0; gr < 2; ++gr) {
-          const float *hl = s_hl + (ob * 2 + (gr ^ first)) * 4 * kNR + 32 * x + lane;
-          const float lr = s_lr[(ob * 2 + (gr ^ first)) * kNR + 32 * x + lane];
-          const float sum = (hl[0] + hl[kNR]) + (hl[2 * kNR] + hl[3 * kNR]);
-          if (lr != -INFINITY) l[x] = fmaf(sum, ptx::ex2(lr - M[x]), l[x]);
-        }
+      for (int gr = 0; gr < 2; ++gr) {
+        const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 2 + (gr ^ first)) * 4 * kNR) + lane;
+        const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 2 + (gr ^ first)) * kNR)[lane];
+        const float2 h0 = hl[0], h1 = hl[kNR / 2], h2 = hl[kNR], h3 = hl[3 * kNR / 2];
+        if (lr.x != -INFINITY) l[0] = fmaf((h0.x + h1.x) + (h2.x + h3.x), ptx::ex2(lr.x - M[0]), l[0]);
+        if (lr.y != -INFINITY) l[1] = fmaf((h0.y + h1.y) + (h2.y + h3.y), ptx::ex2(lr.y - M[1]), l[1]);
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
@@ -597,8 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (w.poff < 0) {
-        cw[lane] = 1.0f / l[0];
-        cw[32 + lane] = 1.0f / l[1];
+        reinterpret_cast<float2 *>(cw)[lane] = make_float2(1.0f / l[0], 1.0f / l[1]);
         __syncwarp();
         // (row pointers stepped from row to row)
         int hh = w.row0 - div_g(w.row0) * g;
@@ -627,9 +712,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (qd == 0) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            if (32 * x + lane < w.rows) {
-              __stcg(part + w.rows * D + 32 * x + lane, M[x]);
-              __stcg(part + w.rows * D + w.rows + 32 * x + lane, l[x]);
+            if (2 * lane + x < w.rows) {
+              __stcg(part + w.rows * D + 2 * lane + x, M[x]);
+              __stcg(part + w.rows * D + w.rows + 2 * lane + x, l[x]);
             }
           }
         }
@@ -647,8 +732,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (chunks > 0) merge_chunks<D, uint16_t>(p, w, g, chunks, qd, 4);
       }
     }
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  } else if (wg == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 0 || warp == 3) {
       // ------------------------------------------------------------------ K / V producers
       const bool is_k = warp == 0;
@@ -769,14 +854,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         published += tiles;
       }
-    } else if (warp >= 17) {
+    } else {
+      issue(std::true_type());
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if (warp == 16) {
+      issue(std::false_type());
+    } else {
       // ------------------------------------------------------------------ Q loaders
       // Query row row0 + rho = j * g + hh at MMA row rho (hi) and nrow + rho (lo), rows past the item zero.  A row's
       // factor 2^e / sqrt(D) in log2 units goes to s_rf.
       const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
       constexpr int CPR = D / 8;     // 16-byte chunks per row, a lane each
       constexpr int RPP = 32 / CPR;  // rows per warp pass
-      constexpr int QB = 4;          // passes in flight
+      constexpr int QB = 2;          // passes in flight
       const int cc = lane % CPR;
       int li = 0;
       for (uint32_t j = 0; ok; ++j, ++li) {
@@ -794,7 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float *rf = s_rf + (li % C::RF) * kNR;
         for (int base = (warp - 17) * RPP; base < nrow; base += kQWarps * RPP * QB) {
           uint4 v[QB];
-  #pragma unroll
+#pragma unroll
           for (int u = 0; u < QB; ++u) {
             const int row = base + u * kQWarps * RPP + lane / CPR;
             v[u] = make_uint4(0, 0, 0, 0);
@@ -803,21 +895,21 @@ __global__ void __launch_bounds__(kThreads, 1)
               v[u] = __ldg(reinterpret_cast<const uint4 *>(qi + (int64_t)(jj * p.Hq + hh) * D));
             }
           }
-  #pragma unroll
+#pragma unroll
           for (int u = 0; u < QB; ++u) {
             const int row = base + u * kQWarps * RPP + lane / CPR;
             if (base + u * kQWarps * RPP < nrow) {  // (nrow is a multiple of RPP: the same for the whole warp)
               const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
               uint32_t big = 0;  // largest magnitude, as bf16 bits
-  #pragma unroll
+#pragma unroll
               for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-  #pragma unroll
+#pragma unroll
               for (int x = 1; x < CPR; x <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, x));
               const bool finite = big < 0x7f80u;
               const int e = finite ? scale_exp(__uint_as_float(big << 16)) : 0;
               const float inv = exp2i(-e);
               uint32_t hi[4], lo[4];
-  #pragma unroll
+#pragma unroll
               for (int i = 0; i < 4; ++i)
                 split2(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv, hi[i], lo[i]);
               const uint32_t half = (cc & 1) * 8;
@@ -830,79 +922,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(B.at(BR::Q_FULL + qb));
-      }
-    } else if (warp == 1 || warp == 16) {
-      // ------------------------------------------------------------------ MMA issuers
-      const bool is_s = warp == 1;
-      uint32_t n = 0;
-      int li = 0;
-      for (uint32_t j = 0; ok; ++j, ++li) {
-        const int slot = j % C::RING;
-        if (!wait_bar(B.at(BR::IT_FULL + slot), (j / C::RING) & 1, s_abort)) { ok = false; break; }
-        const int it = s_ring[slot].it;
-        const int rows = s_ring[slot].w.rows, ntok = s_ring[slot].w.t1 - s_ring[slot].w.t0;
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
-        if (it < 0) break;
-        const int nt = (ntok + kBT - 1) / kBT;
-        const int ncol = (rows + 7) / 8 * 16;  // the MMA's N: hi and lo of the rows rounded up to 8
-        if (is_s) {
-          // S^T(n): K(n) has landed, the item's Q is loaded, the TMEM tile has been read
-          const uint32_t idesc = ptx::idesc_e4m3_f32(kBT, ncol, false, false);
-          const int qb = li & 1;
-          if (!wait_bar(B.at(BR::Q_FULL + qb), (li >> 1) & 1, s_abort)) { ok = false; break; }
-          const uint64_t qd = sdesc<D>(sbase + C::OFF_Q + qb * C::Q_BYTES);
-          for (int t = 0; t < nt; ++t, ++n) {
-            const int st = (int)(n % C::NSK), sb = n & 1;
-            if (!wait_bar(B.at(BR::K_FULL + st), (n / C::NSK) & 1, s_abort) ||
-                !wait_bar(B.at(BR::S_EMPTY + sb), ((n >> 1) & 1) ^ 1, s_abort)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) {
-              ptx::tc_fence_after();
-              const uint64_t kd = sdesc<D>(sbase + C::OFF_K + st * C::KV_TILE);
-  #pragma unroll
-              for (int ks = 0; ks < D / 32; ++ks)  // descriptor addresses are in units of 16 bytes
-                ptx::umma_f8(tmem + sb * 128, kd + 2 * ks, qd + 2 * ks, idesc, ks > 0);
-              ptx::umma_commit(B.at(BR::S_FULL + sb));
-              ptx::umma_commit(B.at(BR::K_EMPTY + st));
-              if (t == nt - 1) ptx::umma_commit(B.at(BR::Q_EMPTY + qb));
-            }
-            __syncwarp();
-          }
-        } else {
-          // PV(n): P(n) is published, V(n) has landed, the accumulator has been read.  A = V^T, MN-major (for D = 64
-          // both halves of M read the same 64 columns: lanes 64..127 repeat lanes 0..63 and are not used)
-          const uint32_t idesc = ptx::idesc_e4m3_f32(128, ncol, true, true);
-          for (int t = 0; t < nt; ++t, ++n) {
-            const int st = (int)(n % C::NSV), b = n & 1;
-            if (!wait_bar(B.at(BR::O_EMPTY + b), ((n >> 1) & 1) ^ 1, s_abort) ||
-                !wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort) ||
-                !wait_bar(B.at(BR::P_FULL + b), (n >> 1) & 1, s_abort)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) {
-              ptx::tc_fence_after();
-              const uint64_t vd = sdesc<D>(sbase + C::OFF_V + st * C::KV_TILE);
-              const uint64_t pd = ptx::sdesc_sw128(sbase + C::OFF_P + b * C::P_BYTES, C::P_BYTES, 1024);
-  #pragma unroll
-              for (int ks = 0; ks < kBT / 32; ++ks)
-                ptx::umma_f8(tmem + 256 + b * 128, vd + ((ks * 32 * D) >> 4), pd + ((ks * 32 * 128) >> 4), idesc, ks > 0);
-              ptx::umma_commit(B.at(BR::O_FULL + b));
-              ptx::umma_commit(B.at(BR::V_EMPTY + st));
-            }
-            __syncwarp();
-          }
-        }
-      }
-      if (lane == 0) {
-        // every MMA the issuers issued must finish before the TMEM is released
-        ptx::umma_commit(B.at(BR::MMA_DONE));
-        const long long c0 = clock64();
-        while (!ptx::mbar_try_wait(B.at(BR::MMA_DONE), 0) && clock64() - c0 < kWaitCycles) {
-        }
       }
     }
   }
