@@ -42,15 +42,19 @@ namespace {
 
 constexpr int kBT = 128;            // KV tokens per tile (the M of S^T)
 constexpr int kNR = kTcRowsPerItem; // query rows per item at most
-constexpr int kThreads = 640;
-constexpr int kSoftmaxWarps = 8;
+constexpr int kThreads = 896;
+constexpr int kSoftmaxWarps = 16;
 constexpr int kQWarps = 3;
-constexpr uint32_t kTmemCols = 512; // S^T[2] at columns 0 / 128, O^T[2] at 256 / 384
+constexpr uint32_t kTmemCols = 512; // S^T[4] at columns 0, 64, 128, 192, O^T[2] (hi and lo rows) at 256 / 384
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
 constexpr uint32_t kAhead = 3;      // the item loader takes the next item when the K producer is this many tiles from
                                     // the end of what is published
-constexpr float kHead = 8.0f;       // log2 of a tile's largest P: 256, below e4m3's 448
-constexpr float kLazy = 64.0f;      // the running references follow a row's maximum when it is this far above (log2)
+constexpr float kHead = 6.0f;       // log2 of P at a row's reference
+constexpr float kUp = 2.6f;         // a tile's maximum may be this far above the reference (with its rounding: P <= 431, e4m3
+                                    // holds 448)
+constexpr float kDown = 4.0f;       // ... and this far below
+constexpr float kFar = 30.0f;       // what is this far below the largest reference so far weighs nothing
+constexpr float kLazy = 64.0f;      // the correction's running references follow a row's when it is this far above (log2)
 constexpr float kLeastScaleLog2 = -100.0f;  // a V scale of 0 weighs as 2^-100, so that its keys still count in the sums
 static_assert(kNR == 64, "TMEM and shared-memory layout assume 64 rows per item");
 
@@ -59,8 +63,8 @@ struct Cfg {
   static constexpr int KV_TILE = kBT * D;       // bytes of K (or V) of one tile
   static constexpr int Q_BYTES = 2 * kNR * D;   // hi rows, then lo rows
   static constexpr int P_BYTES = kBT * 2 * kNR; // [128 tokens][hi rows, lo rows]
-  static constexpr int NSK = D == 128 ? 4 : 8;  // K ring stages
-  static constexpr int NSV = D == 128 ? 4 : 8;  // V ring stages
+  static constexpr int NSK = D == 128 ? 3 : 6;  // K ring stages
+  static constexpr int NSV = D == 128 ? 3 : 6;  // V ring stages
   static constexpr int SC = 16;                 // slots of the scales' ring: tile n in n % SC
   static constexpr int RF = 8;                  // slots of the row factors' ring: item li in li % RF
   static constexpr int RING = 4;                // slots of the item ring
@@ -68,17 +72,17 @@ struct Cfg {
   static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
   static constexpr int OFF_V = OFF_K + NSK * KV_TILE;
   static constexpr int OFF_P = OFF_V + NSV * KV_TILE;
-  static constexpr int OFF_BAR = OFF_P + 2 * P_BYTES;
-  static constexpr int N_BAR = 2 * NSK + 2 * NSV + 18 + 2 * RING + 5;
+  static constexpr int OFF_BAR = OFF_P + 4 * P_BYTES;
+  static constexpr int N_BAR = 2 * NSK + 2 * NSV + 28 + 2 * RING + 7;
   static constexpr int OFF_SC = (OFF_BAR + N_BAR * 8 + 15) / 16 * 16;  // float2 [SC][8]: a page's K and V scale
   static constexpr int OFF_RF = OFF_SC + SC * 64;                      // float [RF][64]
-  static constexpr int OFF_RED = OFF_RF + RF * kNR * 4;                // [2 groups][2][4][32] row maxima per quadrant, bf16 pairs
-  static constexpr int OFF_MW = OFF_RED + 2 * 2 * 4 * 32 * 4;         // float [8][2][64] per warp: 8 - m, sum factors
-  static constexpr int OFF_M = OFF_MW + kSoftmaxWarps * 2 * kNR * 4;   // float [4][64] m of tile n in n % 4
-  static constexpr int OFF_CW = OFF_M + 4 * kNR * 4;                   // float [4][64] per correction warp
-  static constexpr int OFF_HL = OFF_CW + 4 * kNR * 4;                  // float [2][2][4][64] row-sum shares
-  static constexpr int OFF_LR = OFF_HL + 2 * 2 * 4 * kNR * 4;          // float [2][2][64] their references
-  static constexpr int OFF_NAN = OFF_LR + 2 * 2 * kNR * 4;             // int [2][D] first row that a NaN value reaches
+  static constexpr int OFF_RED = OFF_RF + RF * kNR * 4;                // [4 groups][2][4][8] row maxima per quadrant, bf16 pairs
+  static constexpr int OFF_MW = OFF_RED + 4 * 2 * 4 * 8 * 4;           // float [16][16] per warp: kHead - reference
+  static constexpr int OFF_M = OFF_MW + kSoftmaxWarps * 16 * 4;        // float [8][64] references of tile n in n % 8
+  static constexpr int OFF_CW = OFF_M + 8 * kNR * 4;                   // float [4][64] per correction warp
+  static constexpr int OFF_HL = OFF_CW + 4 * kNR * 4;                  // float [2][4 groups][4][16] row-sum shares
+  static constexpr int OFF_LR = OFF_HL + 2 * 4 * 4 * 16 * 4;           // float [2][4 groups][16] their references
+  static constexpr int OFF_NAN = OFF_LR + 2 * 4 * 16 * 4;              // int [2][D] first row that a NaN value reaches
   static constexpr int OFF_MISC = OFF_NAN + 2 * D * 4;
   static constexpr int OFF_RING = OFF_MISC + 32;
   static constexpr int SMEM = OFF_RING + RING * 64 + 1024;             // + slack to align the base to 1024
@@ -94,17 +98,18 @@ struct Bars {
   using C = Cfg<D>;
   uint32_t base;
   static constexpr int K_FULL = 0, K_EMPTY = C::NSK, V_FULL = 2 * C::NSK, V_EMPTY = V_FULL + C::NSV;
-  static constexpr int Q_FULL = V_EMPTY + C::NSV, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, S_EMPTY = S_FULL + 2;
-  static constexpr int P_FULL = S_EMPTY + 2;   // [2] P of tile n in buffer n & 1
-  static constexpr int O_FULL = P_FULL + 2;    // [2] PV of tile n is done: its O is complete, its P buffer free
+  static constexpr int Q_FULL = V_EMPTY + C::NSV, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, S_EMPTY = S_FULL + 4;
+  static constexpr int P_FULL = S_EMPTY + 4;   // [4] P of tile n in buffer n & 3
+  static constexpr int P_EMPTY = P_FULL + 4;   // [4] PV of tile n is done
+  static constexpr int O_FULL = P_EMPTY + 4;   // [2] ... and its O is complete
   static constexpr int O_EMPTY = O_FULL + 2;   // [2] the correction warps have read it
   static constexpr int EP_FULL = O_EMPTY + 2;  // [2] per item parity: the softmax warps handed their sums over
   static constexpr int EP_EMPTY = EP_FULL + 2; // [2] the correction warps have read them
   static constexpr int MMA_DONE = EP_EMPTY + 2;  // the two MMA issuers, at the end
   static constexpr int IT_FULL = MMA_DONE + 1, IT_EMPTY = IT_FULL + C::RING;
   static constexpr int EGRP = IT_EMPTY + C::RING;  // the correction warps
-  static constexpr int RED = EGRP + 1;         // [2] per softmax group: its four warps, once per tile
-  static constexpr int FIN = RED + 2;          // every warp, once: its last access to TMEM is done
+  static constexpr int RED = EGRP + 1;         // [4] per softmax group: its four warps, once per tile
+  static constexpr int FIN = RED + 4;          // every warp, once: its last access to TMEM is done
   static_assert(FIN + 1 <= C::N_BAR, "barrier count");
   __device__ __forceinline__ uint32_t at(int i) const { return base + 8 * i; }
 };
@@ -128,11 +133,10 @@ __device__ __forceinline__ bool item_ok(const AttnParams &p, const WorkItem &w) 
          w.row0 >= 0 && w.nrg >= 1 && w.nrg <= p.row_groups && w.rg >= 0 && w.rg < w.nrg;
 }
 
-// Transposing sum over the 32 lanes of a warp (v is consumed): on return lane i holds the sum over all
-// lanes of v[i].
-__device__ __forceinline__ float warp_transpose_sum(float (&v)[32], int lane) {
+// Transposing sum over the 32 lanes of a warp (v is consumed): lanes i and 16 + i get the sum over all lanes of v[i].
+__device__ __forceinline__ float warp_transpose_sum(float (&v)[16], int lane) {
 #pragma unroll
-  for (int w = 16; w >= 1; w >>= 1) {
+  for (int w = 8; w >= 1; w >>= 1) {
     const bool up = (lane & w) != 0;
 #pragma unroll
     for (int i = 0; i < w; ++i) {
@@ -141,7 +145,7 @@ __device__ __forceinline__ float warp_transpose_sum(float (&v)[32], int lane) {
       v[i] = keep + __shfl_xor_sync(0xffffffffu, send, w);
     }
   }
-  return v[0];
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
 }
 
 __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {  // NaN never wins
@@ -150,10 +154,10 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {  // NaN neve
   return r;
 }
 
-// Transposing maximum of bf16 pairs over the 32 lanes of a warp (v is consumed): lanes i and 16 + i get that of v[i].
-__device__ __forceinline__ uint32_t warp_transpose_max(uint32_t (&v)[16], int lane) {
+// Transposing maximum of bf16 pairs over the 32 lanes of a warp (v is consumed): lane i gets that of v[i & 7].
+__device__ __forceinline__ uint32_t warp_transpose_max(uint32_t (&v)[8], int lane) {
 #pragma unroll
-  for (int w = 8; w >= 1; w >>= 1) {
+  for (int w = 4; w >= 1; w >>= 1) {
     const bool up = (lane & w) != 0;
 #pragma unroll
     for (int i = 0; i < w; ++i) {
@@ -162,7 +166,8 @@ __device__ __forceinline__ uint32_t warp_transpose_max(uint32_t (&v)[16], int la
       v[i] = bmax2(keep, __shfl_xor_sync(0xffffffffu, send, w));
     }
   }
-  return bmax2(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
+  const uint32_t y = bmax2(v[0], __shfl_xor_sync(0xffffffffu, v[0], 8));
+  return bmax2(y, __shfl_xor_sync(0xffffffffu, y, 16));
 }
 
 __device__ __forceinline__ float lg2(float x) {
@@ -170,13 +175,22 @@ __device__ __forceinline__ float lg2(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The parts of an item's rows (rounded up to 8), one, two or four of at most 16 rows, in whole units of 8: part i starts
+// at row(i).
+struct Parts {
+  int n, units;
+  __device__ __forceinline__ explicit Parts(int nrow) : n(nrow <= 16 ? 1 : nrow <= 32 ? 2 : 4), units(nrow / 8) {}
+  __device__ __forceinline__ int row(int i) const { return i * units / n * 8; }
+};
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
-// hi and lo codes (two of each) of two values of magnitude at most 448: x = hi + lo / 16
+// hi and lo codes (two of each) of two values of magnitude at most 448: x = hi + lo, or hi + lo / 16 (S16)
+template <bool S16>
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
   hi = e4m3x2(a, b);
   const uint32_t h = e4m3x2_to_h2(hi);
-  const __half2 r = __hmul2(__hsub2(__floats2half2_rn(a, b), *reinterpret_cast<const __half2 *>(&h)), __floats2half2_rn(16.0f, 16.0f));
+  __half2 r = __hsub2(__floats2half2_rn(a, b), *reinterpret_cast<const __half2 *>(&h));
+  if (S16) r = __hmul2(r, __floats2half2_rn(16.0f, 16.0f));
   lo = e4m3x2_h(*reinterpret_cast<const uint32_t *>(&r));
 }
 
@@ -230,9 +244,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(BR::K_EMPTY, C::NSK + 2 * C::NSV, 1);
     init(BR::Q_FULL, 2, kQWarps);
     init(BR::Q_EMPTY, 2, 1);
-    init(BR::S_FULL, 2, 1);
-    init(BR::S_EMPTY, 2, 4);   // the tile's softmax group
-    init(BR::P_FULL, 2, 4);
+    init(BR::S_FULL, 4, 1);
+    init(BR::S_EMPTY, 4, 16);  // the warps of the tile's softmax groups, four, two or one arrival each
+    init(BR::P_FULL, 4, 16);
+    init(BR::P_EMPTY, 4, 1);
     init(BR::O_FULL, 2, 1);
     init(BR::O_EMPTY, 2, 4);   // the correction warps
     init(BR::EP_FULL, 2, kSoftmaxWarps);
@@ -241,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(BR::IT_FULL, C::RING, 1);
     init(BR::IT_EMPTY, C::RING, 4 + kQWarps + kSoftmaxWarps + 4);  // KV producers, MMA issuers, Q, softmax, correction
     init(BR::EGRP, 1, 4);
-    init(BR::RED, 2, 4);
+    init(BR::RED, 4, 4);       // a group's warps
     init(BR::FIN, 1, kThreads / 32);
     *s_issued = 0;
     *s_abort = 0;
@@ -279,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto div_g = [&](int row) -> int { return (int)(((unsigned)row * gm) >> 16); };
   bool ok = true;
 
-  // ------------------------------------------------------------------ MMA issuers: S^T by warp 1, PV by warp 16
+  // ------------------------------------------------------------------ MMA issuers: S^T by warp 1, PV by warp 24
   auto issue = [&](auto which) {
     constexpr bool is_s = decltype(which)::value;
     uint32_t n = 0;
@@ -293,17 +308,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
       if (it < 0) break;
       const int nt = (ntok + kBT - 1) / kBT;
-      const int ncol = (rows + 7) / 8 * 16;  // the MMA's N: hi and lo of the rows rounded up to 8
       if constexpr (is_s) {
         // S^T(n): K(n) has landed, the item's Q is loaded, the TMEM tile has been read
-        const uint32_t idesc = ptx::idesc_e4m3_f32(kBT, ncol, false, false);
+        const uint32_t idesc = ptx::idesc_e4m3_f32(kBT, (rows + 15) / 16 * 16, false, false);
         const int qb = li & 1;
         if (!wait_bar(B.at(BR::Q_FULL + qb), (li >> 1) & 1, s_abort)) { ok = false; break; }
         const uint64_t qd = sdesc<D>(sbase + C::OFF_Q + qb * C::Q_BYTES);
         for (int t = 0; t < nt; ++t, ++n) {
-          const int st = (int)(n % C::NSK), sb = n & 1;
+          const int st = (int)(n % C::NSK), sb = n & 3;
           if (!wait_bar(B.at(BR::K_FULL + st), (n / C::NSK) & 1, s_abort) ||
-              !wait_bar(B.at(BR::S_EMPTY + sb), ((n >> 1) & 1) ^ 1, s_abort)) {
+              !wait_bar(B.at(BR::S_EMPTY + sb), ((n >> 2) & 1) ^ 1, s_abort)) {
             ok = false;
             break;
           }
@@ -311,8 +325,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::tc_fence_after();
             const uint64_t kd = sdesc<D>(sbase + C::OFF_K + st * C::KV_TILE);
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)  // descriptor addresses are in units of 16 bytes
-              ptx::umma_f8(tmem + sb * 128, kd + 2 * ks, qd + 2 * ks, idesc, ks > 0);
+            for (int ks = 0; ks < D / 32; ++ks) {  // descriptor addresses are in units of 16 bytes
+              ptx::umma_f8(tmem + sb * kNR, kd + 2 * ks, qd + 2 * ks, idesc, ks > 0);
+              ptx::umma_f8(tmem + sb * kNR, kd + 2 * ks, qd + ((kNR * D) >> 4) + 2 * ks, idesc, 1);
+            }
             ptx::umma_commit(B.at(BR::S_FULL + sb));
             ptx::umma_commit(B.at(BR::K_EMPTY + st));
             if (t == nt - 1) ptx::umma_commit(B.at(BR::Q_EMPTY + qb));
@@ -322,23 +338,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         // PV(n): P(n) is published, V(n) has landed, the accumulator has been read.  A = V^T, MN-major (for D = 64
         // both halves of M read the same 64 columns: lanes 64..127 repeat lanes 0..63 and are not used)
-        const uint32_t idesc = ptx::idesc_e4m3_f32(128, ncol, true, true);
+        const uint32_t idesc = ptx::idesc_e4m3_f32(128, (rows + 7) / 8 * 16, true, true);  // N: hi and lo of the rows
         for (int t = 0; t < nt; ++t, ++n) {
-          const int st = (int)(n % C::NSV), b = n & 1;
+          const int st = (int)(n % C::NSV), b = n & 1, pb = n & 3;
           if (!wait_bar(B.at(BR::O_EMPTY + b), ((n >> 1) & 1) ^ 1, s_abort) ||
               !wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort) ||
-              !wait_bar(B.at(BR::P_FULL + b), (n >> 1) & 1, s_abort)) {
+              !wait_bar(B.at(BR::P_FULL + pb), (n >> 2) & 1, s_abort)) {
             ok = false;
             break;
           }
           if (lane == 0) {
             ptx::tc_fence_after();
             const uint64_t vd = sdesc<D>(sbase + C::OFF_V + st * C::KV_TILE);
-            const uint64_t pd = ptx::sdesc_sw128(sbase + C::OFF_P + b * C::P_BYTES, C::P_BYTES, 1024);
+            const uint64_t pd = ptx::sdesc_sw128(sbase + C::OFF_P + pb * C::P_BYTES, C::P_BYTES, 1024);
 #pragma unroll
             for (int ks = 0; ks < kBT / 32; ++ks)
               ptx::umma_f8(tmem + 256 + b * 128, vd + ((ks * 32 * D) >> 4), pd + ((ks * 32 * 128) >> 4), idesc, ks > 0);
             ptx::umma_commit(B.at(BR::O_FULL + b));
+            ptx::umma_commit(B.at(BR::P_EMPTY + pb));
             ptx::umma_commit(B.at(BR::V_EMPTY + st));
           }
           __syncwarp();
@@ -354,17 +371,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   };
 
-  // registers: 20 warps launch with 96 each, 1920 a lane in all = 8 x 144 + 4 x 112 + 4 x 48 + 4 x 32.  (Each split stands at the
+  // registers: 28 warps launch with 72 each, 2016 a lane in all = 16 x 72 + 4 x 120 + 8 x 48.  (Each split stands at the
   // head of its own branch: after a join the compiler counts with the least.)
   const int wg = warp >> 2;
-  if (wg == 1 || wg == 3) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+  if (wg >= 1 && wg <= 4) {
     // ------------------------------------------------------------------ softmax warps
+    // Four groups of four warps, a group at most 16 rows of a tile: up to 16 rows the groups take turns by tile, up to 32
+    // two pairs of groups do, a half of the rows each, and above that each group takes a quarter of the rows of every
+    // tile.  A thread holds one key's scores for the group's rows and its share of their sums.  A group's four warps
+    // agree on the rows' maxima over the tile, and from them on P's references: a row's reference follows its maximum when that
+    // leaves [-4, 2.6] around it.
     const int qd = warp & 3;                // TMEM lane quadrant: keys 32*qd .. 32*qd + 31 of a tile
-    const int grp = warp >= 12 ? 1 : 0;     // takes the tiles of this parity
+    const int grp = wg - 1;
     const uint32_t lane_addr = (uint32_t)(qd * 32) << 16;
-    float *mw = reinterpret_cast<float *>(smem + C::OFF_MW) + (grp * 4 + qd) * 2 * kNR;  // 8 - m per row, this warp's copy
-    float *bw = mw + kNR;                                                                // 2^(m - 8 - L)
+    const int l8 = lane & 7;
+    float *mw = reinterpret_cast<float *>(smem + C::OFF_MW) + (grp * 4 + qd) * 16;  // kHead - reference per row, this warp's copy
+    uint32_t *red = reinterpret_cast<uint32_t *>(smem + C::OFF_RED) + grp * 2 * 4 * 8;
     uint32_t n0 = 0;                        // tiles before the item
     uint32_t mine = 0;                      // tiles of this group so far
     int li = 0;
@@ -380,153 +402,142 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int ob = li & 1;
       const int ntiles = (t1 - t0 + kBT - 1) / kBT;
       const int nfull = (max(t0, min(t1, ctx + 1)) - t0) / kBT;  // tiles whose keys every row sees
-      const int nrow = (rows + 7) / 8 * 8, nu = nrow / 8;
-      const float *rf = s_rf + (li % C::RF) * kNR;
-      float2 lp[kNR / 2];  // this thread's (key's) share of every row sum
+      const int nrow = (rows + 7) / 8 * 8;
+      const Parts pt(nrow);
+      const int part = grp & (pt.n - 1);
+      const int r0 = pt.row(part);                   // the group's rows: r0 .. r0 + 8 nu - 1
+      const int nu = (pt.row(part + 1) - r0) / 8;
+      const uint32_t share = 4 / pt.n;               // a warp's arrivals per tile (sixteen in all)
+      const float *rf = s_rf + (li % C::RF) * kNR + r0;
+      float2 lp[8];  // this thread's (key's) share of every row sum
 #pragma unroll
-      for (int i = 0; i < kNR / 2; ++i) lp[i] = make_float2(0.0f, 0.0f);
-      float L[2] = {-INFINITY, -INFINITY};  // the sums' references, rows 2 lane and 2 lane + 1
-      for (int t = (int)((n0 ^ grp) & 1); t < ntiles; t += 2, ++mine) {
+      for (int i = 0; i < 8; ++i) lp[i] = make_float2(0.0f, 0.0f);
+      float m[2] = {-INFINITY, -INFINITY};    // the references, rows r0 + 2 l8 and the next
+      float most[2] = {-INFINITY, -INFINITY}; // the largest so far
+      float lsv0 = 0.0f;                      // log2 of V's scale at the group's first key: the sums count in its inverse
+      if (lane < 16) mw[lane] = 0.0f;         // (a row without a reference: its weights are 2^-inf)
+      __syncwarp();
+      bool fresh = true;
+      const int step = 4 / pt.n;
+      for (int t = (grp / pt.n - (int)n0) & (step - 1); t < ntiles; t += step, ++mine) {
         const uint32_t n = n0 + t;
-        if (!wait_bar(B.at(BR::S_FULL + grp), (n >> 1) & 1, s_abort)) { ok = false; break; }
+        const int buf = n & 3;
+        if (!wait_bar(B.at(BR::S_FULL + buf), (n >> 2) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
+        uint32_t v[16];
+        ptx::tmem_ld16(tmem + lane_addr + buf * kNR + r0, v);
         const float2 sc = s_sc[(n % C::SC) * 8 + qd * 2 + (lane >> 4)];
         const float lsv = fmaxf(lg2(sc.y), kLeastScaleLog2);
-        const uint32_t at = tmem + lane_addr + grp * 128;
-        // causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked
-        // too.  Only an item's last tiles (from nfull on) have such keys.
-        const int tok = t0 + t * kBT + qd * 32 + lane;
-        const int jmin = t < nfull ? 0 : tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0));
-        // First pass: the scores (log2 units, plus log2 of V's scale) from their halves, back to TMEM, and the maxima
-        // of the rows over this warp's keys as bf16 pairs: lane i gets rows 2 i and 2 i + 1.
-        uint32_t top = 0xff80ff80u;
+        if (fresh) {
+          lsv0 = fmaxf(lg2(s_sc[(n % C::SC) * 8].y), kLeastScaleLog2);
+          fresh = false;
+        }
+        ptx::tmem_wait_ld();
+        // the scores are in registers: the tile may be overwritten
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::S_EMPTY + buf), share);
+        float x[16];  // in log2 units, plus log2 of V's scale
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          if (nu > 4 * hf) {
-            uint32_t wd[16];
+        for (int i = 0; i < 16; i += 4) {
+          const float4 r4 = *reinterpret_cast<const float4 *>(rf + i);
 #pragma unroll
-            for (int c = 2 * hf; c < 2 * hf + 2; ++c) {
-              if (nu > 2 * c) {
-                uint32_t hi[16], lo[16];
-                ptx::tmem_ld16(at + 16 * c, hi);
-                ptx::tmem_ld16(at + nrow + 16 * c, lo);
-                ptx::tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                  const float4 r4 = *reinterpret_cast<const float4 *>(rf + 16 * c + i);
-#pragma unroll
-                  for (int q = 0; q < 4; q += 2) {
-                    const float2 s = __ffma2_rn(make_float2(__uint_as_float(lo[i + q]), __uint_as_float(lo[i + q + 1])), both(0.0625f),
-                                                make_float2(__uint_as_float(hi[i + q]), __uint_as_float(hi[i + q + 1])));
-                    const float2 u = __fmul2_rn(q == 0 ? make_float2(r4.x, r4.y) : make_float2(r4.z, r4.w), both(sc.x));
-                    const float2 v = __ffma2_rn(s, u, both(lsv));
-                    hi[i + q] = __float_as_uint(v.x);
-                    hi[i + q + 1] = __float_as_uint(v.y);
-                  }
-                }
-                if (t >= nfull) {
-#pragma unroll
-                  for (int i = 0; i < 16; ++i)
-                    if (16 * c + i < jmin) hi[i] = 0xff800000u;
-                }
-                ptx::tmem_st16(at + 16 * c, hi);  // (past nrow: over low halves that have been read)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) wd[8 * (c & 1) + i] = pack_bf16(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1]));
-              } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) wd[8 * (c & 1) + i] = 0xff80ff80u;
-              }
-            }
-            const uint32_t tw = warp_transpose_max(wd, lane);
-            if (lane >> 4 == hf) top = tw;
+          for (int q = 0; q < 4; q += 2) {
+            const float2 u = __fmul2_rn(q == 0 ? make_float2(r4.x, r4.y) : make_float2(r4.z, r4.w), both(sc.x));
+            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[i + q]), __uint_as_float(v[i + q + 1])), u, both(lsv));
+            x[i + q] = y.x;
+            x[i + q + 1] = y.y;
           }
         }
-        ptx::tmem_wait_st();
-        uint32_t *red = reinterpret_cast<uint32_t *>(smem + C::OFF_RED) + (grp * 2 + (mine & 1)) * 4 * 32;
-        red[qd * 32 + lane] = top;
+        // Causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked too.
+        // Only an item's last tiles (from nfull on) have such keys.
+        if (__builtin_expect(t >= nfull, 0)) {
+          const int tok = t0 + t * kBT + qd * 32 + lane;
+          const int jmin = tok >= t1 ? 16 : max(0, min(16, g * max(tok - ctx, 0) - row0 - r0));
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (i < jmin) x[i] = -INFINITY;
+        }
+        // the rows' maxima over this warp's keys as bf16 pairs (lane i & 7 gets rows 2 i and 2 i + 1), then the group's
+        uint32_t wd[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wd[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        uint32_t top = warp_transpose_max(wd, lane);
+        uint32_t *rd = red + (mine & 1) * 4 * 8;
+        if (lane < 8) rd[qd * 8 + lane] = top;
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(B.at(BR::RED + grp));
         if (!wait_bar(B.at(BR::RED + grp), mine & 1, s_abort)) { ok = false; break; }
-        // the group's maxima, rounded up: 2^-8 of their magnitude covers the rounding to bf16
-        top = bmax2(bmax2(red[lane], red[32 + lane]), bmax2(red[64 + lane], red[96 + lane]));
-        float m[2] = {__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)};
-        bool move = false;
-        float al[2], f0[2], f1[2];
+        top = bmax2(bmax2(rd[l8], rd[8 + l8]), bmax2(rd[16 + l8], rd[24 + l8]));
+        {
+          // (rounded up: 2^-8 of their magnitude covers the rounding to bf16)
+          float now[2] = {__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)};
+          bool move[2];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          if (m[y] != -INFINITY) m[y] = fmaf(fabsf(m[y]), 0x1p-8f, m[y]);
-          al[y] = 1.0f;
-          if (!(m[y] <= L[y] + kLazy)) {  // (a NaN too)
-            if (L[y] != -INFINITY) {
-              al[y] = ptx::ex2(L[y] - m[y]);
-              move = true;
-            }
-            L[y] = m[y];
+          for (int y = 0; y < 2; ++y) {
+            if (now[y] != -INFINITY) now[y] = fmaf(fabsf(now[y]), 0x1p-8f, now[y]);
+            move[y] = !(now[y] <= m[y] + kUp) || (now[y] < m[y] - kDown && now[y] > most[y] - kFar);  // (a NaN too)
           }
-          f0[y] = m[y] == -INFINITY ? 0.0f : kHead - m[y];
-          f1[y] = m[y] == -INFINITY ? 0.0f : ptx::ex2(m[y] - L[y] - kHead);
-        }
-        reinterpret_cast<float2 *>(mw)[lane] = make_float2(f0[0], f0[1]);
-        reinterpret_cast<float2 *>(bw)[lane] = make_float2(f1[0], f1[1]);
-        if (__any_sync(0xffffffffu, move)) {
+          if (__any_sync(0xffffffffu, move[0] || move[1])) {
+            float al[2];
 #pragma unroll
-          for (int i = 0; i < kNR / 2; ++i) {
-            const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
-            lp[i] = __fmul2_rn(lp[i], make_float2(a0, a1));
-          }
-        }
-        // P buffer n & 1 is free again once PV(n - 2) is done (and the maxima of tile n - 4 have been read by then)
-        if (n >= 2 && !wait_bar(B.at(BR::O_FULL + grp), ((n - 2) >> 1) & 1, s_abort)) { ok = false; break; }
-        if (qd == 0) reinterpret_cast<float2 *>(s_m + (n & 3) * kNR)[lane] = make_float2(m[0], m[1]);
-        __syncwarp();
-        // Second pass: P = 2^(s - m + 8), its shares of the sums, its two parts
-        const float2 inv2 = both(ptx::ex2(-lsv));
-        uint8_t *prow = smem + C::OFF_P + grp * C::P_BYTES + (qd * 32 + lane) * 128;
-        const int sw = lane & 7;
-#pragma unroll
-        for (int c = 0; c < kNR / 16; ++c) {
-          if (nu > 2 * c) {
-            uint32_t x[16];
-            ptx::tmem_ld16(at + 16 * c, x);
-            ptx::tmem_wait_ld();
-#pragma unroll
-            for (int u = 2 * c; u < 2 * c + 2; ++u) {
-              if (u < nu) {
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const float4 m4 = reinterpret_cast<const float4 *>(mw + 8 * u)[h], b4 = reinterpret_cast<const float4 *>(bw + 8 * u)[h];
-#pragma unroll
-                  for (int q = 0; q < 2; ++q) {
-                    const int i = 8 * u + 4 * h + 2 * q;
-                    const float2 a = __fadd2_rn(make_float2(__uint_as_float(x[i & 15]), __uint_as_float(x[(i & 15) + 1])),
-                                                q == 0 ? make_float2(m4.x, m4.y) : make_float2(m4.z, m4.w));
-                    const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
-                    lp[i >> 1] = __ffma2_rn(e, __fmul2_rn(q == 0 ? make_float2(b4.x, b4.y) : make_float2(b4.z, b4.w), inv2), lp[i >> 1]);
-                    split2(e.x, e.y, hi[2 * h + q], lo[2 * h + q]);
-                  }
-                }
-                const int oh = 8 * u, ol = nrow + 8 * u;
-                *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+            for (int y = 0; y < 2; ++y) {
+              al[y] = 1.0f;
+              if (move[y]) {
+                if (m[y] != -INFINITY) al[y] = ptx::ex2(m[y] - now[y]);
+                m[y] = now[y];
+                most[y] = !(now[y] <= most[y]) ? now[y] : most[y];
               }
             }
+            if (lane < 8)
+              reinterpret_cast<float2 *>(mw)[lane] = make_float2(m[0] == -INFINITY ? 0.0f : kHead - m[0], m[1] == -INFINITY ? 0.0f : kHead - m[1]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
+              lp[i] = __fmul2_rn(lp[i], make_float2(a0, a1));
+            }
+            __syncwarp();
           }
         }
-        // the scores have been read: the tile may be overwritten
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(B.at(BR::S_EMPTY + grp));
-        if (t >= nfull) {
+        // P buffer n & 3 is free again once PV(n - 4) is done (and the references of tile n - 8 have been read by then)
+        if (!wait_bar(B.at(BR::P_EMPTY + buf), ((n >> 2) & 1) ^ 1, s_abort)) { ok = false; break; }
+        if (qd == 0 && lane < 4 * nu) reinterpret_cast<float2 *>(s_m + (n & 7) * kNR + r0)[lane] = make_float2(m[0], m[1]);
+        // P = 2^(s - m + kHead), its shares of the sums, its two parts
+        const float2 inv2 = both(ptx::ex2(lsv0 - lsv));
+        uint8_t *prow = smem + C::OFF_P + buf * C::P_BYTES + (qd * 32 + lane) * 128;
+        const int sw = lane & 7;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (u < nu) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float4 m4 = reinterpret_cast<const float4 *>(mw + 8 * u)[h];
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                const int i = 8 * u + 4 * h + 2 * q;
+                const float2 a = __fadd2_rn(make_float2(x[i], x[i + 1]), q == 0 ? make_float2(m4.x, m4.y) : make_float2(m4.z, m4.w));
+                const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
+                lp[i >> 1] = __ffma2_rn(e, inv2, lp[i >> 1]);
+                split2<true>(e.x, e.y, hi[2 * h + q], lo[2 * h + q]);
+              }
+            }
+            const int oh = r0 + 8 * u, ol = nrow + oh;
+            *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+            *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+          }
+        }
+        if (__builtin_expect(t >= nfull && part == 0, 0)) {
           // slots past the request's tokens hold anything, and a NaN times a weight of zero is NaN: zeros in their
           // place.  A value of the new tokens that is NaN is taken out, too, and put back at the end for the rows
           // that see it.
-          const int st = (int)(n % C::NSV);
+          const int st = (int)(n % C::NSV), tok = t0 + t * kBT + qd * 32 + lane;
           if (!wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort)) { ok = false; break; }
           uint8_t *vt = smem + C::OFF_V + st * C::KV_TILE;
           const int row = qd * 32 + lane;
           uint32_t bad = 0;
           if (tok > ctx) {
+#pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
               uint4 *v = reinterpret_cast<uint4 *>(vt + swz<D>(row, c));
               if (tok >= t1) {
@@ -541,6 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (__any_sync(0xffffffffu, bad != 0)) {
             if (!wait_bar(B.at(BR::EP_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
+#pragma unroll 1
             for (int i = 0; i < D; ++i) {
               if (bad & (1u << (i >> 4))) {
                 uint8_t *v = vt + swz<D>(row, i >> 4) + (i & 15);
@@ -556,29 +568,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         // P(n) is published
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(B.at(BR::P_FULL + grp));
+        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::P_FULL + buf), share);
       }
       if (!ok) break;
       n0 += ntiles;
       // ---- hand the sums over to the correction warps, which must be done with those of item li - 2
-      float ls[2][32];
+      float ls[16];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        ls[0][i] = i & 1 ? lp[i >> 1].y : lp[i >> 1].x;
-        ls[1][i] = i & 1 ? lp[16 + (i >> 1)].y : lp[16 + (i >> 1)].x;
-      }
-      const float sh0 = warp_transpose_sum(ls[0], lane);
-      const float sh1 = nu > 4 ? warp_transpose_sum(ls[1], lane) : 0.0f;
+      for (int i = 0; i < 16; ++i) ls[i] = i & 1 ? lp[i >> 1].y : lp[i >> 1].x;
+      const float sum = warp_transpose_sum(ls, lane);
       if (!wait_bar(B.at(BR::EP_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
-      float *hl = s_hl + ((ob * 2 + grp) * 4 + qd) * kNR;
-      hl[lane] = sh0;
-      hl[32 + lane] = sh1;
-      if (qd == 0) reinterpret_cast<float2 *>(s_lr + (ob * 2 + grp) * kNR)[lane] = make_float2(L[0], L[1]);
+      if (lane < 16) s_hl[((ob * 4 + grp) * 4 + qd) * 16 + lane] = sum;
+      if (qd == 0 && lane < 8)
+        reinterpret_cast<float2 *>(s_lr + (ob * 4 + grp) * 16)[lane] = make_float2(m[0] - lsv0 - kHead, m[1] - lsv0 - kHead);
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_FULL + ob));
     }
-  } else if (wg == 2) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+  } else if (wg == 5) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
     // ------------------------------------------------------------------ correction warps
     // Thread d (lane d of O^T) keeps head-dim index d of every row: acc += (hi + lo / 16) 2^(m - M - 8) per tile, M a
     // row's reference, which follows its maximum when that is 2^64 above.
@@ -614,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait_bar(B.at(BR::O_FULL + b), (n >> 1) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
         bool move = false;
-        const float2 m2 = reinterpret_cast<const float2 *>(s_m + (n & 3) * kNR)[lane];
+        const float2 m2 = reinterpret_cast<const float2 *>(s_m + (n & 7) * kNR)[lane];
         const float m[2] = {m2.x, m2.y};
         float al[2], f[2];
 #pragma unroll
@@ -630,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           f[x] = m[x] == -INFINITY ? 0.0f : ptx::ex2(m[x] - M[x] - kHead);
         }
         reinterpret_cast<float2 *>(cw)[lane] = make_float2(f[0], f[1]);
-        if (__any_sync(0xffffffffu, move)) {
+        if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
 #pragma unroll
           for (int i = 0; i < kNR / 2; ++i) {
             const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
@@ -638,19 +645,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         __syncwarp();
+        const uint32_t at = tmem + lane_addr + 256 + b * 128;
 #pragma unroll
         for (int c = 0; c < kNR / 8; ++c) {
           if (8 * c < nrow) {
             uint32_t hi[8], lo[8];
-            ptx::tmem_ld8(tmem + lane_addr + 256 + b * 128 + 8 * c, hi);
-            ptx::tmem_ld8(tmem + lane_addr + 256 + b * 128 + nrow + 8 * c, lo);
+            ptx::tmem_ld8(at + 8 * c, hi);
+            ptx::tmem_ld8(at + nrow + 8 * c, lo);
             ptx::tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 fr = *reinterpret_cast<const float2 *>(cw + 8 * c + 2 * i);
-              const float2 o = __ffma2_rn(make_float2(__uint_as_float(lo[2 * i]), __uint_as_float(lo[2 * i + 1])), both(0.0625f),
-                                          make_float2(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1])));
-              acc[4 * c + i] = __ffma2_rn(o, fr, acc[4 * c + i]);
+            for (int i = 0; i < 8; i += 4) {
+              const float4 f4 = *reinterpret_cast<const float4 *>(cw + 8 * c + i);
+#pragma unroll
+              for (int q = 0; q < 4; q += 2) {
+                const float2 o = __ffma2_rn(make_float2(__uint_as_float(lo[i + q]), __uint_as_float(lo[i + q + 1])), both(0.0625f),
+                                            make_float2(__uint_as_float(hi[i + q]), __uint_as_float(hi[i + q + 1])));
+                acc[4 * c + (i + q) / 2] = __ffma2_rn(o, q == 0 ? make_float2(f4.x, f4.y) : make_float2(f4.z, f4.w), acc[4 * c + (i + q) / 2]);
+              }
             }
           }
         }
@@ -659,19 +670,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(B.at(BR::O_EMPTY + b));
       }
       if (!ok || !wait_bar(B.at(BR::EP_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
-      // the row sums: eight shares, four against each group's references.  The group that had the item's first tile
-      // comes first, so that results repeat to the bit whatever the CTA did before.
-      const uint32_t first = (n - ntiles) & 1;
+      // the row sums: four shares of each group that had the row, against its references.  The group that had the
+      // item's first tile comes first, so that results repeat to the bit whatever the CTA did before.
       const int nan0 = dval ? s_nan[ob * D + d] : INT32_MAX;
       if (dval) s_nan[ob * D + d] = INT32_MAX;
       float l[2] = {0.0f, 0.0f};
+      {
+        const Parts pt(nrow);
+        int part = 0;  // of rows 2 lane and 2 lane + 1
+        for (int i = 1; i < pt.n; ++i) part += 2 * lane >= pt.row(i);
+        const int at = (2 * lane - pt.row(part)) / 2 & 7, turns = 4 / pt.n, first = (int)(n - ntiles);
 #pragma unroll
-      for (int gr = 0; gr < 2; ++gr) {
-        const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 2 + (gr ^ first)) * 4 * kNR) + lane;
-        const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 2 + (gr ^ first)) * kNR)[lane];
-        const float2 h0 = hl[0], h1 = hl[kNR / 2], h2 = hl[kNR], h3 = hl[3 * kNR / 2];
-        if (lr.x != -INFINITY) l[0] = fmaf((h0.x + h1.x) + (h2.x + h3.x), ptx::ex2(lr.x - M[0]), l[0]);
-        if (lr.y != -INFINITY) l[1] = fmaf((h0.y + h1.y) + (h2.y + h3.y), ptx::ex2(lr.y - M[1]), l[1]);
+        for (int i = 0; i < 4; ++i) {
+          if (i >= turns) break;
+          const int gr = ((first + i) & (turns - 1)) * pt.n + part;
+          const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 4 + gr) * 4 * 16) + at;
+          const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 4 + gr) * 16)[at];
+          const float2 h0 = hl[0], h1 = hl[8], h2 = hl[16], h3 = hl[24];
+          if (lr.x != -INFINITY) l[0] = fmaf((h0.x + h1.x) + (h2.x + h3.x), ptx::ex2(lr.x - M[0]), l[0]);
+          if (lr.y != -INFINITY) l[1] = fmaf((h0.y + h1.y) + (h2.y + h3.y), ptx::ex2(lr.y - M[1]), l[1]);
+        }
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
@@ -721,7 +739,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ---- the last chunk of this (request, head, row group) to finish merges all ----
         __threadfence();
         if (!group_sync()) { ok = false; break; }
-        if (warp == 8 && lane == 0) {
+        if (qd == 0 && lane == 0) {
           const int chunks = p.req_chunks[w.r];
           const int done = atomicAdd(p.pair_done + ((int64_t)w.r * p.Hkv + w.h) * p.row_groups + w.rg, 1);
           *s_last = done == chunks - 1 ? chunks : 0;
@@ -858,12 +876,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       issue(std::true_type());
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-    if (warp == 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 24) {
       issue(std::false_type());
     } else {
       // ------------------------------------------------------------------ Q loaders
-      // Query row row0 + rho = j * g + hh at MMA row rho (hi) and nrow + rho (lo), rows past the item zero.  A row's
+      // Query row row0 + rho = j * g + hh at MMA row rho (hi) and 64 + rho (lo), rows past the item up to the MMA's N zero.  A row's
       // factor 2^e / sqrt(D) in log2 units goes to s_rf.
       const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
       constexpr int CPR = D / 8;     // 16-byte chunks per row, a lane each
@@ -879,12 +897,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
         if (it < 0) break;
-        const int qb = li & 1, nrow = (rows + 7) / 8 * 8;
+        const int qb = li & 1, nrow = (rows + 15) / 16 * 16;
         if (!wait_bar(B.at(BR::Q_EMPTY + qb), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
         const uint16_t *qi = static_cast<const uint16_t *>(p.q) + ((int64_t)q0 * p.Hq + h * g) * D + cc * 8;
         uint8_t *qs = smem + C::OFF_Q + qb * C::Q_BYTES;
         float *rf = s_rf + (li % C::RF) * kNR;
-        for (int base = (warp - 17) * RPP; base < nrow; base += kQWarps * RPP * QB) {
+        for (int base = (warp - 25) * RPP; base < nrow; base += kQWarps * RPP * QB) {
           uint4 v[QB];
 #pragma unroll
           for (int u = 0; u < QB; ++u) {
@@ -911,10 +929,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t hi[4], lo[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                split2(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv, hi[i], lo[i]);
+                split2<false>(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv, hi[i], lo[i]);
               const uint32_t half = (cc & 1) * 8;
               *reinterpret_cast<uint2 *>(qs + swz<D>(row, cc >> 1) + half) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-              *reinterpret_cast<uint2 *>(qs + swz<D>(nrow + row, cc >> 1) + half) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+              *reinterpret_cast<uint2 *>(qs + swz<D>(kNR + row, cc >> 1) + half) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
               if (cc == 0) rf[row] = finite ? exp2i(e) * scale_log2 : NAN;
             }
           }
