@@ -404,10 +404,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int nfull = (max(t0, min(t1, ctx + 1)) - t0) / kBT;  // tiles whose keys every row sees
       const int nrow = (rows + 7) / 8 * 8;
       const Parts pt(nrow);
-      const int part = grp & (pt.n - 1);
+      // A group's tiles are those of its number modulo the turns, whatever the number of parts: so it has at least one of
+      // any four tiles, and the phase of a barrier that it waits for is never two ahead of what it has seen.
+      const int turns = 4 / pt.n, part = grp / turns;
       const int r0 = pt.row(part);                   // the group's rows: r0 .. r0 + 8 nu - 1
       const int nu = (pt.row(part + 1) - r0) / 8;
-      const uint32_t share = 4 / pt.n;               // a warp's arrivals per tile (sixteen in all)
+      const uint32_t share = turns;                  // a warp's arrivals per tile (sixteen in all)
       const float *rf = s_rf + (li % C::RF) * kNR + r0;
       float2 lp[8];  // this thread's (key's) share of every row sum
 #pragma unroll
@@ -418,8 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane < 16) mw[lane] = 0.0f;         // (a row without a reference: its weights are 2^-inf)
       __syncwarp();
       bool fresh = true;
-      const int step = 4 / pt.n;
-      for (int t = (grp / pt.n - (int)n0) & (step - 1); t < ntiles; t += step, ++mine) {
+      for (int t = (grp - (int)n0) & (turns - 1); t < ntiles; t += turns, ++mine) {
         const uint32_t n = n0 + t;
         const int buf = n & 3;
         if (!wait_bar(B.at(BR::S_FULL + buf), (n >> 2) & 1, s_abort)) { ok = false; break; }
@@ -532,7 +533,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           // place.  A value of the new tokens that is NaN is taken out, too, and put back at the end for the rows
           // that see it.
           const int st = (int)(n % C::NSV), tok = t0 + t * kBT + qd * 32 + lane;
-          if (!wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort)) { ok = false; break; }
+          // (first the stage's tile before, PV(n - NSV), then V(n): in one step the wait could pass on the phase before)
+          if (!wait_bar(B.at(BR::V_EMPTY + st), ((n / C::NSV) & 1) ^ 1, s_abort) ||
+              !wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort)) {
+            ok = false;
+            break;
+          }
           uint8_t *vt = smem + C::OFF_V + st * C::KV_TILE;
           const int row = qd * 32 + lane;
           uint32_t bad = 0;
@@ -683,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (i >= turns) break;
-          const int gr = ((first + i) & (turns - 1)) * pt.n + part;
+          const int gr = part * turns + ((first + i) & (turns - 1));
           const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 4 + gr) * 4 * 16) + at;
           const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 4 + gr) * 16)[at];
           const float2 h0 = hl[0], h1 = hl[8], h2 = hl[16], h3 = hl[24];

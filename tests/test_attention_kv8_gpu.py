@@ -142,6 +142,18 @@ def test_pages_in_order_and_a_batch():
     c.check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_items_of_mixed_row_counts(D):
+    # several items per SM, of 4 to 64 query rows and one to a few dozen tiles, in one order after the other
+    rng = np.random.default_rng(D)
+    c = Case(40 + D, k=rng.integers(0, 16, 96), ctx=np.where(rng.random(96) < 0.5, rng.integers(0, 300, 96), rng.integers(0, 5000, 96)), D=D)
+    c.run()
+    c.check()
+    a = c.t["out"].clone()
+    c.run()
+    assert torch.equal(a, c.t["out"])
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "one_late", "one_early"])
 def test_scores_far_apart(order):
     # keys whose scores rise or fall by hundreds along the sequence, or one key that takes nearly all
