@@ -1,8 +1,15 @@
 // logprobs.cu -- log probabilities of given tokens with the rows' entropies and top alternatives
 // (include/wisp_logprobs.h), and the tokens that a verified batch committed.
 //
-// With m = max z, s = sum exp(z - m) and w = sum exp(z - m) (z - m): log p(y) = z_y - m - log s and
-// entropy = log s - w / s.
+// One pass over a row, which a cluster of one to eight CTAs shares (rows are few when a server answers a step, and one
+// CTA alone would take a row's length at its own rate).  A thread keeps a reference r near the largest logit it has seen and
+// sums s = sum exp(z - r) and w = sum exp(z - r) (z - r) in fp32; the reference moves only when a logit is kLazy above it,
+// and pairs (r, s, w) join over threads, warps and CTAs:
+//   to a reference m >= r:  s' = s f,  w' = (w + s (r - m)) f,  f = exp(r - m);   log p(y) = z_y - m - log s,
+//   entropy = log s - w / s.
+// Alternatives are 64-bit keys, the logit's bits in an order-preserving form above the inverted id, so that a larger key is a
+// better token and ties need no care.  Warps collect the keys above a threshold that n keys of the CTA are known to reach,
+// and cut their lists to the best n whenever these fill; the first threshold is the n-th largest of a warp's 32 lane maxima.
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 #include "wisp_logprobs.h"
@@ -14,12 +21,19 @@ namespace wisp {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kVecs = 4;             // 16-byte loads in flight per thread
 constexpr int kMaxTop = 32;
+constexpr int kList = 32 + 8 * 32;   // a warp's keys: the best so far and one load of every lane
+constexpr int kCutAt = 96;           // lists longer than this are cut at the next opportunity
+constexpr int kMaxCluster = 8;
+constexpr float kLazy = 20.0f;       // a logit this far above the reference moves it
+constexpr float kLeast = -200.0f;    // exp of it and of anything below is 0
 constexpr int kTokThreads = 1024;
 
 struct LogprobParams {
-  int rows, V, top_n;
+  int rows, V, top_n, cluster;
   int64_t stride;
   const void *logits;
   const int32_t *tokens;
@@ -44,20 +58,212 @@ __device__ __forceinline__ float logit_of(uint64_t key) {
 }
 
 __global__ void status_clear_kernel(DeviceStatus *st) {
+  // the row kernel may start: it reports errors only after this grid is done
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   st->code = 0;
   st->pad = 0;
   st->request_id = 0;
 }
+__device__ __forceinline__ void report_row(DeviceStatus *st, int code, int row) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  report(st, code, nullptr, row);
+}
 
-// One CTA per row: the maximum, then the sums, then the alternatives one by one.
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {  // of bf16 pairs
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// A thread's share of a row, then a warp's, a CTA's.
+struct Stat {
+  float r, s, w;
+};
+// `a` and `b` against the larger of their references.  (A reference of -inf: nothing so far.)
+__device__ __forceinline__ Stat join(Stat a, Stat b) {
+  const float m = max_nan(a.r, b.r);
+  const float da = a.r - m, db = b.r - m;
+  const float fa = a.r == -INFINITY ? 0.0f : ex2_approx(da * kLog2e), fb = b.r == -INFINITY ? 0.0f : ex2_approx(db * kLog2e);
+  Stat c;
+  c.r = m;
+  c.s = a.s * fa + b.s * fb;
+  c.w = (fa == 0.0f ? 0.0f : (a.w + a.s * da) * fa) + (fb == 0.0f ? 0.0f : (b.w + b.s * db) * fb);
+  return c;
+}
+
+// Elements of a 16-byte load: 8 bf16 or 4 fp32.
 template <typename T>
+struct Vec {
+  static constexpr int E = sizeof(T) == 2 ? 8 : 4;
+  uint4 v;
+  __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+  __device__ __forceinline__ float at(int i) const {
+    if (E == 4) return __uint_as_float(word(i));
+    return __uint_as_float(i & 1 ? word(i >> 1) & 0xffff0000u : word(i >> 1) << 16);
+  }
+  __device__ __forceinline__ void clear() {  // -inf throughout
+    const uint32_t x = E == 4 ? 0xff800000u : 0xff80ff80u;
+    v = make_uint4(x, x, x, x);
+  }
+};
+template <typename T>
+__device__ __forceinline__ float max_of(const Vec<T> (&x)[kVecs]) {
+  if (Vec<T>::E == 8) {
+    uint32_t m = x[0].v.x;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = max_nan2(m, x[u].word(i));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  float m = x[0].at(0);
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max_nan(m, x[u].at(i));
+  return m;
+}
+
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int m) { return __shfl_xor_sync(0xffffffffu, v, m); }
+// The 32 lanes' keys in falling order (lane 0 gets the largest): bitonic sort.
+__device__ __forceinline__ uint64_t warp_sort(uint64_t k, int lane) {
+#pragma unroll 1
+  for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll 1
+    for (int d = size >> 1; d > 0; d >>= 1) {
+      const uint64_t o = shfl_xor64(k, d);
+      const bool keep_max = ((lane & d) == 0) == ((lane & size) == 0);
+      k = keep_max ? max(k, o) : min(k, o);
+    }
+  }
+  return k;
+}
+// The 32 largest of two sorted sets of 32, sorted.
+__device__ __forceinline__ uint64_t warp_merge(uint64_t a, uint64_t b, int lane) {
+  uint64_t k = max(a, __shfl_sync(0xffffffffu, b, 31 - lane));
+#pragma unroll 1
+  for (int d = 16; d > 0; d >>= 1) {
+    const uint64_t o = shfl_xor64(k, d);
+    k = (lane & d) == 0 ? max(k, o) : min(k, o);
+  }
+  return k;
+}
+
+// A warp's list of candidate keys.
+struct List {
+  uint64_t *keys;  // [kList]
+  int count;
+  int top_n;
+  // the best min(count, 32) keys, sorted, one per lane (0: none)
+  __device__ uint64_t best(int lane) const {
+    uint64_t k = 0;
+    for (int at = 0; at < count; at += 32) k = warp_merge(k, warp_sort(at + lane < count ? keys[at + lane] : 0, lane), lane);
+    return k;
+  }
+  // cut to the best top_n; *threshold rises to the last of them
+  __device__ void cut(int lane, unsigned long long *threshold) {
+    __syncwarp();
+    const uint64_t k = best(lane);
+    __syncwarp();
+    if (lane < top_n) keys[lane] = k;
+    count = min(count, top_n);
+    const uint64_t last = __shfl_sync(0xffffffffu, k, top_n - 1);
+    if (lane == 0 && last > *threshold) atomicMax(threshold, (unsigned long long)last);
+    __syncwarp();
+  }
+};
+
+// The keys of a thread's loads above the threshold, into the warp's list.  id0(u): id of load u's first element.
+template <typename T, typename Id>
+__device__ __noinline__ void collect(const Vec<T> (&x)[kVecs], Id id0, List &list, unsigned long long *threshold, int lane) {
+  constexpr int E = Vec<T>::E;
+  uint64_t thr = *(volatile unsigned long long *)threshold;
+  auto key = [&](int u, int i) -> uint64_t {
+    const float z = x[u].at(i);
+    return z > -INFINITY ? key_of(z, id0(u) + i) : 0;
+  };
+  // many at once (the first loads, or logits that rise along the row): the threshold rises to the top_n-th of the
+  // lanes' largest first
+  uint64_t mine = 0;
+  int n = 0;
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const uint64_t k = key(u, i);
+      mine = max(mine, k);
+      n += k > thr;
+    }
+  if (__reduce_add_sync(0xffffffffu, n) > 64) {
+    const uint64_t t = __shfl_sync(0xffffffffu, warp_sort(mine, lane), list.top_n - 1);
+    if (t > thr) {
+      thr = t - 1;  // (that key itself is to be kept)
+      if (lane == 0) atomicMax(threshold, (unsigned long long)thr);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    for (;;) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) c += key(u, i) > thr;
+      int before = c;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, before, d);
+        if (lane >= d) before += o;
+      }
+      const int total = __shfl_sync(0xffffffffu, before, 31);
+      if (total == 0) break;
+      if (list.count + total > kList) {
+        list.cut(lane, threshold);
+        thr = max(thr, (uint64_t)*(volatile unsigned long long *)threshold);
+        continue;
+      }
+      int at = list.count + before - c;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const uint64_t k = key(u, i);
+        if (k > thr) list.keys[at++] = k;
+      }
+      list.count += total;
+      break;
+    }
+  }
+  if (list.count > kCutAt) list.cut(lane, threshold);
+}
+
+struct Shared {
+  Stat stat[kWarps];
+  uint64_t best[kMaxCluster][kMaxTop];  // the first CTA's: the CTAs' alternatives
+  Stat part[kMaxCluster];               // the first CTA's: the CTAs' sums
+  unsigned long long threshold;
+};
+
+// The address of the same shared-memory object in the cluster's CTA `rank`.
+template <typename P>
+__device__ __forceinline__ uint32_t remote(P *p, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(ptx::smem_u32(p)), "r"(rank));
+  return r;
+}
+
+// A cluster per row.
+template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p) {
-  __shared__ float s_f[2][kThreads / 32];
-  __shared__ uint64_t s_k[kThreads / 32];
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int E = Vec<T>::E;
+  __shared__ Shared sh;
+  __shared__ uint64_t s_list[TOP ? kWarps * kList : 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int csize = p.cluster, row = blockIdx.x / csize, rank = blockIdx.x % csize;
   const int tok = p.tokens[row];
   const T *z = static_cast<const T *>(p.logits) + (int64_t)row * p.stride;
   auto write_all = [&](float v, int id) {
+    if (rank != 0) return;
     if (tid == 0) {
       p.logprob[row] = v;
       if (p.entropy) p.entropy[row] = v;
@@ -67,69 +273,174 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
       p.top_logprobs[(int64_t)row * p.top_n + tid] = v;
     }
   };
-  if (tok < 0) return write_all(0.0f, -1);
+  if (tok < 0) return write_all(0.0f, -1);  // (the same for the whole cluster)
   if (tok >= p.V) {
-    if (tid == 0) report(p.status, WISP_DEV_BAD_TOKEN, nullptr, row);
+    if (tid == 0 && rank == 0) report_row(p.status, WISP_DEV_BAD_TOKEN, row);
     return write_all(NAN, -1);
   }
-  float m = -INFINITY;
-  bool bad = false;
-  for (int i = tid; i < p.V; i += kThreads) {
-    const float v = element(z, i);
-    bad |= !(v < INFINITY);
-    m = fmaxf(m, v);
+  const float zt = rank == 0 && tid == 0 ? element(z, tok) : 0.0f;
+
+  // the row's aligned loads [0, nvec), `head` elements before them and `tail` after
+  const int head = min(p.V, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T));
+  const int nvec = (p.V - head) / E, tail = p.V - head - nvec * E;
+  const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
+  const int per = (nvec + csize - 1) / csize;
+  const int v0 = min(nvec, rank * per), v1 = min(nvec, v0 + per);
+
+  Stat st = {-INFINITY, 0.0f, 0.0f};
+  float2 s2 = make_float2(0.0f, 0.0f), w2 = s2;
+  List list;
+  list.keys = s_list + (TOP ? warp * kList : 0);
+  list.count = 0;
+  list.top_n = p.top_n;
+  if (TOP && tid == 0) sh.threshold = 0;
+  if (TOP) __syncthreads();
+  float thr = -INFINITY;  // the threshold's logit
+
+  auto take = [&](const Vec<T> (&x)[kVecs], auto id0) {
+    const float cm = max_of<T>(x);
+    if (cm != -INFINITY) {
+      if (!(cm <= st.r + kLazy)) {  // (a NaN too: it stays)
+        if (st.r == -INFINITY) {
+          st.r = cm;
+        } else {
+          const float d = st.r - cm, f = ex2_approx(d * kLog2e);
+          // (f = 0: d may be past what a product holds)
+          w2 = f == 0.0f ? make_float2(0.0f, 0.0f) : make_float2((w2.x + s2.x * d) * f, (w2.y + s2.y * d) * f);
+          s2 = make_float2(s2.x * f, s2.y * f);
+          st.r = cm;
+        }
+      }
+      const float2 mr = make_float2(-st.r, -st.r), l2e = make_float2(kLog2e, kLog2e);
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) {
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+          float2 d = __fadd2_rn(make_float2(x[u].at(i), x[u].at(i + 1)), mr);
+          d = make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast));
+          const float2 t = __fmul2_rn(d, l2e);
+          const float2 e = make_float2(ex2_approx(t.x), ex2_approx(t.y));
+          s2 = __fadd2_rn(s2, e);
+          w2 = __ffma2_rn(e, d, w2);
+        }
+      }
+    }
+    if (cm != cm) s2.x = NAN;
+    if (TOP) {
+      if (__any_sync(0xffffffffu, cm >= thr && cm != -INFINITY)) {
+        collect<T>(x, id0, list, &sh.threshold, lane);
+        const uint64_t t = *(volatile unsigned long long *)&sh.threshold;
+        thr = t ? logit_of(t) : -INFINITY;
+      }
+    }
+  };
+
+  Vec<T> cur[kVecs], nxt[kVecs];
+  auto load = [&](int base, Vec<T> (&x)[kVecs]) {
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+      const int i = base + u * kThreads + tid;
+      if (i < v1)
+        x[u].v = __ldg(zv + i);
+      else
+        x[u].clear();
+    }
+  };
+  if (v0 < v1) load(v0, cur);
+  for (int base = v0; base < v1; base += kThreads * kVecs) {
+    if (base + kThreads * kVecs < v1) load(base + kThreads * kVecs, nxt);
+    take(cur, [&](int u) { return head + (base + u * kThreads + tid) * E; });
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) cur[u] = nxt[u];
   }
-  m = ptx::warp_max(m);
-  if (lane == 0) s_f[0][warp] = m;
-  bad = __syncthreads_or(bad);
-  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, s_f[0][w]);
-  if (bad || m == -INFINITY) {
-    if (tid == 0) report(p.status, WISP_DEV_BAD_PROB, nullptr, row);
-    return write_all(NAN, -1);
+  if (rank == 0 && warp == 0 && head + tail > 0) {  // the elements around the aligned loads, one per lane
+    const int id = lane < head ? lane : head + nvec * E + lane - head;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) cur[u].clear();
+    if (lane < head + tail) {
+      const float v = element(z, id);
+      if (E == 4)
+        cur[0].v.x = __float_as_uint(v);
+      else
+        cur[0].v.x = (cur[0].v.x & 0xffff0000u) | __float_as_uint(v) >> 16;
+    }
+    take(cur, [&](int u) { return id + u; });
   }
-  __syncthreads();
-  float s = 0.0f, a = 0.0f;
-  for (int i = tid; i < p.V; i += kThreads) {
-    const float d = element(z, i) - m, e = expf(d);
-    s += e;
-    if (d > -INFINITY) a += e * d;
-  }
+
+  st.s = s2.x + s2.y;
+  st.w = w2.x + w2.y;
+#pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, o);
-    a += __shfl_xor_sync(0xffffffffu, a, o);
+    Stat b;
+    b.r = __shfl_xor_sync(0xffffffffu, st.r, o);
+    b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
+    b.w = __shfl_xor_sync(0xffffffffu, st.w, o);
+    st = join(st, b);
   }
-  if (lane == 0) {
-    s_f[0][warp] = s;
-    s_f[1][warp] = a;
+  if (lane == 0) sh.stat[warp] = st;
+  uint64_t best = 0;
+  if (TOP) {
+    best = list.best(lane);
+    __syncwarp();
+    list.keys[lane] = best;
   }
   __syncthreads();
-  s = a = 0.0f;
-  for (int w = 0; w < kThreads / 32; ++w) {
-    s += s_f[0][w];
-    a += s_f[1][w];
-  }
-  const float ls = logf(s);
-  if (tid == 0) {
-    p.logprob[row] = element(z, tok) - m - ls;
-    if (p.entropy) p.entropy[row] = ls - a / s;
-  }
-  uint64_t last = ~0ull;
-  for (int t = 0; t < p.top_n; ++t) {
-    uint64_t best = 0;
-    for (int i = tid; i < p.V; i += kThreads) {
-      const uint64_t k = key_of(element(z, i), i);
-      if (k < last && k > best) best = k;
+  if (warp == 0) {
+    st = sh.stat[0];
+    for (int w = 1; w < kWarps; ++w) st = join(st, sh.stat[w]);
+    if (TOP)
+      for (int w = 1; w < kWarps; ++w) best = warp_merge(best, s_list[w * kList + lane], lane);
+    if (csize > 1) {  // to the first CTA
+      if (TOP) {
+        const uint32_t at = remote(&sh.best[rank][lane], 0);
+        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(at), "l"(best) : "memory");
+      }
+      if (lane == 0) {
+        const uint32_t at = remote(&sh.part[rank], 0);
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(st.r) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(st.s) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(st.w) : "memory");
+      }
     }
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (lane == 0) s_k[warp] = best;
-    __syncthreads();
-    for (int w = 0; w < kThreads / 32; ++w) best = max(best, s_k[w]);
-    __syncthreads();
-    if (tid == 0) {
-      p.top_tokens[(int64_t)row * p.top_n + t] = best ? id_of(best) : -1;
-      p.top_logprobs[(int64_t)row * p.top_n + t] = best ? logit_of(best) - m - ls : -INFINITY;
+  }
+  if (csize > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  if (rank != 0 || warp != 0) return;
+  for (int c = 1; c < csize; ++c) {
+    st = join(st, sh.part[c]);
+    if (TOP) best = warp_merge(best, sh.best[c][lane], lane);
+  }
+  const bool bad = !(st.r > -INFINITY && st.r < INFINITY && st.s > 0.0f && st.s < INFINITY);
+  if (bad) {
+    if (lane == 0) report_row(p.status, WISP_DEV_BAD_PROB, row);
+    return write_all(NAN, -1);
+  }
+  const float ls = logf(st.s);
+  if (lane == 0) {
+    p.logprob[row] = zt - st.r - ls;
+    if (p.entropy) p.entropy[row] = ls - st.w / st.s;
+  }
+  if (TOP) {
+    // fewer than top_n logits above -inf: tokens at -inf follow, by their ids; among the first 64 there are enough
+    const unsigned have = __ballot_sync(0xffffffffu, best != 0);
+    int id = best ? id_of(best) : -1;
+    float lp = best ? logit_of(best) - st.r - ls : -INFINITY;
+    const int n = __popc(have);
+    if (n < p.top_n) {
+      int found = n;
+      for (int i = 0; i < min(p.V, 2 * kMaxTop) && found < p.top_n; ++i) {
+        if (element(z, i) == -INFINITY) {
+          if (lane == found) id = i;
+          ++found;
+        }
+      }
     }
-    last = best;
+    if (lane < p.top_n) {
+      p.top_tokens[(int64_t)row * p.top_n + lane] = id;
+      p.top_logprobs[(int64_t)row * p.top_n + lane] = lp;
+    }
   }
 }
 
@@ -213,13 +524,30 @@ wisp_status wisp_verify_logprobs(const wisp_logprobs_args *a, void *ws, size_t w
   p.top_logprobs = a->top_logprobs;
   p.status = static_cast<DeviceStatus *>(ws);
   status_clear_kernel<<<1, 1, 0, s>>>(p.status);
-  if (a->rows > 0) {
-    if (a->logits_dtype == WISP_BF16)
-      logprobs_kernel<uint16_t><<<a->rows, kThreads, 0, s>>>(p);
-    else
-      logprobs_kernel<float><<<a->rows, kThreads, 0, s>>>(p);
-  }
-  return cudaGetLastError() == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+  if (cudaGetLastError() != cudaSuccess) return WISP_ERR_CUDA;
+  if (a->rows == 0) return WISP_OK;
+  const bool bf = a->logits_dtype == WISP_BF16, top = a->top_n > 0;
+  // CTAs per row: about four per SM in all, as long as each has a whole round of its threads' loads
+  const int64_t rounds = ((int64_t)a->V * (bf ? 2 : 4) / 16 + kThreads * kVecs - 1) / (kThreads * kVecs);
+  p.cluster = 1;
+  while (p.cluster < kMaxCluster && 2 * p.cluster <= rounds && (int64_t)a->rows * p.cluster < 4 * 152) p.cluster *= 2;
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof cfg);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  if ((int64_t)a->rows * p.cluster > INT32_MAX) return WISP_ERR_UNSUPPORTED;
+  cfg.gridDim = dim3((unsigned)(a->rows * p.cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = bf ? (top ? cudaLaunchKernelEx(&cfg, logprobs_kernel<uint16_t, true>, p) : cudaLaunchKernelEx(&cfg, logprobs_kernel<uint16_t, false>, p))
+                           : (top ? cudaLaunchKernelEx(&cfg, logprobs_kernel<float, true>, p) : cudaLaunchKernelEx(&cfg, logprobs_kernel<float, false>, p));
+  return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 
 wisp_status wisp_verify_committed_tokens(const wisp_accept_args *c, int32_t *row_tokens, void *stream) {
