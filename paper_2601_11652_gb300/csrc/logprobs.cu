@@ -7,9 +7,11 @@
 // and pairs (r, s, w) join over threads, warps and CTAs:
 //   to a reference m >= r:  s' = s f,  w' = (w + s (r - m)) f,  f = exp(r - m);   log p(y) = z_y - m - log s,
 //   entropy = log s - w / s.
-// Alternatives are 64-bit keys, the logit's bits in an order-preserving form above the inverted id, so that a larger key is a
-// better token and ties need no care.  Warps collect the keys above a threshold that n keys of the CTA are known to reach,
-// and cut their lists to the best n whenever these fill; the first threshold is the n-th largest of a warp's 32 lane maxima.
+// Alternatives: the pass only leaves the maximum of each stretch of a thread's loads (32 bf16 or 16 fp32 logits of a vocabulary of
+// 128K) in a table.  A logit that n stretches are known to reach follows from the warps' largest maxima, and only stretches
+// that reach it, a few dozen, are read again (from L2) for their tokens: a test of every logit in the pass took 13 times the
+// time of the pass itself.  Tokens are 64-bit keys, the logit's bits in an order-preserving form above the inverted id, so that a
+// larger key is a better token and ties need no care; lists of keys are cut to the best n whenever they fill.
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 #include "wisp_logprobs.h"
@@ -26,6 +28,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kVecs = 4;             // 16-byte loads in flight per thread
 constexpr int kMaxTop = 32;
 constexpr int kList = 32 + 8 * 32;   // a warp's keys: the best so far and one load of every lane
+constexpr int kTable = 16;           // stretches per thread at most
 constexpr int kCutAt = 96;           // lists longer than this are cut at the next opportunity
 constexpr int kMaxCluster = 8;
 constexpr float kLazy = 20.0f;       // a logit this far above the reference moves it
@@ -50,6 +53,11 @@ __device__ __forceinline__ uint64_t key_of(float z, int id) {
   const uint32_t b = __float_as_uint(z + 0.0f);  // (-0 counts as 0)
   const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
   return (uint64_t)o << 32 | (0xffffffffu - (uint32_t)id);
+}
+// A logit as an integer of the same order.
+__device__ __forceinline__ int order_of(float z) {
+  const int b = __float_as_int(z + 0.0f);
+  return b ^ ((b >> 31) & 0x7fffffff);
 }
 __device__ __forceinline__ int id_of(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 __device__ __forceinline__ float logit_of(uint64_t key) {
@@ -180,7 +188,7 @@ struct List {
 
 // The keys of a thread's loads above the threshold, into the warp's list.  id0(u): id of load u's first element.
 template <typename T, typename Id>
-__device__ __noinline__ void collect(const Vec<T> (&x)[kVecs], Id id0, List &list, unsigned long long *threshold, int lane) {
+__device__ void collect(const Vec<T> (&x)[kVecs], Id id0, List &list, unsigned long long *threshold, int lane) {
   constexpr int E = Vec<T>::E;
   uint64_t thr = *(volatile unsigned long long *)threshold;
   auto key = [&](int u, int i) -> uint64_t {
@@ -239,6 +247,8 @@ __device__ __noinline__ void collect(const Vec<T> (&x)[kVecs], Id id0, List &lis
 
 struct Shared {
   Stat stat[kWarps];
+  int found;                            // stretches to read again
+  int floor;                            // the logit that they reach, in the form of order_of
   uint64_t best[kMaxCluster][kMaxTop];  // the first CTA's: the CTAs' alternatives
   Stat part[kMaxCluster];               // the first CTA's: the CTAs' sums
   unsigned long long threshold;
@@ -258,6 +268,8 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
   constexpr int E = Vec<T>::E;
   __shared__ Shared sh;
   __shared__ uint64_t s_list[TOP ? kWarps * kList : 1];
+  __shared__ float s_max[TOP ? kTable * kThreads : 1];       // the stretches' maxima
+  __shared__ uint16_t s_again[TOP ? kTable * kThreads : 1];  // those to be read again
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int csize = p.cluster, row = blockIdx.x / csize, rank = blockIdx.x % csize;
   const int tok = p.tokens[row];
@@ -289,15 +301,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
 
   Stat st = {-INFINITY, 0.0f, 0.0f};
   float2 s2 = make_float2(0.0f, 0.0f), w2 = s2;
-  List list;
-  list.keys = s_list + (TOP ? warp * kList : 0);
-  list.count = 0;
-  list.top_n = p.top_n;
-  if (TOP && tid == 0) sh.threshold = 0;
-  if (TOP) __syncthreads();
-  float thr = -INFINITY;  // the threshold's logit
+  // a thread's round of loads is a stretch, or several rounds are where the table has not room for all
+  constexpr int kRound = kThreads * kVecs;
+  const int rounds = (v1 - v0 + kRound - 1) / kRound, span = (rounds + kTable - 1) / kTable;
 
-  auto take = [&](const Vec<T> (&x)[kVecs], auto id0) {
+  auto take = [&](const Vec<T> (&x)[kVecs]) -> float {
     const float cm = max_of<T>(x);
     if (cm != -INFINITY) {
       if (!(cm <= st.r + kLazy)) {  // (a NaN too: it stays)
@@ -326,13 +334,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
       }
     }
     if (cm != cm) s2.x = NAN;
-    if (TOP) {
-      if (__any_sync(0xffffffffu, cm >= thr && cm != -INFINITY)) {
-        collect<T>(x, id0, list, &sh.threshold, lane);
-        const uint64_t t = *(volatile unsigned long long *)&sh.threshold;
-        thr = t ? logit_of(t) : -INFINITY;
-      }
-    }
+    return cm;
   };
 
   Vec<T> cur[kVecs], nxt[kVecs];
@@ -347,24 +349,37 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
     }
   };
   if (v0 < v1) load(v0, cur);
-  for (int base = v0; base < v1; base += kThreads * kVecs) {
-    if (base + kThreads * kVecs < v1) load(base + kThreads * kVecs, nxt);
-    take(cur, [&](int u) { return head + (base + u * kThreads + tid) * E; });
+  float most = -INFINITY;
+  int slot = 0, left = span;
+  float stretch = -INFINITY;
+  for (int base = v0; base < v1; base += kRound) {
+    if (base + kRound < v1) load(base + kRound, nxt);
+    const float cm = take(cur);
+    if (TOP) {
+      stretch = fmaxf(stretch, cm);
+      most = fmaxf(most, cm);
+      if (--left == 0 || base + kRound >= v1) {
+        s_max[slot++ * kThreads + tid] = stretch;
+        stretch = -INFINITY;
+        left = span;
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) cur[u] = nxt[u];
   }
-  if (rank == 0 && warp == 0 && head + tail > 0) {  // the elements around the aligned loads, one per lane
-    const int id = lane < head ? lane : head + nvec * E + lane - head;
+  const bool edges = rank == 0 && warp == 0 && head + tail > 0;
+  const int edge_id = lane < head ? lane : head + nvec * E + lane - head;
+  if (edges) {  // the elements around the aligned loads, one per lane
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) cur[u].clear();
     if (lane < head + tail) {
-      const float v = element(z, id);
+      const float v = element(z, edge_id);
       if (E == 4)
         cur[0].v.x = __float_as_uint(v);
       else
         cur[0].v.x = (cur[0].v.x & 0xffff0000u) | __float_as_uint(v) >> 16;
     }
-    take(cur, [&](int u) { return id + u; });
+    take(cur);
   }
 
   st.s = s2.x + s2.y;
@@ -380,6 +395,55 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
   if (lane == 0) sh.stat[warp] = st;
   uint64_t best = 0;
   if (TOP) {
+    // at least top_n threads' maxima reach the least of the warps' q-th largest, q = top_n / 8 rounded up
+    int o = order_of(most), least = 0;
+    for (int i = 0; i < (p.top_n + kWarps - 1) / kWarps; ++i) {
+      least = __reduce_max_sync(0xffffffffu, o);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, o == least)) - 1) o = INT32_MIN;
+    }
+    if (tid == 0) {
+      sh.found = 0;
+      sh.floor = INT32_MAX;
+    }
+    __syncthreads();
+    if (lane == 0) atomicMin(&sh.floor, least);
+    __syncthreads();
+    const int floor = max(sh.floor, order_of(-3.402823466e38f));  // (stretches of -inf: nothing to find)
+    for (int i = 0; i < slot; ++i)
+      if (order_of(s_max[i * kThreads + tid]) >= floor) s_again[atomicAdd(&sh.found, 1)] = (uint16_t)(i * kThreads + tid);
+    if (tid == 0) sh.threshold = ((unsigned long long)((uint32_t)floor ^ 0x80000000u) << 32) - 1;
+    __syncthreads();
+    List list;
+    list.keys = s_list + warp * kList;
+    list.count = 0;
+    list.top_n = p.top_n;
+    const int found = sh.found;
+    for (int at = warp * 32; at < found; at += kThreads) {
+      const int e = at + lane < found ? s_again[at + lane] : -1;
+      for (int r = 0; r < span; ++r) {
+        const int first = e < 0 ? v1 : v0 + (e / kThreads * span + r) * kRound + e % kThreads;
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+          if (first + u * kThreads < v1)
+            cur[u].v = __ldg(zv + first + u * kThreads);
+          else
+            cur[u].clear();
+        }
+        collect<T>(cur, [&](int u) { return head + (first + u * kThreads) * E; }, list, &sh.threshold, lane);
+      }
+    }
+    if (edges) {
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) cur[u].clear();
+      if (lane < head + tail) {
+        const float v = element(z, edge_id);
+        if (E == 4)
+          cur[0].v.x = __float_as_uint(v);
+        else
+          cur[0].v.x = (cur[0].v.x & 0xffff0000u) | __float_as_uint(v) >> 16;
+      }
+      collect<T>(cur, [&](int u) { return edge_id + u; }, list, &sh.threshold, lane);
+    }
     best = list.best(lane);
     __syncwarp();
     list.keys[lane] = best;
@@ -389,7 +453,8 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
     st = sh.stat[0];
     for (int w = 1; w < kWarps; ++w) st = join(st, sh.stat[w]);
     if (TOP)
-      for (int w = 1; w < kWarps; ++w) best = warp_merge(best, s_list[w * kList + lane], lane);
+      for (int w = 1; w < kWarps; ++w)
+        if (s_list[w * kList]) best = warp_merge(best, s_list[w * kList + lane], lane);
     if (csize > 1) {  // to the first CTA
       if (TOP) {
         const uint32_t at = remote(&sh.best[rank][lane], 0);
