@@ -30,6 +30,7 @@ constexpr int kMaxTop = 32;
 constexpr int kList = 32 + 8 * 32;   // a warp's keys: the best so far and one load of every lane
 constexpr int kTable = 16;           // stretches per thread at most
 constexpr int kCutAt = 96;           // lists longer than this are cut at the next opportunity
+constexpr int kFew = kThreads;       // so many keys are put in order by counting; more (many equal logits) go through the warps' lists
 constexpr int kMaxCluster = 8;
 constexpr float kLazy = 20.0f;       // a logit this far above the reference moves it
 constexpr float kLeast = -200.0f;    // exp of it and of anything below is 0
@@ -247,7 +248,7 @@ __device__ void collect(const Vec<T> (&x)[kVecs], Id id0, List &list, unsigned l
 
 struct Shared {
   Stat stat[kWarps];
-  int found;                            // stretches to read again
+  int found, pushed;                    // stretches to read again, keys found in them
   int floor;                            // the logit that they reach, in the form of order_of
   uint64_t best[kMaxCluster][kMaxTop];  // the first CTA's: the CTAs' alternatives
   Stat part[kMaxCluster];               // the first CTA's: the CTAs' sums
@@ -290,6 +291,8 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
     if (tid == 0 && rank == 0) report_row(p.status, WISP_DEV_BAD_TOKEN, row);
     return write_all(NAN, -1);
   }
+  // a CTA's shared memory is written by others only once it runs
+  if (csize > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const float zt = rank == 0 && tid == 0 ? element(z, tok) : 0.0f;
 
   // the row's aligned loads [0, nvec), `head` elements before them and `tail` after
@@ -402,9 +405,14 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
       if (lane == __ffs(__ballot_sync(0xffffffffu, o == least)) - 1) o = INT32_MIN;
     }
     if (tid == 0) {
-      sh.found = 0;
+      sh.found = sh.pushed = 0;
       sh.floor = INT32_MAX;
     }
+    if (warp == 0) sh.best[0][lane] = 0;
+    auto push = [&](uint64_t k) {
+      const int i = atomicAdd(&sh.pushed, 1);
+      if (i < kFew) s_list[i] = k;
+    };
     __syncthreads();
     if (lane == 0) atomicMin(&sh.floor, least);
     __syncthreads();
@@ -413,48 +421,86 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
       if (order_of(s_max[i * kThreads + tid]) >= floor) s_again[atomicAdd(&sh.found, 1)] = (uint16_t)(i * kThreads + tid);
     if (tid == 0) sh.threshold = ((unsigned long long)((uint32_t)floor ^ 0x80000000u) << 32) - 1;
     __syncthreads();
-    List list;
-    list.keys = s_list + warp * kList;
-    list.count = 0;
-    list.top_n = p.top_n;
+    // their tokens: a load of a stretch per thread, and the keys that reach the floor into one list
     const int found = sh.found;
-    for (int at = warp * 32; at < found; at += kThreads) {
-      const int e = at + lane < found ? s_again[at + lane] : -1;
-      for (int r = 0; r < span; ++r) {
-        const int first = e < 0 ? v1 : v0 + (e / kThreads * span + r) * kRound + e % kThreads;
+    for (int i = tid; i < found * kVecs * span; i += kThreads) {
+      const int e = s_again[i / (kVecs * span)], u = i % kVecs, r = i / kVecs % span;
+      const int at = v0 + (e / kThreads * span + r) * kRound + u * kThreads + e % kThreads;
+      if (at < v1) {
+        Vec<T> x;
+        x.v = __ldg(zv + at);
 #pragma unroll
-        for (int u = 0; u < kVecs; ++u) {
-          if (first + u * kThreads < v1)
-            cur[u].v = __ldg(zv + first + u * kThreads);
-          else
-            cur[u].clear();
+        for (int q = 0; q < E; ++q)
+          if (order_of(x.at(q)) >= floor) push(key_of(x.at(q), head + at * E + q));
+      }
+    }
+    if (edges && lane < head + tail) {
+      const float v = element(z, edge_id);
+      if (order_of(v) >= floor) push(key_of(v, edge_id));
+    }
+    __syncthreads();
+    const int pushed = sh.pushed;
+    if (pushed <= kFew) {
+      // a key's place is the number of larger ones
+      if (tid < pushed) {
+        const uint64_t k = s_list[tid];
+        int place = 0;
+        for (int i = 0; i < pushed; ++i) place += s_list[i] > k;
+        if (place < kMaxTop) sh.best[0][place] = k;
+      }
+      __syncthreads();
+      best = warp == 0 ? sh.best[0][lane] : 0;
+    } else {
+      List list;
+      list.keys = s_list + warp * kList;
+      list.count = 0;
+      list.top_n = p.top_n;
+      for (int at = warp * 32; at < found; at += kThreads) {
+        const int e = at + lane < found ? s_again[at + lane] : -1;
+        for (int r = 0; r < span; ++r) {
+          const int first = e < 0 ? v1 : v0 + (e / kThreads * span + r) * kRound + e % kThreads;
+#pragma unroll
+          for (int u = 0; u < kVecs; ++u) {
+            if (first + u * kThreads < v1)
+              cur[u].v = __ldg(zv + first + u * kThreads);
+            else
+              cur[u].clear();
+          }
+          collect<T>(cur, [&](int u) { return head + (first + u * kThreads) * E; }, list, &sh.threshold, lane);
         }
-        collect<T>(cur, [&](int u) { return head + (first + u * kThreads) * E; }, list, &sh.threshold, lane);
       }
-    }
-    if (edges) {
+      if (edges) {
 #pragma unroll
-      for (int u = 0; u < kVecs; ++u) cur[u].clear();
-      if (lane < head + tail) {
-        const float v = element(z, edge_id);
-        if (E == 4)
-          cur[0].v.x = __float_as_uint(v);
-        else
-          cur[0].v.x = (cur[0].v.x & 0xffff0000u) | __float_as_uint(v) >> 16;
+        for (int u = 0; u < kVecs; ++u) cur[u].clear();
+        if (lane < head + tail) {
+          const float v = element(z, edge_id);
+          if (E == 4)
+            cur[0].v.x = __float_as_uint(v);
+          else
+            cur[0].v.x = (cur[0].v.x & 0xffff0000u) | __float_as_uint(v) >> 16;
+        }
+        collect<T>(cur, [&](int u) { return edge_id + u; }, list, &sh.threshold, lane);
       }
-      collect<T>(cur, [&](int u) { return edge_id + u; }, list, &sh.threshold, lane);
+      best = list.best(lane);
+      __syncwarp();
+      list.keys[lane] = best;
+      __syncthreads();
+      if (warp == 0)
+        for (int w = 1; w < kWarps; ++w) best = warp_merge(best, s_list[w * kList + lane], lane);
     }
-    best = list.best(lane);
-    __syncwarp();
-    list.keys[lane] = best;
   }
   __syncthreads();
+  if (csize > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (warp == 0) {
-    st = sh.stat[0];
-    for (int w = 1; w < kWarps; ++w) st = join(st, sh.stat[w]);
-    if (TOP)
-      for (int w = 1; w < kWarps; ++w)
-        if (s_list[w * kList]) best = warp_merge(best, s_list[w * kList + lane], lane);
+    st = sh.stat[lane & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+      Stat b;
+      b.r = __shfl_xor_sync(0xffffffffu, st.r, o);
+      b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
+      b.w = __shfl_xor_sync(0xffffffffu, st.w, o);
+      st = join(st, b);
+    }
     if (csize > 1) {  // to the first CTA
       if (TOP) {
         const uint32_t at = remote(&sh.best[rank][lane], 0);
