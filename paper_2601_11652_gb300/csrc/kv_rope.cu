@@ -19,212 +19,247 @@ namespace wisp {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPasses = 4;  // warp passes over heads per unit of work: so many loads in flight
+constexpr int kThreads = 128;
+constexpr int kCtasPerSM = 8;
 
 struct RopeParams {
-  int Hq, rot16;         // queries' heads; rotated elements / 16
+  int Hq, rot8;          // queries' heads; rotated elements / 8
   int interleaved;
   int group;             // consecutive new rows per K/V unit of an e4m3 cache, at most 16
-  const float *table;    // [positions, 16 * rot16]: cosines, then sines
+  const float *table;    // [positions, 8 * rot8]: cosines, then sines
   const char *q;
   char *q_out;
   int64_t q_stride, k_stride, v_stride;  // bytes between rows
   float *k_scale, *v_scale;
 };
 
-// 16 elements of one head's row per lane, as two groups of 8: those that rotate into each other (lanes
-// below rot16), or two groups that pass.
+// 8 elements of one head's row per lane, as two groups of 4: those that rotate into each other (lanes
+// below rot8), or two groups that pass.  (With 16 elements a lane, a page's rows took twice the registers and an SM half the warps.)
 struct Groups {
-  int a, b;
+  int a, b;  // first elements
   bool turn;
 };
 __device__ __forceinline__ Groups groups_of(int l, const RopeParams &o) {
   Groups g;
-  g.turn = l < o.rot16;
-  if (g.turn) {
-    g.a = o.interleaved ? 2 * l : l;
-    g.b = o.interleaved ? 2 * l + 1 : l + o.rot16;
-  } else {
-    g.a = 2 * l;
-    g.b = 2 * l + 1;
-  }
+  g.turn = l < o.rot8;
+  const bool split = g.turn && !o.interleaved;
+  g.a = split ? 4 * l : 8 * l;
+  g.b = split ? 4 * (l + o.rot8) : 8 * l + 4;
   return g;
 }
 
-__device__ __forceinline__ void load8(const uint16_t *src, float (&x)[16], int at) {
-  const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[at + 2 * i] = __uint_as_float(w[i] << 16);
-    x[at + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// Four elements, as they are in memory.
+template <typename T>
+struct Four {
+  uint32_t w[sizeof(T)];
+  __device__ __forceinline__ void load(const T *src) {
+    if (sizeof(T) == 2) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
+      w[0] = v.x;
+      w[1] = v.y;
+      w[sizeof(T) - 2] = v.z;
+      w[sizeof(T) - 1] = v.w;
+    }
   }
-}
-__device__ __forceinline__ void load8(const float *src, float (&x)[16], int at) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float4 v = __ldg(reinterpret_cast<const float4 *>(src) + h);
-    x[at + 4 * h] = v.x;
-    x[at + 4 * h + 1] = v.y;
-    x[at + 4 * h + 2] = v.z;
-    x[at + 4 * h + 3] = v.w;
+  __device__ __forceinline__ void read(const T *src) {
+    if (sizeof(T) == 2) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(src);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      const uint4 v = *reinterpret_cast<const uint4 *>(src);
+      w[0] = v.x;
+      w[1] = v.y;
+      w[sizeof(T) - 2] = v.z;
+      w[sizeof(T) - 1] = v.w;
+    }
   }
-}
-__device__ __forceinline__ void store8(uint16_t *dst, const float (&x)[16], int at) {
-  uint32_t w[4];
+  __device__ __forceinline__ void get(float *x) const {
+    if (sizeof(T) == 2) {
+      x[0] = __uint_as_float(w[0] << 16);
+      x[1] = __uint_as_float(w[0] & 0xffff0000u);
+      x[2] = __uint_as_float(w[1] << 16);
+      x[3] = __uint_as_float(w[1] & 0xffff0000u);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(x[at + 2 * i], x[at + 2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t *>(&v);
+      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i < (int)sizeof(T) ? i : 0]);
+    }
   }
-  *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store8(float *dst, const float (&x)[16], int at) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    reinterpret_cast<float4 *>(dst)[h] = make_float4(x[at + 4 * h], x[at + 4 * h + 1], x[at + 4 * h + 2], x[at + 4 * h + 3]);
-}
-
-// The lane's 8 cosines and 8 sines of a position.
-struct Angles {
-  float c[8], s[8];
 };
-__device__ __forceinline__ void load_angles(const RopeParams &o, int pos, int l, Angles &t) {
-  const float4 *p = reinterpret_cast<const float4 *>(o.table + (int64_t)pos * 16 * o.rot16 + 8 * l);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float4 c = __ldg(p + h), s = __ldg(p + 2 * o.rot16 + h);
-    t.c[4 * h] = c.x;
-    t.c[4 * h + 1] = c.y;
-    t.c[4 * h + 2] = c.z;
-    t.c[4 * h + 3] = c.w;
-    t.s[4 * h] = s.x;
-    t.s[4 * h + 1] = s.y;
-    t.s[4 * h + 2] = s.z;
-    t.s[4 * h + 3] = s.w;
+__device__ __forceinline__ void store4(uint16_t *dst, const float *x) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+  *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+__device__ __forceinline__ void store4(float *dst, const float *x) { *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]); }
+
+// A lane's 8 elements as they were read; floats only where they are used.
+template <typename T>
+struct Raw {
+  Four<T> a, b;
+  __device__ __forceinline__ void load(const T *row, const Groups &g) {
+    a.load(row + g.a);
+    b.load(row + g.b);
   }
+  __device__ __forceinline__ void read(const T *row, const Groups &g) {  // from shared memory
+    a.read(row + g.a);
+    b.read(row + g.b);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    a.get(x);
+    b.get(x + 4);
+  }
+};
+
+// The lane's 4 cosines and 4 sines of a position.
+struct Angles {
+  float4 c, s;
+};
+__device__ __forceinline__ Angles load_angles(const RopeParams &o, int pos, int l, bool turn) {
+  Angles t = {};
+  if (turn) {
+    const float4 *p = reinterpret_cast<const float4 *>(o.table + (int64_t)pos * 8 * o.rot8) + l;
+    t.c = __ldg(p);
+    t.s = __ldg(p + o.rot8);
+  }
+  return t;
 }
 __device__ __forceinline__ void turn_pair(float &a, float &b, float c, float s) {
   const float u = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
   b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
   a = u;
 }
-__device__ __forceinline__ void rotate(float (&x)[16], const Angles &t, bool interleaved) {
-  if (interleaved) {
+// x rotated where `turn` says so.  (Selected, not branched around: the compiler would hold every row's floats over the branches.)
+template <bool INTER>
+__device__ __forceinline__ void rotate(float (&x)[8], const Angles &t, bool turn) {
+  float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn_pair(x[2 * i], x[2 * i + 1], t.c[i], t.s[i]);
+  for (int i = 0; i < 8; ++i) y[i] = x[i];
+  if (INTER) {
+    turn_pair(y[0], y[1], t.c.x, t.s.x);
+    turn_pair(y[2], y[3], t.c.y, t.s.y);
+    turn_pair(y[4], y[5], t.c.z, t.s.z);
+    turn_pair(y[6], y[7], t.c.w, t.s.w);
   } else {
+    turn_pair(y[0], y[4], t.c.x, t.s.x);
+    turn_pair(y[1], y[5], t.c.y, t.s.y);
+    turn_pair(y[2], y[6], t.c.z, t.s.z);
+    turn_pair(y[3], y[7], t.c.w, t.s.w);
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn_pair(x[i], x[i + 8], t.c[i], t.s[i]);
+  for (int i = 0; i < 8; ++i) x[i] = turn ? y[i] : x[i];
+}
+
+// Heads per unit of whole rows: so many loads in flight.
+template <typename T, int D>
+constexpr int heads_per_unit() { return (sizeof(T) == 2 ? 8 : 4) * (32 / (D / 8)); }
+
+// Heads [h0, h0 + heads_per_unit) of one row: src -> dst, rotated if `turn`.  dst heads are DST_HEAD elements apart.
+// The loads come first, then `where` tells the row's destination (null: none) and position.
+template <typename T, int D, bool INTER, int DST_HEAD, typename Where>
+__device__ __forceinline__ void move_heads(const RopeParams &o, const T *src, int h0, int H, bool turn, Where where) {
+  constexpr int LPR = D / 8, RPP = 32 / LPR, N = heads_per_unit<T, D>() / RPP;
+  const int lane = threadIdx.x & 31, l = lane % LPR;
+  const Groups g = groups_of(l, o);
+  const int h = h0 + lane / LPR, left = H - h;  // this lane's heads: h, h + RPP, ..
+  src += (int64_t)h * D;
+  Raw<T> raw[N] = {};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i * RPP < left) raw[i].load(src + i * RPP * D, g);
+  int pos = 0;
+  T *dst = where(pos);
+  if (!dst) return;
+  dst += (int64_t)h * DST_HEAD;
+  const bool turns = turn && g.turn;
+  const Angles t = load_angles(o, pos, l, turns);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float x[8];
+    raw[i].get(x);
+    if (turn) rotate<INTER>(x, t, turns);
+    if (i * RPP < left) {
+      store4(dst + i * RPP * DST_HEAD + g.a, x);
+      store4(dst + i * RPP * DST_HEAD + g.b, x + 4);
+    }
   }
 }
 
-// Heads [h0, h0 + kPasses * heads per pass) of one row: src -> dst, rotated if `turn`.  dst heads are dst_head
-// elements apart.
-template <typename T, int D>
-__device__ __forceinline__ void move_heads(const RopeParams &o, const T *src, T *dst, int64_t dst_head, int h0, int H, int pos,
-                                           bool turn) {
-  constexpr int LPR = D / 16, RPP = 32 / LPR;
-  const int lane = threadIdx.x & 31, l = lane % LPR;
-  const Groups g = groups_of(l, o);
-  float x[kPasses][16];
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int h = h0 + i * RPP + lane / LPR;
-    if (h < H) {
-      load8(src + (int64_t)h * D + 8 * g.a, x[i], 0);
-      load8(src + (int64_t)h * D + 8 * g.b, x[i], 8);
-    }
-  }
-  if (turn && g.turn) {
-    Angles t;
-    load_angles(o, pos, l, t);
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) rotate(x[i], t, o.interleaved);
-  }
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int h = h0 + i * RPP + lane / LPR;
-    if (h < H) {
-      store8(dst + h * dst_head + 8 * g.a, x[i], 0);
-      store8(dst + h * dst_head + 8 * g.b, x[i], 8);
-    }
-  }
+__device__ __forceinline__ void copy16(void *dst, const void *src) {  // global to shared, asynchronous
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
 }
 
 // One page of one head of an e4m3 cache, by one warp: slots s0 .. s0 + n - 1 are new rows (the first of them at src,
-// at position pos), slots below s0 hold earlier ones.
-template <typename T, int D>
-__device__ __forceinline__ void quantise_page(const RopeParams &o, uint8_t *page, float *scale, const T *src,
+// at position pos), slots below s0 hold earlier ones.  The rows (of earlier ones the codes) are staged in shared memory and
+// read twice, for the scale and for the codes: in registers they would leave an SM a third of its warps.
+template <typename T, int D, bool INTER>
+__device__ __forceinline__ void quantise_page(const RopeParams &o, T *stage, uint8_t *page, float *scale, const T *src,
                                               int64_t src_row, int s0, int n, int pos, bool turn) {
-  constexpr int LPR = D / 16, RPP = 32 / LPR, NP = kKvPage / RPP;
+  constexpr int LPR = D / 8, RPP = 32 / LPR;       // a lane has 8 elements of a row
+  constexpr int CPR = D * sizeof(T) / 16;          // 16-byte pieces of a row
   const int lane = threadIdx.x & 31, l = lane % LPR;
   const Groups g = groups_of(l, o);
-  float x[NP][16];
   const float old_scale = s0 > 0 ? *scale : 1.0f;
-  float amax = 0.0f;
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int slot = i * RPP + lane / LPR;
+  __syncwarp();  // the page before has been read
+  for (int c = lane; c < n * CPR; c += 32)
+    copy16(stage + (s0 + c / CPR) * D + c % CPR * (16 / sizeof(T)),
+           reinterpret_cast<const char *>(src) + (c / CPR) * src_row + c % CPR * 16);
+  for (int c = lane; c < s0 * (D / 16); c += 32)
+    copy16(reinterpret_cast<uint8_t *>(stage + c / (D / 16) * D) + c % (D / 16) * 16, page + c * 16);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+  // the values of a slot below s0 + n
+  auto values = [&](int slot, float (&x)[8]) {
+    const T *row = stage + slot * D;
     if (slot < s0) {
-      const uint2 ca = *reinterpret_cast<const uint2 *>(page + slot * D + 8 * g.a);
-      const uint2 cb = *reinterpret_cast<const uint2 *>(page + slot * D + 8 * g.b);
-      const uint32_t w[4] = {ca.x, ca.y, cb.x, cb.y};
+      const uint8_t *codes = reinterpret_cast<const uint8_t *>(row);
+      const uint32_t w[2] = {*reinterpret_cast<const uint32_t *>(codes + g.a), *reinterpret_cast<const uint32_t *>(codes + g.b)};
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
+      for (int q = 0; q < 4; ++q) {
         const float2 v = h2_to_f2(e4m3x2_to_h2((w[q >> 1] >> (16 * (q & 1))) & 0xffffu));
-        x[i][2 * q] = v.x * old_scale;
-        x[i][2 * q + 1] = v.y * old_scale;
-      }
-    } else if (slot < s0 + n) {
-      const T *row = reinterpret_cast<const T *>(reinterpret_cast<const char *>(src) + (slot - s0) * src_row);
-      load8(row + 8 * g.a, x[i], 0);
-      load8(row + 8 * g.b, x[i], 8);
-      if (turn && g.turn) {
-        Angles t;
-        load_angles(o, pos + slot - s0, l, t);
-        rotate(x[i], t, o.interleaved);
+        x[2 * q] = v.x * old_scale;
+        x[2 * q + 1] = v.y * old_scale;
       }
     } else {
-#pragma unroll
-      for (int q = 0; q < 16; ++q) x[i][q] = 0.0f;
+      Raw<T> raw;
+      raw.read(row, g);
+      raw.get(x);
+      if (turn) rotate<INTER>(x, load_angles(o, pos + slot - s0, l, g.turn), g.turn);
     }
+  };
+  float amax = 0.0f;  // the largest finite magnitude
+#pragma unroll 2
+  for (int slot = lane / LPR; slot < s0 + n; slot += RPP) {
+    float x[8];
+    values(slot, x);
 #pragma unroll
-    for (int q = 0; q < 16; ++q) amax = fmaxf(amax, fabsf(x[i][q]));  // (a NaN loses)
+    for (int q = 0; q < 8; ++q) amax = fmaxf(amax, fabsf(x[q]) < INFINITY ? fabsf(x[q]) : 0.0f);
   }
-  amax = ptx::warp_max(amax);
-  if (amax == INFINITY) {  // the largest finite magnitude decides
-    amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) amax = fmaxf(amax, fabsf(x[i][q]) < INFINITY ? fabsf(x[i][q]) : 0.0f);
-    amax = ptx::warp_max(amax);
-  }
-  const int e = scale_exp(amax);
+  __syncwarp();
+  const int e = scale_exp(ptx::warp_max(amax));
   const float inv = exp2i(-e);
-  const bool rewrite = old_scale != exp2i(e);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int slot = i * RPP + lane / LPR;
-    if (slot < s0 + n && (slot >= s0 || rewrite)) {
-      uint32_t w[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        w[q] = e4m3x2(x[i][4 * q] * inv, x[i][4 * q + 1] * inv) | e4m3x2(x[i][4 * q + 2] * inv, x[i][4 * q + 3] * inv) << 16;
-      *reinterpret_cast<uint2 *>(page + slot * D + 8 * g.a) = make_uint2(w[0], w[1]);
-      *reinterpret_cast<uint2 *>(page + slot * D + 8 * g.b) = make_uint2(w[2], w[3]);
-    }
+  const int first = old_scale != exp2i(e) ? 0 : s0;  // earlier codes stay where the scale does
+#pragma unroll 2
+  for (int slot = first / RPP * RPP + lane / LPR; slot < s0 + n; slot += RPP) {
+    if (slot < first) continue;
+    float x[8];
+    values(slot, x);
+    *reinterpret_cast<uint32_t *>(page + slot * D + g.a) = e4m3x2(x[0] * inv, x[1] * inv) | e4m3x2(x[2] * inv, x[3] * inv) << 16;
+    *reinterpret_cast<uint32_t *>(page + slot * D + g.b) = e4m3x2(x[4] * inv, x[5] * inv) | e4m3x2(x[6] * inv, x[7] * inv) << 16;
   }
+  __syncwarp();
   if (lane == 0) *scale = exp2i(e);
 }
 
 // A warp per unit: first the K/V units (a page of one head, or some heads of one row), then the queries'.
-template <typename T, bool Q8, int D>
-__global__ void __launch_bounds__(kThreads) kv_append_rope_kernel(const KvParams p, const RopeParams o) {
+template <typename T, bool Q8, int D, bool INTER>
+__global__ void __launch_bounds__(kThreads, kCtasPerSM) kv_append_rope_kernel(const KvParams p, const RopeParams o) {
+  __shared__ __align__(16) T s_stage[Q8 ? kThreads / 32 * kKvPage * D : 1];
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the reservation
-  constexpr int HC = kPasses * (32 / (D / 16));        // heads per unit of whole rows
+  constexpr int HC = heads_per_unit<T, D>();
   const int lane = threadIdx.x & 31;
   const int64_t T_rows = p.total_rows;
   const int kvc = (p.Hkv + HC - 1) / HC, qc = (o.Hq + HC - 1) / HC;
@@ -235,9 +270,10 @@ __global__ void __launch_bounds__(kThreads) kv_append_rope_kernel(const KvParams
     if (u >= kv_units) {
       const int64_t x = (u - kv_units) / qc;
       const int c = (int)((u - kv_units) % qc);
-      if (p.row_req[x] < 0) continue;
-      move_heads<T, D>(o, reinterpret_cast<const T *>(o.q + x * o.q_stride), reinterpret_cast<T *>(o.q_out) + x * o.Hq * D, D,
-                       c * HC, o.Hq, p.row_pos[x], true);
+      move_heads<T, D, INTER, D>(o, reinterpret_cast<const T *>(o.q + x * o.q_stride), c * HC, o.Hq, true, [&](int &pos) -> T * {
+        pos = p.row_pos[x];
+        return p.row_req[x] < 0 ? nullptr : reinterpret_cast<T *>(o.q_out) + x * o.Hq * D;
+      });
       continue;
     }
     if (Q8) {
@@ -267,7 +303,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_rope_kernel(const KvParams
         }
         const int64_t ph = (int64_t)page * p.Hkv + h;
         const char *rows = (is_v ? p.v_new + (x0 + src) * o.v_stride : p.k_new + (x0 + src) * o.k_stride);
-        quantise_page<T, D>(o, reinterpret_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + ph * kKvPage * D,
+        quantise_page<T, D, INTER>(o, s_stage + (threadIdx.x >> 5) * kKvPage * D, reinterpret_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + ph * kKvPage * D,
                             (is_v ? o.v_scale : o.k_scale) + ph, reinterpret_cast<const T *>(rows) + (int64_t)h * D,
                             is_v ? o.v_stride : o.k_stride, pp % kKvPage, nn, pp, !is_v);
       }
@@ -275,17 +311,19 @@ __global__ void __launch_bounds__(kThreads) kv_append_rope_kernel(const KvParams
       const int64_t x = u / (2 * kvc);
       const int cv = (int)(u % (2 * kvc));
       const bool is_v = cv >= kvc;
-      const int r = p.row_req[x];
-      if (r < 0) continue;
-      const int pos = p.row_pos[x];
-      const int32_t page = p.block_tables[(int64_t)r * p.max_blocks + pos / kKvPage];
-      if (page < 0 || page >= p.num_blocks) {
-        if (lane == 0) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, r);
-        continue;
-      }
-      T *dst = reinterpret_cast<T *>(is_v ? p.v_cache : p.k_cache) + ((int64_t)page * p.Hkv * kKvPage + pos % kKvPage) * D;
-      move_heads<T, D>(o, reinterpret_cast<const T *>(is_v ? p.v_new + x * o.v_stride : p.k_new + x * o.k_stride), dst,
-                       kKvPage * D, (is_v ? cv - kvc : cv) * HC, p.Hkv, pos, !is_v);
+      move_heads<T, D, INTER, kKvPage * D>(
+          o, reinterpret_cast<const T *>(is_v ? p.v_new + x * o.v_stride : p.k_new + x * o.k_stride), (is_v ? cv - kvc : cv) * HC, p.Hkv,
+          !is_v, [&](int &pos) -> T * {
+            const int r = p.row_req[x];
+            if (r < 0) return nullptr;
+            pos = p.row_pos[x];
+            const int32_t page = p.block_tables[(int64_t)r * p.max_blocks + pos / kKvPage];
+            if (page < 0 || page >= p.num_blocks) {
+              if (lane == 0) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, r);
+              return nullptr;
+            }
+            return reinterpret_cast<T *>(is_v ? p.v_cache : p.k_cache) + ((int64_t)page * p.Hkv * kKvPage + pos % kKvPage) * D;
+          });
     }
   }
 }
@@ -312,8 +350,11 @@ wisp_status rope_check(const wisp_kv_rope_args *a, bool call) {
 
 template <typename T, bool Q8>
 cudaError_t launch(const KvParams &p, const RopeParams &o, const cudaLaunchConfig_t &cfg) {
-  return p.D == 128 ? cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 128>, p, o)
-                    : cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 64>, p, o);
+  if (p.D == 128)
+    return o.interleaved ? cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 128, true>, p, o)
+                         : cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 128, false>, p, o);
+  return o.interleaved ? cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 64, true>, p, o)
+                       : cudaLaunchKernelEx(&cfg, kv_append_rope_kernel<T, Q8, 64, false>, p, o);
 }
 
 }  // namespace
@@ -343,7 +384,7 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   RopeParams o;
   std::memset(&o, 0, sizeof o);
   o.Hq = a->Hq;
-  o.rot16 = a->rot_dim / 16;
+  o.rot8 = a->rot_dim / 8;
   o.interleaved = a->interleaved != 0;
   o.table = a->rope;
   o.q = static_cast<const char *>(a->q);
@@ -357,7 +398,9 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   // about one page start per group of rows: prompts have one every 16 rows, single tokens one each
   o.group = 1;
   while (o.group < kKvPage && 2 * o.group <= kv.total_q_rows / kv.B) o.group *= 2;
-  const int hc = kPasses * (32 / (kv.D / 16));
+  const bool bf = kv.kv_dtype == WISP_BF16;
+  const int hc = kv.D == 128 ? (bf ? heads_per_unit<uint16_t, 128>() : heads_per_unit<float, 128>())
+                             : (bf ? heads_per_unit<uint16_t, 64>() : heads_per_unit<float, 64>());
   const int64_t T = kv.total_q_rows;
   const int64_t units = (q8 ? (T + o.group - 1) / o.group * 2 * kv.Hkv : T * 2 * ((kv.Hkv + hc - 1) / hc)) + T * ((a->Hq + hc - 1) / hc);
   const int64_t blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
@@ -372,8 +415,8 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = kv.kv_dtype == WISP_BF16 ? (q8 ? launch<uint16_t, true>(p, o, cfg) : launch<uint16_t, false>(p, o, cfg))
-                                                 : (q8 ? launch<float, true>(p, o, cfg) : launch<float, false>(p, o, cfg));
+  const cudaError_t e = bf ? (q8 ? launch<uint16_t, true>(p, o, cfg) : launch<uint16_t, false>(p, o, cfg))
+                           : (q8 ? launch<float, true>(p, o, cfg) : launch<float, false>(p, o, cfg));
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 
