@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kPage = kKvPage;
+constexpr int kAhead = 16;       // table entries in flight per lane
 constexpr int kReserveCtas = 8;  // one cluster (the portable maximum): its barrier orders counting before serving
 
 __device__ __forceinline__ int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
@@ -66,7 +67,7 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // Bound by the latency of reading the block tables (4 bytes a page, 0.1-1 MB a batch) and of its barriers.  A
-// warp reads one request's row, lanes side by side and four loads ahead.  64 requests of up to 2048
+// warp reads one request's row, lanes side by side and kAhead loads ahead.  64 requests of up to 2048
 // pages: 16 us with cold caches.
 __global__ void __launch_bounds__(kThreads) __cluster_dims__(kReserveCtas, 1, 1) kv_reserve_kernel(const KvParams p) {
   // the append kernel may be placed now; it waits for this grid before it reads anything
@@ -95,12 +96,12 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kReserveCtas, 1, 1)
       const int32_t *row = p.block_tables + (int64_t)r * p.max_blocks;
       const int nb = (int)((c + k + 1 + kPage - 1) / kPage);
       bool over = false;
-      for (int b0 = 0; b0 < nb; b0 += 128) {
-        int32_t id[4];
+      for (int b0 = 0; b0 < nb; b0 += 32 * kAhead) {
+        int32_t id[kAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) id[u] = b0 + 32 * u + lane < nb ? row[b0 + 32 * u + lane] : 0;
+        for (int u = 0; u < kAhead; ++u) id[u] = b0 + 32 * u + lane < nb ? row[b0 + 32 * u + lane] : 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
           const bool miss = id[u] < 0;
           over |= id[u] >= p.num_blocks;
           if (miss && first == INT32_MAX) first = b0 + 32 * u + lane;

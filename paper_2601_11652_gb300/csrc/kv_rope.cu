@@ -410,7 +410,7 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)(blocks < 4096 ? blocks : 4096));
+  cfg.gridDim = dim3((unsigned)(blocks < 16384 ? blocks : 16384));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cfg.attrs = attr;
