@@ -21,10 +21,12 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kCtasPerSM = 8;
+constexpr int kMaxScan = 1024;  // requests whose first rows a CTA finds itself
 
 struct RopeParams {
   int Hq, rot8;          // queries' heads; rotated elements / 8
   int interleaved;
+  int q_ctas;            // CTAs that rotate queries, the first ones
   int group;             // consecutive new rows per K/V unit of an e4m3 cache, at most 16
   const float *table;    // [positions, 8 * rot8]: cosines, then sines
   const char *q;
@@ -254,28 +256,87 @@ __device__ __forceinline__ void quantise_page(const RopeParams &o, T *stage, uin
   if (lane == 0) *scale = exp2i(e);
 }
 
-// A warp per unit: first the K/V units (a page of one head, or some heads of one row), then the queries'.
+// The requests' first rows, from their lengths as the reservation reads them (negative ones count as 0), in shared memory.
+struct Rows {
+  int32_t first[kMaxScan + 1];
+  int64_t sum[kThreads / 32];
+};
+__device__ void scan_rows(const KvParams &p, Rows &sh) {
+  constexpr int PER = kMaxScan / kThreads;
+  const int tid = threadIdx.x, lane = tid & 31;
+  int64_t k[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * PER + i;
+    k[i] = r < p.B ? (int64_t)max(0, __ldg(p.draft_lens + r)) + 1 : 0;
+    mine += k[i];
+  }
+  int64_t x = mine;
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += o;
+  }
+  if (lane == 31) sh.sum[tid >> 5] = x;
+  __syncthreads();
+  x -= mine;
+  for (int w = 0; w < tid >> 5; ++w) x += sh.sum[w];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    sh.first[tid * PER + i] = (int32_t)(x < INT32_MAX ? x : INT32_MAX);
+    x += k[i];
+  }
+  if (tid == kThreads - 1) sh.first[kMaxScan] = (int32_t)(x < INT32_MAX ? x : INT32_MAX);
+  __syncthreads();
+}
+
+// A warp per unit.  The first o.q_ctas CTAs rotate queries: of up to kMaxScan requests they find a row's request and
+// position themselves and do not wait for the reservation, which leaves all but eight SMs idle (8 prompts of 700-1023 tokens: 39 us with
+// the queries after it, see below for now).  The others write K and V: a page of one head, or some heads of one row.
 template <typename T, bool Q8, int D, bool INTER>
 __global__ void __launch_bounds__(kThreads, kCtasPerSM) kv_append_rope_kernel(const KvParams p, const RopeParams o) {
   __shared__ __align__(16) T s_stage[Q8 ? kThreads / 32 * kKvPage * D : 1];
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the reservation
+  __shared__ Rows s_rows;
   constexpr int HC = heads_per_unit<T, D>();
   const int lane = threadIdx.x & 31;
   const int64_t T_rows = p.total_rows;
-  const int kvc = (p.Hkv + HC - 1) / HC, qc = (o.Hq + HC - 1) / HC;
-  const int64_t groups = Q8 ? (T_rows + o.group - 1) / o.group : T_rows;
-  const int64_t kv_units = groups * 2 * (Q8 ? p.Hkv : kvc), units = kv_units + T_rows * qc;
-  const int64_t nwarps = (int64_t)gridDim.x * (kThreads / 32);
-  for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < units; u += nwarps) {
-    if (u >= kv_units) {
-      const int64_t x = (u - kv_units) / qc;
-      const int c = (int)((u - kv_units) % qc);
+  if ((int)blockIdx.x < o.q_ctas) {
+    const bool alone = p.B <= kMaxScan;
+    if (alone)
+      scan_rows(p, s_rows);
+    else
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int qc = (o.Hq + HC - 1) / HC;
+    const int64_t units = T_rows * qc, nwarps = (int64_t)o.q_ctas * (kThreads / 32);
+    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < units; u += nwarps) {
+      const int64_t x = u / qc;
+      const int c = (int)(u % qc);
       move_heads<T, D, INTER, D>(o, reinterpret_cast<const T *>(o.q + x * o.q_stride), c * HC, o.Hq, true, [&](int &pos) -> T * {
-        pos = p.row_pos[x];
-        return p.row_req[x] < 0 ? nullptr : reinterpret_cast<T *>(o.q_out) + x * o.Hq * D;
+        T *dst = reinterpret_cast<T *>(o.q_out) + x * o.Hq * D;
+        if (!alone) {
+          pos = p.row_pos[x];
+          return p.row_req[x] < 0 ? nullptr : dst;
+        }
+        int lo = 0, hi = kMaxScan;  // the last request whose first row is <= x
+        while (lo < hi - 1) {
+          const int mid = (lo + hi) >> 1;
+          if (s_rows.first[mid] <= x) lo = mid;
+          else hi = mid;
+        }
+        // (requests that the reservation will refuse for their lengths, and rows of nobody)
+        if (lo >= p.B || x >= s_rows.first[lo + 1]) return nullptr;
+        const int64_t k = __ldg(p.draft_lens + lo), ctx = p.context_lens[lo];
+        if (k < 0 || ctx < 0 || ctx + k + 1 > p.max_tokens) return nullptr;
+        pos = (int)(ctx + x - s_rows.first[lo]);
+        return dst;
       });
-      continue;
     }
+    return;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the reservation
+  const int kvc = (p.Hkv + HC - 1) / HC;
+  const int64_t groups = Q8 ? (T_rows + o.group - 1) / o.group : T_rows;
+  const int64_t units = groups * 2 * (Q8 ? p.Hkv : kvc), nwarps = (int64_t)(gridDim.x - o.q_ctas) * (kThreads / 32);
+  for (int64_t u = (int64_t)(blockIdx.x - o.q_ctas) * (kThreads / 32) + (threadIdx.x >> 5); u < units; u += nwarps) {
     if (Q8) {
       const int hv = (int)(u % (2 * p.Hkv));
       const bool is_v = hv >= p.Hkv;
@@ -402,15 +463,23 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   const int hc = kv.D == 128 ? (bf ? heads_per_unit<uint16_t, 128>() : heads_per_unit<float, 128>())
                              : (bf ? heads_per_unit<uint16_t, 64>() : heads_per_unit<float, 64>());
   const int64_t T = kv.total_q_rows;
-  const int64_t units = (q8 ? (T + o.group - 1) / o.group * 2 * kv.Hkv : T * 2 * ((kv.Hkv + hc - 1) / hc)) + T * ((a->Hq + hc - 1) / hc);
-  const int64_t blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
+  const int64_t kv_units = q8 ? (T + o.group - 1) / o.group * 2 * kv.Hkv : T * 2 * ((kv.Hkv + hc - 1) / hc);
+  const int64_t q_units = T * ((a->Hq + hc - 1) / hc);
+  auto ctas = [](int64_t units, int64_t most) {
+    const int64_t n = (units + kThreads / 32 - 1) / (kThreads / 32);
+    return (int)(n < most ? n : most);
+  };
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return WISP_ERR_CUDA;
+  o.q_ctas = ctas(q_units, (int64_t)sms * kCtasPerSM);
   if (kv_reserve_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)(blocks < 16384 ? blocks : 16384));
+  cfg.gridDim = dim3((unsigned)(o.q_ctas + ctas(kv_units, 16384)));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cfg.attrs = attr;
