@@ -456,9 +456,9 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   o.k_scale = a->k_scale;
   o.v_scale = a->v_scale;
   const bool q8 = a->cache_dtype == WISP_E4M3;
-  // about one page start per group of rows: prompts have one every 16 rows, single tokens one each
+  // about half a page start per group of rows: prompts have one every 16 rows, single tokens one each
   o.group = 1;
-  while (o.group < kKvPage && 2 * o.group <= kv.total_q_rows / kv.B) o.group *= 2;
+  while (o.group < kKvPage && 4 * o.group <= kv.total_q_rows / kv.B) o.group *= 2;
   const bool bf = kv.kv_dtype == WISP_BF16;
   const int hc = kv.D == 128 ? (bf ? heads_per_unit<uint16_t, 128>() : heads_per_unit<float, 128>())
                              : (bf ? heads_per_unit<uint16_t, 64>() : heads_per_unit<float, 64>());
@@ -472,7 +472,7 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return WISP_ERR_CUDA;
-  o.q_ctas = ctas(q_units, (int64_t)sms * kCtasPerSM);
+  o.q_ctas = ctas(q_units, (int64_t)sms * 2);  // (four or eight per SM take room from the others)
   if (kv_reserve_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
