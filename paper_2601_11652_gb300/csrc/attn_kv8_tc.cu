@@ -4,27 +4,44 @@
 // 0..c_r + j), with K and V of a page of one head worth code * scale (include/wisp_kv8.h).  K and V go from HBM to the
 // tensor core as they are:
 //   S^T = K Q^T       (M = 128 keys of a tile, N = the item's rows, K = D),     kind::f8f6f4
-//   O^T = V^T P^T     (M = D, N = rows, K = 128 keys)
-// The other operand of each product is split into two e4m3 parts, x = (hi + lo / 16) 2^e, that lie side by side along
-// N: 4 + 4 significant bits, what a bf16 value has, for one pass over K or V in shared memory; the reader of an
-// accumulator adds its two halves.  e is a power of two per query row, and for P per row and tile: P = 2^(s - m + 8)
-// with m the row's maximum over the tile's 128 keys, so that each tile keeps 8 bits down to 2^-13 of its own largest
-// weight and 2^-22 absolutely, whatever other tiles hold (with one exponent for a whole sequence, a key that outweighs the
-// others by 2^17 would cost them their bits).  The key's page scales enter as a factor of S and, as log2, in s,
-// so that V's scale rides on P.  PV products of different tiles have different exponents: each goes to a TMEM
-// accumulator of its own and the correction warps add it to their running sums with 2^(m - M).
+//   O^T += V^T P^T    (M = D, N = 2 * rows, K = 128 keys)
+// The other operand of each product is split into two e4m3 parts, x = (hi + lo) 2^e: 4 + 4 significant bits, what a bf16
+// value has, where hi is normal and lo not below e4m3's least, 2^-9.
+//   * Q: e is one power of two per item, its largest magnitude to at most 448.  Both parts' products add to one
+//     accumulator.  A page's K scale enters as a factor of its keys' scores.
+//   * P = 2^(s + log2(V's scale) - ref + 5): V's scale rides on P, and the sums of a row, which must not have it, take P
+//     times the inverse, in fp32.  hi and lo rows lie side by side along N and are added when O^T is read.
+//   * ref is a row's reference: the maximum of s + log2(scale) over the tile, taken anew only where the row's maximum
+//     over a tile is 3.6 above it (P must stay below 448) or 6 below it (and not 30 below the largest so far, where it
+//     weighs nothing).  So a tile's largest weight is 2^-1 or more and keeps 8 bits, its small ones count in steps of 2^-9.
+//     O^T stays in TMEM for the whole item; only where a reference moves it is read, multiplied and written back.
 //
 // Persistent CTAs (one per SM) take work items (request, KV head, key chunk, row group) from the plan's counter,
-// longest first.  Warp roles:
-//   * warp 2 takes items just in time and publishes them in a 4-slot ring; warps 17-19 split an item's query rows into
+// longest first.  28 warps:
+//   * warps 0 and 3 stream K and V tiles of 128 tokens with TMA, one 16 KB box where the tile's eight pages are
+//     consecutive in the pool, else one box per page; warp 0 also brings the pages' scales;
+//   * warps 1 and 24 issue the MMAs, S^T and PV;
+//   * warp 2 takes items just in time and publishes them in a 4-slot ring; warps 25-27 split an item's query rows into
 //     one of two Q buffers;
-//   * warps 0 and 3 (K and V producers) stream tiles of 128 tokens with TMA, one 16 KB box when the tile's eight pages
-//     are consecutive in the pool, else one box per page; warp 0 also brings the pages' scales;
-//   * warps 1 and 16 issue the MMAs: S^T and PV;
-//   * warps 4-7 and 12-15 (softmax): two groups that take turns by tile, one warp per TMEM lane quadrant: a thread
-//     holds one key's scores for all rows.  A group's four warps agree on the tile's row maxima through shared memory;
-//   * warps 8-11 (correction): thread d keeps head-dim index d of every row's O; they also write the outputs or the
-//     (O, m, l) partials of a split item, whose last chunk merges all.
+//   * warps 4-19, four groups of four: the softmax.  A thread has one key's scores for up to 32 rows.  Items of up to 32
+//     rows: a group has every fourth tile; of more: half of the rows of every second one.  A group's warps agree on the
+//     rows' maxima through shared memory; references go from tile to tile, in order, in a 4-slot ring;
+//   * warps 20-23 write the outputs or the (O, m, l) partials of a split item, whose last chunk merges all.
+//
+// What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
+// SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
+// 4 / 16 / 32 / 36 / 64 rows: 893 / 955 / 1019 / 1477 / 1694 (D = 128; 5.58 TB/s at 4 rows), 679 / 761 / 957 / 1394 / 1600
+// (D = 64).  The bf16 cache's kernel, with twice the bytes: 1468 to 1516 and 823 to 880.  What the choices gave, at 4 / 32 / 64
+// rows of D = 128:
+//   * two groups of warps with O in registers of four correction warps, PV products added there per tile: 990 / 1082 / 1681,
+//     and 1557 at 36 rows, against this one, with O in TMEM;
+//   * groups of at most 24 rows (three or four parts above 32 rows): 955 / 1273 / 2248 against 985 / 1200 / 1701; 16-row parts
+//     pay the group's fixed part (waits, maxima, references: about 230 instructions a warp) twice;
+//   * tensor and TMA instructions issued under elect.sync and not under `lane == 0`: 985 / 1200 / 1701 to 943 / 1129 / 1685;
+//     an MMA took the issuing warp 100 clocks before, 25 after;
+//   * the maxima's loop over a group's rows not unrolled, so that less code goes round: 947 / 1118 / 1658 to 924 / 1080 / 1687;
+//   * a fourth stage for K: 919 / 1081 / 1691 to 893 / 1019 / 1694; for V instead: nothing;
+//   * block ids brought in 12 tiles ahead and scales 8, checked and written four tiles at a time: 1047 to 955 at 4 rows.
 //
 // Every mbarrier wait is bounded in time; an expired wait records WISP_DEV_TIMEOUT and the CTA drains.
 #include "attn_merge.cuh"
@@ -47,14 +64,14 @@ constexpr int kSoftmaxWarps = 16;
 constexpr int kQWarps = 3;
 constexpr uint32_t kTmemCols = 512; // S^T[4] at columns 0, 64, 128, 192, O^T[2] (hi and lo rows) at 256 / 384
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
+constexpr uint32_t kNap = 20000;    // ns
 constexpr uint32_t kAhead = 3;      // the item loader takes the next item when the K producer is this many tiles from
                                     // the end of what is published
-constexpr float kHead = 6.0f;       // log2 of P at a row's reference
-constexpr float kUp = 2.6f;         // a tile's maximum may be this far above the reference (with its rounding: P <= 431, e4m3
-                                    // holds 448)
-constexpr float kDown = 4.0f;       // ... and this far below
+constexpr int kPart = 32;           // rows of a softmax group at most
+constexpr float kHead = 5.0f;       // log2 of P at a row's reference
+constexpr float kUp = 3.6f;         // a tile's maximum may be this far above the reference (P <= 389, e4m3 holds 448)
+constexpr float kDown = 6.0f;       // ... and this far below
 constexpr float kFar = 30.0f;       // what is this far below the largest reference so far weighs nothing
-constexpr float kLazy = 64.0f;      // the correction's running references follow a row's when it is this far above (log2)
 constexpr float kLeastScaleLog2 = -100.0f;  // a V scale of 0 weighs as 2^-100, so that its keys still count in the sums
 static_assert(kNR == 64, "TMEM and shared-memory layout assume 64 rows per item");
 
@@ -63,33 +80,35 @@ struct Cfg {
   static constexpr int KV_TILE = kBT * D;       // bytes of K (or V) of one tile
   static constexpr int Q_BYTES = 2 * kNR * D;   // hi rows, then lo rows
   static constexpr int P_BYTES = kBT * 2 * kNR; // [128 tokens][hi rows, lo rows]
-  static constexpr int NSK = D == 128 ? 3 : 6;  // K ring stages
+  static constexpr int NSK = D == 128 ? 4 : 8;  // K ring stages
   static constexpr int NSV = D == 128 ? 3 : 6;  // V ring stages
   static constexpr int SC = 16;                 // slots of the scales' ring: tile n in n % SC
-  static constexpr int RF = 8;                  // slots of the row factors' ring: item li in li % RF
+  static constexpr int RF = 8;                  // slots of the queries' factors: item li in li % RF
   static constexpr int RING = 4;                // slots of the item ring
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
   static constexpr int OFF_V = OFF_K + NSK * KV_TILE;
   static constexpr int OFF_P = OFF_V + NSV * KV_TILE;
   static constexpr int OFF_BAR = OFF_P + 4 * P_BYTES;
-  static constexpr int N_BAR = 2 * NSK + 2 * NSV + 28 + 2 * RING + 7;
+  static constexpr int N_BAR = 2 * NSK + 2 * NSV + 28 + 2 * RING + 12;
   static constexpr int OFF_SC = (OFF_BAR + N_BAR * 8 + 15) / 16 * 16;  // float2 [SC][8]: a page's K and V scale
-  static constexpr int OFF_RF = OFF_SC + SC * 64;                      // float [RF][64]
-  static constexpr int OFF_RED = OFF_RF + RF * kNR * 4;                // [4 groups][2][4][8] row maxima per quadrant, bf16 pairs
-  static constexpr int OFF_MW = OFF_RED + 4 * 2 * 4 * 8 * 4;           // float [16][16] per warp: kHead - reference
-  static constexpr int OFF_M = OFF_MW + kSoftmaxWarps * 16 * 4;        // float [8][64] references of tile n in n % 8
-  static constexpr int OFF_CW = OFF_M + 8 * kNR * 4;                   // float [4][64] per correction warp
-  static constexpr int OFF_HL = OFF_CW + 4 * kNR * 4;                  // float [2][4 groups][4][16] row-sum shares
-  static constexpr int OFF_LR = OFF_HL + 2 * 4 * 4 * 16 * 4;           // float [2][4 groups][16] their references
-  static constexpr int OFF_NAN = OFF_LR + 2 * 4 * 16 * 4;              // int [2][D] first row that a NaN value reaches
+  static constexpr int OFF_RF = OFF_SC + SC * 64;                      // float [RF]
+  static constexpr int OFF_RED = OFF_RF + RF * 16;                      // float [4 groups][2][4][32] row maxima per quadrant
+  static constexpr int OFF_MW = OFF_RED + 4 * 2 * 4 * 32 * 4;          // float [16][32] per warp: kHead - reference
+  static constexpr int OFF_REF = OFF_MW + kSoftmaxWarps * 32 * 4;      // float4 [4][32] two rows' references, the largest so far
+  static constexpr int OFF_CW = OFF_REF + 4 * kNR * 8;                 // float [4][64] per epilogue warp
+  static constexpr int OFF_HL = OFF_CW + 4 * kNR * 4;                  // float [2][4 groups][4][32] row-sum shares
+  static constexpr int OFF_LR = OFF_HL + 2 * 4 * 4 * 32 * 4;           // float [2][4 groups][32] their references
+  static constexpr int OFF_FIN = OFF_LR + 2 * 4 * 32 * 4;              // float [2][64] O^T's references
+  static constexpr int OFF_NAN = OFF_FIN + 2 * kNR * 4;                // int [2][D] first row that a NaN value reaches
   static constexpr int OFF_MISC = OFF_NAN + 2 * D * 4;
-  static constexpr int OFF_RING = OFF_MISC + 32;
+  static constexpr int OFF_RING = OFF_MISC + 64;
   static constexpr int SMEM = OFF_RING + RING * 64 + 1024;             // + slack to align the base to 1024
   static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
   static_assert(OFF_K % 1024 == 0 && OFF_V % 1024 == 0 && OFF_P % 1024 == 0 && OFF_RING % 16 == 0, "alignment");
-  // a slot is written again once S^T of its tile (or item) and of the tiles NSK (items 2) after it has been read
-  static_assert(SC >= NSK + 4 && RF >= 5, "rings");
+  // A tile's scales are written up to three tiles ahead of its K: then S^T of the tile NSK before that K's is done and the
+  // scores of the tile NSK + 4 before have been read.  An item's factor is written two items ahead.
+  static_assert(SC >= NSK + 4 + 3 && RF >= 5, "rings");
 };
 
 // The CTA's mbarriers: shared-memory addresses at constant offsets from one base.
@@ -101,24 +120,28 @@ struct Bars {
   static constexpr int Q_FULL = V_EMPTY + C::NSV, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, S_EMPTY = S_FULL + 4;
   static constexpr int P_FULL = S_EMPTY + 4;   // [4] P of tile n in buffer n & 3
   static constexpr int P_EMPTY = P_FULL + 4;   // [4] PV of tile n is done
-  static constexpr int O_FULL = P_EMPTY + 4;   // [2] ... and its O is complete
-  static constexpr int O_EMPTY = O_FULL + 2;   // [2] the correction warps have read it
+  static constexpr int O_FULL = P_EMPTY + 4;   // [2] per item parity: its last PV is done
+  static constexpr int O_EMPTY = O_FULL + 2;   // [2] the epilogue warps have read O^T
   static constexpr int EP_FULL = O_EMPTY + 2;  // [2] per item parity: the softmax warps handed their sums over
-  static constexpr int EP_EMPTY = EP_FULL + 2; // [2] the correction warps have read them
+  static constexpr int EP_EMPTY = EP_FULL + 2; // [2] the epilogue warps have read them
   static constexpr int MMA_DONE = EP_EMPTY + 2;  // the two MMA issuers, at the end
   static constexpr int IT_FULL = MMA_DONE + 1, IT_EMPTY = IT_FULL + C::RING;
-  static constexpr int EGRP = IT_EMPTY + C::RING;  // the correction warps
+  static constexpr int EGRP = IT_EMPTY + C::RING;  // the epilogue warps
   static constexpr int RED = EGRP + 1;         // [4] per softmax group: its four warps, once per tile
-  static constexpr int FIN = RED + 4;          // every warp, once: its last access to TMEM is done
+  static constexpr int DEC = RED + 4;          // [4] the references after tile n stand in slot n & 3
+  static constexpr int QX = DEC + 4;           // the Q loaders have an item's largest magnitude
+  static constexpr int FIN = QX + 1;          // every warp, once: its last access to TMEM is done
   static_assert(FIN + 1 <= C::N_BAR, "barrier count");
   __device__ __forceinline__ uint32_t at(int i) const { return base + 8 * i; }
 };
 
+// (The thread is suspended while it waits, for kNap ns at a time: without, the tries of two dozen waiting warps took a third
+// of the SM's instructions.)
 __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort) {
-  if (ptx::mbar_try_wait(b, parity)) return true;
+  if (ptx::mbar_try_wait_sleep(b, parity, kNap)) return true;
   const long long t0 = clock64();
   while (true) {
-    if (ptx::mbar_try_wait(b, parity)) return true;
+    if (ptx::mbar_try_wait_sleep(b, parity, kNap)) return true;
     if (*abort) return false;
     if (clock64() - t0 > kWaitCycles) {
       *abort = 1;
@@ -133,10 +156,11 @@ __device__ __forceinline__ bool item_ok(const AttnParams &p, const WorkItem &w) 
          w.row0 >= 0 && w.nrg >= 1 && w.nrg <= p.row_groups && w.rg >= 0 && w.rg < w.nrg;
 }
 
-// Transposing sum over the 32 lanes of a warp (v is consumed): lanes i and 16 + i get the sum over all lanes of v[i].
-__device__ __forceinline__ float warp_transpose_sum(float (&v)[16], int lane) {
+// Transposing sum over the 32 lanes of a warp (v is consumed): on return lane i holds the sum over all
+// lanes of v[i].
+__device__ __forceinline__ float warp_transpose_sum(float (&v)[32], int lane) {
 #pragma unroll
-  for (int w = 8; w >= 1; w >>= 1) {
+  for (int w = 16; w >= 1; w >>= 1) {
     const bool up = (lane & w) != 0;
 #pragma unroll
     for (int i = 0; i < w; ++i) {
@@ -145,29 +169,14 @@ __device__ __forceinline__ float warp_transpose_sum(float (&v)[16], int lane) {
       v[i] = keep + __shfl_xor_sync(0xffffffffu, send, w);
     }
   }
-  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
+  return v[0];
 }
 
-__device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {  // NaN never wins
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
-// Transposing maximum of bf16 pairs over the 32 lanes of a warp (v is consumed): lane i gets that of v[i & 7].
-__device__ __forceinline__ uint32_t warp_transpose_max(uint32_t (&v)[8], int lane) {
-#pragma unroll
-  for (int w = 4; w >= 1; w >>= 1) {
-    const bool up = (lane & w) != 0;
-#pragma unroll
-    for (int i = 0; i < w; ++i) {
-      const uint32_t keep = up ? v[i + w] : v[i];
-      const uint32_t send = up ? v[i] : v[i + w];
-      v[i] = bmax2(keep, __shfl_xor_sync(0xffffffffu, send, w));
-    }
-  }
-  const uint32_t y = bmax2(v[0], __shfl_xor_sync(0xffffffffu, v[0], 8));
-  return bmax2(y, __shfl_xor_sync(0xffffffffu, y, 16));
+// The largest of the lanes' values (a NaN never is).
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ float lg2(float x) {
@@ -175,23 +184,34 @@ __device__ __forceinline__ float lg2(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// The parts of an item's rows (rounded up to 8), one, two or four of at most 16 rows, in whole units of 8: part i starts
-// at row(i).
+
+// The parts of an item's rows (rounded up to 8), one or two of at most kPart rows, in whole units of 8: part i starts at
+// row(i).
 struct Parts {
   int n, units;
-  __device__ __forceinline__ explicit Parts(int nrow) : n(nrow <= 16 ? 1 : nrow <= 32 ? 2 : 4), units(nrow / 8) {}
+  __device__ __forceinline__ explicit Parts(int nrow) : n(nrow <= kPart ? 1 : 2), units(nrow / 8) {}
   __device__ __forceinline__ int row(int i) const { return i * units / n * 8; }
 };
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
-// hi and lo codes (two of each) of two values of magnitude at most 448: x = hi + lo, or hi + lo / 16 (S16)
-template <bool S16>
-__device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
-  hi = e4m3x2(a, b);
-  const uint32_t h = e4m3x2_to_h2(hi);
-  __half2 r = __hsub2(__floats2half2_rn(a, b), *reinterpret_cast<const __half2 *>(&h));
-  if (S16) r = __hmul2(r, __floats2half2_rn(16.0f, 16.0f));
-  lo = e4m3x2_h(*reinterpret_cast<const uint32_t *>(&r));
+// Four values of magnitude at most 448 as hi + lo, four e4m3 codes each: lo is what hi's rounding left (exact in fp16),
+// rounded.
+__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t &hi, uint32_t &lo) {
+  asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 p0, p1, q0, q1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h0, %3, %2;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h1, %5, %4;\n\t"
+      "cvt.rn.f16x2.f32 p0, %3, %2;\n\t"
+      "cvt.rn.f16x2.f32 p1, %5, %4;\n\t"
+      "cvt.rn.f16x2.e4m3x2 q0, h0;\n\t"
+      "cvt.rn.f16x2.e4m3x2 q1, h1;\n\t"
+      "sub.rn.f16x2 p0, p0, q0;\n\t"
+      "sub.rn.f16x2 p1, p1, q1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l0, p0;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l1, p1;\n\t"
+      "mov.b32 %0, {h0, h1};\n\t"
+      "mov.b32 %1, {l0, l1};\n\t}"
+      : "=r"(hi), "=r"(lo)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
 }
 
 // Byte offset of 16-byte chunk c of row `row` in a swizzled tile with rows of D bytes.
@@ -218,8 +238,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t sbase = ptx::smem_u32(smem);
   const BR B{sbase + C::OFF_BAR};
   float2 *s_sc = reinterpret_cast<float2 *>(smem + C::OFF_SC);
-  float *s_rf = reinterpret_cast<float *>(smem + C::OFF_RF);
-  float *s_m = reinterpret_cast<float *>(smem + C::OFF_M);
+  float *s_qf = reinterpret_cast<float *>(smem + C::OFF_RF);
+  volatile uint32_t *s_qmax = reinterpret_cast<volatile uint32_t *>(smem + C::OFF_MISC + 32);
+  float4 *s_ref = reinterpret_cast<float4 *>(smem + C::OFF_REF);
+  float *s_fin = reinterpret_cast<float *>(smem + C::OFF_FIN);
   float *s_hl = reinterpret_cast<float *>(smem + C::OFF_HL);
   float *s_lr = reinterpret_cast<float *>(smem + C::OFF_LR);
   int *s_nan = reinterpret_cast<int *>(smem + C::OFF_NAN);
@@ -245,18 +267,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(BR::Q_FULL, 2, kQWarps);
     init(BR::Q_EMPTY, 2, 1);
     init(BR::S_FULL, 4, 1);
-    init(BR::S_EMPTY, 4, 16);  // the warps of the tile's softmax groups, four, two or one arrival each
+    init(BR::S_EMPTY, 4, 16);  // the warps of the tile's softmax groups, four or two arrivals each
     init(BR::P_FULL, 4, 16);
     init(BR::P_EMPTY, 4, 1);
     init(BR::O_FULL, 2, 1);
-    init(BR::O_EMPTY, 2, 4);   // the correction warps
+    init(BR::O_EMPTY, 2, 4);   // the epilogue warps
     init(BR::EP_FULL, 2, kSoftmaxWarps);
     init(BR::EP_EMPTY, 2, 4);
     init(BR::MMA_DONE, 1, 2);
     init(BR::IT_FULL, C::RING, 1);
     init(BR::IT_EMPTY, C::RING, 4 + kQWarps + kSoftmaxWarps + 4);  // KV producers, MMA issuers, Q, softmax, correction
     init(BR::EGRP, 1, 4);
+    init(BR::QX, 1, kQWarps);
     init(BR::RED, 4, 4);       // a group's warps
+    init(BR::DEC, 4, 16);      // the warps of the tile's softmax groups, as for S_EMPTY
     init(BR::FIN, 1, kThreads / 32);
     *s_issued = 0;
     *s_abort = 0;
@@ -321,7 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = false;
             break;
           }
-          if (lane == 0) {
+          __syncwarp();
+          if (ptx::elect_one()) {
             ptx::tc_fence_after();
             const uint64_t kd = sdesc<D>(sbase + C::OFF_K + st * C::KV_TILE);
 #pragma unroll
@@ -336,33 +361,36 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
       } else {
-        // PV(n): P(n) is published, V(n) has landed, the accumulator has been read.  A = V^T, MN-major (for D = 64
-        // both halves of M read the same 64 columns: lanes 64..127 repeat lanes 0..63 and are not used)
+        // PV(n): P(n) is published, V(n) has landed and, for an item's first tile, the accumulator has been read.  A = V^T,
+        // MN-major (for D = 64 both halves of M read the same 64 columns: lanes 64..127 repeat lanes 0..63 and are not used)
         const uint32_t idesc = ptx::idesc_e4m3_f32(128, (rows + 7) / 8 * 16, true, true);  // N: hi and lo of the rows
+        const int ob = li & 1;
         for (int t = 0; t < nt; ++t, ++n) {
-          const int st = (int)(n % C::NSV), b = n & 1, pb = n & 3;
-          if (!wait_bar(B.at(BR::O_EMPTY + b), ((n >> 1) & 1) ^ 1, s_abort) ||
+          const int st = (int)(n % C::NSV), pb = n & 3;
+          if ((t == 0 && !wait_bar(B.at(BR::O_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) ||
               !wait_bar(B.at(BR::V_FULL + st), (n / C::NSV) & 1, s_abort) ||
               !wait_bar(B.at(BR::P_FULL + pb), (n >> 2) & 1, s_abort)) {
             ok = false;
             break;
           }
-          if (lane == 0) {
+          __syncwarp();
+          if (ptx::elect_one()) {
             ptx::tc_fence_after();
             const uint64_t vd = sdesc<D>(sbase + C::OFF_V + st * C::KV_TILE);
             const uint64_t pd = ptx::sdesc_sw128(sbase + C::OFF_P + pb * C::P_BYTES, C::P_BYTES, 1024);
 #pragma unroll
             for (int ks = 0; ks < kBT / 32; ++ks)
-              ptx::umma_f8(tmem + 256 + b * 128, vd + ((ks * 32 * D) >> 4), pd + ((ks * 32 * 128) >> 4), idesc, ks > 0);
-            ptx::umma_commit(B.at(BR::O_FULL + b));
+              ptx::umma_f8(tmem + 256 + ob * 128, vd + ((ks * 32 * D) >> 4), pd + ((ks * 32 * 128) >> 4), idesc, t > 0 || ks > 0);
             ptx::umma_commit(B.at(BR::P_EMPTY + pb));
             ptx::umma_commit(B.at(BR::V_EMPTY + st));
+            if (t == nt - 1) ptx::umma_commit(B.at(BR::O_FULL + ob));
           }
           __syncwarp();
         }
       }
     }
-    if (lane == 0) {
+    __syncwarp();
+    if (ptx::elect_one()) {
       // every MMA the issuers issued must finish before the TMEM is released
       ptx::umma_commit(B.at(BR::MMA_DONE));
       const long long c0 = clock64();
@@ -371,22 +399,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   };
 
-  // registers: 28 warps launch with 72 each, 2016 a lane in all = 16 x 72 + 4 x 120 + 8 x 48.  (Each split stands at the
+  // registers: 28 warps launch with 72 each, 2016 a lane in all = 16 x 88 + 4 x 72 + 8 x 40.  (Each split stands at the
   // head of its own branch: after a join the compiler counts with the least.)
   const int wg = warp >> 2;
   if (wg >= 1 && wg <= 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
     // ------------------------------------------------------------------ softmax warps
-    // Four groups of four warps, a group at most 16 rows of a tile: up to 16 rows the groups take turns by tile, up to 32
-    // two pairs of groups do, a half of the rows each, and above that each group takes a quarter of the rows of every
-    // tile.  A thread holds one key's scores for the group's rows and its share of their sums.  A group's four warps
-    // agree on the rows' maxima over the tile, and from them on P's references: a row's reference follows its maximum when that
-    // leaves [-4, 2.6] around it.
+    // A group's four warps, one per TMEM lane quadrant, have at most 32 rows of a tile: of up to 32 rows the groups take
+    // turns by tile, of more two pairs of groups do, a half of the rows each.  A thread holds one key's scores for the
+    // group's rows and its share of their sums.  The warps agree on the rows' maxima over the tile, and from them and the
+    // references after the tile before on P's references.
     const int qd = warp & 3;                // TMEM lane quadrant: keys 32*qd .. 32*qd + 31 of a tile
     const int grp = wg - 1;
     const uint32_t lane_addr = (uint32_t)(qd * 32) << 16;
-    const int l8 = lane & 7;
-    float *mw = reinterpret_cast<float *>(smem + C::OFF_MW) + (grp * 4 + qd) * 16;  // kHead - reference per row, this warp's copy
-    uint32_t *red = reinterpret_cast<uint32_t *>(smem + C::OFF_RED) + grp * 2 * 4 * 8;
+    const int lw = min(lane & 15, kPart / 2 - 1);
+    float *mw = reinterpret_cast<float *>(smem + C::OFF_MW) + (grp * 4 + qd) * 32;  // kHead - reference per row, this warp's copy
+    float4 *red = reinterpret_cast<float4 *>(smem + C::OFF_RED) + grp * 2 * 4 * 8;
     uint32_t n0 = 0;                        // tiles before the item
     uint32_t mine = 0;                      // tiles of this group so far
     int li = 0;
@@ -409,125 +437,161 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int turns = 4 / pt.n, part = grp / turns;
       const int r0 = pt.row(part);                   // the group's rows: r0 .. r0 + 8 nu - 1
       const int nu = (pt.row(part + 1) - r0) / 8;
-      const uint32_t share = turns;                  // a warp's arrivals per tile (sixteen in all)
-      const float *rf = s_rf + (li % C::RF) * kNR + r0;
-      float2 lp[8];  // this thread's (key's) share of every row sum
+      float2 lp[kPart / 2];  // this thread's (key's) share of every row sum
 #pragma unroll
-      for (int i = 0; i < 8; ++i) lp[i] = make_float2(0.0f, 0.0f);
-      float m[2] = {-INFINITY, -INFINITY};    // the references, rows r0 + 2 l8 and the next
-      float most[2] = {-INFINITY, -INFINITY}; // the largest so far
+      for (int i = 0; i < kPart / 2; ++i) lp[i] = make_float2(0.0f, 0.0f);
+      float m[2] = {-INFINITY, -INFINITY};    // the references that lp counts in, rows r0 + 2 lw and the next
       float lsv0 = 0.0f;                      // log2 of V's scale at the group's first key: the sums count in its inverse
-      if (lane < 16) mw[lane] = 0.0f;         // (a row without a reference: its weights are 2^-inf)
+      if (lane < kPart) mw[lane] = 0.0f;      // (a row without a reference: its weights are 2^-inf)
       __syncwarp();
+      float qf = 0.0f;                        // the queries' factor
       bool fresh = true;
       for (int t = (grp - (int)n0) & (turns - 1); t < ntiles; t += turns, ++mine) {
         const uint32_t n = n0 + t;
         const int buf = n & 3;
         if (!wait_bar(B.at(BR::S_FULL + buf), (n >> 2) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
-        uint32_t v[16];
-        ptx::tmem_ld16(tmem + lane_addr + buf * kNR + r0, v);
         const float2 sc = s_sc[(n % C::SC) * 8 + qd * 2 + (lane >> 4)];
         const float lsv = fmaxf(lg2(sc.y), kLeastScaleLog2);
         if (fresh) {
+          qf = s_qf[li % C::RF];
           lsv0 = fmaxf(lg2(s_sc[(n % C::SC) * 8].y), kLeastScaleLog2);
           fresh = false;
         }
-        ptx::tmem_wait_ld();
-        // the scores are in registers: the tile may be overwritten
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::S_EMPTY + buf), share);
-        float x[16];  // in log2 units, plus log2 of V's scale
+        const float fk = sc.x * qf;
+        // the scores of unit u (log2 units, plus log2 of V's scale).  Causal mask: key tok is visible to row jr iff
+        // row0 + jr >= g * (tok - ctx); keys past the item are masked too.  Only an item's last tiles (from nfull on)
+        // have such keys.
+        auto scores = [&](int u, float (&x)[8]) {
+          uint32_t v[8];
+          ptx::tmem_ld8(tmem + lane_addr + buf * kNR + r0 + 8 * u, v);
+          ptx::tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const float4 r4 = *reinterpret_cast<const float4 *>(rf + i);
+          for (int i = 0; i < 4; ++i) {
+            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), both(fk), both(lsv));
+            x[2 * i] = y.x;
+            x[2 * i + 1] = y.y;
+          }
+          if (__builtin_expect(t >= nfull, 0)) {
+            const int tok = t0 + t * kBT + qd * 32 + lane;
+            const int jmin = tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0 - r0));
 #pragma unroll
-          for (int q = 0; q < 4; q += 2) {
-            const float2 u = __fmul2_rn(q == 0 ? make_float2(r4.x, r4.y) : make_float2(r4.z, r4.w), both(sc.x));
-            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[i + q]), __uint_as_float(v[i + q + 1])), u, both(lsv));
-            x[i + q] = y.x;
-            x[i + q + 1] = y.y;
+            for (int i = 0; i < 8; ++i)
+              if (8 * u + i < jmin) x[i] = -INFINITY;
+          }
+        };
+        float4 *rd = red + (mine & 1) * 4 * 8;
+#pragma unroll 1
+        for (int u = 0; u < kPart / 8; ++u) {
+          if (u < nu) {
+            float x[8];
+            scores(u, x);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = warp_max(x[i]);
+            if (lane == 0) {
+              rd[qd * 8 + 2 * u] = make_float4(y[0], y[1], y[2], y[3]);
+              rd[qd * 8 + 2 * u + 1] = make_float4(y[4], y[5], y[6], y[7]);
+            }
           }
         }
-        // Causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked too.
-        // Only an item's last tiles (from nfull on) have such keys.
-        if (__builtin_expect(t >= nfull, 0)) {
-          const int tok = t0 + t * kBT + qd * 32 + lane;
-          const int jmin = tok >= t1 ? 16 : max(0, min(16, g * max(tok - ctx, 0) - row0 - r0));
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (i < jmin) x[i] = -INFINITY;
-        }
-        // the rows' maxima over this warp's keys as bf16 pairs (lane i & 7 gets rows 2 i and 2 i + 1), then the group's
-        uint32_t wd[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) wd[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        uint32_t top = warp_transpose_max(wd, lane);
-        uint32_t *rd = red + (mine & 1) * 4 * 8;
-        if (lane < 8) rd[qd * 8 + lane] = top;
+        // ... then the group's, and the references after the tile before
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(B.at(BR::RED + grp));
-        if (!wait_bar(B.at(BR::RED + grp), mine & 1, s_abort)) { ok = false; break; }
-        top = bmax2(bmax2(rd[l8], rd[8 + l8]), bmax2(rd[16 + l8], rd[24 + l8]));
-        {
-          // (rounded up: 2^-8 of their magnitude covers the rounding to bf16)
-          float now[2] = {__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)};
-          bool move[2];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            if (now[y] != -INFINITY) now[y] = fmaf(fabsf(now[y]), 0x1p-8f, now[y]);
-            move[y] = !(now[y] <= m[y] + kUp) || (now[y] < m[y] - kDown && now[y] > most[y] - kFar);  // (a NaN too)
-          }
-          if (__any_sync(0xffffffffu, move[0] || move[1])) {
-            float al[2];
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              al[y] = 1.0f;
-              if (move[y]) {
-                if (m[y] != -INFINITY) al[y] = ptx::ex2(m[y] - now[y]);
-                m[y] = now[y];
-                most[y] = !(now[y] <= most[y]) ? now[y] : most[y];
-              }
-            }
-            if (lane < 8)
-              reinterpret_cast<float2 *>(mw)[lane] = make_float2(m[0] == -INFINITY ? 0.0f : kHead - m[0], m[1] == -INFINITY ? 0.0f : kHead - m[1]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
-              lp[i] = __fmul2_rn(lp[i], make_float2(a0, a1));
-            }
-            __syncwarp();
-          }
+        if (!wait_bar(B.at(BR::RED + grp), mine & 1, s_abort) ||
+            (n > 0 && !wait_bar(B.at(BR::DEC + ((n - 1) & 3)), ((n - 1) >> 2) & 1, s_abort))) {
+          ok = false;
+          break;
         }
-        // P buffer n & 3 is free again once PV(n - 4) is done (and the references of tile n - 8 have been read by then)
+        float2 top = reinterpret_cast<const float2 *>(rd)[lw];  // (of rows that the group has)
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+          const float2 y = reinterpret_cast<const float2 *>(rd + 8 * i)[lw];
+          top = make_float2(fmaxf(top.x, y.x), fmaxf(top.y, y.y));
+        }
+        if (lw >= 4 * nu) top = both(-INFINITY);
+        float4 ref = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);  // two rows' references, the largest so far
+        if (t > 0) ref = s_ref[((n - 1) & 3) * (kNR / 2) + r0 / 2 + lw];
+        const float old[2] = {ref.x, ref.y};
+        // (a NaN moves a reference, too)
+        if (!(top.x <= ref.x + kUp) || (top.x < ref.x - kDown && top.x > ref.z - kFar)) {
+          ref.x = top.x;
+          ref.z = !(top.x <= ref.z) ? top.x : ref.z;
+        }
+        if (!(top.y <= ref.y + kUp) || (top.y < ref.y - kDown && top.y > ref.w - kFar)) {
+          ref.y = top.y;
+          ref.w = !(top.y <= ref.w) ? top.y : ref.w;
+        }
+        if (qd == 0 && lane < 4 * nu) s_ref[(n & 3) * (kNR / 2) + r0 / 2 + lane] = ref;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::DEC + buf), turns);
+        // (a NaN differs from itself: its sums become NaN, whatever the factor)
+        if (__builtin_expect(__any_sync(0xffffffffu, ref.x != m[0] || ref.y != m[1]), 0)) {
+          const float a0 = m[0] == -INFINITY || ref.x == m[0] ? 1.0f : ptx::ex2(m[0] - ref.x);
+          const float a1 = m[1] == -INFINITY || ref.y == m[1] ? 1.0f : ptx::ex2(m[1] - ref.y);
+#pragma unroll
+          for (int i = 0; i < kPart / 2; ++i)
+            lp[i] = __fmul2_rn(lp[i], make_float2(__shfl_sync(0xffffffffu, a0, i), __shfl_sync(0xffffffffu, a1, i)));
+          m[0] = ref.x;
+          m[1] = ref.y;
+          if (lane < kPart / 2)
+            reinterpret_cast<float2 *>(mw)[lane] = make_float2(m[0] == -INFINITY ? 0.0f : kHead - m[0], m[1] == -INFINITY ? 0.0f : kHead - m[1]);
+          __syncwarp();
+        }
+        // P buffer n & 3 is free again once PV(n - 4) is done
         if (!wait_bar(B.at(BR::P_EMPTY + buf), ((n >> 2) & 1) ^ 1, s_abort)) { ok = false; break; }
-        if (qd == 0 && lane < 4 * nu) reinterpret_cast<float2 *>(s_m + (n & 7) * kNR + r0)[lane] = make_float2(m[0], m[1]);
-        // P = 2^(s - m + kHead), its shares of the sums, its two parts
+        if (__builtin_expect(t > 0 && __any_sync(0xffffffffu, ref.x != old[0] || ref.y != old[1]), 0)) {
+          // O^T so far counts in the references before: PV(n - 1) is the last product on it
+          if (!wait_bar(B.at(BR::P_EMPTY + ((n - 1) & 3)), ((n - 1) >> 2) & 1, s_abort)) { ok = false; break; }
+          ptx::tc_fence_after();
+          const float f0 = old[0] == -INFINITY || ref.x == old[0] ? 1.0f : ptx::ex2(old[0] - ref.x);
+          const float f1 = old[1] == -INFINITY || ref.y == old[1] ? 1.0f : ptx::ex2(old[1] - ref.y);
+#pragma unroll 1
+          for (int u = 0; u < 2 * nu; ++u) {  // hi, then lo
+            const uint32_t at = tmem + lane_addr + 256 + ob * 128 + (u < nu ? r0 + 8 * u : nrow + r0 + 8 * (u - nu));
+            const int from = 4 * (u < nu ? u : u - nu);  // the lane of the rows' factors
+            uint32_t y[8];
+            ptx::tmem_ld8(at, y);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              y[i] = __float_as_uint(__uint_as_float(y[i]) * __shfl_sync(0xffffffffu, i & 1 ? f1 : f0, from + i / 2));
+            ptx::tmem_st8(at, y);
+          }
+          ptx::tmem_wait_st();
+          ptx::tc_fence_before();
+          __syncwarp();
+        }
+        // P = 2^(s - reference + kHead), its shares of the sums, its two parts
         const float2 inv2 = both(ptx::ex2(lsv0 - lsv));
         uint8_t *prow = smem + C::OFF_P + buf * C::P_BYTES + (qd * 32 + lane) * 128;
         const int sw = lane & 7;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < kPart / 8; ++u) {
           if (u < nu) {
-            uint32_t hi[4], lo[4];
+            float x[8];
+            scores(u, x);
+            uint32_t hi[2], lo[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float4 m4 = reinterpret_cast<const float4 *>(mw + 8 * u)[h];
-#pragma unroll
-              for (int q = 0; q < 2; ++q) {
-                const int i = 8 * u + 4 * h + 2 * q;
-                const float2 a = __fadd2_rn(make_float2(x[i], x[i + 1]), q == 0 ? make_float2(m4.x, m4.y) : make_float2(m4.z, m4.w));
-                const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
-                lp[i >> 1] = __ffma2_rn(e, inv2, lp[i >> 1]);
-                split2<true>(e.x, e.y, hi[2 * h + q], lo[2 * h + q]);
-              }
+              const int i = 4 * h;
+              const float2 a = __fadd2_rn(make_float2(x[i], x[i + 1]), make_float2(m4.x, m4.y));
+              const float2 c = __fadd2_rn(make_float2(x[i + 2], x[i + 3]), make_float2(m4.z, m4.w));
+              const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y)), f = make_float2(ptx::ex2(c.x), ptx::ex2(c.y));
+              lp[4 * u + 2 * h] = __ffma2_rn(e, inv2, lp[4 * u + 2 * h]);
+              lp[4 * u + 2 * h + 1] = __ffma2_rn(f, inv2, lp[4 * u + 2 * h + 1]);
+              split4(e.x, e.y, f.x, f.y, hi[h], lo[h]);
             }
             const int oh = r0 + 8 * u, ol = nrow + oh;
-            *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-            *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+            *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0], hi[1]);
+            *reinterpret_cast<uint2 *>(prow + (((ol >> 4) ^ sw) << 4) + (ol & 8)) = make_uint2(lo[0], lo[1]);
           }
         }
+        // the scores have been read: the tile may be overwritten
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::S_EMPTY + buf), turns);
         if (__builtin_expect(t >= nfull && part == 0, 0)) {
           // slots past the request's tokens hold anything, and a NaN times a weight of zero is NaN: zeros in their
           // place.  A value of the new tokens that is NaN is taken out, too, and put back at the end for the rows
@@ -574,35 +638,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         // P(n) is published
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::P_FULL + buf), share);
+        if (lane == 0) ptx::mbar_arrive_n(B.at(BR::P_FULL + buf), turns);  // (sixteen in all)
       }
       if (!ok) break;
       n0 += ntiles;
-      // ---- hand the sums over to the correction warps, which must be done with those of item li - 2
-      float ls[16];
+      // ---- hand the sums over to the epilogue warps, which must be done with those of item li - 2
+      float ls[32];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ls[i] = i & 1 ? lp[i >> 1].y : lp[i >> 1].x;
+      for (int i = 0; i < 32; ++i) ls[i] = i >= kPart ? 0.0f : i & 1 ? lp[i >> 1].y : lp[i >> 1].x;
       const float sum = warp_transpose_sum(ls, lane);
       if (!wait_bar(B.at(BR::EP_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
-      if (lane < 16) s_hl[((ob * 4 + grp) * 4 + qd) * 16 + lane] = sum;
-      if (qd == 0 && lane < 8)
-        reinterpret_cast<float2 *>(s_lr + (ob * 4 + grp) * 16)[lane] = make_float2(m[0] - lsv0 - kHead, m[1] - lsv0 - kHead);
+      s_hl[((ob * 4 + grp) * 4 + qd) * 32 + lane] = sum;
+      if (qd == 0 && lane < kPart / 2) {
+        reinterpret_cast<float2 *>(s_lr + (ob * 4 + grp) * 32)[lane] = make_float2(m[0] - lsv0 - kHead, m[1] - lsv0 - kHead);
+        // (the group of the last tile has the references of O^T)
+        if (((n0 - 1 - grp) & (turns - 1)) == 0 && lane < 4 * nu) reinterpret_cast<float2 *>(s_fin + ob * kNR + r0)[lane] = make_float2(m[0], m[1]);
+      }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_FULL + ob));
     }
   } else if (wg == 5) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
-    // ------------------------------------------------------------------ correction warps
-    // Thread d (lane d of O^T) keeps head-dim index d of every row: acc += (hi + lo / 16) 2^(m - M - 8) per tile, M a
-    // row's reference, which follows its maximum when that is 2^64 above.
+    // ------------------------------------------------------------------ epilogue warps
+    // Thread d (lane d of O^T) writes head-dim index d of every row once the item's last product is done.
     const int qd = warp & 3;
     const int d = qd * 32 + lane;
     const bool dval = d < D;  // for D = 64 the upper two quadrants hold copies
     const uint32_t lane_addr = (uint32_t)(qd * 32) << 16;
     float *cw = reinterpret_cast<float *>(smem + C::OFF_CW) + qd * kNR;
-    uint32_t gph = 0, n = 0;
+    uint32_t gph = 0, n0 = 0;
     int li = 0;
-    // barrier of the four correction warps (an mbarrier, so that the wait is bounded)
+    // barrier of the four epilogue warps (an mbarrier, so that the wait is bounded)
     auto group_sync = [&]() -> bool {
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EGRP));
@@ -617,131 +682,75 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
       if (it < 0) break;
       const int ob = li & 1, nrow = (w.rows + 7) / 8 * 8;
-      const int ntiles = (w.t1 - w.t0 + kBT - 1) / kBT;
-      float2 acc[kNR / 2];
-#pragma unroll
-      for (int i = 0; i < kNR / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
-      float M[2] = {-INFINITY, -INFINITY};  // rows 2 lane and 2 lane + 1
-      for (int t = 0; t < ntiles; ++t, ++n) {
-        const int b = n & 1;
-        if (!wait_bar(B.at(BR::O_FULL + b), (n >> 1) & 1, s_abort)) { ok = false; break; }
-        ptx::tc_fence_after();
-        bool move = false;
-        const float2 m2 = reinterpret_cast<const float2 *>(s_m + (n & 7) * kNR)[lane];
-        const float m[2] = {m2.x, m2.y};
-        float al[2], f[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          al[x] = 1.0f;
-          if (!(m[x] <= M[x] + kLazy)) {  // (a NaN too)
-            if (M[x] != -INFINITY) {
-              al[x] = ptx::ex2(M[x] - m[x]);
-              move = true;
-            }
-            M[x] = m[x];
-          }
-          f[x] = m[x] == -INFINITY ? 0.0f : ptx::ex2(m[x] - M[x] - kHead);
-        }
-        reinterpret_cast<float2 *>(cw)[lane] = make_float2(f[0], f[1]);
-        if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
-#pragma unroll
-          for (int i = 0; i < kNR / 2; ++i) {
-            const float a0 = __shfl_sync(0xffffffffu, al[0], i), a1 = __shfl_sync(0xffffffffu, al[1], i);
-            acc[i] = __fmul2_rn(acc[i], make_float2(a0, a1));
-          }
-        }
-        __syncwarp();
-        const uint32_t at = tmem + lane_addr + 256 + b * 128;
-#pragma unroll
-        for (int c = 0; c < kNR / 8; ++c) {
-          if (8 * c < nrow) {
-            uint32_t hi[8], lo[8];
-            ptx::tmem_ld8(at + 8 * c, hi);
-            ptx::tmem_ld8(at + nrow + 8 * c, lo);
-            ptx::tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-              const float4 f4 = *reinterpret_cast<const float4 *>(cw + 8 * c + i);
-#pragma unroll
-              for (int q = 0; q < 4; q += 2) {
-                const float2 o = __ffma2_rn(make_float2(__uint_as_float(lo[i + q]), __uint_as_float(lo[i + q + 1])), both(0.0625f),
-                                            make_float2(__uint_as_float(hi[i + q]), __uint_as_float(hi[i + q + 1])));
-                acc[4 * c + (i + q) / 2] = __ffma2_rn(o, q == 0 ? make_float2(f4.x, f4.y) : make_float2(f4.z, f4.w), acc[4 * c + (i + q) / 2]);
-              }
-            }
-          }
-        }
-        ptx::tc_fence_before();
-        __syncwarp();  // (cw has been read, too)
-        if (lane == 0) ptx::mbar_arrive(B.at(BR::O_EMPTY + b));
-      }
-      if (!ok || !wait_bar(B.at(BR::EP_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
-      // the row sums: four shares of each group that had the row, against its references.  The group that had the
+      if (!wait_bar(B.at(BR::EP_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
+      // The row sums: four shares of each group that had the row, against its references.  The group that had the
       // item's first tile comes first, so that results repeat to the bit whatever the CTA did before.
       const int nan0 = dval ? s_nan[ob * D + d] : INT32_MAX;
       if (dval) s_nan[ob * D + d] = INT32_MAX;
+      const float2 fin = reinterpret_cast<const float2 *>(s_fin + ob * kNR)[lane];  // rows 2 lane and 2 lane + 1
       float l[2] = {0.0f, 0.0f};
       {
         const Parts pt(nrow);
-        int part = 0;  // of rows 2 lane and 2 lane + 1
-        for (int i = 1; i < pt.n; ++i) part += 2 * lane >= pt.row(i);
-        const int at = (2 * lane - pt.row(part)) / 2 & 7, turns = 4 / pt.n, first = (int)(n - ntiles);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= turns) break;
+        int part = 0;  // of the two rows
+        if (pt.n == 2) part = 2 * lane >= pt.row(1);
+        const int at = min((2 * lane - pt.row(part)) / 2, 15), turns = 4 / pt.n, first = (int)n0;
+#pragma unroll 1
+        for (int i = 0; i < turns; ++i) {
           const int gr = part * turns + ((first + i) & (turns - 1));
-          const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 4 + gr) * 4 * 16) + at;
-          const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 4 + gr) * 16)[at];
-          const float2 h0 = hl[0], h1 = hl[8], h2 = hl[16], h3 = hl[24];
-          if (lr.x != -INFINITY) l[0] = fmaf((h0.x + h1.x) + (h2.x + h3.x), ptx::ex2(lr.x - M[0]), l[0]);
-          if (lr.y != -INFINITY) l[1] = fmaf((h0.y + h1.y) + (h2.y + h3.y), ptx::ex2(lr.y - M[1]), l[1]);
+          const float2 *hl = reinterpret_cast<const float2 *>(s_hl + (ob * 4 + gr) * 4 * 32) + at;
+          const float2 lr = reinterpret_cast<const float2 *>(s_lr + (ob * 4 + gr) * 32)[at];
+          const float2 h0 = hl[0], h1 = hl[16], h2 = hl[32], h3 = hl[48];
+          if (lr.x != -INFINITY) l[0] = fmaf((h0.x + h1.x) + (h2.x + h3.x), ptx::ex2(lr.x + kHead - fin.x), l[0]);
+          if (lr.y != -INFINITY) l[1] = fmaf((h0.y + h1.y) + (h2.y + h3.y), ptx::ex2(lr.y + kHead - fin.y), l[1]);
+        }
+      }
+      n0 += (w.t1 - w.t0 + kBT - 1) / kBT;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
+      const bool whole = w.poff < 0;
+      float *part = p.partials + w.poff;
+      reinterpret_cast<float2 *>(cw)[lane] = whole ? make_float2(1.0f / l[0], 1.0f / l[1]) : both(1.0f);
+      if (!whole && qd == 0) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (2 * lane + x < w.rows) {
+            __stcg(part + w.rows * D + 2 * lane + x, x ? fin.y : fin.x);
+            __stcg(part + w.rows * D + w.rows + 2 * lane + x, l[x]);
+          }
         }
       }
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
-      if (nan0 != INT32_MAX) {  // a value that is NaN: rows from nan0 on see it
+      if (!wait_bar(B.at(BR::O_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
+      ptx::tc_fence_after();
+      // (row pointers stepped from row to row)
+      int hh = w.row0 - div_g(w.row0) * g;
+      uint16_t *og = static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + div_g(w.row0)) * p.Hq + w.h * g + hh) * D + d;
+      const int wrap = (p.Hq - g + 1) * D;  // from a position's last head to the next one's first
+      const uint32_t at = tmem + lane_addr + 256 + ob * 128;
+#pragma unroll 1
+      for (int r = 0; r < nrow; r += 8) {
+        uint32_t hi[8], lo[8];
+        ptx::tmem_ld8(at + r, hi);
+        ptx::tmem_ld8(at + nrow + r, lo);
+        ptx::tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < kNR / 2; ++i) {
-          if (2 * i >= nan0) acc[i].x = NAN;
-          if (2 * i + 1 >= nan0) acc[i].y = NAN;
+        for (int i = 0; i < 8; ++i) {
+          float o = (__uint_as_float(hi[i]) + __uint_as_float(lo[i])) * cw[r + i];
+          if (r + i >= nan0) o = NAN;  // a value that is NaN: rows from nan0 on see it
+          if (dval && r + i < w.rows) {
+            if (whole)
+              *og = __bfloat16_as_ushort(__float2bfloat16_rn(o));
+            else
+              __stcg(part + (int64_t)(r + i) * D + d, o);
+          }
+          og += hh == g - 1 ? wrap : D;
+          hh = hh == g - 1 ? 0 : hh + 1;
         }
       }
-      if (w.poff < 0) {
-        reinterpret_cast<float2 *>(cw)[lane] = make_float2(1.0f / l[0], 1.0f / l[1]);
-        __syncwarp();
-        // (row pointers stepped from row to row)
-        int hh = w.row0 - div_g(w.row0) * g;
-        uint16_t *og = static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + div_g(w.row0)) * p.Hq + w.h * g + hh) * D + d;
-        const int wrap = (p.Hq - g + 1) * D;  // from a position's last head to the next one's first
-#pragma unroll
-        for (int i = 0; i < kNR; i += 2) {
-          if (i < w.rows) {
-            const float2 f = *reinterpret_cast<const float2 *>(cw + i);
-            if (dval) *og = __bfloat16_as_ushort(__float2bfloat16_rn(acc[i / 2].x * f.x));
-            og += hh == g - 1 ? wrap : D;
-            hh = hh == g - 1 ? 0 : hh + 1;
-            if (dval && i + 1 < w.rows) *og = __bfloat16_as_ushort(__float2bfloat16_rn(acc[i / 2].y * f.y));
-            og += hh == g - 1 ? wrap : D;
-            hh = hh == g - 1 ? 0 : hh + 1;
-          }
-        }
-        __syncwarp();  // cw is written again by the next item
-      } else {
-        float *part = p.partials + w.poff;
-#pragma unroll
-        for (int i = 0; i < kNR; i += 2) {
-          if (dval && i < w.rows) __stcg(part + (int64_t)i * D + d, acc[i / 2].x);
-          if (dval && i + 1 < w.rows) __stcg(part + (int64_t)(i + 1) * D + d, acc[i / 2].y);
-        }
-        if (qd == 0) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (2 * lane + x < w.rows) {
-              __stcg(part + w.rows * D + 2 * lane + x, M[x]);
-              __stcg(part + w.rows * D + w.rows + 2 * lane + x, l[x]);
-            }
-          }
-        }
+      ptx::tc_fence_before();
+      __syncwarp();  // (cw has been read, too)
+      if (lane == 0) ptx::mbar_arrive(B.at(BR::O_EMPTY + ob));
+      if (!whole) {
         // ---- the last chunk of this (request, head, row group) to finish merges all ----
         __threadfence();
         if (!group_sync()) { ok = false; break; }
@@ -757,17 +766,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (wg == 0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 0 || warp == 3) {
-      // ------------------------------------------------------------------ K / V producers
-      const bool is_k = warp == 0;
-      constexpr uint32_t ns = C::NSK;
-      static_assert(C::NSK == C::NSV, "one ring length");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    // ------------------------------------------------------------------ K / V producers
+    auto produce = [&](auto which) {
+      constexpr bool is_k = decltype(which)::value;
+      constexpr uint32_t ns = is_k ? C::NSK : C::NSV;
       const CUtensorMap *tm1 = is_k ? &tmk : &tmv;
       const CUtensorMap *tm8 = is_k ? &tmk8 : &tmv8;
       const uint32_t off_t = sbase + (is_k ? C::OFF_K : C::OFF_V);
       const uint32_t full = B.at(is_k ? BR::K_FULL : BR::V_FULL), empty = B.at(is_k ? BR::K_EMPTY : BR::V_EMPTY);
-      uint32_t tile_n = 0;
+      uint32_t tile_n = 0, s = 0, phase = 1;  // the ring's stage and its barrier's parity
       for (uint32_t j = 0; ok; ++j) {
         const int slot = j % C::RING;
         if (!wait_bar(B.at(BR::IT_FULL + slot), (j / C::RING) & 1, s_abort)) { ok = false; break; }
@@ -782,48 +790,58 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int i = base + lane;
           return i < nblk ? __ldg(bt + i) : -1;
         };
+        auto valid = [&](int bid) -> bool { return bid >= 0 && bid < p.num_blocks; };
         // the scales of a lane's block (K's producer brings both; blocks that do not exist: any)
         auto scales = [&](int bid) -> float2 {
-          if (!is_k || bid < 0 || bid >= p.num_blocks) return make_float2(1.0f, 1.0f);
+          if (!is_k || !valid(bid)) return make_float2(1.0f, 1.0f);
           const int64_t at = (int64_t)bid * p.Hkv + h;
           return make_float2(__ldg(p.k_scale + at), __ldg(p.v_scale + at));
         };
-        int cur = fetch(0), nxt = fetch(32);  // block ids of tiles t..t+3 and t+4..t+7
+        // block ids of tiles t..t+3, t+4..t+7 and t+8..t+11, the scales of the first two
+        int cur = fetch(0), nxt = fetch(32), far = fetch(64);
         float2 sc_cur = scales(cur), sc_nxt = scales(nxt);
+        unsigned runs = 0;                // bit 8 i + 7 of tiles t..t+3: i's blocks are consecutive and valid
         const int ntiles = (t1 - t0 + kBT - 1) / kBT;
         for (int t = 0; t < ntiles; ++t, ++tile_n) {
-          if (is_k && lane == 0) *s_issued = tile_n;
-          if (t > 0 && (t & 3) == 0) {
-            cur = nxt;
-            sc_cur = sc_nxt;
-            nxt = fetch(32 * ((t >> 2) + 1));
-            sc_nxt = scales(nxt);
+          if ((t & 3) == 0) {
+            if (t > 0) {
+              cur = nxt;
+              nxt = far;
+              far = fetch(8 * t + 64);
+              sc_cur = sc_nxt;
+              sc_nxt = scales(nxt);
+            }
+            const bool good = valid(cur);
+            if (is_k && !good && 8 * t + lane < nblk) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, r);
+            if (!good) cur = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
+            __syncwarp();
+            const int lead = __shfl_sync(0xffffffffu, cur, lane & 24);
+            runs = __ballot_sync(0xffffffffu, good & (cur == lead + (lane & 7)));
           }
-          const int s = (int)(tile_n % ns);
-          const uint32_t round = tile_n / ns;
-          if (!wait_bar(empty + 8 * s, (round & 1) ^ 1, s_abort)) { ok = false; break; }
-          if (lane == 0) ptx::mbar_arrive_expect_tx(full + 8 * s, C::KV_TILE);
+          const int i = t & 3;
+          if (!wait_bar(empty + 8 * s, phase, s_abort)) { ok = false; break; }
+          const int bid = __shfl_sync(0xffffffffu, cur, 8 * i + (lane & 7));
+          if (lane == 0) {
+            if (is_k) *s_issued = tile_n;
+            ptx::mbar_arrive_expect_tx(full + 8 * s, C::KV_TILE);
+          }
           __syncwarp();
-          const int bi = lane & 7;  // block of the tile this lane looks after
-          int bid = __shfl_sync(0xffffffffu, cur, (8 * t + bi) & 31);
-          const int rel = 8 * t + bi;
-          const bool valid = rel < nblk && bid >= 0 && bid < p.num_blocks;
-          if (is_k && lane < 8 && rel < nblk && !valid) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, r);
-          const int b0 = __shfl_sync(0xffffffffu, bid, 0);
-          // eight consecutive valid blocks: one box with the 8-block maps
-          const unsigned contig = __ballot_sync(0xffffffffu, lane < 8 && valid && bid == b0 + lane);
-          if (contig == 0xFFu) {
-            if (lane == 0) ptx::tma_load_4d(off_t + s * C::KV_TILE, tm8, full + 8 * s, 0, 0, h, b0);
+          if (((runs >> (8 * i)) & 0xffu) == 0xffu) {  // one box with the 8-block maps
+            if (ptx::elect_one()) ptx::tma_load_4d(off_t + s * C::KV_TILE, tm8, full + 8 * s, 0, 0, h, bid);
           } else if (lane < 8) {
-            if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
             ptx::tma_load_4d(off_t + s * C::KV_TILE + lane * 16 * D, tm1, full + 8 * s, 0, 0, h, bid);
           }
-          if (is_k) {  // the scales, which may arrive later than the block ids
-            const float sk = __shfl_sync(0xffffffffu, sc_cur.x, (8 * t + bi) & 31);
-            const float sv = __shfl_sync(0xffffffffu, sc_cur.y, (8 * t + bi) & 31);
-            if (lane < 8) s_sc[(tile_n % C::SC) * 8 + bi] = make_float2(sk, sv);
-            __syncwarp();
+          __syncwarp();
+          if (is_k) {  // the scales, which may arrive later than the block ids, of four tiles at a time
+            if (i == 0) {
+              s_sc[((tile_n + (lane >> 3)) % C::SC) * 8 + (lane & 7)] = sc_cur;
+              __syncwarp();
+            }
             if (lane == 0) ptx::mbar_arrive(full + 8 * s);
+          }
+          if (++s == ns) {
+            s = 0;
+            phase ^= 1;
           }
         }
       }
@@ -836,6 +854,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
+    };
+    if (warp == 0) {
+      produce(std::true_type());
+    } else if (warp == 3) {
+      produce(std::false_type());
     } else if (warp == 2) {
       // ------------------------------------------------------------------ item loader
       uint32_t published = 0;  // K tiles of the items published so far
@@ -882,18 +905,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       issue(std::true_type());
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 24) {
       issue(std::false_type());
     } else {
       // ------------------------------------------------------------------ Q loaders
-      // Query row row0 + rho = j * g + hh at MMA row rho (hi) and 64 + rho (lo), rows past the item up to the MMA's N zero.  A row's
-      // factor 2^e / sqrt(D) in log2 units goes to s_rf.
+      // Query row row0 + rho = j * g + hh at MMA row rho (hi) and 64 + rho (lo), rows past the item up to the MMA's N zero.
+      // The rows are read twice, for the item's exponent e (their largest magnitude is at most 448 * 2^e) and for their
+      // parts; the queries' factor 2^e / sqrt(D) in log2 units goes to s_qf (NaN where a query is not finite).
       const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
       constexpr int CPR = D / 8;     // 16-byte chunks per row, a lane each
       constexpr int RPP = 32 / CPR;  // rows per warp pass
-      constexpr int QB = 2;          // passes in flight
-      const int cc = lane % CPR;
+      constexpr int STEP = kQWarps * RPP;
+      const int cc = lane % CPR, wq = warp - 25;
       int li = 0;
       for (uint32_t j = 0; ok; ++j, ++li) {
         const int slot = j % C::RING;
@@ -904,44 +928,48 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(B.at(BR::IT_EMPTY + slot));
         if (it < 0) break;
         const int qb = li & 1, nrow = (rows + 15) / 16 * 16;
-        if (!wait_bar(B.at(BR::Q_EMPTY + qb), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
         const uint16_t *qi = static_cast<const uint16_t *>(p.q) + ((int64_t)q0 * p.Hq + h * g) * D + cc * 8;
+        auto load = [&](int row) -> uint4 {
+          if (row >= rows) return make_uint4(0, 0, 0, 0);
+          const int rj = row0 + row, jj = div_g(rj), hh = rj - jj * g;
+          return __ldg(reinterpret_cast<const uint4 *>(qi + (int64_t)(jj * p.Hq + hh) * D));
+        };
+        uint32_t big = 0;  // largest magnitude, as bf16 bits
+#pragma unroll 4
+        for (int row = wq * RPP + lane / CPR; row < rows; row += STEP) {
+          const uint4 v = load(row);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+        }
+        __syncwarp();
+        big = __reduce_max_sync(0xffffffffu, big);
+        // the three warps' maxima (slot li & 1: its readers of item li - 2 have all arrived at item li - 1 since)
+        if (lane == 0) {
+          s_qmax[(li & 1) * 4 + wq] = big;
+          ptx::mbar_arrive(B.at(BR::QX));
+        }
+        if (!wait_bar(B.at(BR::QX), li & 1, s_abort) || !wait_bar(B.at(BR::Q_EMPTY + qb), ((li >> 1) & 1) ^ 1, s_abort)) {
+          ok = false;
+          break;
+        }
+        big = max(s_qmax[(li & 1) * 4], max(s_qmax[(li & 1) * 4 + 1], s_qmax[(li & 1) * 4 + 2]));
+        const bool finite = big < 0x7f80u;
+        const int e = finite ? scale_exp(__uint_as_float(big << 16)) : 0;
+        const float inv = exp2i(-e);
+        if (wq == 0 && lane == 0) s_qf[li % C::RF] = finite ? exp2i(e) * scale_log2 : NAN;
         uint8_t *qs = smem + C::OFF_Q + qb * C::Q_BYTES;
-        float *rf = s_rf + (li % C::RF) * kNR;
-        for (int base = (warp - 25) * RPP; base < nrow; base += kQWarps * RPP * QB) {
-          uint4 v[QB];
-#pragma unroll
-          for (int u = 0; u < QB; ++u) {
-            const int row = base + u * kQWarps * RPP + lane / CPR;
-            v[u] = make_uint4(0, 0, 0, 0);
-            if (row < rows) {
-              const int rj = row0 + row, jj = div_g(rj), hh = rj - jj * g;
-              v[u] = __ldg(reinterpret_cast<const uint4 *>(qi + (int64_t)(jj * p.Hq + hh) * D));
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < QB; ++u) {
-            const int row = base + u * kQWarps * RPP + lane / CPR;
-            if (base + u * kQWarps * RPP < nrow) {  // (nrow is a multiple of RPP: the same for the whole warp)
-              const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-              uint32_t big = 0;  // largest magnitude, as bf16 bits
-#pragma unroll
-              for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-#pragma unroll
-              for (int x = 1; x < CPR; x <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, x));
-              const bool finite = big < 0x7f80u;
-              const int e = finite ? scale_exp(__uint_as_float(big << 16)) : 0;
-              const float inv = exp2i(-e);
-              uint32_t hi[4], lo[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                split2<false>(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv, hi[i], lo[i]);
-              const uint32_t half = (cc & 1) * 8;
-              *reinterpret_cast<uint2 *>(qs + swz<D>(row, cc >> 1) + half) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-              *reinterpret_cast<uint2 *>(qs + swz<D>(kNR + row, cc >> 1) + half) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-              if (cc == 0) rf[row] = finite ? exp2i(e) * scale_log2 : NAN;
-            }
-          }
+#pragma unroll 2
+        for (int row = wq * RPP + lane / CPR; row < nrow; row += STEP) {
+          const uint4 v = load(row);
+          uint32_t hi[2], lo[2];
+          split4(__uint_as_float(v.x << 16) * inv, __uint_as_float(v.x & 0xffff0000u) * inv, __uint_as_float(v.y << 16) * inv,
+                 __uint_as_float(v.y & 0xffff0000u) * inv, hi[0], lo[0]);
+          split4(__uint_as_float(v.z << 16) * inv, __uint_as_float(v.z & 0xffff0000u) * inv, __uint_as_float(v.w << 16) * inv,
+                 __uint_as_float(v.w & 0xffff0000u) * inv, hi[1], lo[1]);
+          const uint32_t half = (cc & 1) * 8;
+          *reinterpret_cast<uint2 *>(qs + swz<D>(row, cc >> 1) + half) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2 *>(qs + swz<D>(kNR + row, cc >> 1) + half) = make_uint2(lo[0], lo[1]);
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
