@@ -862,6 +862,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 2) {
       // ------------------------------------------------------------------ item loader
       uint32_t published = 0;  // K tiles of the items published so far
+      bool first = true;
       for (uint32_t j = 0; ok; ++j) {
         // items are taken just in time, so that the work counter balances the CTAs to the end, but early enough to
         // hide the way from the claim to the first load
@@ -881,7 +882,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           int it;
           WorkItem w;
           do {
-            it = atomicAdd(&p.header_mut->next_item, 1);
+            // (the first one is the CTA's own: a way to memory and back less before its first load)
+            it = first ? (int)blockIdx.x : p.header->attn_ctas + atomicAdd(&p.header_mut->next_item, 1);
+            first = false;
             if (it >= n_items) { it = -1; break; }
             w = p.items[it];
           } while (!item_ok(p, w));
