@@ -30,7 +30,7 @@
 //
 // What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
 // SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
-// 4 / 16 / 32 / 36 / 64 rows: 893 / 955 / 1019 / 1477 / 1694 (D = 128; 5.58 TB/s at 4 rows), 679 / 761 / 957 / 1394 / 1600
+// 4 / 16 / 32 / 36 / 64 rows: 888 / 936 / 1013 / 1469 / 1688 (D = 128; 5.6 TB/s at 4 rows), 679 / 742 / 955 / 1364 / 1568
 // (D = 64).  The bf16 cache's kernel, with twice the bytes: 1468 to 1516 and 823 to 880.  What the choices gave, at 4 / 32 / 64
 // rows of D = 128:
 //   * two groups of warps with O in registers of four correction warps, PV products added there per tile: 990 / 1082 / 1681,
@@ -41,6 +41,8 @@
 //     an MMA took the issuing warp 100 clocks before, 25 after;
 //   * the maxima's loop over a group's rows not unrolled, so that less code goes round: 947 / 1118 / 1658 to 924 / 1080 / 1687;
 //   * a fourth stage for K: 919 / 1081 / 1691 to 893 / 1019 / 1694; for V instead: nothing;
+//   * pages in no order, eight boxes a tile, from one elected lane and not from eight: 1018 / 1144 / 1702 to 970 / 1094 / 1701
+//     (D = 64: 869 / 989 / 1579 to 761 / 946 / 1594); pages in order lose 1%;
 //   * block ids brought in 12 tiles ahead and scales 8, checked and written four tiles at a time: 1047 to 955 at 4 rows.
 //
 // Every mbarrier wait is bounded in time; an expired wait records WISP_DEV_TIMEOUT and the CTA drains.
@@ -828,8 +830,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (((runs >> (8 * i)) & 0xffu) == 0xffu) {  // one box with the 8-block maps
             if (ptx::elect_one()) ptx::tma_load_4d(off_t + s * C::KV_TILE, tm8, full + 8 * s, 0, 0, h, bid);
-          } else if (lane < 8) {
-            ptx::tma_load_4d(off_t + s * C::KV_TILE + lane * 16 * D, tm1, full + 8 * s, 0, 0, h, bid);
+          } else {
+            int bids[8];
+#pragma unroll
+            for (int b = 0; b < 8; ++b) bids[b] = __shfl_sync(0xffffffffu, bid, b);
+            if (ptx::elect_one()) {
+#pragma unroll
+              for (int b = 0; b < 8; ++b)
+                ptx::tma_load_4d(off_t + s * C::KV_TILE + b * 16 * D, tm1, full + 8 * s, 0, 0, h, bids[b]);
+            }
           }
           __syncwarp();
           if (is_k) {  // the scales, which may arrive later than the block ids, of four tiles at a time
