@@ -7,7 +7,14 @@ requests and runs it through the library over one shared paged KV pool (Sec. 4.5
     wisp_verify_step         attention over the pool and the acceptance pass (Eq. 1-3)
     wisp_kv_commit           c <- c + 1 + L; the rejected drafts' pages go back to the pool
 
-all enqueued on one stream and timed with CUDA events.  The server's clock advances by the measured
+all enqueued on one stream and timed with CUDA events.  With PagedSessions(cache="e4m3") the pool holds 8-bit codes with a
+scale per page and KV head, with PagedSessions(rope=...) payloads carry queries and keys that the append rotates, and with
+VerifyServer(top_n=...) a batch also answers log probabilities of the logit rows that committed a token:
+
+    wisp_kv_reserve_append_rope, wisp_verify_step_kv8, wisp_kv_commit    in the places of the three above
+    wisp_verify_committed_tokens, wisp_verify_logprobs                   after the step
+
+The server's clock advances by the measured
 batch time; every request's completion is checked against its deadline (its SLO), and the measured
 time is recorded beside the estimator's prediction T_hat(B) (Eq. batch_time, Sec. 4.4).  The
 estimator is refitted on the batches measured so far (ordinary least squares), so that each
@@ -51,26 +58,67 @@ def _cat(arrays, tail_shape, dtype):
 
 class PagedSessions:
     """n sessions over one shared paged KV pool, all state on the device: the pool, the free-page
-    stack, per-session block-table rows and context lengths."""
+    stack, per-session block-table rows and context lengths.
 
-    def __init__(self, n_sessions, Hkv, D, dtype, num_blocks, max_blocks, device="cuda"):
+    cache: None (the pool has the payloads' type) or "e4m3" (codes, and k_scale / v_scale per page and KV head).
+    rope: [positions, rot_dim] float32 cosines and sines; the append then rotates new keys (and a batch's queries) by their
+    positions.  interleaved: its pairs are (2i, 2i + 1)."""
+
+    def __init__(self, n_sessions, Hkv, D, dtype, num_blocks, max_blocks, device="cuda", cache=None, rope=None,
+                 interleaved=False):
+        if cache not in (None, "e4m3"):
+            raise ValueError("cache is None or 'e4m3'")
         self.dev = torch.device(device)
         self.dtype = dtype
         tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.k_cache = torch.zeros((num_blocks, Hkv, PAGE, D), dtype=tdt, device=self.dev)
+        self.kv8, self.interleaved = cache == "e4m3", interleaved
+        self.rope = None if rope is None else rope.to(self.dev, torch.float32).contiguous()
+        cdt = torch.float8_e4m3fn if self.kv8 else tdt
+        self.k_cache = torch.zeros((num_blocks, Hkv, PAGE, D), dtype=cdt, device=self.dev)
         self.v_cache = torch.zeros_like(self.k_cache)
+        self.scales = {}
+        if self.kv8:
+            self.scales = {n: torch.ones((num_blocks, Hkv), device=self.dev) for n in ("k_scale", "v_scale")}
         self.free_blocks = torch.arange(num_blocks, dtype=torch.int32, device=self.dev).flip(0).contiguous()
         self.free_count = torch.tensor([num_blocks], dtype=torch.int32, device=self.dev)
         self.tables = torch.full((n_sessions, max_blocks), -1, dtype=torch.int32, device=self.dev)
         self.ctx = torch.zeros(n_sessions, dtype=torch.int32, device=self.dev)
         self.num_blocks, self.max_blocks, self.Hkv, self.D = num_blocks, max_blocks, Hkv, D
-        self.kv_ws = None
+        self.kv_ws = self.commit_ws = None
+
+    @property
+    def projected(self):
+        """Whether rows go through the append that rotates and encodes."""
+        return self.kv8 or self.rope is not None
+
+    def _append_args(self, **kw):
+        """The arguments of the append (wisp_kv_rope_args where it rotates or encodes, else wisp_kv_args)."""
+        pool = dict(free_blocks=self.free_blocks, free_count=self.free_count, k_cache=self.k_cache, v_cache=self.v_cache)
+        if self.projected:
+            kw.pop("accepted_len", None)
+            return wb.make_kv_rope_args(**pool, **self.scales, rope=self.rope, interleaved=self.interleaved, **kw)
+        return wb.make_kv_args(**pool, **kw)
+
+    def _append(self, args, ws, stream):
+        (wb.wisp_kv_reserve_append_rope if self.projected else wb.wisp_kv_reserve_append)(args, ws, stream)
+
+    def _commit_args(self, args, **kw):
+        """The arguments of the commit that follows an append with `args`."""
+        if not self.projected:
+            return args
+        return wb.make_kv_args(free_blocks=self.free_blocks, free_count=self.free_count, **kw)
 
     def _ws(self, args):
-        n = wb.wisp_kv_workspace_size(args)
+        """Workspaces of the append with `args` and of the commit after it, one or two: each call leaves its status."""
+        n = (wb.wisp_kv_rope_workspace_size if self.projected else wb.wisp_kv_workspace_size)(args)
         if self.kv_ws is None or self.kv_ws.numel() < n:
             self.kv_ws = wb.alloc_workspace(n, self.dev)
-        return self.kv_ws
+        if not self.projected:
+            return self.kv_ws, self.kv_ws
+        n = wb.wisp_kv_workspace_size(args.kv)
+        if self.commit_ws is None or self.commit_ws.numel() < n:
+            self.commit_ws = wb.alloc_workspace(n, self.dev)
+        return self.kv_ws, self.commit_ws
 
     def _dev(self, a, torch_dtype=None):
         if self.dtype == "bf16" and a.dtype == np.uint16:
@@ -87,20 +135,17 @@ class PagedSessions:
         ctx = self.ctx[idx].contiguous()
         tables = self.tables[idx].contiguous()
         kn, vn = self._dev(np.concatenate(k_rows)), self._dev(np.concatenate(v_rows))
-        args = wb.make_kv_args(draft_lens=draft, context_lens=ctx, block_tables=tables, free_blocks=self.free_blocks,
-                               free_count=self.free_count, k_cache=self.k_cache, v_cache=self.v_cache, k_new=kn,
-                               v_new=vn, total_q_rows=int(sum(lens)))
-        ws = self._ws(args)
-        wb.wisp_kv_reserve_append(args, ws, stream)
+        batch = dict(draft_lens=draft, context_lens=ctx, block_tables=tables, total_q_rows=int(sum(lens)))
         acc = draft.clone()
-        args = wb.make_kv_args(draft_lens=draft, context_lens=ctx, block_tables=tables, free_blocks=self.free_blocks,
-                               free_count=self.free_count, k_cache=self.k_cache, v_cache=self.v_cache,
-                               accepted_len=acc, total_q_rows=int(sum(lens)))
-        wb.wisp_kv_commit(args, ws, stream)
+        args = self._append_args(**batch, k_new=kn, v_new=vn, accepted_len=acc)
+        ws, cws = self._ws(args)
+        self._append(args, ws, stream)
+        wb.wisp_kv_commit(self._commit_args(args, **batch, accepted_len=acc), cws, stream)
         torch.cuda.synchronize(self.dev)
-        code, rid = wb.wisp_verify_get_device_status(ws)
-        if code != 0:
-            raise RuntimeError(f"prefill: device status {code} (request {rid})")
+        for w in (ws, cws):
+            code, rid = wb.wisp_verify_get_device_status(w)
+            if code != 0:
+                raise RuntimeError(f"prefill: device status {code} (request {rid})")
         self.tables[idx] = tables
         self.ctx[idx] = ctx
 
@@ -110,17 +155,26 @@ class BatchResult:
     sids: list
     accepted_len: np.ndarray
     next_token: np.ndarray
-    gpu_ms: float                 # reserve_append + step + commit, CUDA events on the stream
+    gpu_ms: float                 # append, step, log probabilities and commit, CUDA events on the stream
     out: torch.Tensor             # attention output [T_q, Hq, D] (device)
     block_tables: np.ndarray      # the batch's table rows as the step read them (after reserve)
     context_lens: np.ndarray      # c before the commit
+    # with VerifyServer(top_n=...), per logit row (row Q0_r + i of request r; what follows its i-th draft):
+    row_tokens: np.ndarray | None = None    # the token that the row committed, -1: none
+    logprob: np.ndarray | None = None       # its log probability
+    entropy: np.ndarray | None = None
+    top_tokens: np.ndarray | None = None    # [T_q, top_n]
+    top_logprobs: np.ndarray | None = None
 
 
 class VerifyServer:
-    """Runs verification batches of sessions through the library (reserve -> step -> commit)."""
+    """Runs verification batches of sessions through the library (reserve -> step -> commit).  top_n: None, or how many of
+    the most likely tokens a batch lists beside the committed tokens' log probabilities (0 to 32)."""
 
-    def __init__(self, sessions: PagedSessions, Hq: int, V: int, stream=None):
+    def __init__(self, sessions: PagedSessions, Hq: int, V: int, stream=None, top_n=None):
         self.s = sessions
+        self.top_n = top_n
+        self.lp_ws = None
         self.Hq, self.V = Hq, V
         self.stream = stream
         self.ws = None
@@ -146,37 +200,56 @@ class VerifyServer:
         out = torch.empty_like(q)
         acc = torch.full((B,), -7, dtype=torch.int32, device=dev)
         tok = torch.full((B,), -7, dtype=torch.int32, device=dev)
-        kv = wb.make_kv_args(draft_lens=draft, context_lens=ctx, block_tables=tables, free_blocks=s.free_blocks,
-                             free_count=s.free_count, k_cache=s.k_cache, v_cache=s.v_cache, k_new=kn, v_new=vn,
-                             accepted_len=acc, request_ids=rid, total_q_rows=Tq)
-        attn = wb.make_attn_args(draft_lens=draft, context_lens=ctx, block_tables=tables, q=q, k_cache=s.k_cache,
-                                 v_cache=s.v_cache, out=out, request_ids=rid, num_blocks=s.num_blocks)
+        batch = dict(draft_lens=draft, context_lens=ctx, block_tables=tables, request_ids=rid)
+        # (queries are rotated beside the append, in place)
+        turn = dict(q=q, q_out=q) if s.rope is not None else {}
+        kv = s._append_args(**batch, **turn, k_new=kn, v_new=vn, accepted_len=acc, total_q_rows=Tq)
+        kv_commit = s._commit_args(kv, **batch, accepted_len=acc, total_q_rows=Tq)
+        attn = (wb.make_attn_kv8_args if s.kv8 else wb.make_attn_args)(
+            **batch, **s.scales, q=q, k_cache=s.k_cache, v_cache=s.v_cache, out=out, num_blocks=s.num_blocks)
+        step = wb.wisp_verify_step_kv8 if s.kv8 else wb.wisp_verify_step
         accp = wb.make_accept_args(draft_lens=draft, target_logits=logits, draft_tokens=tokens, draft_probs=probs,
                                    accept_uniforms=au, sample_uniforms=su, accepted_len=acc, next_token=tok,
                                    request_ids=rid)
-        kws = s._ws(kv)
-        n = wb.wisp_verify_workspace_size(attn, accp)
+        kws, cws = s._ws(kv)
+        n = wb.wisp_verify_workspace_size(attn.attn if s.kv8 else attn, accp)
         if self.ws is None or self.ws.numel() < n:
             self.ws = wb.alloc_workspace(n, dev)
+        used = [(kws, "kv"), (self.ws, "verify"), (cws, "commit")]
+        lp = {}
+        if self.top_n is not None:
+            lp = dict(row_tokens=torch.empty(Tq, dtype=torch.int32, device=dev), logprob=torch.empty(Tq, device=dev),
+                      entropy=torch.empty(Tq, device=dev),
+                      top_tokens=torch.empty((Tq, self.top_n), dtype=torch.int32, device=dev),
+                      top_logprobs=torch.empty((Tq, self.top_n), device=dev))
+            lpa = wb.make_logprobs_args(logits=logits, tokens=lp["row_tokens"], **{n: t for n, t in lp.items() if n != "row_tokens"})
+            n = wb.wisp_verify_logprobs_workspace_size(lpa)
+            if self.lp_ws is None or self.lp_ws.numel() < n:
+                self.lp_ws = wb.alloc_workspace(n, dev)
+            used.append((self.lp_ws, "logprobs"))
         stream = self.stream or torch.cuda.current_stream(dev)
         a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         with torch.cuda.stream(stream):
             a.record(stream)
-            wb.wisp_kv_reserve_append(kv, kws, stream)
+            s._append(kv, kws, stream)
             tables_read = tables.clone()  # the rows the step reads (commit rewrites them)
             ctx_read = ctx.clone()
-            wb.wisp_verify_step(attn, accp, self.ws, stream)
-            wb.wisp_kv_commit(kv, kws, stream)
+            step(attn, accp, self.ws, stream)
+            if lp:
+                wb.wisp_verify_committed_tokens(accp, lp["row_tokens"], stream)
+                wb.wisp_verify_logprobs(lpa, self.lp_ws, stream)
+            wb.wisp_kv_commit(kv_commit, cws, stream)
             b.record(stream)
         stream.synchronize()
-        for ws, what in ((kws, "kv"), (self.ws, "verify")):
+        for ws, what in used:
             code, r = wb.wisp_verify_get_device_status(ws)
             if code != 0:
                 raise RuntimeError(f"{what}: device status {code} (request {r})")
         s.tables[idx] = tables
         s.ctx[idx] = ctx
         return BatchResult(list(sids), acc.cpu().numpy(), tok.cpu().numpy(), a.elapsed_time(b), out,
-                           tables_read.cpu().numpy(), ctx_read.cpu().numpy())
+                           tables_read.cpu().numpy(), ctx_read.cpu().numpy(),
+                           **{n: t.cpu().numpy() for n, t in lp.items()})
 
 
 @dataclasses.dataclass
