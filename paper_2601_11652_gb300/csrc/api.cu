@@ -347,8 +347,9 @@ wisp_status launch_attention(const wisp_attn_args *a, KvScales sc, void *ws, con
   // on this stream, and split items are merged inside the kernel by the last chunk to finish
   const int grid = (int)(L.max_items < L.target_items / kItemsPerSM ? L.max_items : L.target_items / kItemsPerSM);
   const bool bf = a->qkv_dtype == WISP_BF16;
-  const cudaError_t e = sc.k ? (bf ? attn_kv8_tc_launch(ap, grid, s) : attn_kv8_f32_launch(ap, grid, s))
-                             : (bf ? attn_tc_launch(ap, grid, s) : attn_f32_launch(ap, grid, s));
+  const cudaError_t e = !bf    ? attn_f32_launch(ap, grid, s)
+                        : sc.k ? attn_kv8_tc_launch(ap, grid, s)
+                               : attn_tc_launch(ap, grid, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 

@@ -25,15 +25,13 @@ struct AttnParams {
 
 // Host launchers (defined next to their kernels): programmatic dependents of the planner, which they wait for
 // before they read the plan.
-// CUDA-core kernel for fp32 KV, D in {64, 128}; `grid` persistent CTAs
+// CUDA-core kernel for fp32 queries, over fp32 or (with scales) e4m3 KV, D in {64, 128}; `grid` persistent CTAs
 cudaError_t attn_f32_setup();  // once per device: shared-memory attributes
 cudaError_t attn_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
 // tcgen05 / TMA kernel for bf16 KV, D in {64, 128}; `grid` persistent CTAs
 cudaError_t attn_tc_setup();
 cudaError_t attn_tc_launch(const AttnParams &p, int grid, cudaStream_t s);
 
-// CUDA-core kernel for e4m3 KV with fp32 queries and outputs, D in {64, 128}; `grid` persistent CTAs
-cudaError_t attn_kv8_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
 // tcgen05 / TMA kernel for e4m3 KV with bf16 queries and outputs
 cudaError_t attn_kv8_tc_setup();
 cudaError_t attn_kv8_tc_launch(const AttnParams &p, int grid, cudaStream_t s);

@@ -1,4 +1,5 @@
-// attn_f32.cu -- paged GQA attention of the verification forward for fp32 KV, on the CUDA cores.
+// attn_f32.cu -- paged GQA attention of the verification forward for fp32 queries, over an fp32 cache or one in 8 bits
+// (include/wisp_kv8.h), on the CUDA cores.
 //
 // Same contract as attn_tc.cu (Sec. 4.4-4.5: request r's k+1 new queries over its L_total = L_cached +
 // L_new paged keys, query j seeing keys 0..c_r + j); products and sums in fp32 (tensor cores would
@@ -28,7 +29,15 @@
 // 285 us, 26.6 TFLOP/s; shared memory is busy 51% of the time there, issue 38%, DRAM 29%.  At RL = 8 and
 // D = 128 the 255 registers do not hold everything: 116 bytes of spills a thread (none at D = 64), 0.2%
 // of its instructions.
+//
+// 8-bit cache: a page of codes comes by one bulk copy and is decoded into the rows that the loops read, K before the
+// scores, V after them; the codes take the room of the second K page.  A page's scales are factors of its scores and of its
+// weights on their way to O.  The loops bound it as before, so a quarter of the bytes takes the time of an fp32 cache:
+// 38 requests of 8192 tokens, D = 128, 4 / 8 / 16 / 32 rows: 564 / 645 / 772 / 1125 us (36 TFLOP/s at 32 rows).
+// 32 requests of 2300 tokens, 20 rows: 256 us, 232 with an fp32 cache; 1102 with the pages decoded once per CTA and four
+// rows a warp.
 #include "attn_merge.cuh"
+#include "fp8.cuh"
 
 #include <cstring>
 
@@ -55,6 +64,8 @@ struct Cfg {
   static_assert(SMEM <= 227 * 1024 - 512, "shared memory of one CTA on sm_103a");
   static_assert(kRows * PLD <= PAGE_F, "P fits a K page");
   static_assert(kRows * D <= 2 * PAGE_F, "a warp's O fits its two K pages");
+  static constexpr int CODES = kPage * D;             // bytes of a K (or V) page of an 8-bit cache
+  static_assert(3 * CODES <= PAGE_F * 4, "two K pages and a V page of codes fit a page");
 };
 
 struct Shared {
@@ -76,19 +87,19 @@ __device__ __forceinline__ bool wait_page(uint64_t *b, uint32_t parity, volatile
 
 // One item by the whole CTA with RL rows per lane (rows <= 4 RL); Q is in shared memory.  `phk`, `phv`:
 // this warp's page copies so far (barrier parities).  Leaves the warps' O, m, l in shared memory.
-template <int D, int RL>
+template <int D, int RL, bool KV8>
 __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w, int g, float *smem, Shared &sh, int warp,
                                           uint32_t &nk, uint32_t &nv) {
   using C = Cfg<D>;
   constexpr int CI = D / 32;  // float4 columns per lane
   const int lane = threadIdx.x & 31, la = lane >> 3, lb = lane & 7;
-  float *kb = smem + warp * C::WARP_F, *vb = kb + 2 * C::PAGE_F;
+  float *kb = smem + warp * C::WARP_F, *vb = kb + (KV8 ? 1 : 2) * C::PAGE_F;
+  uint8_t *kcodes = reinterpret_cast<uint8_t *>(kb + 2 * C::PAGE_F), *vcodes = kcodes + 2 * C::CODES;  // (KV8)
   const float *qs = smem + C::OFF_Q;
   volatile int *abort = &sh.abort_;
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + w.t0 / kPage;
   const int npages = (w.t1 - w.t0 + kPage - 1) / kPage;
-  const float *kc = static_cast<const float *>(p.k_cache), *vc = static_cast<const float *>(p.v_cache);
 
   // page pg of the item: first float of its (block, head), or -1 for a block outside the pool
   auto page_at = [&](int pg) -> int64_t {
@@ -103,7 +114,42 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
     __syncwarp();
     if (lane < n) ptx::bulk_load(ptx::smem_u32(dst + lane * C::LD), src + (int64_t)lane * D, D * 4u, bar);
   };
+  auto load_codes = [&](const uint8_t *src, uint8_t *dst, int bytes, uint64_t *bar) {
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      ptx::mbar_arrive_expect_tx(bar, (uint32_t)bytes);
+      ptx::bulk_load(ptx::smem_u32(dst), src, (uint32_t)bytes, bar);
+    }
+    __syncwarp();
+  };
+  // n rows of codes into rows of floats; whether one of them is NaN
+  auto decode = [&](const uint8_t *codes, float *dst, int n) -> bool {
+    bool nan = false;
+#pragma unroll 4
+    for (int c = lane; c < n * (D / 4); c += 32) {
+      const uint32_t u = reinterpret_cast<const uint32_t *>(codes)[c];
+      const float2 a = h2_to_f2(e4m3x2_to_h2(u & 0xffffu)), b = h2_to_f2(e4m3x2_to_h2(u >> 16));
+      nan |= __vcmpeq4(u & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+      *reinterpret_cast<float4 *>(dst + c / (D / 4) * C::LD + c % (D / 4) * 4) = make_float4(a.x, a.y, b.x, b.y);
+    }
+    __syncwarp();
+    return __any_sync(0xffffffffu, nan);
+  };
   auto rows_of = [&](int pg) { return min(kPage, w.t1 - w.t0 - pg * kPage); };
+  // a page's copy into K buffer `buf`, or into V's
+  auto load_k = [&](int64_t at, uint32_t buf, int n) {
+    if constexpr (KV8)
+      load_codes(static_cast<const uint8_t *>(p.k_cache) + at, kcodes + buf * C::CODES, n * D, &sh.kbar[warp][buf]);
+    else
+      load(static_cast<const float *>(p.k_cache) + at, kb + buf * C::PAGE_F, n, &sh.kbar[warp][buf]);
+  };
+  auto load_v = [&](int64_t at, int n) {
+    if constexpr (KV8)
+      load_codes(static_cast<const uint8_t *>(p.v_cache) + at, vcodes, n * D, &sh.vbar[warp]);
+    else
+      load(static_cast<const float *>(p.v_cache) + at, vb, n, &sh.vbar[warp]);
+  };
 
   float2 o[RL][2 * CI];
   float m[RL], l[RL];
@@ -116,25 +162,31 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
   }
   bool ok = true;
   int64_t at = warp < npages ? page_at(warp) : -1;
-  if (at >= 0) load(kc + at, kb + (nk & 1) * C::PAGE_F, rows_of(warp), &sh.kbar[warp][nk & 1]);
+  if (at >= 0) load_k(at, nk & 1, rows_of(warp));
   for (int pg = warp; pg < npages && ok; pg += kWarps) {
     const int64_t cur = at;
     at = pg + kWarps < npages ? page_at(pg + kWarps) : -1;
     if (cur < 0) {  // outside the pool: the request is flagged, its outputs are unspecified
       if (lane == 0) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, w.r);
-      if (at >= 0) load(kc + at, kb + (nk & 1) * C::PAGE_F, rows_of(pg + kWarps), &sh.kbar[warp][nk & 1]);
+      if (at >= 0) load_k(at, nk & 1, rows_of(pg + kWarps));
       continue;
     }
     const int n = rows_of(pg);
     const uint32_t ks = nk & 1, kpar = (nk >> 1) & 1;
     ++nk;
-    load(vc + cur, vb, n, &sh.vbar[warp]);
-    if (at >= 0) load(kc + at, kb + (nk & 1) * C::PAGE_F, rows_of(pg + kWarps), &sh.kbar[warp][nk & 1]);
+    load_v(cur, n);
+    if (at >= 0) load_k(at, nk & 1, rows_of(pg + kWarps));
+    float ks2 = scale_log2, vs = 1.0f;
+    if constexpr (KV8) {
+      ks2 *= __ldg(p.k_scale + cur / (kPage * D));
+      vs = __ldg(p.v_scale + cur / (kPage * D));
+    }
     const uint32_t vpar = nv & 1;
     ++nv;
     // ---- scores
     if (!wait_page(&sh.kbar[warp][ks], kpar, abort)) { ok = false; }
-    float *kp = kb + ks * C::PAGE_F;
+    float *kp = kb + (KV8 ? 0 : ks) * C::PAGE_F;
+    if constexpr (KV8) decode(kcodes + ks * C::CODES, kp, n);
     float2 s2[RL][2];
 #pragma unroll
     for (int j = 0; j < RL; ++j) s2[j][0] = s2[j][1] = make_float2(0.0f, 0.0f);
@@ -161,8 +213,8 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
 #pragma unroll
     for (int j = 0; j < RL; ++j) {
       const int rho = la + 4 * j;
-      const float a = rho >= vis0 ? (s2[j][0].x + s2[j][0].y) * scale_log2 : -INFINITY;
-      const float b = rho >= vis1 ? (s2[j][1].x + s2[j][1].y) * scale_log2 : -INFINITY;
+      const float a = rho >= vis0 ? (s2[j][0].x + s2[j][0].y) * ks2 : -INFINITY;
+      const float b = rho >= vis1 ? (s2[j][1].x + s2[j][1].y) * ks2 : -INFINITY;
       float mx = fmaxf(a, b);
 #pragma unroll
       for (int x = 1; x < 8; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
@@ -187,16 +239,38 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < RL; ++j) {
-      kp[(la + 4 * j) * C::PLD + lb] = pw[j][0];
-      kp[(la + 4 * j) * C::PLD + lb + 8] = pw[j][1];
+      kp[(la + 4 * j) * C::PLD + lb] = KV8 ? pw[j][0] * vs : pw[j][0];
+      kp[(la + 4 * j) * C::PLD + lb + 8] = KV8 ? pw[j][1] * vs : pw[j][1];
     }
     __syncwarp();
     // ---- O += P V
     if (!wait_page(&sh.vbar[warp], vpar, abort)) { ok = false; }
+    bool nan = false;
+    if constexpr (KV8) nan = decode(vcodes, vb, n);
     if (n < kPage) {  // rows past the item carry weight zero: nothing stale may reach the products
       for (int t = n; t < kPage; ++t)
         for (int d = lane; d < D; d += 32) vb[t * C::LD + d] = 0.0f;
       __syncwarp();
+    }
+    if (KV8 && nan) {  // a key that a row does not see adds nothing, whatever it holds
+#pragma unroll 1
+      for (int t = 0; t < n; ++t) {
+        const int vis = g * max(w.t0 + pg * kPage + t - w.ctx, 0) - w.row0;  // rows >= vis see the key
+#pragma unroll
+        for (int j = 0; j < RL; ++j) {
+          const float x = kp[(la + 4 * j) * C::PLD + t];
+          if (la + 4 * j >= vis) {
+#pragma unroll
+            for (int i = 0; i < CI; ++i) {
+              const float4 v = *reinterpret_cast<const float4 *>(vb + t * C::LD + 4 * lb + 32 * i);
+              o[j][2 * i] = __ffma2_rn(make_float2(x, x), make_float2(v.x, v.y), o[j][2 * i]);
+              o[j][2 * i + 1] = __ffma2_rn(make_float2(x, x), make_float2(v.z, v.w), o[j][2 * i + 1]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      continue;
     }
 #pragma unroll 1
     for (int t = 0; t < kPage; t += 2) {
@@ -244,7 +318,7 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
 
 }  // namespace
 
-template <int D>
+template <int D, bool KV8>
 __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_constant__ AttnParams p) {
   using C = Cfg<D>;
   extern __shared__ __align__(128) float smem[];
@@ -291,14 +365,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
     }
     __syncthreads();
     switch (rl) {
-      case 1: item_rows<D, 1>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 2: item_rows<D, 2>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 3: item_rows<D, 3>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 4: item_rows<D, 4>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 5: item_rows<D, 5>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 6: item_rows<D, 6>(p, w, g, smem, sh, warp, nk, nv); break;
-      case 7: item_rows<D, 7>(p, w, g, smem, sh, warp, nk, nv); break;
-      default: item_rows<D, 8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 1: item_rows<D, 1, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 2: item_rows<D, 2, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 3: item_rows<D, 3, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 4: item_rows<D, 4, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 5: item_rows<D, 5, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 6: item_rows<D, 6, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      case 7: item_rows<D, 7, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
+      default: item_rows<D, 8, KV8>(p, w, g, smem, sh, warp, nk, nv); break;
     }
     __syncthreads();
     // ---- the warps' shares merged: row rho by warp rho mod 8, a lane D / 32 columns
@@ -350,11 +424,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
   if (tid == 0 && *(volatile int *)&sh.abort_) report(p.status, WISP_DEV_TIMEOUT, p.request_ids, -1);
 }
 
+template <int D>
+static cudaError_t setup() {
+  for (auto *k : {attn_f32_kernel<D, false>, attn_f32_kernel<D, true>}) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
 cudaError_t attn_f32_setup() {
-  cudaError_t e = cudaFuncSetAttribute(attn_f32_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::SMEM);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attn_f32_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::SMEM);
-  return e;
+  const cudaError_t e = setup<128>();
+  return e == cudaSuccess ? setup<64>() : e;
 }
 
 cudaError_t attn_f32_launch(const AttnParams &p, int grid, cudaStream_t s) {
@@ -369,7 +449,9 @@ cudaError_t attn_f32_launch(const AttnParams &p, int grid, cudaStream_t s) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cfg.dynamicSmemBytes = p.D == 128 ? Cfg<128>::SMEM : Cfg<64>::SMEM;
-  return p.D == 128 ? cudaLaunchKernelEx(&cfg, attn_f32_kernel<128>, p) : cudaLaunchKernelEx(&cfg, attn_f32_kernel<64>, p);
+  const bool kv8 = p.k_scale != nullptr;
+  if (p.D == 128) return cudaLaunchKernelEx(&cfg, kv8 ? attn_f32_kernel<128, true> : attn_f32_kernel<128, false>, p);
+  return cudaLaunchKernelEx(&cfg, kv8 ? attn_f32_kernel<64, true> : attn_f32_kernel<64, false>, p);
 }
 
 }  // namespace wisp

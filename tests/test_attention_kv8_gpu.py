@@ -212,6 +212,23 @@ def test_a_nan_value_reaches_only_rows_that_see_it():
     assert np.array_equal(np.isnan(out), want)
 
 
+def test_a_nan_value_with_fp32_queries():
+    # row 0 of request 1 sees its NaN value with a weight that underflows to zero
+    c = Case(17, k=[6, 2], ctx=[250, 31], Hq=8, Hkv=2, dtype=torch.float32)
+    bt, hit = c.t["block_tables"], {}
+    for r, j, h, d in ((0, 3, 1, 17), (0, 5, 1, 17), (0, 6, 0, 100), (1, 0, 0, 0)):
+        tok = c.ctx[r] + j
+        c.t["v_cache"].view(torch.uint8)[int(bt[r, tok // PAGE]), h, tok % PAGE, d] = 0x7f
+        hit[(r, h, d)] = min(j, hit.get((r, h, d), 99))
+    c.t["q"][7:] *= 1e4
+    c.run()
+    out = c.t["out"].cpu().numpy().reshape(-1, 2, 4, c.D)
+    want = np.zeros(out.shape, bool)
+    for (r, h, d), j in hit.items():
+        want[7 * r + j: 7 * r + c.k[r] + 1, h, :, d] = True
+    assert np.array_equal(np.isnan(out), want)
+
+
 def test_extreme_magnitudes():
     for kf, vf, qf in ((2.0 ** -40, 2.0 ** 60, 1.0), (2.0 ** 30, 2.0 ** -60, 2.0 ** -30), (1.0, 2.0 ** -90, 1.0), (1.0, 2.0 ** 100, 1.0)):
         c = Case(8, k=[3], ctx=[400], Hq=4, Hkv=2)
