@@ -263,9 +263,13 @@ __device__ __forceinline__ uint32_t remote(P *p, uint32_t rank) {
   return r;
 }
 
-// A cluster per row.
+// A cluster per row.  What bounds it: with many rows the logits' bytes (2432 rows of 128K bf16: 92 us at the copy rate) and, close
+// behind, the instructions, about five an element; with few the way through a CTA's loads and barriers, of which the
+// alternatives have eight more.  Measured, bf16 rows of 128K, without alternatives / with the top 5: 2432 rows 108 / 129 us (5.75, 4.8
+// TB/s), 176 rows 12.8 / 18.8, one row 9.3 / 10.6; 1200 fp32 rows 97 / 109 us (6.3, 5.7 TB/s).  (At 80 registers a thread,
+// three CTAs on an SM and not four, 2432 rows with the top 5 took 134 us.)
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads, TOP ? 4 : 5) logprobs_kernel(const LogprobParams p) {
   constexpr int E = Vec<T>::E;
   __shared__ Shared sh;
   __shared__ uint64_t s_list[TOP ? kWarps * kList : 1];
@@ -638,10 +642,13 @@ wisp_status wisp_verify_logprobs(const wisp_logprobs_args *a, void *ws, size_t w
   if (cudaGetLastError() != cudaSuccess) return WISP_ERR_CUDA;
   if (a->rows == 0) return WISP_OK;
   const bool bf = a->logits_dtype == WISP_BF16, top = a->top_n > 0;
-  // CTAs per row: about four per SM in all, as long as each has a whole round of its threads' loads
+  // CTAs per row: as many as keep all CTAs within three per SM with alternatives (four fit; a CTA's later part, with few loads,
+  // then has others beside it) and five without (as many fit), as long as each has a whole round of its threads' loads.  Rows of
+  // 128K bf16 logits with top 5, for at least four per SM and for at most three: 110 rows 20.4, 14.9 us; 150 25.0, 16.6; 176
+  // 21.0, 18.8; 400 33.3, 30.8.  Without alternatives, at most three and at most five: 176 rows 14.5, 12.8 us.
   const int64_t rounds = ((int64_t)a->V * (bf ? 2 : 4) / 16 + kThreads * kVecs - 1) / (kThreads * kVecs);
   p.cluster = 1;
-  while (p.cluster < kMaxCluster && 2 * p.cluster <= rounds && (int64_t)a->rows * p.cluster < 4 * 152) p.cluster *= 2;
+  while (p.cluster < kMaxCluster && 2 * p.cluster <= rounds && (int64_t)a->rows * 2 * p.cluster <= (top ? 3 : 5) * 152) p.cluster *= 2;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cudaLaunchAttribute attr[2];
