@@ -27,7 +27,7 @@
 // requests of 8192 tokens, 8 KV heads, D = 128: 38.7 TFLOP/s at 32 rows (about half of the fp32
 // rate), 29.0 at 16, 4.4 TB/s at 8, 4.8 TB/s at 4.  32 requests of 512-4096 tokens with 8 to 36 rows:
 // 285 us, 26.6 TFLOP/s; shared memory is busy 51% of the time there, issue 38%, DRAM 29%.  At RL = 8 and
-// D = 128 the 255 registers do not hold everything: 116 bytes of spills a thread (none at D = 64), 0.2%
+// D = 128 the 255 registers do not hold everything: 72 bytes of spills a thread (none at D = 64), 0.2%
 // of its instructions.
 //
 // 8-bit cache: a page of codes comes by one bulk copy and is decoded into the rows that the loops read, K before the
