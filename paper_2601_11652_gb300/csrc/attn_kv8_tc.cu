@@ -30,11 +30,13 @@
 //
 // What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
 // SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
-// 4 / 16 / 32 / 36 / 64 rows: 888 / 936 / 1013 / 1469 / 1688 (D = 128; 5.6 TB/s at 4 rows), 679 / 742 / 955 / 1364 / 1568
-// (D = 64).  The bf16 cache's kernel, with twice the bytes: 1468 to 1516 and 823 to 880.  What the choices gave, at 4 / 32 / 64
-// rows of D = 128:
+// 4 / 16 / 32 / 36 / 64 rows: 890 / 935 / 1011 / 1361 / 1558 (D = 128; 5.6 TB/s at 4 rows), 683 / 726 / 905 / 1274 / 1454
+// (D = 64); pages in no order 964 / 981 / 1012 / 1361 / 1565 and 766 / 794 / 897 / 1283 / 1474.  The bf16 cache's kernel, with twice the bytes: 1468 to 1516 and 823 to 880.
+// Short items are bound by their own start and end, most of it code that is fetched again for every item: one of a
+// single tile takes 4.4 us (4 rows) to 5.4 us (20 rows), one of four tiles 6.1 to 7.3 us.  What the choices gave, at
+// 4 / 32 / 64 rows of D = 128:
 //   * two groups of warps with O in registers of four correction warps, PV products added there per tile: 990 / 1082 / 1681,
-//     and 1557 at 36 rows, against this one, with O in TMEM;
+//     and 1557 at 36 rows;
 //   * groups of at most 24 rows (three or four parts above 32 rows): 955 / 1273 / 2248 against 985 / 1200 / 1701; 16-row parts
 //     pay the group's fixed part (waits, maxima, references: about 230 instructions a warp) twice;
 //   * tensor and TMA instructions issued under elect.sync and not under `lane == 0`: 985 / 1200 / 1701 to 943 / 1129 / 1685;
@@ -43,7 +45,11 @@
 //   * a fourth stage for K: 919 / 1081 / 1691 to 893 / 1019 / 1694; for V instead: nothing;
 //   * pages in no order, eight boxes a tile, from one elected lane and not from eight: 1018 / 1144 / 1702 to 970 / 1094 / 1701
 //     (D = 64: 869 / 989 / 1579 to 761 / 946 / 1594); pages in order lose 1%;
-//   * block ids brought in 12 tiles ahead and scales 8, checked and written four tiles at a time: 1047 to 955 at 4 rows.
+//   * block ids brought in 12 tiles ahead and scales 8, checked and written four tiles at a time: 1047 to 955 at 4 rows;
+//   * less code: masks once, in TMEM, and not wherever scores are read, four rows of O at a time at the end, factors through
+//     shared memory, the queries' second look in a loop: one-tile items 5.3 to 4.4 us (4 rows), 5.9 to 5.4 (20 rows), four-tile
+//     ones 8.1 to 7.3, 36 rows 1473 to 1345.  One copy of the producers for K and V: one-tile items 4.1 us, but 7% slower with
+//     pages in no order.
 //
 // Every mbarrier wait is bounded in time; an expired wait records WISP_DEV_TIMEOUT and the CTA drains.
 #include "attn_merge.cuh"
@@ -51,6 +57,7 @@
 #include "sm100_ptx.cuh"
 
 #include <cudaTypedefs.h>
+#include <cfloat>
 #include <cstring>
 #include <mutex>
 #include <type_traits>
@@ -187,6 +194,11 @@ __device__ __forceinline__ float lg2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // The parts of an item's rows (rounded up to 8), one or two of at most kPart rows, in whole units of 8: part i starts at
 // row(i).
 struct Parts {
@@ -439,6 +451,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int turns = 4 / pt.n, part = grp / turns;
       const int r0 = pt.row(part);                   // the group's rows: r0 .. r0 + 8 nu - 1
       const int nu = (pt.row(part + 1) - r0) / 8;
+      const int ta = (grp - (int)n0) & (turns - 1);  // the group's first tile
+      if (ta >= ntiles) {  // none of the item's
+        n0 += ntiles;
+        if (!wait_bar(B.at(BR::EP_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
+        if (qd == 0) s_lr[(ob * 4 + grp) * 32 + lane] = -INFINITY;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_FULL + ob));
+        continue;
+      }
       float2 lp[kPart / 2];  // this thread's (key's) share of every row sum
 #pragma unroll
       for (int i = 0; i < kPart / 2; ++i) lp[i] = make_float2(0.0f, 0.0f);
@@ -448,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       float qf = 0.0f;                        // the queries' factor
       bool fresh = true;
-      for (int t = (grp - (int)n0) & (turns - 1); t < ntiles; t += turns, ++mine) {
+      for (int t = ta; t < ntiles; t += turns, ++mine) {
         const uint32_t n = n0 + t;
         const int buf = n & 3;
         if (!wait_bar(B.at(BR::S_FULL + buf), (n >> 2) & 1, s_abort)) { ok = false; break; }
@@ -460,10 +481,25 @@ __global__ void __launch_bounds__(kThreads, 1)
           lsv0 = fmaxf(lg2(s_sc[(n % C::SC) * 8].y), kLeastScaleLog2);
           fresh = false;
         }
-        const float fk = sc.x * qf;
-        // the scores of unit u (log2 units, plus log2 of V's scale).  Causal mask: key tok is visible to row jr iff
-        // row0 + jr >= g * (tok - ctx); keys past the item are masked too.  Only an item's last tiles (from nfull on)
-        // have such keys.
+        const float fk = fmaxf(sc.x * qf, FLT_MIN);  // (not 0, so that -inf stays: a score is wrong by 2^-100)
+        // Causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked too.
+        // Only an item's last tiles (from nfull on) have such keys: -inf in their scores' place.
+        if (__builtin_expect(t >= nfull, 0)) {
+          const int tok = t0 + t * kBT + qd * 32 + lane;
+          const int jmin = tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0 - r0));
+#pragma unroll 1
+          for (int u = 0; u < nu; ++u) {
+            uint32_t v[8];
+            ptx::tmem_ld8(tmem + lane_addr + buf * kNR + r0 + 8 * u, v);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (8 * u + i < jmin) v[i] = 0xff800000u;
+            ptx::tmem_st8(tmem + lane_addr + buf * kNR + r0 + 8 * u, v);
+          }
+          ptx::tmem_wait_st();
+        }
+        // the scores of unit u (log2 units, plus log2 of V's scale)
         auto scores = [&](int u, float (&x)[8]) {
           uint32_t v[8];
           ptx::tmem_ld8(tmem + lane_addr + buf * kNR + r0 + 8 * u, v);
@@ -473,13 +509,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), both(fk), both(lsv));
             x[2 * i] = y.x;
             x[2 * i + 1] = y.y;
-          }
-          if (__builtin_expect(t >= nfull, 0)) {
-            const int tok = t0 + t * kBT + qd * 32 + lane;
-            const int jmin = tok >= t1 ? kNR : max(0, min(kNR, g * max(tok - ctx, 0) - row0 - r0));
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (8 * u + i < jmin) x[i] = -INFINITY;
           }
         };
         float4 *rd = red + (mine & 1) * 4 * 8;
@@ -531,9 +560,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (__builtin_expect(__any_sync(0xffffffffu, ref.x != m[0] || ref.y != m[1]), 0)) {
           const float a0 = m[0] == -INFINITY || ref.x == m[0] ? 1.0f : ptx::ex2(m[0] - ref.x);
           const float a1 = m[1] == -INFINITY || ref.y == m[1] ? 1.0f : ptx::ex2(m[1] - ref.y);
+          if (lane < kPart / 2) reinterpret_cast<float2 *>(mw)[lane] = make_float2(a0, a1);
+          __syncwarp();
 #pragma unroll
-          for (int i = 0; i < kPart / 2; ++i)
-            lp[i] = __fmul2_rn(lp[i], make_float2(__shfl_sync(0xffffffffu, a0, i), __shfl_sync(0xffffffffu, a1, i)));
+          for (int i = 0; i < kPart / 4; ++i) {
+            const float4 f = reinterpret_cast<const float4 *>(mw)[i];
+            lp[2 * i] = __fmul2_rn(lp[2 * i], make_float2(f.x, f.y));
+            lp[2 * i + 1] = __fmul2_rn(lp[2 * i + 1], make_float2(f.z, f.w));
+          }
+          __syncwarp();
           m[0] = ref.x;
           m[1] = ref.y;
           if (lane < kPart / 2)
@@ -711,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
       const bool whole = w.poff < 0;
       float *part = p.partials + w.poff;
-      reinterpret_cast<float2 *>(cw)[lane] = whole ? make_float2(1.0f / l[0], 1.0f / l[1]) : both(1.0f);
+      reinterpret_cast<float2 *>(cw)[lane] = whole ? make_float2(rcp(l[0]), rcp(l[1])) : both(1.0f);
       if (!whole && qd == 0) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -730,13 +765,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int wrap = (p.Hq - g + 1) * D;  // from a position's last head to the next one's first
       const uint32_t at = tmem + lane_addr + 256 + ob * 128;
 #pragma unroll 1
-      for (int r = 0; r < nrow; r += 8) {
-        uint32_t hi[8], lo[8];
-        ptx::tmem_ld8(at + r, hi);
-        ptx::tmem_ld8(at + nrow + r, lo);
+      for (int r = 0; r < w.rows; r += 4) {
+        uint32_t hi[4], lo[4];
+        ptx::tmem_ld4(at + r, hi);
+        ptx::tmem_ld4(at + nrow + r, lo);
         ptx::tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
           float o = (__uint_as_float(hi[i]) + __uint_as_float(lo[i])) * cw[r + i];
           if (r + i >= nan0) o = NAN;  // a value that is NaN: rows from nan0 on see it
           if (dval && r + i < w.rows) {
@@ -923,8 +958,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
       // ------------------------------------------------------------------ Q loaders
       // Query row row0 + rho = j * g + hh at MMA row rho (hi) and 64 + rho (lo), rows past the item up to the MMA's N zero.
-      // The rows are read twice, for the item's exponent e (their largest magnitude is at most 448 * 2^e) and for their
-      // parts; the queries' factor 2^e / sqrt(D) in log2 units goes to s_qf (NaN where a query is not finite).
+      // The rows are read twice, for the item's exponent e (their largest finite magnitude is at most 448 * 2^e) and for their
+      // parts; the queries' factor 2^e / sqrt(D) in log2 units goes to s_qf.  What is not finite becomes NaN in both parts, and
+      // the scores of its own row with it.
       const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
       constexpr int CPR = D / 8;     // 16-byte chunks per row, a lane each
       constexpr int RPP = 32 / CPR;  // rows per warp pass
@@ -947,13 +983,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           return __ldg(reinterpret_cast<const uint4 *>(qi + (int64_t)(jj * p.Hq + hh) * D));
         };
         uint32_t big = 0;  // largest magnitude, as bf16 bits
-#pragma unroll 4
-        for (int row = wq * RPP + lane / CPR; row < rows; row += STEP) {
-          const uint4 v = load(row);
+        auto look = [&](const uint4 &v) {
           const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-        }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a = w[i] & 0x7fffu, b = (w[i] >> 16) & 0x7fffu;
+            big = max(big, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+          }
+        };
+        const int first = wq * RPP + lane / CPR;
+#pragma unroll 4
+        for (int row = first; row < rows; row += STEP) look(load(row));
         __syncwarp();
         big = __reduce_max_sync(0xffffffffu, big);
         // the three warps' maxima (slot li & 1: its readers of item li - 2 have all arrived at item li - 1 since)
@@ -961,27 +1001,32 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_qmax[(li & 1) * 4 + wq] = big;
           ptx::mbar_arrive(B.at(BR::QX));
         }
+        uint4 v = load(first);
         if (!wait_bar(B.at(BR::QX), li & 1, s_abort) || !wait_bar(B.at(BR::Q_EMPTY + qb), ((li >> 1) & 1) ^ 1, s_abort)) {
           ok = false;
           break;
         }
         big = max(s_qmax[(li & 1) * 4], max(s_qmax[(li & 1) * 4 + 1], s_qmax[(li & 1) * 4 + 2]));
-        const bool finite = big < 0x7f80u;
-        const int e = finite ? scale_exp(__uint_as_float(big << 16)) : 0;
+        const int e = scale_exp(__uint_as_float(big << 16));
         const float inv = exp2i(-e);
-        if (wq == 0 && lane == 0) s_qf[li % C::RF] = finite ? exp2i(e) * scale_log2 : NAN;
+        if (wq == 0 && lane == 0) s_qf[li % C::RF] = exp2i(e) * scale_log2;
         uint8_t *qs = smem + C::OFF_Q + qb * C::Q_BYTES;
-#pragma unroll 2
-        for (int row = wq * RPP + lane / CPR; row < nrow; row += STEP) {
-          const uint4 v = load(row);
+        auto put = [&](int row, const uint4 &v) {
+          // (x * 0: an infinity becomes NaN)
+          auto low = [&](uint32_t w) { const float x = __uint_as_float(w << 16); return fmaf(x, 0.0f, x * inv); };
+          auto high = [&](uint32_t w) { const float x = __uint_as_float(w & 0xffff0000u); return fmaf(x, 0.0f, x * inv); };
           uint32_t hi[2], lo[2];
-          split4(__uint_as_float(v.x << 16) * inv, __uint_as_float(v.x & 0xffff0000u) * inv, __uint_as_float(v.y << 16) * inv,
-                 __uint_as_float(v.y & 0xffff0000u) * inv, hi[0], lo[0]);
-          split4(__uint_as_float(v.z << 16) * inv, __uint_as_float(v.z & 0xffff0000u) * inv, __uint_as_float(v.w << 16) * inv,
-                 __uint_as_float(v.w & 0xffff0000u) * inv, hi[1], lo[1]);
+          split4(low(v.x), high(v.x), low(v.y), high(v.y), hi[0], lo[0]);
+          split4(low(v.z), high(v.z), low(v.w), high(v.w), hi[1], lo[1]);
           const uint32_t half = (cc & 1) * 8;
           *reinterpret_cast<uint2 *>(qs + swz<D>(row, cc >> 1) + half) = make_uint2(hi[0], hi[1]);
           *reinterpret_cast<uint2 *>(qs + swz<D>(kNR + row, cc >> 1) + half) = make_uint2(lo[0], lo[1]);
+        };
+#pragma unroll 1
+        for (int row = first; row < nrow; row += STEP) {
+          const uint4 now = v;
+          v = load(row + STEP);
+          put(row, now);
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();

@@ -229,6 +229,24 @@ def test_a_nan_value_with_fp32_queries():
     assert np.array_equal(np.isnan(out), want)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_query_that_is_not_finite_reaches_only_its_own_row(dtype, value):
+    c = Case(18, k=[6, 2, 12], ctx=[250, 31, 400], Hq=8, Hkv=2, dtype=dtype)
+    at = ((3, 5, 77), (8, 0, 0), (8, 7, 127), (20, 2, 64))  # query row, head, element
+    for row, h, d in at:
+        c.t["q"][row, h, d] = 0
+    c.run()
+    before = c.t["out"].clone()
+    for row, h, d in at:
+        c.t["q"][row, h, d] = value
+    c.run()
+    hit = torch.zeros(c.t["out"].shape[:2], dtype=torch.bool, device="cuda")
+    for row, h, d in at:
+        hit[row, h] = True
+    assert torch.isnan(c.t["out"][hit]).all() and torch.equal(c.t["out"][~hit], before[~hit])
+
+
 def test_extreme_magnitudes():
     for kf, vf, qf in ((2.0 ** -40, 2.0 ** 60, 1.0), (2.0 ** 30, 2.0 ** -60, 2.0 ** -30), (1.0, 2.0 ** -90, 1.0), (1.0, 2.0 ** 100, 1.0)):
         c = Case(8, k=[3], ctx=[400], Hq=4, Hkv=2)
