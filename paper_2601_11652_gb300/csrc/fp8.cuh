@@ -7,7 +7,6 @@
 
 namespace wisp {
 
-constexpr float kE4m3Max = 448.0f;
 // Exponents of the scales that the library writes: far inside fp32, so that scales, their reciprocals and
 // scaled values never leave it.
 constexpr int kScaleExpMin = -96, kScaleExpMax = 120;
@@ -17,12 +16,6 @@ constexpr int kScaleExpMin = -96, kScaleExpMax = 120;
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-  return r;
-}
-// the same from two halves
-__device__ __forceinline__ uint32_t e4m3x2_h(uint32_t h2) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h2));
   return r;
 }
 // two e4m3 codes (in the low 16 bits) -> two halves, exactly
