@@ -264,10 +264,11 @@ __device__ __forceinline__ uint32_t remote(P *p, uint32_t rank) {
 }
 
 // A cluster per row.  What bounds it: with many rows the logits' bytes (2432 rows of 128K bf16: 92 us at the copy rate) and, close
-// behind, the instructions, about five an element; with few the way through a CTA's loads and barriers, of which the
-// alternatives have eight more.  Measured, bf16 rows of 128K, without alternatives / with the top 5: 2432 rows 108 / 129 us (5.75, 4.8
-// TB/s), 176 rows 12.8 / 18.8, one row 9.3 / 10.6; 1200 fp32 rows 97 / 109 us (6.3, 5.7 TB/s).  (At 80 registers a thread,
-// three CTAs on an SM and not four, 2432 rows with the top 5 took 134 us.)
+// behind, the instructions, about five an element and half as many around it; with few the way through a CTA's loads and
+// barriers, of which the alternatives have eight more.  Measured, bf16 rows of 128K, without alternatives / with the top 5: 2432 rows
+// 104 / 120 us (6.0, 5.2 TB/s), 176 rows 13.0 / 18.3, one row 9.3 / 10.4; 1200 fp32 rows 93 / 106 us (6.6, 5.8 TB/s).  (2432 rows
+// with the top 5: 134 us at 80 registers a thread, three CTAs on an SM and not four; 130 with the next round's loads copied into the
+// present ones and not taken in turn.  A reference in log2 units, one multiply-add for a difference and a product, gained 1%.)
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads, TOP ? 4 : 5) logprobs_kernel(const LogprobParams p) {
   constexpr int E = Vec<T>::E;
@@ -359,9 +360,9 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 5) logprobs_kernel(const L
   float most = -INFINITY;
   int slot = 0, left = span;
   float stretch = -INFINITY;
-  for (int base = v0; base < v1; base += kRound) {
-    if (base + kRound < v1) load(base + kRound, nxt);
-    const float cm = take(cur);
+  auto round = [&](int base, Vec<T> (&now)[kVecs], Vec<T> (&then)[kVecs]) {
+    if (base + kRound < v1) load(base + kRound, then);
+    const float cm = take(now);
     if (TOP) {
       stretch = fmaxf(stretch, cm);
       most = fmaxf(most, cm);
@@ -371,8 +372,10 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 5) logprobs_kernel(const L
         left = span;
       }
     }
-#pragma unroll
-    for (int u = 0; u < kVecs; ++u) cur[u] = nxt[u];
+  };
+  for (int base = v0; base < v1; base += 2 * kRound) {
+    round(base, cur, nxt);
+    if (base + kRound < v1) round(base + kRound, nxt, cur);
   }
   const bool edges = rank == 0 && warp == 0 && head + tail > 0;
   const int edge_id = lane < head ? lane : head + nvec * E + lane - head;
