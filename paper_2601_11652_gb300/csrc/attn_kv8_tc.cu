@@ -464,7 +464,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int i = 0; i < kPart / 2; ++i) lp[i] = make_float2(0.0f, 0.0f);
       float m[2] = {-INFINITY, -INFINITY};    // the references that lp counts in, rows r0 + 2 lw and the next
-      float lsv0 = 0.0f;                      // log2 of V's scale at the group's first key: the sums count in its inverse
       if (lane < kPart) mw[lane] = 0.0f;      // (a row without a reference: its weights are 2^-inf)
       __syncwarp();
       float qf = 0.0f;                        // the queries' factor
@@ -478,7 +477,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float lsv = fmaxf(lg2(sc.y), kLeastScaleLog2);
         if (fresh) {
           qf = s_qf[li % C::RF];
-          lsv0 = fmaxf(lg2(s_sc[(n % C::SC) * 8].y), kLeastScaleLog2);
           fresh = false;
         }
         const float fk = fmaxf(sc.x * qf, FLT_MIN);  // (not 0, so that -inf stays: a score is wrong by 2^-100)
@@ -600,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
         // P = 2^(s - reference + kHead), its shares of the sums, its two parts
-        const float2 inv2 = both(ptx::ex2(lsv0 - lsv));
+        const float2 inv2 = both(ptx::ex2(-lsv));  // (2^100 at most; of 131072 keys of weight 2^5 the sums stay below 2^122)
         uint8_t *prow = smem + C::OFF_P + buf * C::P_BYTES + (qd * 32 + lane) * 128;
         const int sw = lane & 7;
 #pragma unroll
@@ -687,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!wait_bar(B.at(BR::EP_EMPTY + ob), ((li >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
       s_hl[((ob * 4 + grp) * 4 + qd) * 32 + lane] = sum;
       if (qd == 0 && lane < kPart / 2) {
-        reinterpret_cast<float2 *>(s_lr + (ob * 4 + grp) * 32)[lane] = make_float2(m[0] - lsv0 - kHead, m[1] - lsv0 - kHead);
+        reinterpret_cast<float2 *>(s_lr + (ob * 4 + grp) * 32)[lane] = make_float2(m[0] - kHead, m[1] - kHead);
         // (the group of the last tile has the references of O^T)
         if (((n0 - 1 - grp) & (turns - 1)) == 0 && lane < 4 * nu) reinterpret_cast<float2 *>(s_fin + ob * kNR + r0)[lane] = make_float2(m[0], m[1]);
       }

@@ -247,6 +247,43 @@ def test_a_query_that_is_not_finite_reaches_only_its_own_row(dtype, value):
     assert torch.isnan(c.t["out"][hit]).all() and torch.equal(c.t["out"][~hit], before[~hit])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("first", [0.0, 2.0 ** -90, 2.0 ** 60])
+def test_value_scales_far_apart(first, D):
+    # the first page's values have a scale of their own, and the rows' maxima fall by 2^29 from the first tile to the second
+    c = Case(19, k=[10, 3, 15], ctx=[119, 300, 2000], Hq=8, Hkv=2, D=D)
+    t, g = c.t, 4
+    t["q"][:] = 0
+    t["q"][..., 0] = 16  # a key's score is 16 * its element 0 / sqrt(D)
+    for r, ctx in enumerate(c.ctx):
+        ids = t["block_tables"][r].long()
+        t["v_scale"][ids[0]] = first
+        n = (ctx + c.k[r] + PAGE) // PAGE
+        t["k_cache"].view(torch.uint8)[ids[:n], :, :, 0] = 0
+        t["k_scale"][ids[:n]] = 1.0
+        peak = torch.tensor(20.0 / math.log2(math.e) * math.sqrt(D) / 16).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        low = torch.tensor(-9.0 / math.log2(math.e) * math.sqrt(D) / 16).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        t["k_cache"].view(torch.uint8)[ids[2], :, 6, 0] = peak          # key 38
+        t["k_cache"].view(torch.uint8)[ids[8:n], :, :, 0] = low         # keys from 128 on
+    c.run()
+    at = 0
+    for r, (k, ctx) in enumerate(zip(c.k, c.ctx)):
+        L = ctx + k + 1
+        ids = t["block_tables"][r, :(L + PAGE - 1) // PAGE].long()
+        load = lambda x: (t[x + "_cache"].view(torch.uint8)[ids].view(torch.float8_e4m3fn).double() *
+                          t[x + "_scale"][ids].double()[:, :, None, None]).permute(1, 0, 2, 3).reshape(2, -1, D)[:, :L]
+        K, W = load("k"), load("v")
+        s = torch.einsum("jhgd,htd->jhgt", t["q"][at:at + k + 1].double().view(k + 1, 2, g, D), K) / math.sqrt(D)
+        seen = torch.arange(L, device="cuda") <= ctx + torch.arange(k + 1, device="cuda")[:, None]
+        w = torch.softmax(torch.where(seen[:, None, None], s, -math.inf), dim=3)
+        ref, A = torch.einsum("jhgt,htd->jhgd", w, W), torch.einsum("jhgt,htd->jhgd", w, W.abs())
+        got = t["out"][at:at + k + 1].double().view(ref.shape)
+        at += k + 1
+        # besides the usual bound, half of P's least step for every key, against the least P of the largest product's tile
+        top = (w.unsqueeze(-1) * W.abs()[None, :, None]).amax((3, 4))[..., None]
+        assert ((got - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -7 * A + 2.0 ** -9 * top * math.sqrt(L)).all()
+
+
 def test_extreme_magnitudes():
     for kf, vf, qf in ((2.0 ** -40, 2.0 ** 60, 1.0), (2.0 ** 30, 2.0 ** -60, 2.0 ** -30), (1.0, 2.0 ** -90, 1.0), (1.0, 2.0 ** 100, 1.0)):
         c = Case(8, k=[3], ctx=[400], Hq=4, Hkv=2)
