@@ -51,7 +51,9 @@ typedef struct {
 size_t wisp_kv_rope_workspace_size(const wisp_kv_rope_args *a);
 
 /* wisp_kv_reserve_append (pages for tokens 0 .. c_r + k_r, new K/V rows at c_r + j) with the rotation applied to K on
- * the way, and the rotated queries in q_out.  wisp_kv_commit follows a step as for any other cache: it moves no K/V. */
+ * the way, and the rotated queries in q_out.  A request that is refused (for its length, its table or for want of pages) is
+ * left alone altogether: its rows of q_out stay as they are, so that queries rotated in place may be sent again.
+ * wisp_kv_commit follows a step as for any other cache: it moves no K/V. */
 wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

@@ -21,7 +21,6 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kCtasPerSM = 8;
-constexpr int kMaxScan = 1024;  // requests whose first rows a CTA finds itself
 
 struct RopeParams {
   int Hq, rot8;          // queries' heads; rotated elements / 8
@@ -256,81 +255,29 @@ __device__ __forceinline__ void quantise_page(const RopeParams &o, T *stage, uin
   if (lane == 0) *scale = exp2i(e);
 }
 
-// The requests' first rows, from their lengths as the reservation reads them (negative ones count as 0), in shared memory.
-struct Rows {
-  int32_t first[kMaxScan + 1];
-  int64_t sum[kThreads / 32];
-};
-__device__ void scan_rows(const KvParams &p, Rows &sh) {
-  constexpr int PER = kMaxScan / kThreads;
-  const int tid = threadIdx.x, lane = tid & 31;
-  int64_t k[PER], mine = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int r = tid * PER + i;
-    k[i] = r < p.B ? (int64_t)max(0, __ldg(p.draft_lens + r)) + 1 : 0;
-    mine += k[i];
-  }
-  int64_t x = mine;
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t o = __shfl_up_sync(0xffffffffu, x, d);
-    if (lane >= d) x += o;
-  }
-  if (lane == 31) sh.sum[tid >> 5] = x;
-  __syncthreads();
-  x -= mine;
-  for (int w = 0; w < tid >> 5; ++w) x += sh.sum[w];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    sh.first[tid * PER + i] = (int32_t)(x < INT32_MAX ? x : INT32_MAX);
-    x += k[i];
-  }
-  if (tid == kThreads - 1) sh.first[kMaxScan] = (int32_t)(x < INT32_MAX ? x : INT32_MAX);
-  __syncthreads();
-}
-
-// A warp per unit.  The first o.q_ctas CTAs rotate queries: of up to kMaxScan requests they find a row's request and
-// position themselves and do not wait for the reservation, which leaves all but eight SMs idle (8 prompts of 700-1023 tokens: 39 us with
-// the queries after it, 36 beside it).  The others write K and V: a page of one head, or some heads of one row.
-// What bounds it: the reservation's chain of dependent reads in front (8 to 10 us), then HBM.  Measured with the reservation,
-// D = 128, 8 KV and 32 query heads, e4m3 cache: 8 prompts of 700-1023 tokens 36 us (4.4 TB/s; into a bf16 cache 33 us, 5.1 TB/s),
-// 32 of 200-1023 81 us (5.5 TB/s), 256 requests of 2 to 17 rows 24 us (2.4 TB/s), one row 8.8 us.
+// A warp per unit.  The first o.q_ctas CTAs rotate queries, the others write K and V: a page of one head, or some heads of one row.
+// Nothing is written before the reservation is done, whatever it is: queries may be rotated in place, and those of a request
+// that it refuses have to stay as they are.  A warp's first loads are on their way by then.
+// What bounds it: the reservation's chain of dependent reads in front (8 to 10 us), then HBM.  Measured, whole calls with the
+// reservation, D = 128, 8 KV and 32 query heads, e4m3 cache: 8 prompts of 700-1023 tokens 41.5 us, 256 requests of 2 to 17 rows
+// 28.5 us, one row 10.3 us.  (With the queries rotated and stored beside the reservation 38.8, 26.4 and 10.3 us, those of
+// refused requests among them.)
 template <typename T, bool Q8, int D, bool INTER>
 __global__ void __launch_bounds__(kThreads, kCtasPerSM) kv_append_rope_kernel(const KvParams p, const RopeParams o) {
   __shared__ __align__(16) T s_stage[Q8 ? kThreads / 32 * kKvPage * D : 1];
-  __shared__ Rows s_rows;
   constexpr int HC = heads_per_unit<T, D>();
   const int lane = threadIdx.x & 31;
   const int64_t T_rows = p.total_rows;
   if ((int)blockIdx.x < o.q_ctas) {
-    const bool alone = p.B <= kMaxScan;
-    if (alone)
-      scan_rows(p, s_rows);
-    else
-      asm volatile("griddepcontrol.wait;" ::: "memory");
     const int qc = (o.Hq + HC - 1) / HC;
     const int64_t units = T_rows * qc, nwarps = (int64_t)o.q_ctas * (kThreads / 32);
     for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < units; u += nwarps) {
       const int64_t x = u / qc;
       const int c = (int)(u % qc);
       move_heads<T, D, INTER, D>(o, reinterpret_cast<const T *>(o.q + x * o.q_stride), c * HC, o.Hq, true, [&](int &pos) -> T * {
-        T *dst = reinterpret_cast<T *>(o.q_out) + x * o.Hq * D;
-        if (!alone) {
-          pos = p.row_pos[x];
-          return p.row_req[x] < 0 ? nullptr : dst;
-        }
-        int lo = 0, hi = kMaxScan;  // the last request whose first row is <= x
-        while (lo < hi - 1) {
-          const int mid = (lo + hi) >> 1;
-          if (s_rows.first[mid] <= x) lo = mid;
-          else hi = mid;
-        }
-        // (requests that the reservation will refuse for their lengths, and rows of nobody)
-        if (lo >= p.B || x >= s_rows.first[lo + 1]) return nullptr;
-        const int64_t k = __ldg(p.draft_lens + lo), ctx = p.context_lens[lo];
-        if (k < 0 || ctx < 0 || ctx + k + 1 > p.max_tokens) return nullptr;
-        pos = (int)(ctx + x - s_rows.first[lo]);
-        return dst;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        pos = p.row_pos[x];
+        return p.row_req[x] < 0 ? nullptr : reinterpret_cast<T *>(o.q_out) + x * o.Hq * D;
       });
     }
     return;
@@ -476,7 +423,7 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return WISP_ERR_CUDA;
-  o.q_ctas = ctas(q_units, (int64_t)sms * 2);  // (four or eight per SM take room from the others)
+  o.q_ctas = ctas(q_units, (int64_t)sms * 2);  // (8 prompts: with one per SM 51 us, two or four 42, eight 45)
   if (kv_reserve_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);

@@ -307,3 +307,64 @@ def test_empty_batch():
     wb.wisp_kv_reserve_append_rope(a, ws)
     torch.cuda.synchronize()
     assert wb.wisp_verify_get_device_status(ws)[0] == 0 and torch.equal(before, c.t["k_cache"])
+
+
+@pytest.mark.parametrize("B", [3, 1023, 1024, 1025, 1500])
+@pytest.mark.parametrize("why", ["no_blocks", "bad_block"])
+def test_queries_of_a_request_refused_for_its_pages_stay(why, B):
+    """Whatever the batch's size: a refused request's queries are not written, so that in place they may be sent again."""
+    k = [3, 40, 2] + [0] * (B - 3)
+    ctx = [40, 62, 9] + [17] * (B - 3)
+
+    def refuse(c):
+        if why == "no_blocks":  # request 1 wants three pages: it gets none, and those after it that need one neither
+            c.t["free_count"][0] = 2
+            return 7, [1, 2] + list(range(3, B))
+        c.t["block_tables"][1, 0] = 10 ** 6
+        return 2, [1]
+
+    for in_place in (False, True):
+        c = Case(B, k=k, ctx=ctx, D=64, Hq=2, Hkv=1, rot=32)
+        code, skipped = refuse(c)
+        if in_place:
+            c.t["q"] = c.t["q"].clone(memory_format=torch.contiguous_format)
+            c.t["q_out"] = c.t["q"]
+        before = c.snapshot()
+        c.run(expect=code)
+        rows = torch.from_numpy(np.isin(np.repeat(np.arange(B), np.array(k) + 1), skipped)).cuda()
+        assert torch.equal(c.t["q_out"][rows], before["q_out"][rows])
+        c.check(before, skipped=skipped)
+        if in_place and why == "no_blocks":  # pages are freed: the refused requests' own queries, sent again, are rotated once
+            c.t["free_count"][0] = len(c.free)
+            c.t["free_blocks"][:] = torch.tensor(c.free + [0] * (c.t["free_blocks"].numel() - len(c.free)), dtype=torch.int32)
+            c.t["block_tables"].copy_(before["block_tables"])
+            c.t["q"][~rows] = before["q"][~rows]
+            c.run()
+            c.check(before)
+
+
+@pytest.mark.parametrize("B", [1023, 1024, 1025, 1500])
+def test_many_requests(B):
+    rng = np.random.default_rng(B)
+    c = Case(B, k=rng.integers(0, 6, B), ctx=rng.integers(0, 60, B), D=64, Hq=2, Hkv=1)
+    before = c.snapshot()
+    c.run()
+    c.check(before)
+
+
+@pytest.mark.parametrize("B", [5, 1025])
+def test_a_negative_length_and_rows_of_nobody(B):
+    # request 1's length is negative: it counts as 0 where the rows of those after it begin
+    c = Case(B, k=[2, 0, 7] + [1] * (B - 3), ctx=[20, 30, 9] + [33] * (B - 3), D=64, Hq=2, Hkv=1)
+    c.t["draft_lens"][1] = -3
+    before = c.snapshot()
+    assert c.run(expect=1) == 1
+    c.check(before, skipped=[1])
+    assert torch.all(c.t["q_out"][3] == -7)
+    # more rows than the requests have
+    c = Case(B + 1, k=[2, 5, 7] + [1] * (B - 2), ctx=[20, 30, 9] + [33] * (B - 2), D=64, Hq=2, Hkv=1)
+    before = c.snapshot()
+    short = {n: c.t[n][:-1] for n in ("draft_lens", "context_lens", "block_tables")}
+    c.run(expect=1, **short)
+    c.check(before, skipped=[B])
+    assert torch.all(c.t["q_out"][-2:] == -7)
