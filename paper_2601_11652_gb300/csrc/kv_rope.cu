@@ -53,19 +53,6 @@ __device__ __forceinline__ Groups groups_of(int l, const RopeParams &o) {
 template <typename T>
 struct Four {
   uint32_t w[sizeof(T)];
-  __device__ __forceinline__ void load(const T *src) {
-    if (sizeof(T) == 2) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
-      w[0] = v.x;
-      w[1] = v.y;
-    } else {
-      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
-      w[0] = v.x;
-      w[1] = v.y;
-      w[sizeof(T) - 2] = v.z;
-      w[sizeof(T) - 1] = v.w;
-    }
-  }
   __device__ __forceinline__ void read(const T *src) {
     if (sizeof(T) == 2) {
       const uint2 v = *reinterpret_cast<const uint2 *>(src);
@@ -101,11 +88,8 @@ __device__ __forceinline__ void store4(float *dst, const float *x) { *reinterpre
 template <typename T>
 struct Raw {
   Four<T> a, b;
-  __device__ __forceinline__ void load(const T *row, const Groups &g) {
-    a.load(row + g.a);
-    b.load(row + g.b);
-  }
-  __device__ __forceinline__ void read(const T *row, const Groups &g) {  // from shared memory
+  // (plain loads: queries may be rotated in place, and what a kernel writes is not read-only memory to it)
+  __device__ __forceinline__ void read(const T *row, const Groups &g) {
     a.read(row + g.a);
     b.read(row + g.b);
   }
@@ -170,7 +154,7 @@ __device__ __forceinline__ void move_heads(const RopeParams &o, const T *src, in
   Raw<T> raw[N] = {};
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (i * RPP < left) raw[i].load(src + i * RPP * D, g);
+    if (i * RPP < left) raw[i].read(src + i * RPP * D, g);
   int pos = 0;
   T *dst = where(pos);
   if (!dst) return;
