@@ -42,7 +42,7 @@ typedef struct {
   int32_t interleaved;       /* 0: pairs (i, half + i); else pairs (2i, 2i + 1) */
   int32_t Hq;                /* query heads; 0: no queries */
   const void *q;             /* [total_q_rows, Hq, D] */
-  void *q_out;               /* [total_q_rows, Hq, D] packed; may be q itself where q is packed */
+  void *q_out;               /* [total_q_rows, Hq, D] packed; q itself where q is packed, or apart from it */
   int64_t q_stride, k_stride, v_stride;  /* elements between rows of q, k_new and v_new (they may be parts of one
                                             projection output); 0: packed.  A multiple of 16 bytes each */
 } wisp_kv_rope_args;

@@ -340,6 +340,12 @@ wisp_status rope_check(const wisp_kv_rope_args *a, bool call) {
     return stride != 0 && (stride < heads * kv.D || stride > INT64_MAX / es / kv.total_q_rows || stride * es % 16 != 0);
   };
   if (bad(a->k_stride, kv.Hkv) || bad(a->v_stride, kv.Hkv) || (a->Hq > 0 && bad(a->q_stride, a->Hq))) return WISP_ERR_INVALID_ARG;
+  if (a->Hq > 0) {  // q_out over q: the same packed rows, or none
+    const uint64_t row = (uint64_t)a->Hq * kv.D * es, T = kv.total_q_rows, q = (uintptr_t)a->q, out = (uintptr_t)a->q_out;
+    const uint64_t step = a->q_stride ? (uint64_t)a->q_stride * es : row;
+    const bool in_place = q == out && (step == row || T == 1);
+    if (!in_place && q < out + T * row && out < q + (T - 1) * step + row) return WISP_ERR_INVALID_ARG;
+  }
   return WISP_OK;
 }
 

@@ -82,3 +82,16 @@ def test_binding_refuses_what_it_can_see():
         wb._check_scales(torch.zeros(4, 2, 16, 64, dtype=torch.uint8), torch.zeros(4, 2), None)
     with pytest.raises(ValueError):
         wb._check_scales(torch.zeros(4, 2, 16, 64, dtype=torch.uint8), torch.zeros(4, 3))
+
+
+def test_queries_that_overlap_their_output(lib):
+    """In place means the same packed rows; any other overlap would have rows read after they were written."""
+    size = 4 * 8 * 128 * 2
+    call = lambda **kw: lib.wisp_kv_reserve_append_rope(ctypes.byref(_args(**kw)), ctypes.c_void_p(0x100000), 1, None)
+    for kw in (dict(q_out=0x80000, q_stride=8 * 128 + 8), dict(q_out=0x80000 + 16), dict(q_out=0x80000 - 16),
+               dict(q_out=0x80000 + size - 16), dict(q_out=0x80000 + size, q_stride=8 * 128 + 8)):
+        assert call(**kw) == INVALID, kw
+    # (these reach the check of the workspace, which is too small)
+    for kw in (dict(q_out=0x80000), dict(q_out=0x80000, q_stride=8 * 128), dict(q_out=0x80000 + size), dict(q_out=0x80000 - size),
+               dict(q_out=0x80000, Hq=0), dict(kv=dict(B=1, total_q_rows=1), q_out=0x80000, q_stride=16 * 128)):
+        assert call(**kw) == WORKSPACE, kw
