@@ -53,8 +53,14 @@ size_t wisp_kv_rope_workspace_size(const wisp_kv_rope_args *a);
 /* wisp_kv_reserve_append (pages for tokens 0 .. c_r + k_r, new K/V rows at c_r + j) with the rotation applied to K on
  * the way, and the rotated queries in q_out.  A request that is refused (for its length, its table or for want of pages) is
  * left alone altogether: its rows of q_out stay as they are, so that queries rotated in place may be sent again.
- * wisp_kv_commit follows a step as for any other cache: it moves no K/V. */
+ * wisp_kv_commit_rope follows a step. */
 wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/* wisp_kv_commit with the append's limit on lengths: a request with c_r + k_r + 1 > rope_positions, whose rows the append refused,
+ * is flagged WISP_DEV_BAD_LENGTH and left unchanged.  (wisp_kv_commit knows the block table's length only, and would move such a
+ * request's prefix over tokens that were never stored, where its pages exist already.)  Reads what wisp_kv_commit reads of `kv`,
+ * rot_dim and rope_positions; the workspace is wisp_kv_rope_workspace_size's. */
+wisp_status wisp_kv_commit_rope(const wisp_kv_rope_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Attention over an 8-bit cache: wisp_attn_args with k_cache and v_cache e4m3 codes; qkv_dtype is the type of q and out.

@@ -73,7 +73,7 @@ EXPORTED = ["wisp_verify_workspace_size", "wisp_verify_attention", "wisp_verify_
             "wisp_verify_get_device_status", "wisp_verify_status_string", "wisp_verify_device_code_string",
             "wisp_verify_accept_noalloc", "wisp_verify_accept_greedy", "wisp_kv_workspace_size",
             "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope",
-            "wisp_verify_attention_kv8", "wisp_verify_step_kv8", "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
+            "wisp_kv_commit_rope", "wisp_verify_attention_kv8", "wisp_verify_step_kv8", "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
 
 
 def lib_path() -> str:
@@ -118,8 +118,9 @@ def load(path: str | None = None):
     RP = ctypes.POINTER(wisp_kv_rope_args)
     lib.wisp_kv_rope_workspace_size.argtypes = [RP]
     lib.wisp_kv_rope_workspace_size.restype = ctypes.c_size_t
-    lib.wisp_kv_reserve_append_rope.argtypes = [RP, _P, ctypes.c_size_t, _P]
-    lib.wisp_kv_reserve_append_rope.restype = ctypes.c_int
+    for fn in ("wisp_kv_reserve_append_rope", "wisp_kv_commit_rope"):
+        getattr(lib, fn).argtypes = [RP, _P, ctypes.c_size_t, _P]
+        getattr(lib, fn).restype = ctypes.c_int
     A8 = ctypes.POINTER(wisp_attn_kv8_args)
     lib.wisp_verify_attention_kv8.argtypes = [A8, _P, ctypes.c_size_t, _P]
     lib.wisp_verify_attention_kv8.restype = ctypes.c_int
@@ -303,8 +304,8 @@ def wisp_kv_commit(kv: wisp_kv_args, workspace: torch.Tensor, stream=None) -> No
 # ---- rotation on the way into the cache, 8-bit caches (include/wisp_kv8.h) ------------------------
 def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, free_count, k_cache, v_cache, k_new, v_new,
                       rope=None, q=None, q_out=None, k_scale=None, v_scale=None, interleaved=False, request_ids=None,
-                      total_q_rows=None) -> wisp_kv_rope_args:
-    """Fill wisp_kv_rope_args from device tensors: k_new / v_new [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart),
+                      total_q_rows=None, accepted_len=None) -> wisp_kv_rope_args:
+    """Fill wisp_kv_rope_args from device tensors, for the append and (with accepted_len) the commit after it: k_new / v_new [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart),
     caches of their type or e4m3 (torch.float8_e4m3fn or uint8) with k_scale / v_scale [num_blocks, Hkv], rope
     [positions, rot_dim] of cosines and sines (None: no rotation)."""
     (kp, ks), (vp, vs) = _rows_ptr(k_new), _rows_ptr(v_new)
@@ -314,7 +315,7 @@ def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, fr
         raise ValueError("free_blocks must not be longer than the pool")
     a = wisp_kv_rope_args()
     a.kv = make_kv_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, free_blocks=free_blocks,
-                        free_count=free_count, request_ids=request_ids,
+                        free_count=free_count, request_ids=request_ids, accepted_len=accepted_len,
                         total_q_rows=k_new.shape[0] if total_q_rows is None else total_q_rows)
     a.kv.Hkv, a.kv.D, a.kv.kv_dtype, a.cache_dtype = k_new.shape[1], k_new.shape[2], _dtype_code(k_new), _cache_code(k_cache)
     a.kv.block_size = k_cache.shape[2]
@@ -353,6 +354,10 @@ def wisp_kv_rope_workspace_size(a: wisp_kv_rope_args) -> int:
 def wisp_kv_reserve_append_rope(a: wisp_kv_rope_args, workspace: torch.Tensor, stream=None) -> None:
     _check("wisp_kv_reserve_append_rope", load().wisp_kv_reserve_append_rope(
         ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def wisp_kv_commit_rope(a: wisp_kv_rope_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_kv_commit_rope", load().wisp_kv_commit_rope(ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def make_attn_kv8_args(*, draft_lens, context_lens, block_tables, q, k_cache, v_cache, k_scale, v_scale, out, request_ids=None,

@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kThreads) kv_commit_kernel(const KvParams p) {
     int bad = 0;
     if (r < p.B) {
       const int64_t k = p.draft_lens[r], c = p.context_lens[r], L = p.accepted_len[r];
-      if (k < 0 || c < 0 || L < 0 || L > k || c + k + 1 > (int64_t)p.max_blocks * kPage) bad = WISP_DEV_BAD_LENGTH;
+      if (k < 0 || c < 0 || L < 0 || L > k || c + k + 1 > p.max_tokens) bad = WISP_DEV_BAD_LENGTH;
       if (!bad) {
         cnew = c + 1 + L;
         keep = (cnew + kPage - 1) / kPage;
@@ -331,6 +331,13 @@ cudaError_t kv_reserve_launch(const KvParams &p, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+wisp_status kv_commit_launch(const KvParams &p, cudaStream_t s) {
+  if (p.B == 0)
+    return cudaMemsetAsync(p.status, 0, sizeof(DeviceStatus), s) == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+  kv_commit_kernel<<<1, kThreads, 0, s>>>(p);
+  return cudaGetLastError() == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+}
+
 }  // namespace wisp
 
 using namespace wisp;
@@ -372,12 +379,7 @@ wisp_status wisp_kv_commit(const wisp_kv_args *kv, void *ws, size_t ws_bytes, vo
   if (st != WISP_OK) return st;
   const KvLayout L = kv_layout(kv);
   if ((st = kv_ws_ok(ws, ws_bytes, L)) != WISP_OK) return st;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const KvParams p = kv_params(kv, ws, L);
-  if (kv->B == 0)
-    return cudaMemsetAsync(p.status, 0, sizeof(DeviceStatus), s) == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
-  kv_commit_kernel<<<1, kThreads, 0, s>>>(p);
-  return cudaGetLastError() == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+  return kv_commit_launch(kv_params(kv, ws, L), static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

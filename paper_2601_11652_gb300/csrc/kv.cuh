@@ -34,6 +34,8 @@ wisp_status kv_ws_ok(void *ws, size_t bytes, const KvLayout &L);
 // The reservation: pages for tokens 0 .. c + k of every request, the new rows' requests and positions in
 // row_req and row_pos.  Lets its programmatic dependent start at once.
 cudaError_t kv_reserve_launch(const KvParams &p, cudaStream_t s);
+// The commit of a checked batch, up to p.max_tokens.
+wisp_status kv_commit_launch(const KvParams &p, cudaStream_t s);
 
 inline bool al16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 

@@ -349,6 +349,13 @@ wisp_status rope_check(const wisp_kv_rope_args *a, bool call) {
   return WISP_OK;
 }
 
+// wisp_kv_args' own parameters, with the longest sequence that the rotation's table allows.
+KvParams rope_params(const wisp_kv_rope_args *a, void *ws, const KvLayout &L) {
+  KvParams p = kv_params(&a->kv, ws, L);
+  if (a->rot_dim > 0 && a->rope_positions < p.max_tokens) p.max_tokens = a->rope_positions;
+  return p;
+}
+
 template <typename T, bool Q8>
 cudaError_t launch(const KvParams &p, const RopeParams &o, const cudaLaunchConfig_t &cfg) {
   if (p.D == 128)
@@ -378,10 +385,9 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   const KvLayout L = kv_layout(&kv);
   if ((st = kv_ws_ok(ws, ws_bytes, L)) != WISP_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KvParams p = kv_params(&kv, ws, L);
+  const KvParams p = rope_params(a, ws, L);
   if (kv.B == 0)
     return cudaMemsetAsync(p.status, 0, sizeof(DeviceStatus), s) == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
-  if (a->rot_dim > 0 && a->rope_positions < p.max_tokens) p.max_tokens = a->rope_positions;
   RopeParams o;
   std::memset(&o, 0, sizeof o);
   o.Hq = a->Hq;
@@ -428,6 +434,16 @@ wisp_status wisp_kv_reserve_append_rope(const wisp_kv_rope_args *a, void *ws, si
   const cudaError_t e = bf ? (q8 ? launch<uint16_t, true>(p, o, cfg) : launch<uint16_t, false>(p, o, cfg))
                            : (q8 ? launch<float, true>(p, o, cfg) : launch<float, false>(p, o, cfg));
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+}
+
+wisp_status wisp_kv_commit_rope(const wisp_kv_rope_args *a, void *ws, size_t ws_bytes, void *stream) {
+  wisp_status st = rope_check(a, false);
+  if (st != WISP_OK) return st;
+  if ((st = kv_check(&a->kv, false, true)) != WISP_OK) return st;
+  if (a->kv.B > 0 && a->rot_dim > 0 && a->rope_positions <= 0) return WISP_ERR_INVALID_ARG;
+  const KvLayout L = kv_layout(&a->kv);
+  if ((st = kv_ws_ok(ws, ws_bytes, L)) != WISP_OK) return st;
+  return kv_commit_launch(rope_params(a, ws, L), static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -11,7 +11,7 @@ all enqueued on one stream and timed with CUDA events.  With PagedSessions(cache
 scale per page and KV head, with PagedSessions(rope=...) payloads carry queries and keys that the append rotates, and with
 VerifyServer(top_n=...) a batch also answers log probabilities of the logit rows that committed a token:
 
-    wisp_kv_reserve_append_rope, wisp_verify_step_kv8, wisp_kv_commit    in the places of the three above
+    wisp_kv_reserve_append_rope, wisp_verify_step_kv8, wisp_kv_commit_rope    in the places of the three above
     wisp_verify_committed_tokens, wisp_verify_logprobs                   after the step
 
 The server's clock advances by the measured
@@ -92,21 +92,17 @@ class PagedSessions:
         return self.kv8 or self.rope is not None
 
     def _append_args(self, **kw):
-        """The arguments of the append (wisp_kv_rope_args where it rotates or encodes, else wisp_kv_args)."""
+        """The arguments of the append and of the commit after it (wisp_kv_rope_args where it rotates or encodes, else wisp_kv_args)."""
         pool = dict(free_blocks=self.free_blocks, free_count=self.free_count, k_cache=self.k_cache, v_cache=self.v_cache)
         if self.projected:
-            kw.pop("accepted_len", None)
             return wb.make_kv_rope_args(**pool, **self.scales, rope=self.rope, interleaved=self.interleaved, **kw)
         return wb.make_kv_args(**pool, **kw)
 
     def _append(self, args, ws, stream):
         (wb.wisp_kv_reserve_append_rope if self.projected else wb.wisp_kv_reserve_append)(args, ws, stream)
 
-    def _commit_args(self, args, **kw):
-        """The arguments of the commit that follows an append with `args`."""
-        if not self.projected:
-            return args
-        return wb.make_kv_args(free_blocks=self.free_blocks, free_count=self.free_count, **kw)
+    def _commit(self, args, ws, stream):
+        (wb.wisp_kv_commit_rope if self.projected else wb.wisp_kv_commit)(args, ws, stream)
 
     def _ws(self, args):
         """Workspaces of the append with `args` and of the commit after it, one or two: each call leaves its status."""
@@ -115,7 +111,6 @@ class PagedSessions:
             self.kv_ws = wb.alloc_workspace(n, self.dev)
         if not self.projected:
             return self.kv_ws, self.kv_ws
-        n = wb.wisp_kv_workspace_size(args.kv)
         if self.commit_ws is None or self.commit_ws.numel() < n:
             self.commit_ws = wb.alloc_workspace(n, self.dev)
         return self.kv_ws, self.commit_ws
@@ -140,7 +135,7 @@ class PagedSessions:
         args = self._append_args(**batch, k_new=kn, v_new=vn, accepted_len=acc)
         ws, cws = self._ws(args)
         self._append(args, ws, stream)
-        wb.wisp_kv_commit(self._commit_args(args, **batch, accepted_len=acc), cws, stream)
+        self._commit(args, cws, stream)
         torch.cuda.synchronize(self.dev)
         for w in (ws, cws):
             code, rid = wb.wisp_verify_get_device_status(w)
@@ -204,7 +199,6 @@ class VerifyServer:
         # (queries are rotated beside the append, in place)
         turn = dict(q=q, q_out=q) if s.rope is not None else {}
         kv = s._append_args(**batch, **turn, k_new=kn, v_new=vn, accepted_len=acc, total_q_rows=Tq)
-        kv_commit = s._commit_args(kv, **batch, accepted_len=acc, total_q_rows=Tq)
         attn = (wb.make_attn_kv8_args if s.kv8 else wb.make_attn_args)(
             **batch, **s.scales, q=q, k_cache=s.k_cache, v_cache=s.v_cache, out=out, num_blocks=s.num_blocks)
         step = wb.wisp_verify_step_kv8 if s.kv8 else wb.wisp_verify_step
@@ -238,7 +232,7 @@ class VerifyServer:
             if lp:
                 wb.wisp_verify_committed_tokens(accp, lp["row_tokens"], stream)
                 wb.wisp_verify_logprobs(lpa, self.lp_ws, stream)
-            wb.wisp_kv_commit(kv_commit, cws, stream)
+            s._commit(kv, cws, stream)
             b.record(stream)
         stream.synchronize()
         for ws, what in used:

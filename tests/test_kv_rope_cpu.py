@@ -95,3 +95,13 @@ def test_queries_that_overlap_their_output(lib):
     for kw in (dict(q_out=0x80000), dict(q_out=0x80000, q_stride=8 * 128), dict(q_out=0x80000 + size), dict(q_out=0x80000 - size),
                dict(q_out=0x80000, Hq=0), dict(kv=dict(B=1, total_q_rows=1), q_out=0x80000, q_stride=16 * 128)):
         assert call(**kw) == WORKSPACE, kw
+
+
+def test_commit_refusals(lib):
+    call = lambda a, ws=0x100000, size=1: lib.wisp_kv_commit_rope(ctypes.byref(a) if a else None, ctypes.c_void_p(ws), size, None)
+    new = dict(k_new=None, v_new=None, k_cache=None, v_cache=None)
+    good = dict(kv=dict(accepted_len=0xa0000, **new), q=None, q_out=None, rope=None, k_scale=None, v_scale=None)
+    assert call(_args(**good)) == WORKSPACE  # (taken, but for its workspace: it moves no rows)
+    assert call(None) == INVALID and call(_args(**good), None, 1 << 30) == WORKSPACE
+    for kw in (dict(kv=dict(new)), dict(rope_positions=0), dict(rot_dim=-16), dict(kv=dict(accepted_len=0xa0000, free_count=None))):
+        assert call(_args(**{**good, **kw})) == INVALID, kw

@@ -368,3 +368,39 @@ def test_a_negative_length_and_rows_of_nobody(B):
     c.run(expect=1, **short)
     c.check(before, skipped=[B])
     assert torch.all(c.t["q_out"][-2:] == -7)
+
+
+def _round_past_the_rotation(rot):
+    """Request 1 has pages for 80 tokens and wants positions 62 .. 66 of a table for 66: the append refuses it.  Then a step over the
+    pool and the commit."""
+    from paper_2601_11652_gb300 import binding as wb
+    c = Case(8, k=[3, 4, 2], ctx=[40, 62, 9], positions=66, missing=False, Hq=8, Hkv=2, rot=rot)
+    t, B, T, Td, V = c.t, 3, 12, 9, 1000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    acc_len, tok = (torch.full((B,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    a = c.args(accepted_len=acc_len)
+    ws = wb.alloc_workspace(wb.wisp_kv_rope_workspace_size(a))
+    wb.wisp_kv_reserve_append_rope(a, ws)
+    attn = wb.make_attn_kv8_args(draft_lens=t["draft_lens"], context_lens=t["context_lens"], block_tables=t["block_tables"], q=t["q_out"],
+                                 k_cache=t["k_cache"], v_cache=t["v_cache"], k_scale=t["k_scale"], v_scale=t["v_scale"],
+                                 out=torch.empty_like(t["q_out"]))
+    acc = wb.make_accept_args(draft_lens=t["draft_lens"], target_logits=torch.randn((T, V), generator=g, device="cuda"),
+                              draft_tokens=torch.arange(Td, dtype=torch.int32, device="cuda"),
+                              draft_probs=torch.full((Td, V), 1 / V, device="cuda"), accept_uniforms=torch.zeros(Td, device="cuda"),
+                              sample_uniforms=torch.full((B,), 0.5, device="cuda"), accepted_len=acc_len, next_token=tok)
+    vws = wb.alloc_workspace(wb.wisp_verify_workspace_size(attn.attn, acc))
+    wb.wisp_verify_step_kv8(attn, acc, vws)
+    cws = wb.alloc_workspace(wb.wisp_kv_rope_workspace_size(a))
+    wb.wisp_kv_commit_rope(a, cws)
+    torch.cuda.synchronize()
+    return c, acc_len.tolist(), [wb.wisp_verify_get_device_status(w)[0] for w in (ws, vws, cws)], wb.wisp_verify_get_device_status(cws)[1]
+
+
+def test_commit_leaves_a_request_past_the_rotation():
+    c, L, codes, who = _round_past_the_rotation(rot=64)
+    assert codes == [1, 0, 1] and who == 1 and min(L) >= 0
+    assert c.t["context_lens"].tolist() == [40 + 1 + L[0], 62, 9 + 1 + L[2]]
+    # a cache without a rotation: the block table alone limits it
+    c, L, codes, _ = _round_past_the_rotation(rot=0)
+    assert codes == [0, 0, 0]
+    assert c.t["context_lens"].tolist() == [40 + 1 + L[0], 62 + 1 + L[1], 9 + 1 + L[2]]
