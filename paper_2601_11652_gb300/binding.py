@@ -162,11 +162,14 @@ def _stream(stream) -> int | None:
 
 def _rows_ptr(t) -> tuple[int, int]:
     """Pointer and row stride (elements) of [rows, heads, D] rows that may lie apart, as parts of one projection output."""
+    if t.dim() != 3 or t.numel() and (t.stride(2) != 1 or t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("rows must be [rows, heads, D], the heads of a row contiguous")
+    row = t.shape[1] * t.shape[2]
+    if t.shape[0] > 1 and t.stride(0) < row:  # (expanded or overlapping: a stride of 0 would be read as packed rows)
+        raise ValueError("rows must not overlap")
     if not t.is_cuda:
         raise ValueError("device tensors only: the verification step runs on the GPU")
-    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
-        raise ValueError("the heads of a row must be contiguous")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else row
 
 
 def _cache_code(t: torch.Tensor) -> int:
@@ -305,18 +308,28 @@ def wisp_kv_commit(kv: wisp_kv_args, workspace: torch.Tensor, stream=None) -> No
 def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, free_count, k_cache, v_cache, k_new, v_new,
                       rope=None, q=None, q_out=None, k_scale=None, v_scale=None, interleaved=False, request_ids=None,
                       total_q_rows=None, accepted_len=None) -> wisp_kv_rope_args:
-    """Fill wisp_kv_rope_args from device tensors, for the append and (with accepted_len) the commit after it: k_new / v_new [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart),
-    caches of their type or e4m3 (torch.float8_e4m3fn or uint8) with k_scale / v_scale [num_blocks, Hkv], rope
-    [positions, rot_dim] of cosines and sines (None: no rotation)."""
-    (kp, ks), (vp, vs) = _rows_ptr(k_new), _rows_ptr(v_new)
-    if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.shape[1::2] != k_new.shape[1:]:
+    """Fill wisp_kv_rope_args from device tensors, for the append and (with accepted_len) the commit after it: k_new / v_new
+    [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart), caches of their type or e4m3 (torch.float8_e4m3fn or uint8)
+    with k_scale / v_scale [num_blocks, Hkv], rope [positions, rot_dim] of cosines and sines (None: no rotation)."""
+    total = k_new.shape[0] if total_q_rows is None else total_q_rows
+    if v_new.shape[1:] != k_new.shape[1:] or v_new.dtype != k_new.dtype:
+        raise ValueError("k_new and v_new must be [rows, Hkv, D] of one type")
+    if q is not None and (q_out is None or q.dtype != k_new.dtype or q_out.dtype != q.dtype or q_out.shape != q.shape or
+                          q.shape[2:] != k_new.shape[2:]):
+        raise ValueError("q and q_out go together, with the type and head dim of k_new")
+    if min([t.shape[0] for t in (k_new, v_new, q) if t is not None]) < total:
+        raise ValueError("k_new, v_new and q must have total_q_rows rows")
+    if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 2):
+        raise ValueError("the rotation's table is float32 [positions, rot_dim]")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.shape[1::2] != k_new.shape[1:]:
         raise ValueError("k_cache and v_cache must be [num_blocks, Hkv, 16, D] of one type")
     if k_cache.shape[0] < free_blocks.shape[0]:
         raise ValueError("free_blocks must not be longer than the pool")
+    (kp, ks), (vp, vs) = _rows_ptr(k_new), _rows_ptr(v_new)
     a = wisp_kv_rope_args()
     a.kv = make_kv_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, free_blocks=free_blocks,
                         free_count=free_count, request_ids=request_ids, accepted_len=accepted_len,
-                        total_q_rows=k_new.shape[0] if total_q_rows is None else total_q_rows)
+                        total_q_rows=total)
     a.kv.Hkv, a.kv.D, a.kv.kv_dtype, a.cache_dtype = k_new.shape[1], k_new.shape[2], _dtype_code(k_new), _cache_code(k_cache)
     a.kv.block_size = k_cache.shape[2]
     a.kv.k_cache, a.kv.v_cache, a.kv.k_new, a.kv.v_new = _ptr(k_cache), _ptr(v_cache), kp, vp
@@ -325,13 +338,9 @@ def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, fr
         _check_scales(k_cache, k_scale, v_scale)
         a.k_scale, a.v_scale = _ptr(k_scale), _ptr(v_scale)
     if rope is not None:
-        if rope.dtype != torch.float32:
-            raise ValueError("the rotation's table is float32")
         a.rope, a.rope_positions, a.rot_dim = _ptr(rope), rope.shape[0], rope.shape[1]
     a.interleaved = int(interleaved)
     if q is not None:
-        if q.dtype != k_new.dtype or q_out.dtype != q.dtype or q_out.shape != q.shape or q.shape[2] != k_new.shape[2]:
-            raise ValueError("q and q_out must have the type and head dim of k_new")
         a.Hq = q.shape[1]
         a.q, a.q_stride = _rows_ptr(q)
         a.q_out = _ptr(q_out)
@@ -365,6 +374,8 @@ def make_attn_kv8_args(*, draft_lens, context_lens, block_tables, q, k_cache, v_
     """make_attn_args over an e4m3 cache (torch.float8_e4m3fn or uint8) with scales [num_blocks, Hkv]."""
     if _cache_code(k_cache) != WISP_E4M3 or v_cache.dtype != k_cache.dtype:
         raise ValueError("k_cache and v_cache must be e4m3 (torch.float8_e4m3fn or uint8)")
+    if (num_blocks or 0) > k_cache.shape[0] or (total_q_rows or 0) > q.shape[0]:
+        raise ValueError("num_blocks and total_q_rows must not be more than the pool and q have")
     _check_scales(k_cache, k_scale, v_scale)
     a = wisp_attn_kv8_args()
     a.attn = make_attn_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, q=q, k_cache=k_cache,
@@ -387,11 +398,13 @@ def wisp_verify_step_kv8(a: wisp_attn_kv8_args, acc: wisp_accept_args, workspace
 def make_logprobs_args(*, logits, tokens, logprob, entropy=None, top_tokens=None, top_logprobs=None) -> wisp_logprobs_args:
     """Fill wisp_logprobs_args from device tensors: logits [rows, V] (rows may lie apart), tokens [rows] int32 (negative:
     the row is skipped), logprob / entropy [rows] float32, top_tokens int32 and top_logprobs float32 [rows, top_n]."""
-    if not logits.is_cuda:
-        raise ValueError("device tensors only: the verification step runs on the GPU")
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [rows, V], each row contiguous")
     rows, V = logits.shape
+    if rows > 1 and logits.stride(0) < V:  # (expanded or overlapping: a stride of 0 would be read as packed rows)
+        raise ValueError("the rows of logits must not overlap")
+    if not logits.is_cuda:
+        raise ValueError("device tensors only: the verification step runs on the GPU")
     if (top_tokens is None) != (top_logprobs is None):
         raise ValueError("top_tokens and top_logprobs go together")
     if tokens.dtype != torch.int32 or tokens.numel() != rows:

@@ -105,3 +105,38 @@ def test_commit_refusals(lib):
     assert call(None) == INVALID and call(_args(**good), None, 1 << 30) == WORKSPACE
     for kw in (dict(kv=dict(new)), dict(rope_positions=0), dict(rot_dim=-16), dict(kv=dict(accepted_len=0xa0000, free_count=None))):
         assert call(_args(**{**good, **kw})) == INVALID, kw
+
+
+def _tensors(**kw):
+    import torch
+    t, d = torch.zeros, dict(dtype=torch.bfloat16)
+    i = lambda *s: t(s, dtype=torch.int32)
+    base = dict(draft_lens=i(2), context_lens=i(2), block_tables=i(2, 4), free_blocks=i(8), free_count=i(1), k_new=t(4, 2, 64, **d),
+                v_new=t(4, 2, 64, **d), q=t(4, 8, 64, **d), q_out=t(4, 8, 64, **d), k_cache=t(8, 2, 16, 64, dtype=torch.uint8),
+                v_cache=t(8, 2, 16, 64, dtype=torch.uint8), k_scale=t(8, 2), v_scale=t(8, 2), rope=t(64, 64))
+    return {**base, **kw}
+
+
+def test_binding_refuses_rows_that_would_be_read_out_of_range():
+    """Shapes, types and strides that the library cannot see are refused before any pointer is taken (so without a GPU, too)."""
+    import torch
+
+    from paper_2601_11652_gb300 import binding as wb
+    t, d = torch.zeros, dict(dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensors only"):  # (nothing else is wrong with these)
+        wb.make_kv_rope_args(**_tensors())
+    bad = [dict(k_new=t(1, 2, 64, **d).expand(4, 2, 64)), dict(v_new=t(1, 2, 64, **d).expand(4, 2, 64)),
+           dict(q=t(1, 8, 64, **d).expand(4, 8, 64)), dict(k_new=t(1000, **d).as_strided((4, 2, 64), (64, 64, 1))),
+           dict(v_new=t(4, 2, 64)), dict(v_new=t(4, 1, 64, **d)), dict(v_new=t(4, 2, 128, **d)), dict(v_new=t(3, 2, 64, **d)),
+           dict(q=t(3, 8, 64, **d), q_out=t(3, 8, 64, **d)), dict(q_out=None), dict(total_q_rows=5), dict(rope=t(64)),
+           dict(k_cache=t(8, 2, 16, 128, dtype=torch.uint8)), dict(k_new=t(4, 128, **d))]
+    for kw in bad:
+        with pytest.raises(ValueError) as e:
+            wb.make_kv_rope_args(**_tensors(**kw))
+        assert "device tensors only" not in str(e.value), kw
+    attn = dict(draft_lens=t(2, dtype=torch.int32), context_lens=t(2, dtype=torch.int32), block_tables=t(2, 4, dtype=torch.int32),
+                q=t(4, 8, 64, **d), out=t(4, 8, 64, **d), **{n: _tensors()[n] for n in ("k_cache", "v_cache", "k_scale", "v_scale")})
+    for kw in (dict(num_blocks=9), dict(total_q_rows=5)):
+        with pytest.raises(ValueError) as e:
+            wb.make_attn_kv8_args(**attn, **kw)
+        assert "device tensors only" not in str(e.value), kw

@@ -76,3 +76,16 @@ def test_committed_tokens_refusals(lib):
     for kw in (dict(B=-1), dict(total_q_rows=1), dict(total_draft=-1), dict(draft_lens=None), dict(accepted_len=None),
                dict(next_token=None), dict(draft_tokens=None)):
         assert call(acc(**kw)) == INVALID, kw
+
+
+def test_binding_refuses_rows_that_overlap():
+    import torch
+
+    from paper_2601_11652_gb300 import binding as wb
+    out = dict(tokens=torch.zeros(3, dtype=torch.int32), logprob=torch.zeros(3))
+    for z in (torch.zeros(1, 100).expand(3, 100), torch.zeros(1000).as_strided((3, 100), (99, 1)), torch.zeros(300)):
+        with pytest.raises(ValueError) as e:
+            wb.make_logprobs_args(logits=z, **out)
+        assert "device tensors only" not in str(e.value)
+    with pytest.raises(ValueError, match="device tensors only"):
+        wb.make_logprobs_args(logits=torch.zeros(3, 100), **out)
