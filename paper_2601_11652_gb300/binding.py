@@ -160,16 +160,19 @@ def _stream(stream) -> int | None:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
-def _rows_ptr(t) -> tuple[int, int]:
-    """Pointer and row stride (elements) of [rows, heads, D] rows that may lie apart, as parts of one projection output."""
+def _check_rows(t) -> None:
     if t.dim() != 3 or t.numel() and (t.stride(2) != 1 or t.shape[1] > 1 and t.stride(1) != t.shape[2]):
         raise ValueError("rows must be [rows, heads, D], the heads of a row contiguous")
-    row = t.shape[1] * t.shape[2]
-    if t.shape[0] > 1 and t.stride(0) < row:  # (expanded or overlapping: a stride of 0 would be read as packed rows)
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2]:  # (a stride of 0 would be read as packed rows)
         raise ValueError("rows must not overlap")
+
+
+def _rows_ptr(t) -> tuple[int, int]:
+    """Pointer and row stride (elements) of [rows, heads, D] rows that may lie apart, as parts of one projection output."""
+    _check_rows(t)
     if not t.is_cuda:
         raise ValueError("device tensors only: the verification step runs on the GPU")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else row
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
 def _cache_code(t: torch.Tensor) -> int:
@@ -311,6 +314,9 @@ def make_kv_rope_args(*, draft_lens, context_lens, block_tables, free_blocks, fr
     """Fill wisp_kv_rope_args from device tensors, for the append and (with accepted_len) the commit after it: k_new / v_new
     [rows, Hkv, D] and q [rows, Hq, D] (rows may lie apart), caches of their type or e4m3 (torch.float8_e4m3fn or uint8)
     with k_scale / v_scale [num_blocks, Hkv], rope [positions, rot_dim] of cosines and sines (None: no rotation)."""
+    for t in (k_new, v_new, q):
+        if t is not None:
+            _check_rows(t)
     total = k_new.shape[0] if total_q_rows is None else total_q_rows
     if v_new.shape[1:] != k_new.shape[1:] or v_new.dtype != k_new.dtype:
         raise ValueError("k_new and v_new must be [rows, Hkv, D] of one type")
