@@ -71,14 +71,19 @@ __device__ __forceinline__ void merge_chunks(const AttnParams &p, const WorkItem
 #pragma unroll
     for (int q = 0; q < CPL; ++q) a0[q] = a1[q] = 0.0f;
     for (int c0 = 0; c0 < chunks; c0 += 32) {
-      float w0 = 0.0f, w1 = 0.0f;  // lane: chunk c0 + lane
+      float w0 = -1.0f, w1 = -1.0f;  // lane: chunk c0 + lane's weight (none: -1)
       if (c0 + lane < chunks) {
         const float *pm = base + (int64_t)(c0 + lane) * stride + w.rows * D;
         const float mc0 = __ldcg(pm + j0), mc1 = __ldcg(pm + j1);
-        w0 = mc0 == -INFINITY ? 0.0f : ptx::ex2(mc0 - m0);
-        w1 = mc1 == -INFINITY ? 0.0f : ptx::ex2(mc1 - m1);
-        den0 = fmaf(__ldcg(pm + w.rows + j0), w0, den0);
-        den1 = fmaf(__ldcg(pm + w.rows + j1), w1, den1);
+        const float lc0 = __ldcg(pm + w.rows + j0), lc1 = __ldcg(pm + w.rows + j1);
+        if (mc0 != -INFINITY) {
+          w0 = ptx::ex2(mc0 - m0);
+          den0 = fmaf(lc0, w0, den0);
+        }
+        if (mc1 != -INFINITY) {
+          w1 = ptx::ex2(mc1 - m1);
+          den1 = fmaf(lc1, w1, den1);
+        }
       }
       const int nc = min(32, chunks - c0);
 #pragma unroll 1
@@ -92,14 +97,14 @@ __device__ __forceinline__ void merge_chunks(const AttnParams &p, const WorkItem
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          // a chunk with weight zero (none of its keys visible to the row) adds nothing
+          // a chunk none of whose keys the row sees adds nothing; one whose weight is so small that it is zero adds
+          // zero times its O, which is NaN where a value is
           const float x0 = __shfl_sync(0xffffffffu, w0, (c + u) & 31);
           const float x1 = __shfl_sync(0xffffffffu, w1, (c + u) & 31);
-          const bool in = c + u < nc;
 #pragma unroll
           for (int q = 0; q < CPL; ++q) {
-            if (in && x0 != 0.0f) a0[q] = fmaf(v0[u][q], x0, a0[q]);
-            if (in && x1 != 0.0f) a1[q] = fmaf(v1[u][q], x1, a1[q]);
+            if (!(x0 < 0.0f)) a0[q] = fmaf(v0[u][q], x0, a0[q]);
+            if (!(x1 < 0.0f)) a1[q] = fmaf(v1[u][q], x1, a1[q]);
           }
         }
       }

@@ -386,3 +386,53 @@ def test_empty_batch_and_refusals():
             setattr(a, n, v)
         with pytest.raises(wb.WispError):
             wb.wisp_verify_attention_kv8(a, ws)
+
+
+def _set_scores(c, want, scale=2.0 ** -5):
+    """Keys of request r get scores want[r] (log2 units, [L]) for every query: carried by the first two elements, whose codes leave an
+    error of some 2^-7 relative (the checks take the scores from the codes)."""
+    t, D = c.t, c.D
+    t["q"][:] = 0
+    t["q"][..., :2] = 16
+    t["k_scale"][:] = scale
+    for r, s in enumerate(want):
+        x = torch.as_tensor(s, dtype=torch.float64, device="cuda") * math.log(2) * math.sqrt(D) / 16 / scale
+        assert x.abs().max() <= 448
+        hi = x.to(torch.float8_e4m3fn)
+        lo = (x - hi.double()).to(torch.float8_e4m3fn)
+        n = x.numel()
+        tok = torch.arange(n, device="cuda")
+        page = t["block_tables"][r].long()[tok // PAGE]
+        raw = t["k_cache"].view(torch.uint8)
+        for d, y in ((0, hi), (1, lo)):
+            raw[page, :, tok % PAGE, d] = y.view(torch.uint8)[:, None]
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "own"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_nan_value_in_a_chunk_of_no_weight(dtype, cache):
+    # 20005 keys of one request are cut; all keys but the first 64 weigh 2^-200: their chunks add nothing but a value that is NaN
+    from paper_2601_11652_gb300 import binding as wb
+    c = Case(50, k=[4], ctx=[20000], Hq=8, Hkv=2, dtype=dtype, garbage=False)
+    s = torch.full((20005,), -200.0)
+    s[:64] = 0
+    _set_scores(c, [s], scale=0.25)
+    c.run()
+    c.check()
+    want = np.zeros((5, 2, 4, c.D), bool)
+    for tok, h, d in ((5000, 0, 17), (12345, 1, 3)) + (((20003, 1, 99),) if cache == "e4m3" else ()):
+        c.t["v_cache"].view(torch.uint8)[int(c.t["block_tables"][0, tok // PAGE]), h, tok % PAGE, d] = 0x7f
+        want[max(0, tok - 20000):, h, :, d] = True
+    if cache == "e4m3":
+        c.run()
+    else:  # the same values in a cache of the queries' type
+        t = {n: v for n, v in c.t.items() if not n.endswith("_scale")}
+        for x in "kv":
+            t[x + "_cache"] = (c.t[x + "_cache"].float() * c.t[x + "_scale"][:, :, None, None]).to(dtype)
+        a = wb.make_attn_args(**t)
+        ws = wb.alloc_workspace(wb.wisp_verify_workspace_size(a, None))
+        wb.wisp_verify_attention(a, ws)
+        torch.cuda.synchronize()
+        assert wb.wisp_verify_get_device_status(ws)[0] == 0
+    out = c.t["out"].float().cpu().numpy().reshape(-1, 2, 4, c.D)
+    assert np.array_equal(np.isnan(out), want)
