@@ -70,8 +70,8 @@ wisp_status wisp_kv_commit_rope(const wisp_kv_rope_args *a, void *workspace, siz
  * request's tokens are not judged: pages may hold anything there.  Accumulation is fp32.  With bf16 queries, a scale of V
  * below 2^-100 counts as 2^-100 (0, too: its values come out as 2^-100 times their codes), and an
  * element of a query and a weight each enter the products with 8 significant bits (a bf16 value's own) where they are
- * large, small ones in steps: an element of 2^-16 of the largest one among the queries that share a work item, a weight of
- * 2^-8 of the largest one among 128 consecutive keys (weights below 2^-30 of the row's largest may count as nothing).  A
+ * large, small ones in steps: an element of 2^-16 of the largest one among the queries that share a work item, a weight off by
+ * 2^-15 of the largest one among 128 consecutive keys (weights below 2^-30 of the row's largest may count as nothing).  A
  * query that is not finite makes its own row of its head NaN, a value that is NaN the rows that see it in its element.
  */
 typedef struct {

@@ -5,16 +5,18 @@
 // tensor core as they are:
 //   S^T = K Q^T       (M = 128 keys of a tile, N = the item's rows, K = D),     kind::f8f6f4
 //   O^T += V^T P^T    (M = D, N = 2 * rows, K = 128 keys)
-// The other operand of each product is split into two e4m3 parts, x = (hi + lo) 2^e: 4 + 4 significant bits, what a bf16
-// value has, where hi is normal and lo not below e4m3's least, 2^-9.
-//   * Q: e is one power of two per item, its largest magnitude to at most 448.  Both parts' products add to one
-//     accumulator.  A page's K scale enters as a factor of its keys' scores.
-//   * P = 2^(s + log2(V's scale) - ref + 5): V's scale rides on P, and the sums of a row, which must not have it, take P
-//     times the inverse, in fp32.  hi and lo rows lie side by side along N and are added when O^T is read.
+// The other operand of each product is split into two e4m3 parts, with 4 + 4 significant bits, what a bf16 value has:
+//   * Q = (hi + lo) 2^e: e is one power of two per item, its largest magnitude to at most 448.  Both parts' products add to one
+//     accumulator.  An element counts in steps of 2^-9 2^e at least, e4m3's smallest.  A page's K scale enters as a factor of its keys' scores.
+//   * P = 2^(s + log2(V's scale) - ref + 5) = hi + lo / 16: V's scale rides on P, and the sums of a row, which must not have it, take P
+//     times the inverse, in fp32.  hi and lo rows lie side by side along N and are added when O^T is read; until then each has
+//     its own accumulator, so lo may have a factor: it puts P's smallest step at 2^-13.  (Without it, at 2^-9, a thousand
+//     weights of 2^-10 of their tile's largest were lost, which can be a seventh of a row.)
 //   * ref is a row's reference: the maximum of s + log2(scale) over the tile, taken anew only where the row's maximum
-//     over a tile is 3.6 above it (P must stay below 448) or 6 below it (and not 30 below the largest so far, where it
-//     weighs nothing).  So a tile's largest weight is 2^-1 or more and keeps 8 bits, its small ones count in steps of 2^-9.
-//     O^T stays in TMEM for the whole item; only where a reference moves it is read, multiplied and written back.
+//     over a tile is 3.6 above it (P must stay below 448) or 4 below it (and not 30 below the largest so far, where it
+//     weighs nothing).  So a tile's largest P is 2 or more, and a P is off by 2^-8 of itself or 2^-14, whichever is more: 128
+//     keys by at most 2^-8 of their largest together.  O^T stays in TMEM for the whole item; only where a reference moves it is
+//     read, multiplied and written back.
 //
 // Persistent CTAs (one per SM) take work items (request, KV head, key chunk, row group) from the plan's counter,
 // longest first.  28 warps:
@@ -30,8 +32,9 @@
 //
 // What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
 // SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
-// 4 / 16 / 32 / 36 / 64 rows: 890 / 935 / 1011 / 1361 / 1558 (D = 128; 5.6 TB/s at 4 rows), 683 / 726 / 905 / 1274 / 1454
-// (D = 64); pages in no order 964 / 981 / 1012 / 1361 / 1565 and 766 / 794 / 897 / 1283 / 1474.  The bf16 cache's kernel, with twice the bytes: 1468 to 1516 and 823 to 880.
+// 4 / 16 / 32 / 36 / 64 rows: 890 / 930 / 975 / 1395 / 1530 (D = 128; 5.6 TB/s at 4 rows), 715 / 765 / 905 / 1320 / 1520
+// (D = 64); pages in no order 960 / 980 / 1075 / 1385 / 1595 and 770 / 800 / 930 / 1350 / 1530.  The bf16 cache's kernel, with
+// twice the bytes: 1468 to 1516 and 823 to 880.  Lo's factor and the narrower window of the references cost up to 3% of that.
 // Short items are bound by their own start and end, most of it code that is fetched again for every item: one of a
 // single tile takes 4.4 us (4 rows) to 5.4 us (20 rows), one of four tiles 6.1 to 7.3 us.  What the choices gave, at
 // 4 / 32 / 64 rows of D = 128:
@@ -79,7 +82,8 @@ constexpr uint32_t kAhead = 3;      // the item loader takes the next item when 
 constexpr int kPart = 32;           // rows of a softmax group at most
 constexpr float kHead = 5.0f;       // log2 of P at a row's reference
 constexpr float kUp = 3.6f;         // a tile's maximum may be this far above the reference (P <= 389, e4m3 holds 448)
-constexpr float kDown = 6.0f;       // ... and this far below
+constexpr float kDown = 4.0f;       // ... and this far below (P >= 2)
+constexpr int kLoFactor = 16;       // of P's lo part (at most 256 of e4m3's 448)
 constexpr float kFar = 30.0f;       // what is this far below the largest reference so far weighs nothing
 constexpr float kLeastScaleLog2 = -100.0f;  // a V scale of 0 weighs as 2^-100, so that its keys still count in the sums
 static_assert(kNR == 64, "TMEM and shared-memory layout assume 64 rows per item");
@@ -208,24 +212,34 @@ struct Parts {
 };
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
-// Four values of magnitude at most 448 as hi + lo, four e4m3 codes each: lo is what hi's rounding left (exact in fp16),
-// rounded.
+// Four values of magnitude at most 448 as hi + lo / F, four e4m3 codes each: lo is F (1 or 16) times what hi's rounding left
+// (exact in fp16, and at most 16 F), rounded.
+template <int F>
 __device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t &hi, uint32_t &lo) {
-  asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 p0, p1, q0, q1;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f32 h0, %3, %2;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f32 h1, %5, %4;\n\t"
-      "cvt.rn.f16x2.f32 p0, %3, %2;\n\t"
-      "cvt.rn.f16x2.f32 p1, %5, %4;\n\t"
+  static_assert(F == 1 || F == 16, "factor of lo");
+  uint32_t r0, r1;
+  asm("{\n\t.reg .b16 h0, h1;\n\t.reg .b32 p0, p1, q0, q1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h0, %4, %3;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h1, %6, %5;\n\t"
+      "cvt.rn.f16x2.f32 p0, %4, %3;\n\t"
+      "cvt.rn.f16x2.f32 p1, %6, %5;\n\t"
       "cvt.rn.f16x2.e4m3x2 q0, h0;\n\t"
       "cvt.rn.f16x2.e4m3x2 q1, h1;\n\t"
-      "sub.rn.f16x2 p0, p0, q0;\n\t"
-      "sub.rn.f16x2 p1, p1, q1;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 l0, p0;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 l1, p1;\n\t"
-      "mov.b32 %0, {h0, h1};\n\t"
-      "mov.b32 %1, {l0, l1};\n\t}"
-      : "=r"(hi), "=r"(lo)
+      "sub.rn.f16x2 %1, p0, q0;\n\t"
+      "sub.rn.f16x2 %2, p1, q1;\n\t"
+      "mov.b32 %0, {h0, h1};\n\t}"
+      : "=r"(hi), "=r"(r0), "=r"(r1)
       : "f"(a), "f"(b), "f"(c), "f"(d));
+  if (F == 16) {
+    asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(r0) : "r"(0x4c004c00u));
+    asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(r1) : "r"(0x4c004c00u));
+  }
+  asm("{\n\t.reg .b16 l0, l1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l0, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l1, %2;\n\t"
+      "mov.b32 %0, {l0, l1};\n\t}"
+      : "=r"(lo)
+      : "r"(r0), "r"(r1));
 }
 
 // Byte offset of 16-byte chunk c of row `row` in a swizzled tile with rows of D bytes.
@@ -616,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y)), f = make_float2(ptx::ex2(c.x), ptx::ex2(c.y));
               lp[4 * u + 2 * h] = __ffma2_rn(e, inv2, lp[4 * u + 2 * h]);
               lp[4 * u + 2 * h + 1] = __ffma2_rn(f, inv2, lp[4 * u + 2 * h + 1]);
-              split4(e.x, e.y, f.x, f.y, hi[h], lo[h]);
+              split4<kLoFactor>(e.x, e.y, f.x, f.y, hi[h], lo[h]);
             }
             const int oh = r0 + 8 * u, ol = nrow + oh;
             *reinterpret_cast<uint2 *>(prow + (((oh >> 4) ^ sw) << 4) + (oh & 8)) = make_uint2(hi[0], hi[1]);
@@ -770,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float o = (__uint_as_float(hi[i]) + __uint_as_float(lo[i])) * cw[r + i];
+          float o = fmaf(__uint_as_float(lo[i]), 1.0f / kLoFactor, __uint_as_float(hi[i])) * cw[r + i];
           if (r + i >= nan0) o = NAN;  // a value that is NaN: rows from nan0 on see it
           if (dval && r + i < w.rows) {
             if (whole)
@@ -1014,8 +1028,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           auto low = [&](uint32_t w) { const float x = __uint_as_float(w << 16); return fmaf(x, 0.0f, x * inv); };
           auto high = [&](uint32_t w) { const float x = __uint_as_float(w & 0xffff0000u); return fmaf(x, 0.0f, x * inv); };
           uint32_t hi[2], lo[2];
-          split4(low(v.x), high(v.x), low(v.y), high(v.y), hi[0], lo[0]);
-          split4(low(v.z), high(v.z), low(v.w), high(v.w), hi[1], lo[1]);
+          split4<1>(low(v.x), high(v.x), low(v.y), high(v.y), hi[0], lo[0]);
+          split4<1>(low(v.z), high(v.z), low(v.w), high(v.w), hi[1], lo[1]);
           const uint32_t half = (cc & 1) * 8;
           *reinterpret_cast<uint2 *>(qs + swz<D>(row, cc >> 1) + half) = make_uint2(hi[0], hi[1]);
           *reinterpret_cast<uint2 *>(qs + swz<D>(kNR + row, cc >> 1) + half) = make_uint2(lo[0], lo[1]);

@@ -436,3 +436,26 @@ def test_a_nan_value_in_a_chunk_of_no_weight(dtype, cache):
         assert wb.wisp_verify_get_device_status(ws)[0] == 0
     out = c.t["out"].float().cpu().numpy().reshape(-1, 2, 4, c.D)
     assert np.array_equal(np.isnan(out), want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("strong,gap,sd", [(-5.9, 9.2, 0.0), (-5.9, 9.2, 0.3), (-3.75, 15.25, 0.0), (-3.9, 13.0, 0.0), (-2.0, 9.0, 0.3),
+                                           (-8.0, 10.0, 0.0)])
+def test_small_weights_beside_a_strong_key_in_every_tile(strong, gap, sd, D):
+    # a first key with the largest weight, and in every 128 keys one `strong` octaves from it, the others `gap` octaves below that one:
+    # each weighs little, together they carry up to a fifth.  Values of mean 1, so that nothing averages out.
+    B, ctx = 20, 4095  # 160 (request, head) pairs: no sequence is cut
+    c = Case(30, k=[0] * B, ctx=[ctx] * B, D=D, garbage=False)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    want = []
+    for r in range(B):
+        s = torch.full((ctx + 1,), strong - gap, dtype=torch.float64, device="cuda")
+        s += sd * torch.randn(s.shape, generator=g, device="cuda", dtype=torch.float64)
+        s[5 + r::128] = strong
+        s[0] = 0
+        want.append(s)
+    _set_scores(c, want)
+    c.t["v_scale"][:] = 2.0 ** -6
+    c.t["v_cache"] = ((1 + 0.3 * torch.randn(c.t["v_cache"].shape, generator=g, device="cuda")) * 64).to(torch.float8_e4m3fn)
+    c.run()
+    c.check()
