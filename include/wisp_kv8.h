@@ -67,8 +67,9 @@ wisp_status wisp_kv_commit_rope(const wisp_kv_rope_args *a, void *workspace, siz
  * Workspace: wisp_verify_workspace_size(&a->attn, acc).
  *   out[row, h] = sum_t softmax_t(<q[row, h], K[t]> / sqrt(D)) V[t], K[t] = k_code * k_scale, V[t] = v_code * v_scale
  * Scales are finite and not negative (those that the append writes are; others may be any such fp32 value).  Codes past a
- * request's tokens are not judged: pages may hold anything there.  Accumulation is fp32.  With bf16 queries, a scale of V
- * below 2^-100 counts as 2^-100 (0, too: its values come out as 2^-100 times their codes), and an
+ * request's tokens are not judged: pages may hold anything there.  Accumulation is fp32.  With bf16 queries, V scales from 2^-60
+ * to 2^40, and 0, take the tensor cores; a work item that meets others is computed in fp32 on the CUDA cores, many times as slowly.
+ * Otherwise an
  * element of a query and a weight each enter the products with 8 significant bits (a bf16 value's own) where they are
  * large, small ones in steps: an element of 2^-16 of the largest one among the queries that share a work item, a weight off by
  * 2^-15 of the largest one among 128 consecutive keys (weights below 2^-30 of the row's largest may count as nothing).  A

@@ -49,6 +49,7 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kPage = 16;
 constexpr int kRows = kF32RowsPerItem;
+constexpr float kDown = 0x1p-20f;   // factor of an 8-bit cache's values in sums: up to 2^20 of the largest stay finite
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
 
 template <int D>
@@ -179,7 +180,7 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
     float ks2 = scale_log2, vs = 1.0f;
     if constexpr (KV8) {
       ks2 *= __ldg(p.k_scale + cur / (kPage * D));
-      vs = __ldg(p.v_scale + cur / (kPage * D));
+      vs = __ldg(p.v_scale + cur / (kPage * D)) * kDown;
     }
     const uint32_t vpar = nv & 1;
     ++nv;
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
       if (w.poff < 0) {
         const int rj = w.row0 + rho;
         st_cols<CPL>(static_cast<float *>(p.out) + ((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + lane * CPL, acc,
-                     1.0f / den);
+                     (KV8 ? 1.0f / kDown : 1.0f) / den);
       } else {
         float *part = p.partials + w.poff;
 #pragma unroll
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
         __threadfence();
       }
       __syncthreads();
-      if (sh.last > 0) merge_chunks<D, float>(p, w, g, sh.last, warp, kWarps);
+      if (sh.last > 0) merge_chunks<D, float>(p, w, g, sh.last, warp, kWarps, KV8 ? 1.0f / kDown : 1.0f);
     }
   }
   if (tid == 0 && *(volatile int *)&sh.abort_) report(p.status, WISP_DEV_TIMEOUT, p.request_ids, -1);

@@ -28,7 +28,8 @@
 //   * warps 4-19, four groups of four: the softmax.  A thread has one key's scores for up to 32 rows.  Items of up to 32
 //     rows: a group has every fourth tile; of more: half of the rows of every second one.  A group's warps agree on the
 //     rows' maxima through shared memory; references go from tile to tile, in order, in a 4-slot ring;
-//   * warps 20-23 write the outputs or the (O, m, l) partials of a split item, whose last chunk merges all.
+//   * warps 20-23 write the outputs or the (O, m, l) partials of a split item, whose last chunk merges all; at their end they compute
+//     the items with V scales that P cannot carry.
 //
 // What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
 // SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
@@ -85,7 +86,10 @@ constexpr float kUp = 3.6f;         // a tile's maximum may be this far above th
 constexpr float kDown = 4.0f;       // ... and this far below (P >= 2)
 constexpr int kLoFactor = 16;       // of P's lo part (at most 256 of e4m3's 448)
 constexpr float kFar = 30.0f;       // what is this far below the largest reference so far weighs nothing
-constexpr float kLeastScaleLog2 = -100.0f;  // a V scale of 0 weighs as 2^-100, so that its keys still count in the sums
+// log2 of V's scales that P can carry: whatever the pages' order, a key that ex2 flushes to 0 for its page's scale then weighs less than
+// 2^-30 of another, and the sums stay below 2^120 for 2^20 keys.  A page with a scale of 0 counts with the least (its keys still have
+// weight), and V's producer brings zeros for it.  Items with other scales are computed in fp32 (item_in_fp32).
+constexpr float kScaleMin = -60.0f, kScaleMax = 40.0f;
 static_assert(kNR == 64, "TMEM and shared-memory layout assume 64 rows per item");
 
 template <int D>
@@ -104,9 +108,10 @@ struct Cfg {
   static constexpr int OFF_P = OFF_V + NSV * KV_TILE;
   static constexpr int OFF_BAR = OFF_P + 4 * P_BYTES;
   static constexpr int N_BAR = 2 * NSK + 2 * NSV + 28 + 2 * RING + 12;
-  static constexpr int OFF_SC = (OFF_BAR + N_BAR * 8 + 15) / 16 * 16;  // float2 [SC][8]: a page's K and V scale
+  static constexpr int OFF_SC = (OFF_BAR + N_BAR * 8 + 15) / 16 * 16;  // float2 [SC][8]: a page's K scale, log2 of its V scale
   static constexpr int OFF_RF = OFF_SC + SC * 64;                      // float [RF]
-  static constexpr int OFF_RED = OFF_RF + RF * 16;                      // float [4 groups][2][4][32] row maxima per quadrant
+  static constexpr int OFF_FAR = OFF_RF + RF * 4;                      // int [RF] item li has V scales that P cannot carry
+  static constexpr int OFF_RED = OFF_RF + RF * 16;                     // float [4 groups][2][4][32] row maxima per quadrant
   static constexpr int OFF_MW = OFF_RED + 4 * 2 * 4 * 32 * 4;          // float [16][32] per warp: kHead - reference
   static constexpr int OFF_REF = OFF_MW + kSoftmaxWarps * 32 * 4;      // float4 [4][32] two rows' references, the largest so far
   static constexpr int OFF_CW = OFF_REF + 4 * kNR * 8;                 // float [4][64] per epilogue warp
@@ -120,7 +125,8 @@ struct Cfg {
   static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
   static_assert(OFF_K % 1024 == 0 && OFF_V % 1024 == 0 && OFF_P % 1024 == 0 && OFF_RING % 16 == 0, "alignment");
   // A tile's scales are written up to three tiles ahead of its K: then S^T of the tile NSK before that K's is done and the
-  // scores of the tile NSK + 4 before have been read.  An item's factor is written two items ahead.
+  // scores of the tile NSK + 4 before have been read.  An item's factor is written two items ahead, and its mark for V scales while
+  // the epilogue warps have begun the item RING before it at the least.
   static_assert(SC >= NSK + 4 + 3 && RF >= 5, "rings");
 };
 
@@ -254,6 +260,162 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t addr) {  // eight rows of D b
 
 }  // namespace
 
+// A work item on the CUDA cores in fp32, by warp wq of nw: for V scales that P cannot carry.  A warp takes R rows; a lane has one of 32
+// keys for their scores, then D / 32 columns of the keys' values.  Values are taken times 2^-20, so that the sums of up to 2^20 of
+// the largest stay finite.  38 requests of 8192 keys, 8 KV heads, D = 128, 4 / 20 / 64 rows: 4.7 / 9.3 / 18 ms.
+template <int D>
+__device__ __forceinline__ void item_in_fp32(const AttnParams &p, const WorkItem &w, int wq, int nw) {
+  constexpr int R = 4, CPL = D / 32;
+  constexpr float kDownLog2 = 20.0f;
+  const int lane = threadIdx.x & 31, g = p.Hq / p.Hkv;
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+  const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq;
+#pragma unroll 1
+  for (int rho = wq * R; rho < w.rows; rho += nw * R) {
+    int last[R], off[R];  // the last key that a row sees, its elements' offset from the item's first query position
+    float m[R], l[R], acc[R][CPL];
+    const int64_t q0 = ((int64_t)w.q0 * p.Hq + w.h * g) * D;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int rj = w.row0 + min(rho + i, w.rows - 1), j = rj / g;  // (rows past the item: its last one once more)
+      last[i] = min(w.t1 - 1, w.ctx + j);
+      off[i] = (j * p.Hq + rj - j * g) * D;
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) acc[i][c] = 0.0f;
+    }
+#pragma unroll 1
+    for (int base = w.t0; base <= last[R - 1]; base += 32) {
+      const int tok = base + lane, bid = tok <= last[R - 1] ? __ldg(bt + tok / 16) : -1;
+      const bool in = bid >= 0 && bid < p.num_blocks;
+      const int64_t page = in ? (int64_t)bid * p.Hkv + w.h : -1;
+      float e[R], vs = 0.0f, ks = 0.0f;
+#pragma unroll
+      for (int i = 0; i < R; ++i) e[i] = 0.0f;
+      if (in) {
+        ks = __ldg(p.k_scale + page) * scale_log2;
+        vs = __ldg(p.v_scale + page) * exp2f(-kDownLog2);
+        const uint4 *k = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.k_cache) + (page * 16 + tok % 16) * D);
+        const uint16_t *q = static_cast<const uint16_t *>(p.q) + q0;
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          const uint4 kv = __ldg(k + c);
+          const uint32_t kw[4] = {kv.x, kv.y, kv.z, kv.w};
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 qv = __ldg(reinterpret_cast<const uint4 *>(q + off[i] + 16 * c + 8 * h));
+              const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const float2 x = h2_to_f2(e4m3x2_to_h2(kw[2 * h + u / 2] >> (16 * (u & 1)) & 0xffffu));
+                e[i] = fmaf(x.x, __uint_as_float(qw[u] << 16), e[i]);
+                e[i] = fmaf(x.y, __uint_as_float(qw[u] & 0xffff0000u), e[i]);
+              }
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float s = in && tok <= last[i] ? e[i] * ks : -INFINITY;
+        const float mn = fmaxf(m[i], warp_max(s));
+        const float alpha = mn == m[i] ? 1.0f : exp2f(m[i] - mn);
+        e[i] = s == -INFINITY ? 0.0f : exp2f(s - mn);
+        m[i] = mn;
+        l[i] = fmaf(l[i], alpha, e[i]);
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) acc[i][c] *= alpha;
+      }
+#pragma unroll 1
+      for (int k0 = 0; k0 < 32; k0 += 8) {
+        const int64_t pg = __shfl_sync(0xffffffffu, page, k0 & 16);
+        const float y = __shfl_sync(0xffffffffu, vs, k0 & 16);
+        if (pg < 0) continue;
+        const uint8_t *v = static_cast<const uint8_t *>(p.v_cache) + (pg * 16 + k0 % 16) * D + lane * CPL;
+        uint32_t codes[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          codes[k] = CPL == 4 ? __ldg(reinterpret_cast<const uint32_t *>(v + k * D)) : __ldg(reinterpret_cast<const uint16_t *>(v + k * D));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          float z[CPL];
+#pragma unroll
+          for (int c = 0; c < CPL; c += 2) {
+            const float2 x = h2_to_f2(e4m3x2_to_h2(codes[k] >> (8 * c) & 0xffffu));
+            z[c] = y * x.x;
+            z[c + 1] = y * x.y;
+          }
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const float x = __shfl_sync(0xffffffffu, e[i], k0 + k);
+            if (base + k0 + k <= last[i]) {  // (a key that the row does not see adds nothing, whatever it holds)
+#pragma unroll
+              for (int c = 0; c < CPL; ++c) acc[i][c] = fmaf(x, z[c], acc[i][c]);
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+      if (rho + i >= w.rows) continue;
+      if (w.poff < 0) {
+        st_cols<CPL>(static_cast<uint16_t *>(p.out) + q0 + off[i] + lane * CPL, acc[i], exp2f(kDownLog2) / l[i]);
+      } else {  // as the other chunks have them: O and l times 2^(m - kHead) are the sums
+        float *part = p.partials + w.poff;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) __stcg(part + (int64_t)(rho + i) * D + lane * CPL + c, acc[i][c]);
+        if (lane == 0) {
+          __stcg(part + w.rows * D + rho + i, m[i] + (kHead + kDownLog2));
+          __stcg(part + w.rows * D + w.rows + rho + i, l[i] * exp2f(-kDownLog2));
+        }
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// The items that this CTA's four epilogue warps marked, by the same warps at their end (not a call within the loop over items, whose
+// registers and code it would take).  `bar`: the warps' own barrier, at phase `ph`.  False: a wait ran out.
+template <int D>
+__device__ __noinline__ bool far_items(const AttnParams &p, int n_items, uint32_t bar, uint32_t ph, volatile int *s_last,
+                                       volatile int *s_abort) {
+  const int lane = threadIdx.x & 31, qd = (threadIdx.x >> 5) & 3;
+  auto group_sync = [&]() -> bool {
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(bar);
+    return wait_bar(bar, (ph++) & 1, s_abort);
+  };
+  __threadfence();
+  if (!group_sync()) return false;  // (the marks are written)
+  for (int base = 0; base < n_items; base += 32) {
+    const bool mine = base + lane < n_items && __ldcg(&p.items[base + lane].nrg) == -1 - (int)blockIdx.x;
+    for (unsigned left = __ballot_sync(0xffffffffu, mine); left; left &= left - 1) {
+      const WorkItem w = p.items[base + __ffs(left) - 1];
+      item_in_fp32<D>(p, w, qd, 4);
+      if (w.poff < 0) continue;
+      // the last chunk of the (request, head, row group) to finish merges all
+      __threadfence();
+      if (!group_sync()) return false;
+      if (qd == 0 && lane == 0) {
+        const int chunks = p.req_chunks[w.r];
+        const int done = atomicAdd(p.pair_done + ((int64_t)w.r * p.Hkv + w.h) * p.row_groups + w.rg, 1);
+        *s_last = done == chunks - 1 ? chunks : 0;
+        __threadfence();
+      }
+      if (!group_sync()) return false;
+      const int chunks = *s_last;
+      if (chunks > 0) merge_chunks<D, uint16_t>(p, w, p.Hq / p.Hkv, chunks, qd, 4);
+    }
+  }
+  return true;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_kv8_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap tmk,
@@ -267,6 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const BR B{sbase + C::OFF_BAR};
   float2 *s_sc = reinterpret_cast<float2 *>(smem + C::OFF_SC);
   float *s_qf = reinterpret_cast<float *>(smem + C::OFF_RF);
+  volatile int *s_far = reinterpret_cast<volatile int *>(smem + C::OFF_FAR);
   volatile uint32_t *s_qmax = reinterpret_cast<volatile uint32_t *>(smem + C::OFF_MISC + 32);
   float4 *s_ref = reinterpret_cast<float4 *>(smem + C::OFF_REF);
   float *s_fin = reinterpret_cast<float *>(smem + C::OFF_FIN);
@@ -276,6 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + C::OFF_MISC);
   volatile int *s_abort = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 4);
   volatile int *s_last = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 8);
+  volatile int *s_marked = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 16);  // the epilogue warps marked an item
   volatile uint32_t *s_issued = reinterpret_cast<volatile uint32_t *>(smem + C::OFF_MISC + 12);  // K tiles issued
   struct RingSlot {
     int it;
@@ -311,6 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(BR::DEC, 4, 16);      // the warps of the tile's softmax groups, as for S_EMPTY
     init(BR::FIN, 1, kThreads / 32);
     *s_issued = 0;
+    *s_marked = 0;
     *s_abort = 0;
     ptx::fence_mbar_init();
   }
@@ -488,12 +653,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait_bar(B.at(BR::S_FULL + buf), (n >> 2) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
         const float2 sc = s_sc[(n % C::SC) * 8 + qd * 2 + (lane >> 4)];
-        const float lsv = fmaxf(lg2(sc.y), kLeastScaleLog2);
+        const float lsv = sc.y;
         if (fresh) {
           qf = s_qf[li % C::RF];
           fresh = false;
         }
-        const float fk = fmaxf(sc.x * qf, FLT_MIN);  // (not 0, so that -inf stays: a score is wrong by 2^-100)
+        // (not 0, so that -inf stays: a score is wrong by 2^-100; not infinite, so that a score of 0 stays)
+        const float fk = fminf(fmaxf(sc.x * qf, FLT_MIN), FLT_MAX);
         // Causal mask: key tok is visible to row jr iff row0 + jr >= g * (tok - ctx); keys past the item are masked too.
         // Only an item's last tiles (from nfull on) have such keys: -inf in their scores' place.
         if (__builtin_expect(t >= nfull, 0)) {
@@ -612,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
         // P = 2^(s - reference + kHead), its shares of the sums, its two parts
-        const float2 inv2 = both(ptx::ex2(-lsv));  // (2^100 at most; of 131072 keys of weight 2^5 the sums stay below 2^122)
+        const float2 inv2 = both(ptx::ex2(-lsv));
         uint8_t *prow = smem + C::OFF_P + buf * C::P_BYTES + (qd * 32 + lane) * 128;
         const int sw = lane & 7;
 #pragma unroll
@@ -732,6 +898,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (it < 0) break;
       const int ob = li & 1, nrow = (w.rows + 7) / 8 * 8;
       if (!wait_bar(B.at(BR::EP_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
+      if (__builtin_expect(s_far[li % C::RF] != 0, 0)) {  // V scales that P cannot carry: marked, and computed after the others
+        *s_marked = 1;
+        if (qd == 0 && lane == 0) const_cast<WorkItem *>(p.items)[it].nrg = -1 - (int)blockIdx.x;
+        if (dval) s_nan[ob * D + d] = INT32_MAX;
+        n0 += (w.t1 - w.t0 + kBT - 1) / kBT;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(B.at(BR::EP_EMPTY + ob));
+        if (!wait_bar(B.at(BR::O_FULL + ob), (li >> 1) & 1, s_abort)) { ok = false; break; }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(B.at(BR::O_EMPTY + ob));
+        continue;
+      }
       // The row sums: four shares of each group that had the row, against its references.  The group that had the
       // item's first tile comes first, so that results repeat to the bit whatever the CTA did before.
       const int nan0 = dval ? s_nan[ob * D + d] : INT32_MAX;
@@ -814,6 +992,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (chunks > 0) merge_chunks<D, uint16_t>(p, w, g, chunks, qd, 4);
       }
     }
+    if (__builtin_expect(ok && *s_marked, 0)) ok = far_items<D>(p, n_items, B.at(BR::EGRP), gph, s_last, s_abort);
   } else if (wg == 0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     // ------------------------------------------------------------------ K / V producers
@@ -842,13 +1021,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto valid = [&](int bid) -> bool { return bid >= 0 && bid < p.num_blocks; };
         // the scales of a lane's block (K's producer brings both; blocks that do not exist: any)
         auto scales = [&](int bid) -> float2 {
-          if (!is_k || !valid(bid)) return make_float2(1.0f, 1.0f);
+          if (!valid(bid)) return make_float2(1.0f, 1.0f);
           const int64_t at = (int64_t)bid * p.Hkv + h;
-          return make_float2(__ldg(p.k_scale + at), __ldg(p.v_scale + at));
+          return make_float2(is_k ? __ldg(p.k_scale + at) : 1.0f, __ldg(p.v_scale + at));
         };
         // block ids of tiles t..t+3, t+4..t+7 and t+8..t+11, the scales of the first two
         int cur = fetch(0), nxt = fetch(32), far = fetch(64);
         float2 sc_cur = scales(cur), sc_nxt = scales(nxt);
+        bool v_far = false;               // one of the item's V scales so far is one that P cannot carry
         unsigned runs = 0;                // bit 8 i + 7 of tiles t..t+3: i's blocks are consecutive and valid
         const int ntiles = (t1 - t0 + kBT - 1) / kBT;
         for (int t = 0; t < ntiles; ++t, ++tile_n) {
@@ -860,9 +1040,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               sc_cur = sc_nxt;
               sc_nxt = scales(nxt);
             }
-            const bool good = valid(cur);
+            bool good = valid(cur);
             if (is_k && !good && 8 * t + lane < nblk) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, r);
-            if (!good) cur = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
+            if (!is_k) good = good && sc_cur.y != 0.0f;
+            if (!good) cur = p.num_blocks;  // past the item (or invalid, or V scaled by 0): out-of-range box, reads zeros
             __syncwarp();
             const int lead = __shfl_sync(0xffffffffu, cur, lane & 24);
             runs = __ballot_sync(0xffffffffu, good & (cur == lead + (lane & 7)));
@@ -890,7 +1071,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (is_k) {  // the scales, which may arrive later than the block ids, of four tiles at a time
             if (i == 0) {
-              s_sc[((tile_n + (lane >> 3)) % C::SC) * 8 + (lane & 7)] = sc_cur;
+              const float lv = sc_cur.y == 0.0f ? kScaleMin : lg2(sc_cur.y);
+              v_far |= __any_sync(0xffffffffu, !(lv >= kScaleMin && lv <= kScaleMax));
+              if (lane == 0) s_far[j % C::RF] = v_far;
+              s_sc[((tile_n + (lane >> 3)) % C::SC) * 8 + (lane & 7)] = make_float2(sc_cur.x, lv);
               __syncwarp();
             }
             if (lane == 0) ptx::mbar_arrive(full + 8 * s);

@@ -459,3 +459,62 @@ def test_small_weights_beside_a_strong_key_in_every_tile(strong, gap, sd, D):
     c.t["v_cache"] = ((1 + 0.3 * torch.randn(c.t["v_cache"].shape, generator=g, device="cuda")) * 64).to(torch.float8_e4m3fn)
     c.run()
     c.check()
+
+
+def _split_scales(c, pages_of):
+    """Sets the V scale of page i of request r to pages_of(r, i), with codes of magnitude at most 1."""
+    t = c.t
+    raw, x = t["v_cache"].view(torch.uint8), t["v_cache"].float()
+    nan = torch.isnan(x)
+    x = torch.sign(x) * (0.25 + 0.75 * torch.rand(x.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(9)))
+    codes = x.to(torch.float8_e4m3fn).view(torch.uint8)
+    raw[~nan] = codes[~nan]
+    for r, (k, ctx) in enumerate(zip(c.k, c.ctx)):
+        for i in range((ctx + k + PAGE) // PAGE):
+            t["v_scale"][int(t["block_tables"][r, i])] = pages_of(r, i)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("name,of", [
+    ("largest", lambda r, i: 2.0 ** 127), ("subnormal_beside_large", lambda r, i: 2.0 ** 100 if i % 3 == 0 else 2.0 ** -140),
+    ("as_the_append_writes", lambda r, i: 2.0 ** 118 if i == 2 else 2.0 ** -96), ("one_page", lambda r, i: 2.0 ** 90 if (r, i) == (2, 9) else 0.01),
+    ("zero_beside_large", lambda r, i: 0.0 if i % 2 else 2.0 ** 40), ("zero_first", lambda r, i: 0.0 if i < 9 else 0.02),
+    ("at_the_edges", lambda r, i: (2.0 ** -41, 2.0 ** 29, 0.0, 2.0 ** -42, 2.0 ** 30)[(i + r) % 5]),
+    ("zero_beside_small", lambda r, i: 0.0 if i % 2 else 2.0 ** -25), ("zero_beside_not_so_small", lambda r, i: 0.0 if i % 2 else 2.0 ** -15),
+    ("rising", lambda r, i: 2.0 ** (min(118, 3 * i - 96))), ("falling", lambda r, i: 2.0 ** max(-96, 118 - 3 * i))])
+def test_any_value_scales(name, of, D, dtype):
+    c = Case(40, k=[10, 3, 15, 0, 8], ctx=[119, 300, 2000, 0, 700], Hq=8, Hkv=2, D=D, dtype=dtype)
+    _split_scales(c, of)
+    c.run()
+    c.check()
+    a = c.t["out"].clone()
+    c.run()
+    assert torch.equal(a, c.t["out"])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_value_scales_far_apart_in_a_cut_sequence(dtype):
+    # 20001 keys of one request are cut: chunks with ordinary scales, with large ones and with both are merged
+    for of in (lambda r, i: 2.0 ** 110 if i > 900 else 0.01, lambda r, i: 2.0 ** 110 if i % 400 == 7 else 0.01, lambda r, i: 2.0 ** -96 if i % 2 else 2.0 ** -20):
+        c = Case(41, k=[4], ctx=[20000], Hq=8, Hkv=2, dtype=dtype)
+        _split_scales(c, of)
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_value_scales_far_apart_and_values_or_queries_that_are_not_finite(D):
+    c = Case(42, k=[6, 2, 12], ctx=[250, 31, 400], Hq=8, Hkv=2, D=D)
+    _split_scales(c, lambda r, i: 2.0 ** 100 if i % 2 else 2.0 ** -90)
+    bt, want = c.t["block_tables"], np.zeros((23, 2, 4, D), bool)
+    for r, j, h, d in ((0, 3, 1, 17), (0, 6, 0, 50), (1, 0, 0, 0), (2, 12, 1, 63)):
+        tok = c.ctx[r] + j
+        c.t["v_cache"].view(torch.uint8)[int(bt[r, tok // PAGE]), h, tok % PAGE, d] = 0x7f
+        want[(0, 7, 10)[r] + j:(7, 10, 23)[r], h, :, d] = True
+    for row, head, v in ((1, 2, math.inf), (9, 0, math.nan), (12, 7, -math.inf)):
+        c.t["q"][row, head, 3] = v
+        want[row, head // 4, head % 4] = True
+    c.run()
+    out = c.t["out"].float().cpu().numpy().reshape(-1, 2, 4, D)
+    assert np.array_equal(np.isnan(out), want)
