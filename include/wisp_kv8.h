@@ -69,11 +69,12 @@ wisp_status wisp_kv_commit_rope(const wisp_kv_rope_args *a, void *workspace, siz
  * Scales are finite and not negative (those that the append writes are; others may be any such fp32 value).  Codes past a
  * request's tokens are not judged: pages may hold anything there.  Accumulation is fp32.  With bf16 queries, V scales from 2^-60
  * to 2^40, and 0, take the tensor cores; a work item that meets others is computed in fp32 on the CUDA cores, many times as slowly.
- * Otherwise an
- * element of a query and a weight each enter the products with 8 significant bits (a bf16 value's own) where they are
- * large, small ones in steps: an element of 2^-16 of the largest one among the queries that share a work item, a weight off by
- * 2^-15 of the largest one among 128 consecutive keys (weights below 2^-30 of the row's largest may count as nothing).  A
- * query that is not finite makes its own row of its head NaN, a value that is NaN the rows that see it in its element.
+ * Otherwise an element of a query, and a weight times its page's V scale, enter the products with 8 significant bits (a bf16
+ * value's own) where they are large, and smaller ones in steps: an element is off by at most 2^-17 of the largest one among the queries
+ * that share a work item, a key's weight * V scale by 2^-15 of the largest such product among 128 consecutive keys.  A product below
+ * 2^-30 of the row's largest one may count as nothing.  (So a page whose V scale is far above another's also sets the steps of
+ * the elements in which it holds zeros.)  A query that is not finite makes its own row of its head NaN, a value that is NaN the
+ * rows that see it in its element.
  */
 typedef struct {
   wisp_attn_args attn;

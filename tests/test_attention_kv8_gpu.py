@@ -518,3 +518,39 @@ def test_value_scales_far_apart_and_values_or_queries_that_are_not_finite(D):
     c.run()
     out = c.t["out"].float().cpu().numpy().reshape(-1, 2, 4, D)
     assert np.array_equal(np.isnan(out), want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("gap", [8, 14, 20])
+def test_values_of_a_page_with_a_small_scale(gap, D):
+    """Nearly all of the weight is on pages with a small V scale; pages with a scale 2^gap as large and little weight hold zeros in every
+    second element, which thus come from the small ones alone.
+
+    Bound: as in test_matches_the_definition for the scores and the output's rounding, and a key's weight * V scale off by at most 2^-8 of
+    itself or 2^-15 of the largest such product among its 128 keys, whichever is more (in fewer than 128 rows the keys' tiles start at
+    key 0: no sequence is cut)."""
+    B, L = 20, 2048
+    c = Case(31, k=[0] * B, ctx=[L - 1] * B, D=D, garbage=False)
+    t = c.t
+    tok = torch.arange(L, device="cuda")
+    big = tok // PAGE % 4 == 3
+    _set_scores(c, [torch.where(big, -4.0, 0.0).double()] * B)
+    for r in range(B):
+        ids = t["block_tables"][r, :L // PAGE].long()
+        t["v_scale"][ids] = torch.where(big[::PAGE], 2.0 ** (gap - 10), 2.0 ** -10)[:, None]
+        v = 1 + 0.3 * torch.randn((L // PAGE, 8, PAGE, D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(r))
+        v[big[::PAGE], :, :, ::2] = 0
+        t["v_cache"].view(torch.uint8)[ids] = (v * 8).to(torch.float8_e4m3fn).view(torch.uint8)
+    c.run()
+    for r in range(B):
+        ids = t["block_tables"][r, :L // PAGE].long()
+        load = lambda x, s: (t[x + "_cache"].view(torch.uint8)[ids].view(torch.float8_e4m3fn).double() *
+                             (t[x + "_scale"][ids].double()[:, :, None, None] if s else 1)).permute(1, 0, 2, 3).reshape(8, L, D)
+        K, V, code = load("k", True), load("v", True), load("v", False)
+        w = torch.softmax(torch.einsum("hgd,htd->hgt", t["q"][r].double().view(8, 4, D), K) / math.sqrt(D), dim=2)
+        prod = w * t["v_scale"][ids].double().T.repeat_interleave(PAGE, 1)[:, None]
+        top = prod.view(8, 4, -1, 128).amax(3).repeat_interleave(128, 2)
+        ref, A = torch.einsum("hgt,htd->hgd", w, V), torch.einsum("hgt,htd->hgd", w, V.abs())
+        step = torch.einsum("hgt,htd->hgd", torch.maximum(2.0 ** -8 * prod, 2.0 ** -15 * top), code.abs())
+        got = t["out"][r].double().view(ref.shape)
+        assert ((got - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -8 * A + step).all()
