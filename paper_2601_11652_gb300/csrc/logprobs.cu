@@ -641,6 +641,9 @@ wisp_status wisp_verify_logprobs(const wisp_logprobs_args *a, void *ws, size_t w
   p.top_tokens = a->top_tokens;
   p.top_logprobs = a->top_logprobs;
   p.status = static_cast<DeviceStatus *>(ws);
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return WISP_ERR_CUDA;
   status_clear_kernel<<<1, 1, 0, s>>>(p.status);
   if (cudaGetLastError() != cudaSuccess) return WISP_ERR_CUDA;
   if (a->rows == 0) return WISP_OK;
@@ -651,7 +654,7 @@ wisp_status wisp_verify_logprobs(const wisp_logprobs_args *a, void *ws, size_t w
   // 21.0, 18.8; 400 33.3, 30.8.  Without alternatives, at most three and at most five: 176 rows 14.5, 12.8 us.
   const int64_t rounds = ((int64_t)a->V * (bf ? 2 : 4) / 16 + kThreads * kVecs - 1) / (kThreads * kVecs);
   p.cluster = 1;
-  while (p.cluster < kMaxCluster && 2 * p.cluster <= rounds && (int64_t)a->rows * 2 * p.cluster <= (top ? 3 : 5) * 152) p.cluster *= 2;
+  while (p.cluster < kMaxCluster && 2 * p.cluster <= rounds && (int64_t)a->rows * 2 * p.cluster <= (int64_t)(top ? 3 : 5) * sms) p.cluster *= 2;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cudaLaunchAttribute attr[2];
