@@ -663,7 +663,6 @@ wisp_status wisp_verify_logprobs(const wisp_logprobs_args *a, void *ws, size_t w
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = (unsigned)p.cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  if ((int64_t)a->rows * p.cluster > INT32_MAX) return WISP_ERR_UNSUPPORTED;
   cfg.gridDim = dim3((unsigned)(a->rows * p.cluster));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
