@@ -33,12 +33,13 @@
 //
 // What bounds it: up to 32 rows the cache's bytes, above that the softmax's instructions.  A tile of 32 KB (D = 128) takes an
 // SM 735 ns at the measured copy rate (368 ns for D = 64).  Measured, ns per tile and SM, 38 requests of 8192 tokens, for
-// 4 / 16 / 32 / 36 / 64 rows: 890 / 930 / 975 / 1395 / 1530 (D = 128; 5.6 TB/s at 4 rows), 715 / 765 / 905 / 1320 / 1520
-// (D = 64); pages in no order 960 / 980 / 1075 / 1385 / 1595 and 770 / 800 / 930 / 1350 / 1530.  The bf16 cache's kernel, with
-// twice the bytes: 1468 to 1516 and 823 to 880.  Lo's factor and the narrower window of the references cost up to 3% of that.
+// 4 / 16 / 32 / 36 / 64 rows: 920 / 980 / 1045 / 1340 / 1575 (D = 128; 5.4 TB/s at 4 rows), 690 / 735 / 880 / 1255 / 1465
+// (D = 64); pages in no order 975 / 1020 / 1085 / 1380 / 1595 and 775 / 805 / 920 / 1270 / 1475.  The bf16 cache's kernel, with
+// twice the bytes: 1468 to 1516 and 823 to 880.  Lo's factor and the narrower window of the references cost 0 to 3% of that; the code
+// for V scales that P cannot carry, which other items do not run, 0 to 4% up to 32 rows of D = 128 and nothing elsewhere.
 // Short items are bound by their own start and end, most of it code that is fetched again for every item: one of a
-// single tile takes 4.4 us (4 rows) to 5.4 us (20 rows), one of four tiles 6.1 to 7.3 us.  What the choices gave, at
-// 4 / 32 / 64 rows of D = 128:
+// single tile takes 4.4 us (4 rows) to 5.4 us (20 rows), one of four tiles 6.1 to 7.3 us.  What the choices gave
+// as they were made (before those two), at 4 / 32 / 64 rows of D = 128:
 //   * two groups of warps with O in registers of four correction warps, PV products added there per tile: 990 / 1082 / 1681,
 //     and 1557 at 36 rows;
 //   * groups of at most 24 rows (three or four parts above 32 rows): 955 / 1273 / 2248 against 985 / 1200 / 1701; 16-row parts

@@ -242,9 +242,9 @@ __device__ __forceinline__ void quantise_page(const RopeParams &o, T *stage, uin
 // A warp per unit.  The first o.q_ctas CTAs rotate queries, the others write K and V: a page of one head, or some heads of one row.
 // Nothing is written before the reservation is done, whatever it is: queries may be rotated in place, and those of a request
 // that it refuses have to stay as they are.  A warp's first loads are on their way by then.
-// What bounds it: the reservation's chain of dependent reads in front (8 to 10 us), then HBM.  Measured, whole calls with the
-// reservation, D = 128, 8 KV and 32 query heads, e4m3 cache: 8 prompts of 700-1023 tokens 41.5 us, 256 requests of 2 to 17 rows
-// 28.5 us, one row 10.3 us.  (With the queries rotated and stored beside the reservation 38.8, 26.4 and 10.3 us, those of
+// What bounds it: the reservation's chain of dependent reads in front (8 to 10 us), then the latency of its loads (8 prompts: 30 us
+// alone, DRAM busy half of the time).  Measured, whole calls with the reservation, D = 128, 8 KV and 32 query heads, e4m3 cache:
+// 8 prompts of 700-1023 tokens 42 us, 256 requests of 2 to 17 rows 29 us, one row 10.3 us.  (With the queries rotated and stored beside the reservation 38.8, 26.4 and 10.3 us, those of
 // refused requests among them.)
 template <typename T, bool Q8, int D, bool INTER>
 __global__ void __launch_bounds__(kThreads, kCtasPerSM) kv_append_rope_kernel(const KvParams p, const RopeParams o) {
