@@ -49,7 +49,6 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kPage = 16;
 constexpr int kRows = kF32RowsPerItem;
-constexpr float kDown = 0x1p-20f;   // factor of an 8-bit cache's values in sums: up to 2^20 of the largest stay finite
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
 
 template <int D>
@@ -153,7 +152,7 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
   };
 
   float2 o[RL][2 * CI];
-  float m[RL], l[RL];
+  float m[RL], l[RL], down = 1.0f;  // (down: of an 8-bit cache's values, see fp8.cuh)
 #pragma unroll
   for (int j = 0; j < RL; ++j) {
     m[j] = -INFINITY;
@@ -180,7 +179,7 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
     float ks2 = scale_log2, vs = 1.0f;
     if constexpr (KV8) {
       ks2 *= __ldg(p.k_scale + cur / (kPage * D));
-      vs = __ldg(p.v_scale + cur / (kPage * D)) * kDown;
+      vs = __ldg(p.v_scale + cur / (kPage * D));
     }
     const uint32_t vpar = nv & 1;
     ++nv;
@@ -235,6 +234,16 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
 #pragma unroll
         for (int i = 0; i < 2 * CI; ++i) o[j][i] = __fmul2_rn(o[j][i], al);
       }
+    }
+    if constexpr (KV8) {
+      if (vs > kLargeScale && down == 1.0f) {
+        down = kSumDown;
+#pragma unroll
+        for (int j = 0; j < RL; ++j)
+#pragma unroll
+          for (int i = 0; i < 2 * CI; ++i) o[j][i] = __fmul2_rn(o[j][i], make_float2(kSumDown, kSumDown));
+      }
+      vs *= down;
     }
     // ---- P over the K page just read
     __syncwarp();
@@ -311,8 +320,8 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
       *reinterpret_cast<float4 *>(po + rho * D + 4 * lb + 32 * i) =
           make_float4(o[j][2 * i].x, o[j][2 * i].y, o[j][2 * i + 1].x, o[j][2 * i + 1].y);
     if (lb == 0) {
-      sm[rho] = m[j];
-      sl[rho] = l[j];
+      sm[rho] = KV8 && down != 1.0f ? m[j] + kSumDownLog2 : m[j];
+      sl[rho] = KV8 ? l[j] * down : l[j];
     }
   }
 }
@@ -397,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
       if (w.poff < 0) {
         const int rj = w.row0 + rho;
         st_cols<CPL>(static_cast<float *>(p.out) + ((int64_t)(w.q0 + rj / g) * p.Hq + w.h * g + rj % g) * D + lane * CPL, acc,
-                     (KV8 ? 1.0f / kDown : 1.0f) / den);
+                     1.0f / den);
       } else {
         float *part = p.partials + w.poff;
 #pragma unroll
@@ -419,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
         __threadfence();
       }
       __syncthreads();
-      if (sh.last > 0) merge_chunks<D, float>(p, w, g, sh.last, warp, kWarps, KV8 ? 1.0f / kDown : 1.0f);
+      if (sh.last > 0) merge_chunks<D, float>(p, w, g, sh.last, warp, kWarps);
     }
   }
   if (tid == 0 && *(volatile int *)&sh.abort_) report(p.status, WISP_DEV_TIMEOUT, p.request_ids, -1);

@@ -262,19 +262,18 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t addr) {  // eight rows of D b
 }  // namespace
 
 // A work item on the CUDA cores in fp32, by warp wq of nw: for V scales that P cannot carry.  A warp takes R rows; a lane has one of 32
-// keys for their scores, then D / 32 columns of the keys' values.  Values are taken times 2^-20, so that the sums of up to 2^20 of
-// the largest stay finite.  38 requests of 8192 keys, 8 KV heads, D = 128, 4 / 20 / 64 rows: 4.7 / 9.3 / 18 ms.
+// keys for their scores, then D / 32 columns of the keys' values.  From the first V scale above 2^64 on sums are taken times 2^-20, so
+// that up to 2^20 of the largest values stay finite.  38 requests of 8192 keys, 8 KV heads, D = 128, 4 / 20 / 64 rows: 4.7 / 9.3 / 18 ms.
 template <int D>
 __device__ __forceinline__ void item_in_fp32(const AttnParams &p, const WorkItem &w, int wq, int nw) {
   constexpr int R = 4, CPL = D / 32;
-  constexpr float kDownLog2 = 20.0f;
   const int lane = threadIdx.x & 31, g = p.Hq / p.Hkv;
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq;
 #pragma unroll 1
   for (int rho = wq * R; rho < w.rows; rho += nw * R) {
     int last[R], off[R];  // the last key that a row sees, its elements' offset from the item's first query position
-    float m[R], l[R], acc[R][CPL];
+    float m[R], l[R], acc[R][CPL], down = 1.0f;
     const int64_t q0 = ((int64_t)w.q0 * p.Hq + w.h * g) * D;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -296,7 +295,7 @@ __device__ __forceinline__ void item_in_fp32(const AttnParams &p, const WorkItem
       for (int i = 0; i < R; ++i) e[i] = 0.0f;
       if (in) {
         ks = __ldg(p.k_scale + page) * scale_log2;
-        vs = __ldg(p.v_scale + page) * exp2f(-kDownLog2);
+        vs = __ldg(p.v_scale + page);
         const uint4 *k = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.k_cache) + (page * 16 + tok % 16) * D);
         const uint16_t *q = static_cast<const uint16_t *>(p.q) + q0;
 #pragma unroll 1
@@ -330,6 +329,14 @@ __device__ __forceinline__ void item_in_fp32(const AttnParams &p, const WorkItem
 #pragma unroll
         for (int c = 0; c < CPL; ++c) acc[i][c] *= alpha;
       }
+      if (down == 1.0f && __any_sync(0xffffffffu, vs > kLargeScale)) {
+        down = kSumDown;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) acc[i][c] *= down;
+      }
+      vs *= down;
 #pragma unroll 1
       for (int k0 = 0; k0 < 32; k0 += 8) {
         const int64_t pg = __shfl_sync(0xffffffffu, page, k0 & 16);
@@ -365,15 +372,16 @@ __device__ __forceinline__ void item_in_fp32(const AttnParams &p, const WorkItem
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
       if (rho + i >= w.rows) continue;
+      l[i] *= down;
       if (w.poff < 0) {
-        st_cols<CPL>(static_cast<uint16_t *>(p.out) + q0 + off[i] + lane * CPL, acc[i], exp2f(kDownLog2) / l[i]);
+        st_cols<CPL>(static_cast<uint16_t *>(p.out) + q0 + off[i] + lane * CPL, acc[i], 1.0f / l[i]);
       } else {  // as the other chunks have them: O and l times 2^(m - kHead) are the sums
         float *part = p.partials + w.poff;
 #pragma unroll
         for (int c = 0; c < CPL; ++c) __stcg(part + (int64_t)(rho + i) * D + lane * CPL + c, acc[i][c]);
         if (lane == 0) {
-          __stcg(part + w.rows * D + rho + i, m[i] + (kHead + kDownLog2));
-          __stcg(part + w.rows * D + w.rows + rho + i, l[i] * exp2f(-kDownLog2));
+          __stcg(part + w.rows * D + rho + i, m[i] + (down == 1.0f ? kHead : kHead + kSumDownLog2));
+          __stcg(part + w.rows * D + w.rows + rho + i, l[i]);
         }
       }
     }

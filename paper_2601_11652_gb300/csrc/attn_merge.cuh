@@ -46,9 +46,9 @@ __device__ __forceinline__ void st_cols(float *dst, const float (&v)[CPL], float
 // lane holds one chunk's (m, l) of each, the warp reduces the rows' maximum and denominator, and then
 // every lane adds its columns of the chunks' O with the chunk's weight broadcast by a shuffle, four
 // chunks of both rows in flight.  (With one thread per row walking the chunks' (m, l), the merge took
-// about 90 us of a request's 114 us at 16 chunks: serial chains of L2 loads.)  `up`: factor of the outputs.
+// about 90 us of a request's 114 us at 16 chunks: serial chains of L2 loads.)
 template <int D, typename T>
-__device__ __forceinline__ void merge_chunks(const AttnParams &p, const WorkItem &w, int g, int chunks, int wq, int nw, float up = 1.0f) {
+__device__ __forceinline__ void merge_chunks(const AttnParams &p, const WorkItem &w, int g, int chunks, int wq, int nw) {
   const int lane = threadIdx.x & 31;
   const float *base = p.partials + w.pbase;
   const int stride = ((w.rg ? w.row0 / w.rg : w.rows) * (D + 2) + 3) / 4 * 4;  // (groups before the last have equal rows)
@@ -114,7 +114,7 @@ __device__ __forceinline__ void merge_chunks(const AttnParams &p, const WorkItem
       den0 += __shfl_xor_sync(0xffffffffu, den0, o);
       den1 += __shfl_xor_sync(0xffffffffu, den1, o);
     }
-    const float i0 = up / den0, i1 = up / den1;
+    const float i0 = 1.0f / den0, i1 = 1.0f / den1;
     const int rj0 = w.row0 + j0, rj1 = w.row0 + j1;
     st_cols<CPL>(og + ((int64_t)(w.q0 + rj0 / g) * p.Hq + w.h * g + rj0 % g) * D + lane * CPL, a0, i0);
     st_cols<CPL>(og + ((int64_t)(w.q0 + rj1 / g) * p.Hq + w.h * g + rj1 % g) * D + lane * CPL, a1, i1);

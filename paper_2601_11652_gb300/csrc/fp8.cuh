@@ -11,6 +11,10 @@ namespace wisp {
 // scaled values never leave it.
 constexpr int kScaleExpMin = -96, kScaleExpMax = 120;
 
+// Sums of scaled values in fp32: from the first scale above kLargeScale on they are taken times kSumDown (and kSumDownLog2 is added to
+// the maximum that goes with them), so that up to 2^20 of the largest values stay finite.
+constexpr float kLargeScale = 0x1p64f, kSumDown = 0x1p-20f, kSumDownLog2 = 20.0f;
+
 // two values -> two e4m3 codes (a in the low byte): round to nearest even, past +-448 (and +-inf) to +-448,
 // NaN to NaN
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {

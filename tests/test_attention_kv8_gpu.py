@@ -554,3 +554,19 @@ def test_values_of_a_page_with_a_small_scale(gap, D):
         step = torch.einsum("hgt,htd->hgd", torch.maximum(2.0 ** -8 * prod, 2.0 ** -15 * top), code.abs())
         got = t["out"][r].double().view(ref.shape)
         assert ((got - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -8 * A + step).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("e", [-126, -110, -96, -70, -60, 40, 60, 100, 118])
+def test_one_scale_for_all_values(e, D, dtype):
+    """Outputs scale with V: with 2^e in the place of 2^-6 they are 2^(e + 6) times the same, to the bounds of the definition.  (The
+    codes go up to 448, so that outputs stay normal, but for elements below 2^-8 of the largest at the smallest scale.)"""
+    c = Case(60, k=[4, 0, 15], ctx=[700, 20, 5000], Hq=8, Hkv=2, D=D, dtype=dtype)
+    c.t["v_cache"].view(torch.uint8)[:] = torch.where((c.t["v_cache"].view(torch.uint8) & 0x7f) == 0x7f, c.t["v_cache"].view(torch.uint8),
+                                                      (c.t["v_cache"].float().nan_to_num() / 2).to(torch.float8_e4m3fn).view(torch.uint8))
+    c.t["v_scale"][:] = 2.0 ** e
+    c.run()
+    c.t["out"].copy_((c.t["out"].double() * 2.0 ** (-6 - e)).to(dtype))
+    c.t["v_scale"][:] = 2.0 ** -6
+    c.check()
