@@ -61,6 +61,14 @@ class wisp_logprobs_args(ctypes.Structure):
                 ("tokens", _P), ("top_n", _I32), ("logprob", _P), ("entropy", _P), ("top_tokens", _P), ("top_logprobs", _P)]
 
 
+class wisp_prompt_args(ctypes.Structure):
+    _fields_ = [("attn", wisp_attn_args), ("cache_dtype", ctypes.c_int), ("k_scale", _P), ("v_scale", _P)]
+
+
+class wisp_shared_args(ctypes.Structure):
+    _fields_ = [("rows", wisp_prompt_args), ("shared_ids", _P), ("shared_pages", _P)]
+
+
 class WispError(RuntimeError):
     def __init__(self, fn: str, code: int, text: str):
         super().__init__(f"{fn}: {text} (status {code})")
@@ -73,7 +81,9 @@ EXPORTED = ["wisp_verify_workspace_size", "wisp_verify_attention", "wisp_verify_
             "wisp_verify_get_device_status", "wisp_verify_status_string", "wisp_verify_device_code_string",
             "wisp_verify_accept_noalloc", "wisp_verify_accept_greedy", "wisp_kv_workspace_size",
             "wisp_kv_reserve_append", "wisp_kv_commit", "wisp_kv_rope_workspace_size", "wisp_kv_reserve_append_rope",
-            "wisp_kv_commit_rope", "wisp_verify_attention_kv8", "wisp_verify_step_kv8", "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens"]
+            "wisp_kv_commit_rope", "wisp_verify_attention_kv8", "wisp_verify_step_kv8", "wisp_verify_logprobs_workspace_size", "wisp_verify_logprobs", "wisp_verify_committed_tokens",
+            "wisp_prompt_workspace_size", "wisp_prompt_attention", "wisp_verify_shared_workspace_size",
+            "wisp_verify_attention_shared"]
 
 
 def lib_path() -> str:
@@ -133,6 +143,12 @@ def load(path: str | None = None):
     lib.wisp_verify_logprobs.restype = ctypes.c_int
     lib.wisp_verify_committed_tokens.argtypes = [CP, _P, _P]
     lib.wisp_verify_committed_tokens.restype = ctypes.c_int
+    for fn, args in (("wisp_prompt_attention", wisp_prompt_args), ("wisp_verify_attention_shared", wisp_shared_args)):
+        getattr(lib, fn).argtypes = [ctypes.POINTER(args), _P, ctypes.c_size_t, _P]
+        getattr(lib, fn).restype = ctypes.c_int
+    for fn, args in (("wisp_prompt_workspace_size", wisp_prompt_args), ("wisp_verify_shared_workspace_size", wisp_shared_args)):
+        getattr(lib, fn).argtypes = [ctypes.POINTER(args)]
+        getattr(lib, fn).restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -450,3 +466,69 @@ def wisp_verify_committed_tokens(acc: wisp_accept_args, row_tokens: torch.Tensor
         raise ValueError("row_tokens must be [total_q_rows] int32")
     _check("wisp_verify_committed_tokens", load().wisp_verify_committed_tokens(
         ctypes.byref(acc), _ptr(row_tokens), _stream(stream)))
+
+
+# ---- attention of whole prompts, and of batches that share pages (include/wisp_prompt.h) -------------
+def make_prompt_args(*, draft_lens, context_lens, block_tables, q, k_cache, v_cache, out, k_scale=None, v_scale=None,
+                     request_ids=None, num_blocks=None, total_q_rows=None) -> wisp_prompt_args:
+    """Fill wisp_prompt_args from device tensors: as make_attn_args, without a limit on the query rows (draft_lens: rows - 1), over a
+    cache of q's type or one in e4m3 (torch.float8_e4m3fn or uint8) with scales [num_blocks, Hkv]."""
+    if q.dim() != 3 or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("q and out must be [rows, Hq, D] of one type")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.shape[3] != q.shape[2]:
+        raise ValueError("k_cache and v_cache must be [num_blocks, Hkv, 16, D] of one type, with the head dim of q")
+    B = draft_lens.numel()
+    if block_tables.dim() != 2 or block_tables.shape[0] < B or context_lens.numel() < B or \
+            any(t.dtype != torch.int32 for t in (draft_lens, context_lens, block_tables)):
+        raise ValueError("draft_lens and context_lens must be [B], block_tables [B, max_blocks], int32")
+    if request_ids is not None and (request_ids.dtype != torch.int64 or request_ids.numel() < B):
+        raise ValueError("request_ids must be [B] int64")
+    if (num_blocks or 0) > k_cache.shape[0] or (total_q_rows or 0) > q.shape[0]:
+        raise ValueError("num_blocks and total_q_rows must not be more than the pool and q have")
+    code = _cache_code(k_cache)
+    if code != WISP_E4M3 and code != _dtype_code(q):
+        raise ValueError("the cache has the queries' type or is e4m3")
+    a = wisp_prompt_args()
+    a.attn = make_attn_args(draft_lens=draft_lens, context_lens=context_lens, block_tables=block_tables, q=q, k_cache=k_cache,
+                            v_cache=v_cache, out=out, request_ids=request_ids, num_blocks=num_blocks, total_q_rows=total_q_rows)
+    a.cache_dtype = code
+    if code == WISP_E4M3:
+        _check_scales(k_cache, k_scale, v_scale)
+        a.k_scale, a.v_scale = _ptr(k_scale), _ptr(v_scale)
+    return a
+
+
+def wisp_prompt_workspace_size(a: wisp_prompt_args) -> int:
+    n = load().wisp_prompt_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise WispError("wisp_prompt_workspace_size", WISP_ERR_INVALID_ARG, "invalid arguments")
+    return int(n)
+
+
+def wisp_prompt_attention(a: wisp_prompt_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_prompt_attention", load().wisp_prompt_attention(
+        ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def make_shared_args(*, shared_ids, shared_pages, draft_lens, **kw) -> wisp_shared_args:
+    """Fill wisp_shared_args: make_prompt_args, and shared_ids / shared_pages [B] int32 (consecutive requests with the same id >= 0 and
+    the same number of pages > 0 share their first pages)."""
+    for t in (shared_ids, shared_pages):
+        if t.dtype != torch.int32 or t.numel() < draft_lens.numel():
+            raise ValueError("shared_ids and shared_pages must be [B] int32")
+    a = wisp_shared_args()
+    a.rows = make_prompt_args(draft_lens=draft_lens, **kw)
+    a.shared_ids, a.shared_pages = _ptr(shared_ids), _ptr(shared_pages)
+    return a
+
+
+def wisp_verify_shared_workspace_size(a: wisp_shared_args) -> int:
+    n = load().wisp_verify_shared_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise WispError("wisp_verify_shared_workspace_size", WISP_ERR_INVALID_ARG, "invalid arguments")
+    return int(n)
+
+
+def wisp_verify_attention_shared(a: wisp_shared_args, workspace: torch.Tensor, stream=None) -> None:
+    _check("wisp_verify_attention_shared", load().wisp_verify_attention_shared(
+        ctypes.byref(a), _ptr(workspace), workspace.numel(), _stream(stream)))

@@ -20,7 +20,7 @@ struct AttnParams {
   float *partials;
   int row_groups;      // row groups per (request, head) at most
   int32_t *pair_done;  // [B * Hkv * row_groups] finished chunks of each split (request, head, row group), zeroed
-                       // by the planner
+                       // by the planner; null (prompt.cuh): another kernel joins the partials
 };
 
 // Host launchers (defined next to their kernels): programmatic dependents of the planner, which they wait for

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
         }
       }
     }
-    if (w.poff >= 0) {
+    if (w.poff >= 0 && p.pair_done) {
       // split: the last chunk of this (request, head, row group) to finish merges all
       __threadfence();
       __syncthreads();

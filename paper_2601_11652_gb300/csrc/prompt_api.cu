@@ -1,0 +1,199 @@
+// prompt_api.cu -- host side of include/wisp_prompt.h: argument checks, workspace and launches.  No allocation, no
+// synchronisation.
+#include <cstring>
+#include <mutex>
+
+#include "prompt.cuh"
+#include "wisp_prompt.h"
+
+using namespace wisp;
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+int g_sms[kMaxDevices];  // SMs of a device that has been set up
+std::mutex g_mu;
+
+wisp_status setup(int *sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return WISP_ERR_CUDA;
+  std::lock_guard<std::mutex> lk(g_mu);
+  if (!g_sms[dev]) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return WISP_ERR_CUDA;
+    if (attn_f32_setup() != cudaSuccess || prompt_tc_setup() != cudaSuccess) return WISP_ERR_CUDA;
+    g_sms[dev] = n;
+  }
+  *sms = g_sms[dev];
+  return WISP_OK;
+}
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+wisp_status check(const wisp_prompt_args *x) {
+  if (!x) return WISP_ERR_INVALID_ARG;
+  const wisp_attn_args *a = &x->attn;
+  if (a->B < 0 || a->Hq <= 0 || a->Hkv <= 0 || a->Hq % a->Hkv != 0) return WISP_ERR_INVALID_ARG;
+  if (a->qkv_dtype != WISP_F32 && a->qkv_dtype != WISP_BF16) return WISP_ERR_INVALID_ARG;
+  if (x->cache_dtype != a->qkv_dtype && x->cache_dtype != WISP_E4M3) return WISP_ERR_INVALID_ARG;
+  if (a->D != 64 && a->D != 128) return WISP_ERR_UNSUPPORTED;
+  if (a->block_size != 16 || a->Hq / a->Hkv > 128) return WISP_ERR_UNSUPPORTED;
+  if (a->B == 0) return WISP_OK;
+  if (a->max_blocks_per_seq <= 0 || a->num_blocks <= 0 || a->total_q_rows < a->B) return WISP_ERR_INVALID_ARG;
+  if (!a->draft_lens || !a->context_lens || !a->block_tables || !a->q || !a->k_cache || !a->v_cache || !a->out)
+    return WISP_ERR_INVALID_ARG;
+  if (!aligned16(a->q) || !aligned16(a->k_cache) || !aligned16(a->v_cache) || !aligned16(a->out)) return WISP_ERR_INVALID_ARG;
+  if (x->cache_dtype == WISP_E4M3 && a->qkv_dtype == WISP_BF16) return WISP_ERR_UNSUPPORTED;
+  if (x->cache_dtype == WISP_E4M3 && (!x->k_scale || !x->v_scale)) return WISP_ERR_INVALID_ARG;
+  if ((int64_t)a->max_blocks_per_seq * a->block_size > INT32_MAX / 2) return WISP_ERR_UNSUPPORTED;
+  if ((int64_t)a->total_q_rows * (a->Hq / a->Hkv) > INT32_MAX / 2) return WISP_ERR_UNSUPPORTED;
+  return WISP_OK;
+}
+
+wisp_status check(const wisp_shared_args *x) {
+  const wisp_status st = check(x ? &x->rows : nullptr);
+  if (st != WISP_OK || x->rows.attn.B == 0) return st;
+  return x->shared_ids && x->shared_pages ? WISP_OK : WISP_ERR_INVALID_ARG;
+}
+
+struct Space {
+  size_t status, header, q_row_start, req_flag, req_run, run_info, segs, items, partials, total;
+  int64_t max_items, partial_cap;
+  int unit_rows;
+  bool fits;
+};
+
+// Rows of a unit, and bounds on items and partials.  Without cuts a request has ceil(rows / unit_rows) units per KV head, a run as
+// many for its rows again, and both leave one partial per row.  Cuts add items and partials of whole units: what the planner's rule
+// makes of them stays below these bounds (several per SM), and where it would not, it makes none.
+Space space(const wisp_attn_args *a, bool shared, int sms) {
+  Space s;
+  const int g = a->Hq / a->Hkv;
+  s.unit_rows = a->qkv_dtype == WISP_BF16 ? 2 * g * prompt_tile_positions(g) : kF32RowsPerItem;
+  const int64_t units = ((int64_t)a->total_q_rows * g / s.unit_rows + a->B) * (shared ? 2 : 1);
+  const int64_t slot = (int64_t)s.unit_rows * (a->D + 2) + 4;
+  const int64_t cuts = (int64_t)(a->qkv_dtype == WISP_BF16 ? 6 : 24) * sms;
+  s.max_items = units * a->Hkv + 4 * cuts;
+  s.partial_cap = cuts * slot + (shared ? 2 * (int64_t)a->total_q_rows * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = (off + bytes + 255) & ~(size_t)255;
+    return at;
+  };
+  const size_t B = (size_t)a->B;
+  s.status = take(sizeof(DeviceStatus));
+  s.header = take(sizeof(PromptHeader));
+  s.q_row_start = take(4 * (B + 1));
+  s.req_flag = take(4 * B);
+  s.req_run = take(4 * B);
+  s.run_info = take(16 * B);
+  s.segs = take(sizeof(Segment) * 2 * B);
+  s.items = take(sizeof(WorkItem) * (size_t)s.max_items);
+  s.partials = take(4 * (size_t)s.partial_cap);
+  s.total = off;
+  s.fits = s.max_items < INT32_MAX / 2 && s.partial_cap < INT32_MAX;
+  return s;
+}
+
+template <typename T>
+T *at(void *ws, size_t off) {
+  return reinterpret_cast<T *>(static_cast<char *>(ws) + off);
+}
+
+size_t workspace_size(const wisp_prompt_args *x, bool shared) {
+  int sms = 0;
+  if (setup(&sms) != WISP_OK) return 0;
+  const Space sp = space(&x->attn, shared, sms);
+  return sp.fits ? sp.total : 0;
+}
+
+wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *pages, void *ws, size_t ws_bytes, void *stream) {
+  const wisp_attn_args *a = &x->attn;
+  int sms = 0;
+  const wisp_status st = setup(&sms);
+  if (st != WISP_OK) return st;
+  const Space sp = space(a, ids != nullptr, sms);
+  if (!sp.fits) return WISP_ERR_UNSUPPORTED;
+  if (!ws || ((uintptr_t)ws & 255) != 0 || ws_bytes < sp.total) return WISP_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool bf = a->qkv_dtype == WISP_BF16;
+  PromptPlan p;
+  std::memset(&p, 0, sizeof p);
+  p.B = a->B;
+  p.Hq = a->Hq;
+  p.Hkv = a->Hkv;
+  p.D = a->D;
+  p.max_blocks_per_seq = a->max_blocks_per_seq;
+  p.total_q_rows = a->total_q_rows;
+  p.unit_rows = sp.unit_rows;
+  p.sms = sms;
+  p.max_items = sp.max_items;
+  p.partial_cap = sp.partial_cap;
+  p.draft_lens = a->draft_lens;
+  p.context_lens = a->context_lens;
+  p.shared_ids = ids;
+  p.shared_pages = pages;
+  p.request_ids = a->request_ids;
+  p.status = at<DeviceStatus>(ws, sp.status);
+  p.header = at<PromptHeader>(ws, sp.header);
+  p.q_row_start = at<int32_t>(ws, sp.q_row_start);
+  p.req_flag = at<int32_t>(ws, sp.req_flag);
+  p.req_run = at<int32_t>(ws, sp.req_run);
+  p.run_info = at<int32_t>(ws, sp.run_info);
+  p.segs = at<Segment>(ws, sp.segs);
+  p.items = at<WorkItem>(ws, sp.items);
+  p.partials = at<float>(ws, sp.partials);
+  p.out = a->out;
+  if (prompt_plan_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
+  if (a->B == 0) return WISP_OK;
+  AttnParams ap;
+  std::memset(&ap, 0, sizeof ap);
+  ap.B = a->B;
+  ap.Hq = a->Hq;
+  ap.Hkv = a->Hkv;
+  ap.D = a->D;
+  ap.max_blocks_per_seq = a->max_blocks_per_seq;
+  ap.num_blocks = a->num_blocks;
+  ap.request_ids = a->request_ids;
+  ap.block_tables = a->block_tables;
+  ap.q = a->q;
+  ap.k_cache = a->k_cache;
+  ap.v_cache = a->v_cache;
+  if (x->cache_dtype == WISP_E4M3) {
+    ap.k_scale = x->k_scale;
+    ap.v_scale = x->v_scale;
+  }
+  ap.out = a->out;
+  ap.status = p.status;
+  ap.header = &p.header->h;
+  ap.header_mut = &p.header->h;
+  ap.items = p.items;
+  ap.partials = p.partials;  // (pair_done stays null: the merge kernel joins them)
+  const int grid = (int)(sp.max_items < sms ? sp.max_items : sms);
+  cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : attn_f32_launch(ap, grid, s);
+  if (e == cudaSuccess) e = prompt_merge_launch(p, !bf, s);
+  return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wisp_prompt_workspace_size(const wisp_prompt_args *a) { return check(a) == WISP_OK ? workspace_size(a, false) : 0; }
+
+wisp_status wisp_prompt_attention(const wisp_prompt_args *a, void *ws, size_t ws_bytes, void *stream) {
+  const wisp_status st = check(a);
+  return st != WISP_OK ? st : call(a, nullptr, nullptr, ws, ws_bytes, stream);
+}
+
+size_t wisp_verify_shared_workspace_size(const wisp_shared_args *a) {
+  return check(a) == WISP_OK ? workspace_size(&a->rows, true) : 0;
+}
+
+wisp_status wisp_verify_attention_shared(const wisp_shared_args *a, void *ws, size_t ws_bytes, void *stream) {
+  const wisp_status st = check(a);
+  return st != WISP_OK ? st : call(&a->rows, a->shared_ids, a->shared_pages, ws, ws_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,692 @@
+// prompt_tc.cu -- tensor-core attention with many query rows: prompts, and the rows of requests that share a prefix
+// (bf16 queries, paged cache, include/wisp_prompt.h).
+//
+// An item (prompt.cuh) is up to two tiles of 128 query rows of one KV head, row = position * g + head of the group, over a chunk of
+// keys.  Per key tile of 128 and stream (a stream: 128 rows in the MMA's M):
+//   S = Q K^T         M = 128 rows, N = 128 keys, K = D; fp32 in TMEM, a row per lane
+//   P = 2^(S - m)     by 128 threads, one row each: no exchange between threads; bf16, back to TMEM over S
+//   O += P V          M = 128 rows, N = D, K = 128 keys; A from TMEM, fp32 in TMEM
+// m follows the row's maximum loosely: it moves (and O, l are rescaled) only where a tile's maximum is more than 2^8 above it, so
+// weights stay below 2^8 and rescales are rare after a row's first tiles.  Sums and O keep their relative precision at any
+// exponent; a weight is rounded to bf16 (2^-9) for the second product, the row sum adds it before that.
+//
+// An item of more than one tile of rows runs its tiles as two streams over the same key tiles; one of a single tile runs
+// the even and the odd key tiles as two streams of the same rows, joined at the end.  So there are always two chains
+// (S, softmax, P V) that fill each other's gaps.
+//
+// Persistent CTAs take items from a global counter, longest first.  Warps:
+//   * 0-3, 4-7: softmax and epilogue of stream 0 and 1, a thread per row;
+//   * 8: issues tcgen05.mma.  Stream s's next S follows its P V directly, so that an S that has arrived says that the O before it
+//     is complete, and S may overwrite P;
+//   * 9: takes items, and brings Q (boxes of whole positions), K and V (boxes of one page or of eight consecutive ones) by TMA;
+//   * 10: looks at V where a tile has keys that some row does not see: 0 * NaN would reach every row.  Values that are not finite
+//     are set to zero there and remembered with the first position that sees them; the epilogue writes what they make of its rows.
+// (11: registers are allotted per four warps.)
+// Every wait is bounded: an expired one records WISP_DEV_TIMEOUT and the CTA drains.
+#include "attn_merge.cuh"
+#include "prompt.cuh"
+#include "sm100_ptx.cuh"
+
+#include <cudaTypedefs.h>
+#include <cstring>
+
+namespace wisp {
+
+namespace {
+
+constexpr int kBT = 128;      // keys per tile
+constexpr int kM = 128;       // rows per stream
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;  // S (and P) of the streams at 0 and 128, O at 256 and 256 + D
+constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
+constexpr float kLoose = 8.0f;  // how far (log2) a score may exceed its row's reference
+constexpr int kItemRing = 2;
+
+template <int D>
+struct Cfg {
+  static constexpr int HALVES = D / 64;
+  static constexpr int HALF = kBT * 128;          // a 64-wide half of a tile: [128][128 B], swizzled
+  static constexpr int TILE = HALVES * HALF;
+  static constexpr int NS = D == 128 ? 2 : 4;     // stages of K, and of V
+  static constexpr int OFF_Q = 0;                 // two tiles
+  static constexpr int OFF_K = 2 * TILE;
+  static constexpr int OFF_V = OFF_K + NS * TILE;
+  static constexpr int OFF_BAR = OFF_V + NS * TILE;
+  static constexpr int N_BAR = 40;
+  static constexpr int OFF_RING = OFF_BAR + N_BAR * 8;             // kItemRing x 64 bytes
+  static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;       // tmem base, abort flag, odd-value flags
+  static constexpr int OFF_ML = OFF_MISC + 64;                     // float [2][128]: m, l of stream 1 for the join
+  static constexpr int OFF_ODD = OFF_ML + 2 * kM * 4;              // int [2][3][D] first positions that see NaN, +inf, -inf
+  static constexpr int SMEM = OFF_ODD + 2 * 3 * D * 4 + 1024;      // + slack to align the base to 1024
+  static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
+};
+
+template <int D>
+struct Bars {
+  using C = Cfg<D>;
+  static constexpr int K_FULL = 0, K_EMPTY = C::NS, V_FULL = 2 * C::NS, V_EMPTY = 3 * C::NS;
+  static constexpr int Q_FULL = 4 * C::NS, Q_EMPTY = Q_FULL + 1;
+  static constexpr int S_FULL = Q_EMPTY + 1, P_FULL = S_FULL + 2, O_FULL = P_FULL + 2;  // [2] per stream
+  static constexpr int IT_FULL = O_FULL + 2, IT_EMPTY = IT_FULL + kItemRing;
+  static constexpr int V_CLEAN = IT_EMPTY + kItemRing;   // [NS] the tile's V has been looked at
+  static constexpr int ODD_FREE = V_CLEAN + C::NS;           // [2] per buffer of odd values: its item's epilogues are done
+  static constexpr int ML_FULL = ODD_FREE + 2, ML_EMPTY = ML_FULL + 1;  // stream 1's m and l (and O): published, read
+  static constexpr int MMA_DONE = ML_EMPTY + 1, FIN = MMA_DONE + 1;
+  static_assert(FIN + 1 <= C::N_BAR, "barrier count");
+};
+
+__device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort) {
+  if (ptx::mbar_try_wait(b, parity)) return true;
+  const long long t0 = clock64();
+  while (true) {
+    if (ptx::mbar_try_wait(b, parity)) return true;
+    if (*abort) return false;
+    if (clock64() - t0 > kWaitCycles) {
+      *abort = 1;
+      return false;
+    }
+  }
+}
+
+// What the roles need to know of an item.
+struct Shape {
+  int nt;        // key tiles
+  bool split;    // one tile of rows: its streams take the key tiles in turn
+  int steps;     // S, softmax, P V, over both streams
+  int plain;     // key tiles from the first on that every row of the item sees entirely
+};
+__device__ __forceinline__ Shape shape_of(const WorkItem &w, int tile_rows, int g) {
+  Shape s;
+  s.nt = (w.t1 - w.t0 + kBT - 1) / kBT;
+  s.split = w.rows <= tile_rows;
+  s.steps = s.split ? s.nt : 2 * s.nt;
+  const int all = min(w.t1, w.ctx + w.row0 / g + 1);  // keys that the first row sees
+  s.plain = max(all - w.t0, 0) / kBT;
+  return s;
+}
+
+}  // namespace
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap tmq,
+                     const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
+                     const __grid_constant__ CUtensorMap tmk8, const __grid_constant__ CUtensorMap tmv8) {
+  using C = Cfg<D>;
+  using B = Bars<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = ptx::smem_u32(smem);
+  const uint32_t bars = sbase + C::OFF_BAR;
+  auto bar = [&](int i) -> uint32_t { return bars + 8 * i; };
+  struct RingSlot {
+    int it;
+    int pad[3];
+    WorkItem w;
+  };
+  static_assert(sizeof(RingSlot) <= 64, "item ring slot");
+  RingSlot *s_ring = reinterpret_cast<RingSlot *>(smem + C::OFF_RING);
+  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + C::OFF_MISC);
+  volatile int *s_abort = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 4);
+  volatile int *s_isodd = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 8);  // [2] an item's V held odd values
+  float *s_ml = reinterpret_cast<float *>(smem + C::OFF_ML);
+  int *s_odd = reinterpret_cast<int *>(smem + C::OFF_ODD);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::NS; ++i) {
+      ptx::mbar_init(bar(B::K_FULL + i), 1);
+      ptx::mbar_init(bar(B::K_EMPTY + i), 1);
+      ptx::mbar_init(bar(B::V_FULL + i), 1);
+      ptx::mbar_init(bar(B::V_EMPTY + i), 1);
+      ptx::mbar_init(bar(B::V_CLEAN + i), 1);
+    }
+    ptx::mbar_init(bar(B::Q_FULL), 1);
+    ptx::mbar_init(bar(B::Q_EMPTY), 1);
+    for (int s = 0; s < 2; ++s) {
+      ptx::mbar_init(bar(B::S_FULL + s), 1);
+      ptx::mbar_init(bar(B::P_FULL + s), 4);
+      ptx::mbar_init(bar(B::O_FULL + s), 1);
+      ptx::mbar_init(bar(B::ODD_FREE + s), 8);
+    }
+    for (int i = 0; i < kItemRing; ++i) {
+      ptx::mbar_init(bar(B::IT_FULL + i), 1);
+      ptx::mbar_init(bar(B::IT_EMPTY + i), 8 + 1 + 1);  // softmax warps, MMA issuer, the one that looks at V
+    }
+    ptx::mbar_init(bar(B::ML_FULL), 4);
+    ptx::mbar_init(bar(B::ML_EMPTY), 4);
+    ptx::mbar_init(bar(B::MMA_DONE), 1);
+    ptx::mbar_init(bar(B::FIN), kThreads / 32);
+    *s_abort = 0;
+    s_isodd[0] = s_isodd[1] = 0;
+    ptx::fence_mbar_init();
+  }
+  for (int i = threadIdx.x; i < 2 * 3 * D; i += kThreads) s_odd[i] = INT32_MAX;
+  if (warp == 9 && lane == 0) {
+    ptx::prefetch_tmap(&tmq);
+    ptx::prefetch_tmap(&tmk);
+    ptx::prefetch_tmap(&tmv);
+    ptx::prefetch_tmap(&tmk8);
+    ptx::prefetch_tmap(&tmv8);
+  }
+  __syncwarp();
+  if (warp == 8) {
+    ptx::tmem_alloc(s_tmem, kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  // everything above may overlap the planner (programmatic dependent launch)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int n_items = p.header->n_items;
+  const int g = p.Hq / p.Hkv;
+  const int tile_rows = kM / g * g;  // rows of a tile: whole positions
+
+  // takes the next item from the ring: false at the end
+  auto next_item = [&](uint32_t j, WorkItem &w, bool &ok) -> bool {
+    const int slot = j % kItemRing;
+    if (!wait_bar(bar(B::IT_FULL + slot), (j / kItemRing) & 1, s_abort)) { ok = false; return false; }
+    const int it = s_ring[slot].it;
+    w = s_ring[slot].w;
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(bar(B::IT_EMPTY + slot));
+    return it >= 0;
+  };
+
+  bool ok = true;
+  if (warp < 8) {
+    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 208 + 4 x 88.  (Each split stands at the head of its own
+    // branch: after a join the compiler counts with the least.)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ------------------------------------------------------------------ softmax and epilogue, stream s, a row per thread
+    const int s = warp >> 2;
+    const int row = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + s * kBT, t_o = tmem + lanes + 2 * kBT + s * D;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+    const float2 scale2 = make_float2(scale, scale);
+    uint32_t ns = 0, nml = 0, nof = 0;  // this stream's S tiles, joins and finished O so far
+    WorkItem w;
+    for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
+      const Shape sh = shape_of(w, tile_rows, g);
+      const int tile = sh.split ? 0 : s;
+      const int rho = w.row0 + tile * tile_rows + row;       // row of the (segment, head)
+      const bool mine = row < tile_rows && tile * tile_rows + row < w.rows;
+      const int pos = rho / g, hh = rho - pos * g;
+      const int end = min(w.t1, w.ctx + pos + 1);            // keys that it sees
+      float m = -INFINITY, l = 0.0f;
+      const int first = sh.split ? s : 0, inc = sh.split ? 2 : 1;
+      for (int t = first; t < sh.nt; t += inc) {
+        if (!wait_bar(bar(B::S_FULL + s), ns & 1, s_abort)) { ok = false; break; }
+        ++ns;
+        ptx::tc_fence_after();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ptx::tmem_ld32(t_s + 32 * c, x[c]);
+        ptx::tmem_wait_ld();
+        if (t >= sh.plain) {
+          const int seen = end - (w.t0 + t * kBT);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i >= seen) x[c][i] = 0xff800000u;
+        }
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+#pragma unroll
+          for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][i])), __uint_as_float(x[c][i + 1]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+        if (t == first) {
+          m = top;
+        } else {
+          const bool move = mine && top > m + kLoose;
+          if (__any_sync(0xffffffffu, move)) {
+            // (the O before this S is complete: see the issuer)
+            const float a = move ? ptx::ex2(m - top) : 1.0f;
+            if (move) m = top;
+            l *= a;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              ptx::tmem_ld16(t_o + c, o);
+              ptx::tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
+              ptx::tmem_st16(t_o + c, o);
+            }
+          }
+        }
+        const float mm = m == -INFINITY ? 0.0f : -m;  // (nothing seen so far: every weight is zero)
+        const float2 m2 = make_float2(mm, mm);
+        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float2 a = __ffma2_rn(make_float2(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])), scale2, m2);
+            const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
+            sum[(i >> 1) & 1] = __fadd2_rn(sum[(i >> 1) & 1], e);
+            pk[i >> 1] = pack_bf16(e.x, e.y);
+          }
+          ptx::tmem_st16(t_s + 16 * c, pk);
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        ptx::tmem_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + s));
+      }
+      if (!ok) break;
+      // ---- epilogue: the row's O
+      const bool join = sh.split && sh.nt > 1;
+      const bool any = first < sh.nt;
+      if (any) {
+        if (!wait_bar(bar(B::O_FULL + s), nof & 1, s_abort)) { ok = false; break; }
+        ++nof;
+        ptx::tc_fence_after();
+      }
+      float a0 = 1.0f, a1 = 0.0f;
+      if (join) {
+        if (s == 1) {
+          s_ml[row] = m;
+          s_ml[kM + row] = l;
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(B::ML_FULL));
+          // (stream 0's threads read this O, too)
+          if (!wait_bar(bar(B::ML_EMPTY), nml & 1, s_abort)) { ok = false; break; }
+        } else {
+          if (!wait_bar(bar(B::ML_FULL), nml & 1, s_abort)) { ok = false; break; }
+          ptx::tc_fence_after();
+          const float m1 = s_ml[row], l1 = s_ml[kM + row];
+          const float mj = fmaxf(m, m1);
+          a0 = m == -INFINITY ? 0.0f : ptx::ex2(m - mj);
+          a1 = m1 == -INFINITY ? 0.0f : ptx::ex2(m1 - mj);
+          // (a stream that saw nothing has l = 0, or NaN scores only and l = NaN)
+          l = (m == -INFINITY ? l : l * a0) + (m1 == -INFINITY ? l1 : l1 * a1);
+          m = mj;
+        }
+        ++nml;
+      }
+      if (!(sh.split && s == 1)) {
+        const float inv = 1.0f / l;
+        const bool odd = s_isodd[j & 1] != 0;
+        const int *so = s_odd + (j & 1) * 3 * D;
+        float *part = w.poff >= 0 ? p.partials + w.poff + (int64_t)(tile * tile_rows + row) * D : nullptr;
+        uint16_t *og = static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + pos) * p.Hq + w.h * g + hh) * D;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          ptx::tmem_ld32(t_o + c, o);
+          ptx::tmem_wait_ld();
+          if (join) {
+            uint32_t o1[32];
+            ptx::tmem_ld32(t_o + D + c, o1);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float u = a0 == 0.0f ? 0.0f : __uint_as_float(o[i]) * a0;
+              o[i] = __float_as_uint(a1 == 0.0f ? u : fmaf(__uint_as_float(o1[i]), a1, u));
+            }
+          }
+          if (odd) {
+            for (int i = 0; i < 32; ++i) {
+              const bool nan = pos >= so[c + i], up = pos >= so[D + c + i], down = pos >= so[2 * D + c + i];
+              if (nan || (up && down)) o[i] = 0x7fffffffu;
+              else if (up || down) o[i] = __float_as_uint(__uint_as_float(o[i]) + (up ? INFINITY : -INFINITY));
+            }
+          }
+          if (!mine) continue;
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              __stcg(reinterpret_cast<uint4 *>(part + c + i), make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint32_t v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = pack_bf16(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
+              *reinterpret_cast<uint4 *>(og + c + i) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+          }
+        }
+        if (part && mine) {
+          float *stat = p.partials + w.poff + (int64_t)w.rows * D + tile * tile_rows + row;
+          __stcg(stat, m);
+          __stcg(stat + w.rows, l);
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (join && lane == 0) ptx::mbar_arrive(bar(B::ML_EMPTY));
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 9) {
+      // ------------------------------------------------------------------ items, Q, K, V
+      uint32_t nk = 0, nv = 0;  // tiles so far
+      int claimed = -2;         // (lane 0) the next item, -2: not claimed yet
+      auto claim = [&]() {
+        if (lane == 0 && claimed == -2) {
+          claimed = atomicAdd(&p.header_mut->next_item, 1);
+          if (claimed >= n_items) claimed = -1;
+        }
+      };
+      uint32_t j = 0;
+      for (;; ++j) {
+        const int slot = j % kItemRing;
+        if (!wait_bar(bar(B::IT_EMPTY + slot), ((j / kItemRing) & 1) ^ 1, s_abort)) { ok = false; break; }
+        claim();
+        WorkItem w;
+        int it = 0;
+        if (lane == 0) {
+          it = claimed;
+          claimed = -2;
+          s_ring[slot].it = it;
+          if (it >= 0) s_ring[slot].w = p.items[it];
+        }
+        it = __shfl_sync(0xffffffffu, it, 0);
+        __syncwarp();
+        w = s_ring[slot].w;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(B::IT_FULL + slot));
+        if (it < 0) break;
+        // Q: whole positions of the item's tiles
+        if (!wait_bar(bar(B::Q_EMPTY), (j & 1) ^ 1, s_abort)) { ok = false; break; }
+        const int tiles = w.rows > tile_rows ? 2 : 1;
+        if (lane == 0) {
+          ptx::mbar_arrive_expect_tx(bar(B::Q_FULL), (uint32_t)(tiles * C::HALVES * tile_rows * 128));
+          for (int s = 0; s < tiles; ++s)
+#pragma unroll
+            for (int hf = 0; hf < C::HALVES; ++hf)
+              ptx::tma_load_4d(sbase + C::OFF_Q + s * C::TILE + hf * C::HALF, &tmq, bar(B::Q_FULL), hf * 64, 0, w.h,
+                               w.q0 + w.row0 / g + s * (tile_rows / g));
+        }
+        __syncwarp();
+        // K and V: K one tile ahead
+        const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + w.t0 / 16;
+        const int nblk = (w.t1 - w.t0 + 15) / 16;
+        const int nt = (w.t1 - w.t0 + kBT - 1) / kBT;
+        auto fetch = [&](int tile4) -> int {  // block ids of four tiles, a lane each
+          const int i = tile4 * 32 + lane;
+          return i < nblk ? __ldg(bt + i) : -1;
+        };
+        int prev = -1, cur = -1, next = fetch(0);
+        auto load = [&](bool is_k, int t, int ids) -> bool {
+          const uint32_t n = is_k ? nk : nv;
+          const int s = n % C::NS;
+          const int full = (is_k ? B::K_FULL : B::V_FULL) + s, empty = (is_k ? B::K_EMPTY : B::V_EMPTY) + s;
+          const int rel = 8 * t + (lane & 7);
+          int bid = __shfl_sync(0xffffffffu, ids, rel & 31);
+          if (!wait_bar(bar(empty), ((n / C::NS) & 1) ^ 1, s_abort)) return false;
+          const bool valid = bid >= 0 && bid < p.num_blocks;
+          if (is_k && lane < 8 && rel < nblk && !valid) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, w.r);
+          ++(is_k ? nk : nv);
+          if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full), C::TILE);
+          __syncwarp();
+          const uint32_t dst = sbase + (is_k ? C::OFF_K : C::OFF_V) + s * C::TILE;
+          const int b0 = __shfl_sync(0xffffffffu, bid, 0);
+          if (__ballot_sync(0xffffffffu, lane < 8 && valid && bid == b0 + lane) == 0xffu) {
+            if (lane == 0) {
+#pragma unroll
+              for (int hf = 0; hf < C::HALVES; ++hf)
+                ptx::tma_load_4d(dst + hf * C::HALF, is_k ? &tmk8 : &tmv8, bar(full), hf * 64, 0, w.h, b0);
+            }
+          } else if (lane < 8) {
+            if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
+#pragma unroll
+            for (int hf = 0; hf < C::HALVES; ++hf)
+              ptx::tma_load_4d(dst + hf * C::HALF + lane * (16 * 128), is_k ? &tmk : &tmv, bar(full), hf * 64, 0, w.h, bid);
+          }
+          __syncwarp();
+          return true;
+        };
+        for (int t = 0; t <= nt && ok; ++t) {
+          if ((t & 3) == 0 && t < nt) {
+            prev = cur;
+            cur = next;
+            next = fetch((t >> 2) + 1);
+          }
+          if (t < nt) ok = load(true, t, cur);
+          if (t == max(nt - 2, 0)) claim();  // the next item, early enough to hide the way to it
+          if (t > 0 && ok) ok = load(false, t - 1, (t & 3) == 0 && t < nt ? prev : cur);
+        }
+        if (!ok) break;
+      }
+      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      // drain: what was issued must land before the CTA's shared memory goes away
+      if (lane == 0) {
+        auto drain = [&](int full, uint32_t n) {
+          for (uint32_t k = 0; k < C::NS && k < n; ++k) {
+            const long long t0 = clock64();
+            while (!ptx::mbar_try_wait(bar(full + (n - 1 - k) % C::NS), ((n - 1 - k) / C::NS) & 1) && clock64() - t0 < kWaitCycles) {
+            }
+          }
+        };
+        drain(B::K_FULL, nk);
+        drain(B::V_FULL, nv);
+        if (!ok && j > 0) {  // (a Q that nobody waited for)
+          const long long t0 = clock64();
+          while (!ptx::mbar_try_wait(bar(B::Q_FULL), (j - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {
+          }
+        }
+      }
+    } else if (warp == 8) {
+      // ------------------------------------------------------------------ MMA issuer
+      const uint32_t idesc_s = ptx::idesc_bf16_f32(kM, kBT, false, false);
+      const uint32_t idesc_o = ptx::idesc_bf16_f32(kM, D, false, true);
+      uint32_t k0 = 0;               // key tiles of the items before
+      uint32_t np[2] = {0, 0};       // P tiles so far, per stream
+      WorkItem w;
+      for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
+        const Shape sh = shape_of(w, tile_rows, g);
+        if (!wait_bar(bar(B::Q_FULL), j & 1, s_abort)) { ok = false; break; }
+        auto issue_s = [&](int i) -> bool {  // step i: stream i & 1
+          const int s = i & 1, t = sh.split ? i : i >> 1;
+          const uint32_t n = k0 + t;
+          const int st = n % C::NS;
+          if (!wait_bar(bar(B::K_FULL + st), (n / C::NS) & 1, s_abort)) return false;
+          if (lane == 0) {
+            ptx::tc_fence_after();
+            const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q + (sh.split ? 0 : s) * C::TILE, 16, 1024);
+            const uint64_t kd = ptx::sdesc_sw128(sbase + C::OFF_K + st * C::TILE, 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const int off = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
+              ptx::umma_f16(tmem + s * kBT, qd + off, kd + off, idesc_s, ks > 0);
+            }
+            ptx::umma_commit(bar(B::S_FULL + s));
+            if (sh.split || s == 1) ptx::umma_commit(bar(B::K_EMPTY + st));
+            if (i == sh.steps - 1) ptx::umma_commit(bar(B::Q_EMPTY));
+          }
+          __syncwarp();
+          return true;
+        };
+        ok = issue_s(0) && (sh.steps < 2 || issue_s(1));
+        for (int i = 0; i < sh.steps && ok; ++i) {
+          const int s = i & 1, t = sh.split ? i : i >> 1;
+          const uint32_t n = k0 + t;
+          const int st = n % C::NS;
+          if ((sh.split || s == 0)) {
+            if (!wait_bar(bar(B::V_FULL + st), (n / C::NS) & 1, s_abort) ||
+                !wait_bar(bar(B::V_CLEAN + st), (n / C::NS) & 1, s_abort)) {
+              ok = false;
+              break;
+            }
+          }
+          if (!wait_bar(bar(B::P_FULL + s), np[s] & 1, s_abort)) { ok = false; break; }
+          ++np[s];
+          if (lane == 0) {
+            ptx::tc_fence_after();
+            const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::HALF, 1024);
+            const bool first = sh.split ? i < 2 : t == 0;
+#pragma unroll
+            for (int ks = 0; ks < kBT / 16; ++ks)
+              ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + s * kBT + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o, !first || ks > 0);
+            if (sh.split || s == 1) ptx::umma_commit(bar(B::V_EMPTY + st));
+            if (i + 2 >= sh.steps) ptx::umma_commit(bar(B::O_FULL + s));
+          }
+          __syncwarp();
+          if (i + 2 < sh.steps) ok = issue_s(i + 2);
+        }
+        k0 += sh.nt;
+      }
+      if (lane == 0) {
+        // every MMA issued must finish before the TMEM is released
+        ptx::umma_commit(bar(B::MMA_DONE));
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(bar(B::MMA_DONE), 0) && clock64() - t0 < kWaitCycles) {
+        }
+      }
+    } else if (warp == 10) {
+      // ------------------------------------------------------------------ V of tiles that some row does not see entirely
+      uint32_t k0 = 0;
+      WorkItem w;
+      for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
+        const Shape sh = shape_of(w, tile_rows, g);
+        const int ob = j & 1;
+        // this item's buffer of odd values: free, and cleared where it was used
+        if (!wait_bar(bar(B::ODD_FREE + ob), ((j >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
+        if (s_isodd[ob]) {
+          __syncwarp();
+          for (int i = lane; i < 3 * D; i += 32) s_odd[ob * 3 * D + i] = INT32_MAX;
+          s_isodd[ob] = 0;
+          __syncwarp();
+        }
+        for (int t = 0; t < sh.nt; ++t) {
+          const uint32_t n = k0 + t;
+          const int st = n % C::NS;
+          if (!wait_bar(bar(B::V_FULL + st), (n / C::NS) & 1, s_abort)) { ok = false; break; }
+          if (t < sh.plain) {
+            if (lane == 0) ptx::mbar_arrive(bar(B::V_CLEAN + st));
+            continue;
+          }
+#pragma unroll 1
+          for (int x = 0; x < kBT / 32; ++x) {
+            const int row = x * 32 + lane;
+            uint8_t *line = smem + C::OFF_V + st * C::TILE + row * 128;
+            __nv_bfloat162 acc = __floats2bfloat162_rn(0.0f, 0.0f);
+            const __nv_bfloat162 zero = acc;
+#pragma unroll
+            for (int c = 0; c < 8 * C::HALVES; ++c) {  // (no two of eight lanes read the same banks)
+              const uint4 v = *reinterpret_cast<const uint4 *>(line + (c >> 3) * C::HALF + (((c + lane) & 7) << 4));
+              const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u[e]), zero, acc);
+            }
+            if (__low2float(acc) + __high2float(acc) == 0.0f) continue;  // every value is finite
+            const int key = w.t0 + t * kBT + row;
+            for (int c = 0; c < 8 * C::HALVES; ++c)
+              for (int e = 0; e < 8; ++e) {
+                uint16_t *at = reinterpret_cast<uint16_t *>(line + (c >> 3) * C::HALF + ((c & 7) << 4)) + e;
+                const uint32_t bits = *at;
+                if ((bits & 0x7f80u) != 0x7f80u) continue;
+                *at = 0;
+                if (key >= w.t1) continue;  // nobody's
+                const int d = (c >> 3) * 64 + (((c & 7) ^ (row & 7)) << 3) + e;
+                const int kind = (bits & 0x7fu) ? 0 : (bits & 0x8000u) ? 2 : 1;
+                atomicMin(&s_odd[(ob * 3 + kind) * D + d], max(key - w.ctx, 0));  // the first position that sees it
+                s_isodd[ob] = 1;
+              }
+          }
+          __threadfence_block();
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(B::V_CLEAN + st));
+        }
+        k0 += sh.nt;
+      }
+      }
+  }
+
+  if (!ok && lane == 0) report(p.status, WISP_DEV_TIMEOUT, p.request_ids, -1);
+  // teardown: the TMEM is freed once every warp has said that it is done with it
+  __syncwarp();
+  ptx::tc_fence_before();
+  if (lane == 0) ptx::mbar_arrive(bar(B::FIN));
+  if (warp == 8) {
+    const long long t0 = clock64();
+    while (!ptx::mbar_try_wait(bar(B::FIN), 0) && clock64() - t0 < kWaitCycles) {
+    }
+    __syncwarp();
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------- host side
+namespace {
+
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+
+cudaError_t get_encode() {
+  if (g_encode) return cudaSuccess;
+  void *fn = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+  if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+  g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+  return cudaSuccess;
+}
+
+// A 4-D bf16 tensor with D innermost, in boxes of 64 elements (128 bytes, swizzled) x b1 x 1 x b3.
+cudaError_t encode(CUtensorMap *map, const void *base, int D, int64_t n1, int64_t n2, int64_t n3, int b1, int b3) {
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)n1, (cuuint64_t)n2, (cuuint64_t)n3};
+  const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)(n1 * D * 2), (cuuint64_t)(n2 * n1 * D * 2)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)b1, 1, (cuuint32_t)b3};
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D>
+cudaError_t launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t s) {
+  const int g = p.Hq / p.Hkv;
+  CUtensorMap tq, tk, tv, tk8, tv8;
+  cudaError_t e = encode(&tq, p.q, D, g, p.Hkv, total_q_rows, g, kM / g);
+  if (e == cudaSuccess) e = encode(&tk, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
+  if (e == cudaSuccess) e = encode(&tv, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
+  if (e == cudaSuccess) e = encode(&tk8, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, 8);
+  if (e == cudaSuccess) e = encode(&tv8, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, 8);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof cfg);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Cfg<D>::SMEM;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, prompt_tc_kernel<D>, p, tq, tk, tv, tk8, tv8);
+}
+
+}  // namespace
+
+cudaError_t prompt_tc_setup() {
+  cudaError_t e = get_encode();
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(prompt_tc_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prompt_tc_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::SMEM);
+  return e;
+}
+
+cudaError_t prompt_tc_launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t s) {
+  return p.D == 128 ? launch<128>(p, total_q_rows, grid, s) : launch<64>(p, total_q_rows, grid, s);
+}
+
+}  // namespace wisp
