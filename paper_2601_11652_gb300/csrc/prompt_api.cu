@@ -43,7 +43,6 @@ wisp_status check(const wisp_prompt_args *x) {
   if (!a->draft_lens || !a->context_lens || !a->block_tables || !a->q || !a->k_cache || !a->v_cache || !a->out)
     return WISP_ERR_INVALID_ARG;
   if (!aligned16(a->q) || !aligned16(a->k_cache) || !aligned16(a->v_cache) || !aligned16(a->out)) return WISP_ERR_INVALID_ARG;
-  if (x->cache_dtype == WISP_E4M3 && a->qkv_dtype == WISP_BF16) return WISP_ERR_UNSUPPORTED;
   if (x->cache_dtype == WISP_E4M3 && (!x->k_scale || !x->v_scale)) return WISP_ERR_INVALID_ARG;
   if ((int64_t)a->max_blocks_per_seq * a->block_size > INT32_MAX / 2) return WISP_ERR_UNSUPPORTED;
   if ((int64_t)a->total_q_rows * (a->Hq / a->Hkv) > INT32_MAX / 2) return WISP_ERR_UNSUPPORTED;

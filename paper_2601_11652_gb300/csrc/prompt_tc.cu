@@ -22,8 +22,11 @@
 //   * 10: looks at V where a tile has keys that some row does not see: 0 * NaN would reach every row.  Values that are not finite
 //     are set to zero there and remembered with the first position that sees them; the epilogue writes what they make of its rows.
 // (11: registers are allotted per four warps.)
+//   * 12-15, over an 8-bit cache: a tile's codes arrive in the upper half of its stage, or of each warp's part of it, and these warps
+//     write it in bf16, times the page's scale, in place: a lane's row of codes in registers first.
 // Every wait is bounded: an expired one records WISP_DEV_TIMEOUT and the CTA drains.
 #include "attn_merge.cuh"
+#include "fp8.cuh"
 #include "prompt.cuh"
 #include "sm100_ptx.cuh"
 
@@ -36,7 +39,7 @@ namespace {
 
 constexpr int kBT = 128;      // keys per tile
 constexpr int kM = 128;       // rows per stream
-constexpr int kThreads = 384;
+constexpr int threads_of(bool kv8) { return kv8 ? 512 : 384; }
 constexpr uint32_t kTmemCols = 512;  // S (and P) of the streams at 0 and 128, O at 256 and 256 + D
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
 constexpr float kLoose = 8.0f;  // how far (log2) a score may exceed its row's reference
@@ -52,7 +55,7 @@ struct Cfg {
   static constexpr int OFF_K = 2 * TILE;
   static constexpr int OFF_V = OFF_K + NS * TILE;
   static constexpr int OFF_BAR = OFF_V + NS * TILE;
-  static constexpr int N_BAR = 40;
+  static constexpr int N_BAR = 56;
   static constexpr int OFF_RING = OFF_BAR + N_BAR * 8;             // kItemRing x 64 bytes
   static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;       // tmem base, abort flag, odd-value flags
   static constexpr int OFF_ML = OFF_MISC + 64;                     // float [2][128]: m, l of stream 1 for the join
@@ -72,7 +75,8 @@ struct Bars {
   static constexpr int ODD_FREE = V_CLEAN + C::NS;           // [2] per buffer of odd values: its item's epilogues are done
   static constexpr int ML_FULL = ODD_FREE + 2, ML_EMPTY = ML_FULL + 1;  // stream 1's m and l (and O): published, read
   static constexpr int MMA_DONE = ML_EMPTY + 1, FIN = MMA_DONE + 1;
-  static_assert(FIN + 1 <= C::N_BAR, "barrier count");
+  static constexpr int KC_FULL = FIN + 1, VC_FULL = KC_FULL + C::NS;  // [NS] codes have arrived (8-bit cache)
+  static_assert(VC_FULL + C::NS <= C::N_BAR, "barrier count");
 };
 
 __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort) {
@@ -86,6 +90,13 @@ __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile i
       return false;
     }
   }
+}
+
+// two values in bf16, rounded to nearest; past its range (and infinite) its largest
+__device__ __forceinline__ uint32_t bf16x2_sat(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
 }
 
 // What the roles need to know of an item.
@@ -107,13 +118,14 @@ __device__ __forceinline__ Shape shape_of(const WorkItem &w, int tile_rows, int 
 
 }  // namespace
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int D, bool KV8>
+__global__ void __launch_bounds__(threads_of(KV8), 1)
     prompt_tc_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap tmq,
                      const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
                      const __grid_constant__ CUtensorMap tmk8, const __grid_constant__ CUtensorMap tmv8) {
   using C = Cfg<D>;
   using B = Bars<D>;
+  constexpr int kThreads = threads_of(KV8);
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sbase = ptx::smem_u32(smem);
@@ -135,9 +147,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NS; ++i) {
-      ptx::mbar_init(bar(B::K_FULL + i), 1);
+      ptx::mbar_init(bar(B::K_FULL + i), KV8 ? 4 : 1);
       ptx::mbar_init(bar(B::K_EMPTY + i), 1);
-      ptx::mbar_init(bar(B::V_FULL + i), 1);
+      ptx::mbar_init(bar(B::V_FULL + i), KV8 ? 4 : 1);
+      ptx::mbar_init(bar(B::KC_FULL + i), 1);
+      ptx::mbar_init(bar(B::VC_FULL + i), 1);
       ptx::mbar_init(bar(B::V_EMPTY + i), 1);
       ptx::mbar_init(bar(B::V_CLEAN + i), 1);
     }
@@ -151,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kItemRing; ++i) {
       ptx::mbar_init(bar(B::IT_FULL + i), 1);
-      ptx::mbar_init(bar(B::IT_EMPTY + i), 8 + 1 + 1);  // softmax warps, MMA issuer, the one that looks at V
+      ptx::mbar_init(bar(B::IT_EMPTY + i), 8 + 1 + 1 + (KV8 ? 4 : 0));  // softmax warps, MMA issuer, the one that looks at V, decoders
     }
     ptx::mbar_init(bar(B::ML_FULL), 4);
     ptx::mbar_init(bar(B::ML_EMPTY), 4);
@@ -197,9 +211,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   bool ok = true;
   if (warp < 8) {
-    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 208 + 4 x 88.  (Each split stands at the head of its own
-    // branch: after a join the compiler counts with the least.)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 208 + 4 x 88; 16 with 128, 2048 = 8 x 192 + 8 x 64.
+    // (Each split stands at the head of its own branch: after a join the compiler counts with the least.)
+    if constexpr (KV8)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------------------------ softmax and epilogue, stream s, a row per thread
     const int s = warp >> 2;
     const int row = threadIdx.x & 127;
@@ -370,8 +387,81 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
     }
+  } else if (KV8 && warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // ------------------------------------------------------------------ codes to bf16
+    const int row = (warp - 12) * 32 + lane;
+    constexpr int CH = D / 16;  // 16-byte chunks of a row of codes
+    uint32_t k0 = 0;
+    WorkItem w;
+    for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
+      const int nt = (w.t1 - w.t0 + kBT - 1) / kBT, nblk = (w.t1 - w.t0 + 15) / 16;
+      const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + w.t0 / 16;
+      auto page = [&](int t) -> int {
+        const int rel = 8 * t + row / 16;
+        return rel < nblk ? __ldg(bt + rel) : -1;
+      };
+      auto scale_of = [&](const float *sc, int b) { return b >= 0 && b < p.num_blocks ? __ldg(sc + (int64_t)b * p.Hkv + w.h) : 0.0f; };
+      auto decode = [&](uint8_t *tile, float sc) {
+        // its own warp's rows lie over its own codes only
+        const uint8_t *src = tile + (D == 128 ? C::HALF + row * 128 : (warp - 12) * 4096 + 2048 + lane * 64);
+        uint4 v[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = *reinterpret_cast<const uint4 *>(src + (((c + lane) % CH) << 4));
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int at = (c + lane) % CH;
+          const uint32_t u[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+          uint32_t o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float2 f = h2_to_f2(e4m3x2_to_h2(e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xffffu));
+            o[e] = bf16x2_sat(f.x * sc, f.y * sc);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int chunk = 2 * at + e;
+            *reinterpret_cast<uint4 *>(tile + (chunk >> 3) * C::HALF + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) =
+                make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+      };
+      // scales one tile ahead, their pages two
+      int b1 = page(0), b2 = page(1);
+      float ks = scale_of(p.k_scale, b1), vs = scale_of(p.v_scale, b1), vs0 = 0.0f;
+      for (int t = 0; t <= nt; ++t) {
+        float ks1 = 0.0f, vs1 = 0.0f;
+        if (t < nt) {
+          ks1 = scale_of(p.k_scale, b2);
+          vs1 = scale_of(p.v_scale, b2);
+          b2 = page(t + 2);
+          const uint32_t n = k0 + t;
+          const int st = n % C::NS;
+          if (!wait_bar(bar(B::KC_FULL + st), (n / C::NS) & 1, s_abort)) { ok = false; break; }
+          decode(smem + C::OFF_K + st * C::TILE, ks);
+          if (lane == 0) ptx::mbar_arrive(bar(B::K_FULL + st));
+        }
+        if (t > 0) {
+          const uint32_t n = k0 + t - 1;
+          const int st = n % C::NS;
+          if (!wait_bar(bar(B::VC_FULL + st), (n / C::NS) & 1, s_abort)) { ok = false; break; }
+          decode(smem + C::OFF_V + st * C::TILE, vs0);
+          if (lane == 0) ptx::mbar_arrive(bar(B::V_FULL + st));
+        }
+        vs0 = vs;
+        ks = ks1;
+        vs = vs1;
+      }
+      k0 += nt;
+    }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if constexpr (KV8)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
       uint32_t nk = 0, nv = 0;  // tiles so far
@@ -425,28 +515,43 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto load = [&](bool is_k, int t, int ids) -> bool {
           const uint32_t n = is_k ? nk : nv;
           const int s = n % C::NS;
-          const int full = (is_k ? B::K_FULL : B::V_FULL) + s, empty = (is_k ? B::K_EMPTY : B::V_EMPTY) + s;
+          const int full = (KV8 ? (is_k ? B::KC_FULL : B::VC_FULL) : (is_k ? B::K_FULL : B::V_FULL)) + s;
+          const int empty = (is_k ? B::K_EMPTY : B::V_EMPTY) + s;
           const int rel = 8 * t + (lane & 7);
           int bid = __shfl_sync(0xffffffffu, ids, rel & 31);
           if (!wait_bar(bar(empty), ((n / C::NS) & 1) ^ 1, s_abort)) return false;
           const bool valid = bid >= 0 && bid < p.num_blocks;
           if (is_k && lane < 8 && rel < nblk && !valid) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, w.r);
           ++(is_k ? nk : nv);
-          if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full), C::TILE);
+          if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full), KV8 ? C::TILE / 2 : C::TILE);
           __syncwarp();
           const uint32_t dst = sbase + (is_k ? C::OFF_K : C::OFF_V) + s * C::TILE;
           const int b0 = __shfl_sync(0xffffffffu, bid, 0);
-          if (__ballot_sync(0xffffffffu, lane < 8 && valid && bid == b0 + lane) == 0xffu) {
+          const bool row8 = __ballot_sync(0xffffffffu, lane < 8 && valid && bid == b0 + lane) == 0xffu;
+          if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
+          const CUtensorMap *one = is_k ? &tmk : &tmv, *more = is_k ? &tmk8 : &tmv8;
+          if constexpr (KV8) {
+            // codes: where a warp's rows go it finds its two pages (D = 128: in the upper half of the tile; 64: of its own rows)
+            if (D == 128) {
+              if (row8) {
+                if (lane == 0) ptx::tma_load_4d(dst + C::HALF, more, bar(full), 0, 0, w.h, b0);
+              } else if (lane < 8) {
+                ptx::tma_load_4d(dst + C::HALF + lane * (16 * 128), one, bar(full), 0, 0, w.h, bid);
+              }
+            } else if (row8) {
+              if (lane < 4) ptx::tma_load_4d(dst + lane * 4096 + 2048, more, bar(full), 0, 0, w.h, b0 + 2 * lane);
+            } else if (lane < 8) {
+              ptx::tma_load_4d(dst + (lane >> 1) * 4096 + 2048 + (lane & 1) * 1024, one, bar(full), 0, 0, w.h, bid);
+            }
+          } else if (row8) {
             if (lane == 0) {
 #pragma unroll
-              for (int hf = 0; hf < C::HALVES; ++hf)
-                ptx::tma_load_4d(dst + hf * C::HALF, is_k ? &tmk8 : &tmv8, bar(full), hf * 64, 0, w.h, b0);
+              for (int hf = 0; hf < C::HALVES; ++hf) ptx::tma_load_4d(dst + hf * C::HALF, more, bar(full), hf * 64, 0, w.h, b0);
             }
           } else if (lane < 8) {
-            if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
 #pragma unroll
             for (int hf = 0; hf < C::HALVES; ++hf)
-              ptx::tma_load_4d(dst + hf * C::HALF + lane * (16 * 128), is_k ? &tmk : &tmv, bar(full), hf * 64, 0, w.h, bid);
+              ptx::tma_load_4d(dst + hf * C::HALF + lane * (16 * 128), one, bar(full), hf * 64, 0, w.h, bid);
           }
           __syncwarp();
           return true;
@@ -473,8 +578,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         };
-        drain(B::K_FULL, nk);
-        drain(B::V_FULL, nv);
+        drain(KV8 ? B::KC_FULL : B::K_FULL, nk);
+        drain(KV8 ? B::VC_FULL : B::V_FULL, nv);
         if (!ok && j > 0) {  // (a Q that nobody waited for)
           const long long t0 = clock64();
           while (!ptx::mbar_try_wait(bar(B::Q_FULL), (j - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {
@@ -639,27 +744,29 @@ cudaError_t get_encode() {
   return cudaSuccess;
 }
 
-// A 4-D bf16 tensor with D innermost, in boxes of 64 elements (128 bytes, swizzled) x b1 x 1 x b3.
-cudaError_t encode(CUtensorMap *map, const void *base, int D, int64_t n1, int64_t n2, int64_t n3, int b1, int b3) {
+// A 4-D tensor with D innermost, in boxes of b0 elements x b1 x 1 x b3: bf16, 64 elements (128 bytes, swizzled), or codes.
+cudaError_t encode(CUtensorMap *map, bool codes, const void *base, int D, int64_t n1, int64_t n2, int64_t n3, int b1, int b3) {
+  const cuuint64_t es = codes ? 1 : 2;
   const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)n1, (cuuint64_t)n2, (cuuint64_t)n3};
-  const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)(n1 * D * 2), (cuuint64_t)(n2 * n1 * D * 2)};
-  const cuuint32_t box[4] = {64, (cuuint32_t)b1, 1, (cuuint32_t)b3};
+  const cuuint64_t strides[3] = {D * es, n1 * D * es, n2 * n1 * D * es};
+  const cuuint32_t box[4] = {(cuuint32_t)(codes ? D : 64), (cuuint32_t)b1, 1, (cuuint32_t)b3};
   const cuuint32_t ones[4] = {1, 1, 1, 1};
-  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, ones,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = g_encode(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                              const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int D>
+template <int D, bool KV8>
 cudaError_t launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t s) {
-  const int g = p.Hq / p.Hkv;
+  const int g = p.Hq / p.Hkv, more = KV8 && D == 64 ? 2 : 8;  // pages in a box of several
   CUtensorMap tq, tk, tv, tk8, tv8;
-  cudaError_t e = encode(&tq, p.q, D, g, p.Hkv, total_q_rows, g, kM / g);
-  if (e == cudaSuccess) e = encode(&tk, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
-  if (e == cudaSuccess) e = encode(&tv, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
-  if (e == cudaSuccess) e = encode(&tk8, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, 8);
-  if (e == cudaSuccess) e = encode(&tv8, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, 8);
+  cudaError_t e = encode(&tq, false, p.q, D, g, p.Hkv, total_q_rows, g, kM / g);
+  if (e == cudaSuccess) e = encode(&tk, KV8, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
+  if (e == cudaSuccess) e = encode(&tv, KV8, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, 1);
+  if (e == cudaSuccess) e = encode(&tk8, KV8, p.k_cache, D, 16, p.Hkv, p.num_blocks, 16, more);
+  if (e == cudaSuccess) e = encode(&tv8, KV8, p.v_cache, D, 16, p.Hkv, p.num_blocks, 16, more);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
@@ -667,26 +774,32 @@ cudaError_t launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads_of(KV8));
   cfg.dynamicSmemBytes = Cfg<D>::SMEM;
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, prompt_tc_kernel<D>, p, tq, tk, tv, tk8, tv8);
+  return cudaLaunchKernelEx(&cfg, prompt_tc_kernel<D, KV8>, p, tq, tk, tv, tk8, tv8);
+}
+
+template <int D, bool KV8>
+cudaError_t setup() {
+  return cudaFuncSetAttribute(prompt_tc_kernel<D, KV8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
 }
 
 }  // namespace
 
 cudaError_t prompt_tc_setup() {
   cudaError_t e = get_encode();
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(prompt_tc_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prompt_tc_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::SMEM);
-  return e;
+  if (e == cudaSuccess) e = setup<128, false>();
+  if (e == cudaSuccess) e = setup<128, true>();
+  if (e == cudaSuccess) e = setup<64, false>();
+  return e == cudaSuccess ? setup<64, true>() : e;
 }
 
 cudaError_t prompt_tc_launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t s) {
-  return p.D == 128 ? launch<128>(p, total_q_rows, grid, s) : launch<64>(p, total_q_rows, grid, s);
+  if (p.k_scale) return p.D == 128 ? launch<128, true>(p, total_q_rows, grid, s) : launch<64, true>(p, total_q_rows, grid, s);
+  return p.D == 128 ? launch<128, false>(p, total_q_rows, grid, s) : launch<64, false>(p, total_q_rows, grid, s);
 }
 
 }  // namespace wisp

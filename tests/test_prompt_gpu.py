@@ -148,7 +148,7 @@ class Case:
         return worst
 
 
-TYPES = [(BF, None), (F32, None), (F32, "e4m3")]
+TYPES = [(BF, None), (BF, "e4m3"), (F32, None), (F32, "e4m3")]
 HEADS = [(32, 8, 128), (28, 4, 128), (8, 8, 64), (32, 8, 64), (5, 1, 128), (16, 1, 64)]
 SHAPES = {"one_token": ([0], [0]), "one_row_each": ([0, 0, 0, 0], [0, 1, 15, 300]), "small": ([1, 2, 15, 16, 17], [0, 0, 0, 0, 0]),
           "tiles": ([30, 31, 32, 63, 64, 65], [0, 1, 127, 128, 64, 63]), "mixed": ([199, 0, 500, 7, 128], [0, 700, 33, 1000, 129]),
