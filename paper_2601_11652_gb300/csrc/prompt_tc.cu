@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         // Q: whole positions of the item's tiles
         if (!wait_bar(bar(B::Q_EMPTY), (j & 1) ^ 1, s_abort)) { ok = false; break; }
         const int tiles = w.rows > tile_rows ? 2 : 1;
-        if (lane == 0) {
+        if (ptx::elect_one()) {
           ptx::mbar_arrive_expect_tx(bar(B::Q_FULL), (uint32_t)(tiles * C::HALVES * tile_rows * 128));
           for (int s = 0; s < tiles; ++s)
 #pragma unroll
@@ -523,35 +523,43 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           const bool valid = bid >= 0 && bid < p.num_blocks;
           if (is_k && lane < 8 && rel < nblk && !valid) report(p.status, WISP_DEV_BAD_BLOCK, p.request_ids, w.r);
           ++(is_k ? nk : nv);
-          if (lane == 0) ptx::mbar_arrive_expect_tx(bar(full), KV8 ? C::TILE / 2 : C::TILE);
-          __syncwarp();
           const uint32_t dst = sbase + (is_k ? C::OFF_K : C::OFF_V) + s * C::TILE;
           const int b0 = __shfl_sync(0xffffffffu, bid, 0);
           const bool row8 = __ballot_sync(0xffffffffu, lane < 8 && valid && bid == b0 + lane) == 0xffu;
           if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
+          int bids[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) bids[x] = __shfl_sync(0xffffffffu, bid, x);
           const CUtensorMap *one = is_k ? &tmk : &tmv, *more = is_k ? &tmk8 : &tmv8;
-          if constexpr (KV8) {
-            // codes: where a warp's rows go it finds its two pages (D = 128: in the upper half of the tile; 64: of its own rows)
-            if (D == 128) {
-              if (row8) {
-                if (lane == 0) ptx::tma_load_4d(dst + C::HALF, more, bar(full), 0, 0, w.h, b0);
-              } else if (lane < 8) {
-                ptx::tma_load_4d(dst + C::HALF + lane * (16 * 128), one, bar(full), 0, 0, w.h, bid);
+          if (ptx::elect_one()) {
+            ptx::mbar_arrive_expect_tx(bar(full), KV8 ? C::TILE / 2 : C::TILE);
+            if constexpr (KV8) {
+              // codes: where a warp's rows go it finds its two pages (D = 128: in the upper half of the tile; 64: of its own rows)
+              if (D == 128) {
+                if (row8) {
+                  ptx::tma_load_4d(dst + C::HALF, more, bar(full), 0, 0, w.h, b0);
+                } else {
+#pragma unroll
+                  for (int x = 0; x < 8; ++x) ptx::tma_load_4d(dst + C::HALF + x * (16 * 128), one, bar(full), 0, 0, w.h, bids[x]);
+                }
+              } else if (row8) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) ptx::tma_load_4d(dst + x * 4096 + 2048, more, bar(full), 0, 0, w.h, b0 + 2 * x);
+              } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                  ptx::tma_load_4d(dst + (x >> 1) * 4096 + 2048 + (x & 1) * 1024, one, bar(full), 0, 0, w.h, bids[x]);
               }
             } else if (row8) {
-              if (lane < 4) ptx::tma_load_4d(dst + lane * 4096 + 2048, more, bar(full), 0, 0, w.h, b0 + 2 * lane);
-            } else if (lane < 8) {
-              ptx::tma_load_4d(dst + (lane >> 1) * 4096 + 2048 + (lane & 1) * 1024, one, bar(full), 0, 0, w.h, bid);
-            }
-          } else if (row8) {
-            if (lane == 0) {
 #pragma unroll
               for (int hf = 0; hf < C::HALVES; ++hf) ptx::tma_load_4d(dst + hf * C::HALF, more, bar(full), hf * 64, 0, w.h, b0);
-            }
-          } else if (lane < 8) {
+            } else {
 #pragma unroll
-            for (int hf = 0; hf < C::HALVES; ++hf)
-              ptx::tma_load_4d(dst + hf * C::HALF + lane * (16 * 128), one, bar(full), hf * 64, 0, w.h, bid);
+              for (int x = 0; x < 8; ++x)
+#pragma unroll
+                for (int hf = 0; hf < C::HALVES; ++hf)
+                  ptx::tma_load_4d(dst + hf * C::HALF + x * (16 * 128), one, bar(full), hf * 64, 0, w.h, bids[x]);
+            }
           }
           __syncwarp();
           return true;
@@ -601,7 +609,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           const uint32_t n = k0 + t;
           const int st = n % C::NS;
           if (!wait_bar(bar(B::K_FULL + st), (n / C::NS) & 1, s_abort)) return false;
-          if (lane == 0) {
+          if (ptx::elect_one()) {
             ptx::tc_fence_after();
             const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q + (sh.split ? 0 : s) * C::TILE, 16, 1024);
             const uint64_t kd = ptx::sdesc_sw128(sbase + C::OFF_K + st * C::TILE, 16, 1024);
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           }
           if (!wait_bar(bar(B::P_FULL + s), np[s] & 1, s_abort)) { ok = false; break; }
           ++np[s];
-          if (lane == 0) {
+          if (ptx::elect_one()) {
             ptx::tc_fence_after();
             const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::HALF, 1024);
             const bool first = sh.split ? i < 2 : t == 0;
@@ -646,7 +654,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         }
         k0 += sh.nt;
       }
-      if (lane == 0) {
+      if (ptx::elect_one()) {
         // every MMA issued must finish before the TMEM is released
         ptx::umma_commit(bar(B::MMA_DONE));
         const long long t0 = clock64();
