@@ -51,10 +51,12 @@ struct Cfg {
   static constexpr int HALF = kBT * 128;          // a 64-wide half of a tile: [128][128 B], swizzled
   static constexpr int TILE = HALVES * HALF;
   static constexpr int NS = D == 128 ? 2 : 4;     // stages of K, and of V
-  static constexpr int OFF_Q = 0;                 // two tiles
-  static constexpr int OFF_K = 2 * TILE;
+  static constexpr int NQ = D == 128 ? 1 : 2;     // buffers of an item's two tiles of Q
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = NQ * 2 * TILE;
   static constexpr int OFF_V = OFF_K + NS * TILE;
-  static constexpr int OFF_BAR = OFF_V + NS * TILE;
+  static constexpr int OFF_ST = OFF_V + NS * TILE;  // the epilogue's rows on their way out: 2 KB a warp
+  static constexpr int OFF_BAR = OFF_ST + 8 * 2048;
   static constexpr int N_BAR = 56;
   static constexpr int OFF_RING = OFF_BAR + N_BAR * 8;             // kItemRing x 64 bytes
   static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;       // tmem base, abort flag, odd-value flags
@@ -68,8 +70,8 @@ template <int D>
 struct Bars {
   using C = Cfg<D>;
   static constexpr int K_FULL = 0, K_EMPTY = C::NS, V_FULL = 2 * C::NS, V_EMPTY = 3 * C::NS;
-  static constexpr int Q_FULL = 4 * C::NS, Q_EMPTY = Q_FULL + 1;
-  static constexpr int S_FULL = Q_EMPTY + 1, P_FULL = S_FULL + 2, O_FULL = P_FULL + 2;  // [2] per stream
+  static constexpr int Q_FULL = 4 * C::NS, Q_EMPTY = Q_FULL + 2;  // [NQ]
+  static constexpr int S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, O_FULL = P_FULL + 4;  // [2] per stream
   static constexpr int IT_FULL = O_FULL + 2, IT_EMPTY = IT_FULL + kItemRing;
   static constexpr int V_CLEAN = IT_EMPTY + kItemRing;   // [NS] the tile's V has been looked at
   static constexpr int ODD_FREE = V_CLEAN + C::NS;           // [2] per buffer of odd values: its item's epilogues are done
@@ -126,6 +128,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   using C = Cfg<D>;
   using B = Bars<D>;
   constexpr int kThreads = threads_of(KV8);
+  // P is handed over in two halves of a tile's keys, so that the product with the first overlaps the softmax of the second: 1.3% with
+  // D = 128 (16384 tokens 1571 -> 1550 us); elsewhere the softmax warps' issue slots bound the tile, and it costs 2 to 3%.
+  constexpr int kWhole = D == 128 && !KV8 ? 0 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sbase = ptx::smem_u32(smem);
@@ -155,11 +160,14 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       ptx::mbar_init(bar(B::V_EMPTY + i), 1);
       ptx::mbar_init(bar(B::V_CLEAN + i), 1);
     }
-    ptx::mbar_init(bar(B::Q_FULL), 1);
-    ptx::mbar_init(bar(B::Q_EMPTY), 1);
+    for (int i = 0; i < C::NQ; ++i) {
+      ptx::mbar_init(bar(B::Q_FULL + i), 1);
+      ptx::mbar_init(bar(B::Q_EMPTY + i), 1);
+    }
     for (int s = 0; s < 2; ++s) {
       ptx::mbar_init(bar(B::S_FULL + s), 1);
-      ptx::mbar_init(bar(B::P_FULL + s), 4);
+      ptx::mbar_init(bar(B::P_FULL + s), 4);      // the first half of a tile's keys
+      ptx::mbar_init(bar(B::P_FULL + 2 + s), 4);  // the second
       ptx::mbar_init(bar(B::O_FULL + s), 1);
       ptx::mbar_init(bar(B::ODD_FREE + s), 8);
     }
@@ -231,7 +239,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       const int tile = sh.split ? 0 : s;
       const int rho = w.row0 + tile * tile_rows + row;       // row of the (segment, head)
       const bool mine = row < tile_rows && tile * tile_rows + row < w.rows;
-      const int pos = rho / g, hh = rho - pos * g;
+      const int pos = rho / g;
       const int end = min(w.t1, w.ctx + pos + 1);            // keys that it sees
       float m = -INFINITY, l = 0.0f;
       const int first = sh.split ? s : 0, inc = sh.split ? 2 : 1;
@@ -293,12 +301,14 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             pk[i >> 1] = pack_bf16(e.x, e.y);
           }
           ptx::tmem_st16(t_s + 16 * c, pk);
+          if (c == 3 || (c == 1 && !kWhole)) {  // half of the keys: the product may begin
+            ptx::tmem_wait_st();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + (c - 1) + s));
+          }
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        ptx::tmem_wait_st();
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + s));
       }
       if (!ok) break;
       // ---- epilogue: the row's O
@@ -336,8 +346,32 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         const float inv = 1.0f / l;
         const bool odd = s_isodd[j & 1] != 0;
         const int *so = s_odd + (j & 1) * 3 * D;
-        float *part = w.poff >= 0 ? p.partials + w.poff + (int64_t)(tile * tile_rows + row) * D : nullptr;
-        uint16_t *og = static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + pos) * p.Hq + w.h * g + hh) * D;
+        // a lane's own row goes through the warp's 2 KB in pieces of 64 bytes, so that four lanes store a row's piece together (a lane
+        // storing its row alone touches 32 lines per instruction)
+        const bool part = w.poff >= 0;
+        uint8_t *stage = smem + C::OFF_ST + warp * 2048;
+        const int warp0 = (warp & 3) * 32;                       // the warp's first row of the tile
+        const int rows = min(min(tile_rows, w.rows - tile * tile_rows) - warp0, 32);  // and how many it has
+        auto put = [&](int c, const uint32_t (&v)[4]) {
+          *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+        };
+        // this lane's share of 8 rows at a time: row 8 x + lane / 4, chunk lane % 4
+        auto get = [&](int x) -> uint4 {
+          const int r = 8 * x + (lane >> 2);
+          return *reinterpret_cast<const uint4 *>(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+        };
+        uint8_t *dst[4];  // of those rows
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int r = tile * tile_rows + warp0 + 8 * x + (lane >> 2);  // row of the item
+          if (part) {
+            dst[x] = reinterpret_cast<uint8_t *>(p.partials + w.poff + (int64_t)r * D) + (lane & 3) * 16;
+          } else {
+            const int pj = (w.row0 + r) / g, ph = w.row0 + r - pj * g;
+            dst[x] = reinterpret_cast<uint8_t *>(static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + pj) * p.Hq + w.h * g + ph) * D) +
+                     (lane & 3) * 16;
+          }
+        }
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t o[32];
@@ -360,19 +394,37 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               else if (up || down) o[i] = __float_as_uint(__uint_as_float(o[i]) + (up ? INFINITY : -INFINITY));
             }
           }
-          if (!mine) continue;
+          auto flush = [&](int at) {  // the staged pieces, to byte `at` of their rows
+            __syncwarp();
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (8 * x + (lane >> 2) < rows) {
+                if (part) __stcg(reinterpret_cast<uint4 *>(dst[x] + at), get(x));
+                else *reinterpret_cast<uint4 *>(dst[x] + at) = get(x);
+              }
+            __syncwarp();
+          };
           if (part) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              __stcg(reinterpret_cast<uint4 *>(part + c + i), make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+            for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int i = 16 * hf + 4 * e;
+                const uint32_t v[4] = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+                put(e, v);
+              }
+              flush((c + 16 * hf) * 4);
+            }
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
+            for (int e = 0; e < 4; ++e) {
               uint32_t v[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = pack_bf16(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
-              *reinterpret_cast<uint4 *>(og + c + i) = make_uint4(v[0], v[1], v[2], v[3]);
+              for (int i = 0; i < 4; ++i)
+                v[i] = pack_bf16(__uint_as_float(o[8 * e + 2 * i]) * inv, __uint_as_float(o[8 * e + 2 * i + 1]) * inv);
+              put(e, v);
             }
+            flush(c * 2);
           }
         }
         if (part && mine) {
@@ -464,7 +516,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
-      uint32_t nk = 0, nv = 0;  // tiles so far
+      uint32_t nk = 0, nv = 0, nq = 0;  // tiles and items' Q so far
       int claimed = -2;         // (lane 0) the next item, -2: not claimed yet
       auto claim = [&]() {
         if (lane == 0 && claimed == -2) {
@@ -491,18 +543,6 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(B::IT_FULL + slot));
         if (it < 0) break;
-        // Q: whole positions of the item's tiles
-        if (!wait_bar(bar(B::Q_EMPTY), (j & 1) ^ 1, s_abort)) { ok = false; break; }
-        const int tiles = w.rows > tile_rows ? 2 : 1;
-        if (ptx::elect_one()) {
-          ptx::mbar_arrive_expect_tx(bar(B::Q_FULL), (uint32_t)(tiles * C::HALVES * tile_rows * 128));
-          for (int s = 0; s < tiles; ++s)
-#pragma unroll
-            for (int hf = 0; hf < C::HALVES; ++hf)
-              ptx::tma_load_4d(sbase + C::OFF_Q + s * C::TILE + hf * C::HALF, &tmq, bar(B::Q_FULL), hf * 64, 0, w.h,
-                               w.q0 + w.row0 / g + s * (tile_rows / g));
-        }
-        __syncwarp();
         // K and V: K one tile ahead
         const int32_t *bt = p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + w.t0 / 16;
         const int nblk = (w.t1 - w.t0 + 15) / 16;
@@ -571,6 +611,21 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             next = fetch((t >> 2) + 1);
           }
           if (t < nt) ok = load(true, t, cur);
+          if (t == 0 && ok) {  // Q: whole positions of the item's tiles
+            const int qb = j % C::NQ;
+            if (!wait_bar(bar(B::Q_EMPTY + qb), ((j / C::NQ) & 1) ^ 1, s_abort)) { ok = false; break; }
+            ++nq;
+            const int tiles = w.rows > tile_rows ? 2 : 1;
+            if (ptx::elect_one()) {
+              ptx::mbar_arrive_expect_tx(bar(B::Q_FULL + qb), (uint32_t)(tiles * C::HALVES * tile_rows * 128));
+              for (int s = 0; s < tiles; ++s)
+#pragma unroll
+                for (int hf = 0; hf < C::HALVES; ++hf)
+                  ptx::tma_load_4d(sbase + C::OFF_Q + (qb * 2 + s) * C::TILE + hf * C::HALF, &tmq, bar(B::Q_FULL + qb), hf * 64, 0, w.h,
+                                   w.q0 + w.row0 / g + s * (tile_rows / g));
+            }
+            __syncwarp();
+          }
           if (t == max(nt - 2, 0)) claim();  // the next item, early enough to hide the way to it
           if (t > 0 && ok) ok = load(false, t - 1, (t & 3) == 0 && t < nt ? prev : cur);
         }
@@ -588,9 +643,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         };
         drain(KV8 ? B::KC_FULL : B::K_FULL, nk);
         drain(KV8 ? B::VC_FULL : B::V_FULL, nv);
-        if (!ok && j > 0) {  // (a Q that nobody waited for)
+        for (uint32_t k = 0; k < C::NQ && k < nq; ++k) {
           const long long t0 = clock64();
-          while (!ptx::mbar_try_wait(bar(B::Q_FULL), (j - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {
+          while (!ptx::mbar_try_wait(bar(B::Q_FULL + (nq - 1 - k) % C::NQ), ((nq - 1 - k) / C::NQ) & 1) && clock64() - t0 < kWaitCycles) {
           }
         }
       }
@@ -603,7 +658,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       WorkItem w;
       for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
         const Shape sh = shape_of(w, tile_rows, g);
-        if (!wait_bar(bar(B::Q_FULL), j & 1, s_abort)) { ok = false; break; }
+        const int qb = j % C::NQ;
+        if (!wait_bar(bar(B::Q_FULL + qb), (j / C::NQ) & 1, s_abort)) { ok = false; break; }
         auto issue_s = [&](int i) -> bool {  // step i: stream i & 1
           const int s = i & 1, t = sh.split ? i : i >> 1;
           const uint32_t n = k0 + t;
@@ -611,7 +667,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           if (!wait_bar(bar(B::K_FULL + st), (n / C::NS) & 1, s_abort)) return false;
           if (ptx::elect_one()) {
             ptx::tc_fence_after();
-            const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q + (sh.split ? 0 : s) * C::TILE, 16, 1024);
+            const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q + (qb * 2 + (sh.split ? 0 : s)) * C::TILE, 16, 1024);
             const uint64_t kd = ptx::sdesc_sw128(sbase + C::OFF_K + st * C::TILE, 16, 1024);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
@@ -620,7 +676,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             }
             ptx::umma_commit(bar(B::S_FULL + s));
             if (sh.split || s == 1) ptx::umma_commit(bar(B::K_EMPTY + st));
-            if (i == sh.steps - 1) ptx::umma_commit(bar(B::Q_EMPTY));
+            if (i == sh.steps - 1) ptx::umma_commit(bar(B::Q_EMPTY + qb));
           }
           __syncwarp();
           return true;
@@ -637,19 +693,25 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               break;
             }
           }
-          if (!wait_bar(bar(B::P_FULL + s), np[s] & 1, s_abort)) { ok = false; break; }
-          ++np[s];
-          if (ptx::elect_one()) {
-            ptx::tc_fence_after();
-            const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::HALF, 1024);
-            const bool first = sh.split ? i < 2 : t == 0;
 #pragma unroll
-            for (int ks = 0; ks < kBT / 16; ++ks)
-              ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + s * kBT + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o, !first || ks > 0);
-            if (sh.split || s == 1) ptx::umma_commit(bar(B::V_EMPTY + st));
-            if (i + 2 >= sh.steps) ptx::umma_commit(bar(B::O_FULL + s));
+          for (int half = kWhole; half < 2; ++half) {
+            if (!wait_bar(bar(B::P_FULL + 2 * half + s), np[s] & 1, s_abort)) { ok = false; break; }
+            if (ptx::elect_one()) {
+              ptx::tc_fence_after();
+              const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::HALF, 1024);
+              const bool first = sh.split ? i < 2 : t == 0;
+#pragma unroll
+              for (int ks = kWhole ? 0 : 4 * half; ks < 4 * half + 4; ++ks)
+                ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + s * kBT + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o, !first || ks > 0);
+              if (half == 1) {
+                if (sh.split || s == 1) ptx::umma_commit(bar(B::V_EMPTY + st));
+                if (i + 2 >= sh.steps) ptx::umma_commit(bar(B::O_FULL + s));
+              }
+            }
+            __syncwarp();
           }
-          __syncwarp();
+          if (!ok) break;
+          ++np[s];
           if (i + 2 < sh.steps) ok = issue_s(i + 2);
         }
         k0 += sh.nt;
