@@ -16,12 +16,11 @@
 //
 // Persistent CTAs take items from a global counter, longest first.  Warps:
 //   * 0-3, 4-7: softmax and epilogue of stream 0 and 1, a thread per row;
-//   * 8: issues tcgen05.mma.  Stream s's next S follows its P V directly, so that an S that has arrived says that the O before it
-//     is complete, and S may overwrite P;
+//   * 8, 11: issue tcgen05.mma of stream 0 and 1.  With D = 128 a stream's next S follows its P V directly, so that an S that has
+//     arrived says that the O before it is complete, and S may overwrite P; with D = 64 it comes before, as soon as S has been read;
 //   * 9: takes items, and brings Q (boxes of whole positions), K and V (boxes of one page or of eight consecutive ones) by TMA;
 //   * 10: looks at V where a tile has keys that some row does not see: 0 * NaN would reach every row.  Values that are not finite
 //     are set to zero there and remembered with the first position that sees them; the epilogue writes what they make of its rows.
-// (11: registers are allotted per four warps.)
 //   * 12-15, over an 8-bit cache: a tile's codes arrive in the upper half of its stage, or of each warp's part of it, and these warps
 //     write it in bf16, times the page's scale, in place: a lane's row of codes in registers first.
 // Every wait is bounded: an expired one records WISP_DEV_TIMEOUT and the CTA drains.
@@ -40,7 +39,7 @@ namespace {
 constexpr int kBT = 128;      // keys per tile
 constexpr int kM = 128;       // rows per stream
 constexpr int threads_of(bool kv8) { return kv8 ? 512 : 384; }
-constexpr uint32_t kTmemCols = 512;  // S (and P) of the streams at 0 and 128, O at 256 and 256 + D
+constexpr uint32_t kTmemCols = 512;  // S of the streams at 0 and 128, O at 256 and 256 + D, P: Cfg::P_COL
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
 constexpr float kLoose = 8.0f;  // how far (log2) a score may exceed its row's reference
 constexpr int kItemRing = 2;
@@ -51,6 +50,10 @@ struct Cfg {
   static constexpr int HALF = kBT * 128;          // a 64-wide half of a tile: [128][128 B], swizzled
   static constexpr int TILE = HALVES * HALF;
   static constexpr int NS = D == 128 ? 2 : 4;     // stages of K, and of V
+  // P: over S with D = 128, where S and O fill the TMEM; with D = 64 in columns of its own, and S of the next tile may be computed as soon
+  // as S has been read, beside the softmax (P over S there: 280 us for 48 prompts of up to 1500 tokens)
+  static constexpr bool P_APART = D == 64;
+  static constexpr int P_COL = P_APART ? 384 : 0, P_STEP = P_APART ? 64 : kBT;
   static constexpr int NQ = D == 128 ? 1 : 2;     // buffers of an item's two tiles of Q
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = NQ * 2 * TILE;
@@ -71,12 +74,13 @@ struct Bars {
   using C = Cfg<D>;
   static constexpr int K_FULL = 0, K_EMPTY = C::NS, V_FULL = 2 * C::NS, V_EMPTY = 3 * C::NS;
   static constexpr int Q_FULL = 4 * C::NS, Q_EMPTY = Q_FULL + 2;  // [NQ]
-  static constexpr int S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, O_FULL = P_FULL + 4;  // [2] per stream
+  static constexpr int S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, O_FULL = P_FULL + 4;  // [2] per stream; P_APART: O_FULL after each P V
   static constexpr int IT_FULL = O_FULL + 2, IT_EMPTY = IT_FULL + kItemRing;
   static constexpr int V_CLEAN = IT_EMPTY + kItemRing;   // [NS] the tile's V has been looked at
   static constexpr int ODD_FREE = V_CLEAN + C::NS;           // [2] per buffer of odd values: its item's epilogues are done
   static constexpr int ML_FULL = ODD_FREE + 2, ML_EMPTY = ML_FULL + 1;  // stream 1's m and l (and O): published, read
-  static constexpr int MMA_DONE = ML_EMPTY + 1, FIN = MMA_DONE + 1;
+  static constexpr int S_EMPTY = ML_EMPTY + 1;   // [2] S has been read (P_APART)
+  static constexpr int MMA_DONE = S_EMPTY + 2, FIN = MMA_DONE + 1;
   static constexpr int KC_FULL = FIN + 1, VC_FULL = KC_FULL + C::NS;  // [NS] codes have arrived (8-bit cache)
   static_assert(VC_FULL + C::NS <= C::N_BAR, "barrier count");
 };
@@ -105,15 +109,13 @@ __device__ __forceinline__ uint32_t bf16x2_sat(float a, float b) {
 struct Shape {
   int nt;        // key tiles
   bool split;    // one tile of rows: its streams take the key tiles in turn
-  int steps;     // S, softmax, P V, over both streams
   int plain;     // key tiles from the first on that every row of the item sees entirely
 };
-__device__ __forceinline__ Shape shape_of(const WorkItem &w, int tile_rows, int g) {
+__device__ __forceinline__ Shape shape_of(const WorkItem &w, int tile_rows, int tile_pos) {
   Shape s;
   s.nt = (w.t1 - w.t0 + kBT - 1) / kBT;
   s.split = w.rows <= tile_rows;
-  s.steps = s.split ? s.nt : 2 * s.nt;
-  const int all = min(w.t1, w.ctx + w.row0 / g + 1);  // keys that the first row sees
+  const int all = min(w.t1, w.ctx + 2 * w.rg * tile_pos + 1);  // keys that the first row sees
   s.plain = max(all - w.t0, 0) / kBT;
   return s;
 }
@@ -153,31 +155,32 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NS; ++i) {
       ptx::mbar_init(bar(B::K_FULL + i), KV8 ? 4 : 1);
-      ptx::mbar_init(bar(B::K_EMPTY + i), 1);
+      ptx::mbar_init(bar(B::K_EMPTY + i), 2);  // both streams' issuers
       ptx::mbar_init(bar(B::V_FULL + i), KV8 ? 4 : 1);
       ptx::mbar_init(bar(B::KC_FULL + i), 1);
       ptx::mbar_init(bar(B::VC_FULL + i), 1);
-      ptx::mbar_init(bar(B::V_EMPTY + i), 1);
+      ptx::mbar_init(bar(B::V_EMPTY + i), 2);
       ptx::mbar_init(bar(B::V_CLEAN + i), 1);
     }
     for (int i = 0; i < C::NQ; ++i) {
       ptx::mbar_init(bar(B::Q_FULL + i), 1);
-      ptx::mbar_init(bar(B::Q_EMPTY + i), 1);
+      ptx::mbar_init(bar(B::Q_EMPTY + i), 2);
     }
     for (int s = 0; s < 2; ++s) {
       ptx::mbar_init(bar(B::S_FULL + s), 1);
       ptx::mbar_init(bar(B::P_FULL + s), 4);      // the first half of a tile's keys
       ptx::mbar_init(bar(B::P_FULL + 2 + s), 4);  // the second
       ptx::mbar_init(bar(B::O_FULL + s), 1);
+      ptx::mbar_init(bar(B::S_EMPTY + s), 4);
       ptx::mbar_init(bar(B::ODD_FREE + s), 8);
     }
     for (int i = 0; i < kItemRing; ++i) {
       ptx::mbar_init(bar(B::IT_FULL + i), 1);
-      ptx::mbar_init(bar(B::IT_EMPTY + i), 8 + 1 + 1 + (KV8 ? 4 : 0));  // softmax warps, MMA issuer, the one that looks at V, decoders
+      ptx::mbar_init(bar(B::IT_EMPTY + i), 8 + 2 + 1 + (KV8 ? 4 : 0));  // softmax warps, MMA issuers, the one that looks at V, decoders
     }
     ptx::mbar_init(bar(B::ML_FULL), 4);
     ptx::mbar_init(bar(B::ML_EMPTY), 4);
-    ptx::mbar_init(bar(B::MMA_DONE), 1);
+    ptx::mbar_init(bar(B::MMA_DONE), 2);
     ptx::mbar_init(bar(B::FIN), kThreads / 32);
     *s_abort = 0;
     s_isodd[0] = s_isodd[1] = 0;
@@ -204,7 +207,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int n_items = p.header->n_items;
   const int g = p.Hq / p.Hkv;
-  const int tile_rows = kM / g * g;  // rows of a tile: whole positions
+  const int tile_pos = kM / g, tile_rows = tile_pos * g;  // positions and rows of a tile
 
   // takes the next item from the ring: false at the end
   auto next_item = [&](uint32_t j, WorkItem &w, bool &ok) -> bool {
@@ -219,27 +222,35 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 
   bool ok = true;
   if (warp < 8) {
-    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 208 + 4 x 88; 16 with 128, 2048 = 8 x 192 + 8 x 64.
+    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 200 + 4 x 104; 16 with 128, 2048 = 8 x 184 + 8 x 72.
     // (Each split stands at the head of its own branch: after a join the compiler counts with the least.)
     if constexpr (KV8)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     else
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ------------------------------------------------------------------ softmax and epilogue, stream s, a row per thread
     const int s = warp >> 2;
     const int row = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + s * kBT, t_o = tmem + lanes + 2 * kBT + s * D;
+    const uint32_t t_s = tmem + lanes + s * kBT, t_o = tmem + lanes + 2 * kBT + s * D, t_p = tmem + lanes + C::P_COL + s * C::P_STEP;
+    const int pos0 = row / g;  // of this row within its tile
+    // the epilogue: this lane's rows of the warp (8 x + lane / 4), as offsets from the tile's first row of the output
+    const int warp0 = (warp & 3) * 32;
+    int row_at[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int r = warp0 + 8 * x + (lane >> 2);
+      row_at[x] = (r / g * p.Hq + r % g) * D;
+    }
     const float scale = 1.4426950408889634f / sqrtf((float)D);
     const float2 scale2 = make_float2(scale, scale);
     uint32_t ns = 0, nml = 0, nof = 0;  // this stream's S tiles, joins and finished O so far
     WorkItem w;
     for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
-      const Shape sh = shape_of(w, tile_rows, g);
+      const Shape sh = shape_of(w, tile_rows, tile_pos);
       const int tile = sh.split ? 0 : s;
-      const int rho = w.row0 + tile * tile_rows + row;       // row of the (segment, head)
       const bool mine = row < tile_rows && tile * tile_rows + row < w.rows;
-      const int pos = rho / g;
+      const int pos = (2 * w.rg + tile) * tile_pos + pos0;
       const int end = min(w.t1, w.ctx + pos + 1);            // keys that it sees
       float m = -INFINITY, l = 0.0f;
       const int first = sh.split ? s : 0, inc = sh.split ? 2 : 1;
@@ -251,6 +262,11 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) ptx::tmem_ld32(t_s + 32 * c, x[c]);
         ptx::tmem_wait_ld();
+        if (C::P_APART) {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(B::S_EMPTY + s));
+        }
         if (t >= sh.plain) {
           const int seen = end - (w.t0 + t * kBT);
 #pragma unroll
@@ -270,9 +286,14 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         if (t == first) {
           m = top;
         } else {
+          if (C::P_APART) {  // the P V before: its P is written over, its O may be rescaled
+            if (!wait_bar(bar(B::O_FULL + s), nof & 1, s_abort)) { ok = false; break; }
+            ++nof;
+            ptx::tc_fence_after();
+          }
           const bool move = mine && top > m + kLoose;
           if (__any_sync(0xffffffffu, move)) {
-            // (the O before this S is complete: see the issuer)
+            // (the O before this S is complete)
             const float a = move ? ptx::ex2(m - top) : 1.0f;
             if (move) m = top;
             l *= a;
@@ -300,7 +321,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             sum[(i >> 1) & 1] = __fadd2_rn(sum[(i >> 1) & 1], e);
             pk[i >> 1] = pack_bf16(e.x, e.y);
           }
-          ptx::tmem_st16(t_s + 16 * c, pk);
+          ptx::tmem_st16(t_p + 16 * c, pk);
           if (c == 3 || (c == 1 && !kWhole)) {  // half of the keys: the product may begin
             ptx::tmem_wait_st();
             ptx::tc_fence_before();
@@ -350,7 +371,6 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         // storing its row alone touches 32 lines per instruction)
         const bool part = w.poff >= 0;
         uint8_t *stage = smem + C::OFF_ST + warp * 2048;
-        const int warp0 = (warp & 3) * 32;                       // the warp's first row of the tile
         const int rows = min(min(tile_rows, w.rows - tile * tile_rows) - warp0, 32);  // and how many it has
         auto put = [&](int c, const uint32_t (&v)[4]) {
           *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -361,17 +381,11 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           return *reinterpret_cast<const uint4 *>(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
         };
         uint8_t *dst[4];  // of those rows
+        uint16_t *out0 = static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + (2 * w.rg + tile) * tile_pos) * p.Hq + w.h * g) * D;
+        float *part0 = p.partials + w.poff + (int64_t)(tile * tile_rows + warp0 + (lane >> 2)) * D;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int r = tile * tile_rows + warp0 + 8 * x + (lane >> 2);  // row of the item
-          if (part) {
-            dst[x] = reinterpret_cast<uint8_t *>(p.partials + w.poff + (int64_t)r * D) + (lane & 3) * 16;
-          } else {
-            const int pj = (w.row0 + r) / g, ph = w.row0 + r - pj * g;
-            dst[x] = reinterpret_cast<uint8_t *>(static_cast<uint16_t *>(p.out) + ((int64_t)(w.q0 + pj) * p.Hq + w.h * g + ph) * D) +
-                     (lane & 3) * 16;
-          }
-        }
+        for (int x = 0; x < 4; ++x)
+          dst[x] = (part ? reinterpret_cast<uint8_t *>(part0 + 8 * x * D) : reinterpret_cast<uint8_t *>(out0 + row_at[x])) + (lane & 3) * 16;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t o[32];
@@ -440,7 +454,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
     }
   } else if (KV8 && warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // ------------------------------------------------------------------ codes to bf16
     const int row = (warp - 12) * 32 + lane;
     constexpr int CH = D / 16;  // 16-byte chunks of a row of codes
@@ -511,9 +525,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
     }
   } else {
     if constexpr (KV8)
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
       uint32_t nk = 0, nv = 0, nq = 0;  // tiles and items' Q so far
@@ -622,7 +636,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 #pragma unroll
                 for (int hf = 0; hf < C::HALVES; ++hf)
                   ptx::tma_load_4d(sbase + C::OFF_Q + (qb * 2 + s) * C::TILE + hf * C::HALF, &tmq, bar(B::Q_FULL + qb), hf * 64, 0, w.h,
-                                   w.q0 + w.row0 / g + s * (tile_rows / g));
+                                   w.q0 + (2 * w.rg + s) * tile_pos);
             }
             __syncwarp();
           }
@@ -649,19 +663,33 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           }
         }
       }
-    } else if (warp == 8) {
-      // ------------------------------------------------------------------ MMA issuer
+    } else if (warp != 10) {
+      // ------------------------------------------------------------------ MMA issuers, one per stream
+      // (An MMA takes its issuer about 50 cycles and a commit 100, whatever it computes: one thread for both streams bounded the tile.)
+      const int s = warp == 8 ? 0 : 1;
       const uint32_t idesc_s = ptx::idesc_bf16_f32(kM, kBT, false, false);
       const uint32_t idesc_o = ptx::idesc_bf16_f32(kM, D, false, true);
       uint32_t k0 = 0;               // key tiles of the items before
-      uint32_t np[2] = {0, 0};       // P tiles so far, per stream
+      uint32_t np = 0, ne = 0;       // P tiles and S tiles read so far
       WorkItem w;
       for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
-        const Shape sh = shape_of(w, tile_rows, g);
+        const Shape sh = shape_of(w, tile_rows, tile_pos);
+        const int first = sh.split ? s : 0, inc = sh.split ? 2 : 1;
         const int qb = j % C::NQ;
         if (!wait_bar(bar(B::Q_FULL + qb), (j / C::NQ) & 1, s_abort)) { ok = false; break; }
-        auto issue_s = [&](int i) -> bool {  // step i: stream i & 1
-          const int s = i & 1, t = sh.split ? i : i >> 1;
+        // tiles of the other stream's alone: let go
+        int kt = 0, vt = 0;
+        auto skip = [&](int full, int empty, int &t, int to) -> bool {
+          for (; t < to; ++t) {
+            const int st = (k0 + t) % C::NS;
+            if (!wait_bar(bar(full + st), ((k0 + t) / C::NS) & 1, s_abort)) return false;
+            if (lane == 0) ptx::mbar_arrive(bar(empty + st));
+          }
+          return true;
+        };
+        auto issue_s = [&](int t) -> bool {
+          if (!skip(B::K_FULL, B::K_EMPTY, kt, t)) return false;
+          kt = t + 1;
           const uint32_t n = k0 + t;
           const int st = n % C::NS;
           if (!wait_bar(bar(B::K_FULL + st), (n / C::NS) & 1, s_abort)) return false;
@@ -675,45 +703,54 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               ptx::umma_f16(tmem + s * kBT, qd + off, kd + off, idesc_s, ks > 0);
             }
             ptx::umma_commit(bar(B::S_FULL + s));
-            if (sh.split || s == 1) ptx::umma_commit(bar(B::K_EMPTY + st));
-            if (i == sh.steps - 1) ptx::umma_commit(bar(B::Q_EMPTY + qb));
+            ptx::umma_commit(bar(B::K_EMPTY + st));
+            if (t + inc >= sh.nt) ptx::umma_commit(bar(B::Q_EMPTY + qb));
           }
           __syncwarp();
           return true;
         };
-        ok = issue_s(0) && (sh.steps < 2 || issue_s(1));
-        for (int i = 0; i < sh.steps && ok; ++i) {
-          const int s = i & 1, t = sh.split ? i : i >> 1;
+        if (first < sh.nt) {
+          ok = issue_s(first);
+        } else if (lane == 0) {
+          ptx::mbar_arrive(bar(B::Q_EMPTY + qb));
+        }
+        for (int t = first; t < sh.nt && ok; t += inc) {
+          if (C::P_APART && t + inc < sh.nt) {
+            if (!wait_bar(bar(B::S_EMPTY + s), ne & 1, s_abort)) { ok = false; break; }
+            if (!(ok = issue_s(t + inc))) break;
+          }
+          ++ne;
+          if (!(ok = skip(B::V_FULL, B::V_EMPTY, vt, t))) break;
+          vt = t + 1;
           const uint32_t n = k0 + t;
           const int st = n % C::NS;
-          if ((sh.split || s == 0)) {
-            if (!wait_bar(bar(B::V_FULL + st), (n / C::NS) & 1, s_abort) ||
-                !wait_bar(bar(B::V_CLEAN + st), (n / C::NS) & 1, s_abort)) {
-              ok = false;
-              break;
-            }
+          if (!wait_bar(bar(B::V_FULL + st), (n / C::NS) & 1, s_abort) ||
+              !wait_bar(bar(B::V_CLEAN + st), (n / C::NS) & 1, s_abort)) {
+            ok = false;
+            break;
           }
 #pragma unroll
           for (int half = kWhole; half < 2; ++half) {
-            if (!wait_bar(bar(B::P_FULL + 2 * half + s), np[s] & 1, s_abort)) { ok = false; break; }
+            if (!wait_bar(bar(B::P_FULL + 2 * half + s), np & 1, s_abort)) { ok = false; break; }
             if (ptx::elect_one()) {
               ptx::tc_fence_after();
               const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::HALF, 1024);
-              const bool first = sh.split ? i < 2 : t == 0;
 #pragma unroll
               for (int ks = kWhole ? 0 : 4 * half; ks < 4 * half + 4; ++ks)
-                ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + s * kBT + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o, !first || ks > 0);
+                ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + C::P_COL + s * C::P_STEP + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o,
+                                 t != first || ks > 0);
               if (half == 1) {
-                if (sh.split || s == 1) ptx::umma_commit(bar(B::V_EMPTY + st));
-                if (i + 2 >= sh.steps) ptx::umma_commit(bar(B::O_FULL + s));
+                if (C::P_APART || t + inc >= sh.nt) ptx::umma_commit(bar(B::O_FULL + s));
+                ptx::umma_commit(bar(B::V_EMPTY + st));
               }
             }
             __syncwarp();
           }
           if (!ok) break;
-          ++np[s];
-          if (i + 2 < sh.steps) ok = issue_s(i + 2);
+          ++np;
+          if (!C::P_APART && t + inc < sh.nt) ok = issue_s(t + inc);
         }
+        if (ok) ok = skip(B::K_FULL, B::K_EMPTY, kt, sh.nt) && skip(B::V_FULL, B::V_EMPTY, vt, sh.nt);
         k0 += sh.nt;
       }
       if (ptx::elect_one()) {
@@ -728,7 +765,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       uint32_t k0 = 0;
       WorkItem w;
       for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
-        const Shape sh = shape_of(w, tile_rows, g);
+        const Shape sh = shape_of(w, tile_rows, tile_pos);
         const int ob = j & 1;
         // this item's buffer of odd values: free, and cleared where it was used
         if (!wait_bar(bar(B::ODD_FREE + ob), ((j >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
