@@ -23,6 +23,16 @@ struct AttnParams {
                        // by the planner; null (prompt.cuh): another kernel joins the partials
 };
 
+// Item `it` of the list.  Where the list stands for all KV heads (prompt.cuh) an entry's nrg is the distance of its heads' partials.
+__device__ __forceinline__ WorkItem item_at(const AttnParams &p, int it) {
+  if (p.pair_done) return p.items[it];
+  const int row = it / p.Hkv;
+  WorkItem w = p.items[row];
+  w.h = it - row * p.Hkv;
+  if (w.poff >= 0) w.poff += w.h * w.nrg;
+  return w;
+}
+
 // Host launchers (defined next to their kernels): programmatic dependents of the planner, which they wait for
 // before they read the plan.
 // CUDA-core kernel for fp32 queries, over fp32 or (with scales) e4m3 KV, D in {64, 128}; `grid` persistent CTAs

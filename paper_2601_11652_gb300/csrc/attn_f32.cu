@@ -356,13 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
       do {
         it = atomicAdd(&p.header_mut->next_item, 1);
         if (it >= n_items) it = -1;
-      } while (it >= 0 && p.items[it].t1 <= p.items[it].t0);  // (a refused request's items are empty)
+      } while (it >= 0 && p.pair_done && p.items[it].t1 <= p.items[it].t0);  // (a refused request's items are empty)
       sh.item = it;
     }
     __syncthreads();  // (also: the previous item's shared memory is no longer read)
     const int it = sh.item;
     if (it < 0 || *(volatile int *)&sh.abort_) break;
-    const WorkItem w = p.items[it];
+    const WorkItem w = item_at(p, it);
     // the item's query rows (rows past `rows` up to the lanes' share read as zero)
     const int rl = (w.rows + 3) / 4;
     const float *qg = static_cast<const float *>(p.q);

@@ -4,7 +4,8 @@
 // The work is cut into segments: rows of one KV head that see the same keys but for the causal end.  Request r is segment r, its
 // query rows over its own keys [P_r, c_r + k_r + 1), where P_r is its run's shared prefix or 0; run i of requests that share
 // pages is segment B + i, all its rows over keys [0, P).  A segment's rows are cut into units of `unit_rows`, its keys into chunks
-// of the plan's chunk length; an item (plan.cuh) is a chunk of a unit of one KV head.  Where a row has its keys in more than one item
+// of its chunk length; an item (plan.cuh) is a chunk of a unit of one KV head.  The list holds them without the head: entry i / Hkv and head
+// i mod Hkv make item i (item_at, attn.cuh).  Where a row has its keys in more than one item
 // the items leave partials (O, m, l), and merge_kernel joins them.
 #pragma once
 
@@ -21,8 +22,8 @@ struct Segment {  // 48 bytes
   int32_t units, chunks;
   int32_t pbase;    // first partial (floats), -1: the segment has none, its items write outputs
   int32_t part_h;   // floats of one KV head's partials
-  int32_t first;    // first item (empty ones included)
-  int32_t pad;
+  int32_t first;    // first list entry (empty ones included)
+  int32_t chunk;    // keys per chunk
 };
 static_assert(sizeof(Segment) == 48, "segment layout");
 
@@ -30,15 +31,14 @@ struct PromptHeader {
   PlanHeader h;        // what the attention kernels read
   int32_t partials;    // 1: merge_kernel has work
   int32_t n_runs;
-  int32_t chunk;
-  int32_t pad[5];
+  int32_t pad[6];
 };
 
 struct PromptPlan {
   int B, Hq, Hkv, D, max_blocks_per_seq, total_q_rows;
   int unit_rows;       // rows of a unit: whole positions of the tensor-core kernel's two tiles, or the fp32 kernel's row limit
   int sms;
-  int64_t max_items, partial_cap;
+  int64_t max_rows, partial_cap;  // list entries, floats
   const int32_t *draft_lens, *context_lens, *shared_ids, *shared_pages;  // shared_*: null without runs
   const int64_t *request_ids;
   DeviceStatus *status;
@@ -57,6 +57,7 @@ struct PromptPlan {
 // Rows of a segment that share a partial's slot, and floats of a slot.
 __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D + 2) + 3) / 4 * 4; }
 
+cudaError_t prompt_plan_setup();  // once per device: shared-memory attributes
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s);
 cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s);
 

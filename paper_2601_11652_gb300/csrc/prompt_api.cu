@@ -21,7 +21,7 @@ wisp_status setup(int *sms) {
   if (!g_sms[dev]) {
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return WISP_ERR_CUDA;
-    if (attn_f32_setup() != cudaSuccess || prompt_tc_setup() != cudaSuccess) return WISP_ERR_CUDA;
+    if (attn_f32_setup() != cudaSuccess || prompt_tc_setup() != cudaSuccess || prompt_plan_setup() != cudaSuccess) return WISP_ERR_CUDA;
     g_sms[dev] = n;
   }
   *sms = g_sms[dev];
@@ -57,23 +57,23 @@ wisp_status check(const wisp_shared_args *x) {
 
 struct Space {
   size_t status, header, q_row_start, req_flag, req_run, run_info, segs, items, partials, total;
-  int64_t max_items, partial_cap;
+  int64_t max_rows, partial_cap;
   int unit_rows;
   bool fits;
 };
 
-// Rows of a unit, and bounds on items and partials.  Without cuts a request has ceil(rows / unit_rows) units per KV head, a run as
-// many for its rows again, and both leave one partial per row.  Cuts add items and partials of whole units: what the planner's rule
-// makes of them stays below these bounds (several per SM), and where it would not, it makes none.
+// Rows of a unit, and bounds on list entries and partials.  Without cuts a request has ceil(rows / unit_rows) units, a run as many for its
+// rows again, and both leave one partial per row and head.  Cuts add entries and partials of whole units: by the planner's rule a few
+// items per SM; where they would not fit (a causal prompt's last units are twice as long as the average), it makes none.
 Space space(const wisp_attn_args *a, bool shared, int sms) {
   Space s;
   const int g = a->Hq / a->Hkv;
   s.unit_rows = a->qkv_dtype == WISP_BF16 ? 2 * g * prompt_tile_positions(g) : kF32RowsPerItem;
   const int64_t units = ((int64_t)a->total_q_rows * g / s.unit_rows + a->B) * (shared ? 2 : 1);
   const int64_t slot = (int64_t)s.unit_rows * (a->D + 2) + 4;
-  const int64_t cuts = (int64_t)(a->qkv_dtype == WISP_BF16 ? 6 : 24) * sms;
-  s.max_items = units * a->Hkv + 4 * cuts;
-  s.partial_cap = cuts * slot + (shared ? 2 * (int64_t)a->total_q_rows * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
+  const int64_t cuts = (int64_t)(shared ? 12 : 6) * (a->qkv_dtype == WISP_BF16 ? 1 : 4) * sms / a->Hkv + 8;
+  s.max_rows = units + cuts;
+  s.partial_cap = cuts * a->Hkv * slot + (shared ? 2 * (int64_t)a->total_q_rows * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -88,10 +88,10 @@ Space space(const wisp_attn_args *a, bool shared, int sms) {
   s.req_run = take(4 * B);
   s.run_info = take(16 * B);
   s.segs = take(sizeof(Segment) * 2 * B);
-  s.items = take(sizeof(WorkItem) * (size_t)s.max_items);
+  s.items = take(sizeof(WorkItem) * (size_t)s.max_rows);
   s.partials = take(4 * (size_t)s.partial_cap);
   s.total = off;
-  s.fits = s.max_items < INT32_MAX / 2 && s.partial_cap < INT32_MAX;
+  s.fits = s.max_rows * a->Hkv < INT32_MAX / 2 && s.partial_cap < INT32_MAX;
   return s;
 }
 
@@ -127,7 +127,7 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   p.total_q_rows = a->total_q_rows;
   p.unit_rows = sp.unit_rows;
   p.sms = sms;
-  p.max_items = sp.max_items;
+  p.max_rows = sp.max_rows;
   p.partial_cap = sp.partial_cap;
   p.draft_lens = a->draft_lens;
   p.context_lens = a->context_lens;
@@ -169,7 +169,7 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   ap.header_mut = &p.header->h;
   ap.items = p.items;
   ap.partials = p.partials;  // (pair_done stays null: the merge kernel joins them)
-  const int grid = (int)(sp.max_items < sms ? sp.max_items : sms);
+  const int grid = (int)(sp.max_rows * a->Hkv < sms ? sp.max_rows * a->Hkv : sms);
   cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : attn_f32_launch(ap, grid, s);
   if (e == cudaSuccess) e = prompt_merge_launch(p, !bf, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;

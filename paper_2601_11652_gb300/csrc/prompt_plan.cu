@@ -5,6 +5,7 @@
 #include "attn_merge.cuh"
 #include "prompt.cuh"
 
+#include <algorithm>
 #include <cstring>
 
 namespace wisp {
@@ -15,6 +16,7 @@ constexpr int kThreads = 1024;
 constexpr int kPage = 16;
 constexpr int kBuckets = 1024;     // of the dispatch order, by key tiles of 64
 constexpr int kMinKeys = 256;      // chunks are not shorter
+constexpr int kMinRunKeys = 1024;  // ... nor those of a run's rows, where there are many units
 constexpr int kTile = 128;         // and are whole key tiles
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys
 constexpr int kMaxRows = 1 << 24;  // k_r limit
@@ -44,6 +46,13 @@ __device__ T scan_incl(T v, T *s_w, T *total) {
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// Every thread's v added to *sum in shared memory (one atomic per warp: they are a loop each).
+__device__ __forceinline__ void add_warp(unsigned long long *sum, int64_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0 && v) atomicAdd(sum, (unsigned long long)v);
+}
+
 // Keys of a unit: those that its last row sees.
 __device__ __forceinline__ int unit_end(const Segment &s, int u, int unit_rows, int g) {
   const int last = min((u + 1) * unit_rows, s.npos * g) - 1;
@@ -52,11 +61,22 @@ __device__ __forceinline__ int unit_end(const Segment &s, int u, int unit_rows, 
 
 }  // namespace
 
+// What the planner keeps in shared memory where all segments fit: run_info and the segments.
+struct PlanShared {
+  int32_t run[4 * kThreads];
+  Segment segs[kThreads];
+};
+
+// One CTA, bound by latency: global loads of the lengths, then barriers.  With at most kThreads requests and segments nothing else goes
+// through global memory, and a list entry stands for all KV heads (an item is an entry and a head), so that most batches have at
+// most one per thread.  48 prompts of up to 1500 tokens, 590 entries: PLAN_US us.
 __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPlan p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  PlanShared &sh = *reinterpret_cast<PlanShared *>(plan_smem);
   __shared__ int64_t s_scan[2][32];
   __shared__ int s_iscan[4][32];
-  __shared__ unsigned long long s_keys, s_units, s_items, s_floats;
+  __shared__ unsigned long long s_keys, s_units, s_rows, s_floats;
   __shared__ int s_hist[kBuckets];
   __shared__ int s_first[kThreads + 1];
   __shared__ int s_any;
@@ -72,11 +92,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   s_hist[tid] = 0;
   static_assert(kBuckets == kThreads, "one bucket per thread");
   const int64_t cap_tokens = (int64_t)p.max_blocks_per_seq * kPage;
-  int32_t *run_start = p.run_info, *run_end = p.run_info + p.B, *run_first = p.run_info + 2 * p.B, *run_valid = p.run_info + 3 * p.B;
+  const bool one = p.B <= kThreads;  // every request has a thread
+  const int RS = one ? kThreads : p.B;
+  int32_t *run_start = one ? sh.run : p.run_info;
+  int32_t *run_end = run_start + RS, *run_first = run_start + 2 * RS, *run_valid = run_start + 3 * RS;
 
   // pass 1: offsets, validation, runs
   int64_t carry_k = 0;
   int n_runs = 0;
+  int my_k = 0, my_ctx = 0, my_pages = 0, my_q0 = 0, my_run = -1;  // (of the last chunk: the only one where `one`)
+  bool my_ok = false;
   for (int base = 0; base < p.B; base += kThreads) {
     const int r = base + tid;
     int64_t k = 0;
@@ -84,14 +109,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     bool start = false, last = false;
     if (r < p.B) {
       k = p.draft_lens[r];
+      my_k = (int)k;
       const int64_t c = p.context_lens[r];
+      my_ctx = (int)c;
       if (p.shared_ids) {
         id = p.shared_ids[r];
         pages = p.shared_pages[r];
       }
       const bool in = id >= 0 && pages > 0;
-      start = in && (r == 0 || p.shared_ids[r - 1] != id || p.shared_pages[r - 1] != pages);
-      last = in && (r == p.B - 1 || p.shared_ids[r + 1] != id || p.shared_pages[r + 1] != pages);
+      if (in) {
+        start = r == 0 || p.shared_ids[r - 1] != id || p.shared_pages[r - 1] != pages;
+        last = r == p.B - 1 || p.shared_ids[r + 1] != id || p.shared_pages[r + 1] != pages;
+      }
       if (k < 0) { bad = WISP_DEV_BAD_LENGTH; k = 0; }
       if (!bad && k >= kMaxRows) bad = WISP_DEV_UNSUPPORTED;
       if (!bad && (c < 0 || c + k + 1 > cap_tokens || (in && (int64_t)pages * kPage > c))) bad = WISP_DEV_BAD_LENGTH;
@@ -102,9 +131,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     const int run = n_runs + (p.shared_ids ? scan_incl<int>(start, s_iscan[base / kThreads % 2], &starts) : 0) - 1;
     if (r < p.B) {
       if (!bad && q0 + k + 1 > p.total_q_rows) bad = WISP_DEV_BAD_LENGTH;  // rows outside the caller's buffers
-      p.q_row_start[r] = (int32_t)min(q0, (int64_t)INT32_MAX);
+      my_q0 = (int32_t)min(q0, (int64_t)INT32_MAX);
+      my_ok = !bad;
+      my_pages = pages;
+      my_run = id >= 0 && pages > 0 ? run : -1;
+      p.q_row_start[r] = my_q0;
       p.req_flag[r] = bad ? REQ_BAD : REQ_OK;
-      p.req_run[r] = id >= 0 && pages > 0 ? run : -1;
+      p.req_run[r] = my_run;
       if (bad) report(p.status, bad, p.request_ids, r);
       if (start) {
         run_start[run] = r;
@@ -113,10 +146,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       }
       if (last) run_end[run] = r + 1;
     }
-    __syncthreads();
-    if (r < p.B && !bad && id >= 0 && pages > 0) {
-      atomicMin(&run_first[run], r);
-      atomicAdd(&run_valid[run], 1);
+    if (p.shared_ids) {
+      __syncthreads();
+      // a warp's members of a run together
+      const int key = r < p.B && !bad ? my_run : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, key);
+      if (key >= 0 && (tid & 31) == __ffs(same) - 1) {
+        atomicMin(&run_first[run], r);
+        atomicAdd(&run_valid[run], __popc(same));
+      }
     }
     carry_k += block_k;
     n_runs += starts;
@@ -129,20 +167,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 
   // pass 2: segments, their units, and how many keys all units have
   const int n_segs = p.B + n_runs;
+  const bool few = n_segs <= kThreads;
+  Segment *segs = few ? sh.segs : p.segs;
+  int64_t sum_keys = 0, sum_units = 0;  // of this thread
   for (int i = tid; i < n_segs; i += kThreads) {
     Segment s;
     memset(&s, 0, sizeof s);
     s.pbase = -1;
     if (i < p.B) {
-      const int run = p.req_run[i];
+      const int run = one ? my_run : p.req_run[i];
       const bool shared = run >= 0 && run_valid[run] > 1;
       if (run >= 0 && !shared) p.req_run[i] = -1;
       s.r = i;
-      if (p.req_flag[i] == REQ_OK) {
-        s.q0 = p.q_row_start[i];
-        s.npos = p.draft_lens[i] + 1;
-        s.ctx = p.context_lens[i];
-        s.t0 = shared ? p.shared_pages[i] * kPage : 0;
+      if (one ? my_ok : p.req_flag[i] == REQ_OK) {
+        s.q0 = one ? my_q0 : p.q_row_start[i];
+        s.npos = (one ? my_k : p.draft_lens[i]) + 1;
+        s.ctx = one ? my_ctx : p.context_lens[i];
+        s.t0 = shared ? (one ? my_pages : p.shared_pages[i]) * kPage : 0;
         s.t1 = s.ctx + s.npos;
         if (shared) s.pbase = 0;
       }
@@ -158,53 +199,63 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     if (s.npos > 0) {
       s.units = (int)(((int64_t)s.npos * g + R - 1) / R);
       const int64_t len = ((int64_t)(unit_end(s, 0, R, g) - s.t0) + (s.t1 - s.t0) + 1) / 2;
-      atomicAdd(&s_keys, (unsigned long long)(len * s.units));
-      atomicAdd(&s_units, (unsigned long long)s.units);
+      sum_keys += len * s.units;
+      sum_units += s.units;
       if (s.pbase == 0) s_any = 1;
     }
-    p.segs[i] = s;
+    segs[i] = s;
   }
+  add_warp(&s_keys, sum_keys);
+  add_warp(&s_units, sum_units);
   __syncthreads();
 
   // the chunk length: with at least as many units as SMs, only sequences longer than 5/4 of the average work per SM are cut (a
-  // longest-first order balances the rest, and a cut costs a merge); with fewer, about two items per SM
+  // longest-first order balances the rest, and a cut costs a merge); with fewer, about two items per SM.  The rows of a run are merged
+  // anyway, and a unit of theirs is as long as the prefix: it is cut to an eighth of an SM's work.
   const int64_t keys = (int64_t)s_keys * p.Hkv;
   const bool many = (int64_t)s_units * p.Hkv >= p.sms;
-  int64_t want = many ? (keys + p.sms - 1) / p.sms * 5 / 4 : (keys + 2 * p.sms - 1) / (2 * p.sms);
-  want = (want < kMinKeys ? kMinKeys : want + kTile - 1) / kTile * kTile;
-  int chunk = (int)min(want, (int64_t)kAllKeys);
+  auto rounded = [&](int64_t n, int least) { return (int)min((n < least ? least : n + kTile - 1) / kTile * kTile, (int64_t)kAllKeys); };
+  int chunk = rounded(many ? (keys + p.sms - 1) / p.sms * 5 / 4 : (keys + 2 * p.sms - 1) / (2 * p.sms), kMinKeys);
+  int run_chunk = min(chunk, rounded(keys / p.sms / 8, kMinRunKeys));
+  auto chunks_of = [&](const Segment &s) {
+    const int c = s.ctx == kAllKeys ? run_chunk : chunk;
+    return (s.t1 - s.t0 + c - 1) / c;
+  };
   for (;;) {  // (twice at most: without cuts everything fits, by the host's bounds)
-    if (tid == 0) s_items = s_floats = 0;
+    if (tid == 0) s_rows = s_floats = 0;
     __syncthreads();
+    int64_t sum_rows = 0, sum_floats = 0;
     for (int i = tid; i < n_segs; i += kThreads) {
-      const Segment s = p.segs[i];
+      const Segment s = segs[i];
       if (s.npos <= 0) continue;
-      const int chunks = (s.t1 - s.t0 + chunk - 1) / chunk;
-      atomicAdd(&s_items, (unsigned long long)s.units * chunks * p.Hkv);
+      const int chunks = chunks_of(s);
+      sum_rows += (int64_t)s.units * chunks;
       if (chunks > 1 || s.pbase == 0) {
         const int rows_last = s.npos * g - (s.units - 1) * R;
-        atomicAdd(&s_floats, (unsigned long long)p.Hkv * chunks *
-                                 ((unsigned long long)(s.units - 1) * slot_floats(R, p.D) + slot_floats(rows_last, p.D)));
+        sum_floats += (int64_t)p.Hkv * chunks * ((int64_t)(s.units - 1) * slot_floats(R, p.D) + slot_floats(rows_last, p.D));
       }
     }
+    add_warp(&s_rows, sum_rows);
+    add_warp(&s_floats, sum_floats);
     __syncthreads();
-    if (((int64_t)s_items <= p.max_items && (int64_t)s_floats <= p.partial_cap) || chunk == kAllKeys) break;
-    chunk = kAllKeys;
+    if (((int64_t)s_rows <= p.max_rows && (int64_t)s_floats <= p.partial_cap) || chunk == kAllKeys) break;
+    chunk = run_chunk = kAllKeys;
     __syncthreads();
   }
 
-  // pass 3: items and partials of each segment; lengths of the items
-  int64_t item_carry = 0, float_carry = 0;
+  // pass 3: entries and partials of each segment
+  int64_t row_carry = 0, float_carry = 0;
   for (int base = 0; base < n_segs; base += kThreads) {
     const int i = base + tid;
-    int items = 0;
+    int rows = 0;
     int64_t floats = 0;
     Segment s;
     s.npos = 0;
-    if (i < n_segs) s = p.segs[i];
+    if (i < n_segs) s = segs[i];
     if (s.npos > 0) {
-      s.chunks = (s.t1 - s.t0 + chunk - 1) / chunk;
-      items = s.units * s.chunks * p.Hkv;
+      s.chunk = s.ctx == kAllKeys ? run_chunk : chunk;
+      s.chunks = chunks_of(s);
+      rows = s.units * s.chunks;
       if (s.chunks > 1 || s.pbase == 0) {
         s.part_h = s.chunks * ((s.units - 1) * slot_floats(R, p.D) + slot_floats(s.npos * g - (s.units - 1) * R, p.D));
         floats = (int64_t)s.part_h * p.Hkv;
@@ -212,72 +263,74 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     }
     int ti;
     int64_t tf;
-    const int ii = scan_incl<int>(items, s_iscan[2], &ti);
+    const int ii = scan_incl<int>(rows, s_iscan[2], &ti);
     const int64_t fi = scan_incl<int64_t>(floats, s_scan[0], &tf);
     if (i < n_segs) {
-      if (s.npos > 0 && (item_carry + ii > p.max_items || float_carry + fi > p.partial_cap)) {
+      if (s.npos > 0 && (row_carry + ii > p.max_rows || float_carry + fi > p.partial_cap)) {
         // cannot happen with the host's bounds; refuse rather than overflow
         report(p.status, WISP_DEV_UNSUPPORTED, p.request_ids, s.r);
         s.npos = s.units = s.chunks = 0;
       }
       s.pbase = floats > 0 ? (int32_t)(float_carry + fi - floats) : -1;
       if (s.npos > 0 && floats > 0) s_any = 1;
-      s.first = (int32_t)(item_carry + ii - items);
-      if (s.npos > 0 || i >= p.B) p.segs[i] = s;
+      s.first = (int32_t)(row_carry + ii - rows);
+      if (few) s_first[tid] = s.first;
+      segs[i] = s;
+      if (few) p.segs[i] = s;  // (for the merge)
     }
-    item_carry += ti;
+    row_carry += ti;
     float_carry += tf;
     __syncthreads();
   }
-  const int n_all = (int)min(item_carry, p.max_items);
+  const int n_all = (int)min(row_carry, p.max_rows);
+  const bool single = few && n_all <= kThreads;  // an entry per thread, kept from pass 4 to pass 5
 
-  // passes 4 and 5: the histogram of the items' lengths, then each item at its place in the dispatch order
+  // pass 4: the histogram of the entries' lengths; pass 5: each entry at its place in the dispatch order, longest first
   auto bucket_of = [&](int tokens) { return kBuckets - 1 - min(ceil_div(tokens, 64), kBuckets - 1); };
+  WorkItem w;
+  int bucket = -1;
   for (int pass = 0; pass < 2; ++pass) {
     for (int base = 0; base < n_segs; base += kThreads) {
-      const int i = base + tid;
-      s_first[tid] = i < n_segs ? p.segs[i].first : n_all;
-      if (tid == 0) s_first[kThreads] = base + kThreads < n_segs ? p.segs[base + kThreads].first : n_all;
-      __syncthreads();
-      const int lo = s_first[0], hi = min(s_first[kThreads], n_all);
+      const int in = min(kThreads, n_segs - base);
+      int lo = 0, hi = n_all;
+      if (!few) {
+        if (tid < in) s_first[tid] = segs[base + tid].first;
+        if (tid == 0) s_first[kThreads] = base + kThreads < n_segs ? segs[base + kThreads].first : n_all;
+        __syncthreads();
+        lo = s_first[0];
+        hi = min(s_first[kThreads], n_all);
+      }
       for (int x = lo + tid; x < hi; x += kThreads) {
-        int a = 0, b = min(kThreads, n_segs - base) - 1;  // the last segment whose first item is <= x
-        while (a < b) {
-          const int mid = (a + b + 1) >> 1;
-          if (s_first[mid] <= x) a = mid;
-          else b = mid - 1;
+        if (pass == 0 || !single) {
+          bucket = -1;
+          int a = 0, b = in - 1;  // the last segment whose first entry is <= x
+          while (a < b) {
+            const int mid = (a + b + 1) >> 1;
+            if (s_first[mid] <= x) a = mid;
+            else b = mid - 1;
+          }
+          const Segment s = segs[base + a];
+          if (s.units <= 0) continue;
+          const int rel = x - s.first, u = rel / s.chunks, c = rel - u * s.chunks;
+          if (u >= s.units) continue;
+          w.t0 = s.t0 + c * s.chunk;
+          w.t1 = (int)min((int64_t)unit_end(s, u, R, g), (int64_t)w.t0 + s.chunk);
+          if (w.t1 <= w.t0) continue;  // (the unit ends before this chunk)
+          bucket = bucket_of(w.t1 - w.t0);
+          w.r = s.r;
+          w.h = 0;
+          w.rows = min(R, s.npos * g - u * R);
+          w.q0 = s.q0;
+          w.ctx = s.ctx;
+          w.row0 = u * R;
+          w.rg = u;
+          w.nrg = s.part_h;
+          w.pbase = 0;
+          w.poff = s.pbase < 0 ? -1 : s.pbase + u * s.chunks * slot_floats(R, p.D) + c * slot_floats(w.rows, p.D);
         }
-        const Segment s = p.segs[base + a];
-        if (s.units <= 0) continue;
-        const int rel = x - s.first, per_h = s.units * s.chunks;
-        const int h = rel / per_h, u = rel % per_h / s.chunks, c = rel % s.chunks;
-        if (h >= p.Hkv) continue;
-        const int t0 = s.t0 + c * chunk, t1 = (int)min((int64_t)unit_end(s, u, R, g), (int64_t)t0 + chunk);
-        if (t1 <= t0) continue;  // (the unit ends before this chunk)
-        const int bucket = bucket_of(t1 - t0);
-        if (pass == 0) {
-          atomicAdd(&s_hist[bucket], 1);
-          continue;
-        }
-        const int rows = min(R, s.npos * g - u * R);
-        WorkItem w;
-        w.r = s.r;
-        w.h = h;
-        w.t0 = t0;
-        w.t1 = t1;
-        w.rows = rows;
-        w.q0 = s.q0;
-        w.ctx = s.ctx;
-        w.row0 = u * R;
-        w.rg = u;
-        w.nrg = s.units;
-        w.poff = -1;
-        w.pbase = 0;
-        if (s.pbase >= 0) {
-          w.pbase = s.pbase + h * s.part_h + u * s.chunks * slot_floats(R, p.D);
-          w.poff = w.pbase + c * slot_floats(rows, p.D);
-        }
-        p.items[atomicAdd(&s_hist[bucket], 1)] = w;
+        if (bucket < 0) continue;
+        const int at = atomicAdd(&s_hist[bucket], 1);
+        if (pass == 1) p.items[at] = w;
       }
       __syncthreads();
     }
@@ -290,12 +343,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       if (tid == 0) {
         PromptHeader hd;
         memset(&hd, 0, sizeof hd);
-        hd.h.n_items = total;
+        hd.h.n_items = total * p.Hkv;
         hd.h.chunk_len = chunk;
         hd.h.attn_ctas = p.sms;
         hd.partials = s_any;
         hd.n_runs = n_runs;
-        hd.chunk = chunk;
         *p.header = hd;
       }
       __syncthreads();
@@ -303,93 +355,86 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   }
 }
 
-// The partials of a row joined: O = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m = max m_i.  A CTA takes a query row, its
-// warps take the heads in turn.  Bound by the partials' bytes.
+// The partials of a row joined: O = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m = max m_i.  A warp takes a (query row, head); grid
+// columns are requests, so that no row has to look for its own.  Bound by the partials' bytes.
 template <int D, typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptPlan p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!p.header->partials) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int g = p.Hq / p.Hkv, R = p.unit_rows, chunk = p.header->chunk;
+  const int lane = threadIdx.x & 31;
+  const int g = p.Hq / p.Hkv, R = p.unit_rows;
   constexpr int CPL = D / 32;
-  for (int t = blockIdx.x; t < p.total_q_rows; t += gridDim.x) {
-    int a = 0, b = p.B - 1;  // the row's request
-    while (a < b) {
-      const int mid = (a + b + 1) >> 1;
-      if (p.q_row_start[mid] <= t) a = mid;
-      else b = mid - 1;
-    }
-    if (p.req_flag[a] != REQ_OK || t >= p.q_row_start[a + 1]) continue;
-    const int run = p.req_run[a];
-    Segment s[2];
-    s[0] = p.segs[a];
-    if (run >= 0) s[1] = p.segs[p.B + run];
-    const int n_seg = run >= 0 ? 2 : 1;
-    if (s[0].pbase < 0) continue;  // (its items have written the output)
-    for (int h = warp; h < p.Hq; h += kMergeThreads / 32) {
-      const int hk = h / g, hh = h % g;
-      // per segment: the row's first slot (O, and its m), the distance of slots and how many
+  for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
+    const Segment own = p.segs[r];
+    const int run = p.req_run[r];
+    if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
+    const Segment pre = p.segs[run >= 0 ? p.B + run : r];
+    const int work = own.npos * p.Hq;
+    for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
+      const int j = x / p.Hq, h = x - j * p.Hq, hk = h / g, hh = h - hk * g;
+      // per segment (0: the run's, 1: the request's own): the row's first O and m, the distance of chunks and how many
       const float *po[2], *pm[2];
       int step[2], n[2], nl[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        n[i] = 0;
-        if (i >= n_seg) continue;
-        const int rho = (t - s[i].q0) * g + hh, u = rho / R, rr = rho - u * R;
-        const int rows = min(R, s[i].npos * g - u * R);
+        const Segment &s = i == 0 ? pre : own;
+        const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
+        const int rows = min(R, s.npos * g - u * R);
         step[i] = slot_floats(rows, D);
         nl[i] = rows;
-        n[i] = min(s[i].chunks, (unit_end(s[i], u, R, g) - s[i].t0 + chunk - 1) / chunk);
-        const float *base = p.partials + (s[i].pbase + hk * s[i].part_h + u * s[i].chunks * slot_floats(R, D));
-        po[i] = base + rr * D;
+        n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, (unit_end(s, u, R, g) - s.t0 + s.chunk - 1) / s.chunk);
+        const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
+        po[i] = base + rr * D + lane * CPL;
         pm[i] = base + rows * D + rr;
       }
       const int total = n[0] + n[1];
-      float m = -INFINITY;
-      for (int c = lane; c < total; c += 32) {
-        const bool z = c < n[0];
-        m = fmaxf(m, __ldcg(z ? pm[0] + c * step[0] : pm[1] + (c - n[0]) * step[1]));
-      }
-      m = ptx::warp_max(m);
-      float den = 0.0f, acc[CPL];
+      float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
       for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
-      for (int c0 = 0; c0 < total; c0 += 32) {
-        float w = -1.0f;
-        if (c0 + lane < total) {
-          const int c = c0 + lane;
+      for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
+        const int c = c0 + lane;
+        float mc = -INFINITY, lc = 0.0f;
+        if (c < total) {
           const bool z = c < n[0];
           const float *q = z ? pm[0] + c * step[0] : pm[1] + (c - n[0]) * step[1];
-          const float mc = __ldcg(q), lc = __ldcg(q + (z ? nl[0] : nl[1]));
-          if (mc != -INFINITY) {
-            w = ptx::ex2(mc - m);
-            den = fmaf(lc, w, den);
-          } else if (lc != 0.0f) {
-            den = lc;  // (a NaN: a score that is no number)
-          }
+          mc = __ldcg(q);
+          lc = __ldcg(q + (z ? nl[0] : nl[1]));
         }
+        const float mn = fmaxf(m, ptx::warp_max(mc));
+        if (mn != m) {
+          const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
+          den = m == -INFINITY ? den : den * a;
+#pragma unroll
+          for (int q = 0; q < CPL; ++q) acc[q] *= a;
+          m = mn;
+        }
+        // a chunk none of whose keys the row sees adds nothing (weight -1); its l is 0, or a NaN where its scores are no numbers
+        const float w = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
+        den = mc == -INFINITY ? den + lc : fmaf(lc, w, den);
         const int nc = min(32, total - c0);
 #pragma unroll 4
-        for (int c = 0; c < nc; ++c) {
-          const float x = __shfl_sync(0xffffffffu, w, c);
-          const bool z = c0 + c < n[0];
+        for (int i = 0; i < nc; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i);
           float v[CPL];
-          ld_cols<CPL>((z ? po[0] + (c0 + c) * step[0] : po[1] + (c0 + c - n[0]) * step[1]) + lane * CPL, v);
-          // (a chunk none of whose keys the row sees adds nothing)
+          ld_cols<CPL>(c0 + i < n[0] ? po[0] + (c0 + i) * step[0] : po[1] + (c0 + i - n[0]) * step[1], v);
 #pragma unroll
           for (int q = 0; q < CPL; ++q)
-            if (!(x < 0.0f)) acc[q] = fmaf(v[q], x, acc[q]);
+            if (!(wi < 0.0f)) acc[q] = fmaf(v[q], wi, acc[q]);
         }
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-      st_cols<CPL>(static_cast<T *>(p.out) + ((int64_t)t * p.Hq + h) * D + lane * CPL, acc, 1.0f / den);
+      st_cols<CPL>(static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + h) * D + lane * CPL, acc, 1.0f / den);
     }
   }
 }
 
+cudaError_t prompt_plan_setup() {
+  return cudaFuncSetAttribute(prompt_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanShared));
+}
+
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s) {
-  prompt_plan_kernel<<<1, kThreads, 0, s>>>(p);
+  prompt_plan_kernel<<<1, kThreads, sizeof(PlanShared), s>>>(p);
   return cudaGetLastError();
 }
 
@@ -399,8 +444,11 @@ cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  // about 16 CTAs per SM, or one warp per (row, head)
   const int most = p.sms * 16;
-  cfg.gridDim = dim3((unsigned)(p.total_q_rows < most ? p.total_q_rows : most));
+  const int64_t ctas = std::min<int64_t>(most, ((int64_t)p.total_q_rows * p.Hq + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
+  const int cols = std::min(p.B, most);
+  cfg.gridDim = dim3((unsigned)cols, (unsigned)((ctas + cols - 1) / cols));
   cfg.blockDim = dim3(kMergeThreads);
   cfg.stream = s;
   cfg.attrs = attr;

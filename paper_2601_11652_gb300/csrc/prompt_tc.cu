@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         for (int c = 0; c < 4; ++c) {
           mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-          for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][i])), __uint_as_float(x[c][i + 1]));
+          for (int i = 2; i < 32; i += 2) mx[c] = ptx::max3(mx[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
         }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
         if (t == first) {
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           it = claimed;
           claimed = -2;
           s_ring[slot].it = it;
-          if (it >= 0) s_ring[slot].w = p.items[it];
+          if (it >= 0) s_ring[slot].w = item_at(p, it);
         }
         it = __shfl_sync(0xffffffffu, it, 0);
         __syncwarp();

@@ -260,6 +260,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Maximum of three (a NaN loses to a number).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // Maximum of x over the 32 lanes of a converged warp (every lane gets it; a NaN loses to a number).
 __device__ __forceinline__ float warp_max(float x) {
   float y;
