@@ -21,6 +21,7 @@ constexpr int kTile = 128;         // and are whole key tiles
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys
 constexpr int kMaxRows = 1 << 24;  // k_r limit
 constexpr int kMergeThreads = 128;
+constexpr int kAhead = 4;          // chunks whose O a warp of the merge has on its way
 
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
 template <typename T>
@@ -211,12 +212,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 
   // the chunk length: with at least as many units as SMs, only sequences longer than 5/4 of the average work per SM are cut (a
   // longest-first order balances the rest, and a cut costs a merge); with fewer, about two items per SM.  The rows of a run are merged
-  // anyway, and a unit of theirs is as long as the prefix: it is cut to an eighth of an SM's work.
+  // anyway, and a unit of theirs is as long as the prefix: it is cut to a third of an SM's work (256 requests behind 16384 tokens:
+  // 446 us; to an eighth 470, and to a half 462).
   const int64_t keys = (int64_t)s_keys * p.Hkv;
   const bool many = (int64_t)s_units * p.Hkv >= p.sms;
   auto rounded = [&](int64_t n, int least) { return (int)min((n < least ? least : n + kTile - 1) / kTile * kTile, (int64_t)kAllKeys); };
   int chunk = rounded(many ? (keys + p.sms - 1) / p.sms * 5 / 4 : (keys + 2 * p.sms - 1) / (2 * p.sms), kMinKeys);
-  int run_chunk = min(chunk, rounded(keys / p.sms / 8, kMinRunKeys));
+  int run_chunk = min(chunk, rounded(keys / p.sms / 3, kMinRunKeys));
   auto chunks_of = [&](const Segment &s) {
     const int c = s.ctx == kAllKeys ? run_chunk : chunk;
     return (s.t1 - s.t0 + c - 1) / c;
@@ -391,6 +393,16 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
       float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
       for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
+      // O of the next chunks, on its way while their weights are computed
+      float v[kAhead][CPL];
+      auto fetch = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int c = c0 + i;
+          if (c < total) ld_cols<CPL>(c < n[0] ? po[0] + c * step[0] : po[1] + (c - n[0]) * step[1], v[i]);
+        }
+      };
+      fetch(0);
       for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
         const int c = c0 + lane;
         float mc = -INFINITY, lc = 0.0f;
@@ -412,14 +424,15 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
         const float w = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
         den = mc == -INFINITY ? den + lc : fmaf(lc, w, den);
         const int nc = min(32, total - c0);
-#pragma unroll 4
-        for (int i = 0; i < nc; ++i) {
-          const float wi = __shfl_sync(0xffffffffu, w, i);
-          float v[CPL];
-          ld_cols<CPL>(c0 + i < n[0] ? po[0] + (c0 + i) * step[0] : po[1] + (c0 + i - n[0]) * step[1], v);
+        for (int i0 = 0; i0 < nc; i0 += kAhead) {
 #pragma unroll
-          for (int q = 0; q < CPL; ++q)
-            if (!(wi < 0.0f)) acc[q] = fmaf(v[q], wi, acc[q]);
+          for (int i = 0; i < kAhead; ++i) {
+            const float wi = __shfl_sync(0xffffffffu, w, (i0 + i) & 31);
+#pragma unroll
+            for (int q = 0; q < CPL; ++q)
+              if (i0 + i < nc && !(wi < 0.0f)) acc[q] = fmaf(v[i][q], wi, acc[q]);
+          }
+          fetch(c0 + i0 + kAhead);
         }
       }
 #pragma unroll

@@ -80,7 +80,8 @@ struct Bars {
   static constexpr int ODD_FREE = V_CLEAN + C::NS;           // [2] per buffer of odd values: its item's epilogues are done
   static constexpr int ML_FULL = ODD_FREE + 2, ML_EMPTY = ML_FULL + 1;  // stream 1's m and l (and O): published, read
   static constexpr int S_EMPTY = ML_EMPTY + 1;   // [2] S has been read (P_APART)
-  static constexpr int MMA_DONE = S_EMPTY + 2, FIN = MMA_DONE + 1;
+  static constexpr int TURN = S_EMPTY + 2;       // [2] the stream's issuer may go (P over S)
+  static constexpr int MMA_DONE = TURN + 2, FIN = MMA_DONE + 1;
   static constexpr int KC_FULL = FIN + 1, VC_FULL = KC_FULL + C::NS;  // [NS] codes have arrived (8-bit cache)
   static_assert(VC_FULL + C::NS <= C::N_BAR, "barrier count");
 };
@@ -172,6 +173,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       ptx::mbar_init(bar(B::P_FULL + 2 + s), 4);  // the second
       ptx::mbar_init(bar(B::O_FULL + s), 1);
       ptx::mbar_init(bar(B::S_EMPTY + s), 4);
+      ptx::mbar_init(bar(B::TURN + s), 1);
       ptx::mbar_init(bar(B::ODD_FREE + s), 8);
     }
     for (int i = 0; i < kItemRing; ++i) {
@@ -671,6 +673,19 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       const uint32_t idesc_o = ptx::idesc_bf16_f32(kM, D, false, true);
       uint32_t k0 = 0;               // key tiles of the items before
       uint32_t np = 0, ne = 0;       // P tiles and S tiles read so far
+      // With P over S the issuers take turns: a stream's P V and next S go out together, and the other stream's behind them.  Without
+      // that the tensor core works on both at once, both S arrive together, and then it waits for both softmaxes (3400 cycles a tile
+      // instead of TURN_CYCLES).  An item's turns are as many for both, empty ones of stream 1 included.
+      uint32_t turn = 0;
+      auto my_turn = [&]() -> bool {
+        if (C::P_APART) return true;
+        const bool got = wait_bar(bar(B::TURN + s), (turn & 1) ^ (s == 0 ? 1 : 0), s_abort);
+        ++turn;
+        return got;
+      };
+      auto pass = [&]() {  // by one thread
+        if (!C::P_APART) ptx::mbar_arrive(bar(B::TURN + 1 - s));
+      };
       WorkItem w;
       for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
         const Shape sh = shape_of(w, tile_rows, tile_pos);
@@ -702,6 +717,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               const int off = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
               ptx::umma_f16(tmem + s * kBT, qd + off, kd + off, idesc_s, ks > 0);
             }
+            pass();
             ptx::umma_commit(bar(B::S_FULL + s));
             ptx::umma_commit(bar(B::K_EMPTY + st));
             if (t + inc >= sh.nt) ptx::umma_commit(bar(B::Q_EMPTY + qb));
@@ -709,10 +725,12 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           __syncwarp();
           return true;
         };
+        if (!my_turn()) { ok = false; break; }
         if (first < sh.nt) {
           ok = issue_s(first);
         } else if (lane == 0) {
           ptx::mbar_arrive(bar(B::Q_EMPTY + qb));
+          pass();
         }
         for (int t = first; t < sh.nt && ok; t += inc) {
           if (C::P_APART && t + inc < sh.nt) {
@@ -729,6 +747,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             ok = false;
             break;
           }
+          if (!(ok = my_turn())) break;
 #pragma unroll
           for (int half = kWhole; half < 2; ++half) {
             if (!wait_bar(bar(B::P_FULL + 2 * half + s), np & 1, s_abort)) { ok = false; break; }
@@ -740,6 +759,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
                 ptx::umma_f16_ts(tmem + 2 * kBT + s * D, tmem + C::P_COL + s * C::P_STEP + ks * 8, vd + ((ks * 16 * 128) >> 4), idesc_o,
                                  t != first || ks > 0);
               if (half == 1) {
+                if (t + inc >= sh.nt) pass();
                 if (C::P_APART || t + inc >= sh.nt) ptx::umma_commit(bar(B::O_FULL + s));
                 ptx::umma_commit(bar(B::V_EMPTY + st));
               }
@@ -749,6 +769,10 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           if (!ok) break;
           ++np;
           if (!C::P_APART && t + inc < sh.nt) ok = issue_s(t + inc);
+        }
+        if (ok && sh.split && s == 1 && (sh.nt & 1)) {  // stream 0 has a tile more
+          ok = my_turn();
+          if (ok && lane == 0) pass();
         }
         if (ok) ok = skip(B::K_FULL, B::K_EMPTY, kt, sh.nt) && skip(B::V_FULL, B::V_EMPTY, vt, sh.nt);
         k0 += sh.nt;
