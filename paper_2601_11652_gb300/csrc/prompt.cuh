@@ -9,11 +9,13 @@
 // the items leave partials (O, m, l), and merge_kernel joins them.
 #pragma once
 
+#include <cstddef>
+
 #include "attn.cuh"
 
 namespace wisp {
 
-struct Segment {  // 48 bytes
+struct Segment {  // 64 bytes
   int32_t r;        // whose block table
   int32_t q0;       // first query row
   int32_t npos;     // query positions (0: no work)
@@ -24,20 +26,26 @@ struct Segment {  // 48 bytes
   int32_t part_h;   // floats of one KV head's partials
   int32_t first;    // first list entry (empty ones included)
   int32_t chunk;    // keys per chunk
+  int32_t span;     // > 0: unit u's chunks end at multiples of `chunk` from base + u * span on, not from its first key
+  int32_t base;
+  int32_t shared;   // 1: its rows have keys in another segment, too
+  int32_t pad;
 };
-static_assert(sizeof(Segment) == 48, "segment layout");
+static_assert(sizeof(Segment) == 64, "segment layout");
 
 struct PromptHeader {
   PlanHeader h;        // what the attention kernels read
-  int32_t partials;    // 1: merge_kernel has work
+  int32_t partials;    // 1: the merge has work
   int32_t n_runs;
   int32_t pad[6];
 };
+static_assert(offsetof(PromptHeader, h) == 0, "the kernels that read a PlanHeader find it there");
 
 struct PromptPlan {
   int B, Hq, Hkv, D, max_blocks_per_seq, total_q_rows;
   int unit_rows;       // rows of a unit: whole positions of the tensor-core kernel's two tiles, or the fp32 kernel's row limit
   int sms;
+  int grid;            // CTAs of the tensor-core kernel: each has taken its first item by its index; 0 for the other kernel
   int64_t max_rows, partial_cap;  // list entries, floats
   const int32_t *draft_lens, *context_lens, *shared_ids, *shared_pages;  // shared_*: null without runs
   const int64_t *request_ids;
@@ -50,6 +58,7 @@ struct PromptPlan {
   Segment *segs;         // [2 B]
   WorkItem *items;
   // of the merge
+  int merge_heads;     // heads of a KV head's group that a warp takes one after the other: all, or one where rows are few
   float *partials;
   void *out;
 };

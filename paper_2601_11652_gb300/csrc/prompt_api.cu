@@ -1,5 +1,6 @@
 // prompt_api.cu -- host side of include/wisp_prompt.h: argument checks, workspace and launches.  No allocation, no
 // synchronisation.
+#include <algorithm>
 #include <cstring>
 #include <mutex>
 
@@ -70,8 +71,8 @@ Space space(const wisp_attn_args *a, bool shared, int sms) {
   const int g = a->Hq / a->Hkv;
   s.unit_rows = a->qkv_dtype == WISP_BF16 ? 2 * g * prompt_tile_positions(g) : kF32RowsPerItem;
   const int64_t units = ((int64_t)a->total_q_rows * g / s.unit_rows + a->B) * (shared ? 2 : 1);
-  const int64_t slot = (int64_t)s.unit_rows * (a->D + 2) + 4;
-  const int64_t cuts = (int64_t)(shared ? 12 : 6) * (a->qkv_dtype == WISP_BF16 ? 1 : 4) * sms / a->Hkv + 8;
+  const int64_t slot = std::min<int64_t>(s.unit_rows, (int64_t)a->total_q_rows * g) * (a->D + 2) + 4;
+  const int64_t cuts = (std::min<int64_t>(2 * units * a->Hkv, (int64_t)12 * sms) + 4 * sms) / a->Hkv + 8;
   s.max_rows = units + cuts;
   s.partial_cap = cuts * a->Hkv * slot + (shared ? 2 * (int64_t)a->total_q_rows * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
   size_t off = 0;
@@ -127,6 +128,7 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   p.total_q_rows = a->total_q_rows;
   p.unit_rows = sp.unit_rows;
   p.sms = sms;
+  p.merge_heads = (int64_t)a->total_q_rows * a->Hkv >= 16 * sms ? a->Hq / a->Hkv : 1;
   p.max_rows = sp.max_rows;
   p.partial_cap = sp.partial_cap;
   p.draft_lens = a->draft_lens;
@@ -144,6 +146,8 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   p.items = at<WorkItem>(ws, sp.items);
   p.partials = at<float>(ws, sp.partials);
   p.out = a->out;
+  const int grid = (int)(sp.max_rows * a->Hkv < sms ? sp.max_rows * a->Hkv : sms);
+  p.grid = bf ? grid : 0;
   if (prompt_plan_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   if (a->B == 0) return WISP_OK;
   AttnParams ap;
@@ -169,7 +173,6 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   ap.header_mut = &p.header->h;
   ap.items = p.items;
   ap.partials = p.partials;  // (pair_done stays null: the merge kernel joins them)
-  const int grid = (int)(sp.max_rows * a->Hkv < sms ? sp.max_rows * a->Hkv : sms);
   cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : attn_f32_launch(ap, grid, s);
   if (e == cudaSuccess) e = prompt_merge_launch(p, !bf, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;

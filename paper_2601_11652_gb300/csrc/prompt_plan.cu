@@ -15,13 +15,13 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kPage = 16;
 constexpr int kBuckets = 1024;     // of the dispatch order, by key tiles of 64
-constexpr int kMinKeys = 256;      // chunks are not shorter
-constexpr int kMinRunKeys = 1024;  // ... nor those of a run's rows, where there are many units
+constexpr int kMinKeys = 256;      // chunks are not shorter, nor
+constexpr int kMinFull = 1024;     // of units of more than one tile (their partials cost more)
 constexpr int kTile = 128;         // and are whole key tiles
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys
 constexpr int kMaxRows = 1 << 24;  // k_r limit
 constexpr int kMergeThreads = 128;
-constexpr int kAhead = 4;          // chunks whose O a warp of the merge has on its way
+constexpr int kFew = 4;            // chunks of a row that a warp of the merge has in registers at once
 
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
 template <typename T>
@@ -59,6 +59,11 @@ __device__ __forceinline__ int unit_end(const Segment &s, int u, int unit_rows, 
   const int last = min((u + 1) * unit_rows, s.npos * g) - 1;
   return min(s.t1, s.ctx + last / g + 1);
 }
+
+// Where unit u's chunks are cut: keys of the chunk that its first key falls in, in front of it.
+__device__ __forceinline__ int cut_off(const Segment &s, int u) { return s.span ? (int)((s.base + (int64_t)u * s.span) % s.chunk) : 0; }
+// Chunks of a unit with keys [s.t0, end), and the c-th of them.
+__device__ __forceinline__ int unit_chunks(const Segment &s, int u, int end) { return (end - s.t0 + cut_off(s, u) + s.chunk - 1) / s.chunk; }
 
 }  // namespace
 
@@ -186,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
         s.ctx = one ? my_ctx : p.context_lens[i];
         s.t0 = shared ? (one ? my_pages : p.shared_pages[i]) * kPage : 0;
         s.t1 = s.ctx + s.npos;
-        if (shared) s.pbase = 0;
+        s.shared = shared;
       }
     } else if (run_valid[i - p.B] > 1) {
       const int run = i - p.B, a = run_first[run], b = run_end[run];
@@ -195,14 +200,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       s.npos = min(b < p.B ? p.q_row_start[b] : p.total_q_rows, p.total_q_rows) - s.q0;
       s.ctx = kAllKeys;
       s.t1 = p.shared_pages[a] * kPage;
-      s.pbase = 0;
+      s.shared = 1;
     }
     if (s.npos > 0) {
       s.units = (int)(((int64_t)s.npos * g + R - 1) / R);
       const int64_t len = ((int64_t)(unit_end(s, 0, R, g) - s.t0) + (s.t1 - s.t0) + 1) / 2;
       sum_keys += len * s.units;
       sum_units += s.units;
-      if (s.pbase == 0) s_any = 1;
     }
     segs[i] = s;
   }
@@ -210,29 +214,38 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   add_warp(&s_units, sum_units);
   __syncthreads();
 
-  // the chunk length: with at least as many units as SMs, only sequences longer than 5/4 of the average work per SM are cut (a
-  // longest-first order balances the rest, and a cut costs a merge); with fewer, about two items per SM.  The rows of a run are merged
-  // anyway, and a unit of theirs is as long as the prefix: it is cut to a third of an SM's work (256 requests behind 16384 tokens:
-  // 446 us; to an eighth 470, and to a half 462).
-  const int64_t keys = (int64_t)s_keys * p.Hkv;
+  // Where sequences are cut.  A cut costs a merge, and its chunks begin and end like items of their own.  With at least as many units
+  // as SMs the longest-first order balances units of many lengths: only a segment whose longest unit is above 5/4 of an SM's
+  // average work is cut.  Many units of one length it balances badly (168 equal ones on 152 SMs: two rounds), so where they are
+  // three quarters of all work (the rest fills gaps), they are cut from a fifth of an SM's work on: they lie one behind the other, and every
+  // multiple of an SM's average is a cut, whatever unit it falls in.  (1344 rows behind 16384 tokens: 250 us, 354 without.)  With fewer
+  // units than SMs, about two items per SM.
+  const int64_t keys = (int64_t)s_keys * p.Hkv, avg = (keys + p.sms - 1) / p.sms;
   const bool many = (int64_t)s_units * p.Hkv >= p.sms;
-  auto rounded = [&](int64_t n, int least) { return (int)min((n < least ? least : n + kTile - 1) / kTile * kTile, (int64_t)kAllKeys); };
-  int chunk = rounded(many ? (keys + p.sms - 1) / p.sms * 5 / 4 : (keys + 2 * p.sms - 1) / (2 * p.sms), kMinKeys);
-  int run_chunk = min(chunk, rounded(keys / p.sms / 3, kMinRunKeys));
-  auto chunks_of = [&](const Segment &s) {
-    const int c = s.ctx == kAllKeys ? run_chunk : chunk;
-    return (s.t1 - s.t0 + c - 1) / c;
+  const int64_t want = many ? avg : (avg + 1) / 2;
+  const int average = (int)min((want + kTile - 1) / kTile * kTile, (int64_t)kAllKeys);
+  bool cuts = true;
+  // how a segment is cut: its chunk length, and whether its units are cut as they lie one behind the other
+  auto rule = [&](Segment &s) {
+    const int len = s.t1 - s.t0, shortest = unit_end(s, 0, R, g) - s.t0;
+    const int chunk = max(average, min(R, s.npos * g) > kTile ? kMinFull : kMinKeys);
+    const bool even = s.units > 1 && 2 * (int64_t)shortest > len && 4 * (int64_t)s.units * p.Hkv * len >= 3 * keys;
+    const bool cut = cuts && (many ? (even ? 5 * (int64_t)len > avg : 4 * (int64_t)len > 5 * avg) : len > chunk);
+    s.chunk = cut ? chunk : kAllKeys;
+    s.span = cut && many ? (len + kTile - 1) / kTile * kTile : 0;
+    s.chunks = cut ? (len + (s.span ? chunk - kTile : 0) + chunk - 1) / chunk : 1;  // at most
   };
   for (;;) {  // (twice at most: without cuts everything fits, by the host's bounds)
     if (tid == 0) s_rows = s_floats = 0;
     __syncthreads();
     int64_t sum_rows = 0, sum_floats = 0;
     for (int i = tid; i < n_segs; i += kThreads) {
-      const Segment s = segs[i];
+      Segment s = segs[i];
       if (s.npos <= 0) continue;
-      const int chunks = chunks_of(s);
+      rule(s);
+      const int chunks = s.chunks;
       sum_rows += (int64_t)s.units * chunks;
-      if (chunks > 1 || s.pbase == 0) {
+      if (chunks > 1 || s.shared) {
         const int rows_last = s.npos * g - (s.units - 1) * R;
         sum_floats += (int64_t)p.Hkv * chunks * ((int64_t)(s.units - 1) * slot_floats(R, p.D) + slot_floats(rows_last, p.D));
       }
@@ -240,33 +253,35 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     add_warp(&s_rows, sum_rows);
     add_warp(&s_floats, sum_floats);
     __syncthreads();
-    if (((int64_t)s_rows <= p.max_rows && (int64_t)s_floats <= p.partial_cap) || chunk == kAllKeys) break;
-    chunk = run_chunk = kAllKeys;
+    if (((int64_t)s_rows <= p.max_rows && (int64_t)s_floats <= p.partial_cap) || !cuts) break;
+    cuts = false;
     __syncthreads();
   }
 
   // pass 3: entries and partials of each segment
-  int64_t row_carry = 0, float_carry = 0;
+  int64_t row_carry = 0, float_carry = 0, span_carry = 0;
   for (int base = 0; base < n_segs; base += kThreads) {
     const int i = base + tid;
     int rows = 0;
-    int64_t floats = 0;
+    int64_t floats = 0, spans = 0;
     Segment s;
     s.npos = 0;
     if (i < n_segs) s = segs[i];
     if (s.npos > 0) {
-      s.chunk = s.ctx == kAllKeys ? run_chunk : chunk;
-      s.chunks = chunks_of(s);
+      rule(s);
       rows = s.units * s.chunks;
-      if (s.chunks > 1 || s.pbase == 0) {
+      spans = (int64_t)s.units * s.span;
+      if (s.chunks > 1 || s.shared) {
         s.part_h = s.chunks * ((s.units - 1) * slot_floats(R, p.D) + slot_floats(s.npos * g - (s.units - 1) * R, p.D));
         floats = (int64_t)s.part_h * p.Hkv;
       }
     }
     int ti;
-    int64_t tf;
+    int64_t tf, ts;
     const int ii = scan_incl<int>(rows, s_iscan[2], &ti);
     const int64_t fi = scan_incl<int64_t>(floats, s_scan[0], &tf);
+    const int64_t si = scan_incl<int64_t>(spans, s_scan[1], &ts);
+    s.base = s.span ? (int)((span_carry + si - spans) % s.chunk) : 0;
     if (i < n_segs) {
       if (s.npos > 0 && (row_carry + ii > p.max_rows || float_carry + fi > p.partial_cap)) {
         // cannot happen with the host's bounds; refuse rather than overflow
@@ -282,6 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     }
     row_carry += ti;
     float_carry += tf;
+    span_carry += ts;
     __syncthreads();
   }
   const int n_all = (int)min(row_carry, p.max_rows);
@@ -315,8 +331,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
           if (s.units <= 0) continue;
           const int rel = x - s.first, u = rel / s.chunks, c = rel - u * s.chunks;
           if (u >= s.units) continue;
-          w.t0 = s.t0 + c * s.chunk;
-          w.t1 = (int)min((int64_t)unit_end(s, u, R, g), (int64_t)w.t0 + s.chunk);
+          const int end = unit_end(s, u, R, g), off = cut_off(s, u);
+          w.t0 = s.t0 + max(0, c * s.chunk - off);
+          w.t1 = (int)min((int64_t)end, (int64_t)s.t0 - off + (int64_t)(c + 1) * s.chunk);
           if (w.t1 <= w.t0) continue;  // (the unit ends before this chunk)
           bucket = bucket_of(w.t1 - w.t0);
           w.r = s.r;
@@ -328,7 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
           w.rg = u;
           w.nrg = s.part_h;
           w.pbase = 0;
-          w.poff = s.pbase < 0 ? -1 : s.pbase + u * s.chunks * slot_floats(R, p.D) + c * slot_floats(w.rows, p.D);
+          const bool whole = w.t0 == s.t0 && w.t1 == end && !s.shared;  // its items write the outputs
+          w.poff = s.pbase < 0 || whole ? -1 : s.pbase + u * s.chunks * slot_floats(R, p.D) + c * slot_floats(w.rows, p.D);
         }
         if (bucket < 0) continue;
         const int at = atomicAdd(&s_hist[bucket], 1);
@@ -346,8 +364,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
         PromptHeader hd;
         memset(&hd, 0, sizeof hd);
         hd.h.n_items = total * p.Hkv;
-        hd.h.chunk_len = chunk;
+        hd.h.chunk_len = average;
         hd.h.attn_ctas = p.sms;
+        hd.h.next_item = p.grid;
         hd.partials = s_any;
         hd.n_runs = n_runs;
         *p.header = hd;
@@ -357,87 +376,120 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   }
 }
 
-// The partials of a row joined: O = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m = max m_i.  A warp takes a (query row, head); grid
-// columns are requests, so that no row has to look for its own.  Bound by the partials' bytes.
+// The partials of a row joined: O = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m = max m_i.  A warp takes a query position and a KV
+// head, one row after the other (where units are whole positions they lie in one unit; single rows where rows are few); grid columns are requests, so that no row has to
+// look for its own.  Up to kFew chunks, as almost always, every lane computes their weights itself.  Bound by instructions, then by the
+// partials' bytes (mostly in L2).
 template <int D, typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptPlan p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!p.header->partials) return;
   const int lane = threadIdx.x & 31;
   const int g = p.Hq / p.Hkv, R = p.unit_rows;
+  const bool whole = R % g == 0;
   constexpr int CPL = D / 32;
   for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
     const Segment own = p.segs[r];
     const int run = p.req_run[r];
     if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
     const Segment pre = p.segs[run >= 0 ? p.B + run : r];
-    const int work = own.npos * p.Hq;
+    const int subs = g / p.merge_heads, work = own.npos * p.Hkv * subs;
     for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
-      const int j = x / p.Hq, h = x - j * p.Hq, hk = h / g, hh = h - hk * g;
+      const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
+      T *dst = static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + hk * g + h0) * D + lane * CPL;
       // per segment (0: the run's, 1: the request's own): the row's first O and m, the distance of chunks and how many
       const float *po[2], *pm[2];
       int step[2], n[2], nl[2];
+      for (int hh = h0; hh < h0 + p.merge_heads; ++hh, dst += D) {
+        if (hh == h0 || !whole) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const Segment &s = i == 0 ? pre : own;
-        const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
-        const int rows = min(R, s.npos * g - u * R);
-        step[i] = slot_floats(rows, D);
-        nl[i] = rows;
-        n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, (unit_end(s, u, R, g) - s.t0 + s.chunk - 1) / s.chunk);
-        const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
-        po[i] = base + rr * D + lane * CPL;
-        pm[i] = base + rows * D + rr;
-      }
-      const int total = n[0] + n[1];
-      float m = -INFINITY, den = 0.0f, acc[CPL];
-#pragma unroll
-      for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
-      // O of the next chunks, on its way while their weights are computed
-      float v[kAhead][CPL];
-      auto fetch = [&](int c0) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int c = c0 + i;
-          if (c < total) ld_cols<CPL>(c < n[0] ? po[0] + c * step[0] : po[1] + (c - n[0]) * step[1], v[i]);
-        }
-      };
-      fetch(0);
-      for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
-        const int c = c0 + lane;
-        float mc = -INFINITY, lc = 0.0f;
-        if (c < total) {
-          const bool z = c < n[0];
-          const float *q = z ? pm[0] + c * step[0] : pm[1] + (c - n[0]) * step[1];
-          mc = __ldcg(q);
-          lc = __ldcg(q + (z ? nl[0] : nl[1]));
-        }
-        const float mn = fmaxf(m, ptx::warp_max(mc));
-        if (mn != m) {
-          const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
-          den = m == -INFINITY ? den : den * a;
-#pragma unroll
-          for (int q = 0; q < CPL; ++q) acc[q] *= a;
-          m = mn;
-        }
-        // a chunk none of whose keys the row sees adds nothing (weight -1); its l is 0, or a NaN where its scores are no numbers
-        const float w = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
-        den = mc == -INFINITY ? den + lc : fmaf(lc, w, den);
-        const int nc = min(32, total - c0);
-        for (int i0 = 0; i0 < nc; i0 += kAhead) {
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) {
-            const float wi = __shfl_sync(0xffffffffu, w, (i0 + i) & 31);
-#pragma unroll
-            for (int q = 0; q < CPL; ++q)
-              if (i0 + i < nc && !(wi < 0.0f)) acc[q] = fmaf(v[i][q], wi, acc[q]);
+          for (int i = 0; i < 2; ++i) {
+            const Segment &s = i == 0 ? pre : own;
+            const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
+            const int rows = min(R, s.npos * g - u * R);
+            step[i] = slot_floats(rows, D);
+            nl[i] = rows;
+            n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
+            const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
+            po[i] = base + rr * D + lane * CPL;
+            pm[i] = base + rows * D + rr;
           }
-          fetch(c0 + i0 + kAhead);
-        }
-      }
+        } else {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-      st_cols<CPL>(static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + h) * D + lane * CPL, acc, 1.0f / den);
+          for (int i = 0; i < 2; ++i) {
+            po[i] += D;
+            pm[i] += 1;
+          }
+        }
+        const int total = n[0] + n[1];
+        if (total == 1 && !own.shared) continue;  // (a unit that no cut fell in)
+        auto at = [&](const float *const (&base)[2], int c) { return c < n[0] ? base[0] + c * step[0] : base[1] + (c - n[0]) * step[1]; };
+        float den = 0.0f, acc[CPL];
+#pragma unroll
+        for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
+        // a chunk none of whose keys the row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
+        if (total <= kFew) {
+          float v[kFew][CPL], mc[kFew], lc[kFew], m = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < kFew; ++c) {
+            mc[c] = -INFINITY;
+            lc[c] = 0.0f;
+            if (c < total) {
+              const float *q = at(pm, c);
+              mc[c] = __ldcg(q);
+              lc[c] = __ldcg(q + (c < n[0] ? nl[0] : nl[1]));
+              ld_cols<CPL>(at(po, c), v[c]);
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < kFew; ++c) m = fmaxf(m, mc[c]);
+#pragma unroll
+          for (int c = 0; c < kFew; ++c) {
+            if (mc[c] == -INFINITY) {
+              den += lc[c];
+            } else {
+              const float w = ptx::ex2(mc[c] - m);
+              den = fmaf(lc[c], w, den);
+#pragma unroll
+              for (int q = 0; q < CPL; ++q) acc[q] = fmaf(v[c][q], w, acc[q]);
+            }
+          }
+        } else {
+          float m = -INFINITY;
+          for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
+            const int c = c0 + lane;
+            float mc = -INFINITY, lc = 0.0f;
+            if (c < total) {
+              const float *q = at(pm, c);
+              mc = __ldcg(q);
+              lc = __ldcg(q + (c < n[0] ? nl[0] : nl[1]));
+            }
+            const float mn = fmaxf(m, ptx::warp_max(mc));
+            if (mn != m) {
+              const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
+              den = m == -INFINITY ? den : den * a;
+#pragma unroll
+              for (int q = 0; q < CPL; ++q) acc[q] *= a;
+              m = mn;
+            }
+            const float w = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
+            den = mc == -INFINITY ? den + lc : fmaf(lc, w, den);
+            const int nc = min(32, total - c0);
+#pragma unroll 4
+            for (int i = 0; i < nc; ++i) {
+              const float wi = __shfl_sync(0xffffffffu, w, i);
+              float v[CPL];
+              ld_cols<CPL>(at(po, c0 + i), v);
+#pragma unroll
+              for (int q = 0; q < CPL; ++q)
+                if (!(wi < 0.0f)) acc[q] = fmaf(v[q], wi, acc[q]);
+            }
+          }
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+        }
+        st_cols<CPL>(dst, acc, 1.0f / den);
+      }
     }
   }
 }
@@ -457,9 +509,9 @@ cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  // about 16 CTAs per SM, or one warp per (row, head)
+  // about 16 CTAs per SM, or one per four warps that have work
   const int most = p.sms * 16;
-  const int64_t ctas = std::min<int64_t>(most, ((int64_t)p.total_q_rows * p.Hq + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
+  const int64_t ctas = std::min<int64_t>(most, ((int64_t)p.total_q_rows * p.Hq / p.merge_heads + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
   const int cols = std::min(p.B, most);
   cfg.gridDim = dim3((unsigned)cols, (unsigned)((ctas + cols - 1) / cols));
   cfg.blockDim = dim3(kMergeThreads);

@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
       uint32_t nk = 0, nv = 0, nq = 0;  // tiles and items' Q so far
-      int claimed = -2;         // (lane 0) the next item, -2: not claimed yet
+      int claimed = (int)blockIdx.x < n_items ? (int)blockIdx.x : -1;
       auto claim = [&]() {
         if (lane == 0 && claimed == -2) {
           claimed = atomicAdd(&p.header_mut->next_item, 1);
@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       uint32_t np = 0, ne = 0;       // P tiles and S tiles read so far
       // With P over S the issuers take turns: a stream's P V and next S go out together, and the other stream's behind them.  Without
       // that the tensor core works on both at once, both S arrive together, and then it waits for both softmaxes (3400 cycles a tile
-      // instead of TURN_CYCLES).  An item's turns are as many for both, empty ones of stream 1 included.
+      // instead of 2950).  An item's turns are as many for both, empty ones of stream 1 included.
       uint32_t turn = 0;
       auto my_turn = [&]() -> bool {
         if (C::P_APART) return true;
@@ -735,10 +735,12 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         for (int t = first; t < sh.nt && ok; t += inc) {
           if (C::P_APART && t + inc < sh.nt) {
             if (!wait_bar(bar(B::S_EMPTY + s), ne & 1, s_abort)) { ok = false; break; }
-            if (!(ok = issue_s(t + inc))) break;
+            ok = issue_s(t + inc);
+            if (!ok) break;
           }
           ++ne;
-          if (!(ok = skip(B::V_FULL, B::V_EMPTY, vt, t))) break;
+          ok = skip(B::V_FULL, B::V_EMPTY, vt, t);
+          if (!ok) break;
           vt = t + 1;
           const uint32_t n = k0 + t;
           const int st = n % C::NS;
@@ -747,7 +749,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
             ok = false;
             break;
           }
-          if (!(ok = my_turn())) break;
+          ok = my_turn();
+          if (!ok) break;
 #pragma unroll
           for (int half = kWhole; half < 2; ++half) {
             if (!wait_bar(bar(B::P_FULL + 2 * half + s), np & 1, s_abort)) { ok = false; break; }
