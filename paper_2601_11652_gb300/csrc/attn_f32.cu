@@ -262,7 +262,15 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
         for (int d = lane; d < D; d += 32) vb[t * C::LD + d] = 0.0f;
       __syncwarp();
     }
-    if (KV8 && nan) {  // a key that a row does not see adds nothing, whatever it holds
+    if (!KV8 && w.t0 + pg * kPage + n - 1 > w.ctx + w.row0 / g) {  // (a key that some row does not see)
+#pragma unroll 4
+      for (int c = lane; c < n * (D / 4); c += 32) {
+        const float4 v = *reinterpret_cast<const float4 *>(vb + c / (D / 4) * C::LD + c % (D / 4) * 4);
+        nan |= !(v.x * 0.0f + v.y * 0.0f + v.z * 0.0f + v.w * 0.0f == 0.0f);
+      }
+      nan = __any_sync(0xffffffffu, nan);
+    }
+    if (nan) {  // (or an infinity:) a key that a row does not see adds nothing, whatever it holds
 #pragma unroll 1
       for (int t = 0; t < n; ++t) {
         const int vis = g * max(w.t0 + pg * kPage + t - w.ctx, 0) - w.row0;  // rows >= vis see the key

@@ -69,12 +69,13 @@ struct Space {
 Space space(const wisp_attn_args *a, bool shared, int sms) {
   Space s;
   const int g = a->Hq / a->Hkv;
+  const int64_t T = a->B > 0 ? a->total_q_rows : 0;
   s.unit_rows = a->qkv_dtype == WISP_BF16 ? 2 * g * prompt_tile_positions(g) : kF32RowsPerItem;
-  const int64_t units = ((int64_t)a->total_q_rows * g / s.unit_rows + a->B) * (shared ? 2 : 1);
-  const int64_t slot = std::min<int64_t>(s.unit_rows, (int64_t)a->total_q_rows * g) * (a->D + 2) + 4;
+  const int64_t units = (T * g / s.unit_rows + a->B) * (shared ? 2 : 1);
+  const int64_t slot = std::min<int64_t>(s.unit_rows, T * g) * (a->D + 2) + 4;
   const int64_t cuts = (std::min<int64_t>(2 * units * a->Hkv, (int64_t)12 * sms) + 4 * sms) / a->Hkv + 8;
   s.max_rows = units + cuts;
-  s.partial_cap = cuts * a->Hkv * slot + (shared ? 2 * (int64_t)a->total_q_rows * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
+  s.partial_cap = cuts * a->Hkv * slot + (shared ? 2 * T * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;

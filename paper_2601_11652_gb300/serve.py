@@ -14,6 +14,10 @@ VerifyServer(top_n=...) a batch also answers log probabilities of the logit rows
     wisp_kv_reserve_append_rope, wisp_verify_step_kv8, wisp_kv_commit_rope    in the places of the three above
     wisp_verify_committed_tokens, wisp_verify_logprobs                   after the step
 
+A prompt's own attention is part of PagedSessions.prefill(..., q_rows=...) (wisp_prompt_attention, between append and commit).  Sessions
+that PagedSessions.share has given another session's first pages are batched next to each other, and a batch with several of them reads
+those pages once for all (wisp_verify_attention_shared and wisp_verify_accept in the place of the step).
+
 The server's clock advances by the measured
 batch time; every request's completion is checked against its deadline (its SLO), and the measured
 time is recorded beside the estimator's prediction T_hat(B) (Eq. batch_time, Sec. 4.4).  The
@@ -84,7 +88,8 @@ class PagedSessions:
         self.tables = torch.full((n_sessions, max_blocks), -1, dtype=torch.int32, device=self.dev)
         self.ctx = torch.zeros(n_sessions, dtype=torch.int32, device=self.dev)
         self.num_blocks, self.max_blocks, self.Hkv, self.D = num_blocks, max_blocks, Hkv, D
-        self.kv_ws = self.commit_ws = None
+        self.kv_ws = self.commit_ws = self.prompt_ws = None
+        self.prefix = [(-1, 0)] * n_sessions  # per session: whose first pages it shares (an id), and how many
 
     @property
     def projected(self):
@@ -121,9 +126,10 @@ class PagedSessions:
         t = torch.from_numpy(np.ascontiguousarray(a))
         return t.to(self.dev, dtype=torch_dtype) if torch_dtype else t.to(self.dev)
 
-    def prefill(self, sids, k_rows, v_rows, stream=None):
-        """Give sessions `sids` (empty so far) their prefixes: reserve pages for len(k_rows[i]) tokens,
-        write the rows, and commit them all (as a round whose drafts are all accepted)."""
+    def prefill(self, sids, k_rows, v_rows, stream=None, q_rows=None):
+        """Give sessions `sids` their prefixes, or the next chunk of them: reserve pages for len(k_rows[i]) more tokens, write the rows,
+        and commit them all (as a round whose drafts are all accepted).  With q_rows (per session [tokens, Hq, D]) also the attention of
+        those queries over everything up to them: returns its output [all tokens, Hq, D] (device), else None."""
         idx = torch.tensor(sids, dtype=torch.long, device=self.dev)
         lens = [len(x) for x in k_rows]
         draft = torch.tensor([n - 1 for n in lens], dtype=torch.int32, device=self.dev)
@@ -132,17 +138,51 @@ class PagedSessions:
         kn, vn = self._dev(np.concatenate(k_rows)), self._dev(np.concatenate(v_rows))
         batch = dict(draft_lens=draft, context_lens=ctx, block_tables=tables, total_q_rows=int(sum(lens)))
         acc = draft.clone()
-        args = self._append_args(**batch, k_new=kn, v_new=vn, accepted_len=acc)
+        q = out = None
+        if q_rows is not None:
+            if [len(x) for x in q_rows] != lens:
+                raise ValueError("q_rows and k_rows must have the same numbers of rows")
+            q = self._dev(np.concatenate(q_rows))
+            out = torch.empty_like(q)
+        # (queries are rotated beside the append, in place)
+        turn = dict(q=q, q_out=q) if q is not None and self.rope is not None else {}
+        args = self._append_args(**batch, **turn, k_new=kn, v_new=vn, accepted_len=acc)
         ws, cws = self._ws(args)
+        used = [ws, cws]
         self._append(args, ws, stream)
+        if q is not None:
+            a = wb.make_prompt_args(**batch, **self.scales, q=q, k_cache=self.k_cache, v_cache=self.v_cache, out=out,
+                                    num_blocks=self.num_blocks)
+            n = wb.wisp_prompt_workspace_size(a)
+            if self.prompt_ws is None or self.prompt_ws.numel() < n:
+                self.prompt_ws = wb.alloc_workspace(n, self.dev)
+            wb.wisp_prompt_attention(a, self.prompt_ws, stream)
+            used.append(self.prompt_ws)
         self._commit(args, cws, stream)
         torch.cuda.synchronize(self.dev)
-        for w in (ws, cws):
+        for w in used:
             code, rid = wb.wisp_verify_get_device_status(w)
             if code != 0:
                 raise RuntimeError(f"prefill: device status {code} (request {rid})")
         self.tables[idx] = tables
         self.ctx[idx] = ctx
+        return out
+
+    def share(self, src, sids, tokens):
+        """Let the empty sessions `sids` begin with the first `tokens` tokens of session `src`, whole pages of them, without a copy: their
+        block tables name src's pages, which nobody writes again (a commit gives back only pages behind the tokens that it keeps)."""
+        if tokens <= 0 or tokens % PAGE:
+            raise ValueError("only whole pages are shared")
+        if tokens > int(self.ctx[src]):
+            raise ValueError("the source session does not hold that many tokens")
+        idx = torch.tensor(sids, dtype=torch.long, device=self.dev)
+        if src in sids or len(set(sids)) != len(sids) or bool((self.ctx[idx] != 0).any()) or bool((self.tables[idx] != -1).any()):
+            raise ValueError("sessions that share a prefix must be empty before")
+        pages = tokens // PAGE
+        self.tables[idx, :pages] = self.tables[src, :pages]
+        self.ctx[idx] = tokens
+        for sid in [src, *sids]:
+            self.prefix[sid] = (src, pages)
 
 
 @dataclasses.dataclass
@@ -172,9 +212,31 @@ class VerifyServer:
         self.lp_ws = None
         self.Hq, self.V = Hq, V
         self.stream = stream
-        self.ws = None
+        self.ws = self.shared_ws = None
 
     def run_batch(self, sids, payloads) -> BatchResult:
+        """One verification round of sessions `sids`.  Sessions that share pages are put next to each other for it; the results are in
+        the order of `sids`."""
+        shared = [self.s.prefix[sid] for sid in sids]
+        groups = {g: shared.count(g) for g in shared if g[1] > 0}
+        if not any(n > 1 for n in groups.values()):
+            return self._run(sids, payloads, None)
+        order = sorted(range(len(sids)), key=lambda i: shared[i])  # (stable: a group's sessions as they came)
+        res = self._run([sids[i] for i in order], [payloads[i] for i in order], [shared[i] for i in order])
+        back = np.argsort(order)
+        k = np.array([len(payloads[i].draft_tokens) + 1 for i in order])
+        start = np.concatenate([[0], np.cumsum(k)])
+        rows = np.concatenate([np.arange(start[i], start[i + 1]) for i in back])
+        for f in ("accepted_len", "next_token", "block_tables", "context_lens"):
+            setattr(res, f, getattr(res, f)[back])
+        for f in ("row_tokens", "logprob", "entropy", "top_tokens", "top_logprobs"):
+            if getattr(res, f) is not None:
+                setattr(res, f, getattr(res, f)[rows])
+        res.out = res.out[torch.from_numpy(rows).to(res.out.device)]
+        res.sids = list(sids)
+        return res
+
+    def _run(self, sids, payloads, shared) -> BatchResult:
         s, dev = self.s, self.s.dev
         B = len(sids)
         k = [len(p.draft_tokens) for p in payloads]
@@ -199,17 +261,27 @@ class VerifyServer:
         # (queries are rotated beside the append, in place)
         turn = dict(q=q, q_out=q) if s.rope is not None else {}
         kv = s._append_args(**batch, **turn, k_new=kn, v_new=vn, accepted_len=acc, total_q_rows=Tq)
-        attn = (wb.make_attn_kv8_args if s.kv8 else wb.make_attn_args)(
-            **batch, **s.scales, q=q, k_cache=s.k_cache, v_cache=s.v_cache, out=out, num_blocks=s.num_blocks)
-        step = wb.wisp_verify_step_kv8 if s.kv8 else wb.wisp_verify_step
+        pool = dict(**s.scales, q=q, k_cache=s.k_cache, v_cache=s.v_cache, out=out, num_blocks=s.num_blocks)
         accp = wb.make_accept_args(draft_lens=draft, target_logits=logits, draft_tokens=tokens, draft_probs=probs,
                                    accept_uniforms=au, sample_uniforms=su, accepted_len=acc, next_token=tok,
                                    request_ids=rid)
         kws, cws = s._ws(kv)
-        n = wb.wisp_verify_workspace_size(attn.attn if s.kv8 else attn, accp)
+        used = [(kws, "kv"), (cws, "commit")]
+        if shared is None:
+            attn = (wb.make_attn_kv8_args if s.kv8 else wb.make_attn_args)(**batch, **pool)
+            step = wb.wisp_verify_step_kv8 if s.kv8 else wb.wisp_verify_step
+            n = wb.wisp_verify_workspace_size(attn.attn if s.kv8 else attn, accp)
+        else:
+            ids = torch.tensor(shared, dtype=torch.int32, device=dev)
+            attn = wb.make_shared_args(**batch, **pool, shared_ids=ids[:, 0].contiguous(), shared_pages=ids[:, 1].contiguous())
+            n = wb.wisp_verify_shared_workspace_size(attn)
+            if self.shared_ws is None or self.shared_ws.numel() < n:
+                self.shared_ws = wb.alloc_workspace(n, dev)
+            used.append((self.shared_ws, "attention"))
+            n = wb.wisp_verify_workspace_size(None, accp)
         if self.ws is None or self.ws.numel() < n:
             self.ws = wb.alloc_workspace(n, dev)
-        used = [(kws, "kv"), (self.ws, "verify"), (cws, "commit")]
+        used.append((self.ws, "verify"))
         lp = {}
         if self.top_n is not None:
             lp = dict(row_tokens=torch.empty(Tq, dtype=torch.int32, device=dev), logprob=torch.empty(Tq, device=dev),
@@ -228,7 +300,11 @@ class VerifyServer:
             s._append(kv, kws, stream)
             tables_read = tables.clone()  # the rows the step reads (commit rewrites them)
             ctx_read = ctx.clone()
-            step(attn, accp, self.ws, stream)
+            if shared is None:
+                step(attn, accp, self.ws, stream)
+            else:
+                wb.wisp_verify_attention_shared(attn, self.shared_ws, stream)
+                wb.wisp_verify_accept(accp, self.ws, stream)
             if lp:
                 wb.wisp_verify_committed_tokens(accp, lp["row_tokens"], stream)
                 wb.wisp_verify_logprobs(lpa, self.lp_ws, stream)

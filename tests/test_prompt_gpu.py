@@ -226,3 +226,249 @@ def test_more_requests_than_the_planner_has_threads():
     p = Case(5, k=rng.integers(0, 40, B).tolist(), ctx=rng.integers(0, 90, B).tolist(), Hq=4, Hkv=2, D=64)
     p.run()
     p.check()
+
+
+def bits_of(t):
+    return t.view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()])
+
+
+def put(c, x, r, token, d, value):
+    """Element d of all heads of token `token` of request r; returns the value as the cache holds it."""
+    cache = c.t[x + "_cache"]
+    page, slot = int(c.bt[r, token // PAGE]), token % PAGE
+    if cache.dtype == torch.float8_e4m3fn:
+        assert math.isnan(value)
+        bits_of(cache)[page, :, slot, d] = 0x7f
+    else:
+        cache[page, :, slot, d] = value
+    c.val[x][page, :, slot, d] = value
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 4, 64), (14, 2, 64)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_values_that_are_not_finite(dtype, cache, Hq, Hkv, D, shared):
+    """They reach the rows that see them and no others, in their element; everything else is as without them."""
+    k, ctx = [200, 3, 150], [96 + 70, 96, 96 + 1]
+    c = Case(7, k=k, ctx=ctx, runs=runs_of((0, 6, 3)) if shared else None, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype, cache=cache)
+    inf, nan = math.inf, math.nan
+    odd = [(0, ctx[0] + 50, 5, nan), (0, 100, 3, nan), (1, ctx[1] + 2, 1, nan), (2, ctx[2] + 149, 40, nan), (2, ctx[2] + 150, 41, nan)]
+    if not cache:
+        odd += [(0, ctx[0] + 60, 7, inf), (0, ctx[0] + 90, 7, -inf), (0, ctx[0] + 200, 63, -inf), (2, ctx[2], 8, inf), (2, ctx[2] + 128, 9, -inf)]
+    if shared:
+        odd.append((0, 17, 11, nan))  # in the pages of all
+    clean = {x: c.val[x].clone() for x in "kv"}
+    for r, t, d, v in odd:
+        put(c, "v", r, t, d, v)
+    c.val = clean
+    for r, t, d, v in odd:
+        c.val["v"][int(c.bt[r, t // PAGE]), :, t % PAGE, d] = 0
+    c.run()
+    bf = dtype == BF
+    for r in range(3):
+        at = c.row_of(r)
+        ref, mag, _ = c.reference(r, 0, k[r] + 1)
+        got = c.t["out"][at:at + k[r] + 1].double()
+        want = ref.clone()
+        pos = ctx[r] + torch.arange(k[r] + 1, device="cuda")
+        for rr, t, d, v in odd:
+            if rr == r or t < 96 and shared:
+                sees = (pos >= t)[:, None].expand(-1, Hq)
+                col = want[:, :, d]
+                want[:, :, d] = torch.where(sees, torch.where(torch.isinf(col) & (col != v), nan, v if math.isnan(v) else v + 0 * col), col)
+        fine = torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)])
+        bound = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -10) * mag if bf else 2.0 ** -9 * mag
+        assert ((got - want).abs()[fine] <= bound[fine]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_keys_that_are_not_finite(dtype, D):
+    """A NaN key makes the rows that see it NaN; scores of -inf weigh nothing, and a row that has no other is NaN."""
+    k, ctx = [300], [0]
+    c = Case(8, k=k, ctx=ctx, Hq=4, Hkv=2, D=D, dtype=dtype)
+    c.t["q"][:, :, 0] = 1
+    for t in range(130):
+        put(c, "k", 0, t, 0, -math.inf)
+    put(c, "k", 0, 280, 2, math.nan)
+    c.run()
+    got = c.t["out"].double()
+    assert torch.isnan(got[:130]).all() and torch.isnan(got[280:]).all()
+    c.val["k"][torch.isnan(c.val["k"])] = 0
+    ref, mag, _ = c.reference(0, 130, 280)
+    bound = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -10) * mag if dtype == BF else 2.0 ** -9 * mag
+    assert ((got[130:280] - ref).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("grow", [1, -1])
+def test_scores_that_grow_and_fall(dtype, cache, grow):
+    """Maxima that move from tile to tile, by little and by hundreds of powers of two.  Scores are larger than elsewhere, so their error is
+    counted from the inputs: 2^-17 of sum |q k| / sqrt(D) for the sums, as much again for scaling, both in numerator and denominator."""
+    k, ctx = [700, 90], [0, 600]
+    c = Case(9, k=k, ctx=ctx, Hq=4, Hkv=2, D=128, dtype=dtype, cache=cache, runs=None)
+    for r in range(2):
+        L = ctx[r] + k[r] + 1
+        t = torch.arange((L + PAGE - 1) // PAGE * PAGE, device="cuda").view(-1, PAGE)
+        pages = torch.from_numpy(c.bt[r, :len(t)].astype(np.int64)).cuda()
+        e = torch.div(t[:, :1] if cache else t, 40, rounding_mode="floor")
+        f = torch.exp2((e if grow > 0 else e[-1, -1] - e).float() * 0.5)
+        if cache:
+            c.t["k_scale"][pages] *= torch.exp2(torch.floor(torch.log2(f)))
+            c.val["k"][pages] = c.t["k_cache"][pages].double() * c.t["k_scale"][pages].double()[:, :, None, None]
+        else:
+            x = (c.t["k_cache"][pages].float() * f[:, None, :, None]).to(dtype)
+            c.t["k_cache"][pages], c.val["k"][pages] = x, x.double()
+    c.run()
+    for r in range(2):
+        at, L = c.row_of(r), ctx[r] + k[r] + 1
+        ref, mag, _ = c.reference(r, 0, k[r] + 1)
+        ids = torch.from_numpy(c.bt[r, :(L + PAGE - 1) // PAGE].astype(np.int64)).cuda()
+        K = c.val["k"][ids].permute(1, 0, 2, 3).reshape(2, 1, -1, 128)[:, :, :L].abs()
+        q = c.t["q"][at:at + k[r] + 1].double().view(-1, 2, 2, 128).permute(1, 2, 0, 3).abs()
+        see = torch.arange(L, device="cuda") <= ctx[r] + torch.arange(k[r] + 1, device="cuda")[:, None]
+        S = (q @ K.transpose(2, 3) / math.sqrt(128)).masked_fill(~see, 0).amax(3).permute(2, 0, 1).reshape(k[r] + 1, 4, 1)
+        far = torch.expm1(2 * 2.0 ** -16 * S)
+        got = c.t["out"][at:at + k[r] + 1].double()
+        bound = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -20 + far) * mag if dtype == BF else (2.0 ** -18 + far) * mag
+        # (where the largest weights meet zeros of V.)  A weight below 2^-126 of the row's largest is no normal number and counts as zero: fewer
+        # than 2^10 keys of |v| < 2^3 then leave out less than 2^-113
+        bound = bound + 2.0 ** -113
+        assert torch.isfinite(got).all() and bool(((got - ref).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_that_are_no_powers_of_two(D):
+    for dtype in (BF, F32):
+        c = Case(10, k=[150, 20], ctx=[30, 400], Hq=8, Hkv=2, D=D, dtype=dtype, cache="e4m3", exact_scales=dtype == F32)
+        if dtype == F32:  # (any scale is exact in fp32)
+            f = 1.0 + torch.rand(c.t["k_scale"].shape, device="cuda")
+            c.t["k_scale"] *= f
+            c.val["k"] *= f.double()[:, :, None, None]
+        c.run()
+        c.check()
+
+
+def test_refused_requests_leave_the_others():
+    from paper_2601_11652_gb300 import binding as wb
+    # (too long for its table; a negative length; a block outside the pool; a prefix that is shorter than its shared pages)
+    for bad, code in ((dict(ctx=100000), 1), (dict(k=-3), 1), (dict(block=1 << 29), 2), (dict(block=-5), 2), (dict(pages=40), 1)):
+        for dtype in (BF, F32):
+            runs = runs_of((1, 4, 2), (2, 40 if "pages" in bad else 5, 1), (1, 4, 2))
+            c = Case(11, k=[5, 70, 9, 0, 30], ctx=[64, 200, 90, 70, 64], runs=runs if "pages" not in bad else runs_of((1, 4, 2), (2, 5, 1), (1, 4, 2)),
+                     Hq=4, Hkv=2, D=64, dtype=dtype)
+            skipped = [2]
+            if "pages" in bad:
+                c.t["shared_pages"][2] = 40
+            if "ctx" in bad:
+                c.t["context_lens"][2] = bad["ctx"]
+            if "block" in bad:
+                c.t["block_tables"][2, 3] = bad["block"]
+            if "k" in bad:  # its one row stays in the offsets
+                c = Case(11, k=[5, 70, 0, 0, 30], ctx=[64, 200, 90, 70, 64], runs=runs, Hq=4, Hkv=2, D=64, dtype=dtype)
+                c.t["draft_lens"][2] = bad["k"]
+            c.t["request_ids"] = torch.arange(900, 905, device="cuda")
+            assert c.run(expect=code) == 902
+            c.check(skipped=skipped)
+    # a run whose first request is refused takes its pages from the next
+    c = Case(12, k=[3, 4, 5], ctx=[64, 70, 80], runs=runs_of((1, 4, 3)), Hq=4, Hkv=2, D=64)
+    c.t["block_tables"][1, :4] = torch.from_numpy(c.bt[0, :4]).cuda()
+    c.t["context_lens"][0] = 1 << 20
+    c.run(expect=1)
+    c.check(skipped=[0])
+    # rows that the caller's buffers do not have, and rows of nobody
+    c = Case(13, k=[3, 40, 5], ctx=[64, 70, 80], Hq=4, Hkv=2, D=64)
+    a = wb.make_prompt_args(**c.t, total_q_rows=4 + 41)
+    ws = wb.alloc_workspace(wb.wisp_prompt_workspace_size(a))
+    wb.wisp_prompt_attention(a, ws)
+    assert wb.wisp_verify_get_device_status(ws)[0] == 1
+    c.check(skipped=[2])
+    assert (c.t["out"][45:] == 77).all()
+
+
+def test_outputs_behind_the_last_request_stay():
+    from paper_2601_11652_gb300 import binding as wb
+    for runs in (None, runs_of((0, 2, 2))):
+        c = Case(14, k=[3, 40], ctx=[64, 70], Hq=4, Hkv=2, D=128, runs=runs)
+        rows = c.t["q"].shape[0]
+        for n in ("q", "out"):
+            c.t[n] = torch.cat([c.t[n], torch.full((300, 4, 128), 77, dtype=BF, device="cuda")])
+        a = (wb.make_shared_args if runs else wb.make_prompt_args)(**c.t, total_q_rows=rows)
+        size, call = (wb.wisp_verify_shared_workspace_size, wb.wisp_verify_attention_shared) if runs else \
+            (wb.wisp_prompt_workspace_size, wb.wisp_prompt_attention)
+        ws = wb.alloc_workspace(size(a))
+        call(a, ws)
+        assert wb.wisp_verify_get_device_status(ws)[0] == 0
+        c.check()
+        assert (c.t["out"][rows:] == 77).all()
+
+
+def test_an_empty_batch():
+    from paper_2601_11652_gb300 import binding as wb
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    t = dict(draft_lens=i(0), context_lens=i(0), block_tables=i(0, 1), q=torch.zeros((0, 4, 64), dtype=BF, device="cuda"),
+             k_cache=torch.zeros((1, 2, 16, 64), dtype=BF, device="cuda"), v_cache=torch.zeros((1, 2, 16, 64), dtype=BF, device="cuda"))
+    t["out"] = torch.empty_like(t["q"])
+    a = wb.make_prompt_args(**t)
+    ws = wb.alloc_workspace(wb.wisp_prompt_workspace_size(a))
+    wb.wisp_prompt_attention(a, ws)
+    assert wb.wisp_verify_get_device_status(ws)[0] == 0
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_repeats_to_the_bit_on_streams_and_in_graphs(dtype, cache):
+    """Two cases on two streams at once, each with its workspace, then both captured and replayed on other inputs in the same buffers."""
+    from paper_2601_11652_gb300 import binding as wb
+    cases = [Case(15, k=[900, 3], ctx=[200, 5000], Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache),
+             Case(16, k=[3, 0, 7], ctx=[4000, 3900, 4100], runs=runs_of((0, 240, 3)), Hq=8, Hkv=2, D=64, dtype=dtype, cache=cache)]
+    for c in cases:
+        c.run()
+        c.check()
+    want = [c.t["out"].clone() for c in cases]
+    calls = []
+    for c in cases:
+        c.t["out"].fill_(0)
+        a, n, call = c.args()
+        calls.append((a, wb.alloc_workspace(n), call))
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (a, ws, call), s in zip(calls, streams):
+            call(a, ws, s)
+    torch.cuda.synchronize()
+    for c, w in zip(cases, want):
+        assert torch.equal(c.t["out"], w)
+    for c, (a, ws, call) in zip(cases, calls):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(a, ws)
+        for f in (0.5, -1.0):
+            c.t["q"].mul_(f)
+            c.t["out"].fill_(0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert wb.wisp_verify_get_device_status(ws)[0] == 0
+            c.check()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 2^32 bytes, its pages from the far end."""
+    nb = (1 << 32) // (8 * PAGE * 128 * 2) + 400
+    for cache in (None, "e4m3"):
+        c = Case(17, k=[300, 2], ctx=[40, 900], Hq=16, Hkv=8, D=128, cache=cache)
+        have = c.t["k_cache"].shape[0]
+        for x in "kv":
+            big = torch.zeros((nb, 8, PAGE, 128), dtype=c.t["k_cache"].dtype, device="cuda")
+            bits_of(big)[-have:] = bits_of(c.t[x + "_cache"])
+            c.t[x + "_cache"] = big
+            if cache:
+                s = torch.zeros((nb, 8), device="cuda")
+                s[-have:] = c.t[x + "_scale"]
+                c.t[x + "_scale"] = s
+        c.t["block_tables"] = torch.where(c.t["block_tables"] >= 0, c.t["block_tables"] + (nb - have), c.t["block_tables"])
+        c.run()
+        c.check()
+        del big
+        c.t.clear()
+        torch.cuda.empty_cache()
