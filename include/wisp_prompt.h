@@ -28,7 +28,9 @@ extern "C" {
  * Supported: D in {64, 128}, block_size == 16, Hq / Hkv <= 128, k_r < 2^24.
  * Scores, softmax statistics and outputs accumulate in fp32.  With bf16 queries a weight enters the second product in bf16
  * (relative error 2^-9), and so do code * scale of an e4m3 cache, K and V (exactly where the scale is a power of two of magnitude 2^-100
- * to 2^100; values past the bf16 range count as its largest).  With fp32 queries every product is in fp32.
+ * to 2^100; values past the bf16 range count as its largest).  With fp32 queries every factor enters its product with
+ * 22 significant bits or more: queries, and K and V of an fp32 cache, down to steps of 2^-38 of the largest value of their row; a weight times its
+ * key's largest |V| (its V scale) down to steps of 2^-36 of the row's largest weight times the largest such value among 64 consecutive keys.
  * A key that a row does not see adds nothing to it, whatever its K and V hold (NaN and infinities too; slots past a request's
  * tokens may hold anything).  A NaN that a row does see, or a row whose scores are all -inf, makes that row NaN (of V: in its element).
  */

@@ -20,18 +20,8 @@ struct AttnParams {
   float *partials;
   int row_groups;      // row groups per (request, head) at most
   int32_t *pair_done;  // [B * Hkv * row_groups] finished chunks of each split (request, head, row group), zeroed
-                       // by the planner; null (prompt.cuh): another kernel joins the partials
+                       // by the planner
 };
-
-// Item `it` of the list.  Where the list stands for all KV heads (prompt.cuh) an entry's nrg is the distance of its heads' partials.
-__device__ __forceinline__ WorkItem item_at(const AttnParams &p, int it) {
-  if (p.pair_done) return p.items[it];
-  const int row = it / p.Hkv;
-  WorkItem w = p.items[row];
-  w.h = it - row * p.Hkv;
-  if (w.poff >= 0) w.poff += w.h * w.nrg;
-  return w;
-}
 
 // Host launchers (defined next to their kernels): programmatic dependents of the planner, which they wait for
 // before they read the plan.

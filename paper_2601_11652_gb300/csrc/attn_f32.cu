@@ -262,15 +262,7 @@ __device__ __forceinline__ void item_rows(const AttnParams &p, const WorkItem &w
         for (int d = lane; d < D; d += 32) vb[t * C::LD + d] = 0.0f;
       __syncwarp();
     }
-    if (!KV8 && w.t0 + pg * kPage + n - 1 > w.ctx + w.row0 / g) {  // (a key that some row does not see)
-#pragma unroll 4
-      for (int c = lane; c < n * (D / 4); c += 32) {
-        const float4 v = *reinterpret_cast<const float4 *>(vb + c / (D / 4) * C::LD + c % (D / 4) * 4);
-        nan |= !(v.x * 0.0f + v.y * 0.0f + v.z * 0.0f + v.w * 0.0f == 0.0f);
-      }
-      nan = __any_sync(0xffffffffu, nan);
-    }
-    if (nan) {  // (or an infinity:) a key that a row does not see adds nothing, whatever it holds
+    if (KV8 && nan) {  // a key that a row does not see adds nothing, whatever it holds
 #pragma unroll 1
       for (int t = 0; t < n; ++t) {
         const int vis = g * max(w.t0 + pg * kPage + t - w.ctx, 0) - w.row0;  // rows >= vis see the key
@@ -364,13 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
       do {
         it = atomicAdd(&p.header_mut->next_item, 1);
         if (it >= n_items) it = -1;
-      } while (it >= 0 && p.pair_done && p.items[it].t1 <= p.items[it].t0);  // (a refused request's items are empty)
+      } while (it >= 0 && p.items[it].t1 <= p.items[it].t0);  // (a refused request's items are empty)
       sh.item = it;
     }
     __syncthreads();  // (also: the previous item's shared memory is no longer read)
     const int it = sh.item;
     if (it < 0 || *(volatile int *)&sh.abort_) break;
-    const WorkItem w = item_at(p, it);
+    const WorkItem w = p.items[it];
     // the item's query rows (rows past `rows` up to the lanes' share read as zero)
     const int rl = (w.rows + 3) / 4;
     const float *qg = static_cast<const float *>(p.q);
@@ -425,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_f32_kernel(const __grid_cons
         }
       }
     }
-    if (w.poff >= 0 && p.pair_done) {
+    if (w.poff >= 0) {
       // split: the last chunk of this (request, head, row group) to finish merges all
       __threadfence();
       __syncthreads();

@@ -5,7 +5,7 @@
 // query rows over its own keys [P_r, c_r + k_r + 1), where P_r is its run's shared prefix or 0; run i of requests that share
 // pages is segment B + i, all its rows over keys [0, P).  A segment's rows are cut into units of `unit_rows`, its keys into chunks
 // of its chunk length; an item (plan.cuh) is a chunk of a unit of one KV head.  The list holds them without the head: entry i / Hkv and head
-// i mod Hkv make item i (item_at, attn.cuh).  Where a row has its keys in more than one item
+// i mod Hkv make item i (item_at).  Where a row has its keys in more than one item
 // the items leave partials (O, m, l), and merge_kernel joins them.
 #pragma once
 
@@ -43,9 +43,9 @@ static_assert(offsetof(PromptHeader, h) == 0, "the kernels that read a PlanHeade
 
 struct PromptPlan {
   int B, Hq, Hkv, D, max_blocks_per_seq, total_q_rows;
-  int unit_rows;       // rows of a unit: whole positions of the tensor-core kernel's two tiles, or the fp32 kernel's row limit
+  int unit_rows;       // rows of a unit: whole positions of the kernel's two tiles (bf16 queries) or of its one (fp32)
   int sms;
-  int grid;            // CTAs of the tensor-core kernel: each has taken its first item by its index; 0 for the other kernel
+  int grid;            // CTAs of the attention kernel: each takes its first item by its index
   int64_t max_rows, partial_cap;  // list entries, floats
   const int32_t *draft_lens, *context_lens, *shared_ids, *shared_pages;  // shared_*: null without runs
   const int64_t *request_ids;
@@ -63,6 +63,15 @@ struct PromptPlan {
   void *out;
 };
 
+// Item `it` of the list.  An entry's nrg is the distance of its heads' partials.
+__device__ __forceinline__ WorkItem item_at(const AttnParams &p, int it) {
+  const int row = it / p.Hkv;
+  WorkItem w = p.items[row];
+  w.h = it - row * p.Hkv;
+  if (w.poff >= 0) w.poff += w.h * w.nrg;
+  return w;
+}
+
 // Rows of a segment that share a partial's slot, and floats of a slot.
 __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D + 2) + 3) / 4 * 4; }
 
@@ -70,9 +79,12 @@ cudaError_t prompt_plan_setup();  // once per device: shared-memory attributes
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s);
 cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s);
 
-// tcgen05 kernel (bf16 queries): query positions of one of an item's two 128-row tiles
+// query positions of a tile of 128 rows
 inline int prompt_tile_positions(int g) { return 128 / g; }
 cudaError_t prompt_tc_setup();
 cudaError_t prompt_tc_launch(const AttnParams &p, int total_q_rows, int grid, cudaStream_t s);
+// tcgen05 kernel for fp32 queries: an item is one tile
+cudaError_t prompt_f32_setup();
+cudaError_t prompt_f32_launch(const AttnParams &p, int grid, cudaStream_t s);
 
 }  // namespace wisp

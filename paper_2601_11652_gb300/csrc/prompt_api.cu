@@ -22,7 +22,7 @@ wisp_status setup(int *sms) {
   if (!g_sms[dev]) {
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return WISP_ERR_CUDA;
-    if (attn_f32_setup() != cudaSuccess || prompt_tc_setup() != cudaSuccess || prompt_plan_setup() != cudaSuccess) return WISP_ERR_CUDA;
+    if (prompt_f32_setup() != cudaSuccess || prompt_tc_setup() != cudaSuccess || prompt_plan_setup() != cudaSuccess) return WISP_ERR_CUDA;
     g_sms[dev] = n;
   }
   *sms = g_sms[dev];
@@ -70,7 +70,7 @@ Space space(const wisp_attn_args *a, bool shared, int sms) {
   Space s;
   const int g = a->Hq / a->Hkv;
   const int64_t T = a->B > 0 ? a->total_q_rows : 0;
-  s.unit_rows = a->qkv_dtype == WISP_BF16 ? 2 * g * prompt_tile_positions(g) : kF32RowsPerItem;
+  s.unit_rows = (a->qkv_dtype == WISP_BF16 ? 2 : 1) * g * prompt_tile_positions(g);
   const int64_t units = (T * g / s.unit_rows + a->B) * (shared ? 2 : 1);
   const int64_t slot = std::min<int64_t>(s.unit_rows, T * g) * (a->D + 2) + 4;
   const int64_t cuts = (std::min<int64_t>(2 * units * a->Hkv, (int64_t)12 * sms) + 4 * sms) / a->Hkv + 8;
@@ -148,7 +148,7 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   p.partials = at<float>(ws, sp.partials);
   p.out = a->out;
   const int grid = (int)(sp.max_rows * a->Hkv < sms ? sp.max_rows * a->Hkv : sms);
-  p.grid = bf ? grid : 0;
+  p.grid = grid;
   if (prompt_plan_launch(p, s) != cudaSuccess) return WISP_ERR_CUDA;
   if (a->B == 0) return WISP_OK;
   AttnParams ap;
@@ -173,8 +173,8 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   ap.header = &p.header->h;
   ap.header_mut = &p.header->h;
   ap.items = p.items;
-  ap.partials = p.partials;  // (pair_done stays null: the merge kernel joins them)
-  cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : attn_f32_launch(ap, grid, s);
+  ap.partials = p.partials;
+  cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : prompt_f32_launch(ap, grid, s);
   if (e == cudaSuccess) e = prompt_merge_launch(p, !bf, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
