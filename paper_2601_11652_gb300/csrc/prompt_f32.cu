@@ -201,9 +201,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   bool ok = true;
   if (warp < 4) {
-    // registers: 16 warps launch with 128 each, 512 a lane and warp of a scheduler = 232 + 112 + 112 + 56.  (Each split stands at the head of its
+    // registers: 16 warps launch with 128 each, 512 a lane and warp of a scheduler = 248 + 104 + 104 + 56.  (Each split stands at the head of its
     // own branch: after a join the compiler counts with the least.)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 248;");
     // ------------------------------------------------------------------ softmax and epilogue, a row per thread
     const int row = threadIdx.x;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
     }
   } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     // ------------------------------------------------------------------ tiles into halves: K by warps 4-7, V by 8-11, two threads per key
     const bool is_k = warp < 8;
     const int id = (threadIdx.x & 127), key = id >> 1, half = id & 1;
@@ -485,50 +485,70 @@ __global__ void __launch_bounds__(kThreads, 1)
         float f;  // the key's factor
         bool nonfinite = false;
         constexpr int G = E / 8;  // groups of eight elements, from one of its own on (so that lanes read different banks)
+        constexpr int ES = KV8 ? 1 : 4;
+        uint8_t *src = tile + key * (D * ES) + half * (E * ES);
+        // Values that are not finite become zeros, remembered with the first position that sees them; the row is then read once more.
+        // (A NaN code of K stays: its scores are NaN.)
+        auto patch = [&]() {
+          nonfinite = true;
+#pragma unroll 1
+          for (int i = 0; i < E; ++i) {
+            int kind;
+            if (KV8) {
+              if ((src[i] & 0x7f) != 0x7f) continue;
+              src[i] = 0;
+              kind = 0;
+            } else {
+              float *x = reinterpret_cast<float *>(src) + i;
+              if (fabsf(*x) < INFINITY) continue;
+              kind = *x != *x ? 0 : *x > 0.0f ? 1 : 2;
+              *x = 0.0f;
+            }
+            if (!is_k && real) {
+              atomicMin(&s_odd[(ob * 3 + kind) * D + half * E + i], max(at_key - w.ctx, 0));
+              s_isodd[ob] = 1;
+            }
+          }
+        };
         if constexpr (KV8) {
-          const uint8_t *src = tile + key * D + half * E;
+#pragma unroll 1
+          for (int pass = 0; pass < 2; ++pass) {
+            __half2 any = __floats2half2_rn(0.0f, 0.0f);
+            const __half2 zero = any;
 #pragma unroll
-          for (int i = 0; i < G; ++i) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(src + ((i + id) % G) * 8);
-            h[4 * i] = e4m3x2_to_h2(u.x & 0xffffu);
-            h[4 * i + 1] = e4m3x2_to_h2(u.x >> 16);
-            h[4 * i + 2] = e4m3x2_to_h2(u.y & 0xffffu);
-            h[4 * i + 3] = e4m3x2_to_h2(u.y >> 16);
+            for (int i = 0; i < G; ++i) {
+              const uint2 u = *reinterpret_cast<const uint2 *>(src + ((i + id) % G) * 8);
+              h[4 * i] = e4m3x2_to_h2(u.x & 0xffffu);
+              h[4 * i + 1] = e4m3x2_to_h2(u.x >> 16);
+              h[4 * i + 2] = e4m3x2_to_h2(u.y & 0xffffu);
+              h[4 * i + 3] = e4m3x2_to_h2(u.y >> 16);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) any = __hfma2(*reinterpret_cast<const __half2 *>(&h[4 * i + q]), zero, any);
+            }
+            if (is_k || __low2float(any) + __high2float(any) == 0.0f) break;
+            patch();
           }
           f = sc;
         } else {
-          float v[E];
-          const uint8_t *src = tile + key * (D * 4) + half * (E * 4);
-#pragma unroll
-          for (int i = 0; i < G; ++i) {
-            const float4 a = *reinterpret_cast<const float4 *>(src + ((i + id) % G) * 32);
-            const float4 b = *reinterpret_cast<const float4 *>(src + ((i + id) % G) * 32 + 16);
-            v[8 * i] = a.x; v[8 * i + 1] = a.y; v[8 * i + 2] = a.z; v[8 * i + 3] = a.w;
-            v[8 * i + 4] = b.x; v[8 * i + 5] = b.y; v[8 * i + 6] = b.z; v[8 * i + 7] = b.w;
-          }
-          float amax = 0.0f, any = 0.0f;
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            any = fmaf(v[i], 0.0f, any);
-            amax = fmaxf(amax, fabsf(v[i]));
-          }
-          if (any != 0.0f) {  // (NaN where a value is not finite)
-            nonfinite = true;
+          float v[E], amax;
+#pragma unroll 1
+          for (int pass = 0; pass < 2; ++pass) {
+            float any = 0.0f;
             amax = 0.0f;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-              if (fabsf(v[i]) < INFINITY) {
-                amax = fmaxf(amax, fabsf(v[i]));
-              } else if (!is_k) {
-                if (real) {
-                  const int d = half * E + ((i / 8 + id) % G) * 8 + i % 8;
-                  const int kind = v[i] != v[i] ? 0 : v[i] > 0.0f ? 1 : 2;
-                  atomicMin(&s_odd[(ob * 3 + kind) * D + d], max(at_key - w.ctx, 0));  // the first position that sees it
-                  s_isodd[ob] = 1;
-                }
-                v[i] = 0.0f;
-              }
+            for (int i = 0; i < G; ++i) {
+              const float4 a = *reinterpret_cast<const float4 *>(src + ((i + id) % G) * 32);
+              const float4 b = *reinterpret_cast<const float4 *>(src + ((i + id) % G) * 32 + 16);
+              v[8 * i] = a.x; v[8 * i + 1] = a.y; v[8 * i + 2] = a.z; v[8 * i + 3] = a.w;
+              v[8 * i + 4] = b.x; v[8 * i + 5] = b.y; v[8 * i + 6] = b.z; v[8 * i + 7] = b.w;
             }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              any = fmaf(v[i], 0.0f, any);
+              amax = fmaxf(amax, fabsf(v[i]));
+            }
+            if (any == 0.0f) break;
+            patch();
           }
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
           const int e = row_exp(amax);
@@ -536,21 +556,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           f = pow2(e);
 #pragma unroll
           for (int i = 0; i < E; i += 2) split2(v[i] * s, v[i + 1] * s, h[i / 2], l[i / 2]);
-        }
-        if (KV8 && !is_k) {  // NaN codes
-#pragma unroll
-          for (int i = 0; i < E / 2; ++i) {
-            const float2 v = h2_to_f2(h[i]);
-            if (v.x != v.x || v.y != v.y) {
-              const int d = half * E + ((i / 4 + id) % G) * 8 + 2 * (i % 4);
-              if (real) {
-                if (v.x != v.x) atomicMin(&s_odd[ob * 3 * D + d], max(at_key - w.ctx, 0));
-                if (v.y != v.y) atomicMin(&s_odd[ob * 3 * D + d + 1], max(at_key - w.ctx, 0));
-                s_isodd[ob] = 1;
-              }
-              h[i] = h2(v.x != v.x ? 0.0f : v.x, v.y != v.y ? 0.0f : v.y);
-            }
-          }
         }
         if (!real) f = 0.0f;
         if (is_k) {
