@@ -129,7 +129,7 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   p.total_q_rows = a->total_q_rows;
   p.unit_rows = sp.unit_rows;
   p.sms = sms;
-  p.merge_heads = (int64_t)a->total_q_rows * a->Hkv >= 16 * sms ? a->Hq / a->Hkv : 1;
+  p.merge_heads = (int64_t)a->total_q_rows * a->Hkv >= 4 * sms ? a->Hq / a->Hkv : 1;
   p.max_rows = sp.max_rows;
   p.partial_cap = sp.partial_cap;
   p.draft_lens = a->draft_lens;

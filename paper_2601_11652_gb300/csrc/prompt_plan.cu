@@ -21,7 +21,7 @@ constexpr int kTile = 128;         // and are whole key tiles
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys
 constexpr int kMaxRows = 1 << 24;  // k_r limit
 constexpr int kMergeThreads = 128;
-constexpr int kFew = 4;            // chunks of a row that a warp of the merge has in registers at once
+constexpr int kFew = 4, kHeads = 4; // chunks of a row, and rows, that a warp of the merge has in registers at once
 
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
 template <typename T>
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 }
 
 // The partials of a row joined: O = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m = max m_i.  A warp takes a query position and a KV
-// head, one row after the other (where units are whole positions they lie in one unit; single rows where rows are few); grid columns are requests, so that no row has to
+// head, kHeads rows at a time (units are whole positions, so they lie in one; single rows where rows are few); grid columns are requests, so that no row has to
 // look for its own.  Up to kFew chunks, as almost always, every lane computes their weights itself.  Bound by instructions, then by the
 // partials' bytes (mostly in L2).
 template <int D, typename T>
@@ -386,7 +386,6 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   if (!p.header->partials) return;
   const int lane = threadIdx.x & 31;
   const int g = p.Hq / p.Hkv, R = p.unit_rows;
-  const bool whole = R % g == 0;
   constexpr int CPL = D / 32;
   for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
     const Segment own = p.segs[r];
@@ -396,98 +395,114 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
     const int subs = g / p.merge_heads, work = own.npos * p.Hkv * subs;
     for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
       const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
+      // per segment (0: the run's, 1: the request's own): a row's first O and m, the distance of chunks and how many
+      struct Where {
+        const float *po[2], *pm[2];
+        int step[2], n[2], nl[2];
+      };
+      auto where = [&](int hh) {
+        Where w;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const Segment &s = i == 0 ? pre : own;
+          const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
+          const int rows = min(R, s.npos * g - u * R);
+          w.step[i] = slot_floats(rows, D);
+          w.nl[i] = rows;
+          w.n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
+          const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
+          w.po[i] = base + rr * D + lane * CPL;
+          w.pm[i] = base + rows * D + rr;
+        }
+        return w;
+      };
+      Where w = where(h0);
       T *dst = static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + hk * g + h0) * D + lane * CPL;
-      // per segment (0: the run's, 1: the request's own): the row's first O and m, the distance of chunks and how many
-      const float *po[2], *pm[2];
-      int step[2], n[2], nl[2];
-      for (int hh = h0; hh < h0 + p.merge_heads; ++hh, dst += D) {
-        if (hh == h0 || !whole) {
+      // a chunk none of whose keys a row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
+      if (w.n[0] + w.n[1] <= kFew) {
+        const int total = w.n[0] + w.n[1];
+        if (total == 1 && !own.shared) continue;  // (a unit that no cut fell in)
+        for (int hh = 0; hh < p.merge_heads; hh += kHeads) {
+          // all loads of kHeads rows first
+          float v[kHeads][kFew][CPL], mc[kHeads][kFew], lc[kHeads][kFew];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const Segment &s = i == 0 ? pre : own;
-            const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
-            const int rows = min(R, s.npos * g - u * R);
-            step[i] = slot_floats(rows, D);
-            nl[i] = rows;
-            n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
-            const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
-            po[i] = base + rr * D + lane * CPL;
-            pm[i] = base + rows * D + rr;
-          }
-        } else {
+          for (int x = 0; x < kHeads; ++x)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            po[i] += D;
-            pm[i] += 1;
+            for (int c = 0; c < kFew; ++c) {
+              mc[x][c] = -INFINITY;
+              lc[x][c] = 0.0f;
+              if (c < total && hh + x < p.merge_heads) {
+                const bool z = c < w.n[0];
+                const int at = z ? c * w.step[0] : (c - w.n[0]) * w.step[1];
+                const float *q = (z ? w.pm[0] : w.pm[1]) + at + hh + x;
+                mc[x][c] = __ldcg(q);
+                lc[x][c] = __ldcg(q + (z ? w.nl[0] : w.nl[1]));
+                ld_cols<CPL>((z ? w.po[0] : w.po[1]) + at + (hh + x) * D, v[x][c]);
+              }
+            }
+#pragma unroll
+          for (int x = 0; x < kHeads; ++x) {
+            if (hh + x >= p.merge_heads) break;
+            float m = -INFINITY, den = 0.0f, acc[CPL];
+#pragma unroll
+            for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kFew; ++c) m = fmaxf(m, mc[x][c]);
+#pragma unroll
+            for (int c = 0; c < kFew; ++c) {
+              if (mc[x][c] == -INFINITY) {
+                den += lc[x][c];
+              } else {
+                const float f = ptx::ex2(mc[x][c] - m);
+                den = fmaf(lc[x][c], f, den);
+#pragma unroll
+                for (int q = 0; q < CPL; ++q) acc[q] = fmaf(v[x][c][q], f, acc[q]);
+              }
+            }
+            st_cols<CPL>(dst + (hh + x) * D, acc, 1.0f / den);
           }
         }
-        const int total = n[0] + n[1];
-        if (total == 1 && !own.shared) continue;  // (a unit that no cut fell in)
-        auto at = [&](const float *const (&base)[2], int c) { return c < n[0] ? base[0] + c * step[0] : base[1] + (c - n[0]) * step[1]; };
-        float den = 0.0f, acc[CPL];
+        continue;
+      }
+      for (int hh = 0; hh < p.merge_heads; ++hh, dst += D) {
+        const int total = w.n[0] + w.n[1];
+        auto at = [&](const float *const (&base)[2], int c) {
+          return c < w.n[0] ? base[0] + c * w.step[0] : base[1] + (c - w.n[0]) * w.step[1];
+        };
+        float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
         for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
-        // a chunk none of whose keys the row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
-        if (total <= kFew) {
-          float v[kFew][CPL], mc[kFew], lc[kFew], m = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < kFew; ++c) {
-            mc[c] = -INFINITY;
-            lc[c] = 0.0f;
-            if (c < total) {
-              const float *q = at(pm, c);
-              mc[c] = __ldcg(q);
-              lc[c] = __ldcg(q + (c < n[0] ? nl[0] : nl[1]));
-              ld_cols<CPL>(at(po, c), v[c]);
-            }
+        for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
+          const int c = c0 + lane;
+          float mc = -INFINITY, lc = 0.0f;
+          if (c < total) {
+            const float *q = at(w.pm, c) + hh;
+            mc = __ldcg(q);
+            lc = __ldcg(q + (c < w.n[0] ? w.nl[0] : w.nl[1]));
           }
+          const float mn = fmaxf(m, ptx::warp_max(mc));
+          if (mn != m) {
+            const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
+            den = m == -INFINITY ? den : den * a;
 #pragma unroll
-          for (int c = 0; c < kFew; ++c) m = fmaxf(m, mc[c]);
-#pragma unroll
-          for (int c = 0; c < kFew; ++c) {
-            if (mc[c] == -INFINITY) {
-              den += lc[c];
-            } else {
-              const float w = ptx::ex2(mc[c] - m);
-              den = fmaf(lc[c], w, den);
-#pragma unroll
-              for (int q = 0; q < CPL; ++q) acc[q] = fmaf(v[c][q], w, acc[q]);
-            }
+            for (int q = 0; q < CPL; ++q) acc[q] *= a;
+            m = mn;
           }
-        } else {
-          float m = -INFINITY;
-          for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
-            const int c = c0 + lane;
-            float mc = -INFINITY, lc = 0.0f;
-            if (c < total) {
-              const float *q = at(pm, c);
-              mc = __ldcg(q);
-              lc = __ldcg(q + (c < n[0] ? nl[0] : nl[1]));
-            }
-            const float mn = fmaxf(m, ptx::warp_max(mc));
-            if (mn != m) {
-              const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
-              den = m == -INFINITY ? den : den * a;
-#pragma unroll
-              for (int q = 0; q < CPL; ++q) acc[q] *= a;
-              m = mn;
-            }
-            const float w = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
-            den = mc == -INFINITY ? den + lc : fmaf(lc, w, den);
-            const int nc = min(32, total - c0);
+          const float f = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
+          den = mc == -INFINITY ? den + lc : fmaf(lc, f, den);
+          const int nc = min(32, total - c0);
 #pragma unroll 4
-            for (int i = 0; i < nc; ++i) {
-              const float wi = __shfl_sync(0xffffffffu, w, i);
-              float v[CPL];
-              ld_cols<CPL>(at(po, c0 + i), v);
+          for (int i = 0; i < nc; ++i) {
+            const float fi = __shfl_sync(0xffffffffu, f, i);
+            float v[CPL];
+            ld_cols<CPL>(at(w.po, c0 + i) + hh * D, v);
 #pragma unroll
-              for (int q = 0; q < CPL; ++q)
-                if (!(wi < 0.0f)) acc[q] = fmaf(v[q], wi, acc[q]);
-            }
+            for (int q = 0; q < CPL; ++q)
+              if (!(fi < 0.0f)) acc[q] = fmaf(v[q], fi, acc[q]);
           }
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
         }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
         st_cols<CPL>(dst, acc, 1.0f / den);
       }
     }
@@ -509,8 +524,8 @@ cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  // about 16 CTAs per SM, or one per four warps that have work
-  const int most = p.sms * 16;
+  // about 12 CTAs per SM (three fit), or one per four warps that have work
+  const int most = p.sms * 12;
   const int64_t ctas = std::min<int64_t>(most, ((int64_t)p.total_q_rows * p.Hq / p.merge_heads + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
   const int cols = std::min(p.B, most);
   cfg.gridDim = dim3((unsigned)cols, (unsigned)((ctas + cols - 1) / cols));
