@@ -12,7 +12,7 @@ namespace wisp {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kMaxThreads = 1024;  // of the planner: see prompt_plan_launch
 constexpr int kPage = 16;
 constexpr int kBuckets = 1024;     // of the dispatch order, by key tiles of 64
 constexpr int kMinKeys = 256;      // chunks are not shorter, nor
@@ -26,7 +26,7 @@ constexpr int kFew = 4, kHeads = 4; // chunks of a row, and rows, that a warp of
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
 template <typename T>
 __device__ T scan_incl(T v, T *s_w, T *total) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const T o = __shfl_up_sync(0xffffffffu, v, d);
@@ -34,7 +34,7 @@ __device__ T scan_incl(T v, T *s_w, T *total) {
   }
   if (lane == 31) s_w[w] = v;
   __syncthreads();
-  T t = s_w[lane];
+  T t = lane < warps ? s_w[lane] : (T)0;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const T o = __shfl_up_sync(0xffffffffu, t, d);
@@ -68,18 +68,22 @@ __device__ __forceinline__ int unit_chunks(const Segment &s, int u, int end) { r
 }  // namespace
 
 // What the planner keeps in shared memory where all segments fit: run_info and the segments.
+template <int kThreads>
 struct PlanShared {
   int32_t run[4 * kThreads];
   Segment segs[kThreads];
 };
 
-// One CTA, bound by latency: global loads of the lengths, then barriers.  With at most kThreads requests and segments nothing else goes
+// One CTA.  Its warps all go through all of the code, so what bounds it is their number times the code's length (32 warps: 15400 cycles for one
+// request, THREADS128 with 4): it gets about as many threads as there are segments and list entries.  With at most kThreads requests and segments nothing else goes
 // through global memory, and a list entry stands for all KV heads (an item is an entry and a head), so that most batches have at
 // most one per thread.  48 prompts of up to 1500 tokens, 590 entries: PLAN_US us.
+template <int kThreads>
 __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPlan p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ __align__(16) uint8_t plan_smem[];
-  PlanShared &sh = *reinterpret_cast<PlanShared *>(plan_smem);
+  PlanShared<kThreads> &sh = *reinterpret_cast<PlanShared<kThreads> *>(plan_smem);
+  constexpr int kOwn = kBuckets / kThreads;  // buckets of a thread
   __shared__ int64_t s_scan[2][32];
   __shared__ int s_iscan[4][32];
   __shared__ unsigned long long s_keys, s_units, s_rows, s_floats;
@@ -95,8 +99,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     s_keys = s_units = 0;
     s_any = 0;
   }
-  s_hist[tid] = 0;
-  static_assert(kBuckets == kThreads, "one bucket per thread");
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) s_hist[kOwn * tid + i] = 0;
   const int64_t cap_tokens = (int64_t)p.max_blocks_per_seq * kPage;
   const bool one = p.B <= kThreads;  // every request has a thread
   const int RS = one ? kThreads : p.B;
@@ -355,11 +359,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       __syncthreads();
     }
     if (pass == 0) {
-      const int n = s_hist[tid];
-      int total;
-      const int at = scan_incl<int>(n, s_iscan[3], &total) - n;
-      __syncthreads();
-      s_hist[tid] = at;
+      int n[kOwn], sum = 0, total;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) sum += n[i] = s_hist[kOwn * tid + i];
+      int at = scan_incl<int>(sum, s_iscan[3], &total) - sum;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {  // (a thread's own)
+        s_hist[kOwn * tid + i] = at;
+        at += n[i];
+      }
       if (tid == 0) {
         PromptHeader hd;
         memset(&hd, 0, sizeof hd);
@@ -509,12 +517,34 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
   }
 }
 
+namespace {
+
+template <int kThreads>
+cudaError_t plan_setup() {
+  return cudaFuncSetAttribute(prompt_plan_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanShared<kThreads>));
+}
+template <int kThreads>
+void plan_launch(const PromptPlan &p, cudaStream_t s) {
+  prompt_plan_kernel<kThreads><<<1, kThreads, sizeof(PlanShared<kThreads>), s>>>(p);
+}
+
+}  // namespace
+
 cudaError_t prompt_plan_setup() {
-  return cudaFuncSetAttribute(prompt_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PlanShared));
+  cudaError_t e = plan_setup<128>();
+  if (e == cudaSuccess) e = plan_setup<256>();
+  if (e == cudaSuccess) e = plan_setup<512>();
+  return e == cudaSuccess ? plan_setup<kMaxThreads>() : e;
 }
 
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s) {
-  prompt_plan_kernel<<<1, kThreads, sizeof(PlanShared), s>>>(p);
+  // threads: requests and a few runs have one each, list entries about one (their number is bounded by the rows)
+  const int segs = p.B + (p.shared_ids ? 32 : 0);
+  const int64_t most = std::max<int64_t>(segs, (int64_t)p.total_q_rows * (p.Hq / p.Hkv) / p.unit_rows + p.B);
+  if (most <= 128) plan_launch<128>(p, s);
+  else if (most <= 256) plan_launch<256>(p, s);
+  else if (most <= 512) plan_launch<512>(p, s);
+  else plan_launch<kMaxThreads>(p, s);
   return cudaGetLastError();
 }
 
