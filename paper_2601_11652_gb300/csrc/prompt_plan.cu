@@ -71,7 +71,10 @@ __device__ __forceinline__ int unit_chunks(const Segment &s, int u, int end) { r
 template <int kThreads>
 struct PlanShared {
   int32_t run[4 * kThreads];
-  Segment segs[kThreads];
+  struct {
+    Segment s;
+    int32_t pad;  // (threads read and write theirs together: an odd number of words apart)
+  } segs[kThreads];
 };
 
 // One CTA.  Its warps all go through all of the code, so what bounds it is their number times the code's length (32 warps: 15400 cycles for one
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   // pass 2: segments, their units, and how many keys all units have
   const int n_segs = p.B + n_runs;
   const bool few = n_segs <= kThreads;
-  Segment *segs = few ? sh.segs : p.segs;
+  auto seg = [&](int i) -> Segment & { return few ? sh.segs[i].s : p.segs[i]; };
   int64_t sum_keys = 0, sum_units = 0;  // of this thread
   for (int i = tid; i < n_segs; i += kThreads) {
     Segment s;
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       sum_keys += len * s.units;
       sum_units += s.units;
     }
-    segs[i] = s;
+    seg(i) = s;
   }
   add_warp(&s_keys, sum_keys);
   add_warp(&s_units, sum_units);
@@ -244,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     __syncthreads();
     int64_t sum_rows = 0, sum_floats = 0;
     for (int i = tid; i < n_segs; i += kThreads) {
-      Segment s = segs[i];
+      Segment s = seg(i);
       if (s.npos <= 0) continue;
       rule(s);
       const int chunks = s.chunks;
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     int64_t floats = 0, spans = 0;
     Segment s;
     s.npos = 0;
-    if (i < n_segs) s = segs[i];
+    if (i < n_segs) s = seg(i);
     if (s.npos > 0) {
       rule(s);
       rows = s.units * s.chunks;
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       if (s.npos > 0 && floats > 0) s_any = 1;
       s.first = (int32_t)(row_carry + ii - rows);
       if (few) s_first[tid] = s.first;
-      segs[i] = s;
+      seg(i) = s;
       if (few) p.segs[i] = s;  // (for the merge)
     }
     row_carry += ti;
@@ -316,8 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       const int in = min(kThreads, n_segs - base);
       int lo = 0, hi = n_all;
       if (!few) {
-        if (tid < in) s_first[tid] = segs[base + tid].first;
-        if (tid == 0) s_first[kThreads] = base + kThreads < n_segs ? segs[base + kThreads].first : n_all;
+        if (tid < in) s_first[tid] = seg(base + tid).first;
+        if (tid == 0) s_first[kThreads] = base + kThreads < n_segs ? seg(base + kThreads).first : n_all;
         __syncthreads();
         lo = s_first[0];
         hi = min(s_first[kThreads], n_all);
@@ -331,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
             if (s_first[mid] <= x) a = mid;
             else b = mid - 1;
           }
-          const Segment s = segs[base + a];
+          const Segment s = seg(base + a);
           if (s.units <= 0) continue;
           const int rel = x - s.first, u = rel / s.chunks, c = rel - u * s.chunks;
           if (u >= s.units) continue;
