@@ -53,8 +53,9 @@ struct Cfg {
   static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;
   static constexpr int OFF_KF = OFF_MISC + 64;             // float [kSlots][64]: factors of the keys' scores
   static constexpr int OFF_VF = OFF_KF + kSlots * kBT * 4; // float [kSlots][64]: factors of the keys' weights
-  static constexpr int OFF_VE = OFF_VF + kSlots * kBT * 4; // float [kSlots][4]: factor of the tile's P V; the warps' maxima on the way to it
-  static constexpr int OFF_KX = OFF_VE + kSlots * 16;      // uint32 [kSlots][4]: keys with values that are not finite, 16 a warp (two bits each)
+  static constexpr int OFF_VE = OFF_VF + kSlots * kBT * 4; // float [kSlots]: factor of the tile's P V
+  static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V, by tile
+  static constexpr int OFF_KX = OFF_VM + 32;      // uint32 [kSlots][4]: keys with values that are not finite, 16 a warp (two bits each)
   static constexpr int OFF_ODD = OFF_KX + kSlots * 16;     // int [2][3][D] first positions that see NaN, +inf, -inf
   static constexpr int SMEM = OFF_ODD + 2 * 3 * D * 4 + 1024;  // + slack to align the base to 1024
   static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int *s_abort = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 4);
   volatile int *s_isodd = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 8);  // [2]
   float *s_kf = reinterpret_cast<float *>(smem + C::OFF_KF), *s_vf = reinterpret_cast<float *>(smem + C::OFF_VF);
-  float *s_ve = reinterpret_cast<float *>(smem + C::OFF_VE);
+  float *s_ve = reinterpret_cast<float *>(smem + C::OFF_VE), *s_vm = reinterpret_cast<float *>(smem + C::OFF_VM);
   uint32_t *s_kx = reinterpret_cast<uint32_t *>(smem + C::OFF_KX);
   int *s_odd = reinterpret_cast<int *>(smem + C::OFF_ODD);
 
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int b = k & 1;
         if (!wait_bar(bar(B::O_FULL + b), (k >> 1) & 1, s_abort)) return false;
         ptx::tc_fence_after();
-        const float f = s_ve[(k % kSlots) * 4];
+        const float f = s_ve[k % kSlots];
         const float2 f2 = make_float2(f, f);
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
@@ -533,8 +534,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[E], amax;
 #pragma unroll 1
           for (int pass = 0; pass < 2; ++pass) {
-            float any = 0.0f;
-            amax = 0.0f;
+            float any[4], am[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) any[i] = am[i] = 0.0f;
 #pragma unroll
             for (int i = 0; i < G; ++i) {
               const float4 a = *reinterpret_cast<const float4 *>(src + ((i + id) % G) * 32);
@@ -543,11 +545,14 @@ __global__ void __launch_bounds__(kThreads, 1)
               v[8 * i + 4] = b.x; v[8 * i + 5] = b.y; v[8 * i + 6] = b.z; v[8 * i + 7] = b.w;
             }
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-              any = fmaf(v[i], 0.0f, any);
-              amax = fmaxf(amax, fabsf(v[i]));
-            }
-            if (any == 0.0f) break;
+            for (int i = 0; i < E; i += 8)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {  // (NaN where a value is not finite)
+                any[q] = fmaf(v[i + 2 * q], 0.0f, fmaf(v[i + 2 * q + 1], 0.0f, any[q]));
+                am[q] = ptx::max3(am[q], fabsf(v[i + 2 * q]), fabsf(v[i + 2 * q + 1]));
+              }
+            amax = fmaxf(fmaxf(am[0], am[1]), fmaxf(am[2], am[3]));
+            if ((any[0] + any[1]) + (any[2] + any[3]) == 0.0f) break;
             patch();
           }
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
@@ -555,7 +560,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float s = pow2(-e);
           f = pow2(e);
 #pragma unroll
-          for (int i = 0; i < E; i += 2) split2(v[i] * s, v[i + 1] * s, h[i / 2], l[i / 2]);
+          for (int i = 0; i < E; i += 2) {
+            const float2 y = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(s, s));
+            split2(y.x, y.y, h[i / 2], l[i / 2]);
+          }
         }
         if (!real) f = 0.0f;
         if (is_k) {
@@ -567,15 +575,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else {
           // the tile's largest factor: those of the weights are relative to its power of two
           const float wm = ptx::warp_max(f);
-          if (lane == 0) s_ve[slot * 4 + warp - 8] = wm;
+          if (lane == 0) s_vm[(n & 1) * 4 + warp - 8] = wm;
         }
         if (!together()) { ok = false; break; }  // the tile is in registers
-        float top = 0.0f;
-        if (!is_k) {
-          const float4 m4 = *reinterpret_cast<const float4 *>(s_ve + slot * 4);
-          top = fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w));
-          top = top > 0.0f ? pow2(max((int)(__float_as_uint(top) >> 23) - 127, -126)) : 1.0f;
-          if (half == 0) s_vf[slot * kBT + key] = f / top;
+        if (!is_k && half == 0) {
+          const float4 m4 = *reinterpret_cast<const float4 *>(s_vm + (n & 1) * 4);
+          const float top = fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w));
+          const int e = top > 0.0f ? min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126) : 0;
+          s_vf[slot * kBT + key] = f * pow2(-e);
+          if (id == 0) s_ve[slot] = pow2(e);
         }
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -583,10 +591,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint8_t *at = tile + (c >> 3) * C::KHALF + key * 128 + (((c & 7) ^ (key & 7)) << 4);
           *reinterpret_cast<uint4 *>(at) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
           if constexpr (!KV8) *reinterpret_cast<uint4 *>(at + C::KPART) = make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]);
-        }
-        if (!is_k) {
-          if (!together()) { ok = false; break; }  // (all have read the warps' maxima)
-          if (id == 0) s_ve[slot * 4] = top;
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
