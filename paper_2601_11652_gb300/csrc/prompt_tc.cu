@@ -131,6 +131,10 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   using C = Cfg<D>;
   using B = Bars<D>;
   constexpr int kThreads = threads_of(KV8);
+  // registers: 12 warps launch with 168 each, 16 with 128; per scheduler 3 x 168 = 2 softmax warps + 1, or 4 x 128 = 2 + 1 that decodes + 1.
+  // (Each split stands at the head of its own branch: after a join the compiler counts with the least.)
+  constexpr int kSoftRegs = KV8 ? (D == 128 ? 168 : 184) : 200, kCodeRegs = D == 128 ? 96 : 72, kRestRegs = KV8 ? (D == 128 ? 80 : 72) : 104;
+  static_assert(2 * kSoftRegs + kRestRegs + (KV8 ? kCodeRegs : 0) == (KV8 ? 4 * 128 : 3 * 168), "registers");
   // P is handed over in two halves of a tile's keys, so that the product with the first overlaps the softmax of the second: 1.3% with
   // D = 128 (16384 tokens 1571 -> 1550 us); elsewhere the softmax warps' issue slots bound the tile, and it costs 2 to 3%.
   constexpr int kWhole = D == 128 && !KV8 ? 0 : 1;
@@ -224,12 +228,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 
   bool ok = true;
   if (warp < 8) {
-    // registers: 12 warps launch with 168 each, 2016 a lane in all = 8 x 200 + 4 x 104; 16 with 128, 2048 = 8 x 184 + 8 x 72.
-    // (Each split stands at the head of its own branch: after a join the compiler counts with the least.)
-    if constexpr (KV8)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    else
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // ------------------------------------------------------------------ softmax and epilogue, stream s, a row per thread
     const int s = warp >> 2;
     const int row = threadIdx.x & 127;
@@ -456,7 +455,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
     }
   } else if (KV8 && warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCodeRegs));
     // ------------------------------------------------------------------ codes to bf16
     const int row = (warp - 12) * 32 + lane;
     constexpr int CH = D / 16;  // 16-byte chunks of a row of codes
@@ -484,8 +483,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           uint32_t o[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float2 f = h2_to_f2(e4m3x2_to_h2(e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xffffu));
-            o[e] = bf16x2_sat(f.x * sc, f.y * sc);
+            const float2 f = __fmul2_rn(h2_to_f2(e4m3x2_to_h2(e & 1 ? u[e >> 1] >> 16 : u[e >> 1])), make_float2(sc, sc));
+            o[e] = bf16x2_sat(f.x, f.y);
           }
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
@@ -526,10 +525,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       k0 += nt;
     }
   } else {
-    if constexpr (KV8)
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
       uint32_t nk = 0, nv = 0, nq = 0;  // tiles and items' Q so far
