@@ -6,7 +6,7 @@
 // pages is segment B + i, all its rows over keys [0, P).  A segment's rows are cut into units of `unit_rows`, its keys into chunks
 // of its chunk length; an item (plan.cuh) is a chunk of a unit of one KV head.  The list holds them without the head: entry i / Hkv and head
 // i mod Hkv make item i (item_at).  Where a row has its keys in more than one item
-// the items leave partials (O, m, l), and merge_kernel joins them.
+// the items leave partials (O, m, l), and prompt_merge_kernel joins them.
 #pragma once
 
 #include <cstddef>
@@ -36,14 +36,13 @@ static_assert(sizeof(Segment) == 64, "segment layout");
 struct PromptHeader {
   PlanHeader h;        // what the attention kernels read
   int32_t partials;    // 1: the merge has work
-  int32_t n_runs;
-  int32_t pad[6];
+  int32_t pad[7];
 };
 static_assert(offsetof(PromptHeader, h) == 0, "the kernels that read a PlanHeader find it there");
 
 struct PromptPlan {
   int B, Hq, Hkv, D, max_blocks_per_seq, total_q_rows;
-  int unit_rows;       // rows of a unit: whole positions of the kernel's two tiles (bf16 queries) or of its one (fp32)
+  int unit_rows;       // rows of a unit: whole positions of an item's two tiles (bf16 queries) or of its one (fp32)
   int sms;
   int grid;            // CTAs of the attention kernel: each takes its first item by its index
   int64_t max_rows, partial_cap;  // list entries, floats

@@ -18,7 +18,8 @@ constexpr int kBuckets = 1024;     // of the dispatch order, by key tiles of 64
 constexpr int kMinKeys = 256;      // chunks are not shorter, nor
 constexpr int kMinFull = 1024;     // of units of more than one tile (their partials cost more)
 constexpr int kTile = 128;         // and are whole key tiles
-constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys
+constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys (a table has fewer)
+constexpr int kMaxChunk = 1 << 28; // a segment's keys and two chunks stay below 2^31
 constexpr int kMaxRows = 1 << 24;  // k_r limit
 constexpr int kMergeThreads = 128;
 constexpr int kFew = 4, kHeads = 4; // chunks of a row, and rows, that a warp of the merge has in registers at once
@@ -78,7 +79,7 @@ struct PlanShared {
 };
 
 // One CTA.  Its warps all go through all of the code, so what bounds it is their number times the code's length (32 warps: 15400 cycles for one
-// request, THREADS128 with 4): it gets about as many threads as there are segments and list entries.  With at most kThreads requests and segments nothing else goes
+// request; 10600 with 4): it gets about as many threads as there are segments and list entries.  With at most kThreads requests and segments nothing else goes
 // through global memory, and a list entry stands for all KV heads (an item is an entry and a head), so that most batches have at
 // most one per thread.  48 prompts of up to 1500 tokens, 590 entries: PLAN_US us.
 template <int kThreads>
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   const int64_t keys = (int64_t)s_keys * p.Hkv, avg = (keys + p.sms - 1) / p.sms;
   const bool many = (int64_t)s_units * p.Hkv >= p.sms;
   const int64_t want = many ? avg : (avg + 1) / 2;
-  const int average = (int)min((want + kTile - 1) / kTile * kTile, (int64_t)kAllKeys);
+  const int average = (int)min((want + kTile - 1) / kTile * kTile, (int64_t)kMaxChunk);
   bool cuts = true;
   // how a segment is cut: its chunk length, and whether its units are cut as they lie one behind the other
   auto rule = [&](Segment &s) {
@@ -375,11 +376,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
         PromptHeader hd;
         memset(&hd, 0, sizeof hd);
         hd.h.n_items = total * p.Hkv;
-        hd.h.chunk_len = average;
-        hd.h.attn_ctas = p.sms;
         hd.h.next_item = p.grid;
         hd.partials = s_any;
-        hd.n_runs = n_runs;
         *p.header = hd;
       }
       __syncthreads();
