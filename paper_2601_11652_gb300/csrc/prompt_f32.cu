@@ -222,25 +222,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       float fq = 0.0f;
       if (!wait_bar(bar(B::Q_EMPTY), (j & 1) ^ 1, s_abort)) { ok = false; break; }
       {
+        float4 v[D / 4];  // (all of its loads at once)
+#pragma unroll
+        for (int c = 0; c < D / 4; ++c) v[c] = mine ? __ldg(reinterpret_cast<const float4 *>(qrow) + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         float amax = 0.0f;
-        if (mine) {
-#pragma unroll 8
-          for (int c = 0; c < D; c += 4) {
-            const float4 v = __ldg(reinterpret_cast<const float4 *>(qrow + c));
-            amax = fmaxf(fmaxf(fmaxf(amax, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
-          }
-        }
+#pragma unroll
+        for (int c = 0; c < D / 4; ++c) amax = fmaxf(fmaxf(fmaxf(amax, fabsf(v[c].x)), fmaxf(fabsf(v[c].y), fabsf(v[c].z))), fabsf(v[c].w));
         const int e = amax < INFINITY ? row_exp(amax) : 0;  // (a row with an infinity or a NaN becomes NaN in any case)
         fq = pow2(e) * scale;
         const float s = pow2(-e);
         uint8_t *line = smem + C::OFF_Q + row * 128;
-#pragma unroll 2
+#pragma unroll
         for (int c = 0; c < D; c += 8) {
-          float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
-          if (mine) {
-            a = __ldg(reinterpret_cast<const float4 *>(qrow + c));
-            b = __ldg(reinterpret_cast<const float4 *>(qrow + c) + 1);
-          }
+          const float4 a = v[c / 4], b = v[c / 4 + 1];
           uint4 h, l;
           split2(a.x * s, a.y * s, h.x, l.x);
           split2(a.z * s, a.w * s, h.y, l.y);
