@@ -25,13 +25,17 @@ constexpr int kMergeThreads = 128;
 constexpr int kFew = 4, kHeads = 4; // chunks of a row, and rows, that a warp of the merge has in registers at once
 
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
-template <typename T>
+template <int kThreads, typename T>
 __device__ T scan_incl(T v, T *s_w, T *total) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = kThreads >> 5;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const T o = __shfl_up_sync(0xffffffffu, v, d);
     if (lane >= d) v += o;
+  }
+  if constexpr (kThreads == 32) {
+    *total = __shfl_sync(0xffffffffu, v, 31);
+    return v;
   }
   if (lane == 31) s_w[w] = v;
   __syncthreads();
@@ -87,11 +91,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ __align__(16) uint8_t plan_smem[];
   PlanShared<kThreads> &sh = *reinterpret_cast<PlanShared<kThreads> *>(plan_smem);
-  constexpr int kOwn = kBuckets / kThreads;  // buckets of a thread
+  constexpr int kNb = kThreads == 32 ? 128 : kBuckets, kOwn = kNb / kThreads;  // buckets, and of a thread
   __shared__ int64_t s_scan[2][32];
   __shared__ int s_iscan[4][32];
   __shared__ unsigned long long s_keys, s_units, s_rows, s_floats;
-  __shared__ int s_hist[kBuckets];
+  __shared__ int s_hist[kNb];
   __shared__ int s_first[kThreads + 1];
   __shared__ int s_any;
   const int tid = threadIdx.x;
@@ -140,9 +144,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       if (!bad && (c < 0 || c + k + 1 > cap_tokens || (in && (int64_t)pages * kPage > c))) bad = WISP_DEV_BAD_LENGTH;
     }
     int64_t block_k;
-    const int64_t q0 = carry_k + scan_incl<int64_t>(k, s_scan[base / kThreads % 2], &block_k) - k + r;
+    const int64_t q0 = carry_k + scan_incl<kThreads, int64_t>(k, s_scan[base / kThreads % 2], &block_k) - k + r;
     int starts = 0;
-    const int run = n_runs + (p.shared_ids ? scan_incl<int>(start, s_iscan[base / kThreads % 2], &starts) : 0) - 1;
+    const int run = n_runs + (p.shared_ids ? scan_incl<kThreads, int>(start, s_iscan[base / kThreads % 2], &starts) : 0) - 1;
     if (r < p.B) {
       if (!bad && q0 + k + 1 > p.total_q_rows) bad = WISP_DEV_BAD_LENGTH;  // rows outside the caller's buffers
       my_q0 = (int32_t)min(q0, (int64_t)INT32_MAX);
@@ -211,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       s.shared = 1;
     }
     if (s.npos > 0) {
-      s.units = (int)(((int64_t)s.npos * g + R - 1) / R);
+      s.units = ceil_div(s.npos * g, R);  // (rows times g: below 2^30)
       const int64_t len = ((int64_t)(unit_end(s, 0, R, g) - s.t0) + (s.t1 - s.t0) + 1) / 2;
       sum_keys += len * s.units;
       sum_units += s.units;
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   // three quarters of all work (the rest fills gaps), they are cut from a fifth of an SM's work on: they lie one behind the other, and every
   // multiple of an SM's average is a cut, whatever unit it falls in.  (1344 rows behind 16384 tokens: 250 us, 354 without.)  With fewer
   // units than SMs, about two items per SM.
-  const int64_t keys = (int64_t)s_keys * p.Hkv, avg = (keys + p.sms - 1) / p.sms;
+  const int64_t keys = (int64_t)s_keys * p.Hkv, avg = keys < kAllKeys ? ceil_div((int)keys, p.sms) : (keys + p.sms - 1) / p.sms;  // (a division in 64 bits is 100 instructions)
   const bool many = (int64_t)s_units * p.Hkv >= p.sms;
   const int64_t want = many ? avg : (avg + 1) / 2;
   const int average = (int)min((want + kTile - 1) / kTile * kTile, (int64_t)kMaxChunk);
@@ -286,9 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     }
     int ti;
     int64_t tf, ts;
-    const int ii = scan_incl<int>(rows, s_iscan[2], &ti);
-    const int64_t fi = scan_incl<int64_t>(floats, s_scan[0], &tf);
-    const int64_t si = scan_incl<int64_t>(spans, s_scan[1], &ts);
+    const int ii = scan_incl<kThreads, int>(rows, s_iscan[2], &ti);
+    const int64_t fi = scan_incl<kThreads, int64_t>(floats, s_scan[0], &tf);
+    const int64_t si = scan_incl<kThreads, int64_t>(spans, s_scan[1], &ts);
     s.base = s.span ? (int)((span_carry + si - spans) % s.chunk) : 0;
     if (i < n_segs) {
       if (s.npos > 0 && (row_carry + ii > p.max_rows || float_carry + fi > p.partial_cap)) {
@@ -312,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   const bool single = few && n_all <= kThreads;  // an entry per thread, kept from pass 4 to pass 5
 
   // pass 4: the histogram of the entries' lengths; pass 5: each entry at its place in the dispatch order, longest first
-  auto bucket_of = [&](int tokens) { return kBuckets - 1 - min(ceil_div(tokens, 64), kBuckets - 1); };
+  auto bucket_of = [&](int tokens) { return kNb - 1 - min(ceil_div(tokens, 64), kNb - 1); };
   WorkItem w;
   int bucket = -1;
   for (int pass = 0; pass < 2; ++pass) {
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       int n[kOwn], sum = 0, total;
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) sum += n[i] = s_hist[kOwn * tid + i];
-      int at = scan_incl<int>(sum, s_iscan[3], &total) - sum;
+      int at = scan_incl<kThreads, int>(sum, s_iscan[3], &total) - sum;
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {  // (a thread's own)
         s_hist[kOwn * tid + i] = at;
@@ -391,8 +395,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 // partials' bytes (mostly in L2).
 template <int D, typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptPlan p) {
+  // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
+  const int partials = p.header->partials;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (!p.header->partials) return;
+  if (!partials) return;
   const int lane = threadIdx.x & 31;
   const int g = p.Hq / p.Hkv, R = p.unit_rows;
   constexpr int CPL = D / 32;
@@ -532,7 +538,8 @@ void plan_launch(const PromptPlan &p, cudaStream_t s) {
 }  // namespace
 
 cudaError_t prompt_plan_setup() {
-  cudaError_t e = plan_setup<128>();
+  cudaError_t e = plan_setup<32>();
+  if (e == cudaSuccess) e = plan_setup<128>();
   if (e == cudaSuccess) e = plan_setup<256>();
   if (e == cudaSuccess) e = plan_setup<512>();
   return e == cudaSuccess ? plan_setup<kMaxThreads>() : e;
@@ -540,9 +547,10 @@ cudaError_t prompt_plan_setup() {
 
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s) {
   // threads: requests and a few runs have one each, list entries about one (their number is bounded by the rows)
-  const int segs = p.B + (p.shared_ids ? 32 : 0);
+  const int segs = p.B + (p.shared_ids ? std::min(p.B, 32) : 0);
   const int64_t most = std::max<int64_t>(segs, (int64_t)p.total_q_rows * (p.Hq / p.Hkv) / p.unit_rows + p.B);
-  if (most <= 128) plan_launch<128>(p, s);
+  if (most <= 32) plan_launch<32>(p, s);
+  else if (most <= 128) plan_launch<128>(p, s);
   else if (most <= 256) plan_launch<256>(p, s);
   else if (most <= 512) plan_launch<512>(p, s);
   else plan_launch<kMaxThreads>(p, s);

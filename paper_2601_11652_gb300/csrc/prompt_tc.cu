@@ -529,6 +529,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
     if (warp == 9) {
       // ------------------------------------------------------------------ items, Q, K, V
       uint32_t nk = 0, nv = 0, nq = 0;  // tiles and items' Q so far
+      const WorkItem first_item = item_at(p, blockIdx.x);  // (read beside the items' number: there are at least as many places as CTAs)
       int claimed = (int)blockIdx.x < n_items ? (int)blockIdx.x : -1;
       auto claim = [&]() {
         if (lane == 0 && claimed == -2) {
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           it = claimed;
           claimed = -2;
           s_ring[slot].it = it;
-          if (it >= 0) s_ring[slot].w = item_at(p, it);
+          if (it >= 0) s_ring[slot].w = j == 0 ? first_item : item_at(p, it);
         }
         it = __shfl_sync(0xffffffffu, it, 0);
         __syncwarp();
