@@ -402,13 +402,6 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               o[i] = __float_as_uint(a1 == 0.0f ? u : fmaf(__uint_as_float(o1[i]), a1, u));
             }
           }
-          if (odd) {
-            for (int i = 0; i < 32; ++i) {
-              const bool nan = pos >= so[c + i], up = pos >= so[D + c + i], down = pos >= so[2 * D + c + i];
-              if (nan || (up && down)) o[i] = 0x7fffffffu;
-              else if (up || down) o[i] = __float_as_uint(__uint_as_float(o[i]) + (up ? INFINITY : -INFINITY));
-            }
-          }
           auto flush = [&](int at) {  // the staged pieces, to byte `at` of their rows
             __syncwarp();
 #pragma unroll
@@ -440,6 +433,19 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               put(e, v);
             }
             flush(c * 2);
+          }
+        }
+        if (odd) {  // V held values that are not finite: what they make of the rows that see them
+          __syncwarp();
+          uint16_t *dst16 = out0 + (row / g * p.Hq + row % g) * D;
+          float *dst32 = p.partials + w.poff + (int64_t)(tile * tile_rows + row) * D;
+#pragma unroll 1
+          for (int i = 0; i < D; ++i) {
+            const bool nan = pos >= so[i], up = pos >= so[D + i], down = pos >= so[2 * D + i];
+            if (!mine || !(nan || up || down)) continue;
+            const float add = nan || (up && down) ? __uint_as_float(0x7fffffffu) : up ? INFINITY : -INFINITY;
+            if (part) dst32[i] = __ldcg(dst32 + i) + add;
+            else dst16[i] = (uint16_t)pack_bf16(__uint_as_float((uint32_t)dst16[i] << 16) + add, 0.0f);
           }
         }
         if (part && mine) {
