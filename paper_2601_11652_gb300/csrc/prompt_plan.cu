@@ -110,7 +110,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) s_hist[kOwn * tid + i] = 0;
   const int64_t cap_tokens = (int64_t)p.max_blocks_per_seq * kPage;
-  const bool one = p.B <= kThreads;  // every request has a thread
+  constexpr bool kAll = kThreads < kMaxThreads;  // by the launch's choice: every segment has a thread
+  const bool one = kAll || p.B <= kThreads;      // every request has one
   const int RS = one ? kThreads : p.B;
   int32_t *run_start = one ? sh.run : p.run_info;
   int32_t *run_end = run_start + RS, *run_first = run_start + 2 * RS, *run_valid = run_start + 3 * RS;
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   int n_runs = 0;
   int my_k = 0, my_ctx = 0, my_pages = 0, my_q0 = 0, my_run = -1;  // (of the last chunk: the only one where `one`)
   bool my_ok = false;
-  for (int base = 0; base < p.B; base += kThreads) {
+  for (int base = 0; base < (kAll ? 1 : p.B); base += kThreads) {
     const int r = base + tid;
     int64_t k = 0;
     int bad = 0, pages = 0, id = -1;
@@ -185,10 +186,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 
   // pass 2: segments, their units, and how many keys all units have
   const int n_segs = p.B + n_runs;
-  const bool few = n_segs <= kThreads;
+  const bool few = kAll || n_segs <= kThreads;
   auto seg = [&](int i) -> Segment & { return few ? sh.segs[i].s : p.segs[i]; };
   int64_t sum_keys = 0, sum_units = 0;  // of this thread
-  for (int i = tid; i < n_segs; i += kThreads) {
+  for (int i = tid; i < n_segs; i += kAll ? kAllKeys : kThreads) {
     Segment s;
     memset(&s, 0, sizeof s);
     s.pbase = -1;
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     if (tid == 0) s_rows = s_floats = 0;
     __syncthreads();
     int64_t sum_rows = 0, sum_floats = 0;
-    for (int i = tid; i < n_segs; i += kThreads) {
+    for (int i = tid; i < n_segs; i += kAll ? kAllKeys : kThreads) {
       Segment s = seg(i);
       if (s.npos <= 0) continue;
       rule(s);
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 
   // pass 3: entries and partials of each segment
   int64_t row_carry = 0, float_carry = 0, span_carry = 0;
-  for (int base = 0; base < n_segs; base += kThreads) {
+  for (int base = 0; base < (kAll ? 1 : n_segs); base += kThreads) {
     const int i = base + tid;
     int rows = 0;
     int64_t floats = 0, spans = 0;
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
   WorkItem w;
   int bucket = -1;
   for (int pass = 0; pass < 2; ++pass) {
-    for (int base = 0; base < n_segs; base += kThreads) {
+    for (int base = 0; base < (kAll ? 1 : n_segs); base += kThreads) {
       const int in = min(kThreads, n_segs - base);
       int lo = 0, hi = n_all;
       if (!few) {
@@ -546,9 +547,8 @@ cudaError_t prompt_plan_setup() {
 }
 
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s) {
-  // threads: requests and a few runs have one each, list entries about one (their number is bounded by the rows)
-  const int segs = p.B + (p.shared_ids ? std::min(p.B, 32) : 0);
-  const int64_t most = std::max<int64_t>(segs, (int64_t)p.total_q_rows * (p.Hq / p.Hkv) / p.unit_rows + p.B);
+  // threads: requests and runs have one each, list entries about one (their number is bounded by the rows)
+  const int64_t most = std::max<int64_t>((p.shared_ids ? 2 : 1) * (int64_t)p.B, (int64_t)p.total_q_rows * (p.Hq / p.Hkv) / p.unit_rows + p.B);
   if (most <= 32) plan_launch<32>(p, s);
   else if (most <= 128) plan_launch<128>(p, s);
   else if (most <= 256) plan_launch<256>(p, s);
