@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       my_pages = pages;
       my_run = id >= 0 && pages > 0 ? run : -1;
       p.q_row_start[r] = my_q0;
-      p.req_flag[r] = bad ? REQ_BAD : REQ_OK;
+      if (!kAll) p.req_flag[r] = bad ? REQ_BAD : REQ_OK;
       p.req_run[r] = my_run;
       if (bad) report(p.status, bad, p.request_ids, r);
       if (start) {
@@ -256,12 +256,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
       Segment s = seg(i);
       if (s.npos <= 0) continue;
       rule(s);
-      const int chunks = s.chunks;
-      sum_rows += (int64_t)s.units * chunks;
-      if (chunks > 1 || s.shared) {
+      sum_rows += (int64_t)s.units * s.chunks;
+      s.part_h = 0;
+      if (s.chunks > 1 || s.shared) {
         const int rows_last = s.npos * g - (s.units - 1) * R;
-        sum_floats += (int64_t)p.Hkv * chunks * ((int64_t)(s.units - 1) * slot_floats(R, p.D) + slot_floats(rows_last, p.D));
+        const int64_t floats = s.chunks * ((int64_t)(s.units - 1) * slot_floats(R, p.D) + slot_floats(rows_last, p.D));
+        sum_floats += p.Hkv * floats;
+        s.part_h = (int)min(floats, (int64_t)INT32_MAX);
       }
+      seg(i) = s;
     }
     add_warp(&s_rows, sum_rows);
     add_warp(&s_floats, sum_floats);
@@ -281,13 +284,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
     s.npos = 0;
     if (i < n_segs) s = seg(i);
     if (s.npos > 0) {
-      rule(s);
       rows = s.units * s.chunks;
       spans = (int64_t)s.units * s.span;
-      if (s.chunks > 1 || s.shared) {
-        s.part_h = s.chunks * ((s.units - 1) * slot_floats(R, p.D) + slot_floats(s.npos * g - (s.units - 1) * R, p.D));
-        floats = (int64_t)s.part_h * p.Hkv;
-      }
+      floats = (int64_t)s.part_h * p.Hkv;
     }
     int ti;
     int64_t tf, ts;
