@@ -396,17 +396,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 template <int D, typename T>
 __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptPlan p) {
   // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
-  const int partials = p.header->partials;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (!partials) return;
+  if (!p.header->partials) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
   const int lane = threadIdx.x & 31;
   const int g = p.Hq / p.Hkv, R = p.unit_rows;
   constexpr int CPL = D / 32;
   for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
     const Segment own = p.segs[r];
     const int run = p.req_run[r];
-    if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
     const Segment pre = p.segs[run >= 0 ? p.B + run : r];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
     const int subs = g / p.merge_heads, work = own.npos * p.Hkv * subs;
     for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
       const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
