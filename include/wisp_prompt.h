@@ -25,7 +25,8 @@ extern "C" {
  * chunk of one behind c_r cached tokens; row j sees keys 0 .. c_r + j of its sequence, which must all be in the pool already.
  *   out[row, h] = sum_t softmax_t(<q[row, h], K[t, h / (Hq/Hkv)]> / sqrt(D)) V[t, h / (Hq/Hkv)]
  * The cache has the queries' type, or holds e4m3 codes with a scale per page and KV head (wisp_kv8.h).
- * Supported: D in {64, 128}, block_size == 16, Hq / Hkv <= 128, k_r < 2^24.
+ * Supported: D in {64, 128}, block_size == 16, Hq / Hkv <= 128, k_r < 2^24, and total_q_rows * Hq * (D + 2) < 2^29 with shared pages (partial
+ * results have 32-bit offsets: larger calls may return WISP_ERR_UNSUPPORTED).
  * Scores, softmax statistics and outputs accumulate in fp32.  With bf16 queries a weight enters the second product in bf16
  * (relative error 2^-9), and so do code * scale of an e4m3 cache, K and V (exactly where the scale is a power of two of magnitude 2^-100
  * to 2^100; values past the bf16 range count as its largest).  With fp32 queries every factor enters its product with
