@@ -228,6 +228,43 @@ def test_more_requests_than_the_planner_has_threads():
     p.check()
 
 
+@pytest.mark.parametrize("B", [16, 17, 32, 33, 64, 65, 128, 129, 256, 257, 511, 512, 513])
+@pytest.mark.parametrize("shared", [False, True])
+def test_batches_around_the_planners_sizes(B, shared):
+    """As many requests, and requests and runs, as the planner has threads, and one more; every run has one to three requests."""
+    rng = np.random.default_rng(B)
+    runs = None
+    if shared:
+        runs = [(i, 1 + i % 3) for i in range(B) for _ in range(1 + (i * 7) % 3)][:B]
+    k = rng.integers(0, 4, B).tolist()
+    c = Case(B, k=k, ctx=[(runs[r][1] * PAGE if shared else 0) + int(x) for r, x in enumerate(rng.integers(0, 40, B))], runs=runs, Hq=4, Hkv=2, D=64)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("B", [17, 33, 130])
+def test_runs_of_one_request_each(B):
+    """As many runs as requests, none of which shares anything."""
+    c = Case(B, k=[r % 3 for r in range(B)], ctx=[16 + r for r in range(B)], runs=[(r, 1) for r in range(B)], Hq=2, Hkv=1, D=128)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("k,ctx", [([3], [40000]), ([0, 700, 2], [17000, 5, 33000])])
+def test_more_chunks_than_the_planner_has_threads(dtype, cache, k, ctx):
+    c = Case(11, k=k, ctx=ctx, Hq=4, Hkv=1, D=64, dtype=dtype, cache=cache)
+    nan = ctx[0] + k[0]  # only the last row sees it, and its chunk is one of many
+    c.run()
+    c.check()
+    before = c.t["out"].clone()
+    put(c, "v", 0, nan, 7, math.nan)
+    c.run()
+    same = torch.ones_like(before, dtype=torch.bool)
+    same[k[0], :, 7] = False
+    assert torch.isnan(c.t["out"][k[0], :, 7]).all() and torch.equal(c.t["out"][same], before[same])
+
+
 def bits_of(t):
     return t.view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()])
 
