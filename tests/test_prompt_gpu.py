@@ -489,6 +489,40 @@ def test_repeats_to_the_bit_on_streams_and_in_graphs(dtype, cache):
             c.check()
 
 
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_graph_follows_lengths_and_runs(shared):
+    """A captured call reads lengths, tables, runs and rows anew: replayed on another batch of as many requests and rows, in the same buffers."""
+    from paper_2601_11652_gb300 import binding as wb
+    pages = [8, 8, 3, 3, 3, 0]
+    first = Case(18, k=[200, 3, 0, 9, 31, 1], ctx=[200, 129, 50, 48, 70, 0], Hq=8, Hkv=2, D=128, spare=600,
+                 runs=list(zip([0, 0, 1, 1, 1, -1], pages)) if shared else None)
+    then = Case(19, k=[0, 120, 0, 60, 60, 4], ctx=[17, 900, 64, 7000, 7001, 300], Hq=8, Hkv=2, D=128,
+                runs=list(zip([3, -1, 2, 7, 7, 7], [1, 0, 4, 430, 430, 2])) if shared else None)
+    have = then.t["k_cache"].shape[0]
+    for x in "kv":  # (one pool that is large enough for both)
+        pool = torch.full((have, 2, PAGE, 128), math.nan, dtype=BF, device="cuda")
+        pool[:first.t[x + "_cache"].shape[0]] = first.t[x + "_cache"]
+        first.t[x + "_cache"] = pool
+    tables = torch.full_like(first.t["block_tables"], -1)
+    tables[:, :then.t["block_tables"].shape[1]] = then.t["block_tables"]
+    then.t["block_tables"] = tables
+    inputs = [{n: t.clone() for n, t in c.t.items()} for c in (first, then)]
+    a, n, call = first.args()
+    buffers, ws = first.t, wb.alloc_workspace(n)
+    call(a, ws)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(a, ws)
+    for c, t in ((then, inputs[1]), (first, inputs[0]), (then, inputs[1])):
+        for n in buffers:
+            buffers[n].copy_(t[n])
+        g.replay()
+        torch.cuda.synchronize()
+        assert wb.wisp_verify_get_device_status(ws)[0] == 0
+        c.t = dict(t, out=buffers["out"])
+        c.check()
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 2^32 bytes, its pages from the far end."""
     nb = (1 << 32) // (8 * PAGE * 128 * 2) + 400
