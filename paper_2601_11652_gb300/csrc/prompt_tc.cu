@@ -28,12 +28,13 @@
 // Bound, D = 128: the tensor core; a tile of both streams takes 2950 cycles, 2048 of them at its nominal rate (S reads Q and K from shared
 // memory).  16384 tokens, 32 heads over 8: 1.18 ms alone, 1.86 PFLOP/s of the 1.88 that a library product reaches, 1.32 ms in a row under the
 // power limit; 4096 tokens 96 us; over e4m3 125 us.  D = 64: the softmax warps' chain, two warps a scheduler, 2400 cycles a tile; 48 prompts
-// of up to 1500 tokens 250 us, 0.64 PFLOP/s.  Few rows and keys: latency, most of it code that is fetched for the first time (about ten
+// of up to 1500 tokens 247 us, 0.65 PFLOP/s.  Few rows and keys: latency, most of it code that is fetched for the first time (about ten
 // cycles an instruction), so that less code is faster: 64 tokens, whole call 15 us.
 // Measured and not kept: a part of the exponentials as polynomials (one in eight: 4096 tokens 99 to 109 us, heads of 64 85 to 92); m taken from
 // the tile before (102 to 112); S read a second time instead of held in registers (102 to 121); items of one row tile (2000 tokens 46 to
 // 52); two groups of softmax warps per stream (heads of 64, 84.5 to 101); warps without rows of the item skip its softmax (64 requests
-// with a prefix 81.8 to 82.2, 4096 tokens 98.8 to 101.3).
+// with a prefix 81.8 to 82.2, 4096 tokens 98.8 to 101.3); maxima only where weights come out large (96 to 107, heads of 64 83.7 to 83.2, 48 prompts
+// 250 to 256); the streams' exponentials one after the other (heads of 64 84 to 93).
 #include "attn_merge.cuh"
 #include "fp8.cuh"
 #include "prompt.cuh"
@@ -148,6 +149,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   // P is handed over in two halves of a tile's keys, so that the product with the first overlaps the softmax of the second: 1.3% with
   // D = 128 (16384 tokens 1571 -> 1550 us); elsewhere the softmax warps' issue slots bound the tile, and it costs 2 to 3%.
   constexpr int kWhole = D == 128 && !KV8 ? 0 : 1;
+  // With P in columns of its own the weights are computed beside the P V before and stored behind it: 48 prompts of up to 1500 tokens 250 ->
+  // 247 us (over an 8-bit cache, with fewer registers, 196 -> 200).
+  constexpr bool kBeside = C::P_APART && !KV8;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sbase = ptx::smem_u32(smem);
@@ -294,17 +298,24 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           for (int i = 2; i < 32; i += 2) mx[c] = ptx::max3(mx[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
         }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+        bool done = !kBeside || t == first;
+        auto finish = [&]() -> bool {  // the P V before: its P is written over, its O may be rescaled
+          if (!wait_bar(bar(B::O_FULL + s), nof & 1, s_abort)) return false;
+          ++nof;
+          ptx::tc_fence_after();
+          return true;
+        };
         if (t == first) {
           m = top;
         } else {
-          if (C::P_APART) {  // the P V before: its P is written over, its O may be rescaled
-            if (!wait_bar(bar(B::O_FULL + s), nof & 1, s_abort)) { ok = false; break; }
-            ++nof;
-            ptx::tc_fence_after();
-          }
+          if (C::P_APART && !kBeside && !finish()) { ok = false; break; }
           const bool move = mine && top > m + kLoose;
           if (__any_sync(0xffffffffu, move)) {
-            // (the O before this S is complete)
+            // (P over S: the O before this S is complete)
+            if (kBeside) {
+              if (!finish()) { ok = false; break; }
+              done = true;
+            }
             const float a = move ? ptx::ex2(m - top) : 1.0f;
             if (move) m = top;
             l *= a;
@@ -322,17 +333,25 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         const float mm = m == -INFINITY ? 0.0f : -m;  // (nothing seen so far: every weight is zero)
         const float2 m2 = make_float2(mm, mm);
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
+        uint32_t pk[4][16];
+        auto weigh = [&](int c) {
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const float2 a = __ffma2_rn(make_float2(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])), scale2, m2);
             const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
             sum[(i >> 1) & 1] = __fadd2_rn(sum[(i >> 1) & 1], e);
-            pk[i >> 1] = pack_bf16(e.x, e.y);
+            pk[c][i >> 1] = pack_bf16(e.x, e.y);
           }
-          ptx::tmem_st16(t_p + 16 * c, pk);
+        };
+        if (kBeside) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) weigh(c);
+        }
+        if (kBeside && !done && !finish()) { ok = false; break; }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (!kBeside) weigh(c);
+          ptx::tmem_st16(t_p + 16 * c, pk[c]);
           if (c == 3 || (c == 1 && !kWhole)) {  // half of the keys: the product may begin
             ptx::tmem_wait_st();
             ptx::tc_fence_before();
