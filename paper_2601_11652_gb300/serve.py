@@ -272,8 +272,9 @@ class VerifyServer:
             step = wb.wisp_verify_step_kv8 if s.kv8 else wb.wisp_verify_step
             n = wb.wisp_verify_workspace_size(attn.attn if s.kv8 else attn, accp)
         else:
-            ids = torch.tensor(shared, dtype=torch.int32, device=dev)
-            attn = wb.make_shared_args(**batch, **pool, shared_ids=ids[:, 0].contiguous(), shared_pages=ids[:, 1].contiguous())
+            # (held until the batch is done: the arguments have their addresses only)
+            ids, pages = (torch.tensor(x, dtype=torch.int32, device=dev) for x in zip(*shared))
+            attn = wb.make_shared_args(**batch, **pool, shared_ids=ids, shared_pages=pages)
             n = wb.wisp_verify_shared_workspace_size(attn)
             if self.shared_ws is None or self.shared_ws.numel() < n:
                 self.shared_ws = wb.alloc_workspace(n, dev)

@@ -95,3 +95,29 @@ def test_sessions_behind_one_prompt(cache, Hq, Hkv, D, rot):
     server.run_batch([3], [serve.Payload(x["q"], x["k_new"], x["v_new"], x["logits"], x["draft_tokens"], x["draft_probs"], x["accept_u"],
                                          x["sample_u"])])
     assert server.shared_ws is None
+
+
+def payload_of(x):
+    from paper_2601_11652_gb300 import serve
+    return serve.Payload(x["q"], x["k_new"], x["v_new"], x["logits"], x["draft_tokens"], x["draft_probs"], x["accept_u"], x["sample_u"])
+
+
+@pytest.mark.parametrize("rounds", [6])
+def test_rounds_without_log_probabilities(rounds):
+    """Nothing but the batch's own buffers lies between its arguments and the attention, so that one given back too early would be written over."""
+    from paper_2601_11652_gb300 import build, serve
+    build.build()
+    Hq, Hkv, D, n = 8, 2, 64, 5
+    sess = serve.PagedSessions(n, Hkv, D, "bf16", NB, MB)
+    x = wl.make_round((61, 0), k=99, Hq=Hq, Hkv=Hkv, D=D, V=8)
+    sess.prefill([0], [x["k_new"]], [x["v_new"]])
+    sess.share(0, [1, 2, 3, 4], 96)
+    server = serve.VerifyServer(sess, Hq, V)
+    for i in range(rounds):
+        d = [wl.make_round((62, i, s), k=s, Hq=Hq, Hkv=Hkv, D=D, V=V) for s in range(n)]
+        got = server.run_batch(list(range(n)), [payload_of(y) for y in d])
+        row = 0
+        for s in range(n):
+            m = s + 1
+            check(sess, got.out[row:row + m], got.block_tables[s], 0, values(d[s]["q"]), int(got.context_lens[s]) + torch.arange(m), None, False)
+            row += m
