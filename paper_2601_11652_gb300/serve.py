@@ -56,6 +56,13 @@ class Payload:
     sample_u: float
 
 
+def _after_current(stream, dev):
+    """Let `stream` (a torch stream or a handle) wait for what the current one has to do: a batch's rows, lengths and tables are written
+    there."""
+    s = stream if hasattr(stream, "wait_stream") else torch.cuda.ExternalStream(stream, device=dev)
+    s.wait_stream(torch.cuda.current_stream(dev))
+
+
 def _cat(arrays, tail_shape, dtype):
     return np.concatenate(arrays) if arrays else np.zeros((0, *tail_shape), dtype)
 
@@ -149,6 +156,8 @@ class PagedSessions:
         args = self._append_args(**batch, **turn, k_new=kn, v_new=vn, accepted_len=acc)
         ws, cws = self._ws(args)
         used = [ws, cws]
+        if stream is not None:
+            _after_current(stream, self.dev)
         self._append(args, ws, stream)
         if q is not None:
             a = wb.make_prompt_args(**batch, **self.scales, q=q, k_cache=self.k_cache, v_cache=self.v_cache, out=out,
@@ -296,6 +305,7 @@ class VerifyServer:
             used.append((self.lp_ws, "logprobs"))
         stream = self.stream or torch.cuda.current_stream(dev)
         a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        _after_current(stream, dev)
         with torch.cuda.stream(stream):
             a.record(stream)
             s._append(kv, kws, stream)

@@ -82,3 +82,23 @@ def test_what_the_attention_reads_lives_until_it_is_called(fake):
     server.run_batch([3, 2, 0, 1], [payload(k) for k in (1, 0, 2, 0)])
     ids, pages = fake.read[0]
     assert ids.count(0) == 3 and [p for i, p in zip(ids, pages) if i == 0] == [2, 2, 2]
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_another_stream_waits_for_the_batch_that_it_reads(fake, shared):
+    """Rows, lengths and tables of a batch are written on the current stream."""
+    s = sessions(4, [1, 3], 2)
+    other = Stream(fake.log, "other")
+    server = serve.VerifyServer(s, HQ, V, stream=other)
+    server.run_batch([3, 1] if shared else [2], [payload(1) for _ in range(2 if shared else 1)])
+    assert fake.log.index(("other", "waits for", "current")) < fake.log.index(("wisp_kv_reserve_append", "other"))
+    assert (("attention", "other") in fake.log) == shared
+
+
+@pytest.mark.parametrize("queries", [False, True])
+def test_a_prefill_on_another_stream_waits_for_its_rows(fake, queries):
+    s = sessions(4, [1], 2)
+    z = lambda *x: np.zeros(x, np.float32)
+    s.prefill([2], [z(5, HKV, D)], [z(5, HKV, D)], stream=Stream(fake.log, "other"), q_rows=[z(5, HQ, D)] if queries else None)
+    assert fake.log.index(("other", "waits for", "current")) < fake.log.index(("wisp_kv_reserve_append", "other"))
+    assert (("wisp_prompt_attention", "other") in fake.log) == queries
