@@ -96,7 +96,7 @@ class PagedSessions:
         self.ctx = torch.zeros(n_sessions, dtype=torch.int32, device=self.dev)
         self.num_blocks, self.max_blocks, self.Hkv, self.D = num_blocks, max_blocks, Hkv, D
         self.kv_ws = self.commit_ws = self.prompt_ws = None
-        self.prefix = [(-1, 0)] * n_sessions  # per session: whose first pages it shares (an id), and how many
+        self.prefix = [(-1, 0)] * n_sessions  # per session: the group that it shares its first pages with, and how many (see runs)
 
     @property
     def projected(self):
@@ -142,6 +142,7 @@ class PagedSessions:
         draft = torch.tensor([n - 1 for n in lens], dtype=torch.int32, device=self.dev)
         ctx = self.ctx[idx].contiguous()
         tables = self.tables[idx].contiguous()
+        anew = [sid for sid, c in zip(sids, ctx.tolist()) if c == 0] if any(self.prefix[sid][1] for sid in sids) else []
         kn, vn = self._dev(np.concatenate(k_rows)), self._dev(np.concatenate(v_rows))
         batch = dict(draft_lens=draft, context_lens=ctx, block_tables=tables, total_q_rows=int(sum(lens)))
         acc = draft.clone()
@@ -175,7 +176,18 @@ class PagedSessions:
                 raise RuntimeError(f"prefill: device status {code} (request {rid})")
         self.tables[idx] = tables
         self.ctx[idx] = ctx
+        for sid in anew:  # (what it shared before it was emptied)
+            self.prefix[sid] = (-1, 0)
         return out
+
+    def runs(self, shared, tables, ctx):
+        """shared_ids and shared_pages [B] (device) of a batch, `shared` the sessions' prefixes in its order.  The block tables say what is shared:
+        a session whose first pages are no longer those of its group's first one (it was emptied and filled anew) is alone."""
+        ids, pages = (torch.tensor(x, dtype=torch.int32, device=self.dev) for x in zip(*shared))
+        lead = torch.tensor([shared.index(g) for g in shared], device=self.dev)
+        n = max(p for _, p in shared)
+        same = (tables[:, :n] == tables[lead, :n]) | (torch.arange(n, device=self.dev) >= pages[:, None])
+        return torch.where(same.all(1) & (ctx >= pages * PAGE), ids, -1), pages
 
     def share(self, src, sids, tokens):
         """Let the empty sessions `sids` begin with the first `tokens` tokens of session `src`, whole pages of them, without a copy: their
@@ -282,7 +294,7 @@ class VerifyServer:
             n = wb.wisp_verify_workspace_size(attn.attn if s.kv8 else attn, accp)
         else:
             # (held until the batch is done: the arguments have their addresses only)
-            ids, pages = (torch.tensor(x, dtype=torch.int32, device=dev) for x in zip(*shared))
+            ids, pages = s.runs(shared, tables, ctx)
             attn = wb.make_shared_args(**batch, **pool, shared_ids=ids, shared_pages=pages)
             n = wb.wisp_verify_shared_workspace_size(attn)
             if self.shared_ws is None or self.shared_ws.numel() < n:

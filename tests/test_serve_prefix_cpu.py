@@ -102,3 +102,28 @@ def test_a_prefill_on_another_stream_waits_for_its_rows(fake, queries):
     s.prefill([2], [z(5, HKV, D)], [z(5, HKV, D)], stream=Stream(fake.log, "other"), q_rows=[z(5, HQ, D)] if queries else None)
     assert fake.log.index(("other", "waits for", "current")) < fake.log.index(("wisp_kv_reserve_append", "other"))
     assert (("wisp_prompt_attention", "other") in fake.log) == queries
+
+
+def test_a_session_used_anew_leaves_its_run(fake):
+    """The block tables say what is shared: a session that has been emptied and given other pages reads its own."""
+    s = sessions(6, [1, 2, 3], 2)
+    server = serve.VerifyServer(s, HQ, V)
+    s.tables[2], s.ctx[2] = -1, 0            # emptied, and ...
+    s.tables[2, :3] = torch.tensor([40, 41, 42])
+    s.ctx[2] = 45                            # ... filled again
+    s.tables[3], s.ctx[3] = -1, 0            # emptied
+    server.run_batch([0, 1, 2, 3], [payload(1) for _ in range(4)])
+    assert fake.read[-1] == ([0, 0, -1, -1], [2, 2, 2, 2])
+    s.tables[0], s.ctx[0] = -1, 0            # now the run's own source
+    s.tables[0, :3] = torch.tensor([50, 51, 52])
+    s.ctx[0] = 48
+    server.run_batch([0, 1, 2, 3], [payload(1) for _ in range(4)])
+    assert fake.read[-1][0][1:] == [-1, -1, -1]   # (a run of one is computed alone)
+
+
+def test_a_prefill_of_an_empty_session_ends_its_sharing(fake):
+    s = sessions(6, [1, 2], 2)
+    s.tables[1], s.ctx[1] = -1, 0
+    z = lambda *x: np.zeros(x, np.float32)
+    s.prefill([1, 2], [z(5, HKV, D)] * 2, [z(5, HKV, D)] * 2)
+    assert s.prefix[:3] == [(0, 2), (-1, 0), (0, 2)]  # (session 2 has its shared pages and gets its next tokens)

@@ -121,3 +121,35 @@ def test_rounds_without_log_probabilities(rounds):
             m = s + 1
             check(sess, got.out[row:row + m], got.block_tables[s], 0, values(d[s]["q"]), int(got.context_lens[s]) + torch.arange(m), None, False)
             row += m
+
+
+@pytest.mark.parametrize("filled_by", ["prefill", "rows"])
+def test_a_session_used_anew_reads_its_own_pages(filled_by):
+    from paper_2601_11652_gb300 import build, serve
+    build.build()
+    Hq, Hkv, D, n = 8, 2, 64, 4
+    sess = serve.PagedSessions(n, Hkv, D, "bf16", NB, MB)
+    x = wl.make_round((63, 0), k=99, Hq=Hq, Hkv=Hkv, D=D, V=8)
+    sess.prefill([0], [x["k_new"]], [x["v_new"]])
+    sess.share(0, [1, 2, 3], 64)
+    sess.tables[2], sess.ctx[2] = -1, 0
+    y = wl.make_round((63, 1), k=79, Hq=Hq, Hkv=Hkv, D=D, V=8)
+    if filled_by == "prefill":
+        sess.prefill([2], [y["k_new"]], [y["v_new"]])
+    else:  # (the rows of a session that somebody filled elsewhere)
+        extra = serve.PagedSessions(1, Hkv, D, "bf16", 8, MB)
+        extra.prefill([0], [y["k_new"]], [y["v_new"]])
+        to = torch.arange(NB - 60, NB - 55, device="cuda")
+        for name in ("k_cache", "v_cache"):
+            getattr(sess, name)[to] = getattr(extra, name)[extra.tables[0, :5].long()]
+        sess.tables[2, :5], sess.ctx[2] = to.int(), 80
+        keep = sess.free_blocks[:int(sess.free_count)]
+        keep = keep[~torch.isin(keep, to.int())]
+        sess.free_blocks[:len(keep)] = keep
+        sess.free_count.fill_(len(keep))
+    server = serve.VerifyServer(sess, Hq, V)
+    d = [wl.make_round((64, s), k=2, Hq=Hq, Hkv=Hkv, D=D, V=V) for s in range(n)]
+    got = server.run_batch(list(range(n)), [payload_of(z) for z in d])
+    for s in range(n):
+        check(sess, got.out[3 * s:3 * s + 3], got.block_tables[s], 0, values(d[s]["q"]), int(got.context_lens[s]) + torch.arange(3), None, False)
+    assert got.context_lens.tolist() == [100, 64, 80, 64]
