@@ -18,6 +18,7 @@ struct AttnParams {
   PlanHeader *header_mut;  // same object: the work counter
   const WorkItem *items;  // in dispatch order
   float *partials;
+  int2 *handed_on;     // prompt.cuh: rows (of all query rows) and query heads that are computed once more
   int row_groups;      // row groups per (request, head) at most
   int32_t *pair_done;  // [B * Hkv * row_groups] finished chunks of each split (request, head, row group), zeroed
                        // by the planner

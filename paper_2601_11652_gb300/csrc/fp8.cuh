@@ -22,6 +22,12 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
   return r;
 }
+// two values in bf16, rounded to nearest; past its range (and infinite) its largest
+__device__ __forceinline__ uint32_t bf16x2_sat(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
 // two e4m3 codes (in the low 16 bits) -> two halves, exactly
 __device__ __forceinline__ uint32_t e4m3x2_to_h2(uint32_t codes) {
   uint32_t r;

@@ -28,7 +28,8 @@ struct PlanHeader {
   int32_t partial_floats;
   int32_t next_item;   // work counter of the persistent attention kernel (zeroed by the planner)
   int32_t attn_ctas;   // CTAs of the tensor-core attention that take items (the others exit at once)
-  int32_t pad[3];
+  int32_t handed_on;   // rows in prompt.cuh's list (zeroed by its planner)
+  int32_t pad[2];
 };
 
 constexpr int kItemsPerSM = 2;     // work items per SM when (request, head) pairs are fewer than SMs

@@ -74,9 +74,24 @@ __device__ __forceinline__ WorkItem item_at(const AttnParams &p, int it) {
 // Rows of a segment that share a partial's slot, and floats of a slot.
 __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D + 2) + 3) / 4 * 4; }
 
+// Rows that the attention kernels hand on to prompt_row.cuh, as they cannot hold them.
+//
+// A score becomes a weight in one fused multiply-add, 2^(x scale - m) from the sum x of products.  It is rounded once; but m is a rounded number, so
+// where it is far from zero the largest weight is not 2^0 but up to 2^(half a step of m): references are whole numbers, exact up to 2^24, and a row
+// that has had one beyond kFar is computed once more.
+//
+// A row of an item that writes outputs goes into a list; of one that leaves partials the sign of l says it (l is never negative).
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabsf(m) < INFINITY; }
+__device__ __forceinline__ float marked(float l) { return __uint_as_float(__float_as_uint(l) | 0x80000000u); }
+__device__ __forceinline__ bool is_marked(float l) { return __float_as_uint(l) >> 31; }
+__device__ __forceinline__ void hand_on(const AttnParams &p, int row, int head) {
+  p.handed_on[atomicAdd(&p.header_mut->handed_on, 1)] = make_int2(row, head);
+}
+
 cudaError_t prompt_plan_setup();  // once per device: shared-memory attributes
 cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s);
-cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s);
+cudaError_t prompt_merge_launch(const PromptPlan &p, const AttnParams &a, bool f32, cudaStream_t s);
 
 // query positions of a tile of 128 rows
 inline int prompt_tile_positions(int g) { return 128 / g; }

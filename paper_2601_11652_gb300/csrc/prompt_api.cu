@@ -57,7 +57,7 @@ wisp_status check(const wisp_shared_args *x) {
 }
 
 struct Space {
-  size_t status, header, q_row_start, req_flag, req_run, run_info, segs, items, partials, total;
+  size_t status, header, q_row_start, req_flag, req_run, run_info, segs, items, handed_on, partials, total;
   int64_t max_rows, partial_cap;
   int unit_rows;
   bool fits;
@@ -91,6 +91,7 @@ Space space(const wisp_attn_args *a, bool shared, int sms) {
   s.run_info = take(16 * B);
   s.segs = take(sizeof(Segment) * 2 * B);
   s.items = take(sizeof(WorkItem) * (size_t)s.max_rows);
+  s.handed_on = take(sizeof(int2) * (size_t)(T * a->Hq));
   s.partials = take(4 * (size_t)s.partial_cap);
   s.total = off;
   s.fits = s.max_rows * a->Hkv < INT32_MAX / 2 && s.partial_cap < INT32_MAX;
@@ -174,8 +175,9 @@ wisp_status call(const wisp_prompt_args *x, const int32_t *ids, const int32_t *p
   ap.header_mut = &p.header->h;
   ap.items = p.items;
   ap.partials = p.partials;
+  ap.handed_on = at<int2>(ws, sp.handed_on);
   cudaError_t e = bf ? prompt_tc_launch(ap, a->total_q_rows, grid, s) : prompt_f32_launch(ap, grid, s);
-  if (e == cudaSuccess) e = prompt_merge_launch(p, !bf, s);
+  if (e == cudaSuccess) e = prompt_merge_launch(p, ap, !bf, s);
   return e == cudaSuccess ? WISP_OK : WISP_ERR_CUDA;
 }
 

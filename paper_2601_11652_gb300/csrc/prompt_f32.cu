@@ -60,7 +60,8 @@ struct Cfg {
   static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V, by tile
   static constexpr int OFF_KX = OFF_VM + 32;      // uint32 [kSlots][4]: keys with values that are not finite, 16 a warp (two bits each)
   static constexpr int OFF_ODD = OFF_KX + kSlots * 16;     // int [2][3][D] first positions that see NaN, +inf, -inf
-  static constexpr int SMEM = OFF_ODD + 2 * 3 * D * 4 + 1024;  // + slack to align the base to 1024
+  static constexpr int OFF_FAR = OFF_ODD + 2 * 3 * D * 4;  // uint8 [128]: the row has had a reference far from zero
+  static constexpr int SMEM = OFF_FAR + kM + 1024;         // + slack to align the base to 1024
   static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
 };
 
@@ -138,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   float *s_ve = reinterpret_cast<float *>(smem + C::OFF_VE), *s_vm = reinterpret_cast<float *>(smem + C::OFF_VM);
   uint32_t *s_kx = reinterpret_cast<uint32_t *>(smem + C::OFF_KX);
   int *s_odd = reinterpret_cast<int *>(smem + C::OFF_ODD);
+  uint8_t *s_far = smem + C::OFF_FAR;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -171,6 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::fence_mbar_init();
   }
   for (int i = threadIdx.x; i < 2 * 3 * D; i += kThreads) s_odd[i] = INT32_MAX;
+  if (threadIdx.x < kM) s_far[threadIdx.x] = 0;
   if (warp == 14 && lane == 0) {
     ptx::prefetch_tmap(&tmk);
     ptx::prefetch_tmap(&tmv);
@@ -338,15 +341,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float top = fmaxf(mx[0], mx[1]) * fq;
         bool collected = t == 0;
         if (t == 0) {
-          m = top - kBelow;
+          m = floorf(top) - kBelow;
         } else {
           const bool move = mine && top > m + kLoose;
           if (__any_sync(0xffffffffu, move)) {
             // (the tile before still has the reference from before)
             collected = true;
             if (!collect(n - 1)) { ok = false; break; }
-            const float to = move ? top - kBelow : m;
+            const float to = move ? floorf(top) - kBelow : m;
             const float a = move ? ptx::ex2(m - to) : 1.0f;
+            if (move && is_far(m)) s_far[row] = 1;
             m = to;
             l *= a;
 #pragma unroll
@@ -385,6 +389,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!collected && !collect(n - 1)) { ok = false; break; }
       }
       if (!ok || !collect(n - 1)) { ok = false; break; }
+      const bool far = is_far(m) || s_far[row];
+      s_far[row] = 0;
       // ---- epilogue: the row through the warp's 2 KB in pieces of 64 bytes, so that four lanes store a row's piece together
       if (s_isodd[j & 1]) {
         const int *so = s_odd + (j & 1) * 3 * D;
@@ -428,7 +434,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (part && mine) {
         float *stat = p.partials + w.poff + (int64_t)w.rows * D + row;
         __stcg(stat, m);
-        __stcg(stat + w.rows, l);
+        __stcg(stat + w.rows, far ? marked(l) : l);
+      } else if (far && mine) {
+        hand_on(p, w.q0 + pos, w.h * g + hh0);
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));

@@ -4,6 +4,7 @@
 // runs, the segments (prompt.cuh), the chunk length and the items, longest first.
 #include "attn_merge.cuh"
 #include "prompt.cuh"
+#include "prompt_row.cuh"
 
 #include <algorithm>
 #include <cstring>
@@ -21,7 +22,7 @@ constexpr int kTile = 128;         // and are whole key tiles
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys (a table has fewer)
 constexpr int kMaxChunk = 1 << 28; // a segment's keys and two chunks stay below 2^31
 constexpr int kMaxRows = 1 << 24;  // k_r limit
-constexpr int kMergeThreads = 128;
+constexpr int kMergeThreads = 128, kMergePerSM = 3;  // of the merge; CTAs that fit an SM
 constexpr int kFew = 4, kHeads = 4; // chunks of a row, and rows, that a warp of the merge has in registers at once
 
 // Inclusive block scan; *total the block's sum.  One barrier: s_w (32 values) may be written again only after another one.
@@ -395,13 +396,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 // look for its own.  Up to kFew chunks, as almost always, every lane computes their weights itself.  Bound by instructions, then by the
 // partials' bytes (mostly in L2): 1300 rows of 32 heads of 128, three to five chunks each, 24 us.
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const PromptPlan p) {
+__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __grid_constant__ PromptPlan p, const __grid_constant__ AttnParams a) {
+  const int lane = threadIdx.x & 31;
+  // rows without partials that the attention has handed on, by the CTAs that are there at first (others would only look for their number)
+  const int cta = blockIdx.y * gridDim.x + blockIdx.x, takers = min((int)(gridDim.x * gridDim.y), kMergePerSM * p.sms);
+  int n_on = 0;
+  auto count = [&]() { n_on = cta < takers ? __ldcg(&p.header->h.handed_on) : 0; };
+  auto handed_on = [&]() {
+    for (int i = cta * (kMergeThreads / 32) + (threadIdx.x >> 5); i < n_on; i += takers * (kMergeThreads / 32)) {
+      const int2 x = __ldcg(a.handed_on + i);
+      prompt_row<D, T>(p, a, -1, x.x, x.y);
+    }
+  };
   // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
   if (!p.header->partials) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    count();
+    if (n_on) handed_on();
     return;
   }
-  const int lane = threadIdx.x & 31;
   const int g = p.Hq / p.Hkv, R = p.unit_rows;
   constexpr int CPL = D / 32;
   for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
@@ -409,6 +422,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
     const int run = p.req_run[r];
     const Segment pre = p.segs[run >= 0 ? p.B + run : r];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (r == blockIdx.x) count();
     if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
     const int subs = g / p.merge_heads, work = own.npos * p.Hkv * subs;
     for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
@@ -436,6 +450,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
       };
       Where w = where(h0);
       T *dst = static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + hk * g + h0) * D + lane * CPL;
+      bool again = false;  // a row has been handed on
       // a chunk none of whose keys a row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
       if (w.n[0] + w.n[1] <= kFew) {
         const int total = w.n[0] + w.n[1];
@@ -461,6 +476,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
 #pragma unroll
           for (int x = 0; x < kHeads; ++x) {
             if (hh + x >= p.merge_heads) break;
+            again = again || is_marked(lc[x][0]) || is_marked(lc[x][1]) || is_marked(lc[x][2]) || is_marked(lc[x][3]);
             float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
             for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
@@ -480,51 +496,64 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const Promp
             st_cols<CPL>(dst + (hh + x) * D, acc, 1.0f / den);
           }
         }
-        continue;
-      }
-      for (int hh = 0; hh < p.merge_heads; ++hh, dst += D) {
-        const int total = w.n[0] + w.n[1];
-        auto at = [&](const float *const (&base)[2], int c) {
-          return c < w.n[0] ? base[0] + c * w.step[0] : base[1] + (c - w.n[0]) * w.step[1];
-        };
-        float m = -INFINITY, den = 0.0f, acc[CPL];
+      } else {
+        for (int hh = 0; hh < p.merge_heads; ++hh, dst += D) {
+          const int total = w.n[0] + w.n[1];
+          auto at = [&](const float *const (&base)[2], int c) {
+            return c < w.n[0] ? base[0] + c * w.step[0] : base[1] + (c - w.n[0]) * w.step[1];
+          };
+          float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
-        for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
-        for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
-          const int c = c0 + lane;
-          float mc = -INFINITY, lc = 0.0f;
-          if (c < total) {
-            const float *q = at(w.pm, c) + hh;
-            mc = __ldcg(q);
-            lc = __ldcg(q + (c < w.n[0] ? w.nl[0] : w.nl[1]));
-          }
-          const float mn = fmaxf(m, ptx::warp_max(mc));
-          if (mn != m) {
-            const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
-            den = m == -INFINITY ? den : den * a;
+          for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
+          for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
+            const int c = c0 + lane;
+            float mc = -INFINITY, lc = 0.0f;
+            if (c < total) {
+              const float *q = at(w.pm, c) + hh;
+              mc = __ldcg(q);
+              lc = __ldcg(q + (c < w.n[0] ? w.nl[0] : w.nl[1]));
+              again = again || is_marked(lc);
+            }
+            const float mn = fmaxf(m, ptx::warp_max(mc));
+            if (mn != m) {
+              const float a = m == -INFINITY ? 0.0f : ptx::ex2(m - mn);
+              den = m == -INFINITY ? den : den * a;
 #pragma unroll
-            for (int q = 0; q < CPL; ++q) acc[q] *= a;
-            m = mn;
-          }
-          const float f = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
-          den = mc == -INFINITY ? den + lc : fmaf(lc, f, den);
-          const int nc = min(32, total - c0);
+              for (int q = 0; q < CPL; ++q) acc[q] *= a;
+              m = mn;
+            }
+            const float f = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
+            den = mc == -INFINITY ? den + lc : fmaf(lc, f, den);
+            const int nc = min(32, total - c0);
 #pragma unroll 4
-          for (int i = 0; i < nc; ++i) {
-            const float fi = __shfl_sync(0xffffffffu, f, i);
-            float v[CPL];
-            ld_cols<CPL>(at(w.po, c0 + i) + hh * D, v);
+            for (int i = 0; i < nc; ++i) {
+              const float fi = __shfl_sync(0xffffffffu, f, i);
+              float v[CPL];
+              ld_cols<CPL>(at(w.po, c0 + i) + hh * D, v);
 #pragma unroll
-            for (int q = 0; q < CPL; ++q)
-              if (!(fi < 0.0f)) acc[q] = fmaf(v[q], fi, acc[q]);
+              for (int q = 0; q < CPL; ++q)
+                if (!(fi < 0.0f)) acc[q] = fmaf(v[q], fi, acc[q]);
+            }
           }
-        }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-        st_cols<CPL>(dst, acc, 1.0f / den);
+          for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+          st_cols<CPL>(dst, acc, 1.0f / den);
+        }
+      }
+      if (__any_sync(0xffffffffu, again)) {
+        const int total = w.n[0] + w.n[1];
+        for (int hh = 0; hh < p.merge_heads; ++hh) {
+          bool mine = false;
+          for (int c = lane; c < total; c += 32) {
+            const bool z = c < w.n[0];
+            mine = mine || is_marked(__ldcg((z ? w.pm[0] + c * w.step[0] + w.nl[0] : w.pm[1] + (c - w.n[0]) * w.step[1] + w.nl[1]) + hh));
+          }
+          if (__any_sync(0xffffffffu, mine)) prompt_row<D, T>(p, a, r, own.q0 + j, hk * g + h0 + hh);
+        }
       }
     }
   }
+  if (n_on) handed_on();
 }
 
 namespace {
@@ -559,13 +588,13 @@ cudaError_t prompt_plan_launch(const PromptPlan &p, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s) {
+cudaError_t prompt_merge_launch(const PromptPlan &p, const AttnParams &a, bool f32, cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  // about 12 CTAs per SM (three fit), or one per four warps that have work
+  // about 12 CTAs per SM (kMergePerSM fit), or one per four warps that have work
   const int most = p.sms * 12;
   const int64_t ctas = std::min<int64_t>(most, ((int64_t)p.total_q_rows * p.Hq / p.merge_heads + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
   const int cols = std::min(p.B, most);
@@ -574,8 +603,8 @@ cudaError_t prompt_merge_launch(const PromptPlan &p, bool f32, cudaStream_t s) {
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (f32) return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, float> : prompt_merge_kernel<64, float>, p);
-  return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, uint16_t> : prompt_merge_kernel<64, uint16_t>, p);
+  if (f32) return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, float> : prompt_merge_kernel<64, float>, p, a);
+  return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, uint16_t> : prompt_merge_kernel<64, uint16_t>, p, a);
 }
 
 }  // namespace wisp

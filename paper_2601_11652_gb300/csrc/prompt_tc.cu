@@ -76,7 +76,8 @@ struct Cfg {
   static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;       // tmem base, abort flag, odd-value flags
   static constexpr int OFF_ML = OFF_MISC + 64;                     // float [2][128]: m, l of stream 1 for the join
   static constexpr int OFF_ODD = OFF_ML + 2 * kM * 4;              // int [2][3][D] first positions that see NaN, +inf, -inf
-  static constexpr int SMEM = OFF_ODD + 2 * 3 * D * 4 + 1024;      // + slack to align the base to 1024
+  static constexpr int OFF_FAR = OFF_ODD + 2 * 3 * D * 4;          // uint8 [2][128]: the row has had a reference far from zero
+  static constexpr int SMEM = OFF_FAR + 2 * kM + 1024;             // + slack to align the base to 1024
   static_assert(SMEM <= 227 * 1024, "shared memory of one CTA on sm_103a");
 };
 
@@ -108,13 +109,6 @@ __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile i
       return false;
     }
   }
-}
-
-// two values in bf16, rounded to nearest; past its range (and infinite) its largest
-__device__ __forceinline__ uint32_t bf16x2_sat(float a, float b) {
-  uint32_t r;
-  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
 }
 
 // What the roles need to know of an item.
@@ -169,6 +163,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   volatile int *s_isodd = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 8);  // [2] an item's V held odd values
   float *s_ml = reinterpret_cast<float *>(smem + C::OFF_ML);
   int *s_odd = reinterpret_cast<int *>(smem + C::OFF_ODD);
+  uint8_t *s_far = smem + C::OFF_FAR;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -207,6 +202,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
     ptx::fence_mbar_init();
   }
   for (int i = threadIdx.x; i < 2 * 3 * D; i += kThreads) s_odd[i] = INT32_MAX;
+  if (threadIdx.x < 2 * kM) s_far[threadIdx.x] = 0;
   if (warp == 9 && lane == 0) {
     ptx::prefetch_tmap(&tmq);
     ptx::prefetch_tmap(&tmk);
@@ -306,7 +302,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           return true;
         };
         if (t == first) {
-          m = top;
+          m = floorf(top);
         } else {
           if (C::P_APART && !kBeside && !finish()) { ok = false; break; }
           const bool move = mine && top > m + kLoose;
@@ -316,8 +312,10 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               if (!finish()) { ok = false; break; }
               done = true;
             }
-            const float a = move ? ptx::ex2(m - top) : 1.0f;
-            if (move) m = top;
+            const float to = move ? floorf(top) : m;
+            const float a = move ? ptx::ex2(m - to) : 1.0f;
+            if (move && is_far(m)) s_far[threadIdx.x] = 1;
+            m = to;
             l *= a;
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
@@ -363,6 +361,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       }
       if (!ok) break;
       // ---- epilogue: the row's O
+      bool far = is_far(m) || s_far[threadIdx.x];
+      s_far[threadIdx.x] = 0;
       const bool join = sh.split && sh.nt > 1;
       const bool any = first < sh.nt;
       if (any) {
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       if (join) {
         if (s == 1) {
           s_ml[row] = m;
-          s_ml[kM + row] = l;
+          s_ml[kM + row] = far ? marked(l) : l;
           ptx::tc_fence_before();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(B::ML_FULL));
@@ -384,6 +384,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           if (!wait_bar(bar(B::ML_FULL), nml & 1, s_abort)) { ok = false; break; }
           ptx::tc_fence_after();
           const float m1 = s_ml[row], l1 = s_ml[kM + row];
+          far = far || is_marked(l1);
           const float mj = fmaxf(m, m1);
           a0 = m == -INFINITY ? 0.0f : ptx::ex2(m - mj);
           a1 = m1 == -INFINITY ? 0.0f : ptx::ex2(m1 - mj);
@@ -480,7 +481,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
         if (part && mine) {
           float *stat = p.partials + w.poff + (int64_t)w.rows * D + tile * tile_rows + row;
           __stcg(stat, m);
-          __stcg(stat + w.rows, l);
+          __stcg(stat + w.rows, far ? marked(l) : l);
+        } else if (far && mine) {
+          hand_on(p, w.q0 + pos, w.h * g + row % g);
         }
         ptx::tc_fence_before();
         __syncwarp();

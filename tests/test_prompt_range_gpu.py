@@ -1,0 +1,70 @@
+"""The attention of prompts and of shared prefixes at the ends of what its types hold: finite inputs give finite outputs, and what a row
+does not see changes none of its bits.  Definition and bounds as in test_prompt_gpu.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_prompt_gpu import BF, F32, PAGE, TYPES, Case, _lib, bits_of, runs_of  # noqa: F401 (_lib builds the library)
+
+pytestmark = pytest.mark.gpu
+
+
+def scale_tokens(c, x, a, b, e):
+    """K or V (x) of tokens a .. b - 1 of every request times 2^e: in the cache, or in the scales of an e4m3 cache (whole pages)."""
+    for r in range(len(c.k)):
+        L = c.ctx[r] + c.k[r] + 1
+        for p in range(a // PAGE, (min(b, L) + PAGE - 1) // PAGE):
+            page = int(c.bt[r, p])
+            if x + "_scale" in c.t:
+                assert a % PAGE == 0 and (b % PAGE == 0 or b >= L)
+                c.t[x + "_scale"][page] *= 2.0 ** e
+                c.val[x][page] = c.t[x + "_cache"][page].double() * c.t[x + "_scale"][page].double()[:, None, None]
+            else:
+                s = slice(max(a - p * PAGE, 0), min(b - p * PAGE, PAGE))
+                y = c.t[x + "_cache"]
+                y[page, :, s] = (y[page, :, s].double() * 2.0 ** e).to(y.dtype)
+                c.val[x][page, :, s] = y[page, :, s].double()
+
+
+def far_scores(c, e):
+    """Scores of up to 2^e sqrt(D), in steps of a quarter of that.  Every sum is a whole number of small powers of two, exact in any order, so
+    that equal scores are equal, and a row is the mean of V over the keys of its largest score; other weights are below 2^-126 but where e is
+    small, and there check()'s bounds hold as anywhere."""
+    g = torch.Generator(device="cuda").manual_seed(e)
+    a = e // 2
+    c.t["q"].fill_(2.0 ** a)
+    shape = c.t["k_cache"].shape[:3]
+    u = torch.tensor([1.0, 0.75, 0.5, -1.0], device="cuda")[torch.randint(0, 4, shape, generator=g, device="cuda")]
+    u[:, :, 0] = 0.5
+    u[torch.rand(shape[0], generator=g, device="cuda") < 0.7] = -1.0  # (whole tiles without the largest, too)
+    u = u[..., None].expand(*shape, c.D)
+    if "k_scale" in c.t:
+        c.t["k_cache"] = u.to(torch.float8_e4m3fn).contiguous()
+        c.t["k_scale"].fill_(2.0 ** (e - a))
+    else:
+        c.t["k_cache"] = (u * 2.0 ** (e - a)).to(c.t["q"].dtype).contiguous()
+    c.val["k"] = u.double() * 2.0 ** (e - a)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("e", [13, 15, 16, 17, 18, 24, 26, 28, 30, 33, 40, 100])
+def test_scores_far_from_zero(dtype, cache, D, e):
+    c = Case(e + D, k=[250, 3, 61], ctx=[0, 70, 500], Hq=4, Hkv=2, D=D, dtype=dtype, cache=cache)
+    far_scores(c, e)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads", [(8, 8, 64), (28, 4, 128)])
+@pytest.mark.parametrize("k,ctx,runs", [([3], [40000], None), ([9, 0, 30, 2], [3000, 700, 5000, 2000], None),
+                                        ([1, 0, 4, 2, 7], [350, 320, 900, 64, 3000], runs_of((0, 20, 3), (-1, 0, 1), (1, 7, 1)))])
+def test_scores_far_from_zero_in_chunks(dtype, cache, heads, k, ctx, runs):
+    c = Case(5, k=k, ctx=ctx, Hq=heads[0], Hkv=heads[1], D=heads[2], dtype=dtype, cache=cache, runs=runs)
+    far_scores(c, 40)
+    c.t["q"][2:4] *= 2.0 ** -40  # (a row whose scores are small beside them)
+    c.run()
+    c.check()
