@@ -31,7 +31,8 @@ extern "C" {
  * (relative error 2^-9), and so do code * scale of an e4m3 cache, K and V (exactly where the scale is a power of two of magnitude 2^-100
  * to 2^100; values past the bf16 range count as its largest).  With fp32 queries every factor enters its product with
  * 22 significant bits or more: queries, and K and V of an fp32 cache, down to steps of 2^-38 of the largest value of their row; a weight times its
- * key's largest |V| (its V scale) down to steps of 2^-36 of the row's largest weight times the largest such value among 64 consecutive keys.
+ * key's largest |V| (its V scale) down to steps of 2^-36 of the row's largest weight times the largest such value that the row sees among 64
+ * consecutive keys.
  * A key that a row does not see adds nothing to it, whatever its K and V hold (NaN and infinities too; slots past a request's
  * tokens may hold anything).  A NaN that a row does see, or a row whose scores are all -inf, makes that row NaN (of V: in its element).
  */

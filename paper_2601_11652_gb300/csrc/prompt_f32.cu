@@ -34,8 +34,9 @@ constexpr int kBT = 64;       // keys per tile
 constexpr int kM = 128;       // rows
 constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;  // S at 0 and 64, P at 128 and 192 (h, then l), O at 256 and 384
-constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
+constexpr uint32_t kWaitCycles = 3000000000u;  // about one and a half seconds: a wait that long is a failure
 constexpr float kLoose = 14.0f, kBelow = 11.0f;  // log2: weights are at most 2^kLoose; a moved reference lies kBelow under the maximum
+constexpr int kLeast = -90;   // of d (see there): rows beyond are handed on, as their small weights times 2^d are no normal numbers
 constexpr int kItemRing = 2;
 constexpr int kSlots = 8;     // of the keys' factors, by tile: the eighth next tile is converted after this one's softmax is done
 
@@ -56,8 +57,8 @@ struct Cfg {
   static constexpr int OFF_MISC = OFF_RING + kItemRing * 64;
   static constexpr int OFF_KF = OFF_MISC + 64;             // float [kSlots][64]: factors of the keys' scores
   static constexpr int OFF_VF = OFF_KF + kSlots * kBT * 4; // float [kSlots][64]: factors of the keys' weights
-  static constexpr int OFF_VE = OFF_VF + kSlots * kBT * 4; // float [kSlots]: factor of the tile's P V
-  static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V, by tile
+  static constexpr int OFF_VE = OFF_VF + kSlots * kBT * 4; // int [kSlots]: exponent that the tile's factors are relative to
+  static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V (or the first key's), by tile
   static constexpr int OFF_KX = OFF_VM + 32;      // uint32 [kSlots][4]: keys with values that are not finite, 16 a warp (two bits each)
   static constexpr int OFF_ODD = OFF_KX + kSlots * 16;     // int [2][3][D] first positions that see NaN, +inf, -inf
   static constexpr int OFF_FAR = OFF_ODD + 2 * 3 * D * 4;  // uint8 [128]: the row has had a reference far from zero
@@ -80,16 +81,16 @@ struct Bars {
 };
 
 __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort) {
-  if (ptx::mbar_try_wait(b, parity)) return true;
-  const long long t0 = clock64();
-  while (true) {
-    if (ptx::mbar_try_wait(b, parity)) return true;
+  const uint32_t t0 = clock();
+#pragma unroll 1
+  while (!ptx::mbar_try_wait(b, parity)) {
     if (*abort) return false;
-    if (clock64() - t0 > kWaitCycles) {
+    if ((uint32_t)clock() - t0 > kWaitCycles) {
       *abort = 1;
       return false;
     }
   }
+  return true;
 }
 
 // Instruction descriptor, kind::f16: fp32 accumulate, fp16 A (K-major) and B.
@@ -100,6 +101,8 @@ __device__ constexpr uint32_t idesc_f16(int N, bool b_mn_major) {
 // The exponent e of a row whose largest finite magnitude is `amax`: values times 2^-e stay below 2^15.  (2^-e and 2^e are normal numbers.)
 __device__ __forceinline__ int row_exp(float amax) { return max((int)(__float_as_uint(amax) >> 23) - 127 - 14, -126); }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+// The exponent of a factor (0 of 0).
+__device__ __forceinline__ int exp_of(float x) { return x > 0.0f ? max((int)(__float_as_uint(x) >> 23) - 127, -126) : 0; }
 
 __device__ __forceinline__ uint32_t h2(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
@@ -136,7 +139,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int *s_abort = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 4);
   volatile int *s_isodd = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 8);  // [2]
   float *s_kf = reinterpret_cast<float *>(smem + C::OFF_KF), *s_vf = reinterpret_cast<float *>(smem + C::OFF_VF);
-  float *s_ve = reinterpret_cast<float *>(smem + C::OFF_VE), *s_vm = reinterpret_cast<float *>(smem + C::OFF_VM);
+  int *s_ve = reinterpret_cast<int *>(smem + C::OFF_VE);
+  float *s_vm = reinterpret_cast<float *>(smem + C::OFF_VM);
   uint32_t *s_kx = reinterpret_cast<uint32_t *>(smem + C::OFF_KX);
   int *s_odd = reinterpret_cast<int *>(smem + C::OFF_ODD);
   uint8_t *s_far = smem + C::OFF_FAR;
@@ -256,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(bar(B::Q_FULL));
 
       float m = -INFINITY, l = 0.0f;
+      int ev = 0;  // of the tile before
       float2 o[D / 2];
 #pragma unroll
       for (int i = 0; i < D / 2; ++i) o[i] = make_float2(0.0f, 0.0f);
@@ -264,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int b = k & 1;
         if (!wait_bar(bar(B::O_FULL + b), (k >> 1) & 1, s_abort)) return false;
         ptx::tc_fence_after();
-        const float f = s_ve[k % kSlots];
+        const float f = pow2(ev);
         const float2 f2 = make_float2(f, f);
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
@@ -285,6 +290,53 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int b = n & 1, slot = n % kSlots;
         if (!wait_bar(bar(B::S_FULL + b), (n >> 1) & 1, s_abort)) { ok = false; break; }
         ptx::tc_fence_after();
+        const int base = w.t0 + t * kBT;
+        const float *vf = s_vf + slot * kBT;
+        int d = 0;
+        // Scores that are not those of the product are put right where they lie, in TMEM: the code of a tile's usual way, and of the other roles beside
+        // it, has to stay in the instruction cache (with this in registers 4096 tokens took 668 us, 610 so; heads of 64 423 and 387).
+        const uint4 kx = KV8 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4 *>(s_kx + slot * 4);
+        if ((kx.x | kx.y | kx.z | kx.w) || base + kBT > all) {
+          const uint32_t t_s = tmem + lanes + b * kBT;
+          if (kx.x | kx.y | kx.z | kx.w) {
+            // scores of keys with values that are not finite, from the values themselves
+#pragma unroll 1
+            for (int k = 0; k < kBT; ++k) {
+              const uint32_t word = k < 16 ? kx.x : k < 32 ? kx.y : k < 48 ? kx.z : kx.w;
+              if (!((word >> (2 * (k & 15))) & 3u) || base + k >= w.t1) continue;
+              const int bid = __ldg(p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + (base + k) / 16);
+              const float *kr = static_cast<const float *>(p.k_cache) + (((int64_t)bid * p.Hkv + w.h) * 16 + (base + k) % 16) * D;
+              float s = 0.0f;
+              if (mine)
+                for (int c = 0; c < D; ++c) s = fmaf(__ldg(qrow + c), __ldg(kr + c), s);
+              __syncwarp();
+              ptx::tmem_st1(t_s + k, __float_as_uint(s * (scale / fq)));
+            }
+            ptx::tmem_wait_st();
+          }
+          if (base + kBT > all) {
+            const int seen = end - base;
+#pragma unroll 1
+            for (int c = 0; c < kBT; c += 16) {
+              uint32_t y[16];
+              ptx::tmem_ld16(t_s + c, y);
+              ptx::tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (c + i >= seen) y[i] = 0xff800000u;
+              ptx::tmem_st16(t_s + c, y);
+            }
+            ptx::tmem_wait_st();
+            // Here V's factors are relative to the first key's (elsewhere to the largest), and a row's weights are computed with 2^d, d the distance to
+            // the largest factor that it sees (d goes back into their sum and into P V): what it does not see has no say in its bits.
+            if (!wait_bar(bar(B::V_FULL + n % C::NS), (n / C::NS) & 1, s_abort)) { ok = false; break; }
+            float most = 0.0f;
+#pragma unroll 4
+            for (int i = 0; i < kBT; ++i) most = fmaxf(most, i < seen ? vf[i] : 0.0f);
+            d = -exp_of(most);
+            if (d < kLeast) s_far[row] = 1;
+          }
+        }
         uint32_t x[2][32];
         ptx::tmem_ld32(tmem + lanes + b * kBT, x[0]);
         ptx::tmem_ld32(tmem + lanes + b * kBT + 32, x[1]);
@@ -303,33 +355,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           y[1] = __float_as_uint(u.y);
           y[2] = __float_as_uint(v.x);
           y[3] = __float_as_uint(v.y);
-        }
-        const int base = w.t0 + t * kBT;
-        if (!KV8) {
-          // scores of keys with values that are not finite, from the values themselves
-          const uint4 kx = *reinterpret_cast<const uint4 *>(s_kx + slot * 4);
-          if (kx.x | kx.y | kx.z | kx.w) {
-#pragma unroll 1
-            for (int k = 0; k < kBT; ++k) {
-              const uint32_t word = k < 16 ? kx.x : k < 32 ? kx.y : k < 48 ? kx.z : kx.w;
-              if (!((word >> (2 * (k & 15))) & 3u) || base + k >= w.t1) continue;
-              const int bid = __ldg(p.block_tables + (int64_t)w.r * p.max_blocks_per_seq + (base + k) / 16);
-              const float *kr = static_cast<const float *>(p.k_cache) + (((int64_t)bid * p.Hkv + w.h) * 16 + (base + k) % 16) * D;
-              float s = 0.0f;
-              if (mine)
-                for (int c = 0; c < D; ++c) s = fmaf(__ldg(qrow + c), __ldg(kr + c), s);
-              s *= scale / fq;
-#pragma unroll
-              for (int i = 0; i < kBT; ++i)
-                if (i == k) x[i >> 5][i & 31] = __float_as_uint(s);
-            }
-          }
-        }
-        if (base + kBT > all) {
-          const int seen = end - base;
-#pragma unroll
-          for (int i = 0; i < kBT; ++i)
-            if (i >= seen) x[i >> 5][i & 31] = 0xff800000u;
         }
         float mx[2];
 #pragma unroll
@@ -357,11 +382,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < D / 2; ++i) o[i] = __fmul2_rn(o[i], make_float2(a, a));
           }
         }
-        const float mm = m == -INFINITY ? 0.0f : -m;  // (nothing seen so far: every weight is zero)
-        const float2 m2 = make_float2(mm, mm), fq2 = make_float2(fq, fq);
-        const float *vf = s_vf + slot * kBT;
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
         if (!wait_bar(bar(B::V_FULL + n % C::NS), (n / C::NS) & 1, s_abort)) { ok = false; break; }  // (its factors)
+        const float mm = (m == -INFINITY ? 0.0f : -m) + (float)d;  // (nothing seen so far: every weight is zero)
+        const float2 m2 = make_float2(mm, mm), fq2 = make_float2(fq, fq);
 #pragma unroll
         for (int c = 0; c < kBT; c += 16) {
           uint32_t ph[8], pl[8];
@@ -372,36 +396,27 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int q = 0; q < 2; ++q) {
               const uint32_t *y = &x[(c + i) >> 5][((c + i) & 31) + 2 * q];
               const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), fq2, m2);
-              const float2 e = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
-              sum[q] = __fadd2_rn(sum[q], e);
-              const float2 u = __fmul2_rn(e, q == 0 ? make_float2(f.x, f.y) : make_float2(f.z, f.w));
+              const float2 p2 = make_float2(ptx::ex2(a.x), ptx::ex2(a.y));
+              sum[q] = __fadd2_rn(sum[q], p2);
+              const float2 u = __fmul2_rn(p2, q == 0 ? make_float2(f.x, f.y) : make_float2(f.z, f.w));
               split2(u.x, u.y, ph[i / 2 + q], pl[i / 2 + q]);
             }
           }
           ptx::tmem_st8(tmem + lanes + 128 + b * 64 + c / 2, ph);
           ptx::tmem_st8(tmem + lanes + 128 + b * 64 + 32 + c / 2, pl);
         }
-        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        l = fmaf((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y), pow2(-d), l);
         ptx::tmem_wait_st();
         ptx::tc_fence_before();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + b));
         if (!collected && !collect(n - 1)) { ok = false; break; }
+        ev = s_ve[slot] - d;
       }
       if (!ok || !collect(n - 1)) { ok = false; break; }
       const bool far = is_far(m) || s_far[row];
       s_far[row] = 0;
       // ---- epilogue: the row through the warp's 2 KB in pieces of 64 bytes, so that four lanes store a row's piece together
-      if (s_isodd[j & 1]) {
-        const int *so = s_odd + (j & 1) * 3 * D;
-#pragma unroll
-        for (int i = 0; i < D; ++i) {
-          float &v = i & 1 ? o[i / 2].y : o[i / 2].x;
-          const bool nan = pos >= so[i], up = pos >= so[D + i], down = pos >= so[2 * D + i];
-          if (nan || (up && down)) v = __uint_as_float(0x7fffffffu);
-          else if (up || down) v += up ? INFINITY : -INFINITY;
-        }
-      }
       const bool part = w.poff >= 0;
       const float inv = part ? 1.0f : 1.0f / l;
       uint8_t *stage = smem + C::OFF_ST + warp * 2048;
@@ -418,8 +433,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int c = 0; c < D; c += 16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 a = o[(c + 4 * i) / 2], b = o[(c + 4 * i) / 2 + 1];
-          *reinterpret_cast<float4 *>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = make_float4(a.x * inv, a.y * inv, b.x * inv, b.y * inv);
+          const float2 c1 = __fmul2_rn(o[(c + 4 * i) / 2], make_float2(inv, inv)), c2 = __fmul2_rn(o[(c + 4 * i) / 2 + 1], make_float2(inv, inv));
+          *reinterpret_cast<float4 *>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = make_float4(c1.x, c1.y, c2.x, c2.y);
         }
         __syncwarp();
 #pragma unroll
@@ -430,6 +445,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                    *reinterpret_cast<const float4 *>(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)));
         }
         __syncwarp();
+      }
+      if (s_isodd[j & 1]) {  // V held values that are not finite: what they make of the rows that see them (short code: see the scores)
+        const int *so = s_odd + (j & 1) * 3 * D;
+        float *at = part ? p.partials + w.poff + (int64_t)row * D : static_cast<float *>(p.out) + ((int64_t)(w.q0 + pos) * p.Hq + w.h * g + hh0) * D;
+#pragma unroll 1
+        for (int i = 0; i < D; ++i) {
+          const bool nan = pos >= so[i], up = pos >= so[D + i], down = pos >= so[2 * D + i];
+          if (mine && (nan || up || down)) at[i] = __ldcg(at + i) + (nan || (up && down) ? __uint_as_float(0x7fffffffu) : up ? INFINITY : -INFINITY);
+        }
       }
       if (part && mine) {
         float *stat = p.partials + w.poff + (int64_t)w.rows * D + row;
@@ -458,6 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     WorkItem w;
     for (uint32_t j = 0; ok && next_item(j, w, ok); ++j) {
       const int nt = tiles_of(w), ob = j & 1;
+      const int all = min(w.t1, w.ctx + w.rg * tile_pos + 1);  // keys that the first row sees
       if (!is_k) {
         // this item's buffer of odd values: free, and cleared where it was used
         if (!wait_bar(bar(B::ODD_FREE + ob), ((j >> 1) & 1) ^ 1, s_abort)) { ok = false; break; }
@@ -487,6 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint8_t *tile = smem + off + st * C::TILE;
         const int at_key = w.t0 + t * kBT + key;
         const bool real = at_key < w.t1;  // (others are nobody's and count as zeros)
+        const bool part = w.t0 + (t + 1) * kBT > all;
         uint32_t h[E / 2], l[KV8 ? 1 : E / 2];
         float f;  // the key's factor
         bool nonfinite = false;
@@ -563,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
           const int e = row_exp(amax);
           const float s = pow2(-e);
-          f = pow2(e);
+          f = is_k || amax > 0.0f ? pow2(e) : 0.0f;
 #pragma unroll
           for (int i = 0; i < E; i += 2) {
             const float2 y = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(s, s));
@@ -572,23 +598,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!real) f = 0.0f;
         if (is_k) {
-          if (half == 0) s_kf[slot * kBT + key] = real ? f : 1.0f;
+          if (half == 0) s_kf[slot * kBT + key] = real ? fmaxf(f, 0x1p-149f) : 1.0f;  // (not zero: masked scores are -inf before it comes in)
           if (!KV8) {
             const uint32_t odd = __ballot_sync(0xffffffffu, nonfinite && real);
             if (lane == 0) s_kx[slot * 4 + warp - 4] = odd;
           }
         } else {
-          // the tile's largest factor: those of the weights are relative to its power of two
-          const float wm = ptx::warp_max(f);
+          // what the tile's factors are relative to: the power of two of the largest, or where some row does not see all keys, of the first key's
+          const float wm = part ? f : ptx::warp_max(f);
           if (lane == 0) s_vm[(n & 1) * 4 + warp - 8] = wm;
         }
         if (!together()) { ok = false; break; }  // the tile is in registers
         if (!is_k && half == 0) {
+          // (a factor that is 2^120 of the first key's or more counts for rows that do not see it)
           const float4 m4 = *reinterpret_cast<const float4 *>(s_vm + (n & 1) * 4);
-          const float top = fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w));
-          const int e = top > 0.0f ? min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126) : 0;
-          s_vf[slot * kBT + key] = f * pow2(-e);
-          if (id == 0) s_ve[slot] = pow2(e);
+          const int e = exp_of(part ? m4.x : fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w))), e2 = e / 2;
+          s_vf[slot * kBT + key] = fminf(f * pow2(-e2) * pow2(e2 - e), 0x1p120f);
+          if (id == 0) s_ve[slot] = e;
         }
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -655,17 +681,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int b0 = __shfl_sync(0xffffffffu, bid, 0);
           const bool row4 = __ballot_sync(0xffffffffu, lane < 4 && valid && bid == b0 + lane) == 0xfu;
           if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
-          int bids[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) bids[x] = __shfl_sync(0xffffffffu, bid, x);
-          if (ptx::elect_one()) {
+          if (lane == 0) {
             ptx::mbar_arrive_expect_tx(bar(full), kRaw);
-            if (row4) {
-              ptx::tma_load_4d(dst, is_k ? &tmk4 : &tmv4, bar(full), 0, 0, w.h, b0);
-            } else {
-#pragma unroll
-              for (int x = 0; x < 4; ++x) ptx::tma_load_4d(dst + x * (kRaw / 4), is_k ? &tmk : &tmv, bar(full), 0, 0, w.h, bids[x]);
-            }
+            if (row4) ptx::tma_load_4d(dst, is_k ? &tmk4 : &tmv4, bar(full), 0, 0, w.h, b0);
+          }
+#pragma unroll 1
+          for (int x = 0; x < 4 && !row4; ++x) {
+            const int one = __shfl_sync(0xffffffffu, bid, x);
+            if (lane == 0) ptx::tma_load_4d(dst + x * (kRaw / 4), is_k ? &tmk : &tmv, bar(full), 0, 0, w.h, one);
           }
           __syncwarp();
           return true;
@@ -675,7 +698,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             cur = next;
             next = fetch((t >> 3) + 1);
           }
-          ok = load(true, t) && load(false, t);
+#pragma unroll 1
+          for (int kv = 0; kv < 2 && ok; ++kv) ok = load(kv == 0, t);
           if (t == max(nt - 4, 0)) claim();  // the next item, early enough to hide the way to it
         }
         if (!ok) break;
@@ -683,12 +707,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
       // drain: what was issued must land before the CTA's shared memory goes away
       if (lane == 0) {
+#pragma unroll 1
         for (int x = 0; x < 2; ++x) {
           const int full = x ? B::VR_FULL : B::KR_FULL;
           const uint32_t n = x ? nv : nk;
+#pragma unroll 1
           for (uint32_t k = 0; k < C::NS && k < n; ++k) {
-            const long long t0 = clock64();
-            while (!ptx::mbar_try_wait(bar(full + (n - 1 - k) % C::NS), ((n - 1 - k) / C::NS) & 1) && clock64() - t0 < kWaitCycles) {
+            const uint32_t t0 = clock();
+            while (!ptx::mbar_try_wait(bar(full + (n - 1 - k) % C::NS), ((n - 1 - k) / C::NS) & 1) && (uint32_t)clock() - t0 < kWaitCycles) {
             }
           }
         }
@@ -712,7 +738,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q, 16, 1024);
               const uint64_t kd = ptx::sdesc_sw128(sbase + C::OFF_K + st * C::TILE, 16, 1024);
               // l h, h l, h h
-#pragma unroll
+#pragma unroll 1
               for (int x = 0; x < 3; ++x) {
                 if (KV8 && x == 1) continue;
 #pragma unroll
@@ -733,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ptx::elect_one()) {
               ptx::tc_fence_after();
               const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::KHALF, 1024);
-#pragma unroll
+#pragma unroll 1
               for (int x = 0; x < 3; ++x) {
                 if (KV8 && x == 1) continue;
 #pragma unroll
@@ -751,8 +777,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ptx::elect_one()) {
         // every MMA issued must finish before the TMEM is released
         ptx::umma_commit(bar(B::MMA_DONE));
-        const long long t0 = clock64();
-        while (!ptx::mbar_try_wait(bar(B::MMA_DONE), 0) && clock64() - t0 < kWaitCycles) {
+        const uint32_t t0 = clock();
+        while (!ptx::mbar_try_wait(bar(B::MMA_DONE), 0) && (uint32_t)clock() - t0 < kWaitCycles) {
         }
       }
     }
@@ -764,8 +790,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   ptx::tc_fence_before();
   if (lane == 0) ptx::mbar_arrive(bar(B::FIN));
   if (warp == 12) {
-    const long long t0 = clock64();
-    while (!ptx::mbar_try_wait(bar(B::FIN), 0) && clock64() - t0 < kWaitCycles) {
+    const uint32_t t0 = clock();
+    while (!ptx::mbar_try_wait(bar(B::FIN), 0) && (uint32_t)clock() - t0 < kWaitCycles) {
     }
     __syncwarp();
     ptx::tc_fence_after();

@@ -68,3 +68,41 @@ def test_scores_far_from_zero_in_chunks(dtype, cache, heads, k, ctx, runs):
     c.t["q"][2:4] *= 2.0 ** -40  # (a row whose scores are small beside them)
     c.run()
     c.check()
+
+
+SPLIT = ([250, 3, 190, 61], [0, 70, 33, 500])  # rows and contexts; what changes lies in the middle of tiles
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [16, 48, 160, 528])
+@pytest.mark.parametrize("e", [40, 100])
+def test_values_behind_a_row_change_none_of_its_bits(dtype, cache, D, at, e):
+    k, ctx = SPLIT
+    c = Case(at + D, k=k, ctx=ctx, Hq=4, Hkv=2, D=D, dtype=dtype, cache=cache)
+    c.run()
+    c.check()
+    before = c.t["out"].clone()
+    scale_tokens(c, "v", at, 1 << 20, e)
+    c.run()
+    for r in range(len(k)):
+        n = min(max(at - ctx[r], 0), k[r] + 1)  # rows that do not see them
+        row = c.row_of(r)
+        assert torch.equal(c.t["out"][row:row + n], before[row:row + n]), r
+    assert torch.isfinite(c.t["out"]).all()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("runs", [None, runs_of((0, 20, 3))])
+@pytest.mark.parametrize("e", [-80, -40, 30, 44, 60, 80])
+def test_outputs_scale_with_values(dtype, cache, runs, e):
+    """Powers of two in all of V are powers of two in the outputs, bit by bit."""
+    c = Case(23, k=[140, 9, 30], ctx=[320, 350, 2000], Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache, runs=runs)
+    c.run()
+    before = c.t["out"].clone()
+    if cache:
+        c.t["v_scale"] *= 2.0 ** e
+    else:
+        c.t["v_cache"] = (c.t["v_cache"].double() * 2.0 ** e).to(dtype)
+    c.run()
+    assert torch.equal(c.t["out"].double(), before.double() * 2.0 ** e)
