@@ -80,6 +80,9 @@ __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D 
 // where it is far from zero the largest weight is not 2^0 but up to 2^(half a step of m): references are whole numbers, exact up to 2^24, and a row
 // that has had one beyond kFar is computed once more.
 //
+// The kernel for fp32 queries hands on rows whose queries are past 2^44, and (rows of a tile that not all see) rows whose largest V is 2^90 times
+// that of the tile's first key.
+//
 // A row of an item that writes outputs goes into a list; of one that leaves partials the sign of l says it (l is never negative).
 constexpr float kFar = 0x1p20f;
 __device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabsf(m) < INFINITY; }

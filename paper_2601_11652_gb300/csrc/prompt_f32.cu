@@ -36,6 +36,7 @@ constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;  // S at 0 and 64, P at 128 and 192 (h, then l), O at 256 and 384
 constexpr uint32_t kWaitCycles = 3000000000u;  // about one and a half seconds: a wait that long is a failure
 constexpr float kLoose = 14.0f, kBelow = 11.0f;  // log2: weights are at most 2^kLoose; a moved reference lies kBelow under the maximum
+constexpr int kDown = 31;     // of keys' factors (log2)
 constexpr int kLeast = -90;   // of d (see there): rows beyond are handed on, as their small weights times 2^d are no normal numbers
 constexpr int kItemRing = 2;
 constexpr int kSlots = 8;     // of the keys' factors, by tile: the eighth next tile is converted after this one's softmax is done
@@ -239,7 +240,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < D / 4; ++c) amax = fmaxf(fmaxf(fmaxf(amax, fabsf(v[c].x)), fmaxf(fabsf(v[c].y), fabsf(v[c].z))), fabsf(v[c].w));
         const int e = amax < INFINITY ? row_exp(amax) : 0;  // (a row with an infinity or a NaN becomes NaN in any case)
-        fq = pow2(e) * scale;
+        // (a product of halves is below 2^37, a key's factor has 2^-kDown of it: up to fq, which has it back, nothing leaves fp32 that the score
+        // does not.  Rows of a factor past 2^30, and keys of 2^-113, cannot be held so.)
+        fq = pow2(min(e, 30) + kDown) * scale;
+        if (e > 30) s_far[row] = 1;
         const float s = pow2(-e);
         uint8_t *line = smem + C::OFF_Q + row * 128;
 #pragma unroll
@@ -598,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!real) f = 0.0f;
         if (is_k) {
-          if (half == 0) s_kf[slot * kBT + key] = real ? fmaxf(f, 0x1p-149f) : 1.0f;  // (not zero: masked scores are -inf before it comes in)
+          if (half == 0) s_kf[slot * kBT + key] = real ? fmaxf(f * pow2(-kDown), 0x1p-149f) : 1.0f;  // (not zero: masked scores are -inf before)
           if (!KV8) {
             const uint32_t odd = __ballot_sync(0xffffffffu, nonfinite && real);
             if (lane == 0) s_kx[slot * 4 + warp - 4] = odd;

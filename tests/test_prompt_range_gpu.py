@@ -93,6 +93,61 @@ def test_values_behind_a_row_change_none_of_its_bits(dtype, cache, D, at, e):
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [16, 160, 528])
+@pytest.mark.parametrize("e", [30, 100])
+def test_keys_behind_a_row_change_none_of_its_bits(dtype, cache, D, at, e):
+    k, ctx = SPLIT
+    c = Case(at + D, k=k, ctx=ctx, Hq=4, Hkv=2, D=D, dtype=dtype, cache=cache)
+    c.run()
+    before = c.t["out"].clone()
+    scale_tokens(c, "k", at, 1 << 20, e)
+    c.run()
+    for r in range(len(k)):
+        n = min(max(at - ctx[r], 0), k[r] + 1)  # rows that do not see them
+        row = c.row_of(r)
+        assert torch.equal(c.t["out"][row:row + n], before[row:row + n]), r
+    assert torch.isfinite(c.t["out"]).all()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("runs", [None, runs_of((0, 20, 3))])
+@pytest.mark.parametrize("e", [-110, -80, -45, -30, 30, 45, 80, 100, 112])
+def test_scores_do_not_depend_on_where_their_magnitude_lies(dtype, cache, runs, e):
+    """Keys times 2^e and queries times 2^-e: the same scores.  Powers of two are exact in every step, so that the outputs are equal to the bit,
+    but for fp32 queries past 2^45, which are computed apart (check()'s bound)."""
+    c = Case(24, k=[140, 9, 30], ctx=[320, 350, 2000], Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache, runs=runs)
+    c.run()
+    before = c.t["out"].clone()
+    c.t["q"] = (c.t["q"].double() * 2.0 ** -e).to(dtype)
+    if cache:
+        c.t["k_scale"] = (c.t["k_scale"].double() * 2.0 ** e).float()
+    else:
+        c.t["k_cache"] = (c.t["k_cache"].double() * 2.0 ** e).to(dtype)
+    c.val["k"] = c.val["k"] * 2.0 ** e
+    c.run()
+    if dtype == BF or e > -42:
+        assert torch.equal(c.t["out"], before)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("q,k", [(0, 113), (0, 118), (-100, 110), (60, 60), (118, 0)])
+def test_equal_scores_of_any_size(dtype, cache, q, k):
+    """Queries of 2^q, keys of 2^k: every row is the mean of the V that it sees."""
+    c = Case(25, k=[140, 9, 30], ctx=[320, 350, 2000], Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache)
+    c.t["q"].fill_(2.0 ** q)
+    if cache:
+        c.t["k_cache"] = torch.ones_like(c.val["k"]).to(torch.float8_e4m3fn)
+        c.t["k_scale"].fill_(2.0 ** k)
+    else:
+        c.t["k_cache"].fill_(2.0 ** k)
+    c.val["k"] = torch.full_like(c.val["k"], 2.0 ** k)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("runs", [None, runs_of((0, 20, 3))])
 @pytest.mark.parametrize("e", [-80, -40, 30, 44, 60, 80])
 def test_outputs_scale_with_values(dtype, cache, runs, e):
