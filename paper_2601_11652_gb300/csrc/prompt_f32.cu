@@ -37,6 +37,7 @@ constexpr uint32_t kTmemCols = 512;  // S at 0 and 64, P at 128 and 192 (h, then
 constexpr uint32_t kWaitCycles = 3000000000u;  // about one and a half seconds: a wait that long is a failure
 constexpr float kLoose = 14.0f, kBelow = 11.0f;  // log2: weights are at most 2^kLoose; a moved reference lies kBelow under the maximum
 constexpr int kDown = 31;     // of keys' factors (log2)
+constexpr int kMost = 76;     // of V's exponents: rows beyond are handed on (weights of 2^14, halves of 2^15: O could leave fp32 from 2^20 keys on)
 constexpr int kLeast = -90;   // of d (see there): rows beyond are handed on, as their small weights times 2^d are no normal numbers
 constexpr int kItemRing = 2;
 constexpr int kSlots = 8;     // of the keys' factors, by tile: the eighth next tile is converted after this one's softmax is done
@@ -416,6 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + b));
         if (!collected && !collect(n - 1)) { ok = false; break; }
         ev = s_ve[slot] - d;
+        if (ev > kMost && base < end) s_far[row] = 1;
       }
       if (!ok || !collect(n - 1)) { ok = false; break; }
       const bool far = is_far(m) || s_far[row];

@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 namespace wisp {
 
@@ -70,6 +71,17 @@ __device__ __forceinline__ int unit_end(const Segment &s, int u, int unit_rows, 
 __device__ __forceinline__ int cut_off(const Segment &s, int u) { return s.span ? (int)((s.base + (int64_t)u * s.span) % s.chunk) : 0; }
 // Chunks of a unit with keys [s.t0, end), and the c-th of them.
 __device__ __forceinline__ int unit_chunks(const Segment &s, int u, int end) { return (end - s.t0 + cut_off(s, u) + s.chunk - 1) / s.chunk; }
+
+// Outputs that this thread has written
+template <int CPL, typename T>
+__device__ __forceinline__ bool not_finite(const T *out) {
+  constexpr uint32_t kInf = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
+  const std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t> *bits = reinterpret_cast<const std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t> *>(out);
+  bool any = false;
+#pragma unroll
+  for (int q = 0; q < CPL; ++q) any = any || (bits[q] & kInf) == kInf;
+  return any;
+}
 
 }  // namespace
 
@@ -396,61 +408,60 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 // look for its own.  Up to kFew chunks, as almost always, every lane computes their weights itself.  Bound by instructions, then by the
 // partials' bytes (mostly in L2): 1300 rows of 32 heads of 128, three to five chunks each, 24 us.
 template <int D, typename T>
-__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __grid_constant__ PromptPlan p, const __grid_constant__ AttnParams a) {
+__global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kernel(const __grid_constant__ PromptPlan p, const __grid_constant__ AttnParams a) {
   const int lane = threadIdx.x & 31;
-  // rows without partials that the attention has handed on, by the CTAs that are there at first (others would only look for their number)
-  const int cta = blockIdx.y * gridDim.x + blockIdx.x, takers = min((int)(gridDim.x * gridDim.y), kMergePerSM * p.sms);
-  int n_on = 0;
-  auto count = [&]() { n_on = cta < takers ? __ldcg(&p.header->h.handed_on) : 0; };
-  auto handed_on = [&]() {
-    for (int i = cta * (kMergeThreads / 32) + (threadIdx.x >> 5); i < n_on; i += takers * (kMergeThreads / 32)) {
-      const int2 x = __ldcg(a.handed_on + i);
-      prompt_row<D, T>(p, a, -1, x.x, x.y);
-    }
-  };
-  // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
-  if (!p.header->partials) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    count();
-    if (n_on) handed_on();
-    return;
-  }
-  const int g = p.Hq / p.Hkv, R = p.unit_rows;
+  const int g = p.Hq / p.Hkv, R = p.unit_rows, subs = g / p.merge_heads;
   constexpr int CPL = D / 32;
-  for (int r = blockIdx.x; r < p.B; r += gridDim.x) {
+  const int x0 = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5), x_step = gridDim.y * (kMergeThreads / 32);
+  // Rows that are computed once more (prompt.cuh), all of them behind the others: those among this warp's own, and the list's, by as many CTAs as
+  // there are SMs (where every warp of all CTAs looked for their number, a prompt of 64 tokens took 1.3 us more, in a row for that line).
+  const int cta = blockIdx.y * gridDim.x + blockIdx.x, takers = min((int)(gridDim.x * gridDim.y), p.sms);
+  int n_on = 0;
+  uint32_t marks = 0;  // its sign: that of all l
+  float zero = 0.0f;   // NaN: some sum is not finite
+
+  // Work x of request r: a query position and some heads.  Per segment (0: the run's, 1: the request's own): a row's first O and m, the distance of
+  // chunks and how many.
+  struct Where {
+    const float *po[2], *pm[2];
+    int step[2], n[2], nl[2];
+  };
+  auto where = [&](const Segment &own, const Segment &pre, int run, int j, int hk, int hh) {
+    Where w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Segment &s = i == 0 ? pre : own;
+      const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
+      const int rows = min(R, s.npos * g - u * R);
+      w.step[i] = slot_floats(rows, D);
+      w.nl[i] = rows;
+      w.n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
+      const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
+      w.po[i] = base + rr * D + lane * CPL;
+      w.pm[i] = base + rows * D + rr;
+    }
+    return w;
+  };
+
+  // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
+  const bool partials = p.header->partials;
+  if (!partials) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (cta >= takers || !__syncthreads_or(threadIdx.x == 0 ? __ldcg(&p.header->h.handed_on) : 0)) return;
+    n_on = __ldcg(&p.header->h.handed_on);
+  }
+  for (int r = blockIdx.x; r < p.B && partials; r += gridDim.x) {
     const Segment own = p.segs[r];
     const int run = p.req_run[r];
     const Segment pre = p.segs[run >= 0 ? p.B + run : r];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (r == blockIdx.x) count();
+    if (r == blockIdx.x && cta < takers) n_on = __ldcg(&p.header->h.handed_on);
     if (own.npos <= 0 || own.pbase < 0) continue;  // (refused, or its items have written the outputs)
-    const int subs = g / p.merge_heads, work = own.npos * p.Hkv * subs;
-    for (int x = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); x < work; x += gridDim.y * (kMergeThreads / 32)) {
+    const int work = own.npos * p.Hkv * subs;
+    for (int x = x0; x < work; x += x_step) {
       const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
-      // per segment (0: the run's, 1: the request's own): a row's first O and m, the distance of chunks and how many
-      struct Where {
-        const float *po[2], *pm[2];
-        int step[2], n[2], nl[2];
-      };
-      auto where = [&](int hh) {
-        Where w;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const Segment &s = i == 0 ? pre : own;
-          const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
-          const int rows = min(R, s.npos * g - u * R);
-          w.step[i] = slot_floats(rows, D);
-          w.nl[i] = rows;
-          w.n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
-          const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
-          w.po[i] = base + rr * D + lane * CPL;
-          w.pm[i] = base + rows * D + rr;
-        }
-        return w;
-      };
-      Where w = where(h0);
+      const Where w = where(own, pre, run, j, hk, h0);
       T *dst = static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + hk * g + h0) * D + lane * CPL;
-      bool again = false;  // a row has been handed on
       // a chunk none of whose keys a row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
       if (w.n[0] + w.n[1] <= kFew) {
         const int total = w.n[0] + w.n[1];
@@ -476,7 +487,8 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __gri
 #pragma unroll
           for (int x = 0; x < kHeads; ++x) {
             if (hh + x >= p.merge_heads) break;
-            again = again || is_marked(lc[x][0]) || is_marked(lc[x][1]) || is_marked(lc[x][2]) || is_marked(lc[x][3]);
+#pragma unroll
+            for (int c = 0; c < kFew; ++c) marks |= __float_as_uint(lc[x][c]);
             float m = -INFINITY, den = 0.0f, acc[CPL];
 #pragma unroll
             for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
@@ -493,6 +505,8 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __gri
                 for (int q = 0; q < CPL; ++q) acc[q] = fmaf(v[x][c][q], f, acc[q]);
               }
             }
+#pragma unroll
+            for (int q = 0; q < CPL; ++q) zero = fmaf(acc[q], 0.0f, zero);
             st_cols<CPL>(dst + (hh + x) * D, acc, 1.0f / den);
           }
         }
@@ -512,7 +526,7 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __gri
               const float *q = at(w.pm, c) + hh;
               mc = __ldcg(q);
               lc = __ldcg(q + (c < w.n[0] ? w.nl[0] : w.nl[1]));
-              again = again || is_marked(lc);
+              marks |= __float_as_uint(lc);
             }
             const float mn = fmaxf(m, ptx::warp_max(mc));
             if (mn != m) {
@@ -537,23 +551,57 @@ __global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(const __gri
           }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+#pragma unroll
+          for (int q = 0; q < CPL; ++q) zero = fmaf(acc[q], 0.0f, zero);
           st_cols<CPL>(dst, acc, 1.0f / den);
-        }
-      }
-      if (__any_sync(0xffffffffu, again)) {
-        const int total = w.n[0] + w.n[1];
-        for (int hh = 0; hh < p.merge_heads; ++hh) {
-          bool mine = false;
-          for (int c = lane; c < total; c += 32) {
-            const bool z = c < w.n[0];
-            mine = mine || is_marked(__ldcg((z ? w.pm[0] + c * w.step[0] + w.nl[0] : w.pm[1] + (c - w.n[0]) * w.step[1] + w.nl[1]) + hh));
-          }
-          if (__any_sync(0xffffffffu, mine)) prompt_row<D, T>(p, a, r, own.q0 + j, hk * g + h0 + hh);
         }
       }
     }
   }
-  if (n_on) handed_on();
+
+  const bool again = __any_sync(0xffffffffu, (marks >> 31) || !(zero == 0.0f));
+  int r = blockIdx.x, x = x0, hh = 0, i = cta * (kMergeThreads / 32) + (threadIdx.x >> 5);
+  while (true) {
+    int row, head;
+    bool whole;
+    if (again && r < p.B) {
+      const Segment own = p.segs[r];
+      if (own.npos <= 0 || own.pbase < 0 || x >= own.npos * p.Hkv * subs) {
+        r += gridDim.x;
+        x = x0;
+        continue;
+      }
+      const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
+      const int run = p.req_run[r];
+      const Where w = where(own, p.segs[run >= 0 ? p.B + run : r], run, j, hk, h0);
+      const int total = w.n[0] + w.n[1];
+      row = own.q0 + j;
+      head = hk * g + h0 + hh;
+      bool mine = false, scores = false;  // (of scores that are no numbers a row is not finite rightly)
+      for (int c = lane; c < total; c += 32) {
+        const float l = __ldcg((c < w.n[0] ? w.pm[0] + c * w.step[0] + w.nl[0] : w.pm[1] + (c - w.n[0]) * w.step[1] + w.nl[1]) + hh);
+        mine = mine || is_marked(l);
+        scores = scores || !(fabsf(l) < INFINITY);
+      }
+      whole = __any_sync(0xffffffffu, mine);
+      const bool odd = not_finite<CPL>(static_cast<T *>(p.out) + ((int64_t)row * p.Hq + head) * D + lane * CPL);
+      const bool skip = (total == 1 && !own.shared) || !(whole || (__any_sync(0xffffffffu, odd) && !__any_sync(0xffffffffu, scores)));
+      if (++hh == p.merge_heads) {
+        hh = 0;
+        x += x_step;
+      }
+      if (skip) continue;
+    } else if (i < n_on) {
+      const int2 e = __ldcg(a.handed_on + i);
+      i += takers * (kMergeThreads / 32);
+      row = e.x;
+      head = e.y & ~kOnlyNotFinite;
+      whole = !(e.y & kOnlyNotFinite);
+    } else {
+      break;
+    }
+    prompt_row<D, T>(p, a, row, head, !whole);
+  }
 }
 
 namespace {

@@ -47,22 +47,20 @@ __device__ __forceinline__ void row_codes(const uint8_t *src, float sc, float (&
   }
 }
 
-// Output row `row` (of all query rows), query head `head`, of request r (-1: found by its row).  Keys in turn, eight at a time; the output is kept
+// Output row `row` (of all query rows), query head `head`.  Keys in turn, eight at a time; the output is kept
 // normalised, o' = o (l a / l') + sum_i v_i (w_i / l'), so that it never leaves the range of the values.  Reads K and V once per row from L2,
 // about 35 instructions a key: a whole prompt of 16384 tokens this way would take some tenths of a second, a thousand times the tensor cores' time.
+// only_not_finite: only the elements whose output is not finite (others keep what they have).
 template <int D, typename T>
-__device__ __noinline__ void prompt_row(const PromptPlan &p, const AttnParams &a, int r, int row, int head) {
+__device__ __forceinline__ void prompt_row(const PromptPlan &p, const AttnParams &a, int row, int head, bool only_not_finite) {
   constexpr bool kBf = sizeof(T) == 2;
   constexpr int CPL = D / 32, kKeys = 8;
   const int lane = threadIdx.x & 31, hk = head / (p.Hq / p.Hkv);
-  if (r < 0) {  // the last request whose first row is not behind it
-    int lo = 0, hi = p.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (p.q_row_start[mid] <= row) lo = mid;
-      else hi = mid - 1;
-    }
-    r = lo;
+  int r = 0;  // its request: the last one whose first row is not behind it
+  for (int hi = p.B - 1; r < hi;) {
+    const int mid = (r + hi + 1) >> 1;
+    if (p.q_row_start[mid] <= row) r = mid;
+    else hi = mid - 1;
   }
   const Segment &own = p.segs[r];
   const int run = p.req_run[r], shared = own.t0 / 16;  // pages that the run's first request names
@@ -133,7 +131,15 @@ __device__ __noinline__ void prompt_row(const PromptPlan &p, const AttnParams &a
       for (int c = 0; c < CPL; ++c) o[c] = fmaf(s[i] * inv, v[c], o[c]);
     }
   }
-  st_cols<CPL>(static_cast<T *>(p.out) + at, o, l == 0.0f ? __uint_as_float(0x7fffffffu) : 1.0f);
+  T *out = static_cast<T *>(p.out) + at;
+  if (only_not_finite) {  // (l is finite, and so are the elements that stay)
+    float had[CPL];
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) had[c] = sizeof(T) == 2 ? __uint_as_float((uint32_t)out[c] << 16) : (float)out[c];
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) o[c] = fabsf(had[c]) < INFINITY ? had[c] : o[c];
+  }
+  st_cols<CPL>(out, o, l == 0.0f ? __uint_as_float(0x7fffffffu) : 1.0f);
 }
 
 }  // namespace wisp

@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           dst[x] = (part ? reinterpret_cast<uint8_t *>(part0 + 8 * x * D) : reinterpret_cast<uint8_t *>(out0 + row_at[x])) + (lane & 3) * 16;
+        float2 zero = make_float2(0.0f, 0.0f);  // NaN where a sum is not finite
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t o[32];
@@ -432,6 +433,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               o[i] = __float_as_uint(a1 == 0.0f ? u : fmaf(__uint_as_float(o1[i]), a1, u));
             }
           }
+#pragma unroll
+          for (int i = 0; i < 32; i += 2)
+            zero = __ffma2_rn(make_float2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), make_float2(0.0f, 0.0f), zero);
           auto flush = [&](int at) {  // the staged pieces, to byte `at` of their rows
             __syncwarp();
 #pragma unroll
@@ -482,8 +486,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           float *stat = p.partials + w.poff + (int64_t)w.rows * D + tile * tile_rows + row;
           __stcg(stat, m);
           __stcg(stat + w.rows, far ? marked(l) : l);
-        } else if (far && mine) {
-          hand_on(p, w.q0 + pos, w.h * g + row % g);
+        } else if (mine && (far || (!(zero.x + zero.y == 0.0f) && fabsf(l) < INFINITY))) {
+          hand_on(p, w.q0 + pos, (w.h * g + row % g) | (far ? 0 : kOnlyNotFinite));
         }
         ptx::tc_fence_before();
         __syncwarp();

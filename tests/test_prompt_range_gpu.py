@@ -161,3 +161,43 @@ def test_outputs_scale_with_values(dtype, cache, runs, e):
         c.t["v_cache"] = (c.t["v_cache"].double() * 2.0 ** e).to(dtype)
     c.run()
     assert torch.equal(c.t["out"].double(), before.double() * 2.0 ** e)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads", [(8, 8, 64), (28, 4, 128)])
+@pytest.mark.parametrize("k,ctx,runs", [([140, 9, 30], [320, 350, 2000], None), ([3], [40000], None), ([700, 0], [0, 5000], None),
+                                        ([1, 0, 4, 2, 7], [350, 320, 900, 64, 3000], runs_of((0, 20, 3), (-1, 0, 1), (1, 7, 1)))])
+@pytest.mark.parametrize("alike", [False, True])
+def test_values_near_the_largest(dtype, cache, heads, k, ctx, runs, alike):
+    """V of up to 2^127; alike: all of them so, and the outputs their mean."""
+    c = Case(31, k=k, ctx=ctx, Hq=heads[0], Hkv=heads[1], D=heads[2], dtype=dtype, cache=cache, runs=runs)
+    v = c.val["v"]
+    if alike:
+        v = torch.where(torch.isnan(v), v, torch.ones_like(v))
+    e = 126 - math.floor(math.log2(v[~torch.isnan(v)].abs().max()))
+    if cache:
+        if alike:
+            c.t["v_cache"] = v.to(torch.float8_e4m3fn)
+            c.t["v_scale"].fill_(2.0 ** e)
+        else:
+            c.t["v_scale"] = (c.t["v_scale"].double() * 2.0 ** e).float()
+    else:
+        c.t["v_cache"] = (v * 2.0 ** e).to(dtype)
+    c.val["v"] = v * 2.0 ** e
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_a_value_near_the_largest_among_others(dtype, cache):
+    """One token's V (one page's scales) of 2^120 times the others'; rows in front of it keep their bits."""
+    c = Case(32, k=[250, 100, 30], ctx=[0, 70, 3000], Hq=4, Hkv=2, D=128, dtype=dtype, cache=cache)
+    c.run()
+    before = c.t["out"].clone()
+    scale_tokens(c, "v", 96, 112 if cache else 97, 120)
+    c.run()
+    for r in range(2):
+        n = 96 - c.ctx[r]
+        row = c.row_of(r)
+        assert torch.equal(c.t["out"][row:row + n], before[row:row + n]), r
+    c.check()
