@@ -81,7 +81,7 @@ __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D 
 // that has had one beyond kFar is computed once more.
 //
 // The kernel for fp32 queries hands on rows whose queries are past 2^44, and (rows of a tile that not all see) rows whose largest V is 2^90 times
-// that of the tile's first key.
+// that of the first one that it sees in the tile.
 //
 // Sums of weights times values are not normalised before the end: with bf16 queries, whose V no kernel looks at, a row whose sums are not finite
 // (weights are up to 2^8) is handed on for the elements where they are not, with fp32 queries one that sees V past 2^91; and a row whose joined partials

@@ -60,7 +60,7 @@ struct Cfg {
   static constexpr int OFF_KF = OFF_MISC + 64;             // float [kSlots][64]: factors of the keys' scores
   static constexpr int OFF_VF = OFF_KF + kSlots * kBT * 4; // float [kSlots][64]: factors of the keys' weights
   static constexpr int OFF_VE = OFF_VF + kSlots * kBT * 4; // int [kSlots]: exponent that the tile's factors are relative to
-  static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V (or the first key's), by tile
+  static constexpr int OFF_VM = OFF_VE + kSlots * 4;       // float [2][4]: largest factors of the warps that convert V (or the first one's that is not zero), by tile
   static constexpr int OFF_KX = OFF_VM + 32;      // uint32 [kSlots][4]: keys with values that are not finite, 16 a warp (two bits each)
   static constexpr int OFF_ODD = OFF_KX + kSlots * 16;     // int [2][3][D] first positions that see NaN, +inf, -inf
   static constexpr int OFF_FAR = OFF_ODD + 2 * 3 * D * 4;  // uint8 [128]: the row has had a reference far from zero
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               ptx::tmem_st16(t_s + c, y);
             }
             ptx::tmem_wait_st();
-            // Here V's factors are relative to the first key's (elsewhere to the largest), and a row's weights are computed with 2^d, d the distance to
+            // Here V's factors are relative to the first that is not zero (elsewhere to the largest), and a row's weights are computed with 2^d, d the distance to
             // the largest factor that it sees (d goes back into their sum and into P V): what it does not see has no say in its bits.
             if (!wait_bar(bar(B::V_FULL + n % C::NS), (n / C::NS) & 1, s_abort)) { ok = false; break; }
             float most = 0.0f;
@@ -610,15 +610,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) s_kx[slot * 4 + warp - 4] = odd;
           }
         } else {
-          // what the tile's factors are relative to: the power of two of the largest, or where some row does not see all keys, of the first key's
-          const float wm = part ? f : ptx::warp_max(f);
+          // what the tile's factors are relative to: the power of two of the largest, or where some row does not see all keys, of
+          // the first key whose V is not zero (rows that do not see it have nothing from this tile)
+          const uint32_t some = __ballot_sync(0xffffffffu, f > 0.0f);
+          const float wm = part ? __shfl_sync(0xffffffffu, f, some ? __ffs(some) - 1 : 0) : ptx::warp_max(f);
           if (lane == 0) s_vm[(n & 1) * 4 + warp - 8] = wm;
         }
         if (!together()) { ok = false; break; }  // the tile is in registers
         if (!is_k && half == 0) {
-          // (a factor that is 2^120 of the first key's or more counts for rows that do not see it)
+          // (a factor that is 2^120 of it or more counts for rows that do not see it)
           const float4 m4 = *reinterpret_cast<const float4 *>(s_vm + (n & 1) * 4);
-          const int e = exp_of(part ? m4.x : fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w))), e2 = e / 2;
+          const float first = m4.x > 0.0f ? m4.x : m4.y > 0.0f ? m4.y : m4.z > 0.0f ? m4.z : m4.w;
+          const int e = exp_of(part ? first : fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w))), e2 = e / 2;
           s_vf[slot * kBT + key] = fminf(f * pow2(-e2) * pow2(e2 - e), 0x1p120f);
           if (id == 0) s_ve[slot] = e;
         }

@@ -201,3 +201,30 @@ def test_a_value_near_the_largest_among_others(dtype, cache):
         row = c.row_of(r)
         assert torch.equal(c.t["out"][row:row + n], before[row:row + n]), r
     c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("e", [0, -60, -100, -118, 80])
+@pytest.mark.parametrize("zeros", [1, 5, 70])
+def test_zero_values_in_front(dtype, cache, e, zeros):
+    """The first tokens' V is zero and the others' 2^e: rows that see zeros only are zero, others as everywhere (e4m3: whole pages, by their
+    scales).  Outputs below fp32's normal numbers have steps of 2^-149: with weights of up to 2^14 in front of them, 2^-135."""
+    c = Case(33, k=[150, 40, 3], ctx=[0, 20, 2000], Hq=4, Hkv=2, D=64, dtype=dtype, cache=cache)
+    scale_tokens(c, "v", 0, 1 << 20, e)
+    for r in range(3):
+        n = (zeros + 15) // 16 * 16 if cache else zeros
+        for t in range(min(n, c.ctx[r] + c.k[r] + 1)):
+            page, slot = int(c.bt[r, t // PAGE]), t % PAGE
+            if cache:
+                c.t["v_scale"][page] = 0
+            else:
+                c.t["v_cache"][page, :, slot] = 0
+            c.val["v"][page, :, slot] = 0
+    c.run()
+    bf = dtype == BF
+    for r in range(3):
+        at = c.row_of(r)
+        ref, mag, _ = c.reference(r, 0, c.k[r] + 1)
+        got = c.t["out"][at:at + c.k[r] + 1].double()
+        bound = (2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -10) * mag if bf else 2.0 ** -9 * mag) + 2.0 ** -133
+        assert bool(((got - ref).abs() <= bound).all()), r
