@@ -33,6 +33,9 @@ struct Segment {  // 64 bytes
 };
 static_assert(sizeof(Segment) == 64, "segment layout");
 
+// Of the planner's chunks: whole key tiles, and not shorter than this, of units of more than one tile of rows (whose partials cost more) than that.
+constexpr int kChunkTile = 128, kLeastChunk = 256, kLeastFullChunk = 1024;
+
 struct PromptHeader {
   PlanHeader h;        // what the attention kernels read
   int32_t partials;    // 1: the merge has work

@@ -65,17 +65,25 @@ struct Space {
 
 // Rows of a unit, and bounds on list entries and partials.  Without cuts a request has ceil(rows / unit_rows) units, a run as many for its
 // rows again, and both leave one partial per row and head.  Cuts add entries and partials of whole units: by the planner's rule a few
-// items per SM; where they would not fit (a causal prompt's last units are twice as long as the average), it makes none.
+// items per SM, and no unit has more chunks than its keys (at most a table's) are cut into with the shortest ones; where they would not fit (a causal
+// prompt's last units are twice as long as the average), it makes none.
 Space space(const wisp_attn_args *a, bool shared, int sms) {
   Space s;
   const int g = a->Hq / a->Hkv;
   const int64_t T = a->B > 0 ? a->total_q_rows : 0;
   s.unit_rows = (a->qkv_dtype == WISP_BF16 ? 2 : 1) * g * prompt_tile_positions(g);
   const int64_t units = (T * g / s.unit_rows + a->B) * (shared ? 2 : 1);
-  const int64_t slot = std::min<int64_t>(s.unit_rows, T * g) * (a->D + 2) + 4;
+  const int64_t tokens = (int64_t)a->max_blocks_per_seq * a->block_size;
+  // chunks of a unit, at most: its first one may end anywhere
+  auto chunks = [&](int shortest) -> int64_t { return tokens <= kChunkTile ? 1 : 2 + (tokens - kChunkTile - 1) / shortest; };
+  auto slot = [&](int rows) { return std::min<int64_t>(rows, T * g) * (a->D + 2) + 4; };
+  auto partials = [&](int shortest, int rows) { return chunks(shortest) > 1 ? chunks(shortest) * slot(rows) : 0; };
   const int64_t cuts = (std::min<int64_t>(2 * units * a->Hkv, (int64_t)12 * sms) + 4 * sms) / a->Hkv + 8;
-  s.max_rows = units + cuts;
-  s.partial_cap = cuts * a->Hkv * slot + (shared ? 2 * T * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
+  // (units of two tiles, with bf16 queries: a segment of one tile of rows is one unit, and there are as many segments as requests and runs)
+  const int64_t small = partials(kLeastChunk, std::min(s.unit_rows, kChunkTile)), full = partials(kLeastFullChunk, s.unit_rows);
+  const int64_t possible = s.unit_rows <= kChunkTile ? units * small : std::min(units * std::max(small, full), units * full + a->B * (shared ? 2 : 1) * small);
+  s.max_rows = units + std::min(cuts, units * (chunks(kLeastChunk) - 1));
+  s.partial_cap = std::min(cuts * slot(s.unit_rows), possible) * a->Hkv + (shared ? 2 * T * a->Hq * (a->D + 2) + 4 * units * a->Hkv : 0);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;

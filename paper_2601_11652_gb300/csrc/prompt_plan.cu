@@ -17,9 +17,7 @@ namespace {
 constexpr int kMaxThreads = 1024;  // of the planner: see prompt_plan_launch
 constexpr int kPage = 16;
 constexpr int kBuckets = 1024;     // of the dispatch order, by key tiles of 64
-constexpr int kMinKeys = 256;      // chunks are not shorter, nor
-constexpr int kMinFull = 1024;     // of units of more than one tile (their partials cost more)
-constexpr int kTile = 128;         // and are whole key tiles
+constexpr int kMinKeys = kLeastChunk, kMinFull = kLeastFullChunk, kTile = kChunkTile;
 constexpr int kAllKeys = 1 << 30;  // the context of a run's segment: every row sees all its keys (a table has fewer)
 constexpr int kMaxChunk = 1 << 28; // a segment's keys and two chunks stay below 2^31
 constexpr int kMaxRows = 1 << 24;  // k_r limit

@@ -228,3 +228,26 @@ def test_zero_values_in_front(dtype, cache, e, zeros):
         got = c.t["out"][at:at + c.k[r] + 1].double()
         bound = (2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -10) * mag if bf else 2.0 ** -9 * mag) + 2.0 ** -133
         assert bool(((got - ref).abs() <= bound).all()), r
+
+
+def test_workspace_follows_what_can_be_cut():
+    """Partials are reserved for sequences that are long enough to be cut (sizes in bytes, D + 2 floats a row)."""
+    from paper_2601_11652_gb300 import binding as wb
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    for rows, pages, most in ((64, 4, 1 << 20), (128, 8, 1 << 20), (2000, 125, 120 << 20), (64, 16, 3 * 2 * 8 * 256 * 130 * 4 + (1 << 20))):
+        q = torch.empty((rows, 32, 128), dtype=BF, device="cuda")
+        kv = torch.empty((pages, 8, 16, 128), dtype=BF, device="cuda")
+        a = wb.make_prompt_args(draft_lens=i(1), context_lens=i(1), block_tables=i(1, pages), q=q, k_cache=kv, v_cache=kv, out=q)
+        assert wb.wisp_prompt_workspace_size(a) < most, (rows, pages)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,ctx", [(1, 127), (1, 128), (1, 129), (1, 255), (1, 256), (1, 257), (1, 1024), (3, 2047), (200, 0), (300, 800), (70, 1300), (500, 560)])
+@pytest.mark.parametrize("copies", [1, 3, 40])
+def test_tables_as_wide_as_their_sequences(dtype, n, ctx, copies):
+    """The workspace is sized by the table's width: no longer sequence fits behind it."""
+    runs = runs_of((0, ctx // 16, copies)) if ctx >= 16 else None
+    for r in (None, runs):
+        c = Case(n + ctx, k=[n - 1] * copies, ctx=[ctx] * copies, Hq=8, Hkv=2, D=64, dtype=dtype, runs=r, spare=0)
+        c.run()
+        c.check()
