@@ -27,7 +27,8 @@ extern "C" {
  * The cache has the queries' type, or holds e4m3 codes with a scale per page and KV head (wisp_kv8.h).
  * Supported: D in {64, 128}, block_size == 16, Hq / Hkv <= 128, k_r < 2^24, and total_q_rows * Hq * (D + 2) < 2^29 with shared pages (partial
  * results have 32-bit offsets: larger calls may return WISP_ERR_UNSUPPORTED).
- * Scores, softmax statistics and outputs accumulate in fp32.  With bf16 queries a weight enters the second product in bf16
+ * Scores, softmax statistics and outputs accumulate in fp32, and finite inputs whose scores fp32 holds give finite outputs (a weight below 2^-110 of
+ * the sum of its row's counts as zero).  With bf16 queries a weight enters the second product in bf16
  * (relative error 2^-9), and so do code * scale of an e4m3 cache, K and V (exactly where the scale is a power of two of magnitude 2^-100
  * to 2^100; values past the bf16 range count as its largest).  With fp32 queries every factor enters its product with
  * 22 significant bits or more: queries, and K and V of an fp32 cache, down to steps of 2^-38 of the largest value of their row; a weight times its

@@ -83,20 +83,15 @@ __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D 
 // where it is far from zero the largest weight is not 2^0 but up to 2^(half a step of m): references are whole numbers, exact up to 2^24, and a row
 // that has had one beyond kFar is computed once more.
 //
-// The kernel for fp32 queries hands on rows whose queries are past 2^44, and (rows of a tile that not all see) rows whose largest V is 2^90 times
+// The kernel for fp32 queries hands on rows whose queries are past 2^44, and (rows of a tile that not all see) rows whose largest V is 2^78 times
 // that of the first one that it sees in the tile.
 //
-// Sums of weights times values are not normalised before the end: with bf16 queries, whose V no kernel looks at, a row whose sums are not finite
-// (weights are up to 2^8) is handed on for the elements where they are not, with fp32 queries one that sees V past 2^91; and a row whose joined partials
-// are not finite.
-//
-// A row of an item that writes outputs goes into a list; of one that leaves partials the sign of l says it (l is never negative).
-constexpr float kFar = 0x1p20f;
+// They go into a list, once for every item that they are handed on from; the merge does not write those whose partials say so by the sign of their l
+// (which is never negative).
+constexpr float kFar = 0x1p23f;
 __device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabsf(m) < INFINITY; }
 __device__ __forceinline__ float marked(float l) { return __uint_as_float(__float_as_uint(l) | 0x80000000u); }
 __device__ __forceinline__ bool is_marked(float l) { return __float_as_uint(l) >> 31; }
-// (the elements of a row whose sums are not finite: those that are keep their bits)
-constexpr int kOnlyNotFinite = 1 << 30;
 __device__ __forceinline__ void hand_on(const AttnParams &p, int row, int head) {
   p.handed_on[atomicAdd(&p.header_mut->handed_on, 1)] = make_int2(row, head);
 }

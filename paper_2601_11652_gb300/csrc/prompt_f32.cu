@@ -9,7 +9,7 @@
 //                  bits off rather than rounding, a bias of up to 2^-24 per step: over a tile's 12 steps it stays at fp32's own error, over a
 //                  long sequence it would not.)
 // e4m3 codes are halves already: h alone, and two products instead of three.
-// P is at most 2^14 (m moves where a tile's maximum is above that, and lies 2^11 below the maximum then), so that a weight's absolute steps, 2^-25 of
+// P is at most 2^14 (m moves where a tile's maximum is above that, which is 2^11 to 2^12 then), so that a weight's absolute steps, 2^-25 of
 // these units, are 2^-36 of the row's largest.
 //
 // An item is one tile of 128 rows.  Persistent CTAs, 16 warps: 0-3 softmax and epilogue; 4-7 and 8-11 turn a K and a V tile into halves, in
@@ -35,10 +35,12 @@ constexpr int kM = 128;       // rows
 constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;  // S at 0 and 64, P at 128 and 192 (h, then l), O at 256 and 384
 constexpr uint32_t kWaitCycles = 3000000000u;  // about one and a half seconds: a wait that long is a failure
-constexpr float kLoose = 14.0f, kBelow = 11.0f;  // log2: weights are at most 2^kLoose; a moved reference lies kBelow under the maximum
+// Sums of weights stay below 1, so that O never leaves the values' range: a tile adds 1/2 at most, as its largest score lies kRoom or more below the
+// reference (log2), and with 1/2 in it the reference moves up by kRoom.  A new one lies kAbove above the largest score.
+constexpr float kRoom = 7.0f, kAbove = 10.0f;
+constexpr int kUp = 21;       // P is weights times 2^kUp: at most 2^14
 constexpr int kDown = 31;     // of keys' factors (log2)
-constexpr int kMost = 76;     // of V's exponents: rows beyond are handed on (weights of 2^14, halves of 2^15: O could leave fp32 from 2^20 keys on)
-constexpr int kLeast = -90;   // of d (see there): rows beyond are handed on, as their small weights times 2^d are no normal numbers
+constexpr int kLeast = -78;   // of d (see there): rows beyond are handed on, as their small weights times 2^d are no normal numbers
 constexpr int kItemRing = 2;
 constexpr int kSlots = 8;     // of the keys' factors, by tile: the eighth next tile is converted after this one's softmax is done
 
@@ -274,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int b = k & 1;
         if (!wait_bar(bar(B::O_FULL + b), (k >> 1) & 1, s_abort)) return false;
         ptx::tc_fence_after();
-        const float f = pow2(ev);
+        const float f = ev >= -126 ? pow2(ev) : __int_as_float(1 << (ev + 149));  // (no normal number)
         const float2 f2 = make_float2(f, f);
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float most = 0.0f;
 #pragma unroll 4
             for (int i = 0; i < kBT; ++i) most = fmaxf(most, i < seen ? vf[i] : 0.0f);
-            d = -exp_of(most);
+            d = most > 0.0f ? kUp - exp_of(most) : 0;
             if (d < kLeast) s_far[row] = 1;
           }
         }
@@ -371,17 +373,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float top = fmaxf(mx[0], mx[1]) * fq;
         bool collected = t == 0;
         if (t == 0) {
-          m = floorf(top) - kBelow;
+          m = floorf(top) + kAbove;
         } else {
-          const bool move = mine && top > m + kLoose;
+          const bool move = mine && (top > m - kRoom || l > 0.5f);
           if (__any_sync(0xffffffffu, move)) {
             // (the tile before still has the reference from before)
             collected = true;
             if (!collect(n - 1)) { ok = false; break; }
-            const float to = move ? floorf(top) - kBelow : m;
+            const float to = top > m - kRoom ? floorf(top) + kAbove : m + kRoom;
             const float a = move ? ptx::ex2(m - to) : 1.0f;
             if (move && is_far(m)) s_far[row] = 1;
-            m = to;
+            if (move) m = to;
             l *= a;
 #pragma unroll
             for (int i = 0; i < D / 2; ++i) o[i] = __fmul2_rn(o[i], make_float2(a, a));
@@ -417,7 +419,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) ptx::mbar_arrive(bar(B::P_FULL + b));
         if (!collected && !collect(n - 1)) { ok = false; break; }
         ev = s_ve[slot] - d;
-        if (ev > kMost && base < end) s_far[row] = 1;
       }
       if (!ok || !collect(n - 1)) { ok = false; break; }
       const bool far = is_far(m) || s_far[row];
@@ -465,9 +466,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         float *stat = p.partials + w.poff + (int64_t)w.rows * D + row;
         __stcg(stat, m);
         __stcg(stat + w.rows, far ? marked(l) : l);
-      } else if (far && mine) {
-        hand_on(p, w.q0 + pos, w.h * g + hh0);
       }
+      if (far && mine) hand_on(p, w.q0 + pos, w.h * g + hh0);
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B::ODD_FREE + (j & 1)));
     }
@@ -622,8 +622,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float4 m4 = *reinterpret_cast<const float4 *>(s_vm + (n & 1) * 4);
           const float first = m4.x > 0.0f ? m4.x : m4.y > 0.0f ? m4.y : m4.z > 0.0f ? m4.z : m4.w;
           const int e = exp_of(part ? first : fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w))), e2 = e / 2;
-          s_vf[slot * kBT + key] = fminf(f * pow2(-e2) * pow2(e2 - e), 0x1p120f);
-          if (id == 0) s_ve[slot] = e;
+          s_vf[slot * kBT + key] = fminf(f * pow2(-e2) * pow2(e2 - e + kUp), 0x1p120f);
+          if (id == 0) s_ve[slot] = e - kUp;
         }
 #pragma unroll
         for (int i = 0; i < G; ++i) {

@@ -8,7 +8,6 @@
 
 #include <algorithm>
 #include <cstring>
-#include <type_traits>
 
 namespace wisp {
 
@@ -69,17 +68,6 @@ __device__ __forceinline__ int unit_end(const Segment &s, int u, int unit_rows, 
 __device__ __forceinline__ int cut_off(const Segment &s, int u) { return s.span ? (int)((s.base + (int64_t)u * s.span) % s.chunk) : 0; }
 // Chunks of a unit with keys [s.t0, end), and the c-th of them.
 __device__ __forceinline__ int unit_chunks(const Segment &s, int u, int end) { return (end - s.t0 + cut_off(s, u) + s.chunk - 1) / s.chunk; }
-
-// Outputs that this thread has written
-template <int CPL, typename T>
-__device__ __forceinline__ bool not_finite(const T *out) {
-  constexpr uint32_t kInf = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
-  const std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t> *bits = reinterpret_cast<const std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t> *>(out);
-  bool any = false;
-#pragma unroll
-  for (int q = 0; q < CPL; ++q) any = any || (bits[q] & kInf) == kInf;
-  return any;
-}
 
 }  // namespace
 
@@ -405,49 +393,24 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_plan_kernel(const PromptPl
 // head, kHeads rows at a time (units are whole positions, so they lie in one; single rows where rows are few); grid columns are requests, so that no row has to
 // look for its own.  Up to kFew chunks, as almost always, every lane computes their weights itself.  Bound by instructions, then by the
 // partials' bytes (mostly in L2): 1300 rows of 32 heads of 128, three to five chunks each, 24 us.
-template <int D, typename T>
+template <int D, typename T, bool KV8>
 __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kernel(const __grid_constant__ PromptPlan p, const __grid_constant__ AttnParams a) {
-  const int lane = threadIdx.x & 31;
-  const int g = p.Hq / p.Hkv, R = p.unit_rows, subs = g / p.merge_heads;
-  constexpr int CPL = D / 32;
-  const int x0 = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5), x_step = gridDim.y * (kMergeThreads / 32);
-  // Rows that are computed once more (prompt.cuh), all of them behind the others: those among this warp's own, and the list's, by as many CTAs as
-  // there are SMs (where every warp of all CTAs looked for their number, a prompt of 64 tokens took 1.3 us more, in a row for that line).
-  const int cta = blockIdx.y * gridDim.x + blockIdx.x, takers = min((int)(gridDim.x * gridDim.y), p.sms);
+  // Rows that are computed once more (prompt.cuh), behind the others, by one CTA per SM (where
+  // every warp of all CTAs looked for their number, a prompt of 64 tokens took 1.3 us more, in a row for that line; every CTA that fits, 1 us).
+  const int cta = blockIdx.y * gridDim.x + blockIdx.x;
   int n_on = 0;
-  uint32_t marks = 0;  // its sign: that of all l
-  float zero = 0.0f;   // NaN: some sum is not finite
-
-  // Work x of request r: a query position and some heads.  Per segment (0: the run's, 1: the request's own): a row's first O and m, the distance of
-  // chunks and how many.
-  struct Where {
-    const float *po[2], *pm[2];
-    int step[2], n[2], nl[2];
-  };
-  auto where = [&](const Segment &own, const Segment &pre, int run, int j, int hk, int hh) {
-    Where w;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const Segment &s = i == 0 ? pre : own;
-      const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
-      const int rows = min(R, s.npos * g - u * R);
-      w.step[i] = slot_floats(rows, D);
-      w.nl[i] = rows;
-      w.n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
-      const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
-      w.po[i] = base + rr * D + lane * CPL;
-      w.pm[i] = base + rows * D + rr;
-    }
-    return w;
-  };
-
   // (the attention's CTAs let this kernel start once the planner is done: what it has written may be read before they are)
   const bool partials = p.header->partials;
   if (!partials) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (cta >= takers || !__syncthreads_or(threadIdx.x == 0 ? __ldcg(&p.header->h.handed_on) : 0)) return;
+    if (cta >= p.sms || !__syncthreads_or(threadIdx.x == 0 ? __ldcg(&p.header->h.handed_on) : 0)) return;
     n_on = __ldcg(&p.header->h.handed_on);
   }
+  const int takers = min((int)(gridDim.x * gridDim.y), p.sms), lane = threadIdx.x & 31;
+  const int g = p.Hq / p.Hkv, R = p.unit_rows, subs = g / p.merge_heads;
+  constexpr int CPL = D / 32;
+  const int x0 = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5), x_step = gridDim.y * (kMergeThreads / 32);
+
   for (int r = blockIdx.x; r < p.B && partials; r += gridDim.x) {
     const Segment own = p.segs[r];
     const int run = p.req_run[r];
@@ -458,7 +421,28 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
     const int work = own.npos * p.Hkv * subs;
     for (int x = x0; x < work; x += x_step) {
       const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
-      const Where w = where(own, pre, run, j, hk, h0);
+      // per segment (0: the run's, 1: the request's own): a row's first O and m, the distance of chunks and how many
+      struct Where {
+        const float *po[2], *pm[2];
+        int step[2], n[2], nl[2];
+      };
+      auto where = [&](int hh) {
+        Where w;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const Segment &s = i == 0 ? pre : own;
+          const int rho = (own.q0 + j - s.q0) * g + hh, u = rho / R, rr = rho - u * R;
+          const int rows = min(R, s.npos * g - u * R);
+          w.step[i] = slot_floats(rows, D);
+          w.nl[i] = rows;
+          w.n[i] = i == 0 && run < 0 ? 0 : min(s.chunks, unit_chunks(s, u, unit_end(s, u, R, g)));
+          const float *base = p.partials + (s.pbase + hk * s.part_h + u * s.chunks * slot_floats(R, D));
+          w.po[i] = base + rr * D + lane * CPL;
+          w.pm[i] = base + rows * D + rr;
+        }
+        return w;
+      };
+      Where w = where(h0);
       T *dst = static_cast<T *>(p.out) + ((int64_t)(own.q0 + j) * p.Hq + hk * g + h0) * D + lane * CPL;
       // a chunk none of whose keys a row sees adds nothing; its m is -inf and its l 0, or a NaN where its scores are no numbers
       if (w.n[0] + w.n[1] <= kFew) {
@@ -485,6 +469,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
 #pragma unroll
           for (int x = 0; x < kHeads; ++x) {
             if (hh + x >= p.merge_heads) break;
+            uint32_t marks = 0;
 #pragma unroll
             for (int c = 0; c < kFew; ++c) marks |= __float_as_uint(lc[x][c]);
             float m = -INFINITY, den = 0.0f, acc[CPL];
@@ -492,6 +477,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
             for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
 #pragma unroll
             for (int c = 0; c < kFew; ++c) m = fmaxf(m, mc[x][c]);
+            m += 2.0f;  // (kFew sums that are each within the values' range)
 #pragma unroll
             for (int c = 0; c < kFew; ++c) {
               if (mc[x][c] == -INFINITY) {
@@ -503,18 +489,18 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
                 for (int q = 0; q < CPL; ++q) acc[q] = fmaf(v[x][c][q], f, acc[q]);
               }
             }
-#pragma unroll
-            for (int q = 0; q < CPL; ++q) zero = fmaf(acc[q], 0.0f, zero);
-            st_cols<CPL>(dst + (hh + x) * D, acc, 1.0f / den);
+            if (!(marks >> 31)) st_cols<CPL>(dst + (hh + x) * D, acc, 1.0f / den);
           }
         }
       } else {
         for (int hh = 0; hh < p.merge_heads; ++hh, dst += D) {
           const int total = w.n[0] + w.n[1];
+          const float room = (float)(32 - __clz(total));  // (their sum stays within the values' range)
           auto at = [&](const float *const (&base)[2], int c) {
             return c < w.n[0] ? base[0] + c * w.step[0] : base[1] + (c - w.n[0]) * w.step[1];
           };
           float m = -INFINITY, den = 0.0f, acc[CPL];
+          bool mark = false;
 #pragma unroll
           for (int q = 0; q < CPL; ++q) acc[q] = 0.0f;
           for (int c0 = 0; c0 < total; c0 += 32) {  // 32 chunks at a time, a lane each
@@ -524,7 +510,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
               const float *q = at(w.pm, c) + hh;
               mc = __ldcg(q);
               lc = __ldcg(q + (c < w.n[0] ? w.nl[0] : w.nl[1]));
-              marks |= __float_as_uint(lc);
+              mark = mark || is_marked(lc);
             }
             const float mn = fmaxf(m, ptx::warp_max(mc));
             if (mn != m) {
@@ -534,7 +520,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
               for (int q = 0; q < CPL; ++q) acc[q] *= a;
               m = mn;
             }
-            const float f = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m);
+            const float f = mc == -INFINITY ? -1.0f : ptx::ex2(mc - m - room);
             den = mc == -INFINITY ? den + lc : fmaf(lc, f, den);
             const int nc = min(32, total - c0);
 #pragma unroll 4
@@ -549,56 +535,39 @@ __global__ void __launch_bounds__(kMergeThreads, kMergePerSM) prompt_merge_kerne
           }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-#pragma unroll
-          for (int q = 0; q < CPL; ++q) zero = fmaf(acc[q], 0.0f, zero);
-          st_cols<CPL>(dst, acc, 1.0f / den);
+          if (!__any_sync(0xffffffffu, mark)) st_cols<CPL>(dst, acc, 1.0f / den);
         }
       }
     }
   }
 
-  const bool again = __any_sync(0xffffffffu, (marks >> 31) || !(zero == 0.0f));
-  int r = blockIdx.x, x = x0, hh = 0, i = cta * (kMergeThreads / 32) + (threadIdx.x >> 5);
-  while (true) {
-    int row, head;
-    bool whole;
-    if (again && r < p.B) {
-      const Segment own = p.segs[r];
-      if (own.npos <= 0 || own.pbase < 0 || x >= own.npos * p.Hkv * subs) {
-        r += gridDim.x;
-        x = x0;
-        continue;
-      }
-      const int y = x / subs, j = y / p.Hkv, hk = y - j * p.Hkv, h0 = (x - y * subs) * p.merge_heads;
-      const int run = p.req_run[r];
-      const Where w = where(own, p.segs[run >= 0 ? p.B + run : r], run, j, hk, h0);
-      const int total = w.n[0] + w.n[1];
-      row = own.q0 + j;
-      head = hk * g + h0 + hh;
-      bool mine = false, scores = false;  // (of scores that are no numbers a row is not finite rightly)
-      for (int c = lane; c < total; c += 32) {
-        const float l = __ldcg((c < w.n[0] ? w.pm[0] + c * w.step[0] + w.nl[0] : w.pm[1] + (c - w.n[0]) * w.step[1] + w.nl[1]) + hh);
-        mine = mine || is_marked(l);
-        scores = scores || !(fabsf(l) < INFINITY);
-      }
-      whole = __any_sync(0xffffffffu, mine);
-      const bool odd = not_finite<CPL>(static_cast<T *>(p.out) + ((int64_t)row * p.Hq + head) * D + lane * CPL);
-      const bool skip = (total == 1 && !own.shared) || !(whole || (__any_sync(0xffffffffu, odd) && !__any_sync(0xffffffffu, scores)));
-      if (++hh == p.merge_heads) {
-        hh = 0;
-        x += x_step;
-      }
-      if (skip) continue;
-    } else if (i < n_on) {
-      const int2 e = __ldcg(a.handed_on + i);
-      i += takers * (kMergeThreads / 32);
-      row = e.x;
-      head = e.y & ~kOnlyNotFinite;
-      whole = !(e.y & kOnlyNotFinite);
-    } else {
-      break;
+  for (int i = kRowsAtOnce * (cta * (kMergeThreads / 32) + (threadIdx.x >> 5)); i < n_on; i += kRowsAtOnce * takers * (kMergeThreads / 32)) {
+    int row[kRowsAtOnce], head[kRowsAtOnce];
+    uint32_t todo = 0;
+#pragma unroll
+    for (int k = 0; k < kRowsAtOnce; ++k) {
+      const int2 e = i + k < n_on ? __ldcg(a.handed_on + i + k) : make_int2(0, 0);
+      row[k] = e.x;
+      head[k] = e.y;
+      todo |= i + k < n_on ? 1u << k : 0u;
     }
-    prompt_row<D, T>(p, a, row, head, !whole);
+#pragma unroll 1
+    while (todo) {  // those of the first one's request and KV head
+      int row0 = 0, hk = 0;
+#pragma unroll
+      for (int k = kRowsAtOnce - 1; k >= 0; --k)
+        if (todo >> k & 1) {
+          row0 = row[k];
+          hk = head[k] / g;
+        }
+      const int r = request_of(p, row0);
+      uint32_t use = 0;
+#pragma unroll
+      for (int k = 0; k < kRowsAtOnce; ++k)
+        if ((todo >> k & 1) && head[k] / g == hk && row[k] >= p.q_row_start[r] && row[k] < p.q_row_start[r + 1]) use |= 1u << k;
+      todo &= ~use;
+      if (p.segs[r].npos > 0) prompt_rows<D, T, KV8>(p, a, r, row, head, hk, use);  // (a run's rows are those of its refused requests, too)
+    }
   }
 }
 
@@ -649,8 +618,12 @@ cudaError_t prompt_merge_launch(const PromptPlan &p, const AttnParams &a, bool f
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (f32) return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, float> : prompt_merge_kernel<64, float>, p, a);
-  return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, uint16_t> : prompt_merge_kernel<64, uint16_t>, p, a);
+  if (a.k_scale) {
+    if (f32) return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, float, true> : prompt_merge_kernel<64, float, true>, p, a);
+    return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, uint16_t, true> : prompt_merge_kernel<64, uint16_t, true>, p, a);
+  }
+  if (f32) return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, float, false> : prompt_merge_kernel<64, float, false>, p, a);
+  return cudaLaunchKernelEx(&cfg, p.D == 128 ? prompt_merge_kernel<128, uint16_t, false> : prompt_merge_kernel<64, uint16_t, false>, p, a);
 }
 
 }  // namespace wisp

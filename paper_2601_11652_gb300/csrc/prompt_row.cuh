@@ -1,5 +1,5 @@
-// prompt_row.cuh -- one row of the attention of prompt.cuh by one warp in plain fp32, for the rare rows that the tensor-core kernels hand on:
-// values near the ends of fp32, where their scaled operands or their unnormalised sums leave what they can hold.
+// prompt_row.cuh -- one row of the attention of prompt.cuh by one warp in plain fp32, for the rare rows that the tensor-core kernels hand on
+// (prompt.cuh): scores so far from zero that their steps are powers of two of their weights, and fp32 operands too far apart.
 #pragma once
 
 #include "attn_merge.cuh"
@@ -47,99 +47,128 @@ __device__ __forceinline__ void row_codes(const uint8_t *src, float sc, float (&
   }
 }
 
-// Output row `row` (of all query rows), query head `head`.  Keys in turn, eight at a time; the output is kept
-// normalised, o' = o (l a / l') + sum_i v_i (w_i / l'), so that it never leaves the range of the values.  Reads K and V once per row from L2,
-// about 35 instructions a key: a whole prompt of 16384 tokens this way would take some tenths of a second, a thousand times the tensor cores' time.
-// only_not_finite: only the elements whose output is not finite (others keep what they have).
-template <int D, typename T>
-__device__ __forceinline__ void prompt_row(const PromptPlan &p, const AttnParams &a, int row, int head, bool only_not_finite) {
+// Output rows row[i] (of all query rows), query heads head[i], i in the mask `use`: of request r and KV head hk.  Keys in turn, eight at a time; lane
+// 8 i + k (modulo kSums) has row i's score of the k-th, its softmax is among eight lanes.  Outputs are kept normalised, o' = o (l a / l') + sum_k v_k (w_k / l'), so
+// that they never leave the range of the values.  Bound by instructions: all rows of a prompt of 8192 tokens, 32 heads over 8
+// of 128, 130 ms (the tensor cores 0.3).  Four rows at once took 82, but with 13 KB more code the merge took 1.3 us more where nothing is handed on.
+constexpr int kRowsAtOnce = 2;
+template <int D, typename T, bool KV8>
+__device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParams &a, int r, const int (&row)[kRowsAtOnce], const int (&head)[kRowsAtOnce],
+                                            int hk, uint32_t use) {
   constexpr bool kBf = sizeof(T) == 2;
-  constexpr int CPL = D / 32, kKeys = 8;
-  const int lane = threadIdx.x & 31, hk = head / (p.Hq / p.Hkv);
-  int r = 0;  // its request: the last one whose first row is not behind it
+  constexpr int CPL = D / 32, kKeys = 8, kSums = kRowsAtOnce * kKeys;
+  const int lane = threadIdx.x & 31;
+  const Segment &own = p.segs[r];
+  const int run = p.req_run[r], shared = own.t0 / 16;  // pages that the run's first request names
+  const int32_t *bt = a.block_tables + (int64_t)r * a.max_blocks_per_seq;
+  const int32_t *bt0 = a.block_tables + (int64_t)(run >= 0 ? p.segs[p.B + run].r : r) * a.max_blocks_per_seq;
+  float q[kRowsAtOnce][CPL], o[kRowsAtOnce][CPL], down = 1.0f, up = 1.0f, amax = 0.0f;
+  int64_t at[kRowsAtOnce];
+  int seen[kRowsAtOnce], most = 0;
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const bool has = use >> i & 1;
+    at[i] = has ? ((int64_t)row[i] * p.Hq + head[i]) * D + lane * CPL : 0;
+    seen[i] = has ? own.ctx + (row[i] - own.q0) + 1 : 0;
+    most = max(most, seen[i]);
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) q[i][c] = o[i][c] = 0.0f;
+    if (has) row_values<CPL>(static_cast<const T *>(a.q) + at[i], q[i]);
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) amax = fmaxf(amax, fabsf(q[i][c]));
+  }
+  // codes times their scale may be past fp32 where the scores are not: 2^-16 of the scale goes to the queries, if they have room
+  if (!kBf && KV8 && ptx::warp_max(amax) < 0x1p100f) {
+    down = 0x1p-16f;
+    up = 0x1p16f;
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i)
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) q[i][c] *= up;
+  int mine = 0;  // keys that this lane's row sees
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) mine = lane % kSums / kKeys == i ? seen[i] : mine;
+  const float scale = 1.4426950408889634f / sqrtf((float)D);
+  float m = -INFINITY, l = 0.0f;  // of this lane's row
+  for (int t = 0; t < most; t += kKeys) {
+    const int page = t / 16, bid = __ldg((page < shared ? bt0 : bt) + page);
+    const bool valid = bid >= 0 && bid < a.num_blocks;  // (else its keys and values count as zeros, as in the tensor-core kernels)
+    const int64_t head0 = (int64_t)(valid ? bid : 0) * a.Hkv + hk, src = (head0 * 16 + t % 16) * D + lane * CPL;
+    float s[kSums], v[kKeys][CPL];
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) {  // (a page's slots behind the rows' keys may hold anything, but they are there)
+      float x[CPL];
+      if (KV8) {
+        row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.k_cache) + src + k * D, __ldg(a.k_scale + head0) * down, x);
+        row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.v_cache) + src + k * D, __ldg(a.v_scale + head0), v[k]);
+      } else {
+        row_values<CPL>(static_cast<const T *>(a.k_cache) + src + k * D, x);
+        row_values<CPL>(static_cast<const T *>(a.v_cache) + src + k * D, v[k]);
+      }
+#pragma unroll
+      for (int i = 0; i < kRowsAtOnce; ++i) {
+        float y = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) y = fmaf(q[i][c], x[c], y);
+        s[i * kKeys + k] = y;
+      }
+    }
+    // kSums sums over the lanes: every lane ends with the one of its number (modulo kSums)
+#pragma unroll
+    for (int d = 16; d >= kSums; d >>= 1)
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
+#pragma unroll
+    for (int d = kSums / 2; d > 0; d >>= 1)
+#pragma unroll
+      for (int i = 0; i < d; ++i) {
+        const float keep = lane & d ? s[i + d] : s[i], give = lane & d ? s[i] : s[i + d];
+        s[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+      }
+    const float x = t + (lane & 7) < mine ? (valid ? __fmul_rn(s[0], scale) : 0.0f) : -INFINITY;
+    float mn = x;
+#pragma unroll
+    for (int d = 1; d < kKeys; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+    mn = fmaxf(mn, m);
+    const float ref = mn == -INFINITY ? 0.0f : mn, e = ptx::ex2(__fadd_rn(x, -ref));
+    float sum = e;
+#pragma unroll
+    for (int d = 1; d < kKeys; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const float old = l * (m == mn ? 1.0f : ptx::ex2(m - ref));
+    m = mn;
+    l = old + sum;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l, keep = old * inv, w = e * inv;  // (0: scores of -inf so far)
+#pragma unroll
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      const float f = __shfl_sync(0xffffffffu, keep, i * kKeys);
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) o[i][c] *= f;
+#pragma unroll
+      for (int k = 0; k < kKeys; ++k) {
+        const float g = __shfl_sync(0xffffffffu, w, i * kKeys + k);
+        if (t + k < seen[i] && valid)
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) o[i][c] = fmaf(g, v[k][c], o[i][c]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const float sum = __shfl_sync(0xffffffffu, l, i * kKeys);
+    if (use >> i & 1) st_cols<CPL>(static_cast<T *>(p.out) + at[i], o[i], sum == 0.0f ? __uint_as_float(0x7fffffffu) : 1.0f);
+  }
+}
+
+// The request of a row: the last one whose first row is not behind it.
+__device__ __forceinline__ int request_of(const PromptPlan &p, int row) {
+  int r = 0;
   for (int hi = p.B - 1; r < hi;) {
     const int mid = (r + hi + 1) >> 1;
     if (p.q_row_start[mid] <= row) r = mid;
     else hi = mid - 1;
   }
-  const Segment &own = p.segs[r];
-  const int run = p.req_run[r], shared = own.t0 / 16;  // pages that the run's first request names
-  const int32_t *bt = a.block_tables + (int64_t)r * a.max_blocks_per_seq;
-  const int32_t *bt0 = a.block_tables + (int64_t)(run >= 0 ? p.segs[p.B + run].r : r) * a.max_blocks_per_seq;
-  const int seen = own.ctx + (row - own.q0) + 1;
-  const int64_t at = ((int64_t)row * p.Hq + head) * D + lane * CPL;
-  float q[CPL], o[CPL];
-  row_values<CPL>(static_cast<const T *>(a.q) + at, q);
-  float amax = 0.0f;
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) {
-    amax = fmaxf(amax, fabsf(q[c]));
-    o[c] = 0.0f;
-  }
-  // codes times their scale may be past fp32 where the scores are not: 2^-16 of the scale goes to the queries, if they have room
-  const bool move = !kBf && a.k_scale && ptx::warp_max(amax) < 0x1p100f;
-  const float down = move ? 0x1p-16f : 1.0f;
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) q[c] *= move ? 0x1p16f : 1.0f;
-  const float scale = 1.4426950408889634f / sqrtf((float)D);
-  float m = -INFINITY, l = 0.0f;
-  for (int t = 0; t < seen; t += kKeys) {
-    const int page = t / 16, bid = __ldg((page < shared ? bt0 : bt) + page);
-    const bool valid = bid >= 0 && bid < a.num_blocks;  // (else its keys and values count as zeros, as in the tensor-core kernels)
-    const int64_t head0 = (int64_t)(valid ? bid : 0) * a.Hkv + hk, src = (head0 * 16 + t % 16) * D + lane * CPL;
-    float s[kKeys];
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      float k[CPL];
-      if (a.k_scale) row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.k_cache) + src + i * D, __ldg(a.k_scale + head0) * down, k);
-      else row_values<CPL>(static_cast<const T *>(a.k_cache) + src + i * D, k);
-      s[i] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) s[i] = fmaf(q[c], k[c], s[i]);
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-      for (int i = 0; i < kKeys; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
-    float mn = m;
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      s[i] = t + i < seen ? (valid ? __fmul_rn(s[i], scale) : 0.0f) : -INFINITY;
-      mn = fmaxf(mn, s[i]);
-    }
-    const float ref = mn == -INFINITY ? 0.0f : mn;
-    float ln = l * (m == mn ? 1.0f : ptx::ex2(m - ref));
-    const float old = ln;
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      s[i] = ptx::ex2(__fadd_rn(s[i], -ref));
-      ln += s[i];
-    }
-    m = mn;
-    l = ln;
-    if (ln == 0.0f) continue;  // (scores of -inf so far)
-    const float inv = 1.0f / ln, keep = old * inv;
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) o[c] *= keep;
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      if (t + i >= seen || !valid) continue;
-      float v[CPL];
-      if (a.k_scale) row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.v_cache) + src + i * D, __ldg(a.v_scale + head0), v);
-      else row_values<CPL>(static_cast<const T *>(a.v_cache) + src + i * D, v);
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) o[c] = fmaf(s[i] * inv, v[c], o[c]);
-    }
-  }
-  T *out = static_cast<T *>(p.out) + at;
-  if (only_not_finite) {  // (l is finite, and so are the elements that stay)
-    float had[CPL];
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) had[c] = sizeof(T) == 2 ? __uint_as_float((uint32_t)out[c] << 16) : (float)out[c];
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) o[c] = fabsf(had[c]) < INFINITY ? had[c] : o[c];
-  }
-  st_cols<CPL>(out, o, l == 0.0f ? __uint_as_float(0x7fffffffu) : 1.0f);
+  return r;
 }
 
 }  // namespace wisp

@@ -6,9 +6,8 @@
 //   S = Q K^T         M = 128 rows, N = 128 keys, K = D; fp32 in TMEM, a row per lane
 //   P = 2^(S - m)     by 128 threads, one row each: no exchange between threads; bf16, back to TMEM over S
 //   O += P V          M = 128 rows, N = D, K = 128 keys; A from TMEM, fp32 in TMEM
-// m follows the row's maximum loosely: it moves (and O, l are rescaled) only where a tile's maximum is more than 2^8 above it, so
-// weights stay below 2^8 and rescales are rare after a row's first tiles.  Sums and O keep their relative precision at any
-// exponent; a weight is rounded to bf16 (2^-9) for the second product, the row sum adds it before that.
+// m follows the row's maximum loosely: it moves (and O, l are rescaled) only where a tile's maximum has come 2^7 nearer to it, so rescales are rare after
+// a row's first tiles; see kRoom.  A weight is rounded to bf16 (2^-9) for the second product, the row sum adds it before that.
 //
 // An item of more than one tile of rows runs its tiles as two streams over the same key tiles; one of a single tile runs
 // the even and the odd key tiles as two streams of the same rows, joined at the end.  So there are always two chains
@@ -52,7 +51,11 @@ constexpr int kM = 128;       // rows per stream
 constexpr int threads_of(bool kv8) { return kv8 ? 512 : 384; }
 constexpr uint32_t kTmemCols = 512;  // S of the streams at 0 and 128, O at 256 and 256 + D, P: Cfg::P_COL
 constexpr long long kWaitCycles = 4000000000LL;  // about two seconds: a wait that long is a failure
-constexpr float kLoose = 8.0f;  // how far (log2) a score may exceed its row's reference
+// Sums of weights stay below 1, so that sums of weights times values never leave the values' range: a tile adds 1/2 at most, as its largest score
+// lies kRoom or more below the reference (log2), and with 1/2 in it the reference moves up by kRoom.  A new one lies kAbove above the largest score: 7
+// to 8 more than it has to, as a tile that moves one waits for O (kAbove = 12: 4096 tokens 98 to 107 us).  What is below 2^-126 then counts as zero,
+// 2^-110 of the row's sum.
+constexpr float kRoom = 8.0f, kAbove = 16.0f;
 constexpr int kItemRing = 2;
 
 template <int D>
@@ -309,20 +312,20 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           return true;
         };
         if (t == first) {
-          m = floorf(top);
+          m = floorf(top) + kAbove;
         } else {
           if (C::P_APART && !kBeside && !finish()) { ok = false; break; }
-          const bool move = mine && top > m + kLoose;
+          const bool move = mine && (top > m - kRoom || l > 0.5f);
           if (__any_sync(0xffffffffu, move)) {
             // (P over S: the O before this S is complete)
             if (kBeside) {
               if (!finish()) { ok = false; break; }
               done = true;
             }
-            const float to = move ? floorf(top) : m;
+            const float to = top > m - kRoom ? floorf(top) + kAbove : m + kRoom;
             const float a = move ? ptx::ex2(m - to) : 1.0f;
             if (move && is_far(m)) s_far[threadIdx.x] = 1;
-            m = to;
+            if (move) m = to;
             l *= a;
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           ptx::tc_fence_after();
           const float m1 = s_ml[row], l1 = s_ml[kM + row];
           far = far || is_marked(l1);
-          const float mj = fmaxf(m, m1);
+          const float mj = fmaxf(m, m1) + 1.0f;  // (the two sums together stay below 1, too)
           a0 = m == -INFINITY ? 0.0f : ptx::ex2(m - mj);
           a1 = m1 == -INFINITY ? 0.0f : ptx::ex2(m1 - mj);
           // (a stream that saw nothing has l = 0, or NaN scores only and l = NaN)
@@ -424,7 +427,6 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           dst[x] = (part ? reinterpret_cast<uint8_t *>(part0 + 8 * x * D) : reinterpret_cast<uint8_t *>(out0 + row_at[x])) + (lane & 3) * 16;
-        float2 zero = make_float2(0.0f, 0.0f);  // NaN where a sum is not finite
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t o[32];
@@ -440,9 +442,6 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
               o[i] = __float_as_uint(a1 == 0.0f ? u : fmaf(__uint_as_float(o1[i]), a1, u));
             }
           }
-#pragma unroll
-          for (int i = 0; i < 32; i += 2)
-            zero = __ffma2_rn(make_float2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), make_float2(0.0f, 0.0f), zero);
           auto flush = [&](int at) {  // the staged pieces, to byte `at` of their rows
             __syncwarp();
 #pragma unroll
@@ -493,8 +492,9 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
           float *stat = p.partials + w.poff + (int64_t)w.rows * D + tile * tile_rows + row;
           __stcg(stat, m);
           __stcg(stat + w.rows, far ? marked(l) : l);
-        } else if (mine && (far || (!(zero.x + zero.y == 0.0f) && fabsf(l) < INFINITY))) {
-          hand_on(p, w.q0 + pos, (w.h * g + row % g) | (far ? 0 : kOnlyNotFinite));
+        }
+        if (far && mine) {
+          hand_on(p, w.q0 + pos, w.h * g + row % g);
         }
         ptx::tc_fence_before();
         __syncwarp();
