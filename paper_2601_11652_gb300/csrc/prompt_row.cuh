@@ -62,7 +62,7 @@ __device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParam
   const int run = p.req_run[r], shared = own.t0 / 16;  // pages that the run's first request names
   const int32_t *bt = a.block_tables + (int64_t)r * a.max_blocks_per_seq;
   const int32_t *bt0 = a.block_tables + (int64_t)(run >= 0 ? p.segs[p.B + run].r : r) * a.max_blocks_per_seq;
-  float q[kRowsAtOnce][CPL], o[kRowsAtOnce][CPL], down = 1.0f, up = 1.0f, amax = 0.0f;
+  float q[kRowsAtOnce][CPL], o[kRowsAtOnce][CPL];
   int64_t at[kRowsAtOnce];
   int seen[kRowsAtOnce], most = 0;
 #pragma unroll
@@ -74,18 +74,7 @@ __device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParam
 #pragma unroll
     for (int c = 0; c < CPL; ++c) q[i][c] = o[i][c] = 0.0f;
     if (has) row_values<CPL>(static_cast<const T *>(a.q) + at[i], q[i]);
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) amax = fmaxf(amax, fabsf(q[i][c]));
   }
-  // codes times their scale may be past fp32 where the scores are not: 2^-16 of the scale goes to the queries, if they have room
-  if (!kBf && KV8 && ptx::warp_max(amax) < 0x1p100f) {
-    down = 0x1p-16f;
-    up = 0x1p16f;
-  }
-#pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i)
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) q[i][c] *= up;
   int mine = 0;  // keys that this lane's row sees
 #pragma unroll
   for (int i = 0; i < kRowsAtOnce; ++i) mine = lane % kSums / kKeys == i ? seen[i] : mine;
@@ -95,12 +84,14 @@ __device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParam
     const int page = t / 16, bid = __ldg((page < shared ? bt0 : bt) + page);
     const bool valid = bid >= 0 && bid < a.num_blocks;  // (else its keys and values count as zeros, as in the tensor-core kernels)
     const int64_t head0 = (int64_t)(valid ? bid : 0) * a.Hkv + hk, src = (head0 * 16 + t % 16) * D + lane * CPL;
+    // codes times their scale may be past fp32 where the scores are not
+    const float ks = KV8 ? __ldg(a.k_scale + head0) : 1.0f, down = !kBf && ks > 0x1p60f ? 0x1p-16f : 1.0f;
     float s[kSums], v[kKeys][CPL];
 #pragma unroll
     for (int k = 0; k < kKeys; ++k) {  // (a page's slots behind the rows' keys may hold anything, but they are there)
       float x[CPL];
       if (KV8) {
-        row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.k_cache) + src + k * D, __ldg(a.k_scale + head0) * down, x);
+        row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.k_cache) + src + k * D, ks * down, x);
         row_codes<CPL, kBf>(static_cast<const uint8_t *>(a.v_cache) + src + k * D, __ldg(a.v_scale + head0), v[k]);
       } else {
         row_values<CPL>(static_cast<const T *>(a.k_cache) + src + k * D, x);
@@ -126,7 +117,7 @@ __device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParam
         const float keep = lane & d ? s[i + d] : s[i], give = lane & d ? s[i] : s[i + d];
         s[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
       }
-    const float x = t + (lane & 7) < mine ? (valid ? __fmul_rn(s[0], scale) : 0.0f) : -INFINITY;
+    const float x = t + (lane & 7) < mine ? (valid ? __fmul_rn(s[0], scale / down) : 0.0f) : -INFINITY;
     float mn = x;
 #pragma unroll
     for (int d = 1; d < kKeys; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
@@ -138,7 +129,8 @@ __device__ __forceinline__ void prompt_rows(const PromptPlan &p, const AttnParam
     const float old = l * (m == mn ? 1.0f : ptx::ex2(m - ref));
     m = mn;
     l = old + sum;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l, keep = old * inv, w = e * inv;  // (0: scores of -inf so far)
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (0: scores of -inf so far)
+    const float keep = t < mine ? old * inv : 1.0f, w = t < mine ? e * inv : 0.0f;  // (behind its last key a row stays as it is: what goes with it has no say)
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
       const float f = __shfl_sync(0xffffffffu, keep, i * kKeys);

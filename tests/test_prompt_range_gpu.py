@@ -251,3 +251,26 @@ def test_tables_as_wide_as_their_sequences(dtype, n, ctx, copies):
         c = Case(n + ctx, k=[n - 1] * copies, ctx=[ctx] * copies, Hq=8, Hkv=2, D=64, dtype=dtype, runs=r, spare=0)
         c.run()
         c.check()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_rows_computed_apart_repeat_and_leave_refused_requests(dtype, cache):
+    """Rows with scores far from zero, some of them in a run with a refused request; they repeat to the bit, whatever is computed beside them."""
+    k, ctx, runs = [30, 2, 0, 5, 200], [64, 70, 64, 300, 64], runs_of((1, 4, 3), (-1, 0, 1), (2, 4, 1))
+    c = Case(34, k=k, ctx=ctx, Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache, runs=runs)
+    far_scores(c, 50)
+    c.t["q"][3::7] *= 2.0 ** -50
+    c.run()
+    c.check()
+    first = c.t["out"].clone()
+    for _ in range(5):
+        c.t["out"].fill_(77)
+        c.run()
+        assert torch.equal(c.t["out"], first)
+    c.t["context_lens"][1] = 1 << 20
+    c.t["out"].fill_(77)
+    c.run(expect=1)
+    c.check(skipped=[1])
+    assert (c.t["out"][31:34] == 77).all()
+    same = [r for r in range(238) if not 31 <= r < 34]
+    assert torch.equal(c.t["out"][same], first[same])
