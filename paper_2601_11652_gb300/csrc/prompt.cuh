@@ -80,8 +80,7 @@ __device__ __forceinline__ int slot_floats(int rows, int D) { return (rows * (D 
 // Rows that the attention kernels hand on to prompt_row.cuh, as they cannot hold them.
 //
 // A score becomes a weight in one fused multiply-add, 2^(x scale - m) from the sum x of products.  It is rounded once; but m is a rounded number, so
-// where it is far from zero the largest weight is not 2^0 but up to 2^(half a step of m): references are whole numbers, exact up to 2^24, and a row
-// that has had one beyond kFar is computed once more.
+// where it is far from zero the largest weight is off by up to 2^(half a step of m), and a row that has had one beyond kFar is computed once more.
 //
 // The kernel for fp32 queries hands on rows whose queries are past 2^44, and (rows of a tile that not all see) rows whose largest V is 2^78 times
 // that of the first one that it sees in the tile.

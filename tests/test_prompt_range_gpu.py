@@ -119,14 +119,17 @@ def test_scores_do_not_depend_on_where_their_magnitude_lies(dtype, cache, runs, 
     c = Case(24, k=[140, 9, 30], ctx=[320, 350, 2000], Hq=8, Hkv=2, D=128, dtype=dtype, cache=cache, runs=runs)
     c.run()
     before = c.t["out"].clone()
-    c.t["q"] = (c.t["q"].double() * 2.0 ** -e).to(dtype)
+    q = c.t["q"].double()
+    c.t["q"] = (q * 2.0 ** -e).to(dtype)
+    exact = torch.equal(c.t["q"].double() * 2.0 ** e, q)  # (queries below 2^-14 times 2^-112 are no normal numbers and lose bits)
     if cache:
         c.t["k_scale"] = (c.t["k_scale"].double() * 2.0 ** e).float()
     else:
         c.t["k_cache"] = (c.t["k_cache"].double() * 2.0 ** e).to(dtype)
     c.val["k"] = c.val["k"] * 2.0 ** e
     c.run()
-    if dtype == BF or e > -42:
+    assert exact or e == 112
+    if exact and (dtype == BF or e > -42):
         assert torch.equal(c.t["out"], before)
     c.check()
 
