@@ -15,9 +15,10 @@
 // An item is one tile of 128 rows.  Persistent CTAs, 16 warps: 0-3 softmax and epilogue; 4-7 and 8-11 turn a K and a V tile into halves, in
 // place; 12 and 13 issue S and P V; 14 takes items and loads K and V.  Every wait is bounded.
 // Bound: the softmax warps, one per scheduler: with heads of 64 a tile's way through them (scores, weights, halves, the O before) is 2400 cycles
-// alone and 3100 beside the warps that convert.  4096 tokens, 32 heads over 8 of 128: 609 us, 226 TFLOP/s of the definition's products (three
-// times that on the tensor cores); over e4m3 400 us, 343 TFLOP/s.  2 prompts of 2000 to 3000 tokens, heads of 64: 303 us, 176 TFLOP/s.
-// Q by the warps that convert V, one item ahead, was no faster (609 to 612, over e4m3 400 to 415 us).
+// alone and 3100 beside the warps that convert.  4096 tokens, 32 heads over 8 of 128: 588 us, 234 TFLOP/s of the definition's products (three
+// times that on the tensor cores); over e4m3 409 us, 336 TFLOP/s; heads of 64 371 us, 185 TFLOP/s.
+// Q by the warps that convert V, one item ahead, was no faster (609 to 612, over e4m3 400 to 415 us).  The instruction cache counts: the epilogue's way for V
+// that is not finite as a loop instead of D copies of it took 37 KB of code and (D = 128) 18 us of 610.
 #include "attn_merge.cuh"
 #include "fp8.cuh"
 #include "prompt.cuh"
@@ -36,7 +37,8 @@ constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;  // S at 0 and 64, P at 128 and 192 (h, then l), O at 256 and 384
 constexpr uint32_t kWaitCycles = 3000000000u;  // about one and a half seconds: a wait that long is a failure
 // Sums of weights stay below 1, so that O never leaves the values' range: a tile adds 1/2 at most, as its largest score lies kRoom or more below the
-// reference (log2), and with 1/2 in it the reference moves up by kRoom.  A new one lies kAbove above the largest score.
+// reference (log2), and with 1/2 in it the reference moves up by kRoom.  A new one lies kAbove above the largest score, a whole number, so that it
+// differs from a tile to the next by d (see there) exactly.
 constexpr float kRoom = 7.0f, kAbove = 10.0f;
 constexpr int kUp = 21;       // P is weights times 2^kUp: at most 2^14
 constexpr int kDown = 31;     // of keys' factors (log2)
@@ -301,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float *vf = s_vf + slot * kBT;
         int d = 0;
         // Scores that are not those of the product are put right where they lie, in TMEM: the code of a tile's usual way, and of the other roles beside
-        // it, has to stay in the instruction cache (with this in registers 4096 tokens took 668 us, 610 so; heads of 64 423 and 387).
+        // it, has to stay in the instruction cache (with this in registers 4096 tokens took 668 us, 635 so; heads of 64 423 and 378).
         const uint4 kx = KV8 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4 *>(s_kx + slot * 4);
         if ((kx.x | kx.y | kx.z | kx.w) || base + kBT > all) {
           const uint32_t t_s = tmem + lanes + b * kBT;
@@ -690,14 +692,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int b0 = __shfl_sync(0xffffffffu, bid, 0);
           const bool row4 = __ballot_sync(0xffffffffu, lane < 4 && valid && bid == b0 + lane) == 0xfu;
           if (!valid) bid = p.num_blocks;  // past the item (or invalid): out-of-range box, reads zeros
-          if (lane == 0) {
+          int bids[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) bids[x] = __shfl_sync(0xffffffffu, bid, x);
+          if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(bar(full), kRaw);
-            if (row4) ptx::tma_load_4d(dst, is_k ? &tmk4 : &tmv4, bar(full), 0, 0, w.h, b0);
-          }
-#pragma unroll 1
-          for (int x = 0; x < 4 && !row4; ++x) {
-            const int one = __shfl_sync(0xffffffffu, bid, x);
-            if (lane == 0) ptx::tma_load_4d(dst + x * (kRaw / 4), is_k ? &tmk : &tmv, bar(full), 0, 0, w.h, one);
+            if (row4) {
+              ptx::tma_load_4d(dst, is_k ? &tmk4 : &tmv4, bar(full), 0, 0, w.h, b0);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) ptx::tma_load_4d(dst + x * (kRaw / 4), is_k ? &tmk : &tmv, bar(full), 0, 0, w.h, bids[x]);
+            }
           }
           __syncwarp();
           return true;
@@ -747,7 +752,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t qd = ptx::sdesc_sw128(sbase + C::OFF_Q, 16, 1024);
               const uint64_t kd = ptx::sdesc_sw128(sbase + C::OFF_K + st * C::TILE, 16, 1024);
               // l h, h l, h h
-#pragma unroll 1
+#pragma unroll
               for (int x = 0; x < 3; ++x) {
                 if (KV8 && x == 1) continue;
 #pragma unroll
@@ -768,7 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ptx::elect_one()) {
               ptx::tc_fence_after();
               const uint64_t vd = ptx::sdesc_sw128(sbase + C::OFF_V + st * C::TILE, C::KHALF, 1024);
-#pragma unroll 1
+#pragma unroll
               for (int x = 0; x < 3; ++x) {
                 if (KV8 && x == 1) continue;
 #pragma unroll
