@@ -24,10 +24,10 @@
 //     write it in bf16, times the page's scale, in place: a lane's row of codes in registers first.
 // Every wait is bounded: an expired one records WISP_DEV_TIMEOUT and the CTA drains.
 //
-// Bound, D = 128: the tensor core; a tile of both streams takes 2950 cycles, 2048 of them at its nominal rate (S reads Q and K from shared
-// memory).  16384 tokens, 32 heads over 8: 1.18 ms alone, 1.86 PFLOP/s of the 1.88 that a library product reaches, 1.32 ms in a row under the
-// power limit; 4096 tokens 96 us; over e4m3 125 us.  D = 64: the softmax warps' chain, two warps a scheduler, 2400 cycles a tile; 48 prompts
-// of up to 1500 tokens 247 us, 0.65 PFLOP/s.  Few rows and keys: latency, most of it code that is fetched for the first time (about ten
+// Bound, D = 128: the tensor core; a tile of both streams takes 2530 cycles, 2048 of them at its nominal rate (S reads Q and K from shared
+// memory).  16384 tokens, 32 heads over 8: 1.17 ms alone, the 1.88 PFLOP/s that a library product reaches, 1.32 ms in a row under the
+// power limit; 4096 tokens 96 us; over e4m3 128 us.  D = 64: the softmax warps' chain, two warps a scheduler, 2400 cycles a tile; 48 prompts
+// of up to 1500 tokens 245 us, 0.66 PFLOP/s.  Few rows and keys: latency, most of it code that is fetched for the first time (about ten
 // cycles an instruction), so that less code is faster: 64 tokens, whole call 15 us.
 // Measured and not kept: a part of the exponentials as polynomials (one in eight: 4096 tokens 99 to 109 us, heads of 64 85 to 92); m taken from
 // the tile before (102 to 112); S read a second time instead of held in registers (102 to 121); items of one row tile (2000 tokens 46 to
@@ -144,8 +144,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
   // (Each split stands at the head of its own branch: after a join the compiler counts with the least.)
   constexpr int kSoftRegs = KV8 ? (D == 128 ? 168 : 184) : 200, kCodeRegs = D == 128 ? 96 : 72, kRestRegs = KV8 ? (D == 128 ? 80 : 72) : 104;
   static_assert(2 * kSoftRegs + kRestRegs + (KV8 ? kCodeRegs : 0) == (KV8 ? 4 * 128 : 3 * 168), "registers");
-  // P is handed over in two halves of a tile's keys, so that the product with the first overlaps the softmax of the second: 1.3% with
-  // D = 128 (16384 tokens 1571 -> 1550 us); elsewhere the softmax warps' issue slots bound the tile, and it costs 2 to 3%.
+  // P is handed over in two halves of a tile's keys, so that the product with the first overlaps the softmax of the second: with D = 128 16384 tokens
+  // 1239 -> 1187 us, 4096 101.5 -> 96.5; elsewhere the softmax warps' issue slots bound the tile, and it costs 2 to 3%.
   constexpr int kWhole = D == 128 && !KV8 ? 0 : 1;
   // With P in columns of its own the weights are computed beside the P V before and stored behind it: 48 prompts of up to 1500 tokens 250 ->
   // 247 us (over an 8-bit cache, with fewer registers, 196 -> 200).
@@ -721,8 +721,8 @@ __global__ void __launch_bounds__(threads_of(KV8), 1)
       uint32_t k0 = 0;               // key tiles of the items before
       uint32_t np = 0, ne = 0;       // P tiles and S tiles read so far
       // With P over S the issuers take turns: a stream's P V and next S go out together, and the other stream's behind them.  Without
-      // that the tensor core works on both at once, both S arrive together, and then it waits for both softmaxes (3400 cycles a tile
-      // instead of 2950).  An item's turns are as many for both, empty ones of stream 1 included.
+      // that the tensor core works on both at once, both S arrive together, and then it waits for both softmaxes (a seventh more cycles
+      // a tile).  An item's turns are as many for both, empty ones of stream 1 included.
       uint32_t turn = 0;
       auto my_turn = [&]() -> bool {
         if (C::P_APART) return true;
