@@ -99,7 +99,7 @@ Space space(const wisp_attn_args *a, bool shared, int sms) {
   s.run_info = take(16 * B);
   s.segs = take(sizeof(Segment) * 2 * B);
   s.items = take(sizeof(WorkItem) * (size_t)s.max_rows);
-  s.handed_on = take(sizeof(int2) * (size_t)(s.max_rows * a->Hkv * s.unit_rows));  // (every row of every item)
+  s.handed_on = take(sizeof(int2) * (size_t)(T * a->Hq + s.partial_cap / (a->D + 2)));  // (every row of every item: it writes an output or a partial)
   s.partials = take(4 * (size_t)s.partial_cap);
   s.total = off;
   s.fits = s.max_rows * a->Hkv < INT32_MAX / 2 && s.partial_cap < INT32_MAX;

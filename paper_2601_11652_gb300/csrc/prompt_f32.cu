@@ -18,7 +18,7 @@
 // alone and 3100 beside the warps that convert.  4096 tokens, 32 heads over 8 of 128: 588 us, 234 TFLOP/s of the definition's products (three
 // times that on the tensor cores); over e4m3 409 us, 336 TFLOP/s; heads of 64 371 us, 185 TFLOP/s.
 // Q by the warps that convert V, one item ahead, was no faster (609 to 612, over e4m3 400 to 415 us).  The instruction cache counts: the epilogue's way for V
-// that is not finite as a loop instead of D copies of it took 37 KB of code and (D = 128) 18 us of 610.
+// that is not finite as a loop instead of D copies of it took 42 KB of code and (D = 128) 43 us of 635.
 #include "attn_merge.cuh"
 #include "fp8.cuh"
 #include "prompt.cuh"

@@ -277,3 +277,15 @@ def test_rows_computed_apart_repeat_and_leave_refused_requests(dtype, cache):
     assert (c.t["out"][31:34] == 77).all()
     same = [r for r in range(238) if not 31 <= r < 34]
     assert torch.equal(c.t["out"][same], first[same])
+
+
+def test_workspace_of_many_heads():
+    """What is reserved for rows that are computed apart follows the rows, not the tiles that they are in: 1024 requests of one row, 64 heads."""
+    from paper_2601_11652_gb300 import binding as wb
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    q = torch.empty((1024, 64, 64), dtype=BF, device="cuda")
+    kv = torch.empty((8, 64, 16, 64), dtype=BF, device="cuda")
+    t = dict(draft_lens=i(1024), context_lens=i(1024), block_tables=i(1024, 8), q=q, k_cache=kv, v_cache=kv, out=q)
+    assert wb.wisp_prompt_workspace_size(wb.make_prompt_args(**t)) < 4 << 20
+    rows = 1024 * 64  # a partial for the run's keys and one for the request's own
+    assert wb.wisp_verify_shared_workspace_size(wb.make_shared_args(**t, shared_ids=i(1024), shared_pages=i(1024))) < 2 * rows * 66 * 4 + (12 << 20)
